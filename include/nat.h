@@ -27,7 +27,7 @@
  *   - Device-side conditions that cannot be known at launch (a bounded wait
  *     that ran out, n_sel above the stated capacity, a target outside the
  *     vocabulary) are recorded in the 32-bit status word at the start of the
- *     loss workspace (see NAT_DEV_* bits, nat_poll_status); kernels never trap.
+ *     loss or attention workspace (see NAT_DEV_* bits, nat_poll_status); kernels never trap.
  *   - Alignment: mask, pi, surv and q arrays, the compacted lists and every
  *     matrix must start on a 16-byte boundary (the kernels use 16-byte
  *     accesses); a misaligned pointer is refused with NAT_ERR_INVALID_ARG.
@@ -50,9 +50,10 @@ typedef enum {
   NAT_ERR_CUDA = -4         /* a CUDA runtime/driver call failed; see nat_last_error() */
 } nat_status;
 
-/* Bits of the device status word (first 4 bytes of a loss workspace). */
+/* Bits of the device status word (first 4 bytes of a loss or attention workspace). */
 #define NAT_DEV_TIMEOUT 1u  /* a bounded mbarrier wait gave up; outputs are invalid */
-#define NAT_DEV_CAPACITY 2u /* *n_sel exceeded n_sel_cap; surplus rows were ignored */
+#define NAT_DEV_CAPACITY 2u /* *n_sel exceeded n_sel_cap (attention: cu_seqlens exceeded cap, or is
+                                not ascending); surplus rows were ignored */
 #define NAT_DEV_FALLBACK 4u /* informational: nat_policy_loss_fwd_bwd redid some row chunk with
                                the two-pass kernels (results are valid) */
 #define NAT_DEV_BAD_TARGET 8u /* some selected token's target lies outside [0, V): that token
@@ -346,6 +347,118 @@ int nat_policy_loss_fwd_bwd(const nat_loss_params* params /* host */, const void
                             const int32_t* n_sel, int64_t n_sel_cap, const float* dloss,
                             float* loss, float* logp, float* lse, void* dHidden, float* dW,
                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The transformer body on packed sequences (Section 4, the paragraph on compute savings:
+ * under RPC the model processes the prefixes 1..L_i only).  After nat_gather_rows the
+ * prefixes lie packed, sel_offsets is their cu_seqlens and *n_sel their number of rows; the
+ * operators below take both from the device, with the host's bound `cap` on the rows.  Rows at
+ * or after the last sequence are neither read into a result nor written.  Every sum is taken in
+ * 32 bits and in a fixed order: a call repeated on the same inputs reproduces its outputs bit
+ * for bit.
+ *
+ * Causal attention with grouped heads.  Token i of a sequence attends to tokens j <= i of the
+ * same sequence; query head h reads key head h / (n_heads / n_kv_heads):
+ *   S_ij = scale q_i . k_j,   lse_i = log sum_{j<=i} exp S_ij,   out_i = sum_{j<=i} exp(S_ij - lse_i) v_j
+ * and, for a gradient dout of out, with P = exp(S - lse), delta_i = dout_i . out_i:
+ *   dS_ij = P_ij (dout_i . v_j - delta_i),   dq_i = scale sum_j dS_ij k_j,
+ *   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij dout_i   (summed over the heads of a group).
+ * cu_seqlens int32 [B+1] on the device, ascending; sequences may be empty.  Rows at or after cap
+ * are left out and NAT_DEV_CAPACITY is raised in the status word at the head of the workspace.
+ * q, dq [cap, n_heads, head_dim] with q_stride elements from a token to the next, heads
+ * contiguous; k, dk and v, dv [cap, n_kv_heads, head_dim] with k_stride, v_stride; out, dout with
+ * o_stride (q, k and v may be column blocks of one projection's output).  lse float32
+ * [cap, n_heads].  head_dim a multiple of 8, at most 128; at most 64 query heads share a key head;
+ * strides are multiples of 8 elements, rows 16-byte aligned.  Outputs must not overlap inputs.
+ * dtype NAT_BF16: products on the tensor cores with fp32 accumulation, P and dS rounded to
+ * bfloat16 for the second product; NAT_F32: plain fp32 arithmetic (meant for small problems).
+ * workspace: nat_attn_workspace_bytes(params, B, cap), shared by forward and backward; it holds
+ * nothing that must survive between them.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t dtype;  /* NAT_F32 | NAT_BF16 */
+  float scale;    /* of the scores, usually head_dim^-1/2 */
+  int32_t reserved; /* set to 0 */
+  int64_t q_stride, k_stride, v_stride, o_stride; /* elements from a token's row to the next */
+} nat_attn_params;
+
+size_t nat_attn_workspace_bytes(const nat_attn_params* params /* host */, int32_t B, int64_t cap);
+int nat_attn_fwd(const nat_attn_params* params /* host */, int32_t B, const int32_t* cu_seqlens,
+                 int64_t cap, const void* q, const void* k, const void* v, void* out, float* lse,
+                 void* workspace, size_t workspace_bytes, void* stream);
+int nat_attn_bwd(const nat_attn_params* params /* host */, int32_t B, const int32_t* cu_seqlens,
+                 int64_t cap, const void* q, const void* k, const void* v, const void* out,
+                 const float* lse, const void* dout, void* dq, void* dk, void* dv, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The join of two blocks: post-norm of the block's output y, gate and residual scale, and the next
+ * block's pre-norm.  For each row (all norms are root-mean-square norms over d elements):
+ *   n = y rstd_y w_post,   rstd_y = (mean(y^2) + eps)^-1/2
+ *   r = alpha x + gate n            (the residual stream, in dtype)
+ *   h = r rstd_r w_pre,    rstd_r = (mean(r^2) + eps)^-1/2   (r before its rounding)
+ * x, y, r, h [cap, d] row-major in dtype; w_post, w_pre float32 [d]; rstd_y, rstd_r float32 [cap];
+ * gate float32, [d] with NAT_GATE_CHANNEL, [cap] with NAT_GATE_ROW, NULL with NAT_GATE_NONE
+ * (a factor of one).  Parts may be left out with NULL: w_post (n = y, rstd_y not written),
+ * w_pre (no h, no rstd_r), y (r = alpha x; then w_post and gate are NULL too).
+ * y8, r8 with y8_scales, r8_scales, all or none: 8-bit checkpoints of y and of the stored r, the
+ * same bytes as nat_ckpt8_store writes (y8 only where there is a y).
+ * n_rows: device int32 scalar (NULL: cap); rows at or after it are not touched.
+ * d a multiple of 8, at most 8192; matrices, weights and codes 16-byte aligned.
+ *
+ * Backward, for gradients dr (of r from its other uses; NULL means zero, allowed where w_pre is
+ * given) and dh (of h):
+ *   dr' = dr + rstd_r (u - rhat mean(u rhat)),   u = dh w_pre, rhat = r rstd_r;   dx = alpha dr'
+ *   dn = gate dr',  v = dn w_post,  yhat = y rstd_y,   dy = rstd_y (v - yhat mean(v yhat))
+ *   dw_pre = sum_rows dh rhat,  dw_post = sum_rows dn yhat,
+ *   dgate = sum_rows dr' n  [d]   or   sum_columns dr' n  [cap], by gate_mode.
+ * The weights' gradients are float32 and overwritten.  y and r come as the forward's rows or both as its
+ * checkpoints (then y = r = NULL); rstd_y and rstd_r are the forward's.
+ * workspace (backward only): nat_resnorm_workspace_bytes(params, cap) bytes.
+ * ------------------------------------------------------------------------- */
+#define NAT_GATE_NONE 0
+#define NAT_GATE_CHANNEL 1
+#define NAT_GATE_ROW 2
+
+typedef struct {
+  int32_t d;
+  int32_t dtype;     /* NAT_F32 | NAT_BF16 */
+  int32_t gate_mode; /* NAT_GATE_* */
+  float eps;
+  float alpha;       /* residual scale */
+  int32_t reserved;  /* set to 0 */
+} nat_resnorm_params;
+
+size_t nat_resnorm_workspace_bytes(const nat_resnorm_params* params /* host */, int64_t cap);
+int nat_resnorm_fwd(const nat_resnorm_params* params /* host */, const void* x, const void* y,
+                    const float* w_post, const float* gate, const float* w_pre,
+                    const int32_t* n_rows, int64_t cap, void* r, void* h, float* rstd_y,
+                    float* rstd_r, int8_t* y8, float* y8_scales, int8_t* r8, float* r8_scales,
+                    void* stream);
+int nat_resnorm_bwd(const nat_resnorm_params* params /* host */, const void* y, const void* r,
+                    const int8_t* y8, const float* y8_scales, const int8_t* r8,
+                    const float* r8_scales, const float* w_post, const float* gate,
+                    const float* w_pre, const float* rstd_y, const float* rstd_r,
+                    const int32_t* n_rows, int64_t cap, const void* dr, const void* dh, void* dx,
+                    void* dy, float* dw_post, float* dgate, float* dw_pre, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits.  Each group of 128 consecutive columns of a row (the last one
+ * may be shorter) holds int8 codes and one float32 scale:
+ *   top = max |x|,   code = round(x (127 / top)) to nearest even,   scale = top / 127,
+ * and reads back as code scale, rounded to dtype: off by at most scale / 2 before that rounding.
+ * A group with top < 2^-120 is stored as zeros; a group that holds an infinity or a NaN gets a NaN scale
+ * and reads back as NaN.
+ *   src, dst [cap, d] in dtype, codes int8 [cap, d], scales float32 [cap, ceil(d / 128)];
+ *   d a multiple of 8, at most 2^20; n_rows a device int32 scalar (NULL: cap); rows at or after it
+ *   are not touched.  Rows and codes 16-byte aligned.
+ * ------------------------------------------------------------------------- */
+int nat_ckpt8_store(int32_t dtype, int64_t d, const void* src, const int32_t* n_rows, int64_t cap,
+                    int8_t* codes, float* scales, void* stream);
+int nat_ckpt8_load(int32_t dtype, int64_t d, const int8_t* codes, const float* scales,
+                   const int32_t* n_rows, int64_t cap, void* dst, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Per-kernel timing of the bf16 loss kernels (a measurement aid of this library;

@@ -1,0 +1,188 @@
+// Entry points of the packed causal attention: argument checks, workspace, the plan kernel.
+#include "nat_attn.cuh"
+
+namespace nat {
+namespace attn {
+namespace {
+
+constexpr int kBuckets = 1024;
+
+// Lists the tiles of all sequences, longest work first: under a causal mask the tiles of a
+// sequence cost 1, 2, ... tiles of keys (queries' plans) or as much in the opposite order (keys'
+// plan), and blocks that take the list in turn finish together when the short ones come last.
+// A counting sort by cost; the order inside a bucket is not fixed, which no result depends on.
+// Sequence bounds are clamped to [0, cap], so no list entry points outside the buffers whatever
+// cu_seqlens holds.
+__global__ void __launch_bounds__(1024)
+plan_kernel(const int32_t* __restrict__ cu, int32_t B, int64_t cap, int tile, int by_rest,
+            int64_t max_entries, Entry* __restrict__ list, Head* head, int which, int first) {
+  __shared__ uint32_t bucket[kBuckets];
+  __shared__ int longest;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  bucket[threadIdx.x] = 0u;
+  if (threadIdx.x == 0) longest = 0;
+  __syncthreads();
+  auto bounds = [&](int i, int& lo, int& hi) {
+    lo = (int)min((int64_t)max(cu[i], 0), cap);
+    hi = (int)min((int64_t)max(cu[i + 1], 0), cap);
+    if (hi < lo) hi = lo;
+  };
+  for (int i = threadIdx.x; i < B; i += blockDim.x) {
+    int lo, hi;
+    bounds(i, lo, hi);
+    atomicMax(&longest, (hi - lo + tile - 1) / tile);
+  }
+  __syncthreads();
+  int shift = 0;
+  while ((longest >> shift) >= kBuckets) ++shift;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int i = warp; i < B; i += 32) {
+      int lo, hi;
+      bounds(i, lo, hi);
+      const int tiles = (hi - lo + tile - 1) / tile;
+      for (int t = lane; t < tiles; t += 32) {
+        const int cost = by_rest ? tiles - t : t + 1;
+        const uint32_t at = atomicAdd(&bucket[kBuckets - 1 - (cost >> shift)], 1u);
+        if (pass == 1 && at < max_entries) list[at] = Entry{lo, hi, lo + t * tile, 0};
+      }
+    }
+    __syncthreads();
+    if (pass == 0) {  // exclusive scan of the counts, costliest bucket first
+      const uint32_t mine = bucket[threadIdx.x];
+      uint32_t run = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+        if (lane >= o) run += left;
+      }
+      __shared__ uint32_t warp_sum[32];
+      if (lane == 31) warp_sum[warp] = run;
+      __syncthreads();
+      uint32_t before = 0u;
+      for (int w = 0; w < warp; ++w) before += warp_sum[w];
+      bucket[threadIdx.x] = before + run - mine;
+      if (threadIdx.x == kBuckets - 1) {
+        const uint32_t total = before + run;
+        head->count[which] = (uint32_t)min((int64_t)total, max_entries);
+        // more rows than the buffers hold, or bounds that are not ascending
+        const uint32_t bad = ((int64_t)cu[B] > cap || total > max_entries) ? NAT_DEV_CAPACITY : 0u;
+        if (first) head->status = bad;
+        else if (bad) atomicOr(&head->status, bad);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+int check(const char* who, const nat_attn_params* p, int32_t B, int64_t cap) {
+  if (!p) return fail(NAT_ERR_INVALID_ARG, "%s: params is null", who);
+  if (p->dtype != NAT_F32 && p->dtype != NAT_BF16)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, p->dtype);
+  if (p->n_heads <= 0 || p->n_kv_heads <= 0 || p->head_dim <= 0 || B < 0 || cap < 0 ||
+      cap > 0x7FFFFFFFll)
+    return fail(NAT_ERR_INVALID_ARG, "%s: head counts and head_dim must be positive, B >= 0, cap in [0, 2^31)", who);
+  if (p->n_heads % p->n_kv_heads != 0)
+    return fail(NAT_ERR_INVALID_ARG, "%s: n_heads must be a multiple of n_kv_heads", who);
+  if (p->head_dim % 8 != 0 || p->head_dim > 128)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: head_dim must be a multiple of 8, at most 128 (head_dim = %d)",
+                who, p->head_dim);
+  if (p->n_heads / p->n_kv_heads > 64 || p->n_heads > 65535)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: at most 64 query heads share a key head, and 65535 in all", who);
+  if (!(p->scale - p->scale == 0.f)) return fail(NAT_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  const int64_t strides[4] = {p->q_stride, p->k_stride, p->v_stride, p->o_stride};
+  for (int i = 0; i < 4; ++i) {
+    const int64_t width = (int64_t)(i == 0 || i == 3 ? p->n_heads : p->n_kv_heads) * p->head_dim;
+    if (strides[i] < width)
+      return fail(NAT_ERR_INVALID_ARG, "%s: a token's row (stride %lld) is shorter than its heads (%lld)",
+                  who, (long long)strides[i], (long long)width);
+    if (strides[i] % 8 != 0 || strides[i] >= (1ll << 31))
+      return fail(NAT_ERR_UNSUPPORTED, "%s: strides must be multiples of 8 elements, below 2^31", who);
+  }
+  return NAT_OK;
+}
+
+int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool bwd) {
+  if (!a.cu_seqlens || !a.q || !a.k || !a.v || !a.out || !a.lse)
+    return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (bwd && (!a.dout || !a.dq || !a.dk || !a.dv))
+    return fail(NAT_ERR_INVALID_ARG, "%s: null gradient", who);
+  const uintptr_t all = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.out |
+                        (uintptr_t)a.dout | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv;
+  if (all & 15u) return fail(NAT_ERR_INVALID_ARG, "%s: rows must be 16-byte aligned", who);
+  const size_t need = layout(a.p, a.B, a.cap).total;
+  if (!a.workspace || workspace_bytes < need)
+    return fail(NAT_ERR_CAPACITY, "%s: workspace too small (%zu < %zu)", who, workspace_bytes, need);
+  if ((uintptr_t)a.workspace & 255u)
+    return fail(NAT_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+  return NAT_OK;
+}
+
+}  // namespace
+
+int plan_tile(const nat_attn_params& p, Plan which) {
+  return 32;
+}
+
+Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
+  Layout l;
+  size_t at = 256;
+  for (int w = 0; w < 3; ++w) {
+    // a sequence's last tile may be part full: at most one extra tile for each sequence
+    l.entries[w] = cap / plan_tile(p, (Plan)w) + B;
+    l.plan_off[w] = at;
+    at = align_up(at + (size_t)l.entries[w] * sizeof(Entry), 256);
+  }
+  l.delta_off = at;
+  l.total = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
+  return l;
+}
+
+int launch_plan(const Args& a, const Layout& l, Plan which, bool first) {
+  plan_kernel<<<1, 1024, 0, a.stream>>>(a.cu_seqlens, a.B, a.cap, plan_tile(a.p, which),
+                                        which == kPlanDkv ? 1 : 0, l.entries[which],
+                                        entries(a, l, which), head(a), (int)which, first ? 1 : 0);
+  NAT_LAUNCH_CHECK("plan_kernel");
+  return NAT_OK;
+}
+
+}  // namespace attn
+}  // namespace nat
+
+extern "C" {
+
+size_t nat_attn_workspace_bytes(const nat_attn_params* p, int32_t B, int64_t cap) {
+  if (nat::attn::check("nat_attn_workspace_bytes", p, B, cap) != NAT_OK) return 0;
+  return nat::attn::layout(*p, B, cap).total;
+}
+
+int nat_attn_fwd(const nat_attn_params* p, int32_t B, const int32_t* cu_seqlens, int64_t cap,
+                 const void* q, const void* k, const void* v, void* out, float* lse,
+                 void* workspace, size_t workspace_bytes, void* stream) {
+  int s = nat::attn::check("nat_attn_fwd", p, B, cap);
+  if (s != NAT_OK || B == 0 || cap == 0) return s;
+  nat::attn::Args a{};
+  a.p = *p; a.B = B; a.cu_seqlens = cu_seqlens; a.cap = cap; a.q = q; a.k = k; a.v = v;
+  a.out = out; a.lse = lse; a.workspace = workspace; a.stream = (cudaStream_t)stream;
+  s = nat::attn::check_buffers("nat_attn_fwd", a, workspace_bytes, false);
+  if (s != NAT_OK) return s;
+  const nat::attn::Layout l = nat::attn::layout(*p, B, cap);
+  return p->dtype == NAT_F32 ? nat::attn::f32_fwd(a, l) : nat::attn::bf16_fwd(a, l);
+}
+
+int nat_attn_bwd(const nat_attn_params* p, int32_t B, const int32_t* cu_seqlens, int64_t cap,
+                 const void* q, const void* k, const void* v, const void* out, const float* lse,
+                 const void* dout, void* dq, void* dk, void* dv, void* workspace,
+                 size_t workspace_bytes, void* stream) {
+  int s = nat::attn::check("nat_attn_bwd", p, B, cap);
+  if (s != NAT_OK || B == 0 || cap == 0) return s;
+  nat::attn::Args a{};
+  a.p = *p; a.B = B; a.cu_seqlens = cu_seqlens; a.cap = cap; a.q = q; a.k = k; a.v = v;
+  a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse); a.dout = dout; a.dq = dq;
+  a.dk = dk; a.dv = dv; a.workspace = workspace; a.stream = (cudaStream_t)stream;
+  s = nat::attn::check_buffers("nat_attn_bwd", a, workspace_bytes, true);
+  if (s != NAT_OK) return s;
+  const nat::attn::Layout l = nat::attn::layout(*p, B, cap);
+  return p->dtype == NAT_F32 ? nat::attn::f32_bwd(a, l) : nat::attn::bf16_bwd(a, l);
+}
+
+}  // extern "C"

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libnat_b200.so")
 
 NAT_SEL_URS, NAT_SEL_RPC, NAT_SEL_DET = 0, 1, 2
 NAT_F32, NAT_BF16 = 0, 1
+NAT_GATE_NONE, NAT_GATE_CHANNEL, NAT_GATE_ROW = 0, 1, 2
 NAT_DEV_TIMEOUT, NAT_DEV_CAPACITY, NAT_DEV_FALLBACK, NAT_DEV_BAD_TARGET = 1, 2, 4, 8
 
 SYMBOLS = (
@@ -24,7 +25,9 @@ SYMBOLS = (
     "nat_compact_static_max_tokens", "nat_policy_loss_fwd_bwd", "nat_trace_begin",
     "nat_trace_end", "nat_select_survival", "nat_gather_rows", "nat_scatter_rows",
     "nat_poll_status", "nat_compact_prefix", "nat_select_cutlaw",
-    "nat_select_cutlaw_workspace_bytes",
+    "nat_select_cutlaw_workspace_bytes", "nat_attn_workspace_bytes", "nat_attn_fwd",
+    "nat_attn_bwd", "nat_resnorm_workspace_bytes", "nat_resnorm_fwd", "nat_resnorm_bwd",
+    "nat_ckpt8_store", "nat_ckpt8_load",
 )
 TRACE_KINDS = ("fwd", "dz", "dh", "dw", "e")
 
@@ -45,6 +48,19 @@ class LossParams(ctypes.Structure):
                 ("hidden_is_compact", ctypes.c_int32), ("accumulate_dW", ctypes.c_int32),
                 ("kl_beta", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("ref_logp", ctypes.c_void_p)]
+
+
+class AttnParams(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("o_stride", ctypes.c_int64)]
+
+
+class ResnormParams(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("gate_mode", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("alpha", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -99,6 +115,22 @@ def load():
     lib.nat_trace_begin.restype = ctypes.c_int
     lib.nat_trace_end.restype = ctypes.c_int
     lib.nat_trace_end.argtypes = [vp, vp]
+    lib.nat_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.nat_attn_workspace_bytes.argtypes = [ctypes.POINTER(AttnParams), i32, i64]
+    lib.nat_attn_fwd.argtypes = [ctypes.POINTER(AttnParams), i32, vp, i64] + [vp] * 6 + \
+        [ctypes.c_size_t, vp]
+    lib.nat_attn_bwd.argtypes = [ctypes.POINTER(AttnParams), i32, vp, i64] + [vp] * 10 + \
+        [ctypes.c_size_t, vp]
+    lib.nat_resnorm_workspace_bytes.restype = ctypes.c_size_t
+    lib.nat_resnorm_workspace_bytes.argtypes = [ctypes.POINTER(ResnormParams), i64]
+    lib.nat_resnorm_fwd.argtypes = [ctypes.POINTER(ResnormParams)] + [vp] * 6 + [i64] + [vp] * 9
+    lib.nat_resnorm_bwd.argtypes = [ctypes.POINTER(ResnormParams)] + [vp] * 12 + [i64] + \
+        [vp] * 8 + [ctypes.c_size_t, vp]
+    lib.nat_ckpt8_store.argtypes = [i32, i64, vp, vp, i64, vp, vp, vp]
+    lib.nat_ckpt8_load.argtypes = [i32, i64, vp, vp, vp, i64, vp, vp]
+    for name in ("nat_attn_fwd", "nat_attn_bwd", "nat_resnorm_fwd", "nat_resnorm_bwd",
+                 "nat_ckpt8_store", "nat_ckpt8_load"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("nat_grpo_adv", "nat_select", "nat_compact", "nat_policy_loss_fwd",
                  "nat_policy_loss_bwd", "nat_policy_loss_fwd_bwd"):
         getattr(lib, name).restype = ctypes.c_int
@@ -238,6 +270,162 @@ def nat_policy_loss_fwd_bwd(params, hidden, W, targets, old_logp, adv, pi, cu_se
         _ptr(pi), _ptr(cu_seqlens), _ptr(sel_idx), _ptr(sel_resp), _ptr(n_sel), n_sel_cap,
         _ptr(dloss), _ptr(loss), _ptr(logp), _ptr(lse), _ptr(dHidden), _ptr(dW), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream()))
+
+
+# -- the transformer body on packed sequences ------------------------------------------
+_DTYPES = {torch.float32: NAT_F32, torch.bfloat16: NAT_BF16}
+GROUP8 = 128                 # columns that share a scale in an 8-bit checkpoint
+
+
+def _rows(what, t, dtype, shape, strided=False):
+    """Pointer of a device tensor of at least `shape` (leading size: at least), checked:
+    type, device, extent, and contiguity (a token stride of its own where `strided`)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise NatError(f"{what}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise NatError(f"{what}: on {t.device}, not on the current CUDA device")
+    if t.dim() != len(shape) or t.shape[0] < shape[0] or tuple(t.shape[1:]) != tuple(shape[1:]):
+        raise NatError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    inner = t[0] if strided and t.shape[0] else t
+    if t.numel() and not inner.is_contiguous():
+        raise NatError(f"{what}: not contiguous")
+    return t.data_ptr()
+
+
+def _workspace(t):
+    if t.device.index != torch.cuda.current_device() or not t.is_contiguous():
+        raise NatError("workspace: must be contiguous, on the current CUDA device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def attn_params(n_heads, n_kv_heads, head_dim, dtype, scale=None):
+    """Head layout of the packed causal attention; ``scale`` defaults to head_dim^-1/2.  The
+    strides are those of contiguous tensors; nat_attn_fwd / nat_attn_bwd set them from theirs."""
+    q, kv = n_heads * head_dim, n_kv_heads * head_dim
+    return AttnParams(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                      dtype=_DTYPES.get(dtype, dtype),
+                      scale=head_dim ** -0.5 if scale is None else scale, reserved=0, q_stride=q,
+                      k_stride=kv, v_stride=kv, o_stride=q)
+
+
+def nat_attn_workspace_bytes(params, B, cap):
+    return load().nat_attn_workspace_bytes(ctypes.byref(params), B, cap)
+
+
+def _attn_call(params, B, cu_seqlens, cap, tensors, lse):
+    """(pointers, params with the tensors' strides) of a call; `tensors` maps names to
+    (tensor, stride field, head count)."""
+    dtype = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
+    p = AttnParams()
+    ctypes.memmove(ctypes.byref(p), ctypes.byref(params), ctypes.sizeof(p))
+    strides, ptrs = {}, {}
+    for name, (t, field, heads) in tensors.items():
+        ptrs[name] = _rows(name, t, dtype, (cap, heads, params.head_dim), strided=True)
+        if t.shape[0] > 1 and strides.setdefault(field, t.stride(0)) != t.stride(0):
+            raise NatError(f"{name}: token stride {t.stride(0)}, its counterpart has {strides[field]}")
+    for field, stride in strides.items():
+        setattr(p, field, stride)
+    ptrs["cu_seqlens"] = _rows("cu_seqlens", cu_seqlens, torch.int32, (B + 1,))
+    ptrs["lse"] = _rows("lse", lse, torch.float32, (cap, params.n_heads))
+    return ptrs, p
+
+
+def nat_attn_fwd(params, B, cu_seqlens, cap, q, k, v, out, lse, workspace):
+    h, kv = params.n_heads, params.n_kv_heads
+    t, p = _attn_call(params, B, cu_seqlens, cap, {
+        "q": (q, "q_stride", h), "k": (k, "k_stride", kv), "v": (v, "v_stride", kv),
+        "out": (out, "o_stride", h)}, lse)
+    ws, nbytes = _workspace(workspace)
+    _check(load().nat_attn_fwd(ctypes.byref(p), B, t["cu_seqlens"], cap, t["q"], t["k"], t["v"],
+                               t["out"], t["lse"], ws, nbytes, _stream()))
+
+
+def nat_attn_bwd(params, B, cu_seqlens, cap, q, k, v, out, lse, dout, dq, dk, dv, workspace):
+    """dq, dk, dv have the token strides of q, k, v, and dout that of out."""
+    h, kv = params.n_heads, params.n_kv_heads
+    t, p = _attn_call(params, B, cu_seqlens, cap, {
+        "q": (q, "q_stride", h), "k": (k, "k_stride", kv), "v": (v, "v_stride", kv),
+        "out": (out, "o_stride", h), "dout": (dout, "o_stride", h), "dq": (dq, "q_stride", h),
+        "dk": (dk, "k_stride", kv), "dv": (dv, "v_stride", kv)}, lse)
+    ws, nbytes = _workspace(workspace)
+    _check(load().nat_attn_bwd(ctypes.byref(p), B, t["cu_seqlens"], cap, t["q"], t["k"], t["v"],
+                               t["out"], t["lse"], t["dout"], t["dq"], t["dk"], t["dv"], ws,
+                               nbytes, _stream()))
+
+
+def resnorm_params(d, dtype, eps=1e-6, alpha=1.0, gate="none"):
+    """``gate``: "none", "channel" (a factor for each column) or "row" (one for each row)."""
+    gate = {"none": NAT_GATE_NONE, "channel": NAT_GATE_CHANNEL, "row": NAT_GATE_ROW}.get(gate, gate)
+    return ResnormParams(d=d, dtype=_DTYPES.get(dtype, dtype), gate_mode=gate, eps=eps, alpha=alpha,
+                         reserved=0)
+
+
+def nat_resnorm_workspace_bytes(params, cap):
+    return load().nat_resnorm_workspace_bytes(ctypes.byref(params), cap)
+
+
+def _pair8(what, pair, cap, d):
+    if pair is None:
+        return None, None
+    return (_rows(what, pair[0], torch.int8, (cap, d)),
+            _rows(what + " scales", pair[1], torch.float32, (cap, (d + GROUP8 - 1) // GROUP8)))
+
+
+def _resnorm_call(params, cap, n_rows, rows, gate, vectors, per_row):
+    d = params.d
+    dtype = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
+    t = {k: _rows(k, v, dtype, (cap, d)) for k, v in rows.items()}
+    t.update({k: _rows(k, v, torch.float32, (d,)) for k, v in vectors.items()})
+    t.update({k: _rows(k, v, torch.float32, (cap,)) for k, v in per_row.items()})
+    of = (cap,) if params.gate_mode == NAT_GATE_ROW else (d,)
+    t.update({k: _rows(k, v, torch.float32, of) for k, v in gate.items()})
+    t["n_rows"] = _rows("n_rows", n_rows, torch.int32, (1,))
+    return t
+
+
+def nat_resnorm_fwd(params, x, y, w_post, gate, w_pre, n_rows, cap, r, h, rstd_y, rstd_r, y8=None,
+                    r8=None):
+    """y8, r8: None, or (codes, scales) of the 8-bit checkpoints to leave."""
+    t = _resnorm_call(params, cap, n_rows, dict(x=x, y=y, r=r, h=h), dict(gate=gate),
+                      dict(w_post=w_post, w_pre=w_pre), dict(rstd_y=rstd_y, rstd_r=rstd_r))
+    _check(load().nat_resnorm_fwd(
+        ctypes.byref(params), t["x"], t["y"], t["w_post"], t["gate"], t["w_pre"], t["n_rows"], cap,
+        t["r"], t["h"], t["rstd_y"], t["rstd_r"], *_pair8("y8", y8, cap, params.d),
+        *_pair8("r8", r8, cap, params.d), _stream()))
+
+
+def nat_resnorm_bwd(params, y, r, w_post, gate, w_pre, rstd_y, rstd_r, n_rows, cap, dr, dh, dx, dy,
+                    dw_post, dgate, dw_pre, workspace, y8=None, r8=None):
+    """y and r as rows, or None with y8 and r8 = (codes, scales)."""
+    t = _resnorm_call(params, cap, n_rows, dict(y=y, r=r, dr=dr, dh=dh, dx=dx, dy=dy),
+                      dict(gate=gate, dgate=dgate),
+                      dict(w_post=w_post, w_pre=w_pre, dw_post=dw_post, dw_pre=dw_pre),
+                      dict(rstd_y=rstd_y, rstd_r=rstd_r))
+    ws, nbytes = _workspace(workspace)
+    _check(load().nat_resnorm_bwd(
+        ctypes.byref(params), t["y"], t["r"], *_pair8("y8", y8, cap, params.d),
+        *_pair8("r8", r8, cap, params.d), t["w_post"], t["gate"], t["w_pre"], t["rstd_y"],
+        t["rstd_r"], t["n_rows"], cap, t["dr"], t["dh"], t["dx"], t["dy"], t["dw_post"],
+        t["dgate"], t["dw_pre"], ws, nbytes, _stream()))
+
+
+def nat_ckpt8_store(src, n_rows, cap, codes, scales):
+    """8-bit checkpoint of rows [0, n_rows) (a device scalar; None: cap) of src [cap, d]."""
+    d = src.shape[-1]
+    c, sc = _pair8("codes", (codes, scales), cap, d)
+    _check(load().nat_ckpt8_store(_DTYPES.get(src.dtype, -1), d,
+                                  _rows("src", src, src.dtype, (cap, d)),
+                                  _rows("n_rows", n_rows, torch.int32, (1,)), cap, c, sc, _stream()))
+
+
+def nat_ckpt8_load(codes, scales, n_rows, cap, dst):
+    d = dst.shape[-1]
+    c, sc = _pair8("codes", (codes, scales), cap, d)
+    _check(load().nat_ckpt8_load(_DTYPES.get(dst.dtype, -1), d, c, sc,
+                                 _rows("n_rows", n_rows, torch.int32, (1,)), cap,
+                                 _rows("dst", dst, dst.dtype, (cap, d)), _stream()))
 
 
 def nat_trace_begin():
