@@ -120,6 +120,7 @@ int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool b
 }  // namespace
 
 int plan_tile(const nat_attn_params& p, Plan which) {
+  if (p.dtype == NAT_BF16 && which == kPlanFwd) return 2 * (128 / (p.n_heads / p.n_kv_heads));
   return 32;
 }
 

@@ -1,0 +1,460 @@
+// Packed causal attention on the tensor cores (tcgen05 + TMEM + TMA), bfloat16.
+//
+// The query heads of a group are folded into the rows of a tile: a tile holds TQ = 128 / g tokens
+// times the g heads that share a key head, row r = token (r / g), head (r % g), which one 3-D TMA
+// box loads.  Grouped heads then share every key tile, and the diagonal of the causal mask
+// wastes TQ tokens instead of 128.
+//
+// Forward, one persistent block per multiprocessor, twelve warps:
+//   warps 0-3, 4-7  softmax of row tile 0 and 1: one thread a row, all 128 scores in registers
+//   warp 8          issues the MMAs: S = Q K^T (both in shared memory), O += P V (P in tensor memory)
+//   warp 9          TMA loads of Q, K, V through a ring (warps 10, 11 only lend their registers)
+// Two row tiles alternate, so the tensor cores work on one while the other is in its softmax; they
+// share K and V, which halves the operand feed.  Tensor memory: S0 S1 O0 O1, 128 columns each; P
+// (bf16 pairs) overwrites the first half of its S.  O is rescaled only when a row's maximum has
+// grown by more than 2^8 since the last time: P stays below 2^8 and the sums in fp32 lose nothing.
+#include <cuda.h>
+
+#include "nat_attn.cuh"
+#include "nat_attn_tc.cuh"
+
+namespace nat {
+namespace attn {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRescale = 8.f;  // growth of a row's maximum (log2) that is left in P
+
+struct FwdParams {
+  const Entry* list;
+  const uint32_t* count;
+  uint32_t* status;
+  __nv_bfloat16* out;
+  float* lse;
+  int64_t o_stride;
+  int n_heads, n_kv_heads, group, tq, head_dim;
+  float scale;
+};
+
+template <int DP>
+struct FwdShape {
+  static constexpr int kNP = DP / 64;                       // 64-column panels of a tile
+  static constexpr uint32_t kTile = kNP * kPanel;
+  static constexpr int kStages = DP == 128 ? 4 : 8;
+  static constexpr uint32_t kSmem = 1024 + (2 + kStages) * kTile + 512;
+};
+
+// What all roles derive from a list entry.
+struct Unit {
+  int seq_lo, seq_hi, lo, head, nk[2], kv_hi;
+};
+__device__ __forceinline__ Unit unit_of(const FwdParams& p, uint32_t u) {
+  const Entry e = p.list[u / p.n_kv_heads];
+  Unit w;
+  w.seq_lo = e.seq_lo;
+  w.seq_hi = e.seq_hi;
+  w.lo = e.lo;
+  w.head = (int)(u % p.n_kv_heads);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int first = e.lo + t * p.tq, end = min(first + p.tq, e.seq_hi);
+    w.nk[t] = first < e.seq_hi ? (end - e.seq_lo + kRows - 1) / kRows : 0;
+  }
+  w.kv_hi = min(e.lo + 2 * p.tq, e.seq_hi);
+  return w;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(384, 1)
+attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                const __grid_constant__ CUtensorMap map_v, const FwdParams p) {
+  using R = FwdShape<DP>;
+  constexpr int kNS = R::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* ring = smem + 2 * R::kTile;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(ring + kNS * R::kTile);
+  uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *p_full = bars + 6, *o_done = bars + 8;
+  uint64_t *raw = bars + 10, *drain = bars + 11, *full = bars + 12, *empty = bars + 12 + kNS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 2 * kNS);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
+
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      tc::mbar_init(&q_full[t], 1);
+      tc::mbar_init(&q_empty[t], 1);
+      tc::mbar_init(&s_full[t], 1);
+      tc::mbar_init(&p_full[t], 128);
+      tc::mbar_init(&o_done[t], 1);
+    }
+    tc::mbar_init(raw, 1);
+    tc::mbar_init(drain, 1);
+    for (int s = 0; s < kNS; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    *abort_flag = 0u;
+    tc::fence_barrier_init();
+  }
+  if (warp == 8) {
+    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  // 168 registers a thread at launch: the softmax warpgroups, which hold a row of scores, take
+  // some of the third's (2 x 192 + 120 = 3 x 168)
+  if (warp >= 8) {
+  regs_dec<120>();
+  if (warp == 9) {
+    // ---------------------------------------------------------------- loads
+    uint32_t item = 0, raw_turns = 0, q_turns[2] = {0, 0};
+    bool ok = true;
+    const uint32_t q_bytes = (uint32_t)(p.group * p.tq) * 128u * R::kNP;
+    auto load_q = [&](const Unit& w, int t) {
+      if (w.nk[t] == 0) return;
+      ok = ok && warp_wait(&q_empty[t], (q_turns[t] & 1) ^ 1, abort_flag);
+      if (!ok) return;
+      ++q_turns[t];
+      if (lane == 0) {
+        tc::mbar_arrive_expect_tx(&q_full[t], q_bytes);
+        for (int c = 0; c < R::kNP; ++c)
+          tma_load_3d(tc::smem_u32(smem + t * R::kTile + c * kPanel), &map_q, &q_full[t], c * 64,
+                      w.head * p.group, w.lo + t * p.tq);
+      }
+    };
+    auto load_kv = [&](const CUtensorMap* map, const Unit& w, int j, bool is_v) {
+      const int s = item % kNS;
+      ok = ok && warp_wait(&empty[s], ((item / kNS) & 1) ^ 1, abort_flag);
+      if (!ok) return;
+      ++item;
+      const int row = w.seq_lo + j * kRows, valid = w.kv_hi - row;
+      const bool fix = is_v && valid < kRows;
+      uint64_t* bar = fix ? raw : &full[s];
+      uint8_t* dst = ring + s * R::kTile;
+      if (lane == 0) {
+        tc::mbar_arrive_expect_tx(bar, R::kTile);
+        for (int c = 0; c < R::kNP; ++c)
+          tma_load_3d(tc::smem_u32(dst + c * kPanel), map, bar, c * 64, w.head, row);
+      }
+      if (fix) {
+        ok = warp_wait(raw, raw_turns & 1, abort_flag);
+        ++raw_turns;
+        if (!ok) return;
+        zero_rows<R::kNP>(dst, valid, lane);
+        if (lane == 0) tc::mbar_arrive(&full[s]);
+      }
+    };
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit w = unit_of(p, u);
+      const int n = max(w.nk[0], w.nk[1]);
+      for (int j = 0; ok && j < n; ++j) {
+        if (j == 0) load_q(w, 0);
+        load_kv(&map_k, w, j, false);
+        if (j == 0) load_q(w, 1);
+        load_kv(&map_v, w, j, true);
+      }
+    }
+    // the block must not leave with a copy in flight: every tile that was loaded has to have landed
+    if (!ok) {
+      uint32_t never = 0u;
+      if (raw_turns) tc::mbar_wait(raw, (raw_turns - 1) & 1, &never, 1000000000ull), never = 0u;
+      for (uint32_t i = item > (uint32_t)kNS ? item - kNS : 0; i < item; ++i)
+        tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, &never, 1000000000ull), never = 0u;
+      for (int t = 0; t < 2; ++t)
+        if (q_turns[t]) tc::mbar_wait(&q_full[t], (q_turns[t] - 1) & 1, &never, 1000000000ull), never = 0u;
+    }
+  } else if (warp == 8) {
+    // ---------------------------------------------------------------- MMAs
+    if (lane == 0) {
+      constexpr uint32_t kIdescS = tc::instr_desc_bf16(128, 128, 0, 0);
+      constexpr uint32_t kIdescO = tc::instr_desc_bf16(128, DP, 0, 1);
+      const int ksteps = (p.head_dim + 15) / 16;
+      const uint32_t q_addr = tc::smem_u32(smem), ring_addr = tc::smem_u32(ring);
+      uint32_t item = 0, q_turns[2] = {0, 0}, p_turns[2] = {0, 0};
+      bool ok = true;
+      auto take = [&](uint32_t i) {
+        ok = ok && tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, abort_flag);
+        tc::fence_after_sync();
+      };
+      auto scores = [&](int t, uint32_t k_item) {
+        const uint32_t a = q_addr + t * R::kTile, b = ring_addr + (k_item % kNS) * R::kTile;
+#pragma unroll 1
+        for (int kk = 0; kk < ksteps; ++kk)
+          tc::umma_bf16(tmem + t * 128, desc_kmajor(a, kk), desc_kmajor(b, kk), kIdescS, kk > 0);
+        tc::umma_commit(&s_full[t]);
+      };
+      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Unit w = unit_of(p, u);
+        const int n = max(w.nk[0], w.nk[1]);
+        // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
+        take(item);
+        for (int t = 0; ok && t < 2; ++t)
+          if (w.nk[t]) {
+            ok = tc::mbar_wait(&q_full[t], q_turns[t] & 1, abort_flag);
+            ++q_turns[t];
+            tc::fence_after_sync();
+            if (!ok) break;
+            scores(t, item);
+            if (w.nk[t] == 1) tc::umma_commit(&q_empty[t]);
+          }
+        if (!ok) break;
+        tc::umma_commit(&empty[item % kNS]);
+        for (int j = 0; ok && j < n; ++j) {
+          const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
+          bool have_v = false, have_k = false;
+#pragma unroll 1
+          for (int t = 0; ok && t < 2; ++t) {
+            if (j >= w.nk[t]) continue;
+            if (!have_v) take(v_item), have_v = true;
+            ok = ok && tc::mbar_wait(&p_full[t], p_turns[t] & 1, abort_flag);
+            ++p_turns[t];
+            if (!ok) break;
+            tc::fence_after_sync();
+            const uint32_t b = ring_addr + (v_item % kNS) * R::kTile;
+#pragma unroll 1
+            for (int kk = 0; kk < 8; ++kk)
+              umma_ts_bf16(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, desc_mnmajor(b, kk), kIdescO,
+                           j > 0 || kk > 0);
+            tc::umma_commit(&o_done[t]);
+            if (j + 1 < w.nk[t]) {
+              if (!have_k) take(k_next), have_k = true;
+              if (!ok) break;
+              scores(t, k_next);
+              if (j + 2 == w.nk[t]) tc::umma_commit(&q_empty[t]);
+            }
+          }
+          if (!ok) break;
+          tc::umma_commit(&empty[v_item % kNS]);
+          if (have_k) tc::umma_commit(&empty[k_next % kNS]);
+        }
+        item += 2 * n;
+      }
+      // every MMA has to have finished before the tensor memory is given back
+      tc::umma_commit(drain);
+      uint32_t never = 0u;
+      tc::mbar_wait(drain, 0, &never);
+    }
+  }
+  } else {
+    // ------------------------------------------------------------- softmax
+    regs_inc<192>();
+    const int t = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16;
+    const uint32_t s_addr = tmem + t * 128 + lane_base, o_addr = tmem + 256 + t * 128 + lane_base;
+    const int token_in = row / p.group, head_in = row % p.group;
+    // the maximum is taken before the scale, which therefore has to be positive: a negative one
+    // gives its sign, and zero itself, to the scores
+    const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f;
+    const float sc = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
+    uint32_t s_turns = 0, pv = 0;
+    bool ok = true;
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit w = unit_of(p, u);
+      const int nk = w.nk[t], first = w.lo + t * p.tq, token = first + token_in;
+      const bool valid = row < p.group * p.tq && token < w.seq_hi;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < nk; ++j) {
+        ok = warp_wait(&s_full[t], s_turns & 1, abort_flag);
+        ++s_turns;
+        if (!ok) break;
+        tc::fence_after_sync();
+        uint32_t sr[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tc::tmem_ld32_issue(s_addr + c * 32, sr + c * 32);
+        tc::tmem_ld_wait(sr);
+#pragma unroll
+        for (int c = 1; c < 4; ++c) tc::tmem_ld_pin(sr + c * 32);
+        float s[128];
+#pragma unroll
+        for (int c = 0; c < 128; ++c) s[c] = __uint_as_float(sr[c]);
+        if (sign != 1.f) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c) s[c] *= sign;
+        }
+        const int kv0 = w.seq_lo + j * kRows;
+        if (kv0 + kRows - 1 > first) {  // the tile touches the diagonal
+          const int last = token - kv0;
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c > last) s[c] = -INFINITY;
+        }
+        float top[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], s[c]);
+        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float base = m;
+        if (j == 0) {
+          m = base = now;
+        } else {
+          const bool grow = valid && (now - m) * sc > kRescale;
+          if (__any_sync(0xFFFFFFFFu, grow)) {
+            ok = warp_wait(&o_done[t], (pv + j - 1) & 1, abort_flag);
+            if (!ok) break;
+            tc::fence_after_sync();
+            const float f = grow ? ex2((m - now) * sc) : 1.f;
+            if (grow) m = now;
+            l *= f;
+#pragma unroll
+            for (int c = 0; c < DP / 8; ++c) {  // few columns at a time: the scores stay in registers
+              uint32_t o[8];
+              tmem_ld8(o_addr + c * 8, o);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st8(o_addr + c * 8, o);
+            }
+            base = m;
+          }
+        }
+        // a row whose scores are all minus infinity so far has no maximum to subtract
+        const float shift = base == -INFINITY ? 0.f : base * sc;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            const float a = ex2(fmaf(s[half * 64 + 2 * c], sc, -shift));
+            const float b = ex2(fmaf(s[half * 64 + 2 * c + 1], sc, -shift));
+            sum[(2 * c) & 3] += a;
+            sum[(2 * c + 1) & 3] += b;
+            pk[c] = bf16_pair(a, b);
+          }
+          tmem_st32(s_addr + half * 32, pk);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_st_wait();
+        tc::fence_before_sync();
+        tc::mbar_arrive(&p_full[t]);
+      }
+      if (!ok) break;
+      if (nk == 0) continue;
+      ok = warp_wait(&o_done[t], (pv + nk - 1) & 1, abort_flag);
+      if (!ok) break;
+      pv += nk;
+      tc::fence_after_sync();
+      const int head = w.head * p.group + head_in;
+      const float inv = 1.f / l;
+      __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * p.head_dim;
+#pragma unroll
+      for (int c = 0; c < DP / 32; ++c) {
+        float o[32];
+        tc::tmem_ld32(o_addr + c * 32, o);
+        if (valid) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float* x = o + 8 * i;
+            if (c * 32 + 8 * i < p.head_dim)
+              *reinterpret_cast<uint4*>(dst + c * 32 + 8 * i) =
+                  make_uint4(bf16_pair(x[0] * inv, x[1] * inv), bf16_pair(x[2] * inv, x[3] * inv),
+                             bf16_pair(x[4] * inv, x[5] * inv), bf16_pair(x[6] * inv, x[7] * inv));
+          }
+        }
+      }
+      if (valid)
+        p.lse[(int64_t)token * p.n_heads + head] = fmaf(m, sc * kLn2, logf(l));
+      tc::fence_before_sync();
+    }
+  }
+
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
+  if (warp == 8) tc::tmem_dealloc(tmem, 512);
+}
+
+// ------------------------------------------------------------------------- host side
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int get_encoder(EncodeTiledFn* out) {
+  static EncodeTiledFn cached = nullptr;
+  if (!cached) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    NAT_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
+    if (qres != cudaDriverEntryPointSuccess || !fn)
+      return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    cached = reinterpret_cast<EncodeTiledFn>(fn);
+  }
+  *out = cached;
+  return NAT_OK;
+}
+
+// [cap, heads, D] with a token stride; a box of 64 columns x box_heads x box_tokens, zero outside.
+int make_map(CUtensorMap* map, const void* base, int D, int heads, int64_t cap, int64_t stride,
+             int box_heads, int box_tokens) {
+  EncodeTiledFn enc;
+  int s = get_encoder(&enc);
+  if (s != NAT_OK) return s;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)cap};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
+                         box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  return NAT_OK;
+}
+
+int sm_count(int* n) {
+  int dev = 0;
+  NAT_CUDA(cudaGetDevice(&dev));
+  NAT_CUDA(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
+  return NAT_OK;
+}
+
+template <int DP>
+int fwd(const Args& a, const Layout& l) {
+  const nat_attn_params& p = a.p;
+  const int group = p.n_heads / p.n_kv_heads, tq = kRows / group;
+  int sms = 0;
+  int s = require_sm100();
+  if (s == NAT_OK) s = sm_count(&sms);
+  CUtensorMap mq, mk, mv;
+  if (s == NAT_OK) s = make_map(&mq, a.q, p.head_dim, p.n_heads, a.cap, p.q_stride, group, tq);
+  if (s == NAT_OK) s = make_map(&mk, a.k, p.head_dim, p.n_kv_heads, a.cap, p.k_stride, 1, kRows);
+  if (s == NAT_OK) s = make_map(&mv, a.v, p.head_dim, p.n_kv_heads, a.cap, p.v_stride, 1, kRows);
+  if (s != NAT_OK) return s;
+  NAT_CUDA(cudaFuncSetAttribute(attn_fwd_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)FwdShape<DP>::kSmem));
+  s = launch_plan(a, l, kPlanFwd, true);
+  if (s != NAT_OK) return s;
+  FwdParams fp{};
+  fp.list = entries(a, l, kPlanFwd);
+  fp.count = &head(a)->count[kPlanFwd];
+  fp.status = &head(a)->status;
+  fp.out = (__nv_bfloat16*)a.out;
+  fp.lse = a.lse;
+  fp.o_stride = p.o_stride;
+  fp.n_heads = p.n_heads;
+  fp.n_kv_heads = p.n_kv_heads;
+  fp.group = group;
+  fp.tq = tq;
+  fp.head_dim = p.head_dim;
+  fp.scale = p.scale;
+  const int64_t units = l.entries[kPlanFwd] * p.n_kv_heads;
+  const unsigned grid = (unsigned)min((int64_t)sms, units);
+  attn_fwd_kernel<DP><<<grid, 384, FwdShape<DP>::kSmem, a.stream>>>(mq, mk, mv, fp);
+  NAT_LAUNCH_CHECK("attn_fwd_kernel");
+  return NAT_OK;
+}
+
+}  // namespace
+
+int bf16_fwd(const Args& a, const Layout& l) {
+  return a.p.head_dim <= 64 ? fwd<64>(a, l) : fwd<128>(a, l);
+}
+
+}  // namespace attn
+}  // namespace nat

@@ -277,9 +277,6 @@ int f32_fwd(const Args& a, const Layout& l) {
 int f32_bwd(const Args& a, const Layout& l) {
   return a.p.head_dim <= 64 ? bwd<float, 64>(a, l) : bwd<float, 128>(a, l);
 }
-int bf16_fwd(const Args& a, const Layout& l) {
-  return a.p.head_dim <= 64 ? fwd<__nv_bfloat16, 64>(a, l) : fwd<__nv_bfloat16, 128>(a, l);
-}
 int bf16_bwd(const Args& a, const Layout& l) {
   return a.p.head_dim <= 64 ? bwd<__nv_bfloat16, 64>(a, l) : bwd<__nv_bfloat16, 128>(a, l);
 }

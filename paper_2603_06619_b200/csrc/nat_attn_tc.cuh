@@ -1,0 +1,119 @@
+// Tensor-core helpers of the packed attention beyond nat_tc.cuh: an A operand in tensor memory,
+// tensor-memory stores, 3-D tile loads, and the operand tiles' geometry.
+#pragma once
+
+#include "nat_tc.cuh"
+
+namespace nat {
+namespace attn {
+
+constexpr int kRows = 128;                          // rows of every operand tile
+constexpr uint32_t kPanel = kRows * 128;            // 128 rows of 64 bfloat16 columns, 128-byte swizzle
+
+// D[tmem] (+)= A[tmem] * B[smem], A of bf16 pairs packed along K into 32-bit columns.
+__device__ __forceinline__ void umma_ts_bf16(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc,
+                                             uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// 32 consecutive 32-bit columns of this thread's lane; complete after tmem_st_wait().
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+      "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+      "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+               : "memory");
+}
+
+// Eight columns, complete on return.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(taddr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap* map, uint64_t* bar,
+                                            int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_dst),
+      "l"(map), "r"(tc::smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// A wait of a whole warp: all lanes go on, or all give up.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  return __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar, parity, abort_flag));
+}
+
+// Registers a thread of the calling warpgroup from here on; the shares of a block must add up to
+// what it was launched with.
+template <int N>
+__device__ __forceinline__ void regs_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Product of two K-major tiles (rows x D each): step `kk` covers 16 of D's columns.
+__device__ __forceinline__ uint64_t desc_kmajor(uint32_t tile, int kk) {
+  return tc::smem_desc_sw128(tile + (uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32, 16, 1024);
+}
+// A tile whose rows are the contraction: step `kk` covers 16 rows, D is the contiguous dimension.
+__device__ __forceinline__ uint64_t desc_mnmajor(uint32_t tile, int kk) {
+  return tc::smem_desc_sw128(tile + (uint32_t)kk * 2048, kPanel, 1024);
+}
+
+// Zeroes rows [first, 128) of a tile of NP panels that TMA has finished writing (one warp), for
+// the tensor cores to read: the rows belong to another sequence, or to none, and a weight of
+// zero would not hide an infinity or a NaN in them.
+template <int NP>
+__device__ __forceinline__ void zero_rows(uint8_t* tile, int first, int lane) {
+  for (int i = lane; i < (kRows - first) * 8 * NP; i += 32) {
+    const int panel = i / ((kRows - first) * 8), in = i % ((kRows - first) * 8);
+    *reinterpret_cast<uint4*>(tile + panel * kPanel + first * 128 + in * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  tc::fence_proxy_async();
+  __syncwarp();
+}
+
+}  // namespace attn
+}  // namespace nat
