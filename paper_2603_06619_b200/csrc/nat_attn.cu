@@ -13,9 +13,21 @@ constexpr int kBuckets = 1024;
 // A counting sort by cost; the order inside a bucket is not fixed, which no result depends on.
 // Sequence bounds are clamped to [0, cap], so no list entry points outside the buffers whatever
 // cu_seqlens holds.
-__global__ void __launch_bounds__(1024)
-plan_kernel(const int32_t* __restrict__ cu, int32_t B, int64_t cap, int tile, int by_rest,
-            int64_t max_entries, Entry* __restrict__ list, Head* head, int which, int first) {
+struct PlanArgs {
+  const int32_t* cu;
+  int32_t B;
+  int64_t cap, max_entries;
+  int tile, by_rest, which;
+  Entry* list;
+  Head* head;
+};
+
+__device__ __forceinline__ void plan(const PlanArgs& a) {
+  const int32_t* cu = a.cu;
+  const int32_t B = a.B;
+  const int64_t cap = a.cap, max_entries = a.max_entries;
+  const int tile = a.tile, by_rest = a.by_rest;
+  Entry* list = a.list;
   __shared__ uint32_t bucket[kBuckets];
   __shared__ int longest;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -63,13 +75,57 @@ plan_kernel(const int32_t* __restrict__ cu, int32_t B, int64_t cap, int tile, in
       bucket[threadIdx.x] = before + run - mine;
       if (threadIdx.x == kBuckets - 1) {
         const uint32_t total = before + run;
-        head->count[which] = (uint32_t)min((int64_t)total, max_entries);
-        // more rows than the buffers hold, or bounds that are not ascending
-        const uint32_t bad = ((int64_t)cu[B] > cap || total > max_entries) ? NAT_DEV_CAPACITY : 0u;
-        if (first) head->status = bad;
-        else if (bad) atomicOr(&head->status, bad);
+        a.head->count[a.which] = (uint32_t)min((int64_t)total, max_entries);
+        // more rows than the buffers hold, or bounds that are not ascending; a call's plans find the same
+        a.head->status = ((int64_t)cu[B] > cap || total > max_entries) ? NAT_DEV_CAPACITY : 0u;
       }
       __syncthreads();
+    }
+  }
+}
+
+__global__ void __launch_bounds__(1024) plan_kernel(PlanArgs a) { plan(a); }
+
+// What both kernels of the bfloat16 backward pass read, in one launch: their plans (blocks 0 and 1)
+// and, for every row of out, delta = dout . out and lse in units of log 2.  Bound by the read of
+// out and dout.  Half a warp takes a row's 16-byte pieces.
+struct StatsArgs {
+  const __nv_bfloat16 *out, *dout;
+  const float* lse;
+  float *lse2, *delta;
+  int64_t o_stride;
+  int n_heads, head_dim;
+};
+
+__global__ void __launch_bounds__(1024) bwd_prologue_kernel(PlanArgs a, PlanArgs b, StatsArgs s) {
+  if (blockIdx.x < 2) {
+    plan(blockIdx.x == 0 ? a : b);
+    return;
+  }
+  const int64_t rows = min((int64_t)max(a.cu[a.B], 0), a.cap) * s.n_heads;
+  const int lane = threadIdx.x & 15;
+  const int64_t step = (int64_t)(gridDim.x - 2) * 64;
+  // the bound is the block's: both halves of a warp take the same turns
+  for (int64_t base = (int64_t)(blockIdx.x - 2) * 64; base < rows; base += step) {
+    const int64_t row = base + (threadIdx.x >> 4);
+    float dot = 0.f;
+    if (row < rows && lane * 8 < s.head_dim) {
+      const uint32_t token = (uint32_t)(row / s.n_heads), h = (uint32_t)(row - (int64_t)token * s.n_heads);
+      const int64_t at = (int64_t)token * s.o_stride + (int64_t)h * s.head_dim + lane * 8;
+      const uint4 x = __ldg(reinterpret_cast<const uint4*>(s.out + at));
+      const uint4 y = __ldg(reinterpret_cast<const uint4*>(s.dout + at));
+      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        dot = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), dot);
+        dot = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), dot);
+      }
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o, 16);
+    if (row < rows && lane == 0) {
+      s.delta[row] = dot;
+      s.lse2[row] = s.lse[row] * 1.4426950408889634f;
     }
   }
 }
@@ -120,8 +176,9 @@ int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool b
 }  // namespace
 
 int plan_tile(const nat_attn_params& p, Plan which) {
-  if (p.dtype == NAT_BF16 && which == kPlanFwd) return 2 * (128 / (p.n_heads / p.n_kv_heads));
-  return 32;
+  if (p.dtype == NAT_F32) return 32;
+  const int tq = 128 / (p.n_heads / p.n_kv_heads);  // tokens of a tile with the group's heads folded in
+  return which == kPlanFwd ? 2 * tq : which == kPlanDq ? tq : 128;
 }
 
 Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
@@ -134,15 +191,32 @@ Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
     at = align_up(at + (size_t)l.entries[w] * sizeof(Entry), 256);
   }
   l.delta_off = at;
-  l.total = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
+  l.lse2_off = at = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
+  if (p.dtype == NAT_BF16) at = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
+  l.total = at;
   return l;
 }
 
-int launch_plan(const Args& a, const Layout& l, Plan which, bool first) {
-  plan_kernel<<<1, 1024, 0, a.stream>>>(a.cu_seqlens, a.B, a.cap, plan_tile(a.p, which),
-                                        which == kPlanDkv ? 1 : 0, l.entries[which],
-                                        entries(a, l, which), head(a), (int)which, first ? 1 : 0);
+namespace {
+PlanArgs plan_args(const Args& a, const Layout& l, Plan which) {
+  return {a.cu_seqlens, a.B, a.cap, l.entries[which], plan_tile(a.p, which), which == kPlanDkv ? 1 : 0,
+          (int)which, entries(a, l, which), head(a)};
+}
+}  // namespace
+
+int launch_plan(const Args& a, const Layout& l, Plan which) {
+  plan_kernel<<<1, 1024, 0, a.stream>>>(plan_args(a, l, which));
   NAT_LAUNCH_CHECK("plan_kernel");
+  return NAT_OK;
+}
+
+int launch_bwd_prologue(const Args& a, const Layout& l) {
+  const StatsArgs s{(const __nv_bfloat16*)a.out, (const __nv_bfloat16*)a.dout, a.lse, lse2(a, l),
+                    delta(a, l), a.p.o_stride, a.p.n_heads, a.p.head_dim};
+  const int64_t want = (a.cap * a.p.n_heads + 63) / 64;
+  const unsigned blocks = 2 + (unsigned)min(want, (int64_t)148 * 2 * 4);
+  bwd_prologue_kernel<<<blocks, 1024, 0, a.stream>>>(plan_args(a, l, kPlanDq), plan_args(a, l, kPlanDkv), s);
+  NAT_LAUNCH_CHECK("bwd_prologue_kernel");
   return NAT_OK;
 }
 

@@ -42,7 +42,7 @@ enum Plan { kPlanFwd = 0, kPlanDq = 1, kPlanDkv = 2 };
 int plan_tile(const nat_attn_params& p, Plan which);
 
 struct Layout {
-  size_t plan_off[3], delta_off, total;
+  size_t plan_off[3], delta_off, lse2_off, total;
   int64_t entries[3];
 };
 Layout layout(const nat_attn_params& p, int32_t B, int64_t cap);
@@ -55,8 +55,14 @@ inline float* delta(const Args& a, const Layout& l) {
   return reinterpret_cast<float*>((char*)a.workspace + l.delta_off);
 }
 
-// Writes the plan of `which` (and, for the first plan of a call, clears the status word).
-int launch_plan(const Args& a, const Layout& l, Plan which, bool first);
+inline float* lse2(const Args& a, const Layout& l) {
+  return reinterpret_cast<float*>((char*)a.workspace + l.lse2_off);
+}
+
+// Writes the plan of `which` and the status word.
+int launch_plan(const Args& a, const Layout& l, Plan which);
+// Both plans of the bfloat16 backward pass, delta and lse2.
+int launch_bwd_prologue(const Args& a, const Layout& l);
 
 int f32_fwd(const Args& a, const Layout& l);
 int f32_bwd(const Args& a, const Layout& l);

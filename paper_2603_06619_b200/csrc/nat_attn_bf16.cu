@@ -22,7 +22,6 @@ namespace nat {
 namespace attn {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescale = 8.f;  // growth of a row's maximum (log2) that is left in P
 
@@ -390,6 +389,8 @@ int get_encoder(EncodeTiledFn* out) {
   return NAT_OK;
 }
 
+}  // namespace
+
 // [cap, heads, D] with a token stride; a box of 64 columns x box_heads x box_tokens, zero outside.
 int make_map(CUtensorMap* map, const void* base, int D, int heads, int64_t cap, int64_t stride,
              int box_heads, int box_tokens) {
@@ -414,6 +415,8 @@ int sm_count(int* n) {
   return NAT_OK;
 }
 
+namespace {
+
 template <int DP>
 int fwd(const Args& a, const Layout& l) {
   const nat_attn_params& p = a.p;
@@ -428,7 +431,7 @@ int fwd(const Args& a, const Layout& l) {
   if (s != NAT_OK) return s;
   NAT_CUDA(cudaFuncSetAttribute(attn_fwd_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)FwdShape<DP>::kSmem));
-  s = launch_plan(a, l, kPlanFwd, true);
+  s = launch_plan(a, l, kPlanFwd);
   if (s != NAT_OK) return s;
   FwdParams fp{};
   fp.list = entries(a, l, kPlanFwd);

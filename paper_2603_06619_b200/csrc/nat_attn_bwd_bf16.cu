@@ -1,0 +1,650 @@
+// Backward pass of the packed causal attention on the tensor cores, bfloat16.
+//
+// Two kernels, both persistent with one block per multiprocessor, each forming P = exp(S - lse) anew:
+//   dq   a row tile of queries (heads of a group folded in) against its keys: S = Q K^T,
+//        dP = dO V^T, dS = P (dP - delta), dQ += dS K                      (three products)
+//   dkv  a tile of 128 keys against all later queries of its group, transposed: S' = K Q^T,
+//        dP' = V dO^T, dV += P' dO, dK += dS' Q                            (four products)
+// Seven products where one kernel over both would do five, but every sum stays in tensor memory and
+// in a fixed order: no atomics on dQ, no fp32 scratch for it, and results that repeat bit for bit.
+//
+// Warps: 0-3 and 4-7 take the two column halves of the score tile (a thread has 64 columns of one
+// row), 8 issues MMAs, 9 loads tiles by TMA, 10 (dkv) loads lse and delta of the query rows.
+#include <cuda.h>
+
+#include "nat_attn.cuh"
+#include "nat_attn_tc.cuh"
+
+namespace nat {
+namespace attn {
+namespace {
+
+struct BwdParams {
+  const Entry* list;
+  const uint32_t* count;
+  uint32_t* status;
+  const float *lse2, *delta;  // [cap, n_heads]
+  __nv_bfloat16 *dq, *dk, *dv;
+  int64_t q_stride, k_stride, v_stride;
+  int n_heads, n_kv_heads, group, tq, head_dim;
+  float scale;
+};
+
+template <int DP>
+struct BwdShape {
+  static constexpr int kNP = DP / 64;
+  static constexpr uint32_t kTile = kNP * kPanel;
+  static constexpr int kStages = 5;                       // tiles of the ring, beside two resident ones
+  static constexpr uint32_t kTiles = (2 + kStages) * kTile;
+  static constexpr uint32_t kStats = 2 * 2 * kRows * 4;   // lse2 and delta of two row tiles
+  static constexpr uint32_t kSlack = 768;                 // room to round the base up to 1024 bytes
+  static constexpr uint32_t kSmem = kTiles + kStats + 256 + kSlack;
+};
+
+// The tiles need a 1024-byte aligned base.  Dynamic shared memory starts on such a boundary where a
+// kernel has no static shared memory; should it not, the block reports it and does nothing.
+__device__ __forceinline__ uint8_t* tile_base(uint8_t* raw, uint32_t slack, bool* fits) {
+  const uint32_t at = tc::smem_u32(raw), up = (at + 1023u) & ~1023u;
+  *fits = up - at <= slack;
+  return raw + (up - at);
+}
+
+// 64 columns of the thread's row in tensor memory.
+__device__ __forceinline__ void load64(uint32_t addr, float (&x)[64]) {
+  uint32_t r[64];
+  tc::tmem_ld32_issue(addr, r);
+  tc::tmem_ld32_issue(addr + 32, r + 32);
+  tc::tmem_ld_wait(r);
+  tc::tmem_ld_pin(r + 32);
+#pragma unroll
+  for (int c = 0; c < 64; ++c) x[c] = __uint_as_float(r[c]);
+}
+
+// The same as bf16 pairs into the first 32 of the 64 columns they came from: each half of the
+// threads stays in its own columns.
+__device__ __forceinline__ void store64(uint32_t addr, const float (&x)[64]) {
+  uint32_t r[32];
+#pragma unroll
+  for (int c = 0; c < 32; ++c) r[c] = bf16_pair(x[2 * c], x[2 * c + 1]);
+  tmem_st32(addr, r);
+  tmem_st_wait();
+}
+
+// Where step kk (16 of the contraction) of such an operand lies.
+__device__ __forceinline__ uint32_t half_cols(int kk) { return (uint32_t)(kk < 4 ? kk * 8 : 64 + (kk - 4) * 8); }
+
+// D columns [half * DP/2, ...) of an accumulator row, times f, to global memory.
+template <int DP>
+__device__ __forceinline__ void store_acc(uint32_t addr, int half, __nv_bfloat16* dst, int D, float f, bool valid) {
+#pragma unroll
+  for (int c = 0; c < DP / 64; ++c) {
+    const int col = half * (DP / 2) + c * 32;
+    float o[32];
+    tc::tmem_ld32(addr + col, o);
+    if (valid) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* x = o + 8 * i;
+        if (col + 8 * i < D)
+          *reinterpret_cast<uint4*>(dst + col + 8 * i) =
+              make_uint4(bf16_pair(x[0] * f, x[1] * f), bf16_pair(x[2] * f, x[3] * f),
+                         bf16_pair(x[4] * f, x[5] * f), bf16_pair(x[6] * f, x[7] * f));
+      }
+    }
+  }
+}
+
+// Ring of tiles: `item` numbers the loads of a block, stage item % kStages.
+template <int DP>
+struct Loader {
+  using R = BwdShape<DP>;
+  uint8_t* ring;
+  uint64_t *full, *empty, *raw;
+  volatile uint32_t* abort_flag;
+  int lane;
+  uint32_t item = 0, raw_turns = 0;
+  bool ok = true;
+
+  // One tile of the box [.., heads, tokens] at (head, row); rows [valid, 128) are zeroed where `valid`
+  // is below `rows`, the rows that the box brings.
+  __device__ __forceinline__ void load(const CUtensorMap* map, int head, int row, int rows, int valid) {
+    const int s = item % R::kStages;
+    ok = ok && warp_wait(&empty[s], ((item / R::kStages) & 1) ^ 1, abort_flag);
+    if (!ok) return;
+    ++item;
+    const bool fix = valid < rows;
+    uint64_t* bar = fix ? raw : &full[s];
+    uint8_t* dst = ring + s * R::kTile;
+    if (lane == 0) {
+      tc::mbar_arrive_expect_tx(bar, (uint32_t)rows * 128u * R::kNP);
+      for (int c = 0; c < R::kNP; ++c)
+        tma_load_3d(tc::smem_u32(dst + c * kPanel), map, bar, c * 64, head, row);
+    }
+    if (fix) {
+      ok = warp_wait(raw, raw_turns & 1, abort_flag);
+      ++raw_turns;
+      if (!ok) return;
+      zero_rows<R::kNP>(dst, valid, lane);
+      if (lane == 0) tc::mbar_arrive(&full[s]);
+    }
+  }
+
+  // After a wait that gave up: the block must not leave with a copy in flight.
+  __device__ __forceinline__ void land(uint64_t* resident, uint32_t resident_turns) {
+    if (ok) return;
+    uint32_t never = 0u;
+    if (raw_turns) tc::mbar_wait(raw, (raw_turns - 1) & 1, &never, 1000000000ull), never = 0u;
+    for (uint32_t i = item > (uint32_t)R::kStages ? item - R::kStages : 0; i < item; ++i)
+      tc::mbar_wait(&full[i % R::kStages], (i / R::kStages) & 1, &never, 1000000000ull), never = 0u;
+    if (resident_turns) tc::mbar_wait(resident, (resident_turns - 1) & 1, &never, 1000000000ull);
+  }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(384, 1)
+attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+               const BwdParams p) {
+  using R = BwdShape<DP>;
+  constexpr int kNS = R::kStages;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  bool fits;
+  uint8_t* smem = tile_base(smem_raw, R::kSlack, &fits);
+  if (!fits) {
+    if (threadIdx.x == 0) atomicOr(p.status, NAT_DEV_TIMEOUT);
+    return;
+  }
+  uint8_t* ring = smem + 2 * R::kTile;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + R::kTiles + R::kStats);
+  uint64_t *qdo_full = bars, *qdo_empty = bars + 1, *s_full = bars + 2, *dp_full = bars + 4, *ds_full = bars + 5;
+  uint64_t *dq_done = bars + 6, *raw = bars + 7, *drain = bars + 8, *full = bars + 9, *empty = bars + 9 + kNS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9 + 2 * kNS);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
+
+  if (threadIdx.x == 0) {
+    tc::mbar_init(qdo_full, 1);
+    tc::mbar_init(qdo_empty, 1);
+    tc::mbar_init(&s_full[0], 1);
+    tc::mbar_init(&s_full[1], 1);
+    tc::mbar_init(dp_full, 1);
+    tc::mbar_init(ds_full, 256);
+    tc::mbar_init(dq_done, 1);
+    tc::mbar_init(raw, 1);
+    tc::mbar_init(drain, 1);
+    for (int s = 0; s < kNS; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    *abort_flag = 0u;
+    tc::fence_barrier_init();
+  }
+  if (warp == 8) {
+    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = *tmem_slot;  // S/dS in two buffers, dP, dQ: 128 columns each
+  // tiles of keys of a list entry
+  auto tiles_of = [&](const Entry& e) { return (min(e.lo + p.tq, e.seq_hi) - e.seq_lo + kRows - 1) / kRows; };
+
+  if (warp == 9) {
+    Loader<DP> ld{ring, full, empty, raw, abort_flag, lane};
+    uint32_t turns = 0;
+    const int q_rows = p.group * p.tq;
+    for (uint32_t u = blockIdx.x; ld.ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int head = (int)(u % p.n_kv_heads), n = tiles_of(e);
+      ld.ok = warp_wait(qdo_empty, (turns & 1) ^ 1, abort_flag);
+      if (!ld.ok) break;
+      ++turns;
+      if (lane == 0) {
+        tc::mbar_arrive_expect_tx(qdo_full, 2u * (uint32_t)q_rows * 128u * R::kNP);
+        for (int c = 0; c < R::kNP; ++c) {
+          tma_load_3d(tc::smem_u32(smem + c * kPanel), &map_q, qdo_full, c * 64, head * p.group, e.lo);
+          tma_load_3d(tc::smem_u32(smem + R::kTile + c * kPanel), &map_do, qdo_full, c * 64, head * p.group, e.lo);
+        }
+      }
+      const int end = min(e.lo + p.tq, e.seq_hi);
+      for (int j = 0; ld.ok && j < n; ++j) {
+        const int row = e.seq_lo + j * kRows;
+        // K is also the second factor of dS K, where rows past the end must not count; V only
+        // meets the mask of dS
+        ld.load(&map_k, head, row, kRows, min(end - row, kRows));
+        ld.load(&map_v, head, row, kRows, kRows);
+      }
+    }
+    ld.land(qdo_full, turns);
+  } else if (warp == 8) {
+    if (lane == 0) {
+      constexpr uint32_t kIdescS = tc::instr_desc_bf16(128, 128, 0, 0);
+      constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
+      const int ksteps = (p.head_dim + 15) / 16;
+      const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile, ring_addr = tc::smem_u32(ring);
+      uint32_t item = 0, turns = 0, tile = 0;  // `tile` numbers the key tiles of the block
+      bool ok = true;
+      auto take = [&](uint32_t i) {
+        ok = ok && tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, abort_flag);
+        tc::fence_after_sync();
+      };
+      auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
+        const uint32_t b = ring_addr + (i % kNS) * R::kTile;
+#pragma unroll 1
+        for (int kk = 0; kk < ksteps; ++kk)
+          tc::umma_bf16(d, desc_kmajor(a, kk), desc_kmajor(b, kk), kIdescS, kk > 0);
+        tc::umma_commit(bar);
+      };
+      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Entry e = p.list[u / p.n_kv_heads];
+        const int n = tiles_of(e);
+        ok = tc::mbar_wait(qdo_full, turns & 1, abort_flag);
+        ++turns;
+        take(item);  // items K_0 V_0 K_1 V_1 ...
+        if (!ok) break;
+        product(tmem + (tile & 1) * 128, q_addr, item, &s_full[tile & 1]);
+        take(item + 1);
+        if (!ok) break;
+        product(tmem + 256, do_addr, item + 1, dp_full);
+        tc::umma_commit(&empty[(item + 1) % kNS]);
+        if (n == 1) tc::umma_commit(qdo_empty);
+        for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
+          if (j + 1 < n) {
+            take(item + 2);
+            if (!ok) break;
+            product(tmem + ((tile + 1) & 1) * 128, q_addr, item + 2, &s_full[(tile + 1) & 1]);
+          }
+          ok = tc::mbar_wait(ds_full, tile & 1, abort_flag);
+          if (!ok) break;
+          tc::fence_after_sync();
+          if (j + 1 < n) {
+            take(item + 3);
+            if (!ok) break;
+            product(tmem + 256, do_addr, item + 3, dp_full);
+            tc::umma_commit(&empty[(item + 3) % kNS]);
+            if (j + 2 == n) tc::umma_commit(qdo_empty);
+          }
+          const uint32_t b = ring_addr + (item % kNS) * R::kTile, a = tmem + (tile & 1) * 128;
+#pragma unroll 1
+          for (int kk = 0; kk < 8; ++kk)
+            umma_ts_bf16(tmem + 384, a + half_cols(kk), desc_mnmajor(b, kk), kIdescD, j > 0 || kk > 0);
+          tc::umma_commit(&empty[item % kNS]);
+        }
+        if (ok) tc::umma_commit(dq_done);
+      }
+      tc::umma_commit(drain);
+      uint32_t never = 0u;
+      tc::mbar_wait(drain, 0, &never);
+    }
+  } else if (warp < 8) {
+    const int half = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16, mine = lane_base + half * 64;
+    const int token_in = row / p.group, head_in = row % p.group;
+    const float sc = p.scale * kLog2e;
+    uint32_t tile = 0, turns = 0;
+    bool ok = true;
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int n = tiles_of(e), token = e.lo + token_in;
+      const int head = (int)(u % p.n_kv_heads) * p.group + head_in;
+      const bool valid = row < p.group * p.tq && token < e.seq_hi;
+      const int64_t at = (int64_t)token * p.n_heads + head;
+      const float lse2 = valid ? p.lse2[at] : 0.f, delta = valid ? p.delta[at] : 0.f;
+      for (int j = 0; j < n; ++j, ++tile) {
+        ok = warp_wait(&s_full[tile & 1], (tile >> 1) & 1, abort_flag);
+        if (!ok) break;
+        tc::fence_after_sync();
+        const uint32_t s_addr = tmem + (tile & 1) * 128 + mine;
+        float x[64], d[64];
+        load64(s_addr, x);
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c] = ex2(fmaf(x[c], sc, -lse2));
+        ok = warp_wait(dp_full, tile & 1, abort_flag);
+        if (!ok) break;
+        tc::fence_after_sync();
+        load64(tmem + 256 + mine, d);
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c] *= d[c] - delta;
+        const int kv0 = e.seq_lo + j * kRows;
+        if (kv0 + kRows - 1 > e.lo) {  // the tile touches the diagonal
+          const int last = token - kv0 - half * 64;
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c > last) x[c] = 0.f;
+        }
+        store64(s_addr, x);
+        tc::fence_before_sync();
+        tc::mbar_arrive(ds_full);
+      }
+      if (!ok) break;
+      ok = warp_wait(dq_done, turns & 1, abort_flag);
+      if (!ok) break;
+      ++turns;
+      tc::fence_after_sync();
+      store_acc<DP>(tmem + 384 + lane_base, half,
+                    p.dq + (int64_t)token * p.q_stride + (int64_t)head * p.head_dim, p.head_dim, p.scale, valid);
+      tc::fence_before_sync();
+    }
+  }
+
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
+  if (warp == 8) tc::tmem_dealloc(tmem, 512);
+}
+
+template <int DP>
+__global__ void __launch_bounds__(384, 1)
+attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                const BwdParams p) {
+  using R = BwdShape<DP>;
+  constexpr int kNS = R::kStages;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  bool fits;
+  uint8_t* smem = tile_base(smem_raw, R::kSlack, &fits);
+  if (!fits) {
+    if (threadIdx.x == 0) atomicOr(p.status, NAT_DEV_TIMEOUT);
+    return;
+  }
+  uint8_t* ring = smem + 2 * R::kTile;
+  float* stats = reinterpret_cast<float*>(smem + R::kTiles);  // [2][lse2 | delta][128]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + R::kTiles + R::kStats);
+  uint64_t *kv_full = bars, *kv_empty = bars + 1, *s_full = bars + 2, *p_full = bars + 3, *dp_full = bars + 4;
+  uint64_t *ds_full = bars + 5, *done = bars + 6, *raw = bars + 7, *drain = bars + 8, *st_full = bars + 9;
+  uint64_t *st_empty = bars + 11, *full = bars + 13, *empty = bars + 13 + kNS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 13 + 2 * kNS);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
+  const int q_rows = p.group * p.tq;
+
+  if (threadIdx.x == 0) {
+    tc::mbar_init(kv_full, 1);
+    tc::mbar_init(kv_empty, 1);
+    tc::mbar_init(s_full, 1);
+    tc::mbar_init(p_full, 256);
+    tc::mbar_init(dp_full, 1);
+    tc::mbar_init(ds_full, 256);
+    tc::mbar_init(done, 1);
+    tc::mbar_init(raw, 1);
+    tc::mbar_init(drain, 1);
+    for (int s = 0; s < 2; ++s) {
+      tc::mbar_init(&st_full[s], 1);
+      tc::mbar_init(&st_empty[s], 8);
+    }
+    for (int s = 0; s < kNS; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    *abort_flag = 0u;
+    tc::fence_barrier_init();
+  }
+  if (warp == 8) {
+    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_relinquish();
+  }
+  if (q_rows < kRows) {
+    // rows that no load reaches are part of every contraction over queries: zero, once
+    for (uint32_t i = threadIdx.x; i < kNS * R::kTile / 16; i += blockDim.x)
+      reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);
+    tc::fence_proxy_async();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = *tmem_slot;  // S'/P', dP'/dS', dV, dK: 128 columns each
+  // tiles of queries of a list entry: they start at the key tile's first token
+  auto tiles_of = [&](const Entry& e) { return (e.seq_hi - e.lo + p.tq - 1) / p.tq; };
+
+  if (warp == 9) {
+    Loader<DP> ld{ring, full, empty, raw, abort_flag, lane};
+    uint32_t turns = 0;
+    for (uint32_t u = blockIdx.x; ld.ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int head = (int)(u % p.n_kv_heads), n = tiles_of(e);
+      ld.ok = warp_wait(kv_empty, (turns & 1) ^ 1, abort_flag);
+      if (!ld.ok) break;
+      ++turns;
+      if (lane == 0) {
+        tc::mbar_arrive_expect_tx(kv_full, 2u * R::kTile);
+        for (int c = 0; c < R::kNP; ++c) {
+          tma_load_3d(tc::smem_u32(smem + c * kPanel), &map_k, kv_full, c * 64, head, e.lo);
+          tma_load_3d(tc::smem_u32(smem + R::kTile + c * kPanel), &map_v, kv_full, c * 64, head, e.lo);
+        }
+      }
+      for (int j = 0; ld.ok && j < n; ++j) {
+        const int row = e.lo + j * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
+        ld.load(&map_q, head * p.group, row, q_rows, valid);
+        ld.load(&map_do, head * p.group, row, q_rows, valid);
+      }
+    }
+    ld.land(kv_full, turns);
+  } else if (warp == 10) {
+    // lse and delta of the query rows, up to two tiles ahead
+    uint32_t tile = 0;
+    bool ok = true;
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int head = (int)(u % p.n_kv_heads) * p.group, n = tiles_of(e);
+      for (int j = 0; j < n; ++j, ++tile) {
+        const int first = e.lo + j * p.tq, valid = min((e.seq_hi - first) * p.group, q_rows);
+        float a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = lane + 32 * i, token = first + r / p.group;
+          const int64_t at = (int64_t)token * p.n_heads + head + r % p.group;
+          a[i] = r < valid ? __ldg(p.lse2 + at) : 0.f;
+          b[i] = r < valid ? __ldg(p.delta + at) : 0.f;
+        }
+        ok = warp_wait(&st_empty[tile & 1], ((tile >> 1) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        float* slot = stats + (tile & 1) * 2 * kRows;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) slot[lane + 32 * i] = a[i], slot[kRows + lane + 32 * i] = b[i];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&st_full[tile & 1]);
+      }
+    }
+  } else if (warp == 8) {
+    if (lane == 0) {
+      constexpr uint32_t kIdescS = tc::instr_desc_bf16(128, 128, 0, 0);
+      constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
+      const int ksteps = (p.head_dim + 15) / 16;
+      const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile, ring_addr = tc::smem_u32(ring);
+      uint32_t item = 0, turns = 0, tile = 0;
+      bool ok = true;
+      auto take = [&](uint32_t i) {
+        ok = ok && tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, abort_flag);
+        tc::fence_after_sync();
+      };
+      auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
+        const uint32_t b = ring_addr + (i % kNS) * R::kTile;
+#pragma unroll 1
+        for (int kk = 0; kk < ksteps; ++kk)
+          tc::umma_bf16(d, desc_kmajor(a, kk), desc_kmajor(b, kk), kIdescS, kk > 0);
+        tc::umma_commit(bar);
+      };
+      auto accumulate = [&](uint32_t d, uint32_t a, uint32_t i, bool add) {
+        const uint32_t b = ring_addr + (i % kNS) * R::kTile;
+#pragma unroll 1
+        for (int kk = 0; kk < 8; ++kk)
+          umma_ts_bf16(d, a + half_cols(kk), desc_mnmajor(b, kk), kIdescD, add || kk > 0);
+        tc::umma_commit(&empty[i % kNS]);
+      };
+      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Entry e = p.list[u / p.n_kv_heads];
+        const int n = tiles_of(e);
+        ok = tc::mbar_wait(kv_full, turns & 1, abort_flag);
+        ++turns;
+        take(item);  // items Q_0 dO_0 Q_1 dO_1 ...
+        if (!ok) break;
+        product(tmem, k_addr, item, s_full);
+        take(item + 1);
+        if (!ok) break;
+        product(tmem + 128, v_addr, item + 1, dp_full);
+        for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
+          ok = tc::mbar_wait(p_full, tile & 1, abort_flag);
+          if (!ok) break;
+          tc::fence_after_sync();
+          accumulate(tmem + 256, tmem, item + 1, j > 0);  // dV += P' dO
+          if (j + 1 < n) {
+            take(item + 2);
+            if (!ok) break;
+            product(tmem, k_addr, item + 2, s_full);
+          }
+          ok = tc::mbar_wait(ds_full, tile & 1, abort_flag);
+          if (!ok) break;
+          tc::fence_after_sync();
+          accumulate(tmem + 384, tmem + 128, item, j > 0);  // dK += dS' Q
+          if (j + 1 < n) {
+            take(item + 3);
+            if (!ok) break;
+            product(tmem + 128, v_addr, item + 3, dp_full);
+          }
+        }
+        if (ok) {
+          tc::umma_commit(done);
+          tc::umma_commit(kv_empty);
+        }
+      }
+      tc::umma_commit(drain);
+      uint32_t never = 0u;
+      tc::mbar_wait(drain, 0, &never);
+    }
+  } else if (warp < 8) {
+    const int half = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16, mine = lane_base + half * 64;
+    const float sc = p.scale * kLog2e;
+    uint32_t tile = 0, turns = 0;
+    bool ok = true;
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int n = tiles_of(e), key = e.lo + row;
+      for (int j = 0; j < n; ++j, ++tile) {
+        const int first = e.lo + j * p.tq, rows = min((e.seq_hi - first) * p.group, q_rows);
+        const float4* slot = reinterpret_cast<const float4*>(stats + (tile & 1) * 2 * kRows + half * 64);
+        ok = warp_wait(&st_full[tile & 1], (tile >> 1) & 1, abort_flag) && warp_wait(s_full, tile & 1, abort_flag);
+        if (!ok) break;
+        tc::fence_after_sync();
+        float x[64], d[64];
+        load64(tmem + mine, x);
+#pragma unroll
+        for (int c = 0; c < 64; c += 4) {
+          const float4 l = slot[c / 4];
+          x[c] = ex2(fmaf(x[c], sc, -l.x));
+          x[c + 1] = ex2(fmaf(x[c + 1], sc, -l.y));
+          x[c + 2] = ex2(fmaf(x[c + 2], sc, -l.z));
+          x[c + 3] = ex2(fmaf(x[c + 3], sc, -l.w));
+        }
+        // columns of queries before the key, and of rows that are not there
+        const bool edge = first < e.lo + kRows || rows < kRows;
+        const int c_lo = (key - first) * p.group - half * 64, c_hi = rows - half * 64;
+        if (edge) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c < c_lo || c >= c_hi) x[c] = 0.f;
+        }
+        store64(tmem + mine, x);
+        tc::fence_before_sync();
+        tc::mbar_arrive(p_full);
+        ok = warp_wait(dp_full, tile & 1, abort_flag);
+        if (!ok) break;
+        tc::fence_after_sync();
+        load64(tmem + 128 + mine, d);
+#pragma unroll
+        for (int c = 0; c < 64; c += 4) {
+          const float4 l = slot[kRows / 4 + c / 4];
+          x[c] *= d[c] - l.x;
+          x[c + 1] *= d[c + 1] - l.y;
+          x[c + 2] *= d[c + 2] - l.z;
+          x[c + 3] *= d[c + 3] - l.w;
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&st_empty[tile & 1]);
+        if (edge) {  // zero times an infinity that another row left
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c < c_lo || c >= c_hi) x[c] = 0.f;
+        }
+        store64(tmem + 128 + mine, x);
+        tc::fence_before_sync();
+        tc::mbar_arrive(ds_full);
+      }
+      if (!ok) break;
+      ok = warp_wait(done, turns & 1, abort_flag);
+      if (!ok) break;
+      ++turns;
+      tc::fence_after_sync();
+      const bool valid = key < e.seq_hi;
+      const int64_t col = (int64_t)(u % p.n_kv_heads) * p.head_dim;
+      store_acc<DP>(tmem + 256 + lane_base, half, p.dv + (int64_t)key * p.v_stride + col, p.head_dim, 1.f, valid);
+      store_acc<DP>(tmem + 384 + lane_base, half, p.dk + (int64_t)key * p.k_stride + col, p.head_dim, p.scale, valid);
+      tc::fence_before_sync();
+    }
+  }
+
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
+  if (warp == 8) tc::tmem_dealloc(tmem, 512);
+}
+
+template <int DP>
+int bwd(const Args& a, const Layout& l) {
+  const nat_attn_params& p = a.p;
+  const int group = p.n_heads / p.n_kv_heads, tq = kRows / group;
+  int sms = 0;
+  int s = require_sm100();
+  if (s == NAT_OK) s = sm_count(&sms);
+  CUtensorMap mq, mk, mv, mdo;
+  if (s == NAT_OK) s = make_map(&mq, a.q, p.head_dim, p.n_heads, a.cap, p.q_stride, group, tq);
+  if (s == NAT_OK) s = make_map(&mdo, a.dout, p.head_dim, p.n_heads, a.cap, p.o_stride, group, tq);
+  if (s == NAT_OK) s = make_map(&mk, a.k, p.head_dim, p.n_kv_heads, a.cap, p.k_stride, 1, kRows);
+  if (s == NAT_OK) s = make_map(&mv, a.v, p.head_dim, p.n_kv_heads, a.cap, p.v_stride, 1, kRows);
+  if (s != NAT_OK) return s;
+  const int smem = (int)BwdShape<DP>::kSmem;
+  NAT_CUDA(cudaFuncSetAttribute(attn_dq_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  NAT_CUDA(cudaFuncSetAttribute(attn_dkv_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  s = launch_bwd_prologue(a, l);
+  if (s != NAT_OK) return s;
+  BwdParams bp{};
+  bp.status = &head(a)->status;
+  bp.lse2 = lse2(a, l);
+  bp.delta = delta(a, l);
+  bp.dq = (__nv_bfloat16*)a.dq;
+  bp.dk = (__nv_bfloat16*)a.dk;
+  bp.dv = (__nv_bfloat16*)a.dv;
+  bp.q_stride = p.q_stride;
+  bp.k_stride = p.k_stride;
+  bp.v_stride = p.v_stride;
+  bp.n_heads = p.n_heads;
+  bp.n_kv_heads = p.n_kv_heads;
+  bp.group = group;
+  bp.tq = tq;
+  bp.head_dim = p.head_dim;
+  bp.scale = p.scale;
+  auto grid = [&](Plan which) { return (unsigned)min((int64_t)sms, l.entries[which] * p.n_kv_heads); };
+  bp.list = entries(a, l, kPlanDq);
+  bp.count = &head(a)->count[kPlanDq];
+  attn_dq_kernel<DP><<<grid(kPlanDq), 384, smem, a.stream>>>(mq, mk, mv, mdo, bp);
+  NAT_LAUNCH_CHECK("attn_dq_kernel");
+  bp.list = entries(a, l, kPlanDkv);
+  bp.count = &head(a)->count[kPlanDkv];
+  attn_dkv_kernel<DP><<<grid(kPlanDkv), 384, smem, a.stream>>>(mq, mk, mv, mdo, bp);
+  NAT_LAUNCH_CHECK("attn_dkv_kernel");
+  return NAT_OK;
+}
+
+}  // namespace
+
+int bf16_bwd(const Args& a, const Layout& l) {
+  return a.p.head_dim <= 64 ? bwd<64>(a, l) : bwd<128>(a, l);
+}
+
+}  // namespace attn
+}  // namespace nat

@@ -12,18 +12,13 @@ namespace {
 constexpr int kT = 32;         // tokens of a tile, queries and keys alike
 constexpr int kThreads = 128;  // four threads a row
 
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_f32(float x, float* p) { *p = x; }
-__device__ __forceinline__ void from_f32(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
-
 // Rows [lo, lo + 32) of one head into shared memory, zero outside [lo, hi) and past D.
-template <typename T, int DP>
-__device__ __forceinline__ void load_tile(float (*dst)[DP + 4], const T* base, int64_t stride,
+template <int DP>
+__device__ __forceinline__ void load_tile(float (*dst)[DP + 4], const float* base, int64_t stride,
                                           int head, int D, int lo, int hi) {
   for (int i = threadIdx.x; i < kT * DP; i += kThreads) {
     const int r = i / DP, c = i % DP;
-    dst[r][c] = (lo + r < hi && c < D) ? to_f32(base[(int64_t)(lo + r) * stride + (int64_t)head * D + c]) : 0.f;
+    dst[r][c] = (lo + r < hi && c < D) ? base[(int64_t)(lo + r) * stride + (int64_t)head * D + c] : 0.f;
   }
 }
 
@@ -60,14 +55,14 @@ __device__ __forceinline__ void accumulate(const float* w, const float (*m)[DP +
   }
 }
 
-template <typename T, int DP>
-__device__ __forceinline__ void store_row(T* row, int D, int quad, const float (&acc)[DP / 4], float f) {
+template <int DP>
+__device__ __forceinline__ void store_row(float* row, int D, int quad, const float (&acc)[DP / 4], float f) {
 #pragma unroll
   for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int c = (quad + 4 * i) * 4 + j;
-      if (c < D) from_f32(acc[4 * i + j] * f, row + c);
+      if (c < D) row[c] = acc[4 * i + j] * f;
     }
 }
 
@@ -78,7 +73,7 @@ struct Ptrs {
   nat_attn_params p;
 };
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads)
 f32_fwd_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict__ count) {
   if (blockIdx.x >= *count) return;
@@ -90,15 +85,15 @@ f32_fwd_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restric
   const Entry e = list[blockIdx.x];
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
   const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, row = e.lo + r;
-  load_tile<T, DP>(Q, (const T*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
+  load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
   float m = -INFINITY, l = 0.f, acc[DP / 4];
 #pragma unroll
   for (int i = 0; i < DP / 4; ++i) acc[i] = 0.f;
   const int last = min(e.lo + kT, e.seq_hi);
   for (int k0 = e.seq_lo; k0 < last; k0 += kT) {
     __syncthreads();
-    load_tile<T, DP>(K, (const T*)a.k, a.p.k_stride, kh, D, k0, last);
-    load_tile<T, DP>(V, (const T*)a.v, a.p.v_stride, kh, D, k0, last);
+    load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, k0, last);
+    load_tile<DP>(V, (const float*)a.v, a.p.v_stride, kh, D, k0, last);
     __syncthreads();
     float s[8];
     dots<DP>(Q[r], K, quad, s);
@@ -129,13 +124,13 @@ f32_fwd_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restric
     accumulate<DP>(P[r], V, 0, min(kT, row - k0 + 1), quad, acc);
   }
   if (row < e.seq_hi) {
-    store_row<T, DP>((T*)a.o + (int64_t)row * a.p.o_stride + (int64_t)h * D, D, quad, acc, 1.f / l);
+    store_row<DP>((float*)a.o + (int64_t)row * a.p.o_stride + (int64_t)h * D, D, quad, acc, 1.f / l);
     if (quad == 0) a.lse[(int64_t)row * a.p.n_heads + h] = m + logf(l);
   }
 }
 
 // dq of 32 queries of a head; also leaves delta = do . o for the keys' kernel.
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads)
 f32_dq_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict__ count) {
   if (blockIdx.x >= *count) return;
@@ -148,9 +143,9 @@ f32_dq_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict
   const Entry e = list[blockIdx.x];
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
   const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, row = e.lo + r;
-  load_tile<T, DP>(Q, (const T*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
-  load_tile<T, DP>(G, (const T*)a.dout, a.p.o_stride, h, D, e.lo, e.seq_hi);
-  load_tile<T, DP>(K, (const T*)a.out, a.p.o_stride, h, D, e.lo, e.seq_hi);
+  load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
+  load_tile<DP>(G, (const float*)a.dout, a.p.o_stride, h, D, e.lo, e.seq_hi);
+  load_tile<DP>(K, (const float*)a.out, a.p.o_stride, h, D, e.lo, e.seq_hi);
   __syncthreads();
   float delta = 0.f;
   for (int c = quad; c < DP; c += 4) delta = fmaf(G[r][c], K[r][c], delta);
@@ -165,8 +160,8 @@ f32_dq_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict
   const int last = min(e.lo + kT, e.seq_hi);
   for (int k0 = e.seq_lo; k0 < last; k0 += kT) {
     __syncthreads();
-    load_tile<T, DP>(K, (const T*)a.k, a.p.k_stride, kh, D, k0, last);
-    load_tile<T, DP>(V, (const T*)a.v, a.p.v_stride, kh, D, k0, last);
+    load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, k0, last);
+    load_tile<DP>(V, (const float*)a.v, a.p.v_stride, kh, D, k0, last);
     __syncthreads();
     float s[8], dp[8];
     dots<DP>(Q[r], K, quad, s);
@@ -180,11 +175,11 @@ f32_dq_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict
     accumulate<DP>(P[r], K, 0, min(kT, row - k0 + 1), quad, acc);
   }
   if (row < e.seq_hi)
-    store_row<T, DP>((T*)a.dq + (int64_t)row * a.p.q_stride + (int64_t)h * D, D, quad, acc, a.p.scale);
+    store_row<DP>((float*)a.dq + (int64_t)row * a.p.q_stride + (int64_t)h * D, D, quad, acc, a.p.scale);
 }
 
 // dk and dv of 32 keys of a key head: all query heads of its group, all later queries, in order.
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads)
 f32_dkv_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict__ count) {
   if (blockIdx.x >= *count) return;
@@ -198,16 +193,16 @@ f32_dkv_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restric
   const Entry e = list[blockIdx.x];
   const int D = a.p.head_dim, kh = blockIdx.y, group = a.p.n_heads / a.p.n_kv_heads;
   const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, key = e.lo + r;
-  load_tile<T, DP>(K, (const T*)a.k, a.p.k_stride, kh, D, e.lo, e.seq_hi);
-  load_tile<T, DP>(V, (const T*)a.v, a.p.v_stride, kh, D, e.lo, e.seq_hi);
+  load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, e.lo, e.seq_hi);
+  load_tile<DP>(V, (const float*)a.v, a.p.v_stride, kh, D, e.lo, e.seq_hi);
   float dk[DP / 4], dv[DP / 4];
 #pragma unroll
   for (int i = 0; i < DP / 4; ++i) dk[i] = dv[i] = 0.f;
   for (int h = kh * group; h < (kh + 1) * group; ++h)
     for (int q0 = e.lo; q0 < e.seq_hi; q0 += kT) {
       __syncthreads();
-      load_tile<T, DP>(Q, (const T*)a.q, a.p.q_stride, h, D, q0, e.seq_hi);
-      load_tile<T, DP>(G, (const T*)a.dout, a.p.o_stride, h, D, q0, e.seq_hi);
+      load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, q0, e.seq_hi);
+      load_tile<DP>(G, (const float*)a.dout, a.p.o_stride, h, D, q0, e.seq_hi);
       __syncthreads();
       float s[8], dp[8];
       dots<DP>(K[r], Q, quad, s);
@@ -229,8 +224,8 @@ f32_dkv_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restric
       accumulate<DP>(S[r], Q, max(0, key - q0), kT, quad, dk);
     }
   if (key < e.seq_hi) {
-    store_row<T, DP>((T*)a.dk + (int64_t)key * a.p.k_stride + (int64_t)kh * D, D, quad, dk, a.p.scale);
-    store_row<T, DP>((T*)a.dv + (int64_t)key * a.p.v_stride + (int64_t)kh * D, D, quad, dv, 1.f);
+    store_row<DP>((float*)a.dk + (int64_t)key * a.p.k_stride + (int64_t)kh * D, D, quad, dk, a.p.scale);
+    store_row<DP>((float*)a.dv + (int64_t)key * a.p.v_stride + (int64_t)kh * D, D, quad, dv, 1.f);
   }
 }
 
@@ -250,35 +245,32 @@ int launch(K kernel, size_t smem, const Args& a, const Layout& l, Plan which, in
   return NAT_OK;
 }
 
-template <typename T, int DP>
+template <int DP>
 int fwd(const Args& a, const Layout& l) {
-  int s = launch_plan(a, l, kPlanFwd, true);
+  int s = launch_plan(a, l, kPlanFwd);
   if (s != NAT_OK) return s;
   const size_t smem = (3 * kT * (DP + 4) + kT * (kT + 1)) * sizeof(float);
-  return launch(f32_fwd_kernel<T, DP>, smem, a, l, kPlanFwd, a.p.n_heads, "f32_fwd_kernel");
+  return launch(f32_fwd_kernel<DP>, smem, a, l, kPlanFwd, a.p.n_heads, "f32_fwd_kernel");
 }
 
-template <typename T, int DP>
+template <int DP>
 int bwd(const Args& a, const Layout& l) {
-  int s = launch_plan(a, l, kPlanDq, true);
-  if (s == NAT_OK) s = launch_plan(a, l, kPlanDkv, false);
+  int s = launch_plan(a, l, kPlanDq);
+  if (s == NAT_OK) s = launch_plan(a, l, kPlanDkv);
   if (s != NAT_OK) return s;
   const size_t smem = (4 * kT * (DP + 4) + 2 * kT * (kT + 1)) * sizeof(float);
-  s = launch(f32_dq_kernel<T, DP>, smem, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
+  s = launch(f32_dq_kernel<DP>, smem, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
   if (s != NAT_OK) return s;
-  return launch(f32_dkv_kernel<T, DP>, smem, a, l, kPlanDkv, a.p.n_kv_heads, "f32_dkv_kernel");
+  return launch(f32_dkv_kernel<DP>, smem, a, l, kPlanDkv, a.p.n_kv_heads, "f32_dkv_kernel");
 }
 
 }  // namespace
 
 int f32_fwd(const Args& a, const Layout& l) {
-  return a.p.head_dim <= 64 ? fwd<float, 64>(a, l) : fwd<float, 128>(a, l);
+  return a.p.head_dim <= 64 ? fwd<64>(a, l) : fwd<128>(a, l);
 }
 int f32_bwd(const Args& a, const Layout& l) {
-  return a.p.head_dim <= 64 ? bwd<float, 64>(a, l) : bwd<float, 128>(a, l);
-}
-int bf16_bwd(const Args& a, const Layout& l) {
-  return a.p.head_dim <= 64 ? bwd<__nv_bfloat16, 64>(a, l) : bwd<__nv_bfloat16, 128>(a, l);
+  return a.p.head_dim <= 64 ? bwd<64>(a, l) : bwd<128>(a, l);
 }
 
 }  // namespace attn

@@ -7,6 +7,7 @@
 namespace nat {
 namespace attn {
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRows = 128;                          // rows of every operand tile
 constexpr uint32_t kPanel = kRows * 128;            // 128 rows of 64 bfloat16 columns, 128-byte swizzle
 
@@ -101,6 +102,12 @@ __device__ __forceinline__ uint64_t desc_kmajor(uint32_t tile, int kk) {
 __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t tile, int kk) {
   return tc::smem_desc_sw128(tile + (uint32_t)kk * 2048, kPanel, 1024);
 }
+
+// Tensor map of [cap, heads, D] bfloat16 with a token stride: boxes of 64 columns x box_heads x
+// box_tokens, zero outside.
+int make_map(CUtensorMap* map, const void* base, int D, int heads, int64_t cap, int64_t stride,
+             int box_heads, int box_tokens);
+int sm_count(int* n);
 
 // Zeroes rows [first, 128) of a tile of NP panels that TMA has finished writing (one warp), for
 // the tensor cores to read: the rows belong to another sequence, or to none, and a weight of
