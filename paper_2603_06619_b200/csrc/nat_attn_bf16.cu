@@ -172,7 +172,6 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   } else if (warp == 8) {
     // ---------------------------------------------------------------- MMAs
     if (lane == 0) {
-      constexpr uint32_t kIdescS = tc::instr_desc_bf16(128, 128, 0, 0);
       constexpr uint32_t kIdescO = tc::instr_desc_bf16(128, DP, 0, 1);
       const int ksteps = (p.head_dim + 15) / 16;
       const uint32_t q_addr = tc::smem_u32(smem), ring_addr = tc::smem_u32(ring);
@@ -183,10 +182,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         tc::fence_after_sync();
       };
       auto scores = [&](int t, uint32_t k_item) {
-        const uint32_t a = q_addr + t * R::kTile, b = ring_addr + (k_item % kNS) * R::kTile;
-#pragma unroll 1
-        for (int kk = 0; kk < ksteps; ++kk)
-          tc::umma_bf16(tmem + t * 128, desc_kmajor(a, kk), desc_kmajor(b, kk), kIdescS, kk > 0);
+        product_kk<DP>(tmem + t * 128, q_addr + t * R::kTile, ring_addr + (k_item % kNS) * R::kTile, ksteps);
         tc::umma_commit(&s_full[t]);
       };
       for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
@@ -216,11 +212,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             ++p_turns[t];
             if (!ok) break;
             tc::fence_after_sync();
-            const uint32_t b = ring_addr + (v_item % kNS) * R::kTile;
-#pragma unroll 1
+            const uint32_t b = desc_mnmajor(ring_addr + (v_item % kNS) * R::kTile);
+#pragma unroll
             for (int kk = 0; kk < 8; ++kk)
-              umma_ts_bf16(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, desc_mnmajor(b, kk), kIdescO,
-                           j > 0 || kk > 0);
+              umma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, b + step_mnmajor(kk), kIdescO, j > 0 || kk > 0);
             tc::umma_commit(&o_done[t]);
             if (j + 1 < w.nk[t]) {
               if (!have_k) take(k_next), have_k = true;

@@ -71,7 +71,7 @@ __device__ __forceinline__ void store64(uint32_t addr, const float (&x)[64]) {
 }
 
 // Where step kk (16 of the contraction) of such an operand lies.
-__device__ __forceinline__ uint32_t half_cols(int kk) { return (uint32_t)(kk < 4 ? kk * 8 : 64 + (kk - 4) * 8); }
+constexpr __device__ uint32_t half_cols(int kk) { return (uint32_t)(kk < 4 ? kk * 8 : 64 + (kk - 4) * 8); }
 
 // D columns [half * DP/2, ...) of an accumulator row, times f, to global memory.
 template <int DP>
@@ -220,7 +220,6 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     ld.land(qdo_full, turns);
   } else if (warp == 8) {
     if (lane == 0) {
-      constexpr uint32_t kIdescS = tc::instr_desc_bf16(128, 128, 0, 0);
       constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
       const int ksteps = (p.head_dim + 15) / 16;
       const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile, ring_addr = tc::smem_u32(ring);
@@ -231,10 +230,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         tc::fence_after_sync();
       };
       auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
-        const uint32_t b = ring_addr + (i % kNS) * R::kTile;
-#pragma unroll 1
-        for (int kk = 0; kk < ksteps; ++kk)
-          tc::umma_bf16(d, desc_kmajor(a, kk), desc_kmajor(b, kk), kIdescS, kk > 0);
+        product_kk<DP>(d, a, ring_addr + (i % kNS) * R::kTile, ksteps);
         tc::umma_commit(bar);
       };
       for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
@@ -266,10 +262,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             tc::umma_commit(&empty[(item + 3) % kNS]);
             if (j + 2 == n) tc::umma_commit(qdo_empty);
           }
-          const uint32_t b = ring_addr + (item % kNS) * R::kTile, a = tmem + (tile & 1) * 128;
-#pragma unroll 1
+          const uint32_t b = desc_mnmajor(ring_addr + (item % kNS) * R::kTile), a = tmem + (tile & 1) * 128;
+#pragma unroll
           for (int kk = 0; kk < 8; ++kk)
-            umma_ts_bf16(tmem + 384, a + half_cols(kk), desc_mnmajor(b, kk), kIdescD, j > 0 || kk > 0);
+            umma_ts(tmem + 384, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, j > 0 || kk > 0);
           tc::umma_commit(&empty[item % kNS]);
         }
         if (ok) tc::umma_commit(dq_done);
@@ -451,7 +447,6 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
   } else if (warp == 8) {
     if (lane == 0) {
-      constexpr uint32_t kIdescS = tc::instr_desc_bf16(128, 128, 0, 0);
       constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
       const int ksteps = (p.head_dim + 15) / 16;
       const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile, ring_addr = tc::smem_u32(ring);
@@ -462,17 +457,14 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         tc::fence_after_sync();
       };
       auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
-        const uint32_t b = ring_addr + (i % kNS) * R::kTile;
-#pragma unroll 1
-        for (int kk = 0; kk < ksteps; ++kk)
-          tc::umma_bf16(d, desc_kmajor(a, kk), desc_kmajor(b, kk), kIdescS, kk > 0);
+        product_kk<DP>(d, a, ring_addr + (i % kNS) * R::kTile, ksteps);
         tc::umma_commit(bar);
       };
       auto accumulate = [&](uint32_t d, uint32_t a, uint32_t i, bool add) {
-        const uint32_t b = ring_addr + (i % kNS) * R::kTile;
-#pragma unroll 1
+        const uint32_t b = desc_mnmajor(ring_addr + (i % kNS) * R::kTile);
+#pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          umma_ts_bf16(d, a + half_cols(kk), desc_mnmajor(b, kk), kIdescD, add || kk > 0);
+          umma_ts(d, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, add || kk > 0);
         tc::umma_commit(&empty[i % kNS]);
       };
       for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {

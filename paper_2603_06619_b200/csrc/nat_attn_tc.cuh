@@ -11,17 +11,62 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRows = 128;                          // rows of every operand tile
 constexpr uint32_t kPanel = kRows * 128;            // 128 rows of 64 bfloat16 columns, 128-byte swizzle
 
-// D[tmem] (+)= A[tmem] * B[smem], A of bf16 pairs packed along K into 32-bit columns.
-__device__ __forceinline__ void umma_ts_bf16(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc,
-                                             uint32_t idesc, uint32_t accumulate) {
+// Descriptors of 128-byte-swizzled operand tiles, split in words: the upper word (stride offset
+// 1024 bytes, version 1, swizzle mode 2) is the same for all, the lower one holds the address and
+// the leading offset.  A step along the contraction is then one 32-bit addition: one thread
+// issues every MMA, and building 64-bit descriptors for each would take it longer than the MMA.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+
+// A tile whose contiguous columns are the contraction: step kk covers 16 of them.
+__device__ __forceinline__ uint32_t desc_kmajor(uint32_t tile) { return (tile >> 4) | (1u << 16); }
+constexpr __host__ __device__ uint32_t step_kmajor(int kk) {
+  return (uint32_t)(kk >> 2) * (kPanel >> 4) + (uint32_t)(kk & 3) * 2u;
+}
+// A tile whose rows are the contraction: step kk covers 16 of them.
+__device__ __forceinline__ uint32_t desc_mnmajor(uint32_t tile) {
+  return (tile >> 4) | ((kPanel >> 4) << 16);
+}
+constexpr __host__ __device__ uint32_t step_mnmajor(int kk) { return (uint32_t)kk * (2048u >> 4); }
+
+// D[tmem] (+)= A[smem] * B[smem]
+__device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
+                                        bool accumulate) {
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
+      ".reg .b64 a, b;\n"
       "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "mov.b64 a, {%1, %5};\n"
+      "mov.b64 b, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
       "}\n" ::"r"(tmem_d),
-      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kDescHi)
       : "memory");
+}
+
+// D[tmem] (+)= A[tmem] * B[smem], A of bf16 pairs packed along K into 32-bit columns.
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t idesc,
+                                        bool accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b64 b;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "mov.b64 b, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n"
+      "}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kDescHi)
+      : "memory");
+}
+
+// S[tmem] = A B^T of two tiles with D columns each (DP at most).
+template <int DP>
+__device__ __forceinline__ void product_kk(uint32_t tmem_d, uint32_t a_tile, uint32_t b_tile, int ksteps) {
+  constexpr uint32_t kIdesc = tc::instr_desc_bf16(128, 128, 0, 0);
+  const uint32_t a = desc_kmajor(a_tile), b = desc_kmajor(b_tile);
+#pragma unroll
+  for (int kk = 0; kk < DP / 16; ++kk)
+    if (kk < ksteps) umma_ss(tmem_d, a + step_kmajor(kk), b + step_kmajor(kk), kIdesc, kk > 0);
 }
 
 // 32 consecutive 32-bit columns of this thread's lane; complete after tmem_st_wait().
@@ -92,15 +137,6 @@ __device__ __forceinline__ void regs_inc() {
 template <int N>
 __device__ __forceinline__ void regs_dec() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-// Product of two K-major tiles (rows x D each): step `kk` covers 16 of D's columns.
-__device__ __forceinline__ uint64_t desc_kmajor(uint32_t tile, int kk) {
-  return tc::smem_desc_sw128(tile + (uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32, 16, 1024);
-}
-// A tile whose rows are the contraction: step `kk` covers 16 rows, D is the contiguous dimension.
-__device__ __forceinline__ uint64_t desc_mnmajor(uint32_t tile, int kk) {
-  return tc::smem_desc_sw128(tile + (uint32_t)kk * 2048, kPanel, 1024);
 }
 
 // Tensor map of [cap, heads, D] bfloat16 with a token stride: boxes of 64 columns x box_heads x
