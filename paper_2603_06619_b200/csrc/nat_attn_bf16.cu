@@ -74,11 +74,12 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* ring = smem + 2 * R::kTile;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + kNS * R::kTile);
-  uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *p_full = bars + 6, *o_done = bars + 8;
-  uint64_t *raw = bars + 10, *drain = bars + 11, *full = bars + 12, *empty = bars + 12 + kNS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 2 * kNS);
+  uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *o_done = bars + 6, *raw = bars + 8;
+  uint64_t *drain = bars + 9, *p_full = bars + 10;  // p_full [row tile][half of the keys]
+  uint64_t *full = bars + 14, *empty = bars + 14 + kNS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * kNS);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
 
   if (threadIdx.x == 0) {
@@ -86,7 +87,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       tc::mbar_init(&q_full[t], 1);
       tc::mbar_init(&q_empty[t], 1);
       tc::mbar_init(&s_full[t], 1);
-      tc::mbar_init(&p_full[t], 128);
+      tc::mbar_init(&p_full[2 * t], 128);
+      tc::mbar_init(&p_full[2 * t + 1], 128);
       tc::mbar_init(&o_done[t], 1);
     }
     tc::mbar_init(raw, 1);
@@ -105,7 +107,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = uniform(*tmem_slot);
 
   // 168 registers a thread at launch: the softmax warpgroups, which hold a row of scores, take
   // some of the third's (2 x 192 + 120 = 3 x 168)
@@ -171,70 +173,75 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
   } else if (warp == 8) {
     // ---------------------------------------------------------------- MMAs
-    if (lane == 0) {
-      constexpr uint32_t kIdescO = tc::instr_desc_bf16(128, DP, 0, 1);
-      const int ksteps = (p.head_dim + 15) / 16;
-      const uint32_t q_addr = tc::smem_u32(smem), ring_addr = tc::smem_u32(ring);
-      uint32_t item = 0, q_turns[2] = {0, 0}, p_turns[2] = {0, 0};
-      bool ok = true;
-      auto take = [&](uint32_t i) {
-        ok = ok && tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, abort_flag);
-        tc::fence_after_sync();
-      };
-      auto scores = [&](int t, uint32_t k_item) {
+    constexpr uint32_t kIdescO = tc::instr_desc_bf16(128, DP, 0, 1);
+    const int ksteps = (p.head_dim + 15) / 16;
+    const uint32_t q_addr = tc::smem_u32(smem), ring_addr = tc::smem_u32(ring);
+    uint32_t item = 0, q_turns = 0, p_turns = 0;  // bit t of q_turns, p_turns: the next phase of row tile t
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && warp_wait(bar, parity & 1, abort_flag);
+      tc::fence_after_sync();
+    };
+    auto scores = [&](int t, uint32_t k_item, bool last) {
+      if (elect_one()) {
         product_kk<DP>(tmem + t * 128, q_addr + t * R::kTile, ring_addr + (k_item % kNS) * R::kTile, ksteps);
         tc::umma_commit(&s_full[t]);
-      };
-      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-        const Unit w = unit_of(p, u);
-        const int n = max(w.nk[0], w.nk[1]);
-        // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
-        take(item);
-        for (int t = 0; ok && t < 2; ++t)
-          if (w.nk[t]) {
-            ok = tc::mbar_wait(&q_full[t], q_turns[t] & 1, abort_flag);
-            ++q_turns[t];
-            tc::fence_after_sync();
-            if (!ok) break;
-            scores(t, item);
-            if (w.nk[t] == 1) tc::umma_commit(&q_empty[t]);
-          }
-        if (!ok) break;
-        tc::umma_commit(&empty[item % kNS]);
-        for (int j = 0; ok && j < n; ++j) {
-          const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
-          bool have_v = false, have_k = false;
-#pragma unroll 1
-          for (int t = 0; ok && t < 2; ++t) {
-            if (j >= w.nk[t]) continue;
-            if (!have_v) take(v_item), have_v = true;
-            ok = ok && tc::mbar_wait(&p_full[t], p_turns[t] & 1, abort_flag);
-            ++p_turns[t];
-            if (!ok) break;
-            tc::fence_after_sync();
-            const uint32_t b = desc_mnmajor(ring_addr + (v_item % kNS) * R::kTile);
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk)
-              umma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, b + step_mnmajor(kk), kIdescO, j > 0 || kk > 0);
-            tc::umma_commit(&o_done[t]);
-            if (j + 1 < w.nk[t]) {
-              if (!have_k) take(k_next), have_k = true;
-              if (!ok) break;
-              scores(t, k_next);
-              if (j + 2 == w.nk[t]) tc::umma_commit(&q_empty[t]);
-            }
-          }
-          if (!ok) break;
-          tc::umma_commit(&empty[v_item % kNS]);
-          if (have_k) tc::umma_commit(&empty[k_next % kNS]);
-        }
-        item += 2 * n;
+        if (last) tc::umma_commit(&q_empty[t]);
       }
-      // every MMA has to have finished before the tensor memory is given back
-      tc::umma_commit(drain);
-      uint32_t never = 0u;
-      tc::mbar_wait(drain, 0, &never);
+      __syncwarp();
+    };
+    auto release = [&](uint32_t i) {
+      if (elect_one()) tc::umma_commit(&empty[i % kNS]);
+      __syncwarp();
+    };
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit w = unit_of(p, u);
+      const int n = max(w.nk[0], w.nk[1]);
+      // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
+      wait(&full[item % kNS], item / kNS);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (w.nk[t]) {
+          wait(&q_full[t], q_turns >> t);
+          q_turns ^= 1u << t;
+          if (!ok) break;
+          scores(t, item, w.nk[t] == 1);
+        }
+      if (!ok) break;
+      release(item);
+      for (int j = 0; ok && j < n; ++j) {
+        const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
+        wait(&full[v_item % kNS], v_item / kNS);
+        if (j + 1 < n) wait(&full[k_next % kNS], k_next / kNS);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (j >= w.nk[t] || !ok) continue;
+          const uint32_t b = desc_mnmajor(ring_addr + (v_item % kNS) * R::kTile);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            wait(&p_full[2 * t + half], p_turns >> t);
+            if (!ok) break;
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                umma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, b + step_mnmajor(kk), kIdescO, j > 0 || kk > 0);
+              if (half == 1) tc::umma_commit(&o_done[t]);
+            }
+            __syncwarp();
+          }
+          p_turns ^= 1u << t;
+          if (ok && j + 1 < w.nk[t]) scores(t, k_next, j + 2 == w.nk[t]);
+        }
+        if (!ok) break;
+        release(v_item);
+        if (j + 1 < n) release(k_next);
+      }
+      item += 2 * n;
     }
+    // every MMA has to have finished before the tensor memory is given back
+    if (elect_one()) tc::umma_commit(drain);
+    uint32_t never = 0u;
+    tc::mbar_wait(drain, 0, &never);
   }
   } else {
     // ------------------------------------------------------------- softmax
@@ -281,7 +288,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
         float top[4] = {m, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], s[c]);
+        for (int c = 0; c < 128; c += 8)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[i] = max3(top[i], s[c + 2 * i], s[c + 2 * i + 1]);
         const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         float base = m;
         if (j == 0) {
@@ -296,36 +305,39 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             if (grow) m = now;
             l *= f;
 #pragma unroll
-            for (int c = 0; c < DP / 8; ++c) {  // few columns at a time: the scores stay in registers
-              uint32_t o[8];
-              tmem_ld8(o_addr + c * 8, o);
+            for (int c = 0; c < DP / 16; ++c) {  // few columns at a time: the scores stay in registers
+              uint32_t o[16];
+              tmem_ld16(o_addr + c * 16, o);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st8(o_addr + c * 8, o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st16(o_addr + c * 16, o);
             }
             base = m;
           }
         }
         // a row whose scores are all minus infinity so far has no maximum to subtract
         const float shift = base == -INFINITY ? 0.f : base * sc;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const float2 scale2 = {sc, sc}, shift2 = {-shift, -shift};
+        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+        // P goes out in halves: the first one's product runs during the second one's exponentials
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t pk[32];
 #pragma unroll
           for (int c = 0; c < 32; ++c) {
-            const float a = ex2(fmaf(s[half * 64 + 2 * c], sc, -shift));
-            const float b = ex2(fmaf(s[half * 64 + 2 * c + 1], sc, -shift));
-            sum[(2 * c) & 3] += a;
-            sum[(2 * c + 1) & 3] += b;
-            pk[c] = bf16_pair(a, b);
+            float2 e = fma2({s[half * 64 + 2 * c], s[half * 64 + 2 * c + 1]}, scale2, shift2);
+            e.x = ex2(e.x);
+            e.y = ex2(e.y);
+            sum[c & 1] = add2(sum[c & 1], e);
+            pk[c] = bf16_pair(e.x, e.y);
           }
           tmem_st32(s_addr + half * 32, pk);
+          tmem_st_wait();
+          tc::fence_before_sync();
+          tc::mbar_arrive(&p_full[2 * t + half]);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_st_wait();
-        tc::fence_before_sync();
-        tc::mbar_arrive(&p_full[t]);
+        sum[0] = add2(sum[0], sum[1]);
+        l += sum[0].x + sum[0].y;
       }
       if (!ok) break;
       if (nk == 0) continue;

@@ -49,19 +49,8 @@ __device__ __forceinline__ uint8_t* tile_base(uint8_t* raw, uint32_t slack, bool
   return raw + (up - at);
 }
 
-// 64 columns of the thread's row in tensor memory.
-__device__ __forceinline__ void load64(uint32_t addr, float (&x)[64]) {
-  uint32_t r[64];
-  tc::tmem_ld32_issue(addr, r);
-  tc::tmem_ld32_issue(addr + 32, r + 32);
-  tc::tmem_ld_wait(r);
-  tc::tmem_ld_pin(r + 32);
-#pragma unroll
-  for (int c = 0; c < 64; ++c) x[c] = __uint_as_float(r[c]);
-}
-
-// The same as bf16 pairs into the first 32 of the 64 columns they came from: each half of the
-// threads stays in its own columns.
+// 64 values as bf16 pairs into the first 32 of the 64 columns that they came from: each half of
+// the threads stays in its own columns.
 __device__ __forceinline__ void store64(uint32_t addr, const float (&x)[64]) {
   uint32_t r[32];
 #pragma unroll
@@ -294,13 +283,13 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         tc::fence_after_sync();
         const uint32_t s_addr = tmem + (tile & 1) * 128 + mine;
         float x[64], d[64];
-        load64(s_addr, x);
+        tmem_ld64(s_addr, x);
 #pragma unroll
         for (int c = 0; c < 64; ++c) x[c] = ex2(fmaf(x[c], sc, -lse2));
         ok = warp_wait(dp_full, tile & 1, abort_flag);
         if (!ok) break;
         tc::fence_after_sync();
-        load64(tmem + 256 + mine, d);
+        tmem_ld64(tmem + 256 + mine, d);
 #pragma unroll
         for (int c = 0; c < 64; ++c) x[c] *= d[c] - delta;
         const int kv0 = e.seq_lo + j * kRows;
@@ -523,7 +512,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (!ok) break;
         tc::fence_after_sync();
         float x[64], d[64];
-        load64(tmem + mine, x);
+        tmem_ld64(tmem + mine, x);
 #pragma unroll
         for (int c = 0; c < 64; c += 4) {
           const float4 l = slot[c / 4];
@@ -546,7 +535,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         ok = warp_wait(dp_full, tile & 1, abort_flag);
         if (!ok) break;
         tc::fence_after_sync();
-        load64(tmem + 128 + mine, d);
+        tmem_ld64(tmem + 128 + mine, d);
 #pragma unroll
         for (int c = 0; c < 64; c += 4) {
           const float4 l = slot[kRows / 4 + c / 4];

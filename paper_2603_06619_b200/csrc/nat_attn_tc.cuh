@@ -59,10 +59,10 @@ __device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32
       : "memory");
 }
 
-// S[tmem] = A B^T of two tiles with D columns each (DP at most).
-template <int DP>
+// S[tmem] = A B^T of two tiles with D columns each (DP at most), of N rows of B.
+template <int DP, int N = 128>
 __device__ __forceinline__ void product_kk(uint32_t tmem_d, uint32_t a_tile, uint32_t b_tile, int ksteps) {
-  constexpr uint32_t kIdesc = tc::instr_desc_bf16(128, 128, 0, 0);
+  constexpr uint32_t kIdesc = tc::instr_desc_bf16(128, N, 0, 0);
   const uint32_t a = desc_kmajor(a_tile), b = desc_kmajor(b_tile);
 #pragma unroll
   for (int kk = 0; kk < DP / 16; ++kk)
@@ -83,20 +83,36 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
       : "memory");
 }
 
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]),
-               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
-               : "memory");
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
 }
 
-// Eight columns, complete on return.
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
+// 16 columns, complete on return.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+
+// 64 columns, complete on return.
+__device__ __forceinline__ void tmem_ld64(uint32_t addr, float (&x)[64]) {
+  uint32_t r[64];
+  tc::tmem_ld32_issue(addr, r);
+  tc::tmem_ld32_issue(addr + 32, r + 32);
+  tc::tmem_ld_wait(r);
+  tc::tmem_ld_pin(r + 32);
+#pragma unroll
+  for (int c = 0; c < 64; ++c) x[c] = __uint_as_float(r[c]);
 }
 
 __device__ __forceinline__ void tmem_st_wait() {
@@ -110,6 +126,40 @@ __device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap
       " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_dst),
       "l"(map), "r"(tc::smem_u32(bar)), "r"(x), "r"(y), "r"(z)
       : "memory");
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n"
+      ".reg .b64 a, b, c, d;\n"
+      "mov.b64 a, {%2, %3};\n"
+      "mov.b64 b, {%4, %5};\n"
+      "mov.b64 c, {%6, %7};\n"
+      "fma.rn.f32x2 d, a, b, c;\n"
+      "mov.b64 {%0, %1}, d;\n"
+      "}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n"
+      ".reg .b64 a, b, d;\n"
+      "mov.b64 a, {%2, %3};\n"
+      "mov.b64 b, {%4, %5};\n"
+      "add.rn.f32x2 d, a, b;\n"
+      "mov.b64 {%0, %1}, d;\n"
+      "}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -137,6 +187,25 @@ __device__ __forceinline__ void regs_inc() {
 template <int N>
 __device__ __forceinline__ void regs_dec() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// One lane of a converged warp.  Together with a warp index and a tensor-memory address that the
+// compiler knows to be the same in all lanes (uniform()) this keeps the operands of the MMAs in
+// uniform registers: moved there one by one they cost 75 cycles an MMA, more than its 64.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "elect.sync _|p, 0xffffffff;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(one));
+  return one != 0;
+}
+template <typename T>
+__device__ __forceinline__ T uniform(T x) {
+  return __shfl_sync(0xFFFFFFFFu, x, 0);
 }
 
 // Tensor map of [cap, heads, D] bfloat16 with a token stride: boxes of 64 columns x box_heads x
