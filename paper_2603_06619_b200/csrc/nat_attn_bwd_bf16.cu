@@ -149,7 +149,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   uint64_t *dq_done = bars + 6, *raw = bars + 7, *drain = bars + 8, *full = bars + 9, *empty = bars + 9 + kNS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9 + 2 * kNS);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
 
   if (threadIdx.x == 0) {
@@ -176,7 +176,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = *tmem_slot;  // S/dS in two buffers, dP, dQ: 128 columns each
+  const uint32_t tmem = uniform(*tmem_slot);  // S/dS in two buffers, dP, dQ: 128 columns each
   // tiles of keys of a list entry
   auto tiles_of = [&](const Entry& e) { return (min(e.lo + p.tq, e.seq_hi) - e.seq_lo + kRows - 1) / kRows; };
 
@@ -208,61 +208,68 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     }
     ld.land(qdo_full, turns);
   } else if (warp == 8) {
-    if (lane == 0) {
-      constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
-      const int ksteps = (p.head_dim + 15) / 16;
-      const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile, ring_addr = tc::smem_u32(ring);
-      uint32_t item = 0, turns = 0, tile = 0;  // `tile` numbers the key tiles of the block
-      bool ok = true;
-      auto take = [&](uint32_t i) {
-        ok = ok && tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, abort_flag);
-        tc::fence_after_sync();
-      };
-      auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
-        product_kk<DP>(d, a, ring_addr + (i % kNS) * R::kTile, ksteps);
-        tc::umma_commit(bar);
-      };
-      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-        const Entry e = p.list[u / p.n_kv_heads];
-        const int n = tiles_of(e);
-        ok = tc::mbar_wait(qdo_full, turns & 1, abort_flag);
-        ++turns;
-        take(item);  // items K_0 V_0 K_1 V_1 ...
+    constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
+    const int ksteps = (p.head_dim + 15) / 16;
+    const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile, ring_addr = tc::smem_u32(ring);
+    uint32_t item = 0, turns = 0, tile = 0;  // `tile` numbers the key tiles of the block
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && warp_wait(bar, parity & 1, abort_flag);
+      tc::fence_after_sync();
+    };
+    auto take = [&](uint32_t i) { wait(&full[i % kNS], i / kNS); };
+    auto scores = [&](uint32_t i, uint32_t buffer) {  // S = Q K^T
+      if (!ok) return;
+      if (elect_one()) {
+        product_kk<DP>(tmem + buffer * 128, q_addr, ring_addr + (i % kNS) * R::kTile, ksteps);
+        tc::umma_commit(&s_full[buffer]);
+      }
+      __syncwarp();
+    };
+    auto slopes = [&](uint32_t i, bool last) {  // dP = dO V^T, the last reader of V, and of Q and dO
+      if (!ok) return;
+      if (elect_one()) {
+        product_kk<DP>(tmem + 256, do_addr, ring_addr + (i % kNS) * R::kTile, ksteps);
+        tc::umma_commit(dp_full);
+        tc::umma_commit(&empty[i % kNS]);
+        if (last) tc::umma_commit(qdo_empty);
+      }
+      __syncwarp();
+    };
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int n = tiles_of(e);
+      wait(qdo_full, turns);
+      ++turns;
+      take(item);  // items K_0 V_0 K_1 V_1 ...
+      scores(item, tile & 1);
+      take(item + 1);
+      slopes(item + 1, n == 1);
+      for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
+        if (j + 1 < n) {
+          take(item + 2);
+          scores(item + 2, (tile + 1) & 1);
+        }
+        wait(ds_full, tile);
+        if (j + 1 < n) {
+          take(item + 3);
+          slopes(item + 3, j + 2 == n);
+        }
         if (!ok) break;
-        product(tmem + (tile & 1) * 128, q_addr, item, &s_full[tile & 1]);
-        take(item + 1);
-        if (!ok) break;
-        product(tmem + 256, do_addr, item + 1, dp_full);
-        tc::umma_commit(&empty[(item + 1) % kNS]);
-        if (n == 1) tc::umma_commit(qdo_empty);
-        for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
-          if (j + 1 < n) {
-            take(item + 2);
-            if (!ok) break;
-            product(tmem + ((tile + 1) & 1) * 128, q_addr, item + 2, &s_full[(tile + 1) & 1]);
-          }
-          ok = tc::mbar_wait(ds_full, tile & 1, abort_flag);
-          if (!ok) break;
-          tc::fence_after_sync();
-          if (j + 1 < n) {
-            take(item + 3);
-            if (!ok) break;
-            product(tmem + 256, do_addr, item + 3, dp_full);
-            tc::umma_commit(&empty[(item + 3) % kNS]);
-            if (j + 2 == n) tc::umma_commit(qdo_empty);
-          }
+        if (elect_one()) {
           const uint32_t b = desc_mnmajor(ring_addr + (item % kNS) * R::kTile), a = tmem + (tile & 1) * 128;
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)
             umma_ts(tmem + 384, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, j > 0 || kk > 0);
           tc::umma_commit(&empty[item % kNS]);
+          if (j + 1 == n) tc::umma_commit(dq_done);
         }
-        if (ok) tc::umma_commit(dq_done);
+        __syncwarp();
       }
-      tc::umma_commit(drain);
-      uint32_t never = 0u;
-      tc::mbar_wait(drain, 0, &never);
     }
+    if (elect_one()) tc::umma_commit(drain);
+    uint32_t never = 0u;
+    tc::mbar_wait(drain, 0, &never);
   } else if (warp < 8) {
     const int half = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16, mine = lane_base + half * 64;
@@ -343,7 +350,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint64_t *st_empty = bars + 11, *full = bars + 13, *empty = bars + 13 + kNS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 13 + 2 * kNS);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
   const int q_rows = p.group * p.tq;
 
@@ -381,7 +388,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = *tmem_slot;  // S'/P', dP'/dS', dV, dK: 128 columns each
+  const uint32_t tmem = uniform(*tmem_slot);  // S'/P', dP'/dS', dV, dK: 128 columns each
   // tiles of queries of a list entry: they start at the key tile's first token
   auto tiles_of = [&](const Entry& e) { return (e.seq_hi - e.lo + p.tq - 1) / p.tq; };
 
@@ -435,67 +442,67 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     }
   } else if (warp == 8) {
-    if (lane == 0) {
-      constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
-      const int ksteps = (p.head_dim + 15) / 16;
-      const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile, ring_addr = tc::smem_u32(ring);
-      uint32_t item = 0, turns = 0, tile = 0;
-      bool ok = true;
-      auto take = [&](uint32_t i) {
-        ok = ok && tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, abort_flag);
-        tc::fence_after_sync();
-      };
-      auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
+    constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
+    const int ksteps = (p.head_dim + 15) / 16;
+    const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile, ring_addr = tc::smem_u32(ring);
+    uint32_t item = 0, turns = 0, tile = 0;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && warp_wait(bar, parity & 1, abort_flag);
+      tc::fence_after_sync();
+    };
+    auto take = [&](uint32_t i) { wait(&full[i % kNS], i / kNS); };
+    auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
+      if (!ok) return;
+      if (elect_one()) {
         product_kk<DP>(d, a, ring_addr + (i % kNS) * R::kTile, ksteps);
         tc::umma_commit(bar);
-      };
-      auto accumulate = [&](uint32_t d, uint32_t a, uint32_t i, bool add) {
+      }
+      __syncwarp();
+    };
+    auto accumulate = [&](uint32_t d, uint32_t a, uint32_t i, bool add) {
+      if (!ok) return;
+      if (elect_one()) {
         const uint32_t b = desc_mnmajor(ring_addr + (i % kNS) * R::kTile);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
           umma_ts(d, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, add || kk > 0);
         tc::umma_commit(&empty[i % kNS]);
-      };
-      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-        const Entry e = p.list[u / p.n_kv_heads];
-        const int n = tiles_of(e);
-        ok = tc::mbar_wait(kv_full, turns & 1, abort_flag);
-        ++turns;
-        take(item);  // items Q_0 dO_0 Q_1 dO_1 ...
-        if (!ok) break;
-        product(tmem, k_addr, item, s_full);
-        take(item + 1);
-        if (!ok) break;
-        product(tmem + 128, v_addr, item + 1, dp_full);
-        for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
-          ok = tc::mbar_wait(p_full, tile & 1, abort_flag);
-          if (!ok) break;
-          tc::fence_after_sync();
-          accumulate(tmem + 256, tmem, item + 1, j > 0);  // dV += P' dO
-          if (j + 1 < n) {
-            take(item + 2);
-            if (!ok) break;
-            product(tmem, k_addr, item + 2, s_full);
-          }
-          ok = tc::mbar_wait(ds_full, tile & 1, abort_flag);
-          if (!ok) break;
-          tc::fence_after_sync();
-          accumulate(tmem + 384, tmem + 128, item, j > 0);  // dK += dS' Q
-          if (j + 1 < n) {
-            take(item + 3);
-            if (!ok) break;
-            product(tmem + 128, v_addr, item + 3, dp_full);
-          }
+      }
+      __syncwarp();
+    };
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Entry e = p.list[u / p.n_kv_heads];
+      const int n = tiles_of(e);
+      wait(kv_full, turns);
+      ++turns;
+      take(item);  // items Q_0 dO_0 Q_1 dO_1 ...
+      product(tmem, k_addr, item, s_full);
+      take(item + 1);
+      product(tmem + 128, v_addr, item + 1, dp_full);
+      for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
+        wait(p_full, tile);
+        accumulate(tmem + 256, tmem, item + 1, j > 0);  // dV += P' dO
+        if (j + 1 < n) {
+          take(item + 2);
+          product(tmem, k_addr, item + 2, s_full);
         }
-        if (ok) {
-          tc::umma_commit(done);
-          tc::umma_commit(kv_empty);
+        wait(ds_full, tile);
+        accumulate(tmem + 384, tmem + 128, item, j > 0);  // dK += dS' Q
+        if (j + 1 < n) {
+          take(item + 3);
+          product(tmem + 128, v_addr, item + 3, dp_full);
         }
       }
-      tc::umma_commit(drain);
-      uint32_t never = 0u;
-      tc::mbar_wait(drain, 0, &never);
+      if (ok && elect_one()) {
+        tc::umma_commit(done);
+        tc::umma_commit(kv_empty);
+      }
+      __syncwarp();
     }
+    if (elect_one()) tc::umma_commit(drain);
+    uint32_t never = 0u;
+    tc::mbar_wait(drain, 0, &never);
   } else if (warp < 8) {
     const int half = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16, mine = lane_base + half * 64;
