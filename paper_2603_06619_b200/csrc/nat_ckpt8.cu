@@ -71,7 +71,7 @@ ckpt8_kernel(const T* __restrict__ src, T* __restrict__ dst, int8_t* __restrict_
         const int64_t row = base + u * step + (half >> s.gx_log2);
         float x[kChunk];
         rows::widen(raw[u], x);
-        const rows::GroupScale gs = rows::group_scale(rows::group_top(x));
+        const rows::GroupScale gs = rows::group_scale(rows::group_top(raw[u]));
         if (in_row && row < n) {
           __stcs(reinterpret_cast<uint2*>(codes + row * s.d + col), rows::group_codes(x, gs.inv));
           if (lane == 0) scales[row * s.groups + g0] = gs.scale;

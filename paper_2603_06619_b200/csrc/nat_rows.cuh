@@ -79,6 +79,28 @@ __device__ __forceinline__ void store_raw(float* p, const Raw<float>& r) {
   __stcs(reinterpret_cast<float4*>(p) + 1, r.b);
 }
 
+// Asynchronous copies of a thread's own elements into its own slots of shared memory: rows are
+// fetched ahead without registers, and as nobody else reads a slot no barrier is involved, only the
+// thread's wait for its own copies.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* smem, const void* src) {
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem);
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the newest `ahead` groups of copies have landed.
+__device__ __forceinline__ void copies_wait(int ahead) {
+  if (ahead >= 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+__device__ __forceinline__ void copy_raw(Raw<__nv_bfloat16>* slot, const __nv_bfloat16* p) { copy_async<16>(slot, p); }
+__device__ __forceinline__ void copy_raw(Raw<float>* slot, const float* p) {
+  copy_async<16>(&slot->a, p);
+  copy_async<16>(&slot->b, p + 4);
+}
+
 __device__ __forceinline__ void load_weights(const float* p, float (&w)[kChunk]) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(p));
   const float4 b = __ldg(reinterpret_cast<const float4*>(p) + 1);
@@ -96,7 +118,9 @@ __device__ __forceinline__ void load_weights(const float* p, float (&w)[kChunk])
 
 // Largest magnitude among the 16 lanes of a group, as the bits of a float: the order of
 // unsigned integers is that of non-negative floats, with NaN above infinity.
-__device__ __forceinline__ uint32_t group_top(const float (&x)[kChunk]) {
+__device__ __forceinline__ uint32_t group_top(const Raw<float>& r) {
+  float x[kChunk];
+  widen(r, x);
   uint32_t top = 0u;
 #pragma unroll
   for (int i = 0; i < kChunk; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
@@ -104,6 +128,20 @@ __device__ __forceinline__ uint32_t group_top(const float (&x)[kChunk]) {
   for (int o = kGroupLanes / 2; o > 0; o >>= 1)
     top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, kGroupLanes));
   return top;
+}
+// Two bfloat16 at a time; a NaN wins.
+__device__ __forceinline__ uint32_t group_top(const Raw<__nv_bfloat16>& r) {
+  const uint32_t w[4] = {r.v.x & 0x7FFF7FFFu, r.v.y & 0x7FFF7FFFu, r.v.z & 0x7FFF7FFFu, r.v.w & 0x7FFF7FFFu};
+  auto top2 = [](uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  };
+  uint32_t top = top2(top2(w[0], w[1]), top2(w[2], w[3]));
+#pragma unroll
+  for (int o = kGroupLanes / 2; o > 0; o >>= 1)
+    top = top2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, kGroupLanes));
+  return max(top << 16, top & 0xFFFF0000u);
 }
 
 struct GroupScale {
@@ -114,21 +152,26 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t top_bits) {
   const float top = __uint_as_float(top_bits);
   if (top_bits >= 0x7F800000u) return {0.f, __uint_as_float(0x7FC00000u)};
   if (top_bits < (7u << 23)) return {0.f, 0.f};  // below 2^(7 - 127)
-  return {__fdiv_rn(127.f, top), __fdiv_rn(top, 127.f)};
+  // top / 127 by Markstein's division: an FMA gives the exact remainder of the first quotient, which
+  // the second FMA corrects to the rounded one (checked against the division for every exponent)
+  constexpr float kInv = 1.f / 127.f;
+  const float q = __fmul_rn(top, kInv);
+  return {__fdiv_rn(127.f, top), __fmaf_rn(__fmaf_rn(-q, 127.f, top), kInv, q)};
 }
 
 // Codes of eight elements as eight bytes.  |x inv| <= 127 (1 + 2^-22), so adding 1.5 2^23
 // leaves the nearest integer (ties to even) in the low mantissa bits; the product is rounded on its own
 // (an FMA would break ties by its lost bits).
 __device__ __forceinline__ uint2 group_codes(const float (&x)[kChunk], float inv) {
-  uint32_t w[2] = {0u, 0u};
+  uint32_t q[kChunk];
 #pragma unroll
-  for (int i = 0; i < kChunk; ++i) {
-    const float s = inv != 0.f ? __fmul_rn(x[i], inv) : 0.f;  // 0 * infinity would be a NaN
-    const uint32_t q = __float_as_uint(__fadd_rn(s, 12582912.f)) & 0xFFu;
-    w[i >> 2] |= q << (8 * (i & 3));
-  }
-  return make_uint2(w[0], w[1]);
+  for (int i = 0; i < kChunk; ++i)
+    q[i] = __float_as_uint(__fadd_rn(__fmul_rn(x[i], inv), 12582912.f));
+  auto low_bytes = [&](int i) {
+    return __byte_perm(__byte_perm(q[i], q[i + 1], 0x0040), __byte_perm(q[i + 2], q[i + 3], 0x0040), 0x5410);
+  };
+  if (inv == 0.f) return make_uint2(0u, 0u);  // zero times an infinity would be a NaN
+  return make_uint2(low_bytes(0), low_bytes(4));
 }
 
 __device__ __forceinline__ void widen_codes(uint2 c, float scale, float (&x)[kChunk]) {
