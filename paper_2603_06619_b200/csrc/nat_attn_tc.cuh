@@ -2,6 +2,7 @@
 // tensor-memory stores, 3-D tile loads, and the operand tiles' geometry.
 #pragma once
 
+#include "nat_f32x2.cuh"
 #include "nat_tc.cuh"
 
 namespace nat {
@@ -128,34 +129,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap
       : "memory");
 }
 
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n"
-      ".reg .b64 a, b, c, d;\n"
-      "mov.b64 a, {%2, %3};\n"
-      "mov.b64 b, {%4, %5};\n"
-      "mov.b64 c, {%6, %7};\n"
-      "fma.rn.f32x2 d, a, b, c;\n"
-      "mov.b64 {%0, %1}, d;\n"
-      "}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n"
-      ".reg .b64 a, b, d;\n"
-      "mov.b64 a, {%2, %3};\n"
-      "mov.b64 b, {%4, %5};\n"
-      "add.rn.f32x2 d, a, b;\n"
-      "mov.b64 {%0, %1}, d;\n"
-      "}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

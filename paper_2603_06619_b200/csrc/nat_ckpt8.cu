@@ -52,7 +52,7 @@ ckpt8_kernel(const T* __restrict__ src, T* __restrict__ dst, int8_t* __restrict_
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t row = base + u * step + (half >> s.gx_log2);
         if (in_row && row < n) {
-          float x[kChunk];
+          float2 x[rows::kPairs];
           rows::widen_codes(c[u], sc[u], x);
           rows::Raw<T> raw;
           rows::narrow(x, raw);
@@ -69,7 +69,7 @@ ckpt8_kernel(const T* __restrict__ src, T* __restrict__ dst, int8_t* __restrict_
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t row = base + u * step + (half >> s.gx_log2);
-        float x[kChunk];
+        float2 x[rows::kPairs];
         rows::widen(raw[u], x);
         const rows::GroupScale gs = rows::group_scale(rows::group_top(raw[u]));
         if (in_row && row < n) {

@@ -3,16 +3,21 @@
 //
 //   n = y rstd_y w_post,  r = alpha x + gate n,  h = r rstd_r w_pre,  rstd = (mean(.^2) + eps)^-1/2
 //
-// Bound by HBM.  NT threads own a row, each with CH chunks of eight elements in registers, so
-// that a row is read once although its two means follow one another; persistent blocks walk the rows,
-// with the next rows (up to three) on their way into shared memory by asynchronous copies: the loads
-// in flight, 60 KB and more a multiprocessor, are what the bandwidth needs, and registers would not
-// hold them beside the column sums.  Weights stay in L1.
+// Bound by HBM.  NT threads own a row, each with CH chunks of eight elements in registers, and
+// persistent blocks walk the rows, with the next rows on their way into shared memory by asynchronous
+// copies.  What the threads of a row have to agree on is found in ONE sum over the row, because its
+// barrier, not the arithmetic, is what a row waits for: with z = y (w_post gate)
+//   sum r^2 = alpha^2 sum x^2 + 2 alpha rstd_y sum x z + rstd_y^2 sum z^2
+// gives the second norm before r is formed.  Where the terms cancel (below 1/16 of their
+// magnitudes) the row is summed again from r itself.  The weights, multiplied together, are kept in
+// shared memory; from L1 they were half evicted by the rows.
 //
-// Backward, with u = dh w_pre, rhat = r rstd_r, yhat = y rstd_y:
-//   dr = dr_in + rstd_r (u - rhat mean(u rhat)),   dx = alpha dr,   dn = gate dr,
-//   v = dn w_post,  dy = rstd_y (v - yhat mean(v yhat)),
-//   dw_pre = sum dh rhat,  dw_post = sum dn yhat,  dgate = sum dr n  (over rows, or over a row).
+// Backward, with u = dh w_pre, rhat = r rstd_r, yhat = y rstd_y, e = dr_in + rstd_r u, z = yhat w_post gate:
+//   dr = e - rstd_r rhat mean(u rhat),   dx = alpha dr,   v = dr w_post gate,
+//   dy = rstd_y (v - yhat mean(v yhat)),   sum v yhat = sum e z - rstd_r mean(u rhat) sum rhat z
+//   dw_pre = sum dh rhat,  dw_post = sum gate dr yhat,  dgate = sum dr yhat w_post  (over rows, or over a row),
+// again with one sum over the row, of three products.  (The difference in sum v yhat loses no more
+// than the elements of dr, formed by the same difference, have lost.)
 // A gate per column factors out of its sum: dw_post = gate A, dgate = w_post A with one
 // A = sum dr yhat, so a thread keeps two sums per column.  Every block leaves its sums in the
 // workspace and a second kernel adds them in block order: the gradients of the weights repeat
@@ -54,39 +59,53 @@ struct BwdArgs {
   bool has_y;
 };
 
-// Sum over the NT threads of a row, the same in every thread.  `buf` alternates between calls,
-// so one barrier a call is enough: a buffer is written again only after the next call's barrier.
+// N sums over the NT threads of a row, the same in every thread: within the warps, then of the warps'
+// sums, which every warp adds up with the same shuffles.  `buf` alternates between calls, so one
+// barrier a call is enough: a buffer is written again only after the next call's barrier.
 template <int NT, int N>
 struct RowSum {
-  float (*buf)[N * 32];
+  float4* buf;  // [2][NT / 32]
   uint32_t turn = 0;
   __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
-    for (int k = 0; k < N; ++k)
+    for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+      for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
     if (NT > 32) {
       constexpr int W = NT / 32;
-      float* b = buf[turn & 1];
+      float4* b = buf + (turn & 1) * W;
       ++turn;
       if ((threadIdx.x & 31) == 0)
-#pragma unroll
-        for (int k = 0; k < N; ++k) b[k * W + (threadIdx.x >> 5)] = v[k];
+        b[threadIdx.x >> 5] = make_float4(v[0], N > 1 ? v[N > 1 ? 1 : 0] : 0.f, N > 2 ? v[N > 2 ? 2 : 0] : 0.f,
+                                          N > 3 ? v[N > 3 ? 3 : 0] : 0.f);
       __syncthreads();
+      const float4 w = b[threadIdx.x & (W - 1)];
+      const float ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        float s = 0.f;
+      for (int k = 0; k < N; ++k) v[k] = ws[k];
 #pragma unroll
-        for (int w = 0; w < W; ++w) s += b[k * W + w];
-        v[k] = s;
-      }
+      for (int o = W / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
     }
   }
 };
 
-// Threads and rows of a block: below 256 columns a warp has a row to itself, four to a block.
+__device__ __forceinline__ float sum_pairs(const float2& s) { return s.x + s.y; }
+
+// Threads and rows of a block: up to 512 columns a warp has a row to itself, four to a block.
 constexpr __host__ __device__ int block_threads(int nt) { return nt == 32 ? 128 : nt; }
 constexpr __host__ __device__ int block_rows(int nt) { return nt == 32 ? 4 : 1; }
+
+// Threads a multiprocessor, which set the registers a thread may have.  Few threads with their rows
+// on the way beat many that spill (60,000 rows of 4096): forward 302 us with 512, 348 with 768, 335
+// with 1024; leaving checkpoints, which takes twice the instructions, 561, 507, 618; backward, where a
+// thread also keeps the sums of its columns, 536 with 512, 867 with 768.
+constexpr __host__ __device__ int fwd_threads(bool c8) { return c8 ? 768 : 512; }
+constexpr int kBwdThreads = 512;
+constexpr __host__ __device__ int blocks_per_sm(int threads, int nt) {
+  return threads / block_threads(nt) > 0 ? threads / block_threads(nt) : 1;
+}
 
 // Shared memory of a block: [stage][piece of the slot][thread], 16-byte pieces, so that the copies and
 // reads of a warp fall on consecutive addresses.
@@ -110,13 +129,46 @@ __device__ __forceinline__ rows::Raw<T> read_piece(const uint4* slot) {
   return r;
 }
 
+using rows::kPairs;
+
+// Weights in shared memory: w_post times a gate per column (ones where there is neither), and w_pre.
+// For a row of NT threads with CH chunks each they are laid out like the pieces: the two float4 of a
+// chunk a row of threads apart.
+template <int NT, int CH>
+struct Weights {
+  float4* at;  // [2][CH][2][NT]
+  __device__ __forceinline__ void fill(int d, const float* w_post, const float* gate, const float* w_pre) {
+    for (int i = threadIdx.x; i < 2 * CH * NT; i += blockDim.x) {
+      // i numbers float4s of a row: chunk i / 2, its half i % 2
+      const int col = i * 4, t = (i >> 1) % NT, c = (i >> 1) / NT, half = i & 1;
+      float a[4], b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = col + j < d;
+        a[j] = (in && w_post ? w_post[col + j] : 1.f) * (in && gate ? gate[col + j] : 1.f);
+        b[j] = in && w_pre ? w_pre[col + j] : 0.f;
+      }
+      at[(c * 2 + half) * NT + t] = make_float4(a[0], a[1], a[2], a[3]);
+      at[((CH + c) * 2 + half) * NT + t] = make_float4(b[0], b[1], b[2], b[3]);
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ void get(int which, int c, int t, float2 (&w)[kPairs]) const {
+    const float4 a = at[((which * CH + c) * 2) * NT + t], b = at[((which * CH + c) * 2 + 1) * NT + t];
+    w[0] = make_float2(a.x, a.y);
+    w[1] = make_float2(a.z, a.w);
+    w[2] = make_float2(b.x, b.y);
+    w[3] = make_float2(b.z, b.w);
+  }
+};
+
 template <typename T, int NT, int CH, bool C8>
-__global__ void __launch_bounds__(block_threads(NT), 1024 / block_threads(NT))
+__global__ void __launch_bounds__(block_threads(NT), blocks_per_sm(fwd_threads(C8), NT))
 resnorm_fwd_kernel(FwdArgs a) {
   constexpr int RPB = block_rows(NT), P = Pieces<T>::kRaw, BT = block_threads(NT);
-  extern __shared__ uint4 ring[];  // [stages][x, y][CH][P][BT]
-  __shared__ float red[2][32];
-  RowSum<NT, 1> row_sum{red};
+  extern __shared__ uint4 ring[];  // [stages][x, y][CH][P][BT], then the weights
+  __shared__ float4 red[2 * (NT / 32)];
+  RowSum<NT, 4> row_sums{red};
   const int t = threadIdx.x % NT, sub = threadIdx.x / NT;
   const int64_t n = a.n_rows ? min((int64_t)max(*a.n_rows, 0), a.cap) : a.cap;
   const int64_t step = (int64_t)gridDim.x * RPB;
@@ -124,255 +176,271 @@ resnorm_fwd_kernel(FwdArgs a) {
   const T* y = (const T*)a.y;
   auto slot = [&](int stage, int of, int i) { return ring + (((stage * 2 + of) * CH + i) * P) * BT + threadIdx.x; };
   auto fetch = [&](int64_t row, int stage) {
+    if (row < n) {
+      const int64_t at = row * a.d + t * kChunk;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int col = (t + i * NT) * kChunk;
-      if (row < n && col < a.d) {
-        copy_piece<T, NT>(slot(stage, 0, i), x + row * a.d + col);
-        if (y) copy_piece<T, NT>(slot(stage, 1, i), y + row * a.d + col);
-      }
+      for (int i = 0; i < CH; ++i)
+        if ((t + i * NT) * kChunk < a.d) {
+          copy_piece<T, NT>(slot(stage, 0, i), x + at + i * NT * kChunk);
+          if (y) copy_piece<T, NT>(slot(stage, 1, i), y + at + i * NT * kChunk);
+        }
     }
     rows::copies_commit();
   };
+  auto checkpoint = [&](const rows::Raw<T>& raw, int64_t row, int col, int8_t* codes, float* scales) {
+    const rows::GroupScale gs = rows::group_scale(rows::group_top(raw));
+    if (col < a.d) {
+      float2 v[kPairs];
+      rows::widen(raw, v);
+      __stcs(reinterpret_cast<uint2*>(codes + row * a.d + col), rows::group_codes(v, gs.inv));
+      if ((t & 15) == 0) scales[row * a.groups + (col >> 7)] = gs.scale;
+    }
+  };
   int64_t row = (int64_t)blockIdx.x * RPB + sub;
   for (int k = 0; k < a.stages; ++k) fetch(row + k * step, k);
+  Weights<NT, CH> weights{reinterpret_cast<float4*>(ring + a.stages * 2 * CH * P * BT)};
+  weights.fill(a.d, a.w_post, a.gate_mode == NAT_GATE_CHANNEL ? a.gate : nullptr, a.w_pre);
   for (int stage = 0; row < n; row += step, stage = stage + 1 == a.stages ? 0 : stage + 1) {
     const float gate_row = a.gate_mode == NAT_GATE_ROW ? __ldg(a.gate + row) : 1.f;
     rows::copies_wait(a.stages - 1);
-    rows::Raw<T> qy[CH];
-    float r[CH][kChunk], yv[CH][kChunk];
-    float ss[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const bool in = (t + i * NT) * kChunk < a.d;
-      rows::widen(in ? read_piece<T, NT>(slot(stage, 0, i)) : rows::zero_raw<T>(), r[i]);
-      qy[i] = (in && y) ? read_piece<T, NT>(slot(stage, 1, i)) : rows::zero_raw<T>();
-      rows::widen(qy[i], yv[i]);
-#pragma unroll
-      for (int j = 0; j < kChunk; ++j) ss[0] = fmaf(yv[i][j], yv[i][j], ss[0]);
-    }
-    fetch(row + a.stages * step, stage);
-    if (C8 && y) {  // while the copies are issued and the sum is on its way
-#pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        const int col = (t + i * NT) * kChunk;
-        const rows::GroupScale gs = rows::group_scale(rows::group_top(qy[i]));
-        if (col < a.d) {
-          __stcs(reinterpret_cast<uint2*>(a.y8 + row * a.d + col), rows::group_codes(yv[i], gs.inv));
-          if ((t & 15) == 0) a.y8s[row * a.groups + (col >> 7)] = gs.scale;
-        }
-      }
-    }
-    float inv_y = 1.f;
-    if (a.w_post) {
-      row_sum(ss);
-      inv_y = __frsqrt_rn(fmaf(ss[0], a.inv_d, a.eps));
-      if (t == 0) a.rstd_y[row] = inv_y;
-    }
-    ss[0] = 0.f;
+    float2 r[CH][kPairs], z[CH][kPairs];  // x, then r; y w_post gate
+    float2 yy = both(0.f), xx = both(0.f), xz = both(0.f), zz = both(0.f);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int col = (t + i * NT) * kChunk;
       const bool in = col < a.d;
-      if (in) {
-        float w[kChunk], g[kChunk];
+      rows::widen(in ? read_piece<T, NT>(slot(stage, 0, i)) : rows::zero_raw<T>(), r[i]);
+      const rows::Raw<T> qy = (in && y) ? read_piece<T, NT>(slot(stage, 1, i)) : rows::zero_raw<T>();
+      rows::widen(qy, z[i]);
+      float2 w[kPairs];
+      weights.get(0, i, t, w);
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) w[j] = 1.f, g[j] = gate_row;
-        if (a.w_post) rows::load_weights(a.w_post + col, w);
-        if (a.gate_mode == NAT_GATE_CHANNEL) rows::load_weights(a.gate + col, g);
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) {
-          r[i][j] *= a.alpha;
-          if (y) r[i][j] = fmaf(g[j], yv[i][j] * inv_y * w[j], r[i][j]);
-        }
+      for (int j = 0; j < kPairs; ++j) {
+        yy = fma2(z[i][j], z[i][j], yy);
+        z[i][j] = mul2(z[i][j], w[j]);
+        xx = fma2(r[i][j], r[i][j], xx);
+        xz = fma2(r[i][j], z[i][j], xz);
+        zz = fma2(z[i][j], z[i][j], zz);
       }
-      // h is formed from r before its rounding: the norm then adds no error of its own
+      if (C8 && y) checkpoint(qy, row, col, a.y8, a.y8s);
+    }
+    fetch(row + a.stages * step, stage);
+    float sums[4] = {sum_pairs(yy), sum_pairs(xx), sum_pairs(xz), sum_pairs(zz)};
+    row_sums(sums);
+    float inv_y = 1.f;
+    if (a.w_post) {
+      inv_y = __frsqrt_rn(fmaf(sums[0], a.inv_d, a.eps));
+      if (t == 0) a.rstd_y[row] = inv_y;
+    }
+    const float f = inv_y * gate_row;
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) ss[0] = fmaf(r[i][j], r[i][j], ss[0]);
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) r[i][j] = fma2(z[i][j], both(f), mul2(r[i][j], both(a.alpha)));
+    float inv_r = 1.f;
+    if (a.w_pre) {
+      // h is formed from r before its rounding: the norm then adds no error of its own
+      const float own = a.alpha * a.alpha * sums[1] + f * f * sums[3];
+      float square = fmaf(2.f * a.alpha * f, sums[2], own);
+      if (!(square > 0.0625f * own)) {  // the same in all threads of the row
+        float2 rr = both(0.f);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+          for (int j = 0; j < kPairs; ++j) rr = fma2(r[i][j], r[i][j], rr);
+        float again[4] = {sum_pairs(rr), 0.f, 0.f, 0.f};
+        row_sums(again);
+        square = again[0];
+      }
+      inv_r = __frsqrt_rn(fmaf(square, a.inv_d, a.eps));
+      if (t == 0) a.rstd_r[row] = inv_r;
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int col = (t + i * NT) * kChunk;
+      const bool in = col < a.d;
       rows::Raw<T> out;
       rows::narrow(r[i], out);
       if (in) rows::store_raw((T*)a.r + row * a.d + col, out);
-      if (C8) {
-        float rounded[kChunk];  // the checkpoint is of the row as it is stored
-        rows::widen(out, rounded);
-        const rows::GroupScale gs = rows::group_scale(rows::group_top(out));
-        if (in) {
-          __stcs(reinterpret_cast<uint2*>(a.r8 + row * a.d + col), rows::group_codes(rounded, gs.inv));
-          if ((t & 15) == 0) a.r8s[row * a.groups + (col >> 7)] = gs.scale;
-        }
-      }
-    }
-    if (a.w_pre) {
-      row_sum(ss);
-      const float inv_r = __frsqrt_rn(fmaf(ss[0], a.inv_d, a.eps));
-      if (t == 0) a.rstd_r[row] = inv_r;
+      if (C8) checkpoint(out, row, col, a.r8, a.r8s);  // of the row as it is stored
+      if (a.w_pre && in) {
+        float2 w[kPairs];
+        weights.get(1, i, t, w);
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        const int col = (t + i * NT) * kChunk;
-        if (col < a.d) {
-          float w[kChunk];
-          rows::load_weights(a.w_pre + col, w);
-#pragma unroll
-          for (int j = 0; j < kChunk; ++j) w[j] *= r[i][j] * inv_r;
-          rows::Raw<T> out;
-          rows::narrow(w, out);
-          rows::store_raw((T*)a.h + row * a.d + col, out);
-        }
+        for (int j = 0; j < kPairs; ++j) w[j] = mul2(mul2(r[i][j], both(inv_r)), w[j]);
+        rows::narrow(w, out);
+        rows::store_raw((T*)a.h + row * a.d + col, out);
       }
     }
   }
 }
 
-// A thread has one chunk of a row.
-template <typename T, int NT, bool C8>
-__global__ void __launch_bounds__(block_threads(NT), 1024 / block_threads(NT))
+template <typename T, int NT, int CH, bool C8>
+__global__ void __launch_bounds__(block_threads(NT), kBwdThreads / block_threads(NT))
 resnorm_bwd_kernel(BwdArgs a) {
   constexpr int RPB = block_rows(NT), P = Pieces<T>::kRaw, BT = block_threads(NT);
-  // [stages][dr, dh: P pieces each][y, r: P pieces each, or one of codes (8 bytes y, 8 bytes r)][BT]
+  // [stages][CH][dr, dh: P pieces each; y, r: P pieces each, or one of codes (8 bytes y, 8 bytes r)][BT],
+  // then the weights
   constexpr int kPieces = C8 ? 2 * P + 1 : 4 * P;
   extern __shared__ uint4 ring[];
-  __shared__ float red1[2][32], red2[2][64];
-  RowSum<NT, 1> sum1{red1};
-  RowSum<NT, 2> sum2{red2};
-  const int t = threadIdx.x % NT, sub = threadIdx.x / NT, col = t * kChunk;
-  const bool in_row = col < a.d;
+  __shared__ float4 red[2 * (NT / 32)];
+  RowSum<NT, 3> row_sums{red};
+  const int t = threadIdx.x % NT, sub = threadIdx.x / NT;
   const int64_t n = a.n_rows ? min((int64_t)max(*a.n_rows, 0), a.cap) : a.cap;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  float acc[kChunk], acc_pre[kChunk];
+  const bool row_gate = a.gate_mode == NAT_GATE_ROW;
+  float2 acc[CH][kPairs], acc_pre[CH][kPairs];
 #pragma unroll
-  for (int j = 0; j < kChunk; ++j) acc[j] = acc_pre[j] = 0.f;
+  for (int i = 0; i < CH; ++i)
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) acc[i][j] = acc_pre[i][j] = both(0.f);
 
-  auto slot = [&](int stage, int piece) { return ring + (stage * kPieces + piece) * BT + threadIdx.x; };
+  auto col_of = [&](int i) { return (t + i * NT) * kChunk; };
+  auto slot = [&](int stage, int i, int piece) { return ring + ((stage * CH + i) * kPieces + piece) * BT + threadIdx.x; };
   auto fetch = [&](int64_t row, int stage) {
-    if (row < n && in_row) {
-      const int64_t at = row * a.d + col;
-      if (a.dr_in) copy_piece<T, NT>(slot(stage, 0), (const T*)a.dr_in + at);
-      if (a.w_pre) copy_piece<T, NT>(slot(stage, P), (const T*)a.dh + at);
-      if (C8) {
-        uint2* codes = reinterpret_cast<uint2*>(slot(stage, 2 * P));
-        if (a.has_y) rows::copy_async<8>(codes, a.y8 + at);
-        if (a.w_pre) rows::copy_async<8>(codes + 1, a.r8 + at);
-      } else {
-        if (a.has_y) copy_piece<T, NT>(slot(stage, 2 * P), (const T*)a.y + at);
-        if (a.w_pre) copy_piece<T, NT>(slot(stage, 3 * P), (const T*)a.r + at);
+    if (row < n) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        if (col_of(i) >= a.d) continue;
+        const int64_t at = row * a.d + col_of(i);
+        if (a.dr_in) copy_piece<T, NT>(slot(stage, i, 0), (const T*)a.dr_in + at);
+        if (a.w_pre) copy_piece<T, NT>(slot(stage, i, P), (const T*)a.dh + at);
+        if (C8) {
+          uint2* codes = reinterpret_cast<uint2*>(slot(stage, i, 2 * P));
+          if (a.has_y) rows::copy_async<8>(codes, a.y8 + at);
+          if (a.w_pre) rows::copy_async<8>(codes + 1, a.r8 + at);
+        } else {
+          if (a.has_y) copy_piece<T, NT>(slot(stage, i, 2 * P), (const T*)a.y + at);
+          if (a.w_pre) copy_piece<T, NT>(slot(stage, i, 3 * P), (const T*)a.r + at);
+        }
       }
     }
     rows::copies_commit();
   };
   // the row's scalars, one row ahead in registers
-  float inv_y_next = 1.f, inv_r_next = 1.f, gate_next = 1.f, sy_next = 0.f, sr_next = 0.f;
+  float inv_y_next = 1.f, inv_r_next = 0.f, gate_next = 1.f, sy_next[CH], sr_next[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) sy_next[i] = sr_next[i] = 0.f;
   auto fetch_scalars = [&](int64_t row) {
     if (row >= n) return;
     if (a.w_post) inv_y_next = __ldg(a.rstd_y + row);
     if (a.w_pre) inv_r_next = __ldg(a.rstd_r + row);
-    if (a.gate_mode == NAT_GATE_ROW) gate_next = __ldg(a.gate + row);
-    if (C8 && in_row) {
-      if (a.has_y) sy_next = __ldg(a.y8s + row * a.groups + (col >> 7));
-      if (a.w_pre) sr_next = __ldg(a.r8s + row * a.groups + (col >> 7));
+    if (row_gate) gate_next = __ldg(a.gate + row);
+    if (C8) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        if (col_of(i) < a.d) {
+          const int64_t at = row * a.groups + (col_of(i) >> 7);
+          if (a.has_y) sy_next[i] = __ldg(a.y8s + at);
+          if (a.w_pre) sr_next[i] = __ldg(a.r8s + at);
+        }
     }
   };
   int64_t row = (int64_t)blockIdx.x * RPB + sub;
   for (int k = 0; k < a.stages; ++k) fetch(row + k * step, k);
   fetch_scalars(row);
+  Weights<NT, CH> weights{reinterpret_cast<float4*>(ring + a.stages * CH * kPieces * BT)};
+  weights.fill(a.d, a.w_post, a.gate_mode == NAT_GATE_CHANNEL ? a.gate : nullptr, a.w_pre);
   for (int stage = 0; row < n; row += step, stage = stage + 1 == a.stages ? 0 : stage + 1) {
-    const float inv_y = inv_y_next, inv_r = inv_r_next, gate_row = gate_next, sy = sy_next, sr = sr_next;
-    float dr[kChunk], yv[kChunk];
+    const float inv_y = inv_y_next, inv_r = inv_r_next, gate_row = gate_next;
+    float2 e[CH][kPairs], yv[CH][kPairs], rv[CH][kPairs];
+    float2 s_ur = both(0.f), s_ez = both(0.f), s_rz = both(0.f);
     rows::copies_wait(a.stages - 1);
-    if (C8) {
-      const uint4 c = (in_row && a.has_y) ? *slot(stage, 2 * P) : make_uint4(0u, 0u, 0u, 0u);
-      rows::widen_codes(make_uint2(c.x, c.y), sy, yv);
-    } else {
-      rows::widen((in_row && a.has_y) ? read_piece<T, NT>(slot(stage, 2 * P)) : rows::zero_raw<T>(), yv);
-    }
-    rows::widen((in_row && a.dr_in) ? read_piece<T, NT>(slot(stage, 0)) : rows::zero_raw<T>(), dr);
-    if (a.w_pre) {
-      float rv[kChunk], u[kChunk];
-      float s1[1] = {0.f};
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) rv[j] = u[j] = 0.f;
-      if (in_row) {
-        if (C8) {
-          const uint4 c = *slot(stage, 2 * P);
-          rows::widen_codes(make_uint2(c.z, c.w), sr, rv);
-        } else {
-          rows::widen(read_piece<T, NT>(slot(stage, 3 * P)), rv);
-        }
-        rows::widen(read_piece<T, NT>(slot(stage, P)), u);
-        float w[kChunk];
-        rows::load_weights(a.w_pre + col, w);
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) {
-          rv[j] *= inv_r;
-          acc_pre[j] = fmaf(u[j], rv[j], acc_pre[j]);
-          u[j] *= w[j];
-          s1[0] = fmaf(u[j], rv[j], s1[0]);
-        }
+    for (int i = 0; i < CH; ++i) {
+      const bool in = col_of(i) < a.d;
+      float2 u[kPairs], w[kPairs];
+      if (C8) {
+        const uint4 c = in ? *slot(stage, i, 2 * P) : make_uint4(0u, 0u, 0u, 0u);
+        // a piece that was never copied holds old bytes, and its scale is zero
+        rows::widen_codes(make_uint2(c.x, c.y), sy_next[i], yv[i]);
+        rows::widen_codes(make_uint2(c.z, c.w), sr_next[i], rv[i]);
+      } else {
+        rows::widen((in && a.has_y) ? read_piece<T, NT>(slot(stage, i, 2 * P)) : rows::zero_raw<T>(), yv[i]);
+        rows::widen((in && a.w_pre) ? read_piece<T, NT>(slot(stage, i, 3 * P)) : rows::zero_raw<T>(), rv[i]);
       }
-      fetch(row + a.stages * step, stage);
-      fetch_scalars(row + step);
-      sum1(s1);
-      const float m = s1[0] * a.inv_d;
+      rows::widen((in && a.dr_in) ? read_piece<T, NT>(slot(stage, i, 0)) : rows::zero_raw<T>(), e[i]);
+      rows::widen((in && a.w_pre) ? read_piece<T, NT>(slot(stage, i, P)) : rows::zero_raw<T>(), u);
+      weights.get(1, i, t, w);
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) dr[j] = fmaf(inv_r, fmaf(-rv[j], m, u[j]), dr[j]);
-    } else {
-      fetch(row + a.stages * step, stage);
-      fetch_scalars(row + step);
+      for (int j = 0; j < kPairs; ++j) {
+        rv[i][j] = mul2(rv[i][j], both(inv_r));  // rhat
+        acc_pre[i][j] = fma2(u[j], rv[i][j], acc_pre[i][j]);
+        u[j] = mul2(u[j], w[j]);
+        s_ur = fma2(u[j], rv[i][j], s_ur);
+        e[i][j] = fma2(both(inv_r), u[j], e[i][j]);
+      }
+      weights.get(0, i, t, w);
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        yv[i][j] = mul2(yv[i][j], both(inv_y));  // yhat
+        w[j] = mul2(w[j], yv[i][j]);             // z
+        s_ez = fma2(e[i][j], w[j], s_ez);
+        s_rz = fma2(rv[i][j], w[j], s_rz);
+      }
     }
-    if (in_row) {
-      float dx[kChunk];
+    fetch(row + a.stages * step, stage);
+    fetch_scalars(row + step);
+    float sums[3] = {sum_pairs(s_ur), sum_pairs(s_ez), sum_pairs(s_rz)};
+    row_sums(sums);
+    const float m1 = inv_r * sums[0] * a.inv_d, s_vy = fmaf(-m1, sums[2], sums[1]);
+    if (row_gate && t == 0) a.dgate_row[row] = s_vy;  // of dr yhat w_post, without the gate itself
+    const float2 m2 = both(a.w_post ? -gate_row * s_vy * a.inv_d : 0.f);
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) dx[j] = a.alpha * dr[j];
+    for (int i = 0; i < CH; ++i) {
+      if (col_of(i) >= a.d) continue;
+      float2 dx[kPairs], w[kPairs];
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        e[i][j] = fma2(rv[i][j], both(-m1), e[i][j]);  // dr
+        dx[j] = mul2(both(a.alpha), e[i][j]);
+      }
       rows::Raw<T> out;
       rows::narrow(dx, out);
-      rows::store_raw((T*)a.dx + row * a.d + col, out);
-    }
-    if (a.has_y) {
-      float s2[2] = {0.f, 0.f};
-      if (in_row) {
-        float w[kChunk], g[kChunk];
+      rows::store_raw((T*)a.dx + row * a.d + col_of(i), out);
+      if (!a.has_y) continue;
+      weights.get(0, i, t, w);
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) w[j] = 1.f, g[j] = gate_row;
-        if (a.w_post) rows::load_weights(a.w_post + col, w);
-        if (a.gate_mode == NAT_GATE_CHANNEL) rows::load_weights(a.gate + col, g);
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) {
-          yv[j] *= inv_y;  // yhat
-          acc[j] = fmaf(dr[j] * gate_row, yv[j], acc[j]);
-          s2[1] = fmaf(dr[j] * yv[j], w[j], s2[1]);
-          dr[j] *= g[j] * w[j];  // v
-          s2[0] = fmaf(dr[j], yv[j], s2[0]);
-        }
+      for (int j = 0; j < kPairs; ++j) {
+        e[i][j] = mul2(e[i][j], both(gate_row));
+        acc[i][j] = fma2(e[i][j], yv[i][j], acc[i][j]);
+        w[j] = mul2(e[i][j], w[j]);  // v
       }
-      if (a.w_post || a.gate_mode == NAT_GATE_ROW) sum2(s2);
-      if (a.gate_mode == NAT_GATE_ROW && t == 0) a.dgate_row[row] = s2[1];
-      if (in_row) {
-        const float m = s2[0] * a.inv_d;
-        float dy[kChunk];
+      if (a.w_post) {
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) dy[j] = a.w_post ? inv_y * fmaf(-yv[j], m, dr[j]) : dr[j];
-        rows::Raw<T> out;
-        rows::narrow(dy, out);
-        rows::store_raw((T*)a.dy + row * a.d + col, out);
+        for (int j = 0; j < kPairs; ++j) w[j] = mul2(both(inv_y), fma2(yv[i][j], m2, w[j]));
       }
+      rows::narrow(w, out);
+      rows::store_raw((T*)a.dy + row * a.d + col_of(i), out);
     }
   }
 
   // the block's sums; four warps with rows of their own are added in warp order first
   float* p = a.partial + (int64_t)blockIdx.x * 2 * a.d;
   if (RPB == 1) {
-    if (in_row)
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) p[col + j] = acc[j], p[a.d + col + j] = acc_pre[j];
+    for (int i = 0; i < CH; ++i)
+      if (col_of(i) < a.d)
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+          *reinterpret_cast<float2*>(p + col_of(i) + 2 * j) = acc[i][j];
+          *reinterpret_cast<float2*>(p + a.d + col_of(i) + 2 * j) = acc_pre[i][j];
+        }
   } else {
-    __shared__ float part[2][RPB][RPB > 1 ? 32 * kChunk : 1];
+    __shared__ float2 part[2][RPB][RPB > 1 ? CH * 32 * kPairs : 1];
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) part[0][sub][col + j] = acc[j], part[1][sub][col + j] = acc_pre[j];
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        part[0][sub][(t + i * 32) * kPairs + j] = acc[i][j];
+        part[1][sub][(t + i * 32) * kPairs + j] = acc_pre[i][j];
+      }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
       const int which = c >= a.d;
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < RPB; ++w) s += part[which][w][c - which * a.d];
+      for (int w = 0; w < RPB; ++w) s += reinterpret_cast<const float*>(part[which][w])[c - which * a.d];
       p[c] = s;
     }
   }
@@ -406,18 +474,17 @@ resnorm_columns_kernel(const float* __restrict__ partial, int blocks, int d, int
 }
 
 // ---- launch shapes ----------------------------------------------------------------------
-// Threads of a row by its length: two chunks a thread forward, one backward (whose column sums
-// take the registers).
-constexpr int kMaxD = 8192;
+// Threads of a row by its length, two chunks each.
+constexpr int kMaxD = 8192, kChunks = 2;
 
-int threads_of(int d, int chunks) {
+int threads_of(int d) {
   int nt = 32;
-  while (nt * chunks * kChunk < d) nt *= 2;
+  while (nt * kChunks * kChunk < d) nt *= 2;
   return nt;
 }
 
-// Persistent blocks, all resident: 1024 threads a multiprocessor (64 registers each), fewer where
-// the rows on their way would not fit into its shared memory.
+// Persistent blocks, all resident, fewer of them where the rows on their way would not fit into a
+// multiprocessor's shared memory.
 constexpr int kSmemPerSm = 216 * 1024;  // of 228 KB, less 1 KB and the static part a block
 
 struct Shape {
@@ -425,26 +492,29 @@ struct Shape {
   int stages;
   size_t smem;
 };
-Shape shape_of(int nt, size_t stage_bytes, int64_t cap) {
-  int per_sm = 1024 / block_threads(nt);
-  const int fit = (int)(kSmemPerSm / stage_bytes);
+Shape shape_of(int nt, int threads_per_sm, size_t stage_bytes, int64_t cap) {
+  const size_t weights = (size_t)2 * kChunks * 2 * nt * sizeof(float4);
+  int per_sm = blocks_per_sm(threads_per_sm, nt);
+  const int fit = (int)(kSmemPerSm / (stage_bytes + weights));
   if (per_sm > fit) per_sm = fit > 0 ? fit : 1;
   Shape s;
   const int64_t want = (cap + block_rows(nt) - 1) / block_rows(nt);
   s.blocks = max((int64_t)1, min((int64_t)148 * per_sm, want));
-  s.stages = (int)min((size_t)3, max((size_t)1, kSmemPerSm / per_sm / stage_bytes));
-  s.smem = s.stages * stage_bytes;
+  s.stages = (int)min((size_t)3, max((size_t)1, (kSmemPerSm / per_sm - weights) / stage_bytes));
+  s.smem = s.stages * stage_bytes + weights;
   return s;
 }
 
 // Blocks of a backward pass at most: its workspace holds their column sums.
 int64_t max_blocks(int nt, int64_t cap) {
-  return max((int64_t)1, min((int64_t)148 * (1024 / block_threads(nt)), (cap + block_rows(nt) - 1) / block_rows(nt)));
+  return max((int64_t)1, min((int64_t)148 * (kBwdThreads / block_threads(nt)),
+                             (cap + block_rows(nt) - 1) / block_rows(nt)));
 }
 
 template <typename K, typename A>
-int launch(K kernel, A& a, int nt, size_t stage_bytes, cudaStream_t stream, int64_t* blocks, const char* name) {
-  const Shape s = shape_of(nt, stage_bytes, a.cap);
+int launch(K kernel, A& a, int nt, int threads_per_sm, size_t stage_bytes, cudaStream_t stream, int64_t* blocks,
+           const char* name) {
+  const Shape s = shape_of(nt, threads_per_sm, stage_bytes, a.cap);
   a.stages = s.stages;
   *blocks = s.blocks;
   if (s.smem > 32 * 1024)  // with the static part past the 48 KB of a plain launch
@@ -456,15 +526,22 @@ int launch(K kernel, A& a, int nt, size_t stage_bytes, cudaStream_t stream, int6
 
 template <typename T, int NT>
 int launch_fwd(FwdArgs& a, cudaStream_t stream) {
-  constexpr size_t stage = (size_t)2 * 2 * sizeof(rows::Raw<T>) * block_threads(NT);
+  constexpr size_t stage = 2 * kChunks * sizeof(rows::Raw<T>) * block_threads(NT);
   int64_t blocks;
-  return a.r8 ? launch(resnorm_fwd_kernel<T, NT, 2, true>, a, NT, stage, stream, &blocks, "resnorm_fwd_kernel")
-              : launch(resnorm_fwd_kernel<T, NT, 2, false>, a, NT, stage, stream, &blocks, "resnorm_fwd_kernel");
+  return a.r8 ? launch(resnorm_fwd_kernel<T, NT, kChunks, true>, a, NT, fwd_threads(true), stage, stream, &blocks, "resnorm_fwd_kernel")
+              : launch(resnorm_fwd_kernel<T, NT, kChunks, false>, a, NT, fwd_threads(false), stage, stream, &blocks, "resnorm_fwd_kernel");
+}
+
+template <typename T, int NT>
+int launch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
+  constexpr size_t raw = sizeof(rows::Raw<T>), per = kChunks * block_threads(NT);
+  return c8 ? launch(resnorm_bwd_kernel<T, NT, kChunks, true>, a, NT, kBwdThreads, (2 * raw + 16) * per, stream, blocks, "resnorm_bwd_kernel")
+            : launch(resnorm_bwd_kernel<T, NT, kChunks, false>, a, NT, kBwdThreads, 4 * raw * per, stream, blocks, "resnorm_bwd_kernel");
 }
 
 template <typename T>
 int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
-  switch (threads_of(a.d, 2)) {
+  switch (threads_of(a.d)) {
     case 32: return launch_fwd<T, 32>(a, stream);
     case 64: return launch_fwd<T, 64>(a, stream);
     case 128: return launch_fwd<T, 128>(a, stream);
@@ -473,22 +550,14 @@ int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
   }
 }
 
-template <typename T, int NT>
-int launch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  constexpr size_t raw = sizeof(rows::Raw<T>), bt = block_threads(NT);
-  return c8 ? launch(resnorm_bwd_kernel<T, NT, true>, a, NT, (2 * raw + 16) * bt, stream, blocks, "resnorm_bwd_kernel")
-            : launch(resnorm_bwd_kernel<T, NT, false>, a, NT, 4 * raw * bt, stream, blocks, "resnorm_bwd_kernel");
-}
-
 template <typename T>
 int dispatch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  switch (threads_of(a.d, 1)) {
+  switch (threads_of(a.d)) {
     case 32: return launch_bwd<T, 32>(a, c8, stream, blocks);
     case 64: return launch_bwd<T, 64>(a, c8, stream, blocks);
     case 128: return launch_bwd<T, 128>(a, c8, stream, blocks);
     case 256: return launch_bwd<T, 256>(a, c8, stream, blocks);
-    case 512: return launch_bwd<T, 512>(a, c8, stream, blocks);
-    default: return launch_bwd<T, 1024>(a, c8, stream, blocks);
+    default: return launch_bwd<T, 512>(a, c8, stream, blocks);
   }
 }
 
@@ -521,7 +590,7 @@ extern "C" {
 
 size_t nat_resnorm_workspace_bytes(const nat_resnorm_params* p, int64_t cap) {
   if (nat::check_params("nat_resnorm_workspace_bytes", p, cap) != NAT_OK) return 0;
-  const int64_t blocks = nat::max_blocks(nat::threads_of(p->d, 1), cap);
+  const int64_t blocks = nat::max_blocks(nat::threads_of(p->d), cap);
   return nat::align_up((size_t)blocks * 2 * p->d * sizeof(float), 256);
 }
 

@@ -6,9 +6,12 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "nat_f32x2.cuh"
+
 namespace nat {
 namespace rows {
 
+constexpr int kPairs = 4;          // a chunk as pairs for packed arithmetic
 constexpr int kChunk = 8;          // elements a thread moves at a time (16 bytes of bfloat16)
 constexpr int kGroup = 128;        // columns that share a checkpoint scale: 16 chunks, half a warp
 constexpr int kGroupLanes = kGroup / kChunk;
@@ -43,32 +46,31 @@ __device__ __forceinline__ Raw<float> zero_raw<float>() {
   return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 }
 
-__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float (&x)[kChunk]) {
+__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float2 (&x)[kPairs]) {
   const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {  // a bfloat16 is the upper half of the float of the same value
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
+  for (int i = 0; i < kPairs; ++i)  // a bfloat16 is the upper half of the float of the same value
+    x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
 }
-__device__ __forceinline__ void widen(const Raw<float>& r, float (&x)[kChunk]) {
-  x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
-  x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
+__device__ __forceinline__ void widen(const Raw<float>& r, float2 (&x)[kPairs]) {
+  x[0] = make_float2(r.a.x, r.a.y);
+  x[1] = make_float2(r.a.z, r.a.w);
+  x[2] = make_float2(r.b.x, r.b.y);
+  x[3] = make_float2(r.b.z, r.b.w);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&v);
+__device__ __forceinline__ uint32_t pack_bf16(float2 v) {
+  __nv_bfloat162 p = __float22bfloat162_rn(v);
+  return *reinterpret_cast<uint32_t*>(&p);
 }
 
 // Rounds to the rows' type (once, to nearest even).
-__device__ __forceinline__ void narrow(const float (&x)[kChunk], Raw<__nv_bfloat16>& r) {
-  r.v = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]),
-                   pack_bf16(x[6], x[7]));
+__device__ __forceinline__ void narrow(const float2 (&x)[kPairs], Raw<__nv_bfloat16>& r) {
+  r.v = make_uint4(pack_bf16(x[0]), pack_bf16(x[1]), pack_bf16(x[2]), pack_bf16(x[3]));
 }
-__device__ __forceinline__ void narrow(const float (&x)[kChunk], Raw<float>& r) {
-  r.a = make_float4(x[0], x[1], x[2], x[3]);
-  r.b = make_float4(x[4], x[5], x[6], x[7]);
+__device__ __forceinline__ void narrow(const float2 (&x)[kPairs], Raw<float>& r) {
+  r.a = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+  r.b = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
 }
 
 __device__ __forceinline__ void store_raw(__nv_bfloat16* p, const Raw<__nv_bfloat16>& r) {
@@ -101,11 +103,13 @@ __device__ __forceinline__ void copy_raw(Raw<float>* slot, const float* p) {
   copy_async<16>(&slot->b, p + 4);
 }
 
-__device__ __forceinline__ void load_weights(const float* p, float (&w)[kChunk]) {
+__device__ __forceinline__ void load_weights(const float* p, float2 (&w)[kPairs]) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(p));
   const float4 b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-  w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  w[0] = make_float2(a.x, a.y);
+  w[1] = make_float2(a.z, a.w);
+  w[2] = make_float2(b.x, b.y);
+  w[3] = make_float2(b.z, b.w);
 }
 
 // ---- 8-bit checkpoints ----------------------------------------------------------------
@@ -119,11 +123,12 @@ __device__ __forceinline__ void load_weights(const float* p, float (&w)[kChunk])
 // Largest magnitude among the 16 lanes of a group, as the bits of a float: the order of
 // unsigned integers is that of non-negative floats, with NaN above infinity.
 __device__ __forceinline__ uint32_t group_top(const Raw<float>& r) {
-  float x[kChunk];
+  float2 x[kPairs];
   widen(r, x);
   uint32_t top = 0u;
 #pragma unroll
-  for (int i = 0; i < kChunk; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+  for (int i = 0; i < kPairs; ++i)
+    top = max(top, max(__float_as_uint(x[i].x) & 0x7FFFFFFFu, __float_as_uint(x[i].y) & 0x7FFFFFFFu));
 #pragma unroll
   for (int o = kGroupLanes / 2; o > 0; o >>= 1)
     top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, kGroupLanes));
@@ -162,11 +167,13 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t top_bits) {
 // Codes of eight elements as eight bytes.  |x inv| <= 127 (1 + 2^-22), so adding 1.5 2^23
 // leaves the nearest integer (ties to even) in the low mantissa bits; the product is rounded on its own
 // (an FMA would break ties by its lost bits).
-__device__ __forceinline__ uint2 group_codes(const float (&x)[kChunk], float inv) {
+__device__ __forceinline__ uint2 group_codes(const float2 (&x)[kPairs], float inv) {
   uint32_t q[kChunk];
 #pragma unroll
-  for (int i = 0; i < kChunk; ++i)
-    q[i] = __float_as_uint(__fadd_rn(__fmul_rn(x[i], inv), 12582912.f));
+  for (int i = 0; i < kPairs; ++i) {  // the packed forms are contracted to an FMA
+    q[2 * i] = __float_as_uint(__fadd_rn(__fmul_rn(x[i].x, inv), 12582912.f));
+    q[2 * i + 1] = __float_as_uint(__fadd_rn(__fmul_rn(x[i].y, inv), 12582912.f));
+  }
   auto low_bytes = [&](int i) {
     return __byte_perm(__byte_perm(q[i], q[i + 1], 0x0040), __byte_perm(q[i + 2], q[i + 3], 0x0040), 0x5410);
   };
@@ -174,11 +181,11 @@ __device__ __forceinline__ uint2 group_codes(const float (&x)[kChunk], float inv
   return make_uint2(low_bytes(0), low_bytes(4));
 }
 
-__device__ __forceinline__ void widen_codes(uint2 c, float scale, float (&x)[kChunk]) {
+__device__ __forceinline__ void widen_codes(uint2 c, float scale, float2 (&x)[kPairs]) {
 #pragma unroll
-  for (int i = 0; i < kChunk; ++i) {
-    const uint32_t w = i < 4 ? c.x : c.y;
-    x[i] = (float)(int8_t)(w >> (8 * (i & 3))) * scale;
+  for (int i = 0; i < kPairs; ++i) {
+    const uint32_t w = (i < 2 ? c.x : c.y) >> (16 * (i & 1));
+    x[i] = mul2(make_float2((float)(int8_t)w, (float)(int8_t)(w >> 8)), both(scale));
   }
 }
 
