@@ -99,8 +99,9 @@ constexpr __host__ __device__ int block_rows(int nt) { return nt == 32 ? 4 : 1; 
 
 // Threads a multiprocessor, which set the registers a thread may have.  Few threads with their rows
 // on the way beat many that spill (60,000 rows of 4096): forward 302 us with 512, 348 with 768, 335
-// with 1024; leaving checkpoints, which takes twice the instructions, 561, 507, 618; backward, where a
-// thread also keeps the sums of its columns, 536 with 512, 867 with 768.
+// with 1024; leaving checkpoints, which takes twice the instructions, 546, 495, 595; backward, where a
+// thread also keeps the sums of its columns, 530 with 512, 867 with 768 (one chunk a thread: 534 with
+// 768, 590 with 1024).
 constexpr __host__ __device__ int fwd_threads(bool c8) { return c8 ? 768 : 512; }
 constexpr int kBwdThreads = 512;
 constexpr __host__ __device__ int blocks_per_sm(int threads, int nt) {
@@ -475,11 +476,11 @@ resnorm_columns_kernel(const float* __restrict__ partial, int blocks, int d, int
 
 // ---- launch shapes ----------------------------------------------------------------------
 // Threads of a row by its length, two chunks each.
-constexpr int kMaxD = 8192, kChunks = 2;
+constexpr int kMaxD = 8192, kFwdChunks = 2, kBwdChunks = 2;
 
-int threads_of(int d) {
+int threads_of(int d, int chunks) {
   int nt = 32;
-  while (nt * kChunks * kChunk < d) nt *= 2;
+  while (nt * chunks * kChunk < d) nt *= 2;
   return nt;
 }
 
@@ -492,8 +493,8 @@ struct Shape {
   int stages;
   size_t smem;
 };
-Shape shape_of(int nt, int threads_per_sm, size_t stage_bytes, int64_t cap) {
-  const size_t weights = (size_t)2 * kChunks * 2 * nt * sizeof(float4);
+Shape shape_of(int nt, int chunks, int threads_per_sm, size_t stage_bytes, int64_t cap) {
+  const size_t weights = (size_t)2 * chunks * 2 * nt * sizeof(float4);
   int per_sm = blocks_per_sm(threads_per_sm, nt);
   const int fit = (int)(kSmemPerSm / (stage_bytes + weights));
   if (per_sm > fit) per_sm = fit > 0 ? fit : 1;
@@ -512,9 +513,9 @@ int64_t max_blocks(int nt, int64_t cap) {
 }
 
 template <typename K, typename A>
-int launch(K kernel, A& a, int nt, int threads_per_sm, size_t stage_bytes, cudaStream_t stream, int64_t* blocks,
+int launch(K kernel, A& a, int nt, int chunks, int threads_per_sm, size_t stage_bytes, cudaStream_t stream, int64_t* blocks,
            const char* name) {
-  const Shape s = shape_of(nt, threads_per_sm, stage_bytes, a.cap);
+  const Shape s = shape_of(nt, chunks, threads_per_sm, stage_bytes, a.cap);
   a.stages = s.stages;
   *blocks = s.blocks;
   if (s.smem > 32 * 1024)  // with the static part past the 48 KB of a plain launch
@@ -526,22 +527,22 @@ int launch(K kernel, A& a, int nt, int threads_per_sm, size_t stage_bytes, cudaS
 
 template <typename T, int NT>
 int launch_fwd(FwdArgs& a, cudaStream_t stream) {
-  constexpr size_t stage = 2 * kChunks * sizeof(rows::Raw<T>) * block_threads(NT);
+  constexpr size_t stage = 2 * kFwdChunks * sizeof(rows::Raw<T>) * block_threads(NT);
   int64_t blocks;
-  return a.r8 ? launch(resnorm_fwd_kernel<T, NT, kChunks, true>, a, NT, fwd_threads(true), stage, stream, &blocks, "resnorm_fwd_kernel")
-              : launch(resnorm_fwd_kernel<T, NT, kChunks, false>, a, NT, fwd_threads(false), stage, stream, &blocks, "resnorm_fwd_kernel");
+  return a.r8 ? launch(resnorm_fwd_kernel<T, NT, kFwdChunks, true>, a, NT, kFwdChunks, fwd_threads(true), stage, stream, &blocks, "resnorm_fwd_kernel")
+              : launch(resnorm_fwd_kernel<T, NT, kFwdChunks, false>, a, NT, kFwdChunks, fwd_threads(false), stage, stream, &blocks, "resnorm_fwd_kernel");
 }
 
 template <typename T, int NT>
 int launch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  constexpr size_t raw = sizeof(rows::Raw<T>), per = kChunks * block_threads(NT);
-  return c8 ? launch(resnorm_bwd_kernel<T, NT, kChunks, true>, a, NT, kBwdThreads, (2 * raw + 16) * per, stream, blocks, "resnorm_bwd_kernel")
-            : launch(resnorm_bwd_kernel<T, NT, kChunks, false>, a, NT, kBwdThreads, 4 * raw * per, stream, blocks, "resnorm_bwd_kernel");
+  constexpr size_t raw = sizeof(rows::Raw<T>), per = kBwdChunks * block_threads(NT);
+  return c8 ? launch(resnorm_bwd_kernel<T, NT, kBwdChunks, true>, a, NT, kBwdChunks, kBwdThreads, (2 * raw + 16) * per, stream, blocks, "resnorm_bwd_kernel")
+            : launch(resnorm_bwd_kernel<T, NT, kBwdChunks, false>, a, NT, kBwdChunks, kBwdThreads, 4 * raw * per, stream, blocks, "resnorm_bwd_kernel");
 }
 
 template <typename T>
 int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
-  switch (threads_of(a.d)) {
+  switch (threads_of(a.d, kFwdChunks)) {
     case 32: return launch_fwd<T, 32>(a, stream);
     case 64: return launch_fwd<T, 64>(a, stream);
     case 128: return launch_fwd<T, 128>(a, stream);
@@ -552,12 +553,13 @@ int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
 
 template <typename T>
 int dispatch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  switch (threads_of(a.d)) {
+  switch (threads_of(a.d, kBwdChunks)) {
     case 32: return launch_bwd<T, 32>(a, c8, stream, blocks);
     case 64: return launch_bwd<T, 64>(a, c8, stream, blocks);
     case 128: return launch_bwd<T, 128>(a, c8, stream, blocks);
     case 256: return launch_bwd<T, 256>(a, c8, stream, blocks);
-    default: return launch_bwd<T, 512>(a, c8, stream, blocks);
+    case 512: return launch_bwd<T, 512>(a, c8, stream, blocks);
+    default: return launch_bwd<T, 1024>(a, c8, stream, blocks);
   }
 }
 
@@ -590,7 +592,7 @@ extern "C" {
 
 size_t nat_resnorm_workspace_bytes(const nat_resnorm_params* p, int64_t cap) {
   if (nat::check_params("nat_resnorm_workspace_bytes", p, cap) != NAT_OK) return 0;
-  const int64_t blocks = nat::max_blocks(nat::threads_of(p->d), cap);
+  const int64_t blocks = nat::max_blocks(nat::threads_of(p->d, nat::kBwdChunks), cap);
   return nat::align_up((size_t)blocks * 2 * p->d * sizeof(float), 256);
 }
 

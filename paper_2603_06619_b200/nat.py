@@ -277,25 +277,50 @@ _DTYPES = {torch.float32: NAT_F32, torch.bfloat16: NAT_BF16}
 GROUP8 = 128                 # columns that share a scale in an 8-bit checkpoint
 
 
-def _rows(what, t, dtype, shape, strided=False):
-    """Pointer of a device tensor of at least `shape` (leading size: at least), checked:
-    type, device, extent, and contiguity (a token stride of its own where `strided`)."""
-    if t is None:
-        return None
+def _device():
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError):
+        return None                # no CUDA device: no tensor is on it
+
+
+def _raw_stream(device):
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _bad(what, t, dtype, shape, device):
     if t.dtype != dtype:
         raise NatError(f"{what}: expected {dtype}, got {t.dtype}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != device:
         raise NatError(f"{what}: on {t.device}, not on the current CUDA device")
     if t.dim() != len(shape) or t.shape[0] < shape[0] or tuple(t.shape[1:]) != tuple(shape[1:]):
         raise NatError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    inner = t[0] if strided and t.shape[0] else t
-    if t.numel() and not inner.is_contiguous():
-        raise NatError(f"{what}: not contiguous")
+    raise NatError(f"{what}: not contiguous")
+
+
+def _rows(what, t, dtype, shape, device):
+    """Pointer of a contiguous tensor on `device` of that type and shape (leading size: at
+    least); None stays None."""
+    if t is None:
+        return None
+    s = t.shape
+    if (t.dtype is not dtype or t.get_device() != device or len(s) != len(shape) or s[0] < shape[0]
+            or s[1:] != shape[1:] or not t.is_contiguous()):
+        _bad(what, t, dtype, shape, device)
     return t.data_ptr()
 
 
-def _workspace(t):
-    if t.device.index != torch.cuda.current_device() or not t.is_contiguous():
+def _heads(what, t, dtype, shape, device):
+    """The same for [tokens, heads, head_dim] with a token stride of its own."""
+    s = t.shape
+    if (t.dtype is not dtype or t.get_device() != device or len(s) != 3 or s[0] < shape[0]
+            or s[1:] != shape[1:] or t.stride(2) != 1 or (s[1] > 1 and t.stride(1) != s[2])):
+        _bad(what, t, dtype, shape, device)
+    return t.data_ptr()
+
+
+def _workspace(t, device):
+    if t.get_device() != device or not t.is_contiguous():
         raise NatError("workspace: must be contiguous, on the current CUDA device")
     return t.data_ptr(), t.numel() * t.element_size()
 
@@ -315,44 +340,45 @@ def nat_attn_workspace_bytes(params, B, cap):
 
 
 def _attn_call(params, B, cu_seqlens, cap, tensors, lse):
-    """(pointers, params with the tensors' strides) of a call; `tensors` maps names to
-    (tensor, stride field, head count)."""
+    """(pointers, params with the tensors' strides, cu_seqlens, lse, device) of a call; `tensors`
+    holds (name, tensor, stride field, head count)."""
+    device = _device()
     dtype = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
-    p = AttnParams()
-    ctypes.memmove(ctypes.byref(p), ctypes.byref(params), ctypes.sizeof(p))
-    strides, ptrs = {}, {}
-    for name, (t, field, heads) in tensors.items():
-        ptrs[name] = _rows(name, t, dtype, (cap, heads, params.head_dim), strided=True)
-        if t.shape[0] > 1 and strides.setdefault(field, t.stride(0)) != t.stride(0):
-            raise NatError(f"{name}: token stride {t.stride(0)}, its counterpart has {strides[field]}")
+    p = AttnParams.from_buffer_copy(params)
+    strides, ptrs, D = {}, [], params.head_dim
+    for name, t, field, heads in tensors:
+        ptrs.append(_heads(name, t, dtype, (cap, heads, D), device))
+        if t.shape[0] > 1:
+            stride = t.stride(0)
+            if strides.setdefault(field, stride) != stride:
+                raise NatError(f"{name}: token stride {stride}, its counterpart has {strides[field]}")
     for field, stride in strides.items():
         setattr(p, field, stride)
-    ptrs["cu_seqlens"] = _rows("cu_seqlens", cu_seqlens, torch.int32, (B + 1,))
-    ptrs["lse"] = _rows("lse", lse, torch.float32, (cap, params.n_heads))
-    return ptrs, p
+    return (ptrs, p, _rows("cu_seqlens", cu_seqlens, torch.int32, (B + 1,), device),
+            _rows("lse", lse, torch.float32, (cap, params.n_heads), device), device)
 
 
 def nat_attn_fwd(params, B, cu_seqlens, cap, q, k, v, out, lse, workspace):
     h, kv = params.n_heads, params.n_kv_heads
-    t, p = _attn_call(params, B, cu_seqlens, cap, {
-        "q": (q, "q_stride", h), "k": (k, "k_stride", kv), "v": (v, "v_stride", kv),
-        "out": (out, "o_stride", h)}, lse)
-    ws, nbytes = _workspace(workspace)
-    _check(load().nat_attn_fwd(ctypes.byref(p), B, t["cu_seqlens"], cap, t["q"], t["k"], t["v"],
-                               t["out"], t["lse"], ws, nbytes, _stream()))
+    (q, k, v, out), p, cu, lse, device = _attn_call(
+        params, B, cu_seqlens, cap, (("q", q, "q_stride", h), ("k", k, "k_stride", kv),
+                                     ("v", v, "v_stride", kv), ("out", out, "o_stride", h)), lse)
+    ws, nbytes = _workspace(workspace, device)
+    _check(load().nat_attn_fwd(ctypes.byref(p), B, cu, cap, q, k, v, out, lse, ws, nbytes,
+                               _raw_stream(device)))
 
 
 def nat_attn_bwd(params, B, cu_seqlens, cap, q, k, v, out, lse, dout, dq, dk, dv, workspace):
     """dq, dk, dv have the token strides of q, k, v, and dout that of out."""
     h, kv = params.n_heads, params.n_kv_heads
-    t, p = _attn_call(params, B, cu_seqlens, cap, {
-        "q": (q, "q_stride", h), "k": (k, "k_stride", kv), "v": (v, "v_stride", kv),
-        "out": (out, "o_stride", h), "dout": (dout, "o_stride", h), "dq": (dq, "q_stride", h),
-        "dk": (dk, "k_stride", kv), "dv": (dv, "v_stride", kv)}, lse)
-    ws, nbytes = _workspace(workspace)
-    _check(load().nat_attn_bwd(ctypes.byref(p), B, t["cu_seqlens"], cap, t["q"], t["k"], t["v"],
-                               t["out"], t["lse"], t["dout"], t["dq"], t["dk"], t["dv"], ws,
-                               nbytes, _stream()))
+    (q, k, v, out, dout, dq, dk, dv), p, cu, lse, device = _attn_call(
+        params, B, cu_seqlens, cap, (
+            ("q", q, "q_stride", h), ("k", k, "k_stride", kv), ("v", v, "v_stride", kv),
+            ("out", out, "o_stride", h), ("dout", dout, "o_stride", h), ("dq", dq, "q_stride", h),
+            ("dk", dk, "k_stride", kv), ("dv", dv, "v_stride", kv)), lse)
+    ws, nbytes = _workspace(workspace, device)
+    _check(load().nat_attn_bwd(ctypes.byref(p), B, cu, cap, q, k, v, out, lse, dout, dq, dk, dv, ws,
+                               nbytes, _raw_stream(device)))
 
 
 def resnorm_params(d, dtype, eps=1e-6, alpha=1.0, gate="none"):
@@ -366,66 +392,65 @@ def nat_resnorm_workspace_bytes(params, cap):
     return load().nat_resnorm_workspace_bytes(ctypes.byref(params), cap)
 
 
-def _pair8(what, pair, cap, d):
+def _pair8(what, pair, cap, d, device):
     if pair is None:
         return None, None
-    return (_rows(what, pair[0], torch.int8, (cap, d)),
-            _rows(what + " scales", pair[1], torch.float32, (cap, (d + GROUP8 - 1) // GROUP8)))
-
-
-def _resnorm_call(params, cap, n_rows, rows, gate, vectors, per_row):
-    d = params.d
-    dtype = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
-    t = {k: _rows(k, v, dtype, (cap, d)) for k, v in rows.items()}
-    t.update({k: _rows(k, v, torch.float32, (d,)) for k, v in vectors.items()})
-    t.update({k: _rows(k, v, torch.float32, (cap,)) for k, v in per_row.items()})
-    of = (cap,) if params.gate_mode == NAT_GATE_ROW else (d,)
-    t.update({k: _rows(k, v, torch.float32, of) for k, v in gate.items()})
-    t["n_rows"] = _rows("n_rows", n_rows, torch.int32, (1,))
-    return t
+    return (_rows(what, pair[0], torch.int8, (cap, d), device),
+            _rows(what, pair[1], torch.float32, (cap, (d + GROUP8 - 1) // GROUP8), device))
 
 
 def nat_resnorm_fwd(params, x, y, w_post, gate, w_pre, n_rows, cap, r, h, rstd_y, rstd_r, y8=None,
                     r8=None):
     """y8, r8: None, or (codes, scales) of the 8-bit checkpoints to leave."""
-    t = _resnorm_call(params, cap, n_rows, dict(x=x, y=y, r=r, h=h), dict(gate=gate),
-                      dict(w_post=w_post, w_pre=w_pre), dict(rstd_y=rstd_y, rstd_r=rstd_r))
+    dev, d, f32 = _device(), params.d, torch.float32
+    dt = f32 if params.dtype == NAT_F32 else torch.bfloat16
+    rows, vec, per_row = (cap, d), (d,), (cap,)
     _check(load().nat_resnorm_fwd(
-        ctypes.byref(params), t["x"], t["y"], t["w_post"], t["gate"], t["w_pre"], t["n_rows"], cap,
-        t["r"], t["h"], t["rstd_y"], t["rstd_r"], *_pair8("y8", y8, cap, params.d),
-        *_pair8("r8", r8, cap, params.d), _stream()))
+        ctypes.byref(params), _rows("x", x, dt, rows, dev), _rows("y", y, dt, rows, dev),
+        _rows("w_post", w_post, f32, vec, dev),
+        _rows("gate", gate, f32, per_row if params.gate_mode == NAT_GATE_ROW else vec, dev),
+        _rows("w_pre", w_pre, f32, vec, dev), _rows("n_rows", n_rows, torch.int32, (1,), dev), cap,
+        _rows("r", r, dt, rows, dev), _rows("h", h, dt, rows, dev),
+        _rows("rstd_y", rstd_y, f32, per_row, dev), _rows("rstd_r", rstd_r, f32, per_row, dev),
+        *_pair8("y8", y8, cap, d, dev), *_pair8("r8", r8, cap, d, dev), _raw_stream(dev)))
 
 
 def nat_resnorm_bwd(params, y, r, w_post, gate, w_pre, rstd_y, rstd_r, n_rows, cap, dr, dh, dx, dy,
                     dw_post, dgate, dw_pre, workspace, y8=None, r8=None):
     """y and r as rows, or None with y8 and r8 = (codes, scales)."""
-    t = _resnorm_call(params, cap, n_rows, dict(y=y, r=r, dr=dr, dh=dh, dx=dx, dy=dy),
-                      dict(gate=gate, dgate=dgate),
-                      dict(w_post=w_post, w_pre=w_pre, dw_post=dw_post, dw_pre=dw_pre),
-                      dict(rstd_y=rstd_y, rstd_r=rstd_r))
-    ws, nbytes = _workspace(workspace)
+    dev, d, f32 = _device(), params.d, torch.float32
+    dt = f32 if params.dtype == NAT_F32 else torch.bfloat16
+    rows, vec, per_row = (cap, d), (d,), (cap,)
+    of_gate = per_row if params.gate_mode == NAT_GATE_ROW else vec
+    ws, nbytes = _workspace(workspace, dev)
     _check(load().nat_resnorm_bwd(
-        ctypes.byref(params), t["y"], t["r"], *_pair8("y8", y8, cap, params.d),
-        *_pair8("r8", r8, cap, params.d), t["w_post"], t["gate"], t["w_pre"], t["rstd_y"],
-        t["rstd_r"], t["n_rows"], cap, t["dr"], t["dh"], t["dx"], t["dy"], t["dw_post"],
-        t["dgate"], t["dw_pre"], ws, nbytes, _stream()))
+        ctypes.byref(params), _rows("y", y, dt, rows, dev), _rows("r", r, dt, rows, dev),
+        *_pair8("y8", y8, cap, d, dev), *_pair8("r8", r8, cap, d, dev),
+        _rows("w_post", w_post, f32, vec, dev), _rows("gate", gate, f32, of_gate, dev),
+        _rows("w_pre", w_pre, f32, vec, dev), _rows("rstd_y", rstd_y, f32, per_row, dev),
+        _rows("rstd_r", rstd_r, f32, per_row, dev), _rows("n_rows", n_rows, torch.int32, (1,), dev),
+        cap, _rows("dr", dr, dt, rows, dev), _rows("dh", dh, dt, rows, dev),
+        _rows("dx", dx, dt, rows, dev), _rows("dy", dy, dt, rows, dev),
+        _rows("dw_post", dw_post, f32, vec, dev), _rows("dgate", dgate, f32, of_gate, dev),
+        _rows("dw_pre", dw_pre, f32, vec, dev), ws, nbytes, _raw_stream(dev)))
 
 
 def nat_ckpt8_store(src, n_rows, cap, codes, scales):
     """8-bit checkpoint of rows [0, n_rows) (a device scalar; None: cap) of src [cap, d]."""
-    d = src.shape[-1]
-    c, sc = _pair8("codes", (codes, scales), cap, d)
+    dev, d = _device(), src.shape[-1]
+    c, sc = _pair8("codes", (codes, scales), cap, d, dev)
     _check(load().nat_ckpt8_store(_DTYPES.get(src.dtype, -1), d,
-                                  _rows("src", src, src.dtype, (cap, d)),
-                                  _rows("n_rows", n_rows, torch.int32, (1,)), cap, c, sc, _stream()))
+                                  _rows("src", src, src.dtype, (cap, d), dev),
+                                  _rows("n_rows", n_rows, torch.int32, (1,), dev), cap, c, sc,
+                                  _raw_stream(dev)))
 
 
 def nat_ckpt8_load(codes, scales, n_rows, cap, dst):
-    d = dst.shape[-1]
-    c, sc = _pair8("codes", (codes, scales), cap, d)
+    dev, d = _device(), dst.shape[-1]
+    c, sc = _pair8("codes", (codes, scales), cap, d, dev)
     _check(load().nat_ckpt8_load(_DTYPES.get(dst.dtype, -1), d, c, sc,
-                                 _rows("n_rows", n_rows, torch.int32, (1,)), cap,
-                                 _rows("dst", dst, dst.dtype, (cap, d)), _stream()))
+                                 _rows("n_rows", n_rows, torch.int32, (1,), dev), cap,
+                                 _rows("dst", dst, dst.dtype, (cap, d), dev), _raw_stream(dev)))
 
 
 def nat_trace_begin():
