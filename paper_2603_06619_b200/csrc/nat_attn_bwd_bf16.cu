@@ -34,8 +34,11 @@ template <int DP>
 struct BwdShape {
   static constexpr int kNP = DP / 64;
   static constexpr uint32_t kTile = kNP * kPanel;
-  static constexpr int kStages = 5;                       // tiles of the ring, beside two resident ones
-  static constexpr uint32_t kTiles = (2 + kStages) * kTile;
+  // Beside the two resident tiles two rings: A holds the tiles that live long (K in dq, Q in dkv: used
+  // by the first and the last product of a step), B the others.  In one common ring a B tile would
+  // wait for the slot of an A tile that is still in use.
+  static constexpr int kA = DP == 128 ? 3 : 4, kB = DP == 128 ? 2 : 4;
+  static constexpr uint32_t kTiles = (2 + kA + kB) * kTile;
   static constexpr uint32_t kStats = 2 * 2 * kRows * 4;   // lse2 and delta of two row tiles
   static constexpr uint32_t kSlack = 768;                 // room to round the base up to 1024 bytes
   static constexpr uint32_t kSmem = kTiles + kStats + 256 + kSlack;
@@ -83,27 +86,37 @@ __device__ __forceinline__ void store_acc(uint32_t addr, int half, __nv_bfloat16
   }
 }
 
-// Ring of tiles: `item` numbers the loads of a block, stage item % kStages.
+// A ring of N tiles: `item` numbers the loads of a block, stage item % N.
+template <int N>
+struct Ring {
+  uint32_t tiles;  // shared-memory address
+  uint64_t *full, *empty;
+  uint32_t tile_bytes;
+  __device__ __forceinline__ uint32_t tile(uint32_t item) const { return tiles + (item % N) * tile_bytes; }
+  __device__ __forceinline__ uint64_t* full_of(uint32_t item) const { return &full[item % N]; }
+  __device__ __forceinline__ uint64_t* empty_of(uint32_t item) const { return &empty[item % N]; }
+  __device__ __forceinline__ static uint32_t parity(uint32_t item) { return (item / N) & 1; }
+};
+
 template <int DP>
 struct Loader {
   using R = BwdShape<DP>;
-  uint8_t* ring;
-  uint64_t *full, *empty, *raw;
+  uint64_t* raw;
   volatile uint32_t* abort_flag;
   int lane;
-  uint32_t item = 0, raw_turns = 0;
+  uint32_t raw_turns = 0;
   bool ok = true;
 
-  // One tile of the box [.., heads, tokens] at (head, row); rows [valid, 128) are zeroed where `valid`
-  // is below `rows`, the rows that the box brings.
-  __device__ __forceinline__ void load(const CUtensorMap* map, int head, int row, int rows, int valid) {
-    const int s = item % R::kStages;
-    ok = ok && warp_wait(&empty[s], ((item / R::kStages) & 1) ^ 1, abort_flag);
+  // Load number `item` of a ring: a box of `rows` rows of heads from `head` on, tokens from `row` on; rows
+  // [valid, rows) belong to nobody and are zeroed.
+  template <int N>
+  __device__ __forceinline__ void load(const Ring<N>& ring, uint32_t item, uint8_t* tiles, const CUtensorMap* map,
+                                       int head, int row, int rows, int valid) {
+    ok = ok && warp_wait(ring.empty_of(item), ring.parity(item) ^ 1, abort_flag);
     if (!ok) return;
-    ++item;
     const bool fix = valid < rows;
-    uint64_t* bar = fix ? raw : &full[s];
-    uint8_t* dst = ring + s * R::kTile;
+    uint64_t* bar = fix ? raw : ring.full_of(item);
+    uint8_t* dst = tiles + (item % N) * R::kTile;
     if (lane == 0) {
       tc::mbar_arrive_expect_tx(bar, (uint32_t)rows * 128u * R::kNP);
       for (int c = 0; c < R::kNP; ++c)
@@ -114,20 +127,28 @@ struct Loader {
       ++raw_turns;
       if (!ok) return;
       zero_rows<R::kNP>(dst, valid, lane);
-      if (lane == 0) tc::mbar_arrive(&full[s]);
+      if (lane == 0) tc::mbar_arrive(ring.full_of(item));
     }
   }
 
   // After a wait that gave up: the block must not leave with a copy in flight.
-  __device__ __forceinline__ void land(uint64_t* resident, uint32_t resident_turns) {
-    if (ok) return;
+  template <int N>
+  __device__ __forceinline__ void land(const Ring<N>& ring, uint32_t items) {
     uint32_t never = 0u;
-    if (raw_turns) tc::mbar_wait(raw, (raw_turns - 1) & 1, &never, 1000000000ull), never = 0u;
-    for (uint32_t i = item > (uint32_t)R::kStages ? item - R::kStages : 0; i < item; ++i)
-      tc::mbar_wait(&full[i % R::kStages], (i / R::kStages) & 1, &never, 1000000000ull), never = 0u;
-    if (resident_turns) tc::mbar_wait(resident, (resident_turns - 1) & 1, &never, 1000000000ull);
+    for (uint32_t i = items > (uint32_t)N ? items - N : 0; i < items; ++i)
+      tc::mbar_wait(ring.full_of(i), ring.parity(i), &never, 1000000000ull), never = 0u;
+  }
+  __device__ __forceinline__ void land(uint64_t* bar, uint32_t turns) {
+    uint32_t never = 0u;
+    if (turns) tc::mbar_wait(bar, (turns - 1) & 1, &never, 1000000000ull);
   }
 };
+
+// 32 score columns of one thread: P = exp(scale S - lse), the subtrahends one for the row or one a column.
+__device__ __forceinline__ float2 weight(float2 s, float2 scale, float2 minus_lse2) {
+  const float2 e = fma2(s, scale, minus_lse2);
+  return make_float2(ex2(e.x), ex2(e.y));
+}
 
 template <int DP>
 __global__ void __launch_bounds__(384, 1)
@@ -135,7 +156,6 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                const BwdParams p) {
   using R = BwdShape<DP>;
-  constexpr int kNS = R::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   bool fits;
   uint8_t* smem = tile_base(smem_raw, R::kSlack, &fits);
@@ -143,11 +163,13 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     if (threadIdx.x == 0) atomicOr(p.status, NAT_DEV_TIMEOUT);
     return;
   }
-  uint8_t* ring = smem + 2 * R::kTile;
+  uint8_t *tiles_a = smem + 2 * R::kTile, *tiles_b = tiles_a + R::kA * R::kTile;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + R::kTiles + R::kStats);
   uint64_t *qdo_full = bars, *qdo_empty = bars + 1, *s_full = bars + 2, *dp_full = bars + 4, *ds_full = bars + 5;
-  uint64_t *dq_done = bars + 6, *raw = bars + 7, *drain = bars + 8, *full = bars + 9, *empty = bars + 9 + kNS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9 + 2 * kNS);
+  uint64_t *dq_done = bars + 6, *raw = bars + 7, *drain = bars + 8;
+  const Ring<R::kA> ring_k{tc::smem_u32(tiles_a), bars + 9, bars + 9 + R::kA, R::kTile};
+  const Ring<R::kB> ring_v{tc::smem_u32(tiles_b), bars + 9 + 2 * R::kA, bars + 9 + 2 * R::kA + R::kB, R::kTile};
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9 + 2 * (R::kA + R::kB));
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
@@ -162,10 +184,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     tc::mbar_init(dq_done, 1);
     tc::mbar_init(raw, 1);
     tc::mbar_init(drain, 1);
-    for (int s = 0; s < kNS; ++s) {
-      tc::mbar_init(&full[s], 1);
-      tc::mbar_init(&empty[s], 1);
-    }
+    for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[9 + s], 1);
     *abort_flag = 0u;
     tc::fence_barrier_init();
   }
@@ -181,8 +200,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   auto tiles_of = [&](const Entry& e) { return (min(e.lo + p.tq, e.seq_hi) - e.seq_lo + kRows - 1) / kRows; };
 
   if (warp == 9) {
-    Loader<DP> ld{ring, full, empty, raw, abort_flag, lane};
-    uint32_t turns = 0;
+    Loader<DP> ld{raw, abort_flag, lane};
+    uint32_t turns = 0, item = 0;
     const int q_rows = p.group * p.tq;
     for (uint32_t u = blockIdx.x; ld.ok && u < units; u += gridDim.x) {
       const Entry e = p.list[u / p.n_kv_heads];
@@ -198,40 +217,46 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
       }
       const int end = min(e.lo + p.tq, e.seq_hi);
-      for (int j = 0; ld.ok && j < n; ++j) {
+      for (int j = 0; ld.ok && j < n; ++j, ++item) {
         const int row = e.seq_lo + j * kRows;
         // K is also the second factor of dS K, where rows past the end must not count; V only
         // meets the mask of dS
-        ld.load(&map_k, head, row, kRows, min(end - row, kRows));
-        ld.load(&map_v, head, row, kRows, kRows);
+        ld.load(ring_k, item, tiles_a, &map_k, head, row, kRows, min(end - row, kRows));
+        if (ld.ok) ld.load(ring_v, item, tiles_b, &map_v, head, row, kRows, kRows);
       }
     }
-    ld.land(qdo_full, turns);
+    if (!ld.ok) {
+      ld.land(raw, ld.raw_turns);
+      ld.land(ring_k, item + 1);
+      ld.land(ring_v, item + 1);
+      ld.land(qdo_full, turns);
+    }
   } else if (warp == 8) {
     constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
     const int ksteps = (p.head_dim + 15) / 16;
-    const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile, ring_addr = tc::smem_u32(ring);
-    uint32_t item = 0, turns = 0, tile = 0;  // `tile` numbers the key tiles of the block
+    const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile;
+    uint32_t turns = 0, tile = 0;  // `tile` numbers the key tiles of the block, and the items of both rings
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && warp_wait(bar, parity & 1, abort_flag);
       tc::fence_after_sync();
     };
-    auto take = [&](uint32_t i) { wait(&full[i % kNS], i / kNS); };
-    auto scores = [&](uint32_t i, uint32_t buffer) {  // S = Q K^T
+    auto scores = [&](uint32_t i) {  // S = Q K^T
+      wait(ring_k.full_of(i), ring_k.parity(i));
       if (!ok) return;
       if (elect_one()) {
-        product_kk<DP>(tmem + buffer * 128, q_addr, ring_addr + (i % kNS) * R::kTile, ksteps);
-        tc::umma_commit(&s_full[buffer]);
+        product_kk<DP>(tmem + (i & 1) * 128, q_addr, ring_k.tile(i), ksteps);
+        tc::umma_commit(&s_full[i & 1]);
       }
       __syncwarp();
     };
     auto slopes = [&](uint32_t i, bool last) {  // dP = dO V^T, the last reader of V, and of Q and dO
+      wait(ring_v.full_of(i), ring_v.parity(i));
       if (!ok) return;
       if (elect_one()) {
-        product_kk<DP>(tmem + 256, do_addr, ring_addr + (i % kNS) * R::kTile, ksteps);
+        product_kk<DP>(tmem + 256, do_addr, ring_v.tile(i), ksteps);
         tc::umma_commit(dp_full);
-        tc::umma_commit(&empty[i % kNS]);
+        tc::umma_commit(ring_v.empty_of(i));
         if (last) tc::umma_commit(qdo_empty);
       }
       __syncwarp();
@@ -241,27 +266,19 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       const int n = tiles_of(e);
       wait(qdo_full, turns);
       ++turns;
-      take(item);  // items K_0 V_0 K_1 V_1 ...
-      scores(item, tile & 1);
-      take(item + 1);
-      slopes(item + 1, n == 1);
-      for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
-        if (j + 1 < n) {
-          take(item + 2);
-          scores(item + 2, (tile + 1) & 1);
-        }
+      scores(tile);
+      slopes(tile, n == 1);
+      for (int j = 0; ok && j < n; ++j, ++tile) {
+        if (j + 1 < n) scores(tile + 1);
         wait(ds_full, tile);
-        if (j + 1 < n) {
-          take(item + 3);
-          slopes(item + 3, j + 2 == n);
-        }
+        if (j + 1 < n) slopes(tile + 1, j + 2 == n);
         if (!ok) break;
         if (elect_one()) {
-          const uint32_t b = desc_mnmajor(ring_addr + (item % kNS) * R::kTile), a = tmem + (tile & 1) * 128;
+          const uint32_t b = desc_mnmajor(ring_k.tile(tile)), a = tmem + (tile & 1) * 128;
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)
             umma_ts(tmem + 384, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, j > 0 || kk > 0);
-          tc::umma_commit(&empty[item % kNS]);
+          tc::umma_commit(ring_k.empty_of(tile));
           if (j + 1 == n) tc::umma_commit(dq_done);
         }
         __syncwarp();
@@ -283,7 +300,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       const int head = (int)(u % p.n_kv_heads) * p.group + head_in;
       const bool valid = row < p.group * p.tq && token < e.seq_hi;
       const int64_t at = (int64_t)token * p.n_heads + head;
-      const float lse2 = valid ? p.lse2[at] : 0.f, delta = valid ? p.delta[at] : 0.f;
+      const float2 minus_lse2 = both(valid ? -p.lse2[at] : 0.f), minus_delta = both(valid ? -p.delta[at] : 0.f);
       for (int j = 0; j < n; ++j, ++tile) {
         ok = warp_wait(&s_full[tile & 1], (tile >> 1) & 1, abort_flag);
         if (!ok) break;
@@ -292,13 +309,21 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         float x[64], d[64];
         tmem_ld64(s_addr, x);
 #pragma unroll
-        for (int c = 0; c < 64; ++c) x[c] = ex2(fmaf(x[c], sc, -lse2));
+        for (int c = 0; c < 64; c += 2) {
+          const float2 w = weight(make_float2(x[c], x[c + 1]), both(sc), minus_lse2);
+          x[c] = w.x;
+          x[c + 1] = w.y;
+        }
         ok = warp_wait(dp_full, tile & 1, abort_flag);
         if (!ok) break;
         tc::fence_after_sync();
         tmem_ld64(tmem + 256 + mine, d);
 #pragma unroll
-        for (int c = 0; c < 64; ++c) x[c] *= d[c] - delta;
+        for (int c = 0; c < 64; c += 2) {
+          const float2 g = mul2(make_float2(x[c], x[c + 1]), add2(make_float2(d[c], d[c + 1]), minus_delta));
+          x[c] = g.x;
+          x[c + 1] = g.y;
+        }
         const int kv0 = e.seq_lo + j * kRows;
         if (kv0 + kRows - 1 > e.lo) {  // the tile touches the diagonal
           const int last = token - kv0 - half * 64;
@@ -334,7 +359,6 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
                 const BwdParams p) {
   using R = BwdShape<DP>;
-  constexpr int kNS = R::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   bool fits;
   uint8_t* smem = tile_base(smem_raw, R::kSlack, &fits);
@@ -342,13 +366,16 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     if (threadIdx.x == 0) atomicOr(p.status, NAT_DEV_TIMEOUT);
     return;
   }
-  uint8_t* ring = smem + 2 * R::kTile;
-  float* stats = reinterpret_cast<float*>(smem + R::kTiles);  // [2][lse2 | delta][128]
+  uint8_t *tiles_a = smem + 2 * R::kTile, *tiles_b = tiles_a + R::kA * R::kTile;
+  float* stats = reinterpret_cast<float*>(smem + R::kTiles);  // [2][-lse2 | -delta][128]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + R::kTiles + R::kStats);
-  uint64_t *kv_full = bars, *kv_empty = bars + 1, *s_full = bars + 2, *p_full = bars + 3, *dp_full = bars + 4;
-  uint64_t *ds_full = bars + 5, *done = bars + 6, *raw = bars + 7, *drain = bars + 8, *st_full = bars + 9;
-  uint64_t *st_empty = bars + 11, *full = bars + 13, *empty = bars + 13 + kNS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 13 + 2 * kNS);
+  // p_early: the first half of each thread's columns of P' is there
+  uint64_t *kv_full = bars, *kv_empty = bars + 1, *s_full = bars + 2, *dp_full = bars + 3, *done = bars + 4;
+  uint64_t *raw = bars + 5, *drain = bars + 6, *p_full = bars + 7, *ds_full = bars + 8, *p_early = bars + 9;
+  uint64_t *st_full = bars + 10, *st_empty = bars + 12;
+  const Ring<R::kA> ring_q{tc::smem_u32(tiles_a), bars + 14, bars + 14 + R::kA, R::kTile};
+  const Ring<R::kB> ring_do{tc::smem_u32(tiles_b), bars + 14 + 2 * R::kA, bars + 14 + 2 * R::kA + R::kB, R::kTile};
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * (R::kA + R::kB));
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
@@ -368,10 +395,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       tc::mbar_init(&st_full[s], 1);
       tc::mbar_init(&st_empty[s], 8);
     }
-    for (int s = 0; s < kNS; ++s) {
-      tc::mbar_init(&full[s], 1);
-      tc::mbar_init(&empty[s], 1);
-    }
+    tc::mbar_init(p_early, 256);
+    for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[14 + s], 1);
     *abort_flag = 0u;
     tc::fence_barrier_init();
   }
@@ -381,8 +406,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   }
   if (q_rows < kRows) {
     // rows that no load reaches are part of every contraction over queries: zero, once
-    for (uint32_t i = threadIdx.x; i < kNS * R::kTile / 16; i += blockDim.x)
-      reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (uint32_t i = threadIdx.x; i < (R::kA + R::kB) * R::kTile / 16; i += blockDim.x)
+      reinterpret_cast<uint4*>(tiles_a)[i] = make_uint4(0u, 0u, 0u, 0u);
     tc::fence_proxy_async();
   }
   tc::fence_before_sync();
@@ -393,11 +418,18 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   auto tiles_of = [&](const Entry& e) { return (e.seq_hi - e.lo + p.tq - 1) / p.tq; };
 
   if (warp == 9) {
-    Loader<DP> ld{ring, full, empty, raw, abort_flag, lane};
-    uint32_t turns = 0;
+    Loader<DP> ld{raw, abort_flag, lane};
+    uint32_t turns = 0, item = 0;
     for (uint32_t u = blockIdx.x; ld.ok && u < units; u += gridDim.x) {
       const Entry e = p.list[u / p.n_kv_heads];
       const int head = (int)(u % p.n_kv_heads), n = tiles_of(e);
+      auto load_q = [&](int j) {
+        const int row = e.lo + j * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
+        ld.load(ring_q, item, tiles_a, &map_q, head * p.group, row, q_rows, valid);
+      };
+      // the unit's first query tile does not wait for the end of the unit before
+      load_q(0);
+      if (!ld.ok) break;
       ld.ok = warp_wait(kv_empty, (turns & 1) ^ 1, abort_flag);
       if (!ld.ok) break;
       ++turns;
@@ -408,13 +440,18 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           tma_load_3d(tc::smem_u32(smem + R::kTile + c * kPanel), &map_v, kv_full, c * 64, head, e.lo);
         }
       }
-      for (int j = 0; ld.ok && j < n; ++j) {
+      for (int j = 0; ld.ok && j < n; ++j, ++item) {
+        if (j > 0) load_q(j);
         const int row = e.lo + j * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
-        ld.load(&map_q, head * p.group, row, q_rows, valid);
-        ld.load(&map_do, head * p.group, row, q_rows, valid);
+        if (ld.ok) ld.load(ring_do, item, tiles_b, &map_do, head * p.group, row, q_rows, valid);
       }
     }
-    ld.land(kv_full, turns);
+    if (!ld.ok) {
+      ld.land(raw, ld.raw_turns);
+      ld.land(ring_q, item + 1);
+      ld.land(ring_do, item + 1);
+      ld.land(kv_full, turns);
+    }
   } else if (warp == 10) {
     // lse and delta of the query rows, up to two tiles ahead
     uint32_t tile = 0;
@@ -429,8 +466,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         for (int i = 0; i < 4; ++i) {
           const int r = lane + 32 * i, token = first + r / p.group;
           const int64_t at = (int64_t)token * p.n_heads + head + r % p.group;
-          a[i] = r < valid ? __ldg(p.lse2 + at) : 0.f;
-          b[i] = r < valid ? __ldg(p.delta + at) : 0.f;
+          a[i] = r < valid ? -__ldg(p.lse2 + at) : 0.f;
+          b[i] = r < valid ? -__ldg(p.delta + at) : 0.f;
         }
         ok = warp_wait(&st_empty[tile & 1], ((tile >> 1) & 1) ^ 1, abort_flag);
         if (!ok) break;
@@ -444,55 +481,66 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   } else if (warp == 8) {
     constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
     const int ksteps = (p.head_dim + 15) / 16;
-    const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile, ring_addr = tc::smem_u32(ring);
-    uint32_t item = 0, turns = 0, tile = 0;
+    const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile;
+    uint32_t turns = 0, tile = 0;  // `tile` numbers the query tiles of the block, and the items of both rings
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && warp_wait(bar, parity & 1, abort_flag);
       tc::fence_after_sync();
     };
-    auto take = [&](uint32_t i) { wait(&full[i % kNS], i / kNS); };
-    auto product = [&](uint32_t d, uint32_t a, uint32_t i, uint64_t* bar) {
+    auto scores = [&](uint32_t i) {  // S' = K Q^T
+      wait(ring_q.full_of(i), ring_q.parity(i));
       if (!ok) return;
       if (elect_one()) {
-        product_kk<DP>(d, a, ring_addr + (i % kNS) * R::kTile, ksteps);
-        tc::umma_commit(bar);
+        product_kk<DP>(tmem, k_addr, ring_q.tile(i), ksteps);
+        tc::umma_commit(s_full);
       }
       __syncwarp();
     };
-    auto accumulate = [&](uint32_t d, uint32_t a, uint32_t i, bool add) {
+    auto slopes = [&](uint32_t i) {  // dP' = V dO^T
+      wait(ring_do.full_of(i), ring_do.parity(i));
       if (!ok) return;
       if (elect_one()) {
-        const uint32_t b = desc_mnmajor(ring_addr + (i % kNS) * R::kTile);
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk)
-          umma_ts(d, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, add || kk > 0);
-        tc::umma_commit(&empty[i % kNS]);
+        product_kk<DP>(tmem + 128, v_addr, ring_do.tile(i), ksteps);
+        tc::umma_commit(dp_full);
       }
       __syncwarp();
+    };
+    // steps first, first + 1 and first + 4, first + 5 of a product with P' or dS': a half of each thread's columns
+    auto half_steps = [&](uint32_t d, uint32_t a, uint32_t b, int first, bool add) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int kk = first + (k & 1) + (k >> 1) * 4;
+        umma_ts(d, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, add || k > 0);
+      }
     };
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
       const Entry e = p.list[u / p.n_kv_heads];
       const int n = tiles_of(e);
       wait(kv_full, turns);
       ++turns;
-      take(item);  // items Q_0 dO_0 Q_1 dO_1 ...
-      product(tmem, k_addr, item, s_full);
-      take(item + 1);
-      product(tmem + 128, v_addr, item + 1, dp_full);
-      for (int j = 0; ok && j < n; ++j, ++tile, item += 2) {
+      scores(tile);
+      slopes(tile);
+      for (int j = 0; ok && j < n; ++j, ++tile) {
+        const uint32_t dot = desc_mnmajor(ring_do.tile(tile)), qt = desc_mnmajor(ring_q.tile(tile));
+        wait(p_early, tile);  // dV += P' dO
+        if (ok && elect_one()) half_steps(tmem + 256, tmem, dot, 0, j > 0);
+        __syncwarp();
         wait(p_full, tile);
-        accumulate(tmem + 256, tmem, item + 1, j > 0);  // dV += P' dO
-        if (j + 1 < n) {
-          take(item + 2);
-          product(tmem, k_addr, item + 2, s_full);
+        if (ok && elect_one()) {
+          half_steps(tmem + 256, tmem, dot, 2, true);
+          tc::umma_commit(ring_do.empty_of(tile));
         }
-        wait(ds_full, tile);
-        accumulate(tmem + 384, tmem + 128, item, j > 0);  // dK += dS' Q
-        if (j + 1 < n) {
-          take(item + 3);
-          product(tmem + 128, v_addr, item + 3, dp_full);
+        __syncwarp();
+        if (j + 1 < n) scores(tile + 1);
+        wait(ds_full, tile);  // dK += dS' Q
+        if (ok && elect_one()) {
+          half_steps(tmem + 384, tmem + 128, qt, 0, j > 0);
+          half_steps(tmem + 384, tmem + 128, qt, 2, true);
+          tc::umma_commit(ring_q.empty_of(tile));
         }
+        __syncwarp();
+        if (j + 1 < n) slopes(tile + 1);
       }
       if (ok && elect_one()) {
         tc::umma_commit(done);
@@ -520,25 +568,34 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         tc::fence_after_sync();
         float x[64], d[64];
         tmem_ld64(tmem + mine, x);
-#pragma unroll
-        for (int c = 0; c < 64; c += 4) {
-          const float4 l = slot[c / 4];
-          x[c] = ex2(fmaf(x[c], sc, -l.x));
-          x[c + 1] = ex2(fmaf(x[c + 1], sc, -l.y));
-          x[c + 2] = ex2(fmaf(x[c + 2], sc, -l.z));
-          x[c + 3] = ex2(fmaf(x[c + 3], sc, -l.w));
-        }
         // columns of queries before the key, and of rows that are not there
         const bool edge = first < e.lo + kRows || rows < kRows;
         const int c_lo = (key - first) * p.group - half * 64, c_hi = rows - half * 64;
-        if (edge) {
+        uint32_t packed[16];
 #pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (c < c_lo || c >= c_hi) x[c] = 0.f;
+        for (int part = 0; part < 2; ++part) {  // dV's first half runs during the second half's exponentials
+#pragma unroll
+          for (int c = part * 32; c < part * 32 + 32; c += 4) {
+            const float4 l = slot[c / 4];
+            const float2 v = weight(make_float2(x[c], x[c + 1]), both(sc), make_float2(l.x, l.y));
+            const float2 w = weight(make_float2(x[c + 2], x[c + 3]), both(sc), make_float2(l.z, l.w));
+            x[c] = v.x;
+            x[c + 1] = v.y;
+            x[c + 2] = w.x;
+            x[c + 3] = w.y;
+          }
+          if (edge) {
+#pragma unroll
+            for (int c = part * 32; c < part * 32 + 32; ++c)
+              if (c < c_lo || c >= c_hi) x[c] = 0.f;
+          }
+#pragma unroll
+          for (int c = 0; c < 16; ++c) packed[c] = bf16_pair(x[part * 32 + 2 * c], x[part * 32 + 2 * c + 1]);
+          tmem_st16(tmem + mine + part * 16, packed);
+          tmem_st_wait();
+          tc::fence_before_sync();
+          tc::mbar_arrive(part == 0 ? p_early : p_full);
         }
-        store64(tmem + mine, x);
-        tc::fence_before_sync();
-        tc::mbar_arrive(p_full);
         ok = warp_wait(dp_full, tile & 1, abort_flag);
         if (!ok) break;
         tc::fence_after_sync();
@@ -546,10 +603,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll
         for (int c = 0; c < 64; c += 4) {
           const float4 l = slot[kRows / 4 + c / 4];
-          x[c] *= d[c] - l.x;
-          x[c + 1] *= d[c + 1] - l.y;
-          x[c + 2] *= d[c + 2] - l.z;
-          x[c + 3] *= d[c + 3] - l.w;
+          const float2 v = mul2(make_float2(x[c], x[c + 1]), add2(make_float2(d[c], d[c + 1]), make_float2(l.x, l.y)));
+          const float2 w = mul2(make_float2(x[c + 2], x[c + 3]), add2(make_float2(d[c + 2], d[c + 3]), make_float2(l.z, l.w)));
+          x[c] = v.x;
+          x[c + 1] = v.y;
+          x[c + 2] = w.x;
+          x[c + 3] = w.y;
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&st_empty[tile & 1]);
