@@ -185,7 +185,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     auto scores = [&](int t, uint32_t k_item, bool last) {
       if (elect_one()) {
         product_kk<DP>(tmem + t * 128, q_addr + t * R::kTile, ring_addr + (k_item % kNS) * R::kTile, ksteps);
-        tc::umma_commit(&s_full[t]);
+        tc::umma_commit(&s_full[t]);  // which also says that O += P V of the step before is complete
         if (last) tc::umma_commit(&q_empty[t]);
       }
       __syncwarp();
@@ -225,7 +225,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll
               for (int kk = half * 4; kk < half * 4 + 4; ++kk)
                 umma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, b + step_mnmajor(kk), kIdescO, j > 0 || kk > 0);
-              if (half == 1) tc::umma_commit(&o_done[t]);
+              if (half == 1 && j + 1 == w.nk[t]) tc::umma_commit(&o_done[t]);
             }
             __syncwarp();
           }
@@ -253,8 +253,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     // the maximum is taken before the scale, which therefore has to be positive: a negative one
     // gives its sign, and zero itself, to the scores
     const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f;
+    const bool wide = wide_rows(p.out, p.o_stride, p.head_dim);
     const float sc = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
-    uint32_t s_turns = 0, pv = 0;
+    uint32_t s_turns = 0, o_turns = 0;
     bool ok = true;
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
       const Unit w = unit_of(p, u);
@@ -297,10 +298,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           m = base = now;
         } else {
           const bool grow = valid && (now - m) * sc > kRescale;
-          if (__any_sync(0xFFFFFFFFu, grow)) {
-            ok = warp_wait(&o_done[t], (pv + j - 1) & 1, abort_flag);
-            if (!ok) break;
-            tc::fence_after_sync();
+          if (__any_sync(0xFFFFFFFFu, grow)) {  // O is at rest: s_full came after the step before
             const float f = grow ? ex2((m - now) * sc) : 1.f;
             if (grow) m = now;
             l *= f;
@@ -341,9 +339,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
       if (!ok) break;
       if (nk == 0) continue;
-      ok = warp_wait(&o_done[t], (pv + nk - 1) & 1, abort_flag);
+      ok = warp_wait(&o_done[t], o_turns & 1, abort_flag);
       if (!ok) break;
-      pv += nk;
+      ++o_turns;
       tc::fence_after_sync();
       const int head = w.head * p.group + head_in;
       const float inv = 1.f / l;
@@ -352,16 +350,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       for (int c = 0; c < DP / 32; ++c) {
         float o[32];
         tc::tmem_ld32(o_addr + c * 32, o);
-        if (valid) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float* x = o + 8 * i;
-            if (c * 32 + 8 * i < p.head_dim)
-              *reinterpret_cast<uint4*>(dst + c * 32 + 8 * i) =
-                  make_uint4(bf16_pair(x[0] * inv, x[1] * inv), bf16_pair(x[2] * inv, x[3] * inv),
-                             bf16_pair(x[4] * inv, x[5] * inv), bf16_pair(x[6] * inv, x[7] * inv));
-          }
-        }
+        if (valid) store_row32(dst + c * 32, o, inv, p.head_dim - c * 32, wide);
       }
       if (valid)
         p.lse[(int64_t)token * p.n_heads + head] = fmaf(m, sc * kLn2, logf(l));

@@ -9,7 +9,10 @@
 // in a fixed order: no atomics on dQ, no fp32 scratch for it, and results that repeat bit for bit.
 //
 // Warps: 0-3 and 4-7 take the two column halves of the score tile (a thread has 64 columns of one
-// row), 8 issues MMAs, 9 loads tiles by TMA, 10 (dkv) loads lse and delta of the query rows.
+// row), 9 loads tiles by TMA, 11 (dkv) loads lse and delta of the query rows, and 8 and 10 issue the MMAs:
+// the tensor pipe holds about one MMA beyond the running one, so with one issuing warp every wait and
+// every commit between two products leaves it idle.  In dkv the warps have a chain each, S' and dV, dP'
+// and dK, which share no tensor memory; in dq one has S, the other dP and dQ.
 #include <cuda.h>
 
 #include "nat_attn.cuh"
@@ -67,22 +70,14 @@ constexpr __device__ uint32_t half_cols(int kk) { return (uint32_t)(kk < 4 ? kk 
 
 // D columns [half * DP/2, ...) of an accumulator row, times f, to global memory.
 template <int DP>
-__device__ __forceinline__ void store_acc(uint32_t addr, int half, __nv_bfloat16* dst, int D, float f, bool valid) {
+__device__ __forceinline__ void store_acc(uint32_t addr, int half, __nv_bfloat16* dst, int D, float f, bool valid,
+                                          bool wide) {
 #pragma unroll
   for (int c = 0; c < DP / 64; ++c) {
     const int col = half * (DP / 2) + c * 32;
     float o[32];
     tc::tmem_ld32(addr + col, o);
-    if (valid) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* x = o + 8 * i;
-        if (col + 8 * i < D)
-          *reinterpret_cast<uint4*>(dst + col + 8 * i) =
-              make_uint4(bf16_pair(x[0] * f, x[1] * f), bf16_pair(x[2] * f, x[3] * f),
-                         bf16_pair(x[4] * f, x[5] * f), bf16_pair(x[6] * f, x[7] * f));
-      }
-    }
+    if (valid) store_row32(dst + col, o, f, D - col, wide);
   }
 }
 
@@ -146,8 +141,8 @@ struct Loader {
 
 // 32 score columns of one thread: P = exp(scale S - lse), the subtrahends one for the row or one a column.
 __device__ __forceinline__ float2 weight(float2 s, float2 scale, float2 minus_lse2) {
-  const float2 e = fma2(s, scale, minus_lse2);
-  return make_float2(ex2(e.x), ex2(e.y));
+  const float2 x = fma2(s, scale, minus_lse2);
+  return make_float2(ex2(x.x), ex2(x.y));
 }
 
 template <int DP>
@@ -176,14 +171,14 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 
   if (threadIdx.x == 0) {
     tc::mbar_init(qdo_full, 1);
-    tc::mbar_init(qdo_empty, 1);
+    tc::mbar_init(qdo_empty, 2);  // by both MMA warps
     tc::mbar_init(&s_full[0], 1);
     tc::mbar_init(&s_full[1], 1);
     tc::mbar_init(dp_full, 1);
     tc::mbar_init(ds_full, 256);
     tc::mbar_init(dq_done, 1);
     tc::mbar_init(raw, 1);
-    tc::mbar_init(drain, 1);
+    tc::mbar_init(drain, 2);
     for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[9 + s], 1);
     *abort_flag = 0u;
     tc::fence_barrier_init();
@@ -231,7 +226,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ld.land(ring_v, item + 1);
       ld.land(qdo_full, turns);
     }
-  } else if (warp == 8) {
+  } else if (warp == 8 || warp == 10) {
     constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
     const int ksteps = (p.head_dim + 15) / 16;
     const uint32_t q_addr = tc::smem_u32(smem), do_addr = q_addr + R::kTile;
@@ -241,47 +236,48 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ok = ok && warp_wait(bar, parity & 1, abort_flag);
       tc::fence_after_sync();
     };
-    auto scores = [&](uint32_t i) {  // S = Q K^T
-      wait(ring_k.full_of(i), ring_k.parity(i));
-      if (!ok) return;
-      if (elect_one()) {
-        product_kk<DP>(tmem + (i & 1) * 128, q_addr, ring_k.tile(i), ksteps);
-        tc::umma_commit(&s_full[i & 1]);
-      }
-      __syncwarp();
-    };
-    auto slopes = [&](uint32_t i, bool last) {  // dP = dO V^T, the last reader of V, and of Q and dO
-      wait(ring_v.full_of(i), ring_v.parity(i));
-      if (!ok) return;
-      if (elect_one()) {
-        product_kk<DP>(tmem + 256, do_addr, ring_v.tile(i), ksteps);
-        tc::umma_commit(dp_full);
-        tc::umma_commit(ring_v.empty_of(i));
-        if (last) tc::umma_commit(qdo_empty);
-      }
-      __syncwarp();
-    };
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
       const Entry e = p.list[u / p.n_kv_heads];
       const int n = tiles_of(e);
       wait(qdo_full, turns);
       ++turns;
-      scores(tile);
-      slopes(tile, n == 1);
-      for (int j = 0; ok && j < n; ++j, ++tile) {
-        if (j + 1 < n) scores(tile + 1);
-        wait(ds_full, tile);
-        if (j + 1 < n) slopes(tile + 1, j + 2 == n);
-        if (!ok) break;
-        if (elect_one()) {
-          const uint32_t b = desc_mnmajor(ring_k.tile(tile)), a = tmem + (tile & 1) * 128;
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            umma_ts(tmem + 384, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, j > 0 || kk > 0);
-          tc::umma_commit(ring_k.empty_of(tile));
-          if (j + 1 == n) tc::umma_commit(dq_done);
+      if (warp == 10) {
+        for (int j = 0; ok && j < n; ++j, ++tile) {  // S = Q K^T
+          wait(ring_k.full_of(tile), ring_k.parity(tile));
+          // the buffer's dS of two tiles before has been read when the K tile beside it is released
+          if (tile >= 2) wait(ring_k.empty_of(tile - 2), ring_k.parity(tile - 2));
+          if (ok && elect_one()) {
+            product_kk<DP>(tmem + (tile & 1) * 128, q_addr, ring_k.tile(tile), ksteps);
+            tc::umma_commit(&s_full[tile & 1]);
+            if (j + 1 == n) tc::umma_commit(qdo_empty);
+          }
+          __syncwarp();
         }
-        __syncwarp();
+      } else {
+        auto slopes = [&](uint32_t i, bool last) {  // dP = dO V^T
+          wait(ring_v.full_of(i), ring_v.parity(i));
+          if (ok && elect_one()) {
+            product_kk<DP>(tmem + 256, do_addr, ring_v.tile(i), ksteps);
+            tc::umma_commit(dp_full);
+            tc::umma_commit(ring_v.empty_of(i));
+            if (last) tc::umma_commit(qdo_empty);
+          }
+          __syncwarp();
+        };
+        slopes(tile, n == 1);
+        for (int j = 0; ok && j < n; ++j, ++tile) {
+          wait(ds_full, tile);
+          if (ok && elect_one()) {  // dQ += dS K, before dP of the next tile: S of the one after waits for it
+            const uint32_t b = desc_mnmajor(ring_k.tile(tile)), a = tmem + (tile & 1) * 128;
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)
+              umma_ts(tmem + 384, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, j > 0 || kk > 0);
+            tc::umma_commit(ring_k.empty_of(tile));
+            if (j + 1 == n) tc::umma_commit(dq_done);
+          }
+          __syncwarp();
+          if (j + 1 < n) slopes(tile + 1, j + 2 == n);
+        }
       }
     }
     if (elect_one()) tc::umma_commit(drain);
@@ -292,6 +288,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16, mine = lane_base + half * 64;
     const int token_in = row / p.group, head_in = row % p.group;
     const float sc = p.scale * kLog2e;
+    const bool wide = wide_rows(p.dq, p.q_stride, p.head_dim);
     uint32_t tile = 0, turns = 0;
     bool ok = true;
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
@@ -341,7 +338,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ++turns;
       tc::fence_after_sync();
       store_acc<DP>(tmem + 384 + lane_base, half,
-                    p.dq + (int64_t)token * p.q_stride + (int64_t)head * p.head_dim, p.head_dim, p.scale, valid);
+                    p.dq + (int64_t)token * p.q_stride + (int64_t)head * p.head_dim, p.head_dim, p.scale, valid, wide);
       tc::fence_before_sync();
     }
   }
@@ -383,20 +380,20 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 
   if (threadIdx.x == 0) {
     tc::mbar_init(kv_full, 1);
-    tc::mbar_init(kv_empty, 1);
+    tc::mbar_init(kv_empty, 2);  // by both MMA warps, like done and the slots of dO
     tc::mbar_init(s_full, 1);
     tc::mbar_init(p_full, 256);
     tc::mbar_init(dp_full, 1);
     tc::mbar_init(ds_full, 256);
-    tc::mbar_init(done, 1);
+    tc::mbar_init(done, 2);
     tc::mbar_init(raw, 1);
-    tc::mbar_init(drain, 1);
+    tc::mbar_init(drain, 2);
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&st_full[s], 1);
       tc::mbar_init(&st_empty[s], 8);
     }
     tc::mbar_init(p_early, 256);
-    for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[14 + s], 1);
+    for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[14 + s], s < 2 * R::kA + R::kB ? 1 : 2);
     *abort_flag = 0u;
     tc::fence_barrier_init();
   }
@@ -452,7 +449,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       ld.land(ring_do, item + 1);
       ld.land(kv_full, turns);
     }
-  } else if (warp == 10) {
+  } else if (warp == 11) {
     // lse and delta of the query rows, up to two tiles ahead
     uint32_t tile = 0;
     bool ok = true;
@@ -478,7 +475,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (lane == 0) tc::mbar_arrive(&st_full[tile & 1]);
       }
     }
-  } else if (warp == 8) {
+  } else if (warp == 8 || warp == 10) {
     constexpr uint32_t kIdescD = tc::instr_desc_bf16(128, DP, 0, 1);
     const int ksteps = (p.head_dim + 15) / 16;
     const uint32_t k_addr = tc::smem_u32(smem), v_addr = k_addr + R::kTile;
@@ -487,24 +484,6 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && warp_wait(bar, parity & 1, abort_flag);
       tc::fence_after_sync();
-    };
-    auto scores = [&](uint32_t i) {  // S' = K Q^T
-      wait(ring_q.full_of(i), ring_q.parity(i));
-      if (!ok) return;
-      if (elect_one()) {
-        product_kk<DP>(tmem, k_addr, ring_q.tile(i), ksteps);
-        tc::umma_commit(s_full);
-      }
-      __syncwarp();
-    };
-    auto slopes = [&](uint32_t i) {  // dP' = V dO^T
-      wait(ring_do.full_of(i), ring_do.parity(i));
-      if (!ok) return;
-      if (elect_one()) {
-        product_kk<DP>(tmem + 128, v_addr, ring_do.tile(i), ksteps);
-        tc::umma_commit(dp_full);
-      }
-      __syncwarp();
     };
     // steps first, first + 1 and first + 4, first + 5 of a product with P' or dS': a half of each thread's columns
     auto half_steps = [&](uint32_t d, uint32_t a, uint32_t b, int first, bool add) {
@@ -519,28 +498,52 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       const int n = tiles_of(e);
       wait(kv_full, turns);
       ++turns;
-      scores(tile);
-      slopes(tile);
-      for (int j = 0; ok && j < n; ++j, ++tile) {
-        const uint32_t dot = desc_mnmajor(ring_do.tile(tile)), qt = desc_mnmajor(ring_q.tile(tile));
-        wait(p_early, tile);  // dV += P' dO
-        if (ok && elect_one()) half_steps(tmem + 256, tmem, dot, 0, j > 0);
-        __syncwarp();
-        wait(p_full, tile);
-        if (ok && elect_one()) {
-          half_steps(tmem + 256, tmem, dot, 2, true);
-          tc::umma_commit(ring_do.empty_of(tile));
+      if (warp == 8) {
+        auto scores = [&](uint32_t i) {  // S' = K Q^T
+          wait(ring_q.full_of(i), ring_q.parity(i));
+          if (ok && elect_one()) {
+            product_kk<DP>(tmem, k_addr, ring_q.tile(i), ksteps);
+            tc::umma_commit(s_full);
+          }
+          __syncwarp();
+        };
+        scores(tile);
+        for (int j = 0; ok && j < n; ++j, ++tile) {  // dV += P' dO
+          const uint32_t b = desc_mnmajor(ring_do.tile(tile));
+          wait(ring_do.full_of(tile), ring_do.parity(tile));
+          wait(p_early, tile);
+          if (ok && elect_one()) half_steps(tmem + 256, tmem, b, 0, j > 0);
+          __syncwarp();
+          wait(p_full, tile);
+          if (ok && elect_one()) {
+            half_steps(tmem + 256, tmem, b, 2, true);
+            tc::umma_commit(ring_do.empty_of(tile));
+          }
+          __syncwarp();
+          if (j + 1 < n) scores(tile + 1);
         }
-        __syncwarp();
-        if (j + 1 < n) scores(tile + 1);
-        wait(ds_full, tile);  // dK += dS' Q
-        if (ok && elect_one()) {
-          half_steps(tmem + 384, tmem + 128, qt, 0, j > 0);
-          half_steps(tmem + 384, tmem + 128, qt, 2, true);
-          tc::umma_commit(ring_q.empty_of(tile));
+      } else {
+        auto slopes = [&](uint32_t i) {  // dP' = V dO^T
+          wait(ring_do.full_of(i), ring_do.parity(i));
+          if (ok && elect_one()) {
+            product_kk<DP>(tmem + 128, v_addr, ring_do.tile(i), ksteps);
+            tc::umma_commit(dp_full);
+            tc::umma_commit(ring_do.empty_of(i));
+          }
+          __syncwarp();
+        };
+        slopes(tile);
+        for (int j = 0; ok && j < n; ++j, ++tile) {  // dK += dS' Q; S' of this tile was done before dS'
+          const uint32_t b = desc_mnmajor(ring_q.tile(tile));
+          wait(ds_full, tile);
+          if (ok && elect_one()) {
+            half_steps(tmem + 384, tmem + 128, b, 0, j > 0);
+            half_steps(tmem + 384, tmem + 128, b, 2, true);
+            tc::umma_commit(ring_q.empty_of(tile));
+          }
+          __syncwarp();
+          if (j + 1 < n) slopes(tile + 1);
         }
-        __syncwarp();
-        if (j + 1 < n) slopes(tile + 1);
       }
       if (ok && elect_one()) {
         tc::umma_commit(done);
@@ -555,6 +558,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const int half = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u << 16, mine = lane_base + half * 64;
     const float sc = p.scale * kLog2e;
+    const bool wide = wide_rows(p.dk, p.k_stride, p.head_dim) && wide_rows(p.dv, p.v_stride, p.head_dim);
     uint32_t tile = 0, turns = 0;
     bool ok = true;
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
@@ -628,8 +632,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       tc::fence_after_sync();
       const bool valid = key < e.seq_hi;
       const int64_t col = (int64_t)(u % p.n_kv_heads) * p.head_dim;
-      store_acc<DP>(tmem + 256 + lane_base, half, p.dv + (int64_t)key * p.v_stride + col, p.head_dim, 1.f, valid);
-      store_acc<DP>(tmem + 384 + lane_base, half, p.dk + (int64_t)key * p.k_stride + col, p.head_dim, p.scale, valid);
+      store_acc<DP>(tmem + 256 + lane_base, half, p.dv + (int64_t)key * p.v_stride + col, p.head_dim, 1.f, valid, wide);
+      store_acc<DP>(tmem + 384 + lane_base, half, p.dk + (int64_t)key * p.k_stride + col, p.head_dim, p.scale, valid, wide);
       tc::fence_before_sync();
     }
   }

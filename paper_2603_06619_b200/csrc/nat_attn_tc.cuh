@@ -146,6 +146,34 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
+// Whether every head's row of a tensor starts on a 32-byte boundary.
+__device__ __forceinline__ bool wide_rows(const void* base, int64_t stride, int head_dim) {
+  return (((uintptr_t)base | (uintptr_t)(stride * 2) | (uintptr_t)(head_dim * 2)) & 31u) == 0;
+}
+
+// 32 columns of a row, times f, rounded; columns at or after `left` are not there.  Each lane writes a
+// row of its own, so the stores' cost is their number times 32 lines: 32 bytes at a time where
+// the alignment allows.
+__device__ __forceinline__ void store_row32(__nv_bfloat16* dst, const float* o, float f, int left, bool wide) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = bf16_pair(o[2 * i] * f, o[2 * i + 1] * f);
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (16 * i < left)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 16 * i), "r"(w[8 * i]),
+                     "r"(w[8 * i + 1]), "r"(w[8 * i + 2]), "r"(w[8 * i + 3]), "r"(w[8 * i + 4]), "r"(w[8 * i + 5]),
+                     "r"(w[8 * i + 6]), "r"(w[8 * i + 7])
+                     : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (8 * i < left)
+        *reinterpret_cast<uint4*>(dst + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+
 // A wait of a whole warp: all lanes go on, or all give up.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
   return __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar, parity, abort_flag));
