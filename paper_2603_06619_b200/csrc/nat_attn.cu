@@ -14,19 +14,17 @@ constexpr int kBuckets = 1024;
 // Sequence bounds are clamped to [0, cap], so no list entry points outside the buffers whatever
 // cu_seqlens holds.
 struct PlanArgs {
-  const int32_t* cu;
-  int32_t B;
-  int64_t cap, max_entries;
-  int tile, by_rest, which;
+  Batch batch;
+  int by_rest, which;
   Entry* list;
   Head* head;
 };
 
 __device__ __forceinline__ void plan(const PlanArgs& a) {
-  const int32_t* cu = a.cu;
-  const int32_t B = a.B;
-  const int64_t cap = a.cap, max_entries = a.max_entries;
-  const int tile = a.tile, by_rest = a.by_rest;
+  const int32_t* cu = a.batch.cu;
+  const int32_t B = a.batch.B;
+  const int64_t cap = a.batch.cap, max_entries = a.batch.max_entries;
+  const int tile = a.batch.tile, by_rest = a.by_rest;
   Entry* list = a.list;
   __shared__ uint32_t bucket[kBuckets];
   __shared__ int longest;
@@ -34,11 +32,7 @@ __device__ __forceinline__ void plan(const PlanArgs& a) {
   bucket[threadIdx.x] = 0u;
   if (threadIdx.x == 0) longest = 0;
   __syncthreads();
-  auto bounds = [&](int i, int& lo, int& hi) {
-    lo = (int)min((int64_t)max(cu[i], 0), cap);
-    hi = (int)min((int64_t)max(cu[i + 1], 0), cap);
-    if (hi < lo) hi = lo;
-  };
+  auto bounds = [&](int i, int& lo, int& hi) { sequence_bounds(cu, i, cap, lo, hi); };
   for (int i = threadIdx.x; i < B; i += blockDim.x) {
     int lo, hi;
     bounds(i, lo, hi);
@@ -76,17 +70,19 @@ __device__ __forceinline__ void plan(const PlanArgs& a) {
       if (threadIdx.x == kBuckets - 1) {
         const uint32_t total = before + run;
         a.head->count[a.which] = (uint32_t)min((int64_t)total, max_entries);
-        // more rows than the buffers hold, or bounds that are not ascending; a call's plans find the same
-        a.head->status = ((int64_t)cu[B] > cap || total > max_entries) ? NAT_DEV_CAPACITY : 0u;
+        a.head->status = batch_status(a.batch, total);  // a call's plans find the same
       }
       __syncthreads();
     }
   }
 }
 
-__global__ void __launch_bounds__(1024) plan_kernel(PlanArgs a) { plan(a); }
+__global__ void __launch_bounds__(1024) plan_kernel(PlanArgs a) {
+  release_secondary();
+  plan(a);
+}
 
-// What both kernels of the bfloat16 backward pass read, in one launch: their plans (blocks 0 and 1)
+// What the bfloat16 backward pass reads, in one launch: its plans (blocks 0 and 1, where it needs them)
 // and, for every row of out, delta = dout . out and lse in units of log 2.  Bound by the read of
 // out and dout.  Half a warp takes a row's 16-byte pieces.
 struct StatsArgs {
@@ -97,16 +93,17 @@ struct StatsArgs {
   int n_heads, head_dim;
 };
 
-__global__ void __launch_bounds__(1024) bwd_prologue_kernel(PlanArgs a, PlanArgs b, StatsArgs s) {
-  if (blockIdx.x < 2) {
+__global__ void __launch_bounds__(1024) bwd_prologue_kernel(PlanArgs a, PlanArgs b, StatsArgs s, unsigned plans) {
+  release_secondary();
+  if (blockIdx.x < plans) {
     plan(blockIdx.x == 0 ? a : b);
     return;
   }
-  const int64_t rows = min((int64_t)max(a.cu[a.B], 0), a.cap) * s.n_heads;
+  const int64_t rows = min((int64_t)max(a.batch.cu[a.batch.B], 0), a.batch.cap) * s.n_heads;
   const int lane = threadIdx.x & 15;
-  const int64_t step = (int64_t)(gridDim.x - 2) * 64;
+  const int64_t step = (int64_t)(gridDim.x - plans) * 64;
   // the bound is the block's: both halves of a warp take the same turns
-  for (int64_t base = (int64_t)(blockIdx.x - 2) * 64; base < rows; base += step) {
+  for (int64_t base = (int64_t)(blockIdx.x - plans) * 64; base < rows; base += step) {
     const int64_t row = base + (threadIdx.x >> 4);
     float dot = 0.f;
     if (row < rows && lane * 8 < s.head_dim) {
@@ -197,10 +194,13 @@ Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
   return l;
 }
 
+Batch batch(const Args& a, const Layout& l, Plan which) {
+  return {a.cu_seqlens, a.B, plan_tile(a.p, which), a.cap, l.entries[which]};
+}
+
 namespace {
 PlanArgs plan_args(const Args& a, const Layout& l, Plan which) {
-  return {a.cu_seqlens, a.B, a.cap, l.entries[which], plan_tile(a.p, which), which == kPlanDkv ? 1 : 0,
-          (int)which, entries(a, l, which), head(a)};
+  return {batch(a, l, which), which == kPlanDkv ? 1 : 0, (int)which, entries(a, l, which), head(a)};
 }
 }  // namespace
 
@@ -210,13 +210,28 @@ int launch_plan(const Args& a, const Layout& l, Plan which) {
   return NAT_OK;
 }
 
-int launch_bwd_prologue(const Args& a, const Layout& l) {
+int launch_bwd_prologue(const Args& a, const Layout& l, bool plans) {
   const StatsArgs s{(const __nv_bfloat16*)a.out, (const __nv_bfloat16*)a.dout, a.lse, lse2(a, l),
                     delta(a, l), a.p.o_stride, a.p.n_heads, a.p.head_dim};
   const int64_t want = (a.cap * a.p.n_heads + 63) / 64;
-  const unsigned blocks = 2 + (unsigned)min(want, (int64_t)148 * 2 * 4);
-  bwd_prologue_kernel<<<blocks, 1024, 0, a.stream>>>(plan_args(a, l, kPlanDq), plan_args(a, l, kPlanDkv), s);
+  const unsigned first = plans ? 2 : 0, blocks = first + (unsigned)min(want, (int64_t)148 * 2 * 4);
+  bwd_prologue_kernel<<<blocks, 1024, 0, a.stream>>>(plan_args(a, l, kPlanDq), plan_args(a, l, kPlanDkv), s, first);
   NAT_LAUNCH_CHECK("bwd_prologue_kernel");
+  return NAT_OK;
+}
+
+int device(Device* d) {
+  static std::atomic<int> sms[64];  // 0: not asked yet
+  NAT_CUDA(cudaGetDevice(&d->index));
+  if (d->index < 0 || d->index >= 64)
+    return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", d->index);
+  d->sms = sms[d->index].load(std::memory_order_relaxed);
+  if (d->sms == 0) {
+    const int s = require_sm100();
+    if (s != NAT_OK) return s;
+    NAT_CUDA(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->index));
+    sms[d->index].store(d->sms, std::memory_order_relaxed);
+  }
   return NAT_OK;
 }
 

@@ -4,6 +4,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <atomic>
 #include <cstdint>
 
 #include "nat_common.cuh"
@@ -25,6 +26,13 @@ struct Args {
   cudaStream_t stream;
 };
 
+// Sequence i of a batch, clamped to [0, cap] whatever cu_seqlens holds.
+__device__ __forceinline__ void sequence_bounds(const int32_t* cu, int i, int64_t cap, int& lo, int& hi) {
+  lo = (int)min((int64_t)max(__ldg(cu + i), 0), cap);
+  hi = (int)min((int64_t)max(__ldg(cu + i + 1), 0), cap);
+  if (hi < lo) hi = lo;
+}
+
 // Head of the workspace.  `status` is first, where nat_poll_status reads it.
 struct Head {
   uint32_t status;
@@ -35,6 +43,51 @@ struct Head {
 struct Entry {
   int32_t seq_lo, seq_hi, lo, pad;
 };
+
+// The batch itself, for kernels that find their tile without a list.
+struct Batch {
+  const int32_t* cu;
+  int32_t B;
+  int tile;
+  int64_t cap, max_entries;
+};
+
+// Tile number `index` of all tiles in the sequences' order (for one warp; the same in every lane), and how
+// many there are.  Where there are no more tiles than blocks their order does not matter, and the
+// search, a few hundred cycles for every 32 sequences, is cheaper than a kernel that sorts them.
+__device__ __forceinline__ Entry find_entry(const Batch& b, uint32_t index, uint32_t* total) {
+  const int lane = threadIdx.x & 31;
+  uint32_t before = 0u;
+  Entry found{0, 0, 0, 0};
+  for (int base = 0; base < b.B; base += 32) {
+    int lo = 0, hi = 0;
+    if (base + lane < b.B) sequence_bounds(b.cu, base + lane, b.cap, lo, hi);
+    const uint32_t tiles = (uint32_t)((hi - lo + b.tile - 1) / b.tile);
+    uint32_t run = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+      if (lane >= o) run += left;
+    }
+    const uint32_t first = before + run - tiles;
+    const bool mine = index >= first && index < first + tiles;
+    const uint32_t who = __ballot_sync(0xFFFFFFFFu, mine);
+    if (who) {
+      const int from = __ffs(who) - 1;
+      found.seq_lo = __shfl_sync(0xFFFFFFFFu, lo, from);
+      found.seq_hi = __shfl_sync(0xFFFFFFFFu, hi, from);
+      found.lo = found.seq_lo + (int)(index - __shfl_sync(0xFFFFFFFFu, first, from)) * b.tile;
+    }
+    before += __shfl_sync(0xFFFFFFFFu, run, 31);
+  }
+  *total = before;
+  return found;
+}
+
+// What a call finds wrong with its batch: more rows than the buffers hold, or bounds that do not ascend.
+__device__ __forceinline__ uint32_t batch_status(const Batch& b, uint32_t total) {
+  return ((int64_t)__ldg(b.cu + b.B) > b.cap || total > b.max_entries) ? NAT_DEV_CAPACITY : 0u;
+}
 
 enum Plan { kPlanFwd = 0, kPlanDq = 1, kPlanDkv = 2 };
 
@@ -61,8 +114,48 @@ inline float* lse2(const Args& a, const Layout& l) {
 
 // Writes the plan of `which` and the status word.
 int launch_plan(const Args& a, const Layout& l, Plan which);
-// Both plans of the bfloat16 backward pass, delta and lse2.
-int launch_bwd_prologue(const Args& a, const Layout& l);
+// delta and lse2 of the bfloat16 backward pass, and (with `plans`) both its plans.
+int launch_bwd_prologue(const Args& a, const Layout& l, bool plans);
+
+Batch batch(const Args& a, const Layout& l, Plan which);
+
+// Facts of the current device, asked for once.
+struct Device {
+  int index, sms;
+};
+int device(Device* d);
+
+// Kernel launches that may begin before the kernel in front of them on the stream has ended: such a
+// kernel calls wait_for_primary() before it touches anything that one wrote.
+__device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void release_secondary() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... P, typename... A>
+int launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t stream,
+                 const char* name, const A&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const int s = check_cuda(cudaLaunchKernelEx(&cfg, kernel, args...), name);
+  if (s != NAT_OK) return s;
+  NAT_LAUNCH_CHECK(name);
+  return NAT_OK;
+}
+
+// Raises a kernel's shared-memory limit, once for each device.
+template <typename K>
+int allow_smem(K kernel, size_t smem, const Device& d, std::atomic<uint64_t>* devices) {
+  if (devices->load(std::memory_order_relaxed) >> d.index & 1u) return NAT_OK;
+  NAT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  devices->fetch_or(1ull << d.index, std::memory_order_relaxed);
+  return NAT_OK;
+}
 
 int f32_fwd(const Args& a, const Layout& l);
 int f32_bwd(const Args& a, const Layout& l);

@@ -26,7 +26,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescale = 8.f;  // growth of a row's maximum (log2) that is left in P
 
 struct FwdParams {
-  const Entry* list;
+  const Entry* list;  // null where every block has one unit at most and finds it itself
+  Batch batch;
   const uint32_t* count;
   uint32_t* status;
   __nv_bfloat16* out;
@@ -48,8 +49,8 @@ struct FwdShape {
 struct Unit {
   int seq_lo, seq_hi, lo, head, nk[2], kv_hi;
 };
-__device__ __forceinline__ Unit unit_of(const FwdParams& p, uint32_t u) {
-  const Entry e = p.list[u / p.n_kv_heads];
+__device__ __forceinline__ Unit unit_of(const FwdParams& p, const Entry* found, uint32_t u) {
+  const Entry e = p.list ? p.list[u / p.n_kv_heads] : *found;
   Unit w;
   w.seq_lo = e.seq_lo;
   w.seq_hi = e.seq_hi;
@@ -79,8 +80,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint64_t *full = bars + 14, *empty = bars + 14 + kNS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * kNS);
   volatile uint32_t* abort_flag = tmem_slot + 1;
+  Entry* found = reinterpret_cast<Entry*>(tmem_slot + 4);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
 
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
@@ -104,10 +105,21 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     tc::tmem_alloc(tmem_slot, 512);
     tc::tmem_relinquish();
   }
+  if (warp == 9 && !p.list) {
+    uint32_t total;
+    const Entry e = find_entry(p.batch, blockIdx.x / p.n_kv_heads, &total);
+    if (lane == 0) {
+      *found = e;
+      tmem_slot[2] = total;
+      if (blockIdx.x == 0) *p.status = batch_status(p.batch, total);
+    }
+  }
+  wait_for_primary();
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = uniform(*tmem_slot);
+  const uint32_t units = (p.list ? *p.count : tmem_slot[2]) * (uint32_t)p.n_kv_heads;
 
   // 168 registers a thread at launch: the softmax warpgroups, which hold a row of scores, take
   // some of the third's (2 x 192 + 120 = 3 x 168)
@@ -153,7 +165,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     };
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of(p, u);
+      const Unit w = unit_of(p, found, u);
       const int n = max(w.nk[0], w.nk[1]);
       for (int j = 0; ok && j < n; ++j) {
         if (j == 0) load_q(w, 0);
@@ -195,7 +207,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       __syncwarp();
     };
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of(p, u);
+      const Unit w = unit_of(p, found, u);
       const int n = max(w.nk[0], w.nk[1]);
       // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
       wait(&full[item % kNS], item / kNS);
@@ -258,7 +270,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     uint32_t s_turns = 0, o_turns = 0;
     bool ok = true;
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of(p, u);
+      const Unit w = unit_of(p, found, u);
       const int nk = w.nk[t], first = w.lo + t * p.tq, token = first + token_in;
       const bool valid = row < p.group * p.tq && token < w.seq_hi;
       float m = -INFINITY, l = 0.f;
@@ -404,33 +416,29 @@ int make_map(CUtensorMap* map, const void* base, int D, int heads, int64_t cap, 
   return NAT_OK;
 }
 
-int sm_count(int* n) {
-  int dev = 0;
-  NAT_CUDA(cudaGetDevice(&dev));
-  NAT_CUDA(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
-  return NAT_OK;
-}
-
 namespace {
 
 template <int DP>
 int fwd(const Args& a, const Layout& l) {
   const nat_attn_params& p = a.p;
   const int group = p.n_heads / p.n_kv_heads, tq = kRows / group;
-  int sms = 0;
-  int s = require_sm100();
-  if (s == NAT_OK) s = sm_count(&sms);
+  Device dev;
+  int s = device(&dev);
   CUtensorMap mq, mk, mv;
   if (s == NAT_OK) s = make_map(&mq, a.q, p.head_dim, p.n_heads, a.cap, p.q_stride, group, tq);
   if (s == NAT_OK) s = make_map(&mk, a.k, p.head_dim, p.n_kv_heads, a.cap, p.k_stride, 1, kRows);
   if (s == NAT_OK) s = make_map(&mv, a.v, p.head_dim, p.n_kv_heads, a.cap, p.v_stride, 1, kRows);
   if (s != NAT_OK) return s;
-  NAT_CUDA(cudaFuncSetAttribute(attn_fwd_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)FwdShape<DP>::kSmem));
-  s = launch_plan(a, l, kPlanFwd);
+  static std::atomic<uint64_t> allowed;
+  s = allow_smem(attn_fwd_kernel<DP>, FwdShape<DP>::kSmem, dev, &allowed);
+  if (s != NAT_OK) return s;
+  const int64_t units = l.entries[kPlanFwd] * p.n_kv_heads;
+  const bool plan = units > dev.sms;
+  if (plan) s = launch_plan(a, l, kPlanFwd);
   if (s != NAT_OK) return s;
   FwdParams fp{};
-  fp.list = entries(a, l, kPlanFwd);
+  fp.list = plan ? entries(a, l, kPlanFwd) : nullptr;
+  fp.batch = batch(a, l, kPlanFwd);
   fp.count = &head(a)->count[kPlanFwd];
   fp.status = &head(a)->status;
   fp.out = (__nv_bfloat16*)a.out;
@@ -442,9 +450,10 @@ int fwd(const Args& a, const Layout& l) {
   fp.tq = tq;
   fp.head_dim = p.head_dim;
   fp.scale = p.scale;
-  const int64_t units = l.entries[kPlanFwd] * p.n_kv_heads;
-  const unsigned grid = (unsigned)min((int64_t)sms, units);
-  attn_fwd_kernel<DP><<<grid, 384, FwdShape<DP>::kSmem, a.stream>>>(mq, mk, mv, fp);
+  const unsigned grid = (unsigned)min((int64_t)dev.sms, units);
+  const size_t smem = FwdShape<DP>::kSmem;
+  if (plan) return launch_after(attn_fwd_kernel<DP>, grid, 384, smem, a.stream, "attn_fwd_kernel", mq, mk, mv, fp);
+  attn_fwd_kernel<DP><<<grid, 384, smem, a.stream>>>(mq, mk, mv, fp);
   NAT_LAUNCH_CHECK("attn_fwd_kernel");
   return NAT_OK;
 }

@@ -1,11 +1,12 @@
 // Backward pass of the packed causal attention on the tensor cores, bfloat16.
 //
-// Two kernels, both persistent with one block per multiprocessor, each forming P = exp(S - lse) anew:
+// Two parts, both persistent with one block per multiprocessor, each forming P = exp(S - lse) anew; one
+// launch holds the blocks of the first part and, behind them, those of the second:
 //   dq   a row tile of queries (heads of a group folded in) against its keys: S = Q K^T,
 //        dP = dO V^T, dS = P (dP - delta), dQ += dS K                      (three products)
 //   dkv  a tile of 128 keys against all later queries of its group, transposed: S' = K Q^T,
 //        dP' = V dO^T, dV += P' dO, dK += dS' Q                            (four products)
-// Seven products where one kernel over both would do five, but every sum stays in tensor memory and
+// Seven products where one part for both would do five, but every sum stays in tensor memory and
 // in a fixed order: no atomics on dQ, no fp32 scratch for it, and results that repeat bit for bit.
 //
 // Warps: 0-3 and 4-7 take the two column halves of the score tile (a thread has 64 columns of one
@@ -23,7 +24,8 @@ namespace attn {
 namespace {
 
 struct BwdParams {
-  const Entry* list;
+  const Entry* list;  // null where every block has one unit at most and finds it itself
+  Batch batch;
   const uint32_t* count;
   uint32_t* status;
   const float *lse2, *delta;  // [cap, n_heads]
@@ -44,8 +46,25 @@ struct BwdShape {
   static constexpr uint32_t kTiles = (2 + kA + kB) * kTile;
   static constexpr uint32_t kStats = 2 * 2 * kRows * 4;   // lse2 and delta of two row tiles
   static constexpr uint32_t kSlack = 768;                 // room to round the base up to 1024 bytes
-  static constexpr uint32_t kSmem = kTiles + kStats + 256 + kSlack;
+  static constexpr uint32_t kBars = DP == 128 ? 256 : 384;  // barriers, then what Found describes
+  static constexpr uint32_t kSmem = kTiles + kStats + kBars + kSlack;
 };
+
+// Behind the barriers: the address of the block's tensor memory, its abort flag and, without a list, its
+// tile and their number.
+struct Found {
+  uint32_t tmem, abort, total, pad;
+  Entry entry;
+};
+__device__ __forceinline__ void find(const BwdParams& p, uint32_t block, Found* f, bool report) {
+  uint32_t total;
+  const Entry e = find_entry(p.batch, block / p.n_kv_heads, &total);
+  if ((threadIdx.x & 31) == 0) {
+    f->entry = e;
+    f->total = total;
+    if (report && block == 0) *p.status = batch_status(p.batch, total);
+  }
+}
 
 // The tiles need a 1024-byte aligned base.  Dynamic shared memory starts on such a boundary where a
 // kernel has no static shared memory; should it not, the block reports it and does nothing.
@@ -146,10 +165,9 @@ __device__ __forceinline__ float2 weight(float2 s, float2 scale, float2 minus_ls
 }
 
 template <int DP>
-__global__ void __launch_bounds__(384, 1)
-attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
-               const BwdParams p) {
+__device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                        const CUtensorMap& map_do, const BwdParams& p, uint32_t block,
+                                        uint32_t blocks) {
   using R = BwdShape<DP>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   bool fits;
@@ -164,10 +182,9 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   uint64_t *dq_done = bars + 6, *raw = bars + 7, *drain = bars + 8;
   const Ring<R::kA> ring_k{tc::smem_u32(tiles_a), bars + 9, bars + 9 + R::kA, R::kTile};
   const Ring<R::kB> ring_v{tc::smem_u32(tiles_b), bars + 9 + 2 * R::kA, bars + 9 + 2 * R::kA + R::kB, R::kTile};
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9 + 2 * (R::kA + R::kB));
-  volatile uint32_t* abort_flag = tmem_slot + 1;
+  Found* const found = reinterpret_cast<Found*>(bars + ((9 + 2 * (R::kA + R::kB) + 1) & ~1));
+  volatile uint32_t* abort_flag = &found->abort;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
 
   if (threadIdx.x == 0) {
     tc::mbar_init(qdo_full, 1);
@@ -184,13 +201,17 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     tc::fence_barrier_init();
   }
   if (warp == 8) {
-    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_alloc(&found->tmem, 512);
     tc::tmem_relinquish();
   }
+  if (warp == 9 && !p.list) find(p, block, found, true);
+  wait_for_primary();
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = uniform(*tmem_slot);  // S/dS in two buffers, dP, dQ: 128 columns each
+  const uint32_t tmem = uniform(found->tmem);  // S/dS in two buffers, dP, dQ: 128 columns each
+  const uint32_t units = (p.list ? *p.count : found->total) * (uint32_t)p.n_kv_heads;
+  auto entry_of = [&](uint32_t u) { return p.list ? p.list[u / p.n_kv_heads] : found->entry; };
   // tiles of keys of a list entry
   auto tiles_of = [&](const Entry& e) { return (min(e.lo + p.tq, e.seq_hi) - e.seq_lo + kRows - 1) / kRows; };
 
@@ -198,8 +219,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     Loader<DP> ld{raw, abort_flag, lane};
     uint32_t turns = 0, item = 0;
     const int q_rows = p.group * p.tq;
-    for (uint32_t u = blockIdx.x; ld.ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ld.ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int head = (int)(u % p.n_kv_heads), n = tiles_of(e);
       ld.ok = warp_wait(qdo_empty, (turns & 1) ^ 1, abort_flag);
       if (!ld.ok) break;
@@ -236,8 +257,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       ok = ok && warp_wait(bar, parity & 1, abort_flag);
       tc::fence_after_sync();
     };
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int n = tiles_of(e);
       wait(qdo_full, turns);
       ++turns;
@@ -291,8 +312,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const bool wide = wide_rows(p.dq, p.q_stride, p.head_dim);
     uint32_t tile = 0, turns = 0;
     bool ok = true;
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int n = tiles_of(e), token = e.lo + token_in;
       const int head = (int)(u % p.n_kv_heads) * p.group + head_in;
       const bool valid = row < p.group * p.tq && token < e.seq_hi;
@@ -351,10 +372,9 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 }
 
 template <int DP>
-__global__ void __launch_bounds__(384, 1)
-attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
-                const BwdParams p) {
+__device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                        const CUtensorMap& map_do, const BwdParams& p, uint32_t block,
+                                        uint32_t blocks) {
   using R = BwdShape<DP>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   bool fits;
@@ -372,10 +392,9 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint64_t *st_full = bars + 10, *st_empty = bars + 12;
   const Ring<R::kA> ring_q{tc::smem_u32(tiles_a), bars + 14, bars + 14 + R::kA, R::kTile};
   const Ring<R::kB> ring_do{tc::smem_u32(tiles_b), bars + 14 + 2 * R::kA, bars + 14 + 2 * R::kA + R::kB, R::kTile};
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * (R::kA + R::kB));
-  volatile uint32_t* abort_flag = tmem_slot + 1;
+  Found* const found = reinterpret_cast<Found*>(bars + 14 + 2 * (R::kA + R::kB));
+  volatile uint32_t* abort_flag = &found->abort;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t units = *p.count * (uint32_t)p.n_kv_heads;
   const int q_rows = p.group * p.tq;
 
   if (threadIdx.x == 0) {
@@ -398,7 +417,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     tc::fence_barrier_init();
   }
   if (warp == 8) {
-    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_alloc(&found->tmem, 512);
     tc::tmem_relinquish();
   }
   if (q_rows < kRows) {
@@ -407,18 +426,22 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       reinterpret_cast<uint4*>(tiles_a)[i] = make_uint4(0u, 0u, 0u, 0u);
     tc::fence_proxy_async();
   }
+  if (warp == 9 && !p.list) find(p, block, found, false);
+  wait_for_primary();
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = uniform(*tmem_slot);  // S'/P', dP'/dS', dV, dK: 128 columns each
+  const uint32_t tmem = uniform(found->tmem);  // S'/P', dP'/dS', dV, dK: 128 columns each
+  const uint32_t units = (p.list ? *p.count : found->total) * (uint32_t)p.n_kv_heads;
+  auto entry_of = [&](uint32_t u) { return p.list ? p.list[u / p.n_kv_heads] : found->entry; };
   // tiles of queries of a list entry: they start at the key tile's first token
   auto tiles_of = [&](const Entry& e) { return (e.seq_hi - e.lo + p.tq - 1) / p.tq; };
 
   if (warp == 9) {
     Loader<DP> ld{raw, abort_flag, lane};
     uint32_t turns = 0, item = 0;
-    for (uint32_t u = blockIdx.x; ld.ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ld.ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int head = (int)(u % p.n_kv_heads), n = tiles_of(e);
       auto load_q = [&](int j) {
         const int row = e.lo + j * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
@@ -453,8 +476,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     // lse and delta of the query rows, up to two tiles ahead
     uint32_t tile = 0;
     bool ok = true;
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int head = (int)(u % p.n_kv_heads) * p.group, n = tiles_of(e);
       for (int j = 0; j < n; ++j, ++tile) {
         const int first = e.lo + j * p.tq, valid = min((e.seq_hi - first) * p.group, q_rows);
@@ -493,8 +516,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         umma_ts(d, a + half_cols(kk), b + step_mnmajor(kk), kIdescD, add || k > 0);
       }
     };
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int n = tiles_of(e);
       wait(kv_full, turns);
       ++turns;
@@ -561,8 +584,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const bool wide = wide_rows(p.dk, p.k_stride, p.head_dim) && wide_rows(p.dv, p.v_stride, p.head_dim);
     uint32_t tile = 0, turns = 0;
     bool ok = true;
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Entry e = p.list[u / p.n_kv_heads];
+    for (uint32_t u = block; ok && u < units; u += blocks) {
+      const Entry e = entry_of(u);
       const int n = tiles_of(e), key = e.lo + row;
       for (int j = 0; j < n; ++j, ++tile) {
         const int first = e.lo + j * p.tq, rows = min((e.seq_hi - first) * p.group, q_rows);
@@ -646,22 +669,34 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 }
 
 template <int DP>
+__global__ void __launch_bounds__(384, 1)
+attn_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
+                const __grid_constant__ BwdParams dq, const __grid_constant__ BwdParams dkv, unsigned dq_blocks) {
+  if (blockIdx.x < dq_blocks)
+    dq_part<DP>(map_q, map_k, map_v, map_do, dq, blockIdx.x, dq_blocks);
+  else
+    dkv_part<DP>(map_q, map_k, map_v, map_do, dkv, blockIdx.x - dq_blocks, gridDim.x - dq_blocks);
+}
+
+template <int DP>
 int bwd(const Args& a, const Layout& l) {
   const nat_attn_params& p = a.p;
   const int group = p.n_heads / p.n_kv_heads, tq = kRows / group;
-  int sms = 0;
-  int s = require_sm100();
-  if (s == NAT_OK) s = sm_count(&sms);
+  Device dev;
+  int s = device(&dev);
   CUtensorMap mq, mk, mv, mdo;
   if (s == NAT_OK) s = make_map(&mq, a.q, p.head_dim, p.n_heads, a.cap, p.q_stride, group, tq);
   if (s == NAT_OK) s = make_map(&mdo, a.dout, p.head_dim, p.n_heads, a.cap, p.o_stride, group, tq);
   if (s == NAT_OK) s = make_map(&mk, a.k, p.head_dim, p.n_kv_heads, a.cap, p.k_stride, 1, kRows);
   if (s == NAT_OK) s = make_map(&mv, a.v, p.head_dim, p.n_kv_heads, a.cap, p.v_stride, 1, kRows);
+  static std::atomic<uint64_t> allowed;
+  const size_t smem = BwdShape<DP>::kSmem;
+  if (s == NAT_OK) s = allow_smem(attn_bwd_kernel<DP>, smem, dev, &allowed);
   if (s != NAT_OK) return s;
-  const int smem = (int)BwdShape<DP>::kSmem;
-  NAT_CUDA(cudaFuncSetAttribute(attn_dq_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  NAT_CUDA(cudaFuncSetAttribute(attn_dkv_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  s = launch_bwd_prologue(a, l);
+  const int64_t units_q = l.entries[kPlanDq] * p.n_kv_heads, units_k = l.entries[kPlanDkv] * p.n_kv_heads;
+  const bool plan = units_q > dev.sms || units_k > dev.sms;
+  s = launch_bwd_prologue(a, l, plan);
   if (s != NAT_OK) return s;
   BwdParams bp{};
   bp.status = &head(a)->status;
@@ -679,16 +714,16 @@ int bwd(const Args& a, const Layout& l) {
   bp.tq = tq;
   bp.head_dim = p.head_dim;
   bp.scale = p.scale;
-  auto grid = [&](Plan which) { return (unsigned)min((int64_t)sms, l.entries[which] * p.n_kv_heads); };
-  bp.list = entries(a, l, kPlanDq);
-  bp.count = &head(a)->count[kPlanDq];
-  attn_dq_kernel<DP><<<grid(kPlanDq), 384, smem, a.stream>>>(mq, mk, mv, mdo, bp);
-  NAT_LAUNCH_CHECK("attn_dq_kernel");
-  bp.list = entries(a, l, kPlanDkv);
-  bp.count = &head(a)->count[kPlanDkv];
-  attn_dkv_kernel<DP><<<grid(kPlanDkv), 384, smem, a.stream>>>(mq, mk, mv, mdo, bp);
-  NAT_LAUNCH_CHECK("attn_dkv_kernel");
-  return NAT_OK;
+  auto part = [&](Plan which) {
+    BwdParams w = bp;
+    w.list = plan ? entries(a, l, which) : nullptr;
+    w.count = &head(a)->count[which];
+    w.batch = batch(a, l, which);
+    return w;
+  };
+  const unsigned blocks_q = (unsigned)min((int64_t)dev.sms, units_q), blocks_k = (unsigned)min((int64_t)dev.sms, units_k);
+  return launch_after(attn_bwd_kernel<DP>, blocks_q + blocks_k, 384, smem, a.stream, "attn_bwd_kernel", mq, mk, mv, mdo,
+                      part(kPlanDq), part(kPlanDkv), blocks_q);
 }
 
 }  // namespace

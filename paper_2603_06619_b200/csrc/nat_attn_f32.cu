@@ -75,14 +75,16 @@ struct Ptrs {
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads)
-f32_fwd_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict__ count) {
-  if (blockIdx.x >= *count) return;
+f32_fwd_kernel(Ptrs a, Batch batch, Head* head) {
   extern __shared__ float smem[];
+  uint32_t total;
+  const Entry e = find_entry(batch, blockIdx.x, &total);  // by every warp for itself
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
+  if (blockIdx.x >= total) return;
   float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem);
   float(*K)[DP + 4] = Q + kT;
   float(*V)[DP + 4] = K + kT;
   float(*P)[kT + 1] = reinterpret_cast<float(*)[kT + 1]>(V + kT);
-  const Entry e = list[blockIdx.x];
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
   const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, row = e.lo + r;
   load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
@@ -132,15 +134,17 @@ f32_fwd_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restric
 // dq of 32 queries of a head; also leaves delta = do . o for the keys' kernel.
 template <int DP>
 __global__ void __launch_bounds__(kThreads)
-f32_dq_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict__ count) {
-  if (blockIdx.x >= *count) return;
+f32_dq_kernel(Ptrs a, Batch batch, Head* head) {
   extern __shared__ float smem[];
+  uint32_t total;
+  const Entry e = find_entry(batch, blockIdx.x, &total);  // by every warp for itself
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
+  if (blockIdx.x >= total) return;
   float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem);
   float(*G)[DP + 4] = Q + kT;
   float(*K)[DP + 4] = G + kT;
   float(*V)[DP + 4] = K + kT;
   float(*P)[kT + 1] = reinterpret_cast<float(*)[kT + 1]>(V + kT);
-  const Entry e = list[blockIdx.x];
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
   const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, row = e.lo + r;
   load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
@@ -181,16 +185,18 @@ f32_dq_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict
 // dk and dv of 32 keys of a key head: all query heads of its group, all later queries, in order.
 template <int DP>
 __global__ void __launch_bounds__(kThreads)
-f32_dkv_kernel(Ptrs a, const Entry* __restrict__ list, const uint32_t* __restrict__ count) {
-  if (blockIdx.x >= *count) return;
+f32_dkv_kernel(Ptrs a, Batch batch, Head* head) {
   extern __shared__ float smem[];
+  uint32_t total;
+  const Entry e = find_entry(batch, blockIdx.x, &total);  // by every warp for itself
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
+  if (blockIdx.x >= total) return;
   float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem);
   float(*G)[DP + 4] = Q + kT;
   float(*K)[DP + 4] = G + kT;
   float(*V)[DP + 4] = K + kT;
   float(*P)[kT + 1] = reinterpret_cast<float(*)[kT + 1]>(V + kT);
   float(*S)[kT + 1] = P + kT;
-  const Entry e = list[blockIdx.x];
   const int D = a.p.head_dim, kh = blockIdx.y, group = a.p.n_heads / a.p.n_kv_heads;
   const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, key = e.lo + r;
   load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, e.lo, e.seq_hi);
@@ -240,26 +246,21 @@ template <typename K>
 int launch(K kernel, size_t smem, const Args& a, const Layout& l, Plan which, int heads, const char* name) {
   NAT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   kernel<<<dim3((unsigned)l.entries[which], (unsigned)heads), kThreads, smem, a.stream>>>(
-      ptrs(a, l), entries(a, l, which), &head(a)->count[which]);
+      ptrs(a, l), batch(a, l, which), head(a));
   NAT_LAUNCH_CHECK(name);
   return NAT_OK;
 }
 
 template <int DP>
 int fwd(const Args& a, const Layout& l) {
-  int s = launch_plan(a, l, kPlanFwd);
-  if (s != NAT_OK) return s;
   const size_t smem = (3 * kT * (DP + 4) + kT * (kT + 1)) * sizeof(float);
   return launch(f32_fwd_kernel<DP>, smem, a, l, kPlanFwd, a.p.n_heads, "f32_fwd_kernel");
 }
 
 template <int DP>
 int bwd(const Args& a, const Layout& l) {
-  int s = launch_plan(a, l, kPlanDq);
-  if (s == NAT_OK) s = launch_plan(a, l, kPlanDkv);
-  if (s != NAT_OK) return s;
   const size_t smem = (4 * kT * (DP + 4) + 2 * kT * (kT + 1)) * sizeof(float);
-  s = launch(f32_dq_kernel<DP>, smem, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
+  int s = launch(f32_dq_kernel<DP>, smem, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
   if (s != NAT_OK) return s;
   return launch(f32_dkv_kernel<DP>, smem, a, l, kPlanDkv, a.p.n_kv_heads, "f32_dkv_kernel");
 }

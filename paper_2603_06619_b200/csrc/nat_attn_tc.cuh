@@ -213,7 +213,6 @@ __device__ __forceinline__ T uniform(T x) {
 // box_tokens, zero outside.
 int make_map(CUtensorMap* map, const void* base, int D, int heads, int64_t cap, int64_t stride,
              int box_heads, int box_tokens);
-int sm_count(int* n);
 
 // Zeroes rows [first, 128) of a tile of NP panels that TMA has finished writing (one warp), for
 // the tensor cores to read: the rows belong to another sequence, or to none, and a weight of

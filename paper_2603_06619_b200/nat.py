@@ -303,20 +303,22 @@ def _rows(what, t, dtype, shape, device):
     least); None stays None."""
     if t is None:
         return None
-    s = t.shape
-    if (t.dtype is not dtype or t.get_device() != device or len(s) != len(shape) or s[0] < shape[0]
-            or s[1:] != shape[1:] or not t.is_contiguous()):
-        _bad(what, t, dtype, shape, device)
-    return t.data_ptr()
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+        s = t.shape
+        if s == shape or (len(s) == len(shape) and s[0] >= shape[0] and s[1:] == shape[1:]):
+            return t.data_ptr()
+    _bad(what, t, dtype, shape, device)
 
 
 def _heads(what, t, dtype, shape, device):
-    """The same for [tokens, heads, head_dim] with a token stride of its own."""
-    s = t.shape
-    if (t.dtype is not dtype or t.get_device() != device or len(s) != 3 or s[0] < shape[0]
-            or s[1:] != shape[1:] or t.stride(2) != 1 or (s[1] > 1 and t.stride(1) != s[2])):
-        _bad(what, t, dtype, shape, device)
-    return t.data_ptr()
+    """(pointer, token stride or None) of [tokens, heads, head_dim] with a stride of its own."""
+    if t.dtype is dtype and t.get_device() == device:
+        s = t.shape
+        if s == shape or (len(s) == 3 and s[0] >= shape[0] and s[1:] == shape[1:]):
+            st = t.stride()
+            if st[2] == 1 and (s[1] == 1 or st[1] == s[2]):
+                return t.data_ptr(), st[0] if s[0] > 1 else None
+    _bad(what, t, dtype, shape, device)
 
 
 def _workspace(t, device):
@@ -347,11 +349,10 @@ def _attn_call(params, B, cu_seqlens, cap, tensors, lse):
     p = AttnParams.from_buffer_copy(params)
     strides, ptrs, D = {}, [], params.head_dim
     for name, t, field, heads in tensors:
-        ptrs.append(_heads(name, t, dtype, (cap, heads, D), device))
-        if t.shape[0] > 1:
-            stride = t.stride(0)
-            if strides.setdefault(field, stride) != stride:
-                raise NatError(f"{name}: token stride {stride}, its counterpart has {strides[field]}")
+        ptr, stride = _heads(name, t, dtype, (cap, heads, D), device)
+        ptrs.append(ptr)
+        if stride is not None and strides.setdefault(field, stride) != stride:
+            raise NatError(f"{name}: token stride {stride}, its counterpart has {strides[field]}")
     for field, stride in strides.items():
         setattr(p, field, stride)
     return (ptrs, p, _rows("cu_seqlens", cu_seqlens, torch.int32, (B + 1,), device),
