@@ -173,7 +173,7 @@ int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool b
 }  // namespace
 
 int plan_tile(const nat_attn_params& p, Plan which) {
-  if (p.dtype == NAT_F32) return 32;
+  if (p.dtype == NAT_F32) return 64;
   const int tq = 128 / (p.n_heads / p.n_kv_heads);  // tokens of a tile with the group's heads folded in
   return which == kPlanFwd ? 2 * tq : which == kPlanDq ? tq : 128;
 }

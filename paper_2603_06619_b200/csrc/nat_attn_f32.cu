@@ -1,250 +1,328 @@
 // Packed causal attention in plain 32-bit arithmetic (FFMA), forward and backward.
 //
-// Four neighbouring threads share a row (a query; in the keys' kernel a key): each takes every
-// fourth of 32 columns of the score tile and every fourth float4 of the head's columns, so the
-// row's softmax is two shuffles and P passes through shared memory inside one warp only.
+// 256 threads as 16 x 16 over a 64 x 64 score tile, four rows and four columns each: eight float4 from
+// shared memory feed 64 FMAs (the FMA pipe, not shared memory, is the limit).  The 16 threads of a row
+// are half a warp, so its softmax is four shuffles; P passes through shared memory into the second
+// product, whose 64 x D tile the threads share as four rows by D / 16 columns.
 #include "nat_attn.cuh"
 
 namespace nat {
 namespace attn {
 namespace {
 
-constexpr int kT = 32;         // tokens of a tile, queries and keys alike
-constexpr int kThreads = 128;  // four threads a row
+constexpr int kT = 64;         // tokens of a tile, queries and keys alike
+constexpr int kThreads = 256;
+constexpr int kLd = kT + 4;    // leading dimension of a score tile
 
-// Rows [lo, lo + 32) of one head into shared memory, zero outside [lo, hi) and past D.
+// Row-major tile of 64 rows; four floats of padding put eight neighbouring rows into different banks.
 template <int DP>
-__device__ __forceinline__ void load_tile(float (*dst)[DP + 4], const float* base, int64_t stride,
-                                          int head, int D, int lo, int hi) {
-  for (int i = threadIdx.x; i < kT * DP; i += kThreads) {
-    const int r = i / DP, c = i % DP;
-    dst[r][c] = (lo + r < hi && c < D) ? base[(int64_t)(lo + r) * stride + (int64_t)head * D + c] : 0.f;
+struct Tile {
+  static constexpr int kLead = DP + 4, kFloats = kT * kLead;
+  float* at;
+  __device__ __forceinline__ float4 get(int r, int c) const {
+    return *reinterpret_cast<const float4*>(at + r * kLead + c);
   }
-}
-
-// s[j] = a-row . b-row (quad + 4 j)
-template <int DP>
-__device__ __forceinline__ void dots(const float* a, const float (*b)[DP + 4], int quad, float (&s)[8]) {
+  // Rows [lo, lo + 64) of one head, zero outside [lo, hi) and past D.
+  __device__ __forceinline__ void load(const float* base, int64_t stride, int head, int D, int lo, int hi) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) s[j] = 0.f;
+    for (int i = 0; i < kT * DP / 4 / kThreads; ++i) {
+      const int k = threadIdx.x + i * kThreads, r = k / (DP / 4), c = k % (DP / 4) * 4;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (lo + r < hi && c < D)
+        v = __ldg(reinterpret_cast<const float4*>(base + (int64_t)(lo + r) * stride + (int64_t)head * D + c));
+      *reinterpret_cast<float4*>(at + r * kLead + c) = v;
+    }
+  }
+};
+
+// s[i][j] = row (ty + 16 i) of a . row (tx + 16 j) of b
+template <int DP>
+__device__ __forceinline__ void dots(const Tile<DP>& a, const Tile<DP>& b, int ty, int tx, float (&s)[4][4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
   for (int c = 0; c < DP; c += 4) {
-    const float4 x = *reinterpret_cast<const float4*>(a + c);
+    float4 x[4], y[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float4 y = *reinterpret_cast<const float4*>(&b[quad + 4 * j][c]);
-      s[j] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[j]))));
+    for (int i = 0; i < 4; ++i) x[i] = a.get(ty + 16 * i, c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = b.get(tx + 16 * j, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        s[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j]))));
+  }
+}
+
+// acc[i][.] += sum_k w[ty + 16 i][k] m[k][.] over the thread's columns tx 4 + 64 n.  With `masked` only the k
+// in [first, last] of each row count: a weight of zero would not hide an infinity behind it.
+template <int DP, bool MASKED>
+__device__ __forceinline__ void accumulate(const float* w, const Tile<DP>& m, int ty, int tx, const int (&first)[4],
+                                           const int (&last)[4], float (&acc)[4][DP / 16]) {
+#pragma unroll 2
+  for (int k = 0; k < kT; k += 4) {
+    float4 p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * kLd + k);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      float y[DP / 16];
+#pragma unroll
+      for (int n = 0; n < DP / 64; ++n) {
+        const float4 v = m.get(k + kk, tx * 4 + 64 * n);
+        y[4 * n] = v.x; y[4 * n + 1] = v.y; y[4 * n + 2] = v.z; y[4 * n + 3] = v.w;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float f = kk == 0 ? p[i].x : kk == 1 ? p[i].y : kk == 2 ? p[i].z : p[i].w;
+        if (!MASKED || (k + kk >= first[i] && k + kk <= last[i])) {
+#pragma unroll
+          for (int c = 0; c < DP / 16; ++c) acc[i][c] = fmaf(f, y[c], acc[i][c]);
+        }
+      }
     }
   }
 }
 
-// acc[.] += sum_k w[k] m[k][.] over the thread's float4 columns quad + 4 i.  Only the rows
-// [first, last) that the mask leaves: a weight of zero would not hide an infinity behind it.
 template <int DP>
-__device__ __forceinline__ void accumulate(const float* w, const float (*m)[DP + 4], int first,
-                                           int last, int quad, float (&acc)[DP / 4]) {
-  for (int k = first; k < last; ++k) {
-    const float p = w[k];
+__device__ __forceinline__ void store_row(float* row, int D, int tx, const float (&acc)[DP / 16], float f) {
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-      const float4 y = *reinterpret_cast<const float4*>(&m[k][(quad + 4 * i) * 4]);
-      acc[4 * i] = fmaf(p, y.x, acc[4 * i]);
-      acc[4 * i + 1] = fmaf(p, y.y, acc[4 * i + 1]);
-      acc[4 * i + 2] = fmaf(p, y.z, acc[4 * i + 2]);
-      acc[4 * i + 3] = fmaf(p, y.w, acc[4 * i + 3]);
-    }
+  for (int n = 0; n < DP / 64; ++n) {
+    const int c = tx * 4 + 64 * n;
+    if (c < D)
+      *reinterpret_cast<float4*>(row + c) =
+          make_float4(acc[4 * n] * f, acc[4 * n + 1] * f, acc[4 * n + 2] * f, acc[4 * n + 3] * f);
   }
-}
-
-template <int DP>
-__device__ __forceinline__ void store_row(float* row, int D, int quad, const float (&acc)[DP / 4], float f) {
-#pragma unroll
-  for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = (quad + 4 * i) * 4 + j;
-      if (c < D) row[c] = acc[4 * i + j] * f;
-    }
 }
 
 struct Ptrs {
-  const void *q, *k, *v, *out, *dout;
-  void *o, *dq, *dk, *dv;
-  float *lse, *delta;
+  const float *q, *k, *v, *out, *dout;
+  float *o, *dq, *dk, *dv, *lse, *delta;
   nat_attn_params p;
 };
 
-template <int DP>
-__global__ void __launch_bounds__(kThreads)
-f32_fwd_kernel(Ptrs a, Batch batch, Head* head) {
-  extern __shared__ float smem[];
+__device__ __forceinline__ float sum16(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o, 16);
+  return x;
+}
+
+// Every block finds its tile; the first one reports what is wrong with the batch.
+__device__ __forceinline__ bool my_tile(const Batch& batch, Head* head, Entry* e) {
   uint32_t total;
-  const Entry e = find_entry(batch, blockIdx.x, &total);  // by every warp for itself
+  *e = find_entry(batch, blockIdx.x, &total);
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
-  if (blockIdx.x >= total) return;
-  float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem);
-  float(*K)[DP + 4] = Q + kT;
-  float(*V)[DP + 4] = K + kT;
-  float(*P)[kT + 1] = reinterpret_cast<float(*)[kT + 1]>(V + kT);
+  return blockIdx.x < total;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads) f32_fwd_kernel(Ptrs a, Batch batch, Head* head) {
+  extern __shared__ __align__(16) float smem[];
+  Entry e;
+  if (!my_tile(batch, head, &e)) return;
+  Tile<DP> Q{smem}, K{smem + Tile<DP>::kFloats}, V{smem + 2 * Tile<DP>::kFloats};
+  float* P = smem + 3 * Tile<DP>::kFloats;
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
-  const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, row = e.lo + r;
-  load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
-  float m = -INFINITY, l = 0.f, acc[DP / 4];
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  Q.load(a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
+  float m[4], l[4], acc[4][DP / 16];
 #pragma unroll
-  for (int i = 0; i < DP / 4; ++i) acc[i] = 0.f;
-  const int last = min(e.lo + kT, e.seq_hi);
-  for (int k0 = e.seq_lo; k0 < last; k0 += kT) {
-    __syncthreads();
-    load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, k0, last);
-    load_tile<DP>(V, (const float*)a.v, a.p.v_stride, kh, D, k0, last);
-    __syncthreads();
-    float s[8];
-    dots<DP>(Q[r], K, quad, s);
-    float top = m;
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      s[j] = (k0 + quad + 4 * j <= row) ? s[j] * a.p.scale : -INFINITY;
-      top = fmaxf(top, s[j]);
-    }
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    const float base = top == -INFINITY ? 0.f : top;  // every score so far is minus infinity
-    const float keep = expf(m - base);
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float p = expf(s[j] - base);
-      sum += p;
-      P[r][quad + 4 * j] = p;
-    }
-    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-    l = fmaf(l, keep, sum);
-    m = top;
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < DP / 4; ++i) acc[i] *= keep;
-    accumulate<DP>(P[r], V, 0, min(kT, row - k0 + 1), quad, acc);
+    for (int c = 0; c < DP / 16; ++c) acc[i][c] = 0.f;
   }
-  if (row < e.seq_hi) {
-    store_row<DP>((float*)a.o + (int64_t)row * a.p.o_stride + (int64_t)h * D, D, quad, acc, 1.f / l);
-    if (quad == 0) a.lse[(int64_t)row * a.p.n_heads + h] = m + logf(l);
+  const int end = min(e.lo + kT, e.seq_hi), none[4] = {0, 0, 0, 0};
+  for (int k0 = e.seq_lo; k0 < end; k0 += kT) {
+    __syncthreads();
+    K.load(a.k, a.p.k_stride, kh, D, k0, end);
+    V.load(a.v, a.p.v_stride, kh, D, k0, end);
+    __syncthreads();
+    float s[4][4];
+    dots<DP>(Q, K, ty, tx, s);
+    int last[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      last[i] = e.lo + ty + 16 * i - k0;
+      float top = m[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = tx + 16 * j <= last[i] ? s[i][j] * a.p.scale : -INFINITY;
+        top = fmaxf(top, s[i][j]);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, 16));
+      const float base = top == -INFINITY ? 0.f : top;  // every score so far is minus infinity
+      const float keep = expf(m[i] - base);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = expf(s[i][j] - base);
+        sum += p;
+        P[(ty + 16 * i) * kLd + tx + 16 * j] = p;
+      }
+      l[i] = fmaf(l[i], keep, sum16(sum));
+      m[i] = top;
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) acc[i][c] *= keep;
+    }
+    __syncwarp();  // a row's P is written and read by one half warp
+    if (k0 + kT > e.lo) accumulate<DP, true>(P, V, ty, tx, none, last, acc);
+    else accumulate<DP, false>(P, V, ty, tx, none, last, acc);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = e.lo + ty + 16 * i;
+    if (row >= e.seq_hi) continue;
+    store_row<DP>(a.o + (int64_t)row * a.p.o_stride + (int64_t)h * D, D, tx, acc[i], 1.f / l[i]);
+    if (tx == 0) a.lse[(int64_t)row * a.p.n_heads + h] = m[i] + logf(l[i]);
   }
 }
 
-// dq of 32 queries of a head; also leaves delta = do . o for the keys' kernel.
+// dq of 64 queries of a head; also leaves delta = do . o for the keys' kernel.
 template <int DP>
-__global__ void __launch_bounds__(kThreads)
-f32_dq_kernel(Ptrs a, Batch batch, Head* head) {
-  extern __shared__ float smem[];
-  uint32_t total;
-  const Entry e = find_entry(batch, blockIdx.x, &total);  // by every warp for itself
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
-  if (blockIdx.x >= total) return;
-  float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem);
-  float(*G)[DP + 4] = Q + kT;
-  float(*K)[DP + 4] = G + kT;
-  float(*V)[DP + 4] = K + kT;
-  float(*P)[kT + 1] = reinterpret_cast<float(*)[kT + 1]>(V + kT);
+__global__ void __launch_bounds__(kThreads) f32_dq_kernel(Ptrs a, Batch batch, Head* head) {
+  extern __shared__ __align__(16) float smem[];
+  Entry e;
+  if (!my_tile(batch, head, &e)) return;
+  Tile<DP> Q{smem}, G{smem + Tile<DP>::kFloats}, K{smem + 2 * Tile<DP>::kFloats}, V{smem + 3 * Tile<DP>::kFloats};
+  float* P = smem + 4 * Tile<DP>::kFloats;
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
-  const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, row = e.lo + r;
-  load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
-  load_tile<DP>(G, (const float*)a.dout, a.p.o_stride, h, D, e.lo, e.seq_hi);
-  load_tile<DP>(K, (const float*)a.out, a.p.o_stride, h, D, e.lo, e.seq_hi);
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  Q.load(a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
+  G.load(a.dout, a.p.o_stride, h, D, e.lo, e.seq_hi);
+  K.load(a.out, a.p.o_stride, h, D, e.lo, e.seq_hi);
   __syncthreads();
-  float delta = 0.f;
-  for (int c = quad; c < DP; c += 4) delta = fmaf(G[r][c], K[r][c], delta);
-  delta += __shfl_xor_sync(0xFFFFFFFFu, delta, 1);
-  delta += __shfl_xor_sync(0xFFFFFFFFu, delta, 2);
-  const int64_t at = (int64_t)row * a.p.n_heads + h;
-  const float lse = row < e.seq_hi ? a.lse[at] : 0.f;
-  if (row < e.seq_hi && quad == 0) a.delta[at] = delta;
-  float acc[DP / 4];
+  float delta[4], lse[4], acc[4][DP / 16];
 #pragma unroll
-  for (int i = 0; i < DP / 4; ++i) acc[i] = 0.f;
-  const int last = min(e.lo + kT, e.seq_hi);
-  for (int k0 = e.seq_lo; k0 < last; k0 += kT) {
-    __syncthreads();
-    load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, k0, last);
-    load_tile<DP>(V, (const float*)a.v, a.p.v_stride, kh, D, k0, last);
-    __syncthreads();
-    float s[8], dp[8];
-    dots<DP>(Q[r], K, quad, s);
-    dots<DP>(G[r], V, quad, dp);
+  for (int i = 0; i < 4; ++i) {
+    const int row = e.lo + ty + 16 * i;
+    float d = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool seen = k0 + quad + 4 * j <= row;
-      P[r][quad + 4 * j] = seen ? expf(s[j] * a.p.scale - lse) * (dp[j] - delta) : 0.f;
+    for (int n = 0; n < DP / 64; ++n) {
+      const float4 x = G.get(ty + 16 * i, tx * 4 + 64 * n), y = K.get(ty + 16 * i, tx * 4 + 64 * n);
+      d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
+    }
+    delta[i] = sum16(d);
+    const int64_t at = (int64_t)row * a.p.n_heads + h;
+    lse[i] = row < e.seq_hi ? a.lse[at] : 0.f;
+    if (row < e.seq_hi && tx == 0) a.delta[at] = delta[i];
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) acc[i][c] = 0.f;
+  }
+  const int end = min(e.lo + kT, e.seq_hi), none[4] = {0, 0, 0, 0};
+  for (int k0 = e.seq_lo; k0 < end; k0 += kT) {
+    __syncthreads();
+    K.load(a.k, a.p.k_stride, kh, D, k0, end);
+    V.load(a.v, a.p.v_stride, kh, D, k0, end);
+    __syncthreads();
+    float s[4][4], dp[4][4];
+    dots<DP>(Q, K, ty, tx, s);
+    dots<DP>(G, V, ty, tx, dp);
+    int last[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      last[i] = e.lo + ty + 16 * i - k0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        P[(ty + 16 * i) * kLd + tx + 16 * j] =
+            tx + 16 * j <= last[i] ? expf(s[i][j] * a.p.scale - lse[i]) * (dp[i][j] - delta[i]) : 0.f;
     }
     __syncwarp();
-    accumulate<DP>(P[r], K, 0, min(kT, row - k0 + 1), quad, acc);
+    if (k0 + kT > e.lo) accumulate<DP, true>(P, K, ty, tx, none, last, acc);
+    else accumulate<DP, false>(P, K, ty, tx, none, last, acc);
   }
-  if (row < e.seq_hi)
-    store_row<DP>((float*)a.dq + (int64_t)row * a.p.q_stride + (int64_t)h * D, D, quad, acc, a.p.scale);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = e.lo + ty + 16 * i;
+    if (row < e.seq_hi)
+      store_row<DP>(a.dq + (int64_t)row * a.p.q_stride + (int64_t)h * D, D, tx, acc[i], a.p.scale);
+  }
 }
 
-// dk and dv of 32 keys of a key head: all query heads of its group, all later queries, in order.
+// dk and dv of 64 keys of a key head: all query heads of its group, all later queries, in order.
 template <int DP>
-__global__ void __launch_bounds__(kThreads)
-f32_dkv_kernel(Ptrs a, Batch batch, Head* head) {
-  extern __shared__ float smem[];
-  uint32_t total;
-  const Entry e = find_entry(batch, blockIdx.x, &total);  // by every warp for itself
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
-  if (blockIdx.x >= total) return;
-  float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem);
-  float(*G)[DP + 4] = Q + kT;
-  float(*K)[DP + 4] = G + kT;
-  float(*V)[DP + 4] = K + kT;
-  float(*P)[kT + 1] = reinterpret_cast<float(*)[kT + 1]>(V + kT);
-  float(*S)[kT + 1] = P + kT;
+__global__ void __launch_bounds__(kThreads) f32_dkv_kernel(Ptrs a, Batch batch, Head* head) {
+  extern __shared__ __align__(16) float smem[];
+  Entry e;
+  if (!my_tile(batch, head, &e)) return;
+  Tile<DP> Q{smem}, G{smem + Tile<DP>::kFloats}, K{smem + 2 * Tile<DP>::kFloats}, V{smem + 3 * Tile<DP>::kFloats};
+  float *P = smem + 4 * Tile<DP>::kFloats, *S = P + kT * kLd;
   const int D = a.p.head_dim, kh = blockIdx.y, group = a.p.n_heads / a.p.n_kv_heads;
-  const int r = threadIdx.x >> 2, quad = threadIdx.x & 3, key = e.lo + r;
-  load_tile<DP>(K, (const float*)a.k, a.p.k_stride, kh, D, e.lo, e.seq_hi);
-  load_tile<DP>(V, (const float*)a.v, a.p.v_stride, kh, D, e.lo, e.seq_hi);
-  float dk[DP / 4], dv[DP / 4];
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  K.load(a.k, a.p.k_stride, kh, D, e.lo, e.seq_hi);
+  V.load(a.v, a.p.v_stride, kh, D, e.lo, e.seq_hi);
+  float dk[4][DP / 16], dv[4][DP / 16];
 #pragma unroll
-  for (int i = 0; i < DP / 4; ++i) dk[i] = dv[i] = 0.f;
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
+  const int all[4] = {kT, kT, kT, kT};
   for (int h = kh * group; h < (kh + 1) * group; ++h)
     for (int q0 = e.lo; q0 < e.seq_hi; q0 += kT) {
       __syncthreads();
-      load_tile<DP>(Q, (const float*)a.q, a.p.q_stride, h, D, q0, e.seq_hi);
-      load_tile<DP>(G, (const float*)a.dout, a.p.o_stride, h, D, q0, e.seq_hi);
-      __syncthreads();
-      float s[8], dp[8];
-      dots<DP>(K[r], Q, quad, s);
-      dots<DP>(V[r], G, quad, dp);
+      Q.load(a.q, a.p.q_stride, h, D, q0, e.seq_hi);
+      G.load(a.dout, a.p.o_stride, h, D, q0, e.seq_hi);
+      float lse[4], delta[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = quad + 4 * j, row = q0 + i;
-        float p = 0.f, ds = 0.f;
-        if (row >= key && row < e.seq_hi) {
-          const int64_t at = (int64_t)row * a.p.n_heads + h;
-          p = expf(s[j] * a.p.scale - a.lse[at]);
-          ds = p * (dp[j] - a.delta[at]);
+      for (int j = 0; j < 4; ++j) {
+        const int row = q0 + tx + 16 * j;
+        const int64_t at = (int64_t)row * a.p.n_heads + h;
+        lse[j] = row < e.seq_hi ? a.lse[at] : 0.f;
+        delta[j] = row < e.seq_hi ? a.delta[at] : 0.f;
+      }
+      __syncthreads();
+      float s[4][4], dp[4][4];
+      dots<DP>(K, Q, ty, tx, s);
+      dots<DP>(V, G, ty, tx, dp);
+      int first[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        first[i] = e.lo + ty + 16 * i - q0;  // the key's own token is the first query that sees it
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = tx + 16 * j, at = (ty + 16 * i) * kLd + c;
+          const bool seen = c >= first[i] && q0 + c < e.seq_hi;
+          const float p = seen ? expf(s[i][j] * a.p.scale - lse[j]) : 0.f;
+          P[at] = p;
+          S[at] = seen ? p * (dp[i][j] - delta[j]) : 0.f;
         }
-        P[r][i] = p;
-        S[r][i] = ds;
       }
       __syncwarp();
-      accumulate<DP>(P[r], G, max(0, key - q0), kT, quad, dv);
-      accumulate<DP>(S[r], Q, max(0, key - q0), kT, quad, dk);
+      if (q0 < e.lo + kT) {
+        accumulate<DP, true>(P, G, ty, tx, first, all, dv);
+        accumulate<DP, true>(S, Q, ty, tx, first, all, dk);
+      } else {
+        accumulate<DP, false>(P, G, ty, tx, first, all, dv);
+        accumulate<DP, false>(S, Q, ty, tx, first, all, dk);
+      }
     }
-  if (key < e.seq_hi) {
-    store_row<DP>((float*)a.dk + (int64_t)key * a.p.k_stride + (int64_t)kh * D, D, quad, dk, a.p.scale);
-    store_row<DP>((float*)a.dv + (int64_t)key * a.p.v_stride + (int64_t)kh * D, D, quad, dv, 1.f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = e.lo + ty + 16 * i;
+    if (key >= e.seq_hi) continue;
+    store_row<DP>(a.dk + (int64_t)key * a.p.k_stride + (int64_t)kh * D, D, tx, dk[i], a.p.scale);
+    store_row<DP>(a.dv + (int64_t)key * a.p.v_stride + (int64_t)kh * D, D, tx, dv[i], 1.f);
   }
 }
 
 Ptrs ptrs(const Args& a, const Layout& l) {
   Ptrs p{};
-  p.q = a.q; p.k = a.k; p.v = a.v; p.out = a.out; p.dout = a.dout; p.o = a.out; p.dq = a.dq;
-  p.dk = a.dk; p.dv = a.dv; p.lse = a.lse; p.delta = delta(a, l); p.p = a.p;
+  p.q = (const float*)a.q; p.k = (const float*)a.k; p.v = (const float*)a.v; p.out = (const float*)a.out;
+  p.dout = (const float*)a.dout; p.o = (float*)a.out; p.dq = (float*)a.dq; p.dk = (float*)a.dk;
+  p.dv = (float*)a.dv; p.lse = a.lse; p.delta = delta(a, l); p.p = a.p;
   return p;
 }
 
 template <typename K>
-int launch(K kernel, size_t smem, const Args& a, const Layout& l, Plan which, int heads, const char* name) {
-  NAT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+int launch(K kernel, size_t smem, std::atomic<uint64_t>* allowed, const Device& dev, const Args& a, const Layout& l,
+           Plan which, int heads, const char* name) {
+  int s = allow_smem(kernel, smem, dev, allowed);
+  if (s != NAT_OK) return s;
   kernel<<<dim3((unsigned)l.entries[which], (unsigned)heads), kThreads, smem, a.stream>>>(
       ptrs(a, l), batch(a, l, which), head(a));
   NAT_LAUNCH_CHECK(name);
@@ -253,16 +331,25 @@ int launch(K kernel, size_t smem, const Args& a, const Layout& l, Plan which, in
 
 template <int DP>
 int fwd(const Args& a, const Layout& l) {
-  const size_t smem = (3 * kT * (DP + 4) + kT * (kT + 1)) * sizeof(float);
-  return launch(f32_fwd_kernel<DP>, smem, a, l, kPlanFwd, a.p.n_heads, "f32_fwd_kernel");
+  static std::atomic<uint64_t> allowed;
+  Device dev;
+  const int s = device(&dev);
+  if (s != NAT_OK) return s;
+  const size_t smem = (3 * Tile<DP>::kFloats + kT * kLd) * sizeof(float);
+  return launch(f32_fwd_kernel<DP>, smem, &allowed, dev, a, l, kPlanFwd, a.p.n_heads, "f32_fwd_kernel");
 }
 
 template <int DP>
 int bwd(const Args& a, const Layout& l) {
-  const size_t smem = (4 * kT * (DP + 4) + 2 * kT * (kT + 1)) * sizeof(float);
-  int s = launch(f32_dq_kernel<DP>, smem, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
+  static std::atomic<uint64_t> allowed[2];
+  Device dev;
+  int s = device(&dev);
   if (s != NAT_OK) return s;
-  return launch(f32_dkv_kernel<DP>, smem, a, l, kPlanDkv, a.p.n_kv_heads, "f32_dkv_kernel");
+  const size_t smem = (4 * Tile<DP>::kFloats + kT * kLd) * sizeof(float);
+  s = launch(f32_dq_kernel<DP>, smem, &allowed[0], dev, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
+  if (s != NAT_OK) return s;
+  return launch(f32_dkv_kernel<DP>, smem + kT * kLd * sizeof(float), &allowed[1], dev, a, l, kPlanDkv, a.p.n_kv_heads,
+                "f32_dkv_kernel");
 }
 
 }  // namespace
