@@ -133,7 +133,9 @@ def ckpt8_store(x):
         top = np.abs(part).max(axis=1)              # a NaN wins
         fine = np.isfinite(top)
         kept = fine & (top >= np.float32(2.0 ** -120))
-        inv = np.float32(127.0) / np.where(kept, top, np.float32(1.0))
+        # the reciprocal of the mantissa, so that it is rounded to 24 bits for every top
+        mant, expo = np.frexp(np.where(kept, top, np.float32(1.0)))
+        inv = np.ldexp(np.float32(1.0) / mant * np.float32(127.0), -expo)
         with np.errstate(invalid="ignore", over="ignore"):
             q = np.rint(np.where(kept[:, None], part, np.float32(0.0)) * inv[:, None])
         codes[:, i * GROUP8:(i + 1) * GROUP8] = q.astype(np.int8)

@@ -113,7 +113,7 @@ __device__ __forceinline__ void load_weights(const float* p, float2 (&w)[kPairs]
 }
 
 // ---- 8-bit checkpoints ----------------------------------------------------------------
-// A group of 128 columns holds codes q = round(x 127 / top) and one scale top / 127, top the
+// A group of 128 columns holds codes q = round(x ((1 / top) 127)) and one scale top / 127, top the
 // group's largest magnitude: an even grid, so that an element is off by at most half a
 // 127th of the largest magnitude beside it.  Two cases leave that rule: a group whose largest
 // magnitude is below 2^-120 (127 / top would overflow) is stored as zeros, and a group that
@@ -158,19 +158,19 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t top_bits) {
   if (top_bits >= 0x7F800000u) return {0.f, __uint_as_float(0x7FC00000u)};
   if (top_bits < (7u << 23)) return {0.f, 0.f};  // below 2^(7 - 127)
   // top / 127 by Markstein's division: an FMA gives the exact remainder of the first quotient, which
-  // the second FMA corrects to the rounded one (both quotients were checked against the division for every float from 2^-120 up)
+  // the second FMA corrects to the rounded one
   constexpr float kInv = 1.f / 127.f;
   const float q = __fmul_rn(top, kInv);
-  // 127 / top the same way, with the mantissa of top (in [1, 2)) so that no step leaves the normal
-  // range, and a reciprocal that one Newton step makes good; the power of two is exact
+  // 1 / top with the mantissa of top (in [1, 2)), so that no step leaves the normal range: the
+  // approximate reciprocal, which one Newton step rounds correctly; then the factor and, exactly, the
+  // power of two (127 / 2, so that the power stays normal).  Checked on the device for every float from
+  // 2^-120 up, against the division and the rounded reciprocal.
   const float b = __uint_as_float((top_bits & 0x007FFFFFu) | 0x3F800000u);
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
   y = __fmaf_rn(__fmaf_rn(-b, y, 1.f), y, y);
-  const float p = __fmul_rn(63.5f, y);
-  const float inv = __fmaf_rn(__fmaf_rn(-p, b, 63.5f), y, p);  // 127 / 2: the power below stays normal
   const float power = __uint_as_float((255u << 23) - (top_bits & 0x7F800000u));
-  return {__fmul_rn(inv, power), __fmaf_rn(__fmaf_rn(-q, 127.f, top), kInv, q)};
+  return {__fmul_rn(__fmul_rn(63.5f, y), power), __fmaf_rn(__fmaf_rn(-q, 127.f, top), kInv, q)};
 }
 
 // Codes of eight elements as eight bytes.  |x inv| <= 127 (1 + 2^-22), so adding 1.5 2^23
