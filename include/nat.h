@@ -364,7 +364,8 @@ int nat_policy_loss_fwd_bwd(const nat_loss_params* params /* host */, const void
  *   dS_ij = P_ij (dout_i . v_j - delta_i),   dq_i = scale sum_j dS_ij k_j,
  *   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij dout_i   (summed over the heads of a group).
  * cu_seqlens int32 [B+1] on the device, ascending; sequences may be empty.  Rows at or after cap
- * are left out and NAT_DEV_CAPACITY is raised in the status word at the head of the workspace.
+ * are left out, and bounds that do not ascend leave all outputs untouched; either raises
+ * NAT_DEV_CAPACITY in the status word at the head of the workspace.
  * q, dq [cap, n_heads, head_dim] with q_stride elements from a token to the next, heads
  * contiguous; k, dk and v, dv [cap, n_kv_heads, head_dim] with k_stride, v_stride; out, dout with
  * o_stride (q, k and v may be column blocks of one projection's output).  lse float32

@@ -7,51 +7,96 @@ namespace {
 
 constexpr int kBuckets = 1024;
 
-// Lists the tiles of all sequences, longest work first: under a causal mask the tiles of a
-// sequence cost 1, 2, ... tiles of keys (queries' plans) or as much in the opposite order (keys'
-// plan), and blocks that take the list in turn finish together when the short ones come last.
-// A counting sort by cost; the order inside a bucket is not fixed, which no result depends on.
-// Sequence bounds are clamped to [0, cap], so no list entry points outside the buffers whatever
-// cu_seqlens holds.
 struct PlanArgs {
   Batch batch;
-  int by_rest, which;
+  int span;     // tokens of a step
+  int by_rest;  // the steps run from the tile to the sequence's end, not from its start to the tile
+  int heads;    // key heads, which multiply the work
+  int which;
+  bool split;
+  int64_t max_entries;
   Entry* list;
   Head* head;
 };
 
+constexpr int kMinPiece = 8;  // steps: a piece's start, its partial result and their join cost about two
+
+// Lists the tiles of all sequences, longest work first: under a causal mask the tiles of a
+// sequence cost 1, 2, ... tiles of keys (queries' plans) or as much in the opposite order (keys'
+// plan), and blocks that take the list in turn finish together when the short ones come last.  Where
+// tiles are few (`split`) the long ones are cut into equal pieces, so that the work of all heads makes about
+// kSplitBlocks pieces.  A counting sort by steps; the order inside a bucket and the numbering of the slots
+// are not fixed, which no result depends on.  Sequence bounds are clamped to [0, cap], so no list
+// entry points outside the buffers whatever cu_seqlens holds.
 __device__ __forceinline__ void plan(const PlanArgs& a) {
   const int32_t* cu = a.batch.cu;
   const int32_t B = a.batch.B;
-  const int64_t cap = a.batch.cap, max_entries = a.batch.max_entries;
-  const int tile = a.batch.tile, by_rest = a.by_rest;
-  Entry* list = a.list;
-  __shared__ uint32_t bucket[kBuckets];
+  const int64_t cap = a.batch.cap;
+  const int tile = a.batch.tile;
+  __shared__ uint32_t bucket[kBuckets], warp_sum[32], next_slot;
   __shared__ int longest;
+  __shared__ unsigned long long work;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bucket[threadIdx.x] = 0u;
-  if (threadIdx.x == 0) longest = 0;
-  __syncthreads();
-  auto bounds = [&](int i, int& lo, int& hi) { sequence_bounds(cu, i, cap, lo, hi); };
-  for (int i = threadIdx.x; i < B; i += blockDim.x) {
-    int lo, hi;
-    bounds(i, lo, hi);
-    atomicMax(&longest, (hi - lo + tile - 1) / tile);
+  if (threadIdx.x == 0) {
+    longest = 1;
+    work = 0ull;
+    next_slot = 0u;
   }
-  __syncthreads();
-  int shift = 0;
-  while ((longest >> shift) >= kBuckets) ++shift;
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int i = warp; i < B; i += 32) {
-      int lo, hi;
-      bounds(i, lo, hi);
-      const int tiles = (hi - lo + tile - 1) / tile;
-      for (int t = lane; t < tiles; t += 32) {
-        const int cost = by_rest ? tiles - t : t + 1;
-        const uint32_t at = atomicAdd(&bucket[kBuckets - 1 - (cost >> shift)], 1u);
-        if (pass == 1 && at < max_entries) list[at] = Entry{lo, hi, lo + t * tile, 0};
-      }
+  int faults = 0;
+  for (int i = threadIdx.x; i < B; i += blockDim.x) faults |= sequence_fault(cu, i, cap);
+  const bool broken = __syncthreads_or(faults & kBroken), any = __syncthreads_or(faults);
+  if (broken) {
+    if (threadIdx.x == 0) {
+      a.head->count[a.which] = 0u;
+      a.head->status = NAT_DEV_CAPACITY;  // a call's plans find the same
     }
+    return;
+  }
+  auto steps_of = [&](int lo, int hi, int t) {
+    const int first = lo + t * tile;
+    return a.by_rest ? (hi - first + a.span - 1) / a.span : (min(first + tile, hi) - lo + a.span - 1) / a.span;
+  };
+  // visit(lo, hi, t) for every tile t of every sequence
+  auto for_tiles = [&](auto visit) {
+    // all threads together where the sequences are few, a warp each where they are many
+    const bool few = B <= 32;
+    for (int i = few ? 0 : warp; i < B; i += few ? 1 : 32) {
+      int lo, hi;
+      sequence_bounds(cu, i, cap, lo, hi);
+      const int tiles = (hi - lo + tile - 1) / tile;
+      for (int t = few ? threadIdx.x : lane; t < tiles; t += few ? 1024 : 32) visit(lo, hi, t);
+    }
+  };
+  unsigned long long my_work = 0ull;
+  int my_longest = 1;
+  for_tiles([&](int lo, int hi, int t) {
+    const int steps = steps_of(lo, hi, t);
+    my_work += steps;
+    my_longest = max(my_longest, steps);
+  });
+  atomicMax(&longest, my_longest);
+  if (my_work) atomicAdd(&work, my_work);
+  __syncthreads();
+  int chunk = kAllSteps;
+  if (a.split) chunk = (int)max((unsigned long long)kMinPiece, (work * a.heads + kSplitBlocks - 1) / kSplitBlocks);
+  int shift = 0;
+  while ((min(longest, chunk) >> shift) >= kBuckets) ++shift;
+  for (int pass = 0; pass < 2; ++pass) {
+    for_tiles([&](int lo, int hi, int t) {
+      const int steps = steps_of(lo, hi, t);
+      int pieces = (steps - 1) / chunk + 1;
+      const int per = (steps + pieces - 1) / pieces;
+      pieces = (steps + per - 1) / per;
+      uint32_t slot = 0u;
+      if (pass == 1 && pieces > 1) slot = atomicAdd(&next_slot, (uint32_t)pieces);
+      for (int p = 0; p < pieces; ++p) {
+        const int begin = p * per, end = min(steps, begin + per);
+        const uint32_t at = atomicAdd(&bucket[kBuckets - 1 - ((end - begin) >> shift)], 1u);
+        if (pass == 1 && at < a.max_entries)  // always, as the bounds ascend
+          a.list[at] = Entry{lo, hi, lo + t * tile, begin, end, (int32_t)slot, p, pieces};
+      }
+    });
     __syncthreads();
     if (pass == 0) {  // exclusive scan of the counts, costliest bucket first
       const uint32_t mine = bucket[threadIdx.x];
@@ -61,7 +106,6 @@ __device__ __forceinline__ void plan(const PlanArgs& a) {
         const uint32_t left = __shfl_up_sync(0xFFFFFFFFu, run, o);
         if (lane >= o) run += left;
       }
-      __shared__ uint32_t warp_sum[32];
       if (lane == 31) warp_sum[warp] = run;
       __syncthreads();
       uint32_t before = 0u;
@@ -69,8 +113,8 @@ __device__ __forceinline__ void plan(const PlanArgs& a) {
       bucket[threadIdx.x] = before + run - mine;
       if (threadIdx.x == kBuckets - 1) {
         const uint32_t total = before + run;
-        a.head->count[a.which] = (uint32_t)min((int64_t)total, max_entries);
-        a.head->status = batch_status(a.batch, total);  // a call's plans find the same
+        a.head->count[a.which] = total;
+        a.head->status = any ? NAT_DEV_CAPACITY : 0u;
       }
       __syncthreads();
     }
@@ -181,26 +225,45 @@ int plan_tile(const nat_attn_params& p, Plan which) {
 Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
   Layout l;
   size_t at = 256;
+  int64_t pieces[3];
   for (int w = 0; w < 3; ++w) {
     // a sequence's last tile may be part full: at most one extra tile for each sequence
-    l.entries[w] = cap / plan_tile(p, (Plan)w) + B;
+    const int64_t tiles = cap / plan_tile(p, (Plan)w) + B;
+    // Few tiles, each with many steps: cut into pieces.
+    l.split[w] = p.dtype == NAT_BF16 && cap > 1024 && tiles * p.n_kv_heads <= kSplitBlocks;
+    pieces[w] = l.split[w] ? tiles + (kSplitBlocks + p.n_kv_heads - 1) / p.n_kv_heads : 0;
+    l.entries[w] = l.split[w] ? pieces[w] : tiles;
     l.plan_off[w] = at;
     at = align_up(at + (size_t)l.entries[w] * sizeof(Entry), 256);
   }
   l.delta_off = at;
   l.lse2_off = at = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
   if (p.dtype == NAT_BF16) at = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
-  l.total = at;
+  // the forward pass and the backward pass do not run together
+  auto bytes = [&](Plan w) {
+    return align_up((size_t)pieces[w] * p.n_kv_heads * partial_floats(p, w) * sizeof(float), 256);
+  };
+  l.partial_off[kPlanFwd] = l.partial_off[kPlanDq] = at;
+  l.partial_off[kPlanDkv] = at + bytes(kPlanDq);
+  l.total = at + max(bytes(kPlanFwd), bytes(kPlanDq) + bytes(kPlanDkv));
   return l;
 }
 
 Batch batch(const Args& a, const Layout& l, Plan which) {
-  return {a.cu_seqlens, a.B, plan_tile(a.p, which), a.cap, l.entries[which]};
+  return {a.cu_seqlens, a.B, plan_tile(a.p, which), a.cap};
 }
 
 namespace {
 PlanArgs plan_args(const Args& a, const Layout& l, Plan which) {
-  return {batch(a, l, which), which == kPlanDkv ? 1 : 0, (int)which, entries(a, l, which), head(a)};
+  return {batch(a, l, which),
+          which == kPlanDkv ? plan_tile(a.p, kPlanDq) : 128,
+          which == kPlanDkv ? 1 : 0,
+          a.p.n_kv_heads,
+          (int)which,
+          l.split[which],
+          l.entries[which],
+          entries(a, l, which),
+          head(a)};
 }
 }  // namespace
 

@@ -39,29 +39,46 @@ struct Head {
   uint32_t count[3];  // entries of the forward, dq and dkv plans
 };
 
-// One tile of `tile` tokens starting at `lo`, of the sequence that holds rows [seq_lo, seq_hi).
+// One tile of tokens starting at `lo`, of the sequence that holds rows [seq_lo, seq_hi), and the steps
+// [begin, end) of its long axis (keys, or queries in the keys' part).  A tile in several pieces leaves
+// partial results in slots [slot, slot + pieces), which a kernel behind joins in that order.
 struct Entry {
-  int32_t seq_lo, seq_hi, lo, pad;
+  int32_t seq_lo, seq_hi, lo, begin, end, slot, piece, pieces;
 };
+constexpr int32_t kAllSteps = 0x7FFFFFFF;
 
 // The batch itself, for kernels that find their tile without a list.
 struct Batch {
   const int32_t* cu;
   int32_t B;
   int tile;
-  int64_t cap, max_entries;
+  int64_t cap;
 };
+
+// What a call finds wrong with sequence i: kTooLong, more rows than the buffers hold (the surplus is left
+// out), or kBroken, bounds that do not ascend (nothing is computed).
+enum { kTooLong = 1, kBroken = 2 };
+__device__ __forceinline__ int sequence_fault(const int32_t* cu, int i, int64_t cap) {
+  const int lo = __ldg(cu + i), hi = __ldg(cu + i + 1);
+  return (lo < 0 || hi < lo ? kBroken : 0) | ((int64_t)hi > cap ? kTooLong : 0);
+}
 
 // Tile number `index` of all tiles in the sequences' order (for one warp; the same in every lane), and how
 // many there are.  Where there are no more tiles than blocks their order does not matter, and the
 // search, a few hundred cycles for every 32 sequences, is cheaper than a kernel that sorts them.
-__device__ __forceinline__ Entry find_entry(const Batch& b, uint32_t index, uint32_t* total) {
+__device__ __forceinline__ Entry find_entry(const Batch& b, uint32_t index, uint32_t* total, uint32_t* status) {
   const int lane = threadIdx.x & 31;
   uint32_t before = 0u;
-  Entry found{0, 0, 0, 0};
+  Entry found{0, 0, 0, 0, kAllSteps, 0, 0, 1};
+  unsigned faults = 0u;
   for (int base = 0; base < b.B; base += 32) {
     int lo = 0, hi = 0;
-    if (base + lane < b.B) sequence_bounds(b.cu, base + lane, b.cap, lo, hi);
+    int fault = 0;
+    if (base + lane < b.B) {
+      sequence_bounds(b.cu, base + lane, b.cap, lo, hi);
+      fault = sequence_fault(b.cu, base + lane, b.cap);
+    }
+    faults |= __reduce_or_sync(0xFFFFFFFFu, (unsigned)fault);
     const uint32_t tiles = (uint32_t)((hi - lo + b.tile - 1) / b.tile);
     uint32_t run = tiles;
 #pragma unroll
@@ -80,13 +97,9 @@ __device__ __forceinline__ Entry find_entry(const Batch& b, uint32_t index, uint
     }
     before += __shfl_sync(0xFFFFFFFFu, run, 31);
   }
-  *total = before;
+  *status = faults ? NAT_DEV_CAPACITY : 0u;
+  *total = (faults & kBroken) ? 0u : before;
   return found;
-}
-
-// What a call finds wrong with its batch: more rows than the buffers hold, or bounds that do not ascend.
-__device__ __forceinline__ uint32_t batch_status(const Batch& b, uint32_t total) {
-  return ((int64_t)__ldg(b.cu + b.B) > b.cap || total > b.max_entries) ? NAT_DEV_CAPACITY : 0u;
 }
 
 enum Plan { kPlanFwd = 0, kPlanDq = 1, kPlanDkv = 2 };
@@ -95,10 +108,20 @@ enum Plan { kPlanFwd = 0, kPlanDq = 1, kPlanDkv = 2 };
 int plan_tile(const nat_attn_params& p, Plan which);
 
 struct Layout {
-  size_t plan_off[3], delta_off, lse2_off, total;
-  int64_t entries[3];
+  size_t plan_off[3], delta_off, lse2_off, partial_off[3], total;
+  int64_t entries[3];  // of the list
+  bool split[3];       // tiles may be cut into pieces
 };
+
+// Floats of one piece's partial result for one key head.
+inline size_t partial_floats(const nat_attn_params& p, Plan which) {
+  const size_t dp = p.head_dim <= 64 ? 64 : 128;
+  return which == kPlanFwd ? 256 * (dp + 2) : which == kPlanDq ? 128 * dp : 128 * 2 * dp;
+}
 Layout layout(const nat_attn_params& p, int32_t B, int64_t cap);
+
+// Blocks that the splitting of tiles aims at, two for each multiprocessor.
+constexpr int kSplitBlocks = 2 * 148;
 
 inline Entry* entries(const Args& a, const Layout& l, Plan which) {
   return reinterpret_cast<Entry*>((char*)a.workspace + l.plan_off[which]);
@@ -110,6 +133,10 @@ inline float* delta(const Args& a, const Layout& l) {
 
 inline float* lse2(const Args& a, const Layout& l) {
   return reinterpret_cast<float*>((char*)a.workspace + l.lse2_off);
+}
+
+inline float* partials(const Args& a, const Layout& l, Plan which) {
+  return reinterpret_cast<float*>((char*)a.workspace + l.partial_off[which]);
 }
 
 // Writes the plan of `which` and the status word.
@@ -130,13 +157,13 @@ int device(Device* d);
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void release_secondary() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... P, typename... A>
-int launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t stream,
+int launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream,
                  const char* name, const A&... args) {
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

@@ -29,6 +29,7 @@ struct FwdParams {
   const Entry* list;  // null where every block has one unit at most and finds it itself
   Batch batch;
   const uint32_t* count;
+  float* partial;
   uint32_t* status;
   __nv_bfloat16* out;
   float* lse;
@@ -45,10 +46,18 @@ struct FwdShape {
   static constexpr uint32_t kSmem = 1024 + (2 + kStages) * kTile + 512;
 };
 
+template <int DP>
+constexpr __host__ __device__ int fwd_slot() {
+  return 256 * (DP + 2);
+}
+
 // What all roles derive from a list entry.
 struct Unit {
-  int seq_lo, seq_hi, lo, head, nk[2], kv_hi;
+  int seq_lo, seq_hi, lo, head, kv_hi;
+  int begin, nk[2];  // this piece's first key tile and, of each row tile, how many it has
+  int slot, pieces;  // where its partial result goes, if it is not all
 };
+template <bool SPLIT>
 __device__ __forceinline__ Unit unit_of(const FwdParams& p, const Entry* found, uint32_t u) {
   const Entry e = p.list ? p.list[u / p.n_kv_heads] : *found;
   Unit w;
@@ -56,16 +65,20 @@ __device__ __forceinline__ Unit unit_of(const FwdParams& p, const Entry* found, 
   w.seq_hi = e.seq_hi;
   w.lo = e.lo;
   w.head = (int)(u % p.n_kv_heads);
+  w.begin = SPLIT ? e.begin : 0;
+  w.slot = SPLIT ? e.slot + e.piece : 0;
+  w.pieces = SPLIT ? e.pieces : 1;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int first = e.lo + t * p.tq, end = min(first + p.tq, e.seq_hi);
-    w.nk[t] = first < e.seq_hi ? (end - e.seq_lo + kRows - 1) / kRows : 0;
+    const int all = first < e.seq_hi ? (end - e.seq_lo + kRows - 1) / kRows : 0;
+    w.nk[t] = SPLIT ? max(min(all, e.end) - e.begin, 0) : all;
   }
   w.kv_hi = min(e.lo + 2 * p.tq, e.seq_hi);
   return w;
 }
 
-template <int DP>
+template <int DP, bool SPLIT>  // SPLIT: some tiles come in pieces
 __global__ void __launch_bounds__(384, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                 const __grid_constant__ CUtensorMap map_v, const FwdParams p) {
@@ -78,7 +91,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *o_done = bars + 6, *raw = bars + 8;
   uint64_t *drain = bars + 9, *p_full = bars + 10;  // p_full [row tile][half of the keys]
   uint64_t *full = bars + 14, *empty = bars + 14 + kNS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * kNS);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * kNS);  // address, abort flag, total
   volatile uint32_t* abort_flag = tmem_slot + 1;
   Entry* found = reinterpret_cast<Entry*>(tmem_slot + 4);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -106,12 +119,12 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     tc::tmem_relinquish();
   }
   if (warp == 9 && !p.list) {
-    uint32_t total;
-    const Entry e = find_entry(p.batch, blockIdx.x / p.n_kv_heads, &total);
+    uint32_t total, status;
+    const Entry e = find_entry(p.batch, blockIdx.x / p.n_kv_heads, &total, &status);
     if (lane == 0) {
       *found = e;
       tmem_slot[2] = total;
-      if (blockIdx.x == 0) *p.status = batch_status(p.batch, total);
+      if (blockIdx.x == 0) *p.status = status;
     }
   }
   wait_for_primary();
@@ -147,7 +160,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       ok = ok && warp_wait(&empty[s], ((item / kNS) & 1) ^ 1, abort_flag);
       if (!ok) return;
       ++item;
-      const int row = w.seq_lo + j * kRows, valid = w.kv_hi - row;
+      const int row = w.seq_lo + (w.begin + j) * kRows, valid = w.kv_hi - row;
       const bool fix = is_v && valid < kRows;
       uint64_t* bar = fix ? raw : &full[s];
       uint8_t* dst = ring + s * R::kTile;
@@ -165,7 +178,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     };
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of(p, found, u);
+      const Unit w = unit_of<SPLIT>(p, found, u);
       const int n = max(w.nk[0], w.nk[1]);
       for (int j = 0; ok && j < n; ++j) {
         if (j == 0) load_q(w, 0);
@@ -207,7 +220,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       __syncwarp();
     };
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of(p, found, u);
+      const Unit w = unit_of<SPLIT>(p, found, u);
       const int n = max(w.nk[0], w.nk[1]);
       // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
       wait(&full[item % kNS], item / kNS);
@@ -270,7 +283,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     uint32_t s_turns = 0, o_turns = 0;
     bool ok = true;
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of(p, found, u);
+      const Unit w = unit_of<SPLIT>(p, found, u);
       const int nk = w.nk[t], first = w.lo + t * p.tq, token = first + token_in;
       const bool valid = row < p.group * p.tq && token < w.seq_hi;
       float m = -INFINITY, l = 0.f;
@@ -292,7 +305,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll
           for (int c = 0; c < 128; ++c) s[c] *= sign;
         }
-        const int kv0 = w.seq_lo + j * kRows;
+        const int kv0 = w.seq_lo + (w.begin + j) * kRows;
         if (kv0 + kRows - 1 > first) {  // the tile touches the diagonal
           const int last = token - kv0;
 #pragma unroll
@@ -350,22 +363,40 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         l += sum[0].x + sum[0].y;
       }
       if (!ok) break;
-      if (nk == 0) continue;
-      ok = warp_wait(&o_done[t], o_turns & 1, abort_flag);
-      if (!ok) break;
-      ++o_turns;
-      tc::fence_after_sync();
-      const int head = w.head * p.group + head_in;
-      const float inv = 1.f / l;
-      __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * p.head_dim;
-#pragma unroll
-      for (int c = 0; c < DP / 32; ++c) {
-        float o[32];
-        tc::tmem_ld32(o_addr + c * 32, o);
-        if (valid) store_row32(dst + c * 32, o, inv, p.head_dim - c * 32, wide);
+      if (nk == 0 && w.pieces == 1) continue;
+      if (nk > 0) {
+        ok = warp_wait(&o_done[t], o_turns & 1, abort_flag);
+        if (!ok) break;
+        ++o_turns;
+        tc::fence_after_sync();
       }
-      if (valid)
-        p.lse[(int64_t)token * p.n_heads + head] = fmaf(m, sc * kLn2, logf(l));
+      const int head = w.head * p.group + head_in;
+      __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * p.head_dim;
+      float* lse = p.lse + (int64_t)token * p.n_heads + head;
+      if (w.pieces == 1) {
+        const float inv = 1.f / l;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+          float o[32];
+          tc::tmem_ld32(o_addr + c * 32, o);
+          if (valid) store_row32(dst + c * 32, o, inv, p.head_dim - c * 32, wide);
+        }
+        if (valid) *lse = fmaf(m, sc * kLn2, logf(l));
+      } else {
+        // this piece's O, maximum and sum, [column][row]
+        float* own = p.partial + ((int64_t)w.slot * p.n_kv_heads + w.head) * fwd_slot<DP>() + t * 128 + row;
+        if (nk > 0) {
+#pragma unroll
+          for (int c = 0; c < DP / 32; ++c) {
+            float o[32];
+            tc::tmem_ld32(o_addr + c * 32, o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) __stcg(own + (c * 32 + i) * 256, o[i]);
+          }
+        }
+        __stcg(own + DP * 256, nk > 0 ? m : -INFINITY);
+        __stcg(own + (DP + 1) * 256, nk > 0 ? l : 0.f);
+      }
       tc::fence_before_sync();
     }
   }
@@ -375,6 +406,47 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   tc::fence_after_sync();
   if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
   if (warp == 8) tc::tmem_dealloc(tmem, 512);
+}
+
+// Joins the pieces of a tile, in their order: a block takes 16 columns of the 256 rows of a list entry, a
+// thread a row.  out = sum_i w_i O_i / sum_i w_i l_i with w_i = exp(m_i - max m).
+template <int DP>
+__global__ void __launch_bounds__(256) attn_fwd_join_kernel(const FwdParams p) {
+  wait_for_primary();
+  if (blockIdx.x / p.n_kv_heads >= *p.count) return;
+  const Entry e = p.list[blockIdx.x / p.n_kv_heads];
+  if (e.piece != 0 || e.pieces == 1) return;
+  const int kv_head = (int)(blockIdx.x % p.n_kv_heads), col = blockIdx.y * 16, row = threadIdx.x & 127;
+  const int token = e.lo + (threadIdx.x >> 7) * p.tq + row / p.group, head = kv_head * p.group + row % p.group;
+  if (row >= p.group * p.tq || token >= e.seq_hi || col >= p.head_dim) return;
+  const float sign_scale = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
+  const int64_t step = (int64_t)p.n_kv_heads * fwd_slot<DP>();
+  const float* slot = p.partial + ((int64_t)e.slot * p.n_kv_heads + kv_head) * fwd_slot<DP>() + threadIdx.x;
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int i = 0; i < e.pieces; ++i) top = fmaxf(top, slot[i * step + DP * 256]);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) o[k] = 0.f;
+#pragma unroll 2
+  for (int i = 0; i < e.pieces; ++i) {
+    const float* from = slot + i * step;
+    const float m = from[DP * 256], f = ex2((m - base) * sign_scale);
+    sum = fmaf(f, from[(DP + 1) * 256], sum);
+    if (m == -INFINITY) continue;  // a piece without keys for this row, whose O may not be there
+#pragma unroll
+    for (int k = 0; k < 16; ++k) o[k] = fmaf(f, from[(col + k) * 256], o[k]);
+  }
+  const float inv = 1.f / sum;
+  __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * p.head_dim + col;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (col + 8 * k < p.head_dim)
+      *reinterpret_cast<uint4*>(dst + 8 * k) =
+          make_uint4(bf16_pair(o[8 * k] * inv, o[8 * k + 1] * inv), bf16_pair(o[8 * k + 2] * inv, o[8 * k + 3] * inv),
+                     bf16_pair(o[8 * k + 4] * inv, o[8 * k + 5] * inv), bf16_pair(o[8 * k + 6] * inv, o[8 * k + 7] * inv));
+  if (col == 0) p.lse[(int64_t)token * p.n_heads + head] = fmaf(base, sign_scale * kLn2, logf(sum));
 }
 
 // ------------------------------------------------------------------------- host side
@@ -429,17 +501,20 @@ int fwd(const Args& a, const Layout& l) {
   if (s == NAT_OK) s = make_map(&mk, a.k, p.head_dim, p.n_kv_heads, a.cap, p.k_stride, 1, kRows);
   if (s == NAT_OK) s = make_map(&mv, a.v, p.head_dim, p.n_kv_heads, a.cap, p.v_stride, 1, kRows);
   if (s != NAT_OK) return s;
-  static std::atomic<uint64_t> allowed;
-  s = allow_smem(attn_fwd_kernel<DP>, FwdShape<DP>::kSmem, dev, &allowed);
+  const bool split = l.split[kPlanFwd];
+  const auto kernel = split ? attn_fwd_kernel<DP, true> : attn_fwd_kernel<DP, false>;
+  static std::atomic<uint64_t> allowed[2];
+  s = allow_smem(kernel, FwdShape<DP>::kSmem, dev, &allowed[split ? 1 : 0]);
   if (s != NAT_OK) return s;
   const int64_t units = l.entries[kPlanFwd] * p.n_kv_heads;
-  const bool plan = units > dev.sms;
+  const bool plan = units > dev.sms || split;
   if (plan) s = launch_plan(a, l, kPlanFwd);
   if (s != NAT_OK) return s;
   FwdParams fp{};
   fp.list = plan ? entries(a, l, kPlanFwd) : nullptr;
   fp.batch = batch(a, l, kPlanFwd);
   fp.count = &head(a)->count[kPlanFwd];
+  fp.partial = partials(a, l, kPlanFwd);
   fp.status = &head(a)->status;
   fp.out = (__nv_bfloat16*)a.out;
   fp.lse = a.lse;
@@ -452,8 +527,14 @@ int fwd(const Args& a, const Layout& l) {
   fp.scale = p.scale;
   const unsigned grid = (unsigned)min((int64_t)dev.sms, units);
   const size_t smem = FwdShape<DP>::kSmem;
-  if (plan) return launch_after(attn_fwd_kernel<DP>, grid, 384, smem, a.stream, "attn_fwd_kernel", mq, mk, mv, fp);
-  attn_fwd_kernel<DP><<<grid, 384, smem, a.stream>>>(mq, mk, mv, fp);
+  if (plan) {
+    s = launch_after(kernel, dim3(grid), 384, smem, a.stream, "attn_fwd_kernel", mq, mk, mv, fp);
+    if (s == NAT_OK && split)
+      s = launch_after(attn_fwd_join_kernel<DP>, dim3((unsigned)units, DP / 16), 256, 0, a.stream,
+                       "attn_fwd_join_kernel", fp);
+    return s;
+  }
+  kernel<<<grid, 384, smem, a.stream>>>(mq, mk, mv, fp);
   NAT_LAUNCH_CHECK("attn_fwd_kernel");
   return NAT_OK;
 }

@@ -27,6 +27,7 @@ struct BwdParams {
   const Entry* list;  // null where every block has one unit at most and finds it itself
   Batch batch;
   const uint32_t* count;
+  float* partial;
   uint32_t* status;
   const float *lse2, *delta;  // [cap, n_heads]
   __nv_bfloat16 *dq, *dk, *dv;
@@ -57,12 +58,12 @@ struct Found {
   Entry entry;
 };
 __device__ __forceinline__ void find(const BwdParams& p, uint32_t block, Found* f, bool report) {
-  uint32_t total;
-  const Entry e = find_entry(p.batch, block / p.n_kv_heads, &total);
+  uint32_t total, status;
+  const Entry e = find_entry(p.batch, block / p.n_kv_heads, &total, &status);
   if ((threadIdx.x & 31) == 0) {
     f->entry = e;
     f->total = total;
-    if (report && block == 0) *p.status = batch_status(p.batch, total);
+    if (report && block == 0) *p.status = status;
   }
 }
 
@@ -98,6 +99,22 @@ __device__ __forceinline__ void store_acc(uint32_t addr, int half, __nv_bfloat16
     tc::tmem_ld32(addr + col, o);
     if (valid) store_row32(dst + col, o, f, D - col, wide);
   }
+}
+
+// A piece's N accumulators, from tensor-memory column `addr` on, to its slot: [accumulator column][row].
+template <int DP, int N>
+__device__ __forceinline__ void store_piece(const BwdParams& p, const Entry& e, int head, uint32_t addr, int half, int row) {
+  float* own = p.partial + ((int64_t)(e.slot + e.piece) * p.n_kv_heads + head) * (128 * N * DP) + row;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) {
+      const int col = half * (DP / 2) + c * 32;
+      float o[32];
+      tc::tmem_ld32(addr + k * 128 + col, o);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) __stcg(own + (k * DP + col + i) * 128, o[i]);
+    }
 }
 
 // A ring of N tiles: `item` numbers the loads of a block, stage item % N.
@@ -180,9 +197,9 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + R::kTiles + R::kStats);
   uint64_t *qdo_full = bars, *qdo_empty = bars + 1, *s_full = bars + 2, *dp_full = bars + 4, *ds_full = bars + 5;
   uint64_t *dq_done = bars + 6, *raw = bars + 7, *drain = bars + 8;
-  const Ring<R::kA> ring_k{tc::smem_u32(tiles_a), bars + 9, bars + 9 + R::kA, R::kTile};
-  const Ring<R::kB> ring_v{tc::smem_u32(tiles_b), bars + 9 + 2 * R::kA, bars + 9 + 2 * R::kA + R::kB, R::kTile};
-  Found* const found = reinterpret_cast<Found*>(bars + ((9 + 2 * (R::kA + R::kB) + 1) & ~1));
+  const Ring<R::kA> ring_k{tc::smem_u32(tiles_a), bars + 10, bars + 10 + R::kA, R::kTile};
+  const Ring<R::kB> ring_v{tc::smem_u32(tiles_b), bars + 10 + 2 * R::kA, bars + 10 + 2 * R::kA + R::kB, R::kTile};
+  Found* const found = reinterpret_cast<Found*>(bars + 10 + 2 * (R::kA + R::kB));
   volatile uint32_t* abort_flag = &found->abort;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
 
@@ -196,7 +213,7 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
     tc::mbar_init(dq_done, 1);
     tc::mbar_init(raw, 1);
     tc::mbar_init(drain, 2);
-    for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[9 + s], 1);
+    for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[10 + s], 1);
     *abort_flag = 0u;
     tc::fence_barrier_init();
   }
@@ -213,7 +230,9 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
   const uint32_t units = (p.list ? *p.count : found->total) * (uint32_t)p.n_kv_heads;
   auto entry_of = [&](uint32_t u) { return p.list ? p.list[u / p.n_kv_heads] : found->entry; };
   // tiles of keys of a list entry
-  auto tiles_of = [&](const Entry& e) { return (min(e.lo + p.tq, e.seq_hi) - e.seq_lo + kRows - 1) / kRows; };
+  auto tiles_of = [&](const Entry& e) {
+    return min((min(e.lo + p.tq, e.seq_hi) - e.seq_lo + kRows - 1) / kRows, e.end) - e.begin;
+  };
 
   if (warp == 9) {
     Loader<DP> ld{raw, abort_flag, lane};
@@ -234,7 +253,7 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
       }
       const int end = min(e.lo + p.tq, e.seq_hi);
       for (int j = 0; ld.ok && j < n; ++j, ++item) {
-        const int row = e.seq_lo + j * kRows;
+        const int row = e.seq_lo + (e.begin + j) * kRows;
         // K is also the second factor of dS K, where rows past the end must not count; V only
         // meets the mask of dS
         ld.load(ring_k, item, tiles_a, &map_k, head, row, kRows, min(end - row, kRows));
@@ -342,7 +361,7 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
           x[c] = g.x;
           x[c + 1] = g.y;
         }
-        const int kv0 = e.seq_lo + j * kRows;
+        const int kv0 = e.seq_lo + (e.begin + j) * kRows;
         if (kv0 + kRows - 1 > e.lo) {  // the tile touches the diagonal
           const int last = token - kv0 - half * 64;
 #pragma unroll
@@ -358,8 +377,12 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
       if (!ok) break;
       ++turns;
       tc::fence_after_sync();
-      store_acc<DP>(tmem + 384 + lane_base, half,
-                    p.dq + (int64_t)token * p.q_stride + (int64_t)head * p.head_dim, p.head_dim, p.scale, valid, wide);
+      __nv_bfloat16* dst = p.dq + (int64_t)token * p.q_stride + (int64_t)head * p.head_dim;
+      if (e.pieces == 1) {
+        store_acc<DP>(tmem + 384 + lane_base, half, dst, p.head_dim, p.scale, valid, wide);
+      } else {
+        store_piece<DP, 1>(p, e, (int)(u % p.n_kv_heads), tmem + 384 + lane_base, half, row);
+      }
       tc::fence_before_sync();
     }
   }
@@ -435,7 +458,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
   const uint32_t units = (p.list ? *p.count : found->total) * (uint32_t)p.n_kv_heads;
   auto entry_of = [&](uint32_t u) { return p.list ? p.list[u / p.n_kv_heads] : found->entry; };
   // tiles of queries of a list entry: they start at the key tile's first token
-  auto tiles_of = [&](const Entry& e) { return (e.seq_hi - e.lo + p.tq - 1) / p.tq; };
+  auto tiles_of = [&](const Entry& e) { return min((e.seq_hi - e.lo + p.tq - 1) / p.tq, e.end) - e.begin; };
 
   if (warp == 9) {
     Loader<DP> ld{raw, abort_flag, lane};
@@ -444,7 +467,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
       const Entry e = entry_of(u);
       const int head = (int)(u % p.n_kv_heads), n = tiles_of(e);
       auto load_q = [&](int j) {
-        const int row = e.lo + j * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
+        const int row = e.lo + (e.begin + j) * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
         ld.load(ring_q, item, tiles_a, &map_q, head * p.group, row, q_rows, valid);
       };
       // the unit's first query tile does not wait for the end of the unit before
@@ -462,7 +485,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
       }
       for (int j = 0; ld.ok && j < n; ++j, ++item) {
         if (j > 0) load_q(j);
-        const int row = e.lo + j * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
+        const int row = e.lo + (e.begin + j) * p.tq, valid = min((e.seq_hi - row) * p.group, q_rows);
         if (ld.ok) ld.load(ring_do, item, tiles_b, &map_do, head * p.group, row, q_rows, valid);
       }
     }
@@ -480,7 +503,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
       const Entry e = entry_of(u);
       const int head = (int)(u % p.n_kv_heads) * p.group, n = tiles_of(e);
       for (int j = 0; j < n; ++j, ++tile) {
-        const int first = e.lo + j * p.tq, valid = min((e.seq_hi - first) * p.group, q_rows);
+        const int first = e.lo + (e.begin + j) * p.tq, valid = min((e.seq_hi - first) * p.group, q_rows);
         float a[4], b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -588,7 +611,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
       const Entry e = entry_of(u);
       const int n = tiles_of(e), key = e.lo + row;
       for (int j = 0; j < n; ++j, ++tile) {
-        const int first = e.lo + j * p.tq, rows = min((e.seq_hi - first) * p.group, q_rows);
+        const int first = e.lo + (e.begin + j) * p.tq, rows = min((e.seq_hi - first) * p.group, q_rows);
         const float4* slot = reinterpret_cast<const float4*>(stats + (tile & 1) * 2 * kRows + half * 64);
         ok = warp_wait(&st_full[tile & 1], (tile >> 1) & 1, abort_flag) && warp_wait(s_full, tile & 1, abort_flag);
         if (!ok) break;
@@ -655,8 +678,13 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
       tc::fence_after_sync();
       const bool valid = key < e.seq_hi;
       const int64_t col = (int64_t)(u % p.n_kv_heads) * p.head_dim;
-      store_acc<DP>(tmem + 256 + lane_base, half, p.dv + (int64_t)key * p.v_stride + col, p.head_dim, 1.f, valid, wide);
-      store_acc<DP>(tmem + 384 + lane_base, half, p.dk + (int64_t)key * p.k_stride + col, p.head_dim, p.scale, valid, wide);
+      __nv_bfloat16 *dv = p.dv + (int64_t)key * p.v_stride + col, *dk = p.dk + (int64_t)key * p.k_stride + col;
+      if (e.pieces == 1) {
+        store_acc<DP>(tmem + 256 + lane_base, half, dv, p.head_dim, 1.f, valid, wide);
+        store_acc<DP>(tmem + 384 + lane_base, half, dk, p.head_dim, p.scale, valid, wide);
+      } else {
+        store_piece<DP, 2>(p, e, (int)(u % p.n_kv_heads), tmem + 256 + lane_base, half, row);
+      }
       tc::fence_before_sync();
     }
   }
@@ -679,6 +707,44 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     dkv_part<DP>(map_q, map_k, map_v, map_do, dkv, blockIdx.x - dq_blocks, gridDim.x - dq_blocks);
 }
 
+// Adds up the pieces of a tile, in their order: a block takes 16 columns of the 128 rows of a list entry (of
+// dQ, or of dV and dK), a thread a row.
+template <int DP>
+__global__ void __launch_bounds__(128) attn_bwd_join_kernel(const BwdParams dq, const BwdParams dkv, unsigned dq_units) {
+  wait_for_primary();
+  const bool keys = blockIdx.x >= dq_units;
+  const BwdParams& p = keys ? dkv : dq;
+  const unsigned unit = keys ? blockIdx.x - dq_units : blockIdx.x;
+  if (!p.partial || unit / p.n_kv_heads >= *p.count) return;
+  const Entry e = p.list[unit / p.n_kv_heads];
+  if (e.piece != 0 || e.pieces == 1) return;
+  const int kv_head = (int)(unit % p.n_kv_heads), columns = keys ? 2 * DP : DP, row = threadIdx.x;
+  if ((int)blockIdx.y * 16 >= columns) return;
+  const int of = blockIdx.y * 16 / DP, col = blockIdx.y * 16 % DP;  // of keys: dV first, then dK
+  const int token = keys ? e.lo + row : e.lo + row / p.group;
+  if (token >= e.seq_hi || col >= p.head_dim || (!keys && row >= p.group * p.tq)) return;
+  const int64_t size = 128 * columns, step = (int64_t)p.n_kv_heads * size;
+  const float* slot = p.partial + ((int64_t)e.slot * p.n_kv_heads + kv_head) * size + blockIdx.y * 16 * 128 + row;
+  float o[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) o[k] = 0.f;
+#pragma unroll 2
+  for (int i = 0; i < e.pieces; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) o[k] += slot[i * step + k * 128];
+  __nv_bfloat16* dst =
+      !keys ? p.dq + (int64_t)token * p.q_stride + (int64_t)(kv_head * p.group + row % p.group) * p.head_dim
+            : (of == 0 ? p.dv + (int64_t)token * p.v_stride : p.dk + (int64_t)token * p.k_stride) +
+                  (int64_t)kv_head * p.head_dim;
+  const float f = keys && of == 0 ? 1.f : p.scale;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (col + 8 * k < p.head_dim)
+      *reinterpret_cast<uint4*>(dst + col + 8 * k) =
+          make_uint4(bf16_pair(o[8 * k] * f, o[8 * k + 1] * f), bf16_pair(o[8 * k + 2] * f, o[8 * k + 3] * f),
+                     bf16_pair(o[8 * k + 4] * f, o[8 * k + 5] * f), bf16_pair(o[8 * k + 6] * f, o[8 * k + 7] * f));
+}
+
 template <int DP>
 int bwd(const Args& a, const Layout& l) {
   const nat_attn_params& p = a.p;
@@ -695,7 +761,7 @@ int bwd(const Args& a, const Layout& l) {
   if (s == NAT_OK) s = allow_smem(attn_bwd_kernel<DP>, smem, dev, &allowed);
   if (s != NAT_OK) return s;
   const int64_t units_q = l.entries[kPlanDq] * p.n_kv_heads, units_k = l.entries[kPlanDkv] * p.n_kv_heads;
-  const bool plan = units_q > dev.sms || units_k > dev.sms;
+  const bool plan = units_q > dev.sms || units_k > dev.sms || l.split[kPlanDq] || l.split[kPlanDkv];
   s = launch_bwd_prologue(a, l, plan);
   if (s != NAT_OK) return s;
   BwdParams bp{};
@@ -718,12 +784,18 @@ int bwd(const Args& a, const Layout& l) {
     BwdParams w = bp;
     w.list = plan ? entries(a, l, which) : nullptr;
     w.count = &head(a)->count[which];
+    w.partial = l.split[which] ? partials(a, l, which) : nullptr;
     w.batch = batch(a, l, which);
     return w;
   };
   const unsigned blocks_q = (unsigned)min((int64_t)dev.sms, units_q), blocks_k = (unsigned)min((int64_t)dev.sms, units_k);
-  return launch_after(attn_bwd_kernel<DP>, blocks_q + blocks_k, 384, smem, a.stream, "attn_bwd_kernel", mq, mk, mv, mdo,
-                      part(kPlanDq), part(kPlanDkv), blocks_q);
+  const BwdParams dq = part(kPlanDq), dkv = part(kPlanDkv);
+  s = launch_after(attn_bwd_kernel<DP>, dim3(blocks_q + blocks_k), 384, smem, a.stream, "attn_bwd_kernel", mq, mk, mv,
+                   mdo, dq, dkv, blocks_q);
+  if (s == NAT_OK && (l.split[kPlanDq] || l.split[kPlanDkv]))
+    s = launch_after(attn_bwd_join_kernel<DP>, dim3((unsigned)(units_q + units_k), 2 * DP / 16), 128, 0, a.stream,
+                     "attn_bwd_join_kernel", dq, dkv, (unsigned)units_q);
+  return s;
 }
 
 }  // namespace

@@ -112,9 +112,9 @@ __device__ __forceinline__ float sum16(float x) {
 
 // Every block finds its tile; the first one reports what is wrong with the batch.
 __device__ __forceinline__ bool my_tile(const Batch& batch, Head* head, Entry* e) {
-  uint32_t total;
-  *e = find_entry(batch, blockIdx.x, &total);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = batch_status(batch, total);
+  uint32_t total, status;
+  *e = find_entry(batch, blockIdx.x, &total, &status);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = status;
   return blockIdx.x < total;
 }
 

@@ -234,6 +234,45 @@ def test_attn_rows_beyond_the_capacity(dtype):
         assert torch.equal(getattr(a, name), getattr(b, name)), name
 
 
+@pytest.mark.parametrize("cap", [150, 3000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attn_bounds_that_do_not_ascend(dtype, cap):
+    a = Attn([60, 90], 4, 2, 64, DT[dtype], seed=10, spare=cap - 150)
+    a.fwd()
+    for cu in ([0, 90, 60], [-5, 20, 40], [5, 2 ** 31 - 1, 40]):
+        a.cu.copy_(torch.tensor(cu, dtype=torch.int32))
+        for t in (a.out, a.dq, a.dk, a.dv):
+            t.fill_(7.0)
+        a.fwd()
+        assert nat.nat_poll_status(a.ws) == nat.NAT_DEV_CAPACITY
+        a.bwd()
+        assert nat.nat_poll_status(a.ws) == nat.NAT_DEV_CAPACITY
+        for t in (a.out, a.dq, a.dk, a.dv):
+            assert (t == 7).all()
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 128), (2, 2, 64), (7, 1, 96), (1, 1, 128)])
+@pytest.mark.parametrize("lengths", [[2100], [1500, 3, 700], [0, 1029, 0, 1]])
+def test_attn_long_rows_of_few_heads(lengths, heads):
+    """Few tiles with many steps: cut into pieces, whose partial results are joined."""
+    a = Attn(lengths, *heads, torch.bfloat16, seed=12)
+    a.check()
+    got = [t[:a.n].clone() for t in (a.out, a.lse, a.dq, a.dk, a.dv)]
+    a.ws.random_(0, 255)
+    for _ in range(3):
+        a.fwd()
+        a.bwd()
+        assert all(torch.equal(x, y[:a.n]) for x, y in zip(got, (a.out, a.lse, a.dq, a.dk, a.dv)))
+
+
+def test_attn_long_rows_with_growing_scores():
+    a = Attn([1900], 4, 2, 64, torch.bfloat16, seed=13)
+    ramp = torch.linspace(0.05, 6.0, a.cap, device="cuda")[:, None, None]
+    a.k.copy_((a.k[:1].float().abs() * ramp).to(torch.bfloat16))
+    a.q.copy_(a.q.abs())
+    a.check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attn_offsets_past_32_bits(dtype):
     """Token strides so wide that the last rows lie more than 2^31 elements behind the first."""
