@@ -229,8 +229,8 @@ Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
   for (int w = 0; w < 3; ++w) {
     // a sequence's last tile may be part full: at most one extra tile for each sequence
     const int64_t tiles = cap / plan_tile(p, (Plan)w) + B;
-    // Few tiles, each with many steps: cut into pieces.
-    l.split[w] = p.dtype == NAT_BF16 && cap > 1024 && tiles * p.n_kv_heads <= kSplitBlocks;
+    // Few tiles (under two for each multiprocessor), each with many steps: cut into pieces.
+    l.split[w] = p.dtype == NAT_BF16 && cap > 1024 && tiles * p.n_kv_heads <= 2 * 148;
     pieces[w] = l.split[w] ? tiles + (kSplitBlocks + p.n_kv_heads - 1) / p.n_kv_heads : 0;
     l.entries[w] = l.split[w] ? pieces[w] : tiles;
     l.plan_off[w] = at;
