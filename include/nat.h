@@ -373,8 +373,13 @@ int nat_policy_loss_fwd_bwd(const nat_loss_params* params /* host */, const void
  * strides are multiples of 8 elements, rows 16-byte aligned.  Outputs must not overlap inputs.
  * dtype NAT_BF16: products on the tensor cores with fp32 accumulation, P and dS rounded to
  * bfloat16 for the second product; NAT_F32: plain fp32 arithmetic (meant for small problems).
+ * Infinities and NaN stay in their sequence.  Within it NAT_F32 confines them to the tokens that see
+ * them; with NAT_BF16 one in v (backward: in q, k or dout) may also reach tokens less than 128 away,
+ * through the masked part of a tile.
  * workspace: nat_attn_workspace_bytes(params, B, cap), shared by forward and backward; it holds
- * nothing that must survive between them.
+ * nothing that must survive between them, and calls that may run at the same time need one each.
+ * (About 100 MB where few long sequences are cut into pieces, 20 bytes a row and head or less otherwise.)
+ * A call with B = 0 or cap = 0 does nothing, not even to the status word.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t n_heads, n_kv_heads, head_dim;

@@ -84,7 +84,7 @@ const char* nat_status_string(int status) {
 
 const char* nat_last_error(void) { return nat::error_buffer(); }
 
-int nat_version(void) { return 2; }
+int nat_version(void) { return 3; }
 
 int nat_poll_status(const void* workspace, void* stream, uint32_t* host_word) {
   if (!workspace || !host_word)

@@ -14,6 +14,10 @@
 // the tensor pipe holds about one MMA beyond the running one, so with one issuing warp every wait and
 // every commit between two products leaves it idle.  In dkv the warps have a chain each, S' and dV, dP'
 // and dK, which share no tensor memory; in dq one has S, the other dP and dQ.
+//
+// 16 sequences of up to 8192 tokens, 32 heads over 8, 128 columns: 4.8 ms, 700 TFLOP/s counted (980 executed), at the
+// 1000 W cap (1450 MHz).  A step of 128 x 128 takes 2640 cycles in dq (products alone 1536) and 2930 in dkv
+// (2048); of either about 1200-1450 are the exponentials, which both halves of the threads take at once.
 #include <cuda.h>
 
 #include "nat_attn.cuh"

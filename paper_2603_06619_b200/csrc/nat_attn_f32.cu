@@ -4,6 +4,9 @@
 // shared memory feed 64 FMAs (the FMA pipe, not shared memory, is the limit).  The 16 threads of a row
 // are half a warp, so its softmax is four shuffles; P passes through shared memory into the second
 // product, whose 64 x D tile the threads share as four rows by D / 16 columns.
+//
+// 8 sequences of 600..700 tokens, 16 heads over 4, 128 columns: forward 0.57 ms (24.6 TFLOP/s counted; a causal tile's
+// masked half included about 30), backward 2.2 ms (16 TFLOP/s, with seven products for the five counted).
 #include "nat_attn.cuh"
 
 namespace nat {

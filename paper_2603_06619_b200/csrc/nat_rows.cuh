@@ -97,12 +97,6 @@ __device__ __forceinline__ void copies_wait(int ahead) {
   else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
-__device__ __forceinline__ void copy_raw(Raw<__nv_bfloat16>* slot, const __nv_bfloat16* p) { copy_async<16>(slot, p); }
-__device__ __forceinline__ void copy_raw(Raw<float>* slot, const float* p) {
-  copy_async<16>(&slot->a, p);
-  copy_async<16>(&slot->b, p + 4);
-}
-
 __device__ __forceinline__ void load_weights(const float* p, float2 (&w)[kPairs]) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(p));
   const float4 b = __ldg(reinterpret_cast<const float4*>(p) + 1);

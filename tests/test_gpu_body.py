@@ -528,3 +528,60 @@ def test_row_operators_past_32_bits():
     nat.nat_resnorm_fwd(p, x, x, w, None, w, None, n, back, h, ry, rr)
     nat.nat_resnorm_fwd(p, tail[0], tail[0], w, None, w, None, 100, r1, h1, ry[:100], rr[:100])
     assert torch.equal(back[-100:], r1) and torch.equal(h[-100:], h1)
+
+
+def test_attn_float32_confines_infinities_to_the_tokens_that_see_them():
+    a, b = (Attn([150], 4, 2, 64, torch.float32, seed=21) for _ in range(2))
+    t = 70
+    for x in (b.k, b.v):
+        x[t] = float("inf")
+    for s in (a, b):
+        s.fwd()
+    assert torch.equal(a.out[:t], b.out[:t]) and torch.equal(a.lse[:t], b.lse[:t])
+    assert not torch.isfinite(b.out[t:150]).any()
+    # a query's infinity reaches the keys that it sees, and no others
+    a, b = (Attn([150], 4, 2, 64, torch.float32, seed=21) for _ in range(2))
+    for s in (a, b):
+        s.fwd()
+    b.dout[t] = float("inf")
+    for s in (a, b):
+        s.bwd()
+    for name in ("dk", "dv"):
+        assert torch.equal(getattr(a, name)[t + 1:150], getattr(b, name)[t + 1:150]), name
+    assert torch.equal(a.dq[:t], b.dq[:t]) and torch.equal(a.dq[t + 1:150], b.dq[t + 1:150])
+
+
+def test_attn_bfloat16_infinities_reach_less_than_128_tokens():
+    a, b = (Attn([900], 4, 2, 64, torch.bfloat16, seed=22) for _ in range(2))
+    t = 500
+    b.v[t] = float("inf")
+    b.k[t] = float("nan")
+    for s in (a, b):
+        s.fwd()
+        s.bwd()
+    keep = t - 127
+    assert torch.equal(a.out[:keep], b.out[:keep]) and torch.equal(a.lse[:t], b.lse[:t])
+    assert torch.equal(a.dq[:keep], b.dq[:keep])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attn_gradient_against_differences(dtype):
+    """The kernel's gradient against differences of the float64 forward along random directions (the
+    kernel's inputs are exact in float64; the differences' own error is below 1e-6 of the norms)."""
+    a = Attn([90, 41], 4, 2, 64, DT[dtype], seed=23, spare=0)
+    a.fwd()
+    a.bwd()
+    q, k, v, w = (_np(t) for t in (a.q, a.k, a.v, a.dout))
+    g = np.random.default_rng(0)
+    f = lambda q, k, v: float((w * ob.attn_fwd(q, k, v, a.cu_h, a.params.scale)[0]).sum())  # noqa: E731
+    for name, which in (("dq", 0), ("dk", 1), ("dv", 2)):
+        got = _np(getattr(a, name))
+        step = g.normal(size=got.shape)
+        lo, hi = [q, k, v], [q, k, v]
+        lo[which], hi[which] = lo[which] - 1e-5 * step, hi[which] + 1e-5 * step
+        want = (f(*hi) - f(*lo)) / 2e-5
+        # a rounding of u of every element moves the sum by at most u times the norms' product; bfloat16
+        # rounds out (which delta reads), P, dS and the result: 4 u of the gradient's largest scale
+        u = _half(DT[dtype]) if dtype == "bf16" else 2.0 ** -16
+        scale = np.linalg.norm(got) * np.linalg.norm(step)
+        assert abs((got * step).sum() - want) <= 4 * u * scale + 1e-6 * scale, name
