@@ -154,29 +154,6 @@ struct Device {
 };
 int device(Device* d);
 
-// Kernel launches that may begin before the kernel in front of them on the stream has ended: such a
-// kernel calls wait_for_primary() before it touches anything that one wrote.
-__device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void release_secondary() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-template <typename... P, typename... A>
-int launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream,
-                 const char* name, const A&... args) {
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  const int s = check_cuda(cudaLaunchKernelEx(&cfg, kernel, args...), name);
-  if (s != NAT_OK) return s;
-  NAT_LAUNCH_CHECK(name);
-  return NAT_OK;
-}
-
 // Raises a kernel's shared-memory limit, once for each device.
 template <typename K>
 int allow_smem(K kernel, size_t smem, const Device& d, std::atomic<uint64_t>* devices) {

@@ -30,13 +30,22 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kT * DP / 4 / kThreads; ++i) {
       const int k = threadIdx.x + i * kThreads, r = k / (DP / 4), c = k % (DP / 4) * 4;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (lo + r < hi && c < D)
-        v = __ldg(reinterpret_cast<const float4*>(base + (int64_t)(lo + r) * stride + (int64_t)head * D + c));
-      *reinterpret_cast<float4*>(at + r * kLead + c) = v;
+      const bool in = lo + r < hi && c < D;
+      const float* src = in ? base + (int64_t)(lo + r) * stride + (int64_t)head * D + c : base;
+      // asynchronous, so that the tiles of a step come together; zero bytes read is zeros written
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                       (uint32_t)__cvta_generic_to_shared(at + r * kLead + c)),
+                   "l"(src), "r"(in ? 16 : 0)
+                   : "memory");
     }
   }
 };
+
+// The tiles that were asked for are there, for all threads.
+__device__ __forceinline__ void tiles_ready() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+}
 
 // s[i][j] = row (ty + 16 i) of a . row (tx + 16 j) of b
 template <int DP>
@@ -144,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) f32_fwd_kernel(Ptrs a, Batch batch, 
     __syncthreads();
     K.load(a.k, a.p.k_stride, kh, D, k0, end);
     V.load(a.v, a.p.v_stride, kh, D, k0, end);
-    __syncthreads();
+    tiles_ready();
     float s[4][4];
     dots<DP>(Q, K, ty, tx, s);
     int last[4];
@@ -199,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) f32_dq_kernel(Ptrs a, Batch batch, H
   Q.load(a.q, a.p.q_stride, h, D, e.lo, e.seq_hi);
   G.load(a.dout, a.p.o_stride, h, D, e.lo, e.seq_hi);
   K.load(a.out, a.p.o_stride, h, D, e.lo, e.seq_hi);
-  __syncthreads();
+  tiles_ready();
   float delta[4], lse[4], acc[4][DP / 16];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -222,7 +231,7 @@ __global__ void __launch_bounds__(kThreads) f32_dq_kernel(Ptrs a, Batch batch, H
     __syncthreads();
     K.load(a.k, a.p.k_stride, kh, D, k0, end);
     V.load(a.v, a.p.v_stride, kh, D, k0, end);
-    __syncthreads();
+    tiles_ready();
     float s[4][4], dp[4][4];
     dots<DP>(Q, K, ty, tx, s);
     dots<DP>(G, V, ty, tx, dp);
@@ -278,7 +287,7 @@ __global__ void __launch_bounds__(kThreads) f32_dkv_kernel(Ptrs a, Batch batch, 
         lse[j] = row < e.seq_hi ? a.lse[at] : 0.f;
         delta[j] = row < e.seq_hi ? a.delta[at] : 0.f;
       }
-      __syncthreads();
+      tiles_ready();
       float s[4][4], dp[4][4];
       dots<DP>(K, Q, ty, tx, s);
       dots<DP>(V, G, ty, tx, dp);

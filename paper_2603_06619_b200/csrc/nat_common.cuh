@@ -36,6 +36,29 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // The tensor-core kernels only exist for compute capability 10.x.
 int require_sm100();
 
+// Kernel launches that may begin before the kernel in front of them on the stream has ended: such a
+// kernel calls wait_for_primary() before it touches anything that one wrote.
+__device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void release_secondary() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... P, typename... A>
+int launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream,
+                 const char* name, const A&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const int s = check_cuda(cudaLaunchKernelEx(&cfg, kernel, args...), name);
+  if (s != NAT_OK) return s;
+  NAT_LAUNCH_CHECK(name);
+  return NAT_OK;
+}
+
 // ---- entry points of the per-dtype loss implementations -------------------
 struct LossArgs {
   nat_loss_params p;

@@ -457,6 +457,7 @@ resnorm_columns_kernel(const float* __restrict__ partial, int blocks, int d, int
                        const float* __restrict__ w_post, const float* __restrict__ gate,
                        float* __restrict__ dw_post, float* __restrict__ dgate,
                        float* __restrict__ dw_pre) {
+  wait_for_primary();
   __shared__ float part[8][33];
   const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;  // over 2 d columns
@@ -668,10 +669,10 @@ int nat_resnorm_bwd(const nat_resnorm_params* p, const void* y, const void* r, c
   if (s != NAT_OK) return s;
   const bool channel = p->gate_mode == NAT_GATE_CHANNEL;
   if (w_post || w_pre || channel) {
-    nat::resnorm_columns_kernel<<<(2 * p->d + 31) / 32, 256, 0, (cudaStream_t)stream>>>(
-        a.partial, (int)blocks, p->d, channel ? 1 : 0, w_post, gate, w_post ? dw_post : nullptr, dgate,
-        w_pre ? dw_pre : nullptr);
-    NAT_LAUNCH_CHECK("resnorm_columns_kernel");
+    return nat::launch_after(nat::resnorm_columns_kernel, dim3((2 * p->d + 31) / 32), 256, 0, (cudaStream_t)stream,
+                             "resnorm_columns_kernel", (const float*)a.partial, (int)blocks, (int)p->d,
+                             channel ? 1 : 0, w_post, gate, w_post ? dw_post : nullptr, dgate,
+                             w_pre ? dw_pre : nullptr);
   }
   return NAT_OK;
 }
