@@ -34,12 +34,10 @@ __device__ __forceinline__ void plan(const PlanArgs& a) {
   const int64_t cap = a.batch.cap;
   const int tile = a.batch.tile;
   __shared__ uint32_t bucket[kBuckets], warp_sum[32], next_slot;
-  __shared__ int longest;
   __shared__ unsigned long long work;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bucket[threadIdx.x] = 0u;
   if (threadIdx.x == 0) {
-    longest = 1;
     work = 0ull;
     next_slot = 0u;
   }
@@ -68,20 +66,16 @@ __device__ __forceinline__ void plan(const PlanArgs& a) {
       for (int t = few ? threadIdx.x : lane; t < tiles; t += few ? 1024 : 32) visit(lo, hi, t);
     }
   };
-  unsigned long long my_work = 0ull;
-  int my_longest = 1;
-  for_tiles([&](int lo, int hi, int t) {
-    const int steps = steps_of(lo, hi, t);
-    my_work += steps;
-    my_longest = max(my_longest, steps);
-  });
-  atomicMax(&longest, my_longest);
-  if (my_work) atomicAdd(&work, my_work);
-  __syncthreads();
   int chunk = kAllSteps;
-  if (a.split) chunk = (int)max((unsigned long long)kMinPiece, (work * a.heads + kSplitBlocks - 1) / kSplitBlocks);
+  if (a.split) {
+    unsigned long long mine = 0ull;
+    for_tiles([&](int lo, int hi, int t) { mine += steps_of(lo, hi, t); });
+    if (mine) atomicAdd(&work, mine);
+    __syncthreads();
+    chunk = (int)max((unsigned long long)kMinPiece, (work * a.heads + kSplitBlocks - 1) / kSplitBlocks);
+  }
   int shift = 0;
-  while ((min(longest, chunk) >> shift) >= kBuckets) ++shift;
+  while ((min((int)((cap + a.span - 1) / a.span), chunk) >> shift) >= kBuckets) ++shift;
   for (int pass = 0; pass < 2; ++pass) {
     for_tiles([&](int lo, int hi, int t) {
       const int steps = steps_of(lo, hi, t);

@@ -140,137 +140,137 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   // 168 registers a thread at launch: the softmax warpgroups, which hold a row of scores, take
   // some of the third's (2 x 192 + 120 = 3 x 168)
   if (warp >= 8) {
-  regs_dec<120>();
-  if (warp == 9) {
-    // ---------------------------------------------------------------- loads
-    uint32_t item = 0, raw_turns = 0, q_turns[2] = {0, 0};
-    bool ok = true;
-    const uint32_t q_bytes = (uint32_t)(p.group * p.tq) * 128u * R::kNP;
-    auto load_q = [&](const Unit& w, int t) {
-      if (w.nk[t] == 0) return;
-      ok = ok && warp_wait(&q_empty[t], (q_turns[t] & 1) ^ 1, abort_flag);
-      if (!ok) return;
-      ++q_turns[t];
-      if (lane == 0) {
-        tc::mbar_arrive_expect_tx(&q_full[t], q_bytes);
-        for (int c = 0; c < R::kNP; ++c)
-          tma_load_3d(tc::smem_u32(smem + t * R::kTile + c * kPanel), &map_q, &q_full[t], c * 64,
-                      w.head * p.group, w.lo + t * p.tq);
-      }
-    };
-    auto load_kv = [&](const CUtensorMap* map, const Unit& w, int j, bool is_v) {
-      const int s = item % kNS;
-      ok = ok && warp_wait(&empty[s], ((item / kNS) & 1) ^ 1, abort_flag);
-      if (!ok) return;
-      ++item;
-      const int row = w.seq_lo + (w.begin + j) * kRows, valid = w.kv_hi - row;
-      const bool fix = is_v && valid < kRows;
-      uint64_t* bar = fix ? raw : &full[s];
-      uint8_t* dst = ring + s * R::kTile;
-      if (lane == 0) {
-        tc::mbar_arrive_expect_tx(bar, R::kTile);
-        for (int c = 0; c < R::kNP; ++c)
-          tma_load_3d(tc::smem_u32(dst + c * kPanel), map, bar, c * 64, w.head, row);
-      }
-      if (fix) {
-        ok = warp_wait(raw, raw_turns & 1, abort_flag);
-        ++raw_turns;
+    regs_dec<120>();
+    if (warp == 9) {
+      // ---------------------------------------------------------------- loads
+      uint32_t item = 0, raw_turns = 0, q_turns[2] = {0, 0};
+      bool ok = true;
+      const uint32_t q_bytes = (uint32_t)(p.group * p.tq) * 128u * R::kNP;
+      auto load_q = [&](const Unit& w, int t) {
+        if (w.nk[t] == 0) return;
+        ok = ok && warp_wait(&q_empty[t], (q_turns[t] & 1) ^ 1, abort_flag);
         if (!ok) return;
-        zero_rows<R::kNP>(dst, valid, lane);
-        if (lane == 0) tc::mbar_arrive(&full[s]);
-      }
-    };
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of<SPLIT>(p, found, u);
-      const int n = max(w.nk[0], w.nk[1]);
-      for (int j = 0; ok && j < n; ++j) {
-        if (j == 0) load_q(w, 0);
-        load_kv(&map_k, w, j, false);
-        if (j == 0) load_q(w, 1);
-        load_kv(&map_v, w, j, true);
-      }
-    }
-    // the block must not leave with a copy in flight: every tile that was loaded has to have landed
-    if (!ok) {
-      uint32_t never = 0u;
-      if (raw_turns) tc::mbar_wait(raw, (raw_turns - 1) & 1, &never, 1000000000ull), never = 0u;
-      for (uint32_t i = item > (uint32_t)kNS ? item - kNS : 0; i < item; ++i)
-        tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, &never, 1000000000ull), never = 0u;
-      for (int t = 0; t < 2; ++t)
-        if (q_turns[t]) tc::mbar_wait(&q_full[t], (q_turns[t] - 1) & 1, &never, 1000000000ull), never = 0u;
-    }
-  } else if (warp == 8) {
-    // ---------------------------------------------------------------- MMAs
-    constexpr uint32_t kIdescO = tc::instr_desc_bf16(128, DP, 0, 1);
-    const int ksteps = (p.head_dim + 15) / 16;
-    const uint32_t q_addr = tc::smem_u32(smem), ring_addr = tc::smem_u32(ring);
-    uint32_t item = 0, q_turns = 0, p_turns = 0;  // bit t of q_turns, p_turns: the next phase of row tile t
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = ok && warp_wait(bar, parity & 1, abort_flag);
-      tc::fence_after_sync();
-    };
-    auto scores = [&](int t, uint32_t k_item, bool last) {
-      if (elect_one()) {
-        product_kk<DP>(tmem + t * 128, q_addr + t * R::kTile, ring_addr + (k_item % kNS) * R::kTile, ksteps);
-        tc::umma_commit(&s_full[t]);  // which also says that O += P V of the step before is complete
-        if (last) tc::umma_commit(&q_empty[t]);
-      }
-      __syncwarp();
-    };
-    auto release = [&](uint32_t i) {
-      if (elect_one()) tc::umma_commit(&empty[i % kNS]);
-      __syncwarp();
-    };
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit w = unit_of<SPLIT>(p, found, u);
-      const int n = max(w.nk[0], w.nk[1]);
-      // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
-      wait(&full[item % kNS], item / kNS);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (w.nk[t]) {
-          wait(&q_full[t], q_turns >> t);
-          q_turns ^= 1u << t;
-          if (!ok) break;
-          scores(t, item, w.nk[t] == 1);
+        ++q_turns[t];
+        if (lane == 0) {
+          tc::mbar_arrive_expect_tx(&q_full[t], q_bytes);
+          for (int c = 0; c < R::kNP; ++c)
+            tma_load_3d(tc::smem_u32(smem + t * R::kTile + c * kPanel), &map_q, &q_full[t], c * 64,
+                        w.head * p.group, w.lo + t * p.tq);
         }
-      if (!ok) break;
-      release(item);
-      for (int j = 0; ok && j < n; ++j) {
-        const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
-        wait(&full[v_item % kNS], v_item / kNS);
-        if (j + 1 < n) wait(&full[k_next % kNS], k_next / kNS);
+      };
+      auto load_kv = [&](const CUtensorMap* map, const Unit& w, int j, bool is_v) {
+        const int s = item % kNS;
+        ok = ok && warp_wait(&empty[s], ((item / kNS) & 1) ^ 1, abort_flag);
+        if (!ok) return;
+        ++item;
+        const int row = w.seq_lo + (w.begin + j) * kRows, valid = w.kv_hi - row;
+        const bool fix = is_v && valid < kRows;
+        uint64_t* bar = fix ? raw : &full[s];
+        uint8_t* dst = ring + s * R::kTile;
+        if (lane == 0) {
+          tc::mbar_arrive_expect_tx(bar, R::kTile);
+          for (int c = 0; c < R::kNP; ++c)
+            tma_load_3d(tc::smem_u32(dst + c * kPanel), map, bar, c * 64, w.head, row);
+        }
+        if (fix) {
+          ok = warp_wait(raw, raw_turns & 1, abort_flag);
+          ++raw_turns;
+          if (!ok) return;
+          zero_rows<R::kNP>(dst, valid, lane);
+          if (lane == 0) tc::mbar_arrive(&full[s]);
+        }
+      };
+      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Unit w = unit_of<SPLIT>(p, found, u);
+        const int n = max(w.nk[0], w.nk[1]);
+        for (int j = 0; ok && j < n; ++j) {
+          if (j == 0) load_q(w, 0);
+          load_kv(&map_k, w, j, false);
+          if (j == 0) load_q(w, 1);
+          load_kv(&map_v, w, j, true);
+        }
+      }
+      // the block must not leave with a copy in flight: every tile that was loaded has to have landed
+      if (!ok) {
+        uint32_t never = 0u;
+        if (raw_turns) tc::mbar_wait(raw, (raw_turns - 1) & 1, &never, 1000000000ull), never = 0u;
+        for (uint32_t i = item > (uint32_t)kNS ? item - kNS : 0; i < item; ++i)
+          tc::mbar_wait(&full[i % kNS], (i / kNS) & 1, &never, 1000000000ull), never = 0u;
+        for (int t = 0; t < 2; ++t)
+          if (q_turns[t]) tc::mbar_wait(&q_full[t], (q_turns[t] - 1) & 1, &never, 1000000000ull), never = 0u;
+      }
+    } else if (warp == 8) {
+      // ---------------------------------------------------------------- MMAs
+      constexpr uint32_t kIdescO = tc::instr_desc_bf16(128, DP, 0, 1);
+      const int ksteps = (p.head_dim + 15) / 16;
+      const uint32_t q_addr = tc::smem_u32(smem), ring_addr = tc::smem_u32(ring);
+      uint32_t item = 0, q_turns = 0, p_turns = 0;  // bit t of q_turns, p_turns: the next phase of row tile t
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = ok && warp_wait(bar, parity & 1, abort_flag);
+        tc::fence_after_sync();
+      };
+      auto scores = [&](int t, uint32_t k_item, bool last) {
+        if (elect_one()) {
+          product_kk<DP>(tmem + t * 128, q_addr + t * R::kTile, ring_addr + (k_item % kNS) * R::kTile, ksteps);
+          tc::umma_commit(&s_full[t]);  // which also says that O += P V of the step before is complete
+          if (last) tc::umma_commit(&q_empty[t]);
+        }
+        __syncwarp();
+      };
+      auto release = [&](uint32_t i) {
+        if (elect_one()) tc::umma_commit(&empty[i % kNS]);
+        __syncwarp();
+      };
+      for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Unit w = unit_of<SPLIT>(p, found, u);
+        const int n = max(w.nk[0], w.nk[1]);
+        // the unit's items are K_0 V_0 K_1 V_1 ...: K_j is item + 2 j, V_j the next
+        wait(&full[item % kNS], item / kNS);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (j >= w.nk[t] || !ok) continue;
-          const uint32_t b = desc_mnmajor(ring_addr + (v_item % kNS) * R::kTile);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            wait(&p_full[2 * t + half], p_turns >> t);
+        for (int t = 0; t < 2; ++t)
+          if (w.nk[t]) {
+            wait(&q_full[t], q_turns >> t);
+            q_turns ^= 1u << t;
             if (!ok) break;
-            if (elect_one()) {
-#pragma unroll
-              for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                umma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, b + step_mnmajor(kk), kIdescO, j > 0 || kk > 0);
-              if (half == 1 && j + 1 == w.nk[t]) tc::umma_commit(&o_done[t]);
-            }
-            __syncwarp();
+            scores(t, item, w.nk[t] == 1);
           }
-          p_turns ^= 1u << t;
-          if (ok && j + 1 < w.nk[t]) scores(t, k_next, j + 2 == w.nk[t]);
-        }
         if (!ok) break;
-        release(v_item);
-        if (j + 1 < n) release(k_next);
+        release(item);
+        for (int j = 0; ok && j < n; ++j) {
+          const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
+          wait(&full[v_item % kNS], v_item / kNS);
+          if (j + 1 < n) wait(&full[k_next % kNS], k_next / kNS);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (j >= w.nk[t] || !ok) continue;
+            const uint32_t b = desc_mnmajor(ring_addr + (v_item % kNS) * R::kTile);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              wait(&p_full[2 * t + half], p_turns >> t);
+              if (!ok) break;
+              if (elect_one()) {
+#pragma unroll
+                for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                  umma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, b + step_mnmajor(kk), kIdescO, j > 0 || kk > 0);
+                if (half == 1 && j + 1 == w.nk[t]) tc::umma_commit(&o_done[t]);
+              }
+              __syncwarp();
+            }
+            p_turns ^= 1u << t;
+            if (ok && j + 1 < w.nk[t]) scores(t, k_next, j + 2 == w.nk[t]);
+          }
+          if (!ok) break;
+          release(v_item);
+          if (j + 1 < n) release(k_next);
+        }
+        item += 2 * n;
       }
-      item += 2 * n;
+      // every MMA has to have finished before the tensor memory is given back
+      if (elect_one()) tc::umma_commit(drain);
+      uint32_t never = 0u;
+      tc::mbar_wait(drain, 0, &never);
     }
-    // every MMA has to have finished before the tensor memory is given back
-    if (elect_one()) tc::umma_commit(drain);
-    uint32_t never = 0u;
-    tc::mbar_wait(drain, 0, &never);
-  }
   } else {
     // ------------------------------------------------------------- softmax
     regs_inc<192>();
