@@ -67,11 +67,11 @@ struct BwdArgs {
 // barrier a call is enough: a buffer is written again only after the next call's barrier.
 template <int NT, int N>
 struct RowSum {
-  float4* buf;  // [2][NT / 32]
+  float4* buf;  // [2][NT / 32], where a row has more than a warp
   uint32_t turn = 0;
   __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = NT < 32 ? NT / 2 : 16; o > 0; o >>= 1)
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
     if (NT > 32) {
@@ -96,17 +96,18 @@ struct RowSum {
 
 __device__ __forceinline__ float sum_pairs(const float2& s) { return s.x + s.y; }
 
-// Threads and rows of a block: up to 512 columns a warp has a row to itself, four to a block.
-constexpr __host__ __device__ int block_threads(int nt) { return nt == 32 ? 128 : nt; }
-constexpr __host__ __device__ int block_rows(int nt) { return nt == 32 ? 4 : 1; }
+// Threads and rows of a block: up to 512 columns a row has a warp or less of its own.  (The rows of a warp take
+// the same turns, the ones past the end idly, for the shuffles' sake.)
+constexpr __host__ __device__ int block_threads(int nt) { return nt <= 32 ? 128 : nt; }
+constexpr __host__ __device__ int block_rows(int nt) { return nt <= 32 ? 128 / nt : 1; }
 
-// Threads a multiprocessor, which set the registers a thread may have.  Few threads with their rows
-// on the way beat many that spill (60,000 rows of 4096): forward 302 us with 512, 348 with 768, 335
-// with 1024; leaving checkpoints, which takes twice the instructions, 546, 495, 595; backward, where a
+// Threads a multiprocessor, which set the registers a thread may have.  For long rows few threads with
+// their rows on the way beat many that spill (60,000 rows of 4096): forward 302 us with 512, 348 with 768,
+// 335 with 1024; leaving checkpoints, which takes twice the instructions, 546, 495, 595; backward, where a
 // thread also keeps the sums of its columns, 530 with 512, 867 with 768 (one chunk a thread: 534 with
-// 768, 590 with 1024).
-constexpr __host__ __device__ int fwd_threads(bool c8) { return c8 ? 768 : 512; }
-constexpr int kBwdThreads = 512;
+// 768, 590 with 1024).  Short rows wait for their sums, so many are kept on the way.
+constexpr __host__ __device__ int fwd_threads(bool c8, int nt) { return nt <= 32 ? 1024 : c8 ? 768 : 512; }
+constexpr __host__ __device__ int bwd_threads(int ch) { return ch == 1 ? 768 : 512; }
 constexpr __host__ __device__ int blocks_per_sm(int threads, int nt) {
   return threads / block_threads(nt) > 0 ? threads / block_threads(nt) : 1;
 }
@@ -167,13 +168,13 @@ struct Weights {
 };
 
 template <typename T, int NT, int CH, bool C8>
-__global__ void __launch_bounds__(block_threads(NT), blocks_per_sm(fwd_threads(C8), NT))
+__global__ void __launch_bounds__(block_threads(NT), blocks_per_sm(fwd_threads(C8, NT), NT))
 resnorm_fwd_kernel(FwdArgs a) {
   constexpr int RPB = block_rows(NT), P = Pieces<T>::kRaw, BT = block_threads(NT);
   extern __shared__ uint4 ring[];  // [stages][x, y][CH][P][BT], then the weights
-  __shared__ float4 red[2 * (NT / 32)];
+  __shared__ float4 red[NT > 32 ? 2 * (NT / 32) : 1];
   RowSum<NT, 4> row_sums{red};
-  const int t = threadIdx.x % NT, sub = threadIdx.x / NT;
+  const int t = threadIdx.x % NT, sub = threadIdx.x / NT, in_warp = NT < 32 ? (threadIdx.x & 31) / NT : 0;
   const int64_t n = a.n_rows ? min((int64_t)max(*a.n_rows, 0), a.cap) : a.cap;
   const int64_t step = (int64_t)gridDim.x * RPB;
   const T* x = (const T*)a.x;
@@ -192,8 +193,8 @@ resnorm_fwd_kernel(FwdArgs a) {
     rows::copies_commit();
   };
   auto checkpoint = [&](const rows::Raw<T>& raw, int64_t row, int col, int8_t* codes, float* scales) {
-    const rows::GroupScale gs = rows::group_scale(rows::group_top(raw));
-    if (col < a.d) {
+    const rows::GroupScale gs = rows::group_scale(rows::group_top<(NT < rows::kGroupLanes ? NT : rows::kGroupLanes)>(raw));
+    if (row < n && col < a.d) {
       float2 v[kPairs];
       rows::widen(raw, v);
       __stcs(reinterpret_cast<uint2*>(codes + row * a.d + col), rows::group_codes(v, gs.inv));
@@ -204,15 +205,16 @@ resnorm_fwd_kernel(FwdArgs a) {
   for (int k = 0; k < a.stages; ++k) fetch(row + k * step, k);
   Weights<NT, CH> weights{reinterpret_cast<float4*>(ring + a.stages * 2 * CH * P * BT)};
   weights.fill(a.d, a.w_post, a.gate_mode == NAT_GATE_CHANNEL ? a.gate : nullptr, a.w_pre);
-  for (int stage = 0; row < n; row += step, stage = stage + 1 == a.stages ? 0 : stage + 1) {
-    const float gate_row = a.gate_mode == NAT_GATE_ROW ? __ldg(a.gate + row) : 1.f;
+  for (int stage = 0; row - in_warp < n; row += step, stage = stage + 1 == a.stages ? 0 : stage + 1) {
+    const bool live = row < n;
+    const float gate_row = live && a.gate_mode == NAT_GATE_ROW ? __ldg(a.gate + row) : 1.f;
     rows::copies_wait(a.stages - 1);
     float2 r[CH][kPairs], z[CH][kPairs];  // x, then r; y w_post gate
     float2 yy = both(0.f), xx = both(0.f), xz = both(0.f), zz = both(0.f);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int col = (t + i * NT) * kChunk;
-      const bool in = col < a.d;
+      const bool in = live && col < a.d;
       rows::widen(in ? read_piece<T, NT>(slot(stage, 0, i)) : rows::zero_raw<T>(), r[i]);
       const rows::Raw<T> qy = (in && y) ? read_piece<T, NT>(slot(stage, 1, i)) : rows::zero_raw<T>();
       rows::widen(qy, z[i]);
@@ -234,7 +236,7 @@ resnorm_fwd_kernel(FwdArgs a) {
     float inv_y = 1.f;
     if (a.w_post) {
       inv_y = __frsqrt_rn(fmaf(sums[0], a.inv_d, a.eps));
-      if (t == 0) a.rstd_y[row] = inv_y;
+      if (live && t == 0) a.rstd_y[row] = inv_y;
     }
     const float f = inv_y * gate_row;
 #pragma unroll
@@ -246,7 +248,8 @@ resnorm_fwd_kernel(FwdArgs a) {
       // h is formed from r before its rounding: the norm then adds no error of its own
       const float own = a.alpha * a.alpha * sums[1] + f * f * sums[3];
       float square = fmaf(2.f * a.alpha * f, sums[2], own);
-      if (!(square > 0.0625f * own)) {  // the same in all threads of the row
+      const bool cancels = !(square > 0.0625f * own);  // the same in all threads of the row
+      if (__any_sync(0xFFFFFFFFu, cancels)) {
         float2 rr = both(0.f);
 #pragma unroll
         for (int i = 0; i < CH; ++i)
@@ -254,15 +257,15 @@ resnorm_fwd_kernel(FwdArgs a) {
           for (int j = 0; j < kPairs; ++j) rr = fma2(r[i][j], r[i][j], rr);
         float again[4] = {sum_pairs(rr), 0.f, 0.f, 0.f};
         row_sums(again);
-        square = again[0];
+        if (cancels) square = again[0];
       }
       inv_r = __frsqrt_rn(fmaf(square, a.inv_d, a.eps));
-      if (t == 0) a.rstd_r[row] = inv_r;
+      if (live && t == 0) a.rstd_r[row] = inv_r;
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int col = (t + i * NT) * kChunk;
-      const bool in = col < a.d;
+      const bool in = live && col < a.d;
       rows::Raw<T> out;
       rows::narrow(r[i], out);
       if (in) rows::store_raw((T*)a.r + row * a.d + col, out);
@@ -280,16 +283,16 @@ resnorm_fwd_kernel(FwdArgs a) {
 }
 
 template <typename T, int NT, int CH, bool C8>
-__global__ void __launch_bounds__(block_threads(NT), kBwdThreads / block_threads(NT))
+__global__ void __launch_bounds__(block_threads(NT), blocks_per_sm(bwd_threads(CH), NT))
 resnorm_bwd_kernel(BwdArgs a) {
   constexpr int RPB = block_rows(NT), P = Pieces<T>::kRaw, BT = block_threads(NT);
   // [stages][CH][dr, dh: P pieces each; y, r: P pieces each, or one of codes (8 bytes y, 8 bytes r)][BT],
   // then the weights
   constexpr int kPieces = C8 ? 2 * P + 1 : 4 * P;
   extern __shared__ uint4 ring[];
-  __shared__ float4 red[2 * (NT / 32)];
+  __shared__ float4 red[NT > 32 ? 2 * (NT / 32) : 1];
   RowSum<NT, 3> row_sums{red};
-  const int t = threadIdx.x % NT, sub = threadIdx.x / NT;
+  const int t = threadIdx.x % NT, sub = threadIdx.x / NT, in_warp = NT < 32 ? (threadIdx.x & 31) / NT : 0;
   const int64_t n = a.n_rows ? min((int64_t)max(*a.n_rows, 0), a.cap) : a.cap;
   const int64_t step = (int64_t)gridDim.x * RPB;
   const bool row_gate = a.gate_mode == NAT_GATE_ROW;
@@ -326,7 +329,12 @@ resnorm_bwd_kernel(BwdArgs a) {
 #pragma unroll
   for (int i = 0; i < CH; ++i) sy_next[i] = sr_next[i] = 0.f;
   auto fetch_scalars = [&](int64_t row) {
-    if (row >= n) return;
+    if (row >= n) {  // a row that only keeps its warp company adds nothing, whatever the one before it held
+      inv_y_next = inv_r_next = 0.f;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) sy_next[i] = sr_next[i] = 0.f;
+      return;
+    }
     if (a.w_post) inv_y_next = __ldg(a.rstd_y + row);
     if (a.w_pre) inv_r_next = __ldg(a.rstd_r + row);
     if (row_gate) gate_next = __ldg(a.gate + row);
@@ -345,14 +353,15 @@ resnorm_bwd_kernel(BwdArgs a) {
   fetch_scalars(row);
   Weights<NT, CH> weights{reinterpret_cast<float4*>(ring + a.stages * CH * kPieces * BT)};
   weights.fill(a.d, a.w_post, a.gate_mode == NAT_GATE_CHANNEL ? a.gate : nullptr, a.w_pre);
-  for (int stage = 0; row < n; row += step, stage = stage + 1 == a.stages ? 0 : stage + 1) {
+  for (int stage = 0; row - in_warp < n; row += step, stage = stage + 1 == a.stages ? 0 : stage + 1) {
+    const bool live = row < n;
     const float inv_y = inv_y_next, inv_r = inv_r_next, gate_row = gate_next;
     float2 e[CH][kPairs], yv[CH][kPairs], rv[CH][kPairs];
     float2 s_ur = both(0.f), s_ez = both(0.f), s_rz = both(0.f);
     rows::copies_wait(a.stages - 1);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const bool in = col_of(i) < a.d;
+      const bool in = live && col_of(i) < a.d;
       float2 u[kPairs], w[kPairs];
       if (C8) {
         const uint4 c = in ? *slot(stage, i, 2 * P) : make_uint4(0u, 0u, 0u, 0u);
@@ -388,11 +397,11 @@ resnorm_bwd_kernel(BwdArgs a) {
     float sums[3] = {sum_pairs(s_ur), sum_pairs(s_ez), sum_pairs(s_rz)};
     row_sums(sums);
     const float m1 = inv_r * sums[0] * a.inv_d, s_vy = fmaf(-m1, sums[2], sums[1]);
-    if (row_gate && t == 0) a.dgate_row[row] = s_vy;  // of dr yhat w_post, without the gate itself
+    if (row_gate && live && t == 0) a.dgate_row[row] = s_vy;  // of dr yhat w_post, without the gate itself
     const float2 m2 = both(a.w_post ? -gate_row * s_vy * a.inv_d : 0.f);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      if (col_of(i) >= a.d) continue;
+      if (!live || col_of(i) >= a.d) continue;
       float2 dx[kPairs], w[kPairs];
 #pragma unroll
       for (int j = 0; j < kPairs; ++j) {
@@ -419,7 +428,7 @@ resnorm_bwd_kernel(BwdArgs a) {
     }
   }
 
-  // the block's sums; four warps with rows of their own are added in warp order first
+  // the block's sums; those of the rows that it holds side by side are added in their order first
   float* p = a.partial + (int64_t)blockIdx.x * 2 * a.d;
   if (RPB == 1) {
 #pragma unroll
@@ -431,13 +440,13 @@ resnorm_bwd_kernel(BwdArgs a) {
           *reinterpret_cast<float2*>(p + a.d + col_of(i) + 2 * j) = acc_pre[i][j];
         }
   } else {
-    __shared__ float2 part[2][RPB][RPB > 1 ? CH * 32 * kPairs : 1];
+    __shared__ float2 part[2][RPB][RPB > 1 ? CH * NT * kPairs : 1];
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int j = 0; j < kPairs; ++j) {
-        part[0][sub][(t + i * 32) * kPairs + j] = acc[i][j];
-        part[1][sub][(t + i * 32) * kPairs + j] = acc_pre[i][j];
+        part[0][sub][(t + i * NT) * kPairs + j] = acc[i][j];
+        part[1][sub][(t + i * NT) * kPairs + j] = acc_pre[i][j];
       }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
@@ -479,13 +488,22 @@ resnorm_columns_kernel(const float* __restrict__ partial, int blocks, int d, int
 }
 
 // ---- launch shapes ----------------------------------------------------------------------
-// Threads of a row by its length, two chunks each.
-constexpr int kMaxD = 8192, kFwdChunks = 2, kBwdChunks = 2;
-
-int threads_of(int d, int chunks) {
+// Threads of a row and chunks of a thread, by the row's length: rows of up to 128 columns share a warp (two
+// of 128, four of 64), up to 512 they have one, beyond that a block.  What bounds a short row is its chain of
+// load, sums and store, so a warp that holds more of them is faster: against a warp a row of two chunks a
+// thread, 55,164 bf16 rows of 64 take 8.4 instead of 26.9 us forward and 22.7 instead of 49.9 us backward with
+// checkpoints, 100,000 of 128 47 instead of 102 us backward.
+constexpr int kMaxD = 8192;
+struct Cut {
+  int nt, ch;
+};
+Cut cut_of(int d) {
+  if (d <= 64) return {8, 1};
+  if (d <= 128) return {16, 1};
+  if (d <= 256) return {32, 1};
   int nt = 32;
-  while (nt * chunks * kChunk < d) nt *= 2;
-  return nt;
+  while (nt * 2 * kChunk < d) nt *= 2;
+  return {nt, 2};
 }
 
 // Persistent blocks, all resident, fewer of them where the rows on their way would not fit into a
@@ -511,8 +529,9 @@ Shape shape_of(int nt, int chunks, int threads_per_sm, size_t stage_bytes, int64
 }
 
 // Blocks of a backward pass at most: its workspace holds their column sums.
-int64_t max_blocks(int nt, int64_t cap) {
-  return max((int64_t)1, min((int64_t)148 * blocks_per_sm(kBwdThreads, nt), (cap + block_rows(nt) - 1) / block_rows(nt)));
+int64_t max_blocks(Cut c, int64_t cap) {
+  return max((int64_t)1, min((int64_t)148 * blocks_per_sm(bwd_threads(c.ch), c.nt),
+                             (cap + block_rows(c.nt) - 1) / block_rows(c.nt)));
 }
 
 template <typename K, typename A>
@@ -528,40 +547,50 @@ int launch(K kernel, A& a, int nt, int chunks, int threads_per_sm, size_t stage_
   return NAT_OK;
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int CH>
 int launch_fwd(FwdArgs& a, cudaStream_t stream) {
-  constexpr size_t stage = 2 * kFwdChunks * sizeof(rows::Raw<T>) * block_threads(NT);
+  constexpr size_t stage = 2 * CH * sizeof(rows::Raw<T>) * block_threads(NT);
   int64_t blocks;
-  return a.r8 ? launch(resnorm_fwd_kernel<T, NT, kFwdChunks, true>, a, NT, kFwdChunks, fwd_threads(true), stage, stream, &blocks, "resnorm_fwd_kernel")
-              : launch(resnorm_fwd_kernel<T, NT, kFwdChunks, false>, a, NT, kFwdChunks, fwd_threads(false), stage, stream, &blocks, "resnorm_fwd_kernel");
+  return a.r8 ? launch(resnorm_fwd_kernel<T, NT, CH, true>, a, NT, CH, fwd_threads(true, NT), stage, stream, &blocks,
+                       "resnorm_fwd_kernel")
+              : launch(resnorm_fwd_kernel<T, NT, CH, false>, a, NT, CH, fwd_threads(false, NT), stage, stream, &blocks,
+                       "resnorm_fwd_kernel");
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int CH>
 int launch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  constexpr size_t raw = sizeof(rows::Raw<T>), per = kBwdChunks * block_threads(NT);
-  return c8 ? launch(resnorm_bwd_kernel<T, NT, kBwdChunks, true>, a, NT, kBwdChunks, kBwdThreads, (2 * raw + 16) * per, stream, blocks, "resnorm_bwd_kernel")
-            : launch(resnorm_bwd_kernel<T, NT, kBwdChunks, false>, a, NT, kBwdChunks, kBwdThreads, 4 * raw * per, stream, blocks, "resnorm_bwd_kernel");
+  constexpr size_t raw = sizeof(rows::Raw<T>), per = CH * block_threads(NT);
+  return c8 ? launch(resnorm_bwd_kernel<T, NT, CH, true>, a, NT, CH, bwd_threads(CH), (2 * raw + 16) * per, stream,
+                     blocks, "resnorm_bwd_kernel")
+            : launch(resnorm_bwd_kernel<T, NT, CH, false>, a, NT, CH, bwd_threads(CH), 4 * raw * per, stream, blocks,
+                     "resnorm_bwd_kernel");
 }
 
 template <typename T>
 int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
-  switch (threads_of(a.d, kFwdChunks)) {
-    case 32: return launch_fwd<T, 32>(a, stream);
-    case 64: return launch_fwd<T, 64>(a, stream);
-    case 128: return launch_fwd<T, 128>(a, stream);
-    case 256: return launch_fwd<T, 256>(a, stream);
-    default: return launch_fwd<T, 512>(a, stream);
+  const Cut c = cut_of(a.d);
+  switch (c.nt) {
+    case 8: return launch_fwd<T, 8, 1>(a, stream);
+    case 16: return launch_fwd<T, 16, 1>(a, stream);
+    case 32: return c.ch == 1 ? launch_fwd<T, 32, 1>(a, stream) : launch_fwd<T, 32, 2>(a, stream);
+    case 64: return launch_fwd<T, 64, 2>(a, stream);
+    case 128: return launch_fwd<T, 128, 2>(a, stream);
+    case 256: return launch_fwd<T, 256, 2>(a, stream);
+    default: return launch_fwd<T, 512, 2>(a, stream);
   }
 }
 
 template <typename T>
 int dispatch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  switch (threads_of(a.d, kBwdChunks)) {
-    case 32: return launch_bwd<T, 32>(a, c8, stream, blocks);
-    case 64: return launch_bwd<T, 64>(a, c8, stream, blocks);
-    case 128: return launch_bwd<T, 128>(a, c8, stream, blocks);
-    case 256: return launch_bwd<T, 256>(a, c8, stream, blocks);
-    default: return launch_bwd<T, 512>(a, c8, stream, blocks);
+  const Cut c = cut_of(a.d);
+  switch (c.nt) {
+    case 8: return launch_bwd<T, 8, 1>(a, c8, stream, blocks);
+    case 16: return launch_bwd<T, 16, 1>(a, c8, stream, blocks);
+    case 32: return c.ch == 1 ? launch_bwd<T, 32, 1>(a, c8, stream, blocks) : launch_bwd<T, 32, 2>(a, c8, stream, blocks);
+    case 64: return launch_bwd<T, 64, 2>(a, c8, stream, blocks);
+    case 128: return launch_bwd<T, 128, 2>(a, c8, stream, blocks);
+    case 256: return launch_bwd<T, 256, 2>(a, c8, stream, blocks);
+    default: return launch_bwd<T, 512, 2>(a, c8, stream, blocks);
   }
 }
 
@@ -594,7 +623,7 @@ extern "C" {
 
 size_t nat_resnorm_workspace_bytes(const nat_resnorm_params* p, int64_t cap) {
   if (nat::check_params("nat_resnorm_workspace_bytes", p, cap) != NAT_OK) return 0;
-  const int64_t blocks = nat::max_blocks(nat::threads_of(p->d, nat::kBwdChunks), cap);
+  const int64_t blocks = nat::max_blocks(nat::cut_of(p->d), cap);
   return nat::align_up((size_t)blocks * 2 * p->d * sizeof(float), 256);
 }
 

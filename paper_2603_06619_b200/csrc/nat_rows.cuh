@@ -114,8 +114,9 @@ __device__ __forceinline__ void load_weights(const float* p, float2 (&w)[kPairs]
 // holds an infinity or a NaN is stored with a NaN scale, so that it reads back as NaN and not
 // as plausible numbers.
 
-// Largest magnitude among the 16 lanes of a group, as the bits of a float: the order of
-// unsigned integers is that of non-negative floats, with NaN above infinity.
+// Largest magnitude among the lanes of a group (16, or the row's where it is shorter), as the bits of a
+// float: the order of unsigned integers is that of non-negative floats, with NaN above infinity.
+template <int LANES = kGroupLanes>
 __device__ __forceinline__ uint32_t group_top(const Raw<float>& r) {
   float2 x[kPairs];
   widen(r, x);
@@ -124,11 +125,12 @@ __device__ __forceinline__ uint32_t group_top(const Raw<float>& r) {
   for (int i = 0; i < kPairs; ++i)
     top = max(top, max(__float_as_uint(x[i].x) & 0x7FFFFFFFu, __float_as_uint(x[i].y) & 0x7FFFFFFFu));
 #pragma unroll
-  for (int o = kGroupLanes / 2; o > 0; o >>= 1)
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, kGroupLanes));
+  for (int o = LANES / 2; o > 0; o >>= 1)
+    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, LANES));
   return top;
 }
 // Two bfloat16 at a time; a NaN wins.
+template <int LANES = kGroupLanes>
 __device__ __forceinline__ uint32_t group_top(const Raw<__nv_bfloat16>& r) {
   const uint32_t w[4] = {r.v.x & 0x7FFF7FFFu, r.v.y & 0x7FFF7FFFu, r.v.z & 0x7FFF7FFFu, r.v.w & 0x7FFF7FFFu};
   auto top2 = [](uint32_t a, uint32_t b) {
@@ -138,8 +140,8 @@ __device__ __forceinline__ uint32_t group_top(const Raw<__nv_bfloat16>& r) {
   };
   uint32_t top = top2(top2(w[0], w[1]), top2(w[2], w[3]));
 #pragma unroll
-  for (int o = kGroupLanes / 2; o > 0; o >>= 1)
-    top = top2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, kGroupLanes));
+  for (int o = LANES / 2; o > 0; o >>= 1)
+    top = top2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o, LANES));
   return max(top << 16, top & 0xFFFF0000u);
 }
 

@@ -432,6 +432,35 @@ def test_resnorm_parts_left_out(parts, ckpt):
         Join(21, 320, torch.bfloat16, gate=gate, parts=parts, ckpt=ckpt, seed=4).check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("n,d", [(1, 64), (1003, 40), (2, 72), (517, 128), (6, 136), (77, 256), (9001, 64), (5, 16)])
+def test_resnorm_rows_that_share_a_warp(n, d, ckpt, dtype):
+    gate = ("none", "channel", "row")[n % 3]
+    Join(n, d, DT[dtype], gate=gate, ckpt=ckpt, seed=n + d).check()
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("d", [64, 128, 256, 512])
+def test_resnorm_a_row_leaves_its_neighbours_alone(d, ckpt):
+    """A row's results do not depend on what the rows beside it hold, infinities and NaN among it."""
+    outs = lambda j: [t for t in (j.r, j.h, j.dx, j.dy, j.rstd_y, j.rstd_r, j.dgate)]  # noqa: E731
+    for n, bad in ((7, 2), (6, 5), (301, 300), (301, 0)):
+        runs = []
+        for value in (None, float("nan"), float("inf")):
+            j = Join(n, d, torch.bfloat16, gate="row", ckpt=ckpt, seed=9)
+            j.n_rows.fill_(n)
+            if value is not None:
+                j.x[bad], j.dr[bad] = value, value
+                j.y[bad, 3] = value
+            j.fwd()
+            j.bwd()
+            runs.append(outs(j))
+        keep = [i for i in range(n) if i != bad]
+        for run in runs[1:]:
+            assert all(torch.equal(a[keep], b[keep]) for a, b in zip(runs[0], run))
+
+
 def test_resnorm_no_rows_and_zero_rows():
     j = Join(0, 256, torch.bfloat16, gate="channel", spare=4)
     j.fwd()
