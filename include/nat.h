@@ -378,7 +378,8 @@ int nat_policy_loss_fwd_bwd(const nat_loss_params* params /* host */, const void
  * through the masked part of a tile.
  * workspace: nat_attn_workspace_bytes(params, B, cap), shared by forward and backward; it holds
  * nothing that must survive between them, and calls that may run at the same time need one each.
- * (About 100 MB where few long sequences are cut into pieces, 20 bytes a row and head or less otherwise.)
+ * (About 100 MB where few long sequences are cut into pieces, 20 bytes a row and head or less otherwise:
+ * a smaller cap or B may need more than a larger one, so ask for each pair that is called.)
  * A call with B = 0 or cap = 0 does nothing, not even to the status word.
  * ------------------------------------------------------------------------- */
 typedef struct {
@@ -421,7 +422,10 @@ int nat_attn_bwd(const nat_attn_params* params /* host */, int32_t B, const int3
  *   dgate = sum_rows dr' n  [d]   or   sum_columns dr' n  [cap], by gate_mode.
  * The weights' gradients are float32 and overwritten.  y and r come as the forward's rows or both as its
  * checkpoints (then y = r = NULL); rstd_y and rstd_r are the forward's.
- * workspace (backward only): nat_resnorm_workspace_bytes(params, cap) bytes.
+ * Each element is read before it is written, by the thread that writes it, so r may lie on x, h on y or x
+ * (not both of r and h on one), and dx and dy on dr, dh, y or r; other overlaps are not allowed.
+ * workspace (backward only): nat_resnorm_workspace_bytes(params, cap) bytes; calls that may run at the
+ * same time need one each.
  * ------------------------------------------------------------------------- */
 #define NAT_GATE_NONE 0
 #define NAT_GATE_CHANNEL 1

@@ -44,6 +44,7 @@ class PackedSublayer:
             self.y8, self.r8 = ((torch.empty(rows, d, dtype=torch.int8, device=dev),
                                  torch.empty(rows, groups, dtype=f32, device=dev)) for _ in range(2))
         self.attn_ws = nat.alloc_workspace(nat.nat_attn_workspace_bytes(self.attn, self.B, self.cap), dev)
+        self.attn_ws[:4].zero_()  # the status word: a call without rows leaves it alone
         self.norm_ws = nat.alloc_workspace(nat.nat_resnorm_workspace_bytes(self.norm, self.cap), dev)
 
     def _split(self, qkv):
@@ -78,4 +79,5 @@ class PackedSublayer:
         return self.dqkv
 
     def status(self):
+        """The NAT_DEV_* bits of the last attention call (waits for the stream); 0 before the first."""
         return nat.nat_poll_status(self.attn_ws)

@@ -472,7 +472,7 @@ def alloc_workspace(nbytes, device):
 
 
 def nat_poll_status(workspace):
-    """The NAT_DEV_* bits the last loss call left in its workspace (waits for the stream)."""
+    """The NAT_DEV_* bits the last loss or attention call left in its workspace (waits for the stream)."""
     word = ctypes.c_uint32(0)
     _check(load().nat_poll_status(_ptr(workspace), _stream(), ctypes.byref(word)))
     return int(word.value)

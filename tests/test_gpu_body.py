@@ -461,6 +461,40 @@ def test_resnorm_a_row_leaves_its_neighbours_alone(d, ckpt):
             assert all(torch.equal(a[keep], b[keep]) for a, b in zip(runs[0], run))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("n,d", [(3001, 64), (700, 200), (2000, 512), (1500, 1024), (300, 8192)])
+def test_resnorm_in_place(n, d, ckpt, dtype):
+    """Outputs on the inputs that they may lie on: the same bits as apart from them."""
+    def run(lay):
+        j = Join(n, d, DT[dtype], gate="channel", ckpt=ckpt, seed=2)
+        if lay == "r on x, h on y":
+            j.r, j.h = j.x, j.y.clone() if not ckpt else j.y
+        elif lay == "h on x":
+            j.h = j.x
+        if lay == "r on x, h on y" and not ckpt:
+            kept, j.y = j.y, j.h  # the forward's y is overwritten by h, the backward reads the copy
+            j.fwd()
+            j.y = kept
+        else:
+            j.fwd()
+        if lay == "dx on dr, dy on dh":
+            j.dx, j.dy = j.dr, j.dh
+        elif lay == "dx on dh, dy on dr":
+            j.dx, j.dy = j.dh, j.dr
+        elif lay == "dx on r, dy on y" and not ckpt:
+            j.dx, j.dy = j.r.clone(), j.y
+            j.r = j.dx
+        out = [t[:n].clone() for t in (j.h,)]
+        r = j.r[:n].clone()
+        j.bwd()
+        return out + [r] + [t[:n].clone() for t in (j.dx, j.dy, j.rstd_y, j.rstd_r)] + [j.dw_post, j.dw_pre, j.dgate]
+
+    apart = run("")
+    for lay in ("r on x, h on y", "h on x", "dx on dr, dy on dh", "dx on dh, dy on dr", "dx on r, dy on y"):
+        assert all(torch.equal(a, b) for a, b in zip(apart, run(lay))), lay
+
+
 def test_resnorm_no_rows_and_zero_rows():
     j = Join(0, 256, torch.bfloat16, gate="channel", spare=4)
     j.fwd()
