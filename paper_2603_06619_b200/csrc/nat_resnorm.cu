@@ -96,18 +96,19 @@ struct RowSum {
 
 __device__ __forceinline__ float sum_pairs(const float2& s) { return s.x + s.y; }
 
-// Threads and rows of a block: up to 512 columns a row has a warp or less of its own.  (The rows of a warp take
+// Threads and rows of a block: short rows have a warp or less of their own.  (The rows of a warp take
 // the same turns, the ones past the end idly, for the shuffles' sake.)
 constexpr __host__ __device__ int block_threads(int nt) { return nt <= 32 ? 128 : nt; }
 constexpr __host__ __device__ int block_rows(int nt) { return nt <= 32 ? 128 / nt : 1; }
 
-// Threads a multiprocessor, which set the registers a thread may have.  For long rows few threads with
-// their rows on the way beat many that spill (60,000 rows of 4096): forward 302 us with 512, 348 with 768,
-// 335 with 1024; leaving checkpoints, which takes twice the instructions, 546, 495, 595; backward, where a
-// thread also keeps the sums of its columns, 530 with 512, 867 with 768 (one chunk a thread: 534 with
-// 768, 590 with 1024).  Short rows wait for their sums, so many are kept on the way.
-constexpr __host__ __device__ int fwd_threads(bool c8, int nt) { return nt <= 32 ? 1024 : c8 ? 768 : 512; }
-constexpr __host__ __device__ int bwd_threads(int ch) { return ch == 1 ? 768 : 512; }
+// Threads a multiprocessor, which set the registers a thread may have.  Few threads with their rows on the way
+// beat many that spill (60,000 rows of 4096): forward 302 us with 512, 348 with 768, 335 with 1024; leaving
+// checkpoints, which takes twice the instructions, 546, 495, 595; backward, where a thread also keeps the sums
+// of its columns, 530 with 512, 867 with 768.  With one chunk a thread the backward has its best between
+// (120e6 bfloat16 elements in rows of 128, plain and from checkpoints: 255 and 251 us with 512, 239 and 238
+// with 640, 270 and 280 with 768, 544 and 434 with 1024).
+constexpr __host__ __device__ int fwd_threads(bool c8, int nt) { return nt <= 32 || c8 ? 768 : 512; }
+constexpr __host__ __device__ int bwd_threads(int ch) { return ch == 1 ? 640 : 512; }
 constexpr __host__ __device__ int blocks_per_sm(int threads, int nt) {
   return threads / block_threads(nt) > 0 ? threads / block_threads(nt) : 1;
 }
@@ -306,8 +307,7 @@ resnorm_bwd_kernel(BwdArgs a) {
   auto slot = [&](int stage, int i, int piece) { return ring + ((stage * CH + i) * kPieces + piece) * BT + threadIdx.x; };
   // A chunk's address as the row's, the same in the block, and the thread's column in it, or as one sum: the
   // first leaves the compiler registers in long rows (120e6 bfloat16 elements in rows of 2048, 4096, 8192: 240,
-  // 236, 241 us against 262, 272, 305), the second is faster in short ones (of 512 and 1024: 301, 239 against
-  // 310, 254; from checkpoints of 512 columns 234 against 291).
+  // 236, 241 us against 262, 272, 305), the second is faster in short ones (of 1024: 239 against 254).
   constexpr bool kRowBase = NT >= 128;
   auto fetch = [&](int64_t row, int stage) {
     if (row < n) {
@@ -499,18 +499,20 @@ resnorm_columns_kernel(const float* __restrict__ partial, int blocks, int d, int
 
 // ---- launch shapes ----------------------------------------------------------------------
 // Threads of a row and chunks of a thread, by the row's length: rows of up to 128 columns share a warp (two
-// of 128, four of 64), up to 512 they have one, beyond that a block.  What bounds a short row is its chain of
-// load, sums and store, so a warp that holds more of them is faster: against a warp a row of two chunks a
-// thread, 55,164 bf16 rows of 64 take 8.4 instead of 26.9 us forward and 22.7 instead of 49.9 us backward with
-// checkpoints, 100,000 of 128 47 instead of 102 us backward.
+// of 128, four of 64), up to 256 (forward 512) they have one, beyond that a block.  What bounds a short row is
+// its chain of load, sums and store, so a warp that holds more of them is faster: against a warp a row of two
+// chunks a thread, 55,164 bf16 rows of 64 take 8.3 instead of 26.9 us forward.  Rows of 257 to 512 backward: one
+// chunk in each of 64 threads against two in 32 (120e6 elements in rows of 512): bfloat16 258 against 298 us, from
+// checkpoints 249 against 234; float32 (60e6) 400 against 376 and 277 against 326.
 constexpr int kMaxD = 8192;
 struct Cut {
   int nt, ch;
 };
-Cut cut_of(int d) {
+Cut cut_of(int d, bool bwd) {
   if (d <= 64) return {8, 1};
   if (d <= 128) return {16, 1};
   if (d <= 256) return {32, 1};
+  if (bwd && d <= 512) return {64, 1};
   int nt = 32;
   while (nt * 2 * kChunk < d) nt *= 2;
   return {nt, 2};
@@ -578,7 +580,7 @@ int launch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
 
 template <typename T>
 int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
-  const Cut c = cut_of(a.d);
+  const Cut c = cut_of(a.d, false);
   switch (c.nt) {
     case 8: return launch_fwd<T, 8, 1>(a, stream);
     case 16: return launch_fwd<T, 16, 1>(a, stream);
@@ -592,12 +594,12 @@ int dispatch_fwd(FwdArgs& a, cudaStream_t stream) {
 
 template <typename T>
 int dispatch_bwd(BwdArgs& a, bool c8, cudaStream_t stream, int64_t* blocks) {
-  const Cut c = cut_of(a.d);
+  const Cut c = cut_of(a.d, true);
   switch (c.nt) {
     case 8: return launch_bwd<T, 8, 1>(a, c8, stream, blocks);
     case 16: return launch_bwd<T, 16, 1>(a, c8, stream, blocks);
-    case 32: return c.ch == 1 ? launch_bwd<T, 32, 1>(a, c8, stream, blocks) : launch_bwd<T, 32, 2>(a, c8, stream, blocks);
-    case 64: return launch_bwd<T, 64, 2>(a, c8, stream, blocks);
+    case 32: return launch_bwd<T, 32, 1>(a, c8, stream, blocks);
+    case 64: return c.ch == 1 ? launch_bwd<T, 64, 1>(a, c8, stream, blocks) : launch_bwd<T, 64, 2>(a, c8, stream, blocks);
     case 128: return launch_bwd<T, 128, 2>(a, c8, stream, blocks);
     case 256: return launch_bwd<T, 256, 2>(a, c8, stream, blocks);
     default: return launch_bwd<T, 512, 2>(a, c8, stream, blocks);
@@ -633,7 +635,7 @@ extern "C" {
 
 size_t nat_resnorm_workspace_bytes(const nat_resnorm_params* p, int64_t cap) {
   if (nat::check_params("nat_resnorm_workspace_bytes", p, cap) != NAT_OK) return 0;
-  const int64_t blocks = nat::max_blocks(nat::cut_of(p->d), cap);
+  const int64_t blocks = nat::max_blocks(nat::cut_of(p->d, true), cap);
   return nat::align_up((size_t)blocks * 2 * p->d * sizeof(float), 256);
 }
 
