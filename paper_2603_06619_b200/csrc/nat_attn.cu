@@ -122,7 +122,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanArgs a) {
 
 // What the bfloat16 backward pass reads, in one launch: its plans (blocks 0 and 1, where it needs them)
 // and, for every row of out, delta = dout . out and lse in units of log 2.  Bound by the read of
-// out and dout.  Half a warp takes a row's 16-byte pieces.
+// out and dout.  (out is bfloat16: the sum of P dP would be free of its rounding, which dq and dk of the first few
+// tokens of a sequence show, but takes the products S and dP of every tile once more.)  Half a warp takes a row's 16-byte pieces.
 struct StatsArgs {
   const __nv_bfloat16 *out, *dout;
   const float* lse;
