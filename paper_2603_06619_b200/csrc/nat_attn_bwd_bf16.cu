@@ -341,7 +341,8 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
       const int head = (int)(u % p.n_kv_heads) * p.group + head_in;
       const bool valid = row < p.group * p.tq && token < e.seq_hi;
       const int64_t at = (int64_t)token * p.n_heads + head;
-      const float2 minus_lse2 = both(valid ? -p.lse2[at] : 0.f), minus_delta = both(valid ? -p.delta[at] : 0.f);
+      const float2 minus_lse2 = both(valid ? -__ldcg(p.lse2 + at) : 0.f);
+      const float2 minus_delta = both(valid ? -__ldcg(p.delta + at) : 0.f);
       for (int j = 0; j < n; ++j, ++tile) {
         ok = warp_wait(&s_full[tile & 1], (tile >> 1) & 1, abort_flag);
         if (!ok) break;
@@ -513,8 +514,8 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
         for (int i = 0; i < 4; ++i) {
           const int r = lane + 32 * i, token = first + r / p.group;
           const int64_t at = (int64_t)token * p.n_heads + head + r % p.group;
-          a[i] = r < valid ? -__ldg(p.lse2 + at) : 0.f;
-          b[i] = r < valid ? -__ldg(p.delta + at) : 0.f;
+          a[i] = r < valid ? -__ldcg(p.lse2 + at) : 0.f;
+          b[i] = r < valid ? -__ldcg(p.delta + at) : 0.f;
         }
         ok = warp_wait(&st_empty[tile & 1], ((tile >> 1) & 1) ^ 1, abort_flag);
         if (!ok) break;

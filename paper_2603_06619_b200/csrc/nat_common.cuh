@@ -37,7 +37,9 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 int require_sm100();
 
 // Kernel launches that may begin before the kernel in front of them on the stream has ended: such a
-// kernel calls wait_for_primary() before it touches anything that one wrote.
+// kernel calls wait_for_primary() before it touches anything that one wrote.  What that one writes is written
+// while this one runs already, so it is never read through the read-only path (__ldg, or a const __restrict__
+// pointer), which takes memory to be unchanged for as long as the kernel runs.
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void release_secondary() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... P, typename... A>

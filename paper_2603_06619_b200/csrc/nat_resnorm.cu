@@ -472,17 +472,15 @@ resnorm_bwd_kernel(BwdArgs a) {
 // Adds the blocks' sums in block order (eight strided runs, joined in order) and applies the
 // factors that were kept out of them.
 __global__ void __launch_bounds__(256)
-resnorm_columns_kernel(const float* __restrict__ partial, int blocks, int d, int gate_channel,
-                       const float* __restrict__ w_post, const float* __restrict__ gate,
-                       float* __restrict__ dw_post, float* __restrict__ dgate,
-                       float* __restrict__ dw_pre) {
+resnorm_columns_kernel(const float* partial, int blocks, int d, int gate_channel, const float* w_post,
+                       const float* gate, float* dw_post, float* dgate, float* dw_pre) {
   wait_for_primary();
   __shared__ float part[8][33];
   const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;  // over 2 d columns
   float s = 0.f;
   if (c < 2 * d)
-    for (int b = run; b < blocks; b += 8) s += partial[(int64_t)b * 2 * d + c];
+    for (int b = run; b < blocks; b += 8) s += __ldcg(partial + (int64_t)b * 2 * d + c);
   part[run][lane] = s;
   __syncthreads();
   if (run != 0 || c >= 2 * d) return;
