@@ -229,8 +229,10 @@ Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
     pieces[w] = l.split[w] ? tiles + (kSplitBlocks + p.n_kv_heads - 1) / p.n_kv_heads : 0;
     l.entries[w] = l.split[w] ? pieces[w] : tiles;
     l.plan_off[w] = at;
-    at = align_up(at + (size_t)l.entries[w] * sizeof(Entry), 256);
+    if (p.dtype == NAT_BF16) at = align_up(at + (size_t)l.entries[w] * sizeof(Entry), 256);
   }
+  l.listed = p.dtype == NAT_F32 && (int64_t)B * p.n_heads > kSearchMost;
+  if (l.listed) at = align_up(at + (size_t)l.entries[kPlanFwd] * sizeof(Entry), 256);
   l.delta_off = at;
   l.lse2_off = at = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);
   if (p.dtype == NAT_BF16) at = align_up(at + (size_t)cap * p.n_heads * sizeof(float), 256);

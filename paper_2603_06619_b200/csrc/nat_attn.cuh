@@ -111,7 +111,15 @@ struct Layout {
   size_t plan_off[3], delta_off, lse2_off, partial_off[3], total;
   int64_t entries[3];  // of the list
   bool split[3];       // tiles may be cut into pieces
+  bool listed;         // float32: the tiles come from a list
 };
+
+// Sequences times heads up to which every block of a float32 call searches cu_seqlens for its tile.  The search
+// takes 32 sequences a turn in every block, so its cost grows with their square; beyond this a list is made
+// first, in a launch of its own.  Forward, searching / listed: 2 heads of 64 columns, 4 tokens a sequence: 512
+// sequences 59 / 79 us, 1024 141 / 145, 65,536 310,000 / 8,600; 8 heads of 128 columns, 64 tokens: 128 sequences
+// 94 / 93, 256 217 / 182, 512 550 / 356; 16 heads of 128 columns, 4 tokens: 64 sequences 73 / 79, 256 327 / 288.
+constexpr int64_t kSearchMost = 2048;
 
 // Floats of one piece's partial result for one key head.
 inline size_t partial_floats(const nat_attn_params& p, Plan which) {

@@ -122,8 +122,14 @@ __device__ __forceinline__ float sum16(float x) {
   return x;
 }
 
-// Every block finds its tile; the first one reports what is wrong with the batch.
-__device__ __forceinline__ bool my_tile(const Batch& batch, Head* head, Entry* e) {
+// Every block takes its tile from the list or, without one, finds it; then the first one reports what is wrong
+// with the batch.
+__device__ __forceinline__ bool my_tile(const Batch& batch, const Entry* list, Head* head, Entry* e) {
+  if (list) {
+    const bool there = blockIdx.x < head->count[kPlanFwd];
+    if (there) *e = list[blockIdx.x];
+    return there;
+  }
   uint32_t total, status;
   *e = find_entry(batch, blockIdx.x, &total, &status);
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->status = status;
@@ -131,10 +137,10 @@ __device__ __forceinline__ bool my_tile(const Batch& batch, Head* head, Entry* e
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads) f32_fwd_kernel(Ptrs a, Batch batch, Head* head) {
+__global__ void __launch_bounds__(kThreads) f32_fwd_kernel(Ptrs a, Batch batch, const Entry* list, Head* head) {
   extern __shared__ __align__(16) float smem[];
   Entry e;
-  if (!my_tile(batch, head, &e)) return;
+  if (!my_tile(batch, list, head, &e)) return;
   Tile<DP> Q{smem}, K{smem + Tile<DP>::kFloats}, V{smem + 2 * Tile<DP>::kFloats};
   float* P = smem + 3 * Tile<DP>::kFloats;
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
@@ -197,10 +203,10 @@ __global__ void __launch_bounds__(kThreads) f32_fwd_kernel(Ptrs a, Batch batch, 
 
 // dq of 64 queries of a head; also leaves delta = do . o for the keys' kernel.
 template <int DP>
-__global__ void __launch_bounds__(kThreads) f32_dq_kernel(Ptrs a, Batch batch, Head* head) {
+__global__ void __launch_bounds__(kThreads) f32_dq_kernel(Ptrs a, Batch batch, const Entry* list, Head* head) {
   extern __shared__ __align__(16) float smem[];
   Entry e;
-  if (!my_tile(batch, head, &e)) return;
+  if (!my_tile(batch, list, head, &e)) return;
   Tile<DP> Q{smem}, G{smem + Tile<DP>::kFloats}, K{smem + 2 * Tile<DP>::kFloats}, V{smem + 3 * Tile<DP>::kFloats};
   float* P = smem + 4 * Tile<DP>::kFloats;
   const int D = a.p.head_dim, h = blockIdx.y, kh = h / (a.p.n_heads / a.p.n_kv_heads);
@@ -258,10 +264,10 @@ __global__ void __launch_bounds__(kThreads) f32_dq_kernel(Ptrs a, Batch batch, H
 
 // dk and dv of 64 keys of a key head: all query heads of its group, all later queries, in order.
 template <int DP>
-__global__ void __launch_bounds__(kThreads) f32_dkv_kernel(Ptrs a, Batch batch, Head* head) {
+__global__ void __launch_bounds__(kThreads) f32_dkv_kernel(Ptrs a, Batch batch, const Entry* list, Head* head) {
   extern __shared__ __align__(16) float smem[];
   Entry e;
-  if (!my_tile(batch, head, &e)) return;
+  if (!my_tile(batch, list, head, &e)) return;
   Tile<DP> Q{smem}, G{smem + Tile<DP>::kFloats}, K{smem + 2 * Tile<DP>::kFloats}, V{smem + 3 * Tile<DP>::kFloats};
   float *P = smem + 4 * Tile<DP>::kFloats, *S = P + kT * kLd;
   const int D = a.p.head_dim, kh = blockIdx.y, group = a.p.n_heads / a.p.n_kv_heads;
@@ -332,23 +338,25 @@ Ptrs ptrs(const Args& a, const Layout& l) {
 
 template <typename K>
 int launch(K kernel, size_t smem, std::atomic<uint64_t>* allowed, const Device& dev, const Args& a, const Layout& l,
-           Plan which, int heads, const char* name) {
+           int heads, const char* name) {
   int s = allow_smem(kernel, smem, dev, allowed);
   if (s != NAT_OK) return s;
-  kernel<<<dim3((unsigned)l.entries[which], (unsigned)heads), kThreads, smem, a.stream>>>(
-      ptrs(a, l), batch(a, l, which), head(a));
+  kernel<<<dim3((unsigned)l.entries[kPlanFwd], (unsigned)heads), kThreads, smem, a.stream>>>(
+      ptrs(a, l), batch(a, l, kPlanFwd), l.listed ? entries(a, l, kPlanFwd) : nullptr, head(a));
   NAT_LAUNCH_CHECK(name);
   return NAT_OK;
 }
 
+// All three kernels have the same tiles, so the forward's list serves them all.
 template <int DP>
 int fwd(const Args& a, const Layout& l) {
   static std::atomic<uint64_t> allowed;
   Device dev;
-  const int s = device(&dev);
+  int s = device(&dev);
+  if (s == NAT_OK && l.listed) s = launch_plan(a, l, kPlanFwd);
   if (s != NAT_OK) return s;
   const size_t smem = (3 * Tile<DP>::kFloats + kT * kLd) * sizeof(float);
-  return launch(f32_fwd_kernel<DP>, smem, &allowed, dev, a, l, kPlanFwd, a.p.n_heads, "f32_fwd_kernel");
+  return launch(f32_fwd_kernel<DP>, smem, &allowed, dev, a, l, a.p.n_heads, "f32_fwd_kernel");
 }
 
 template <int DP>
@@ -356,11 +364,12 @@ int bwd(const Args& a, const Layout& l) {
   static std::atomic<uint64_t> allowed[2];
   Device dev;
   int s = device(&dev);
+  if (s == NAT_OK && l.listed) s = launch_plan(a, l, kPlanFwd);
   if (s != NAT_OK) return s;
   const size_t smem = (4 * Tile<DP>::kFloats + kT * kLd) * sizeof(float);
-  s = launch(f32_dq_kernel<DP>, smem, &allowed[0], dev, a, l, kPlanDq, a.p.n_heads, "f32_dq_kernel");
+  s = launch(f32_dq_kernel<DP>, smem, &allowed[0], dev, a, l, a.p.n_heads, "f32_dq_kernel");
   if (s != NAT_OK) return s;
-  return launch(f32_dkv_kernel<DP>, smem + kT * kLd * sizeof(float), &allowed[1], dev, a, l, kPlanDkv, a.p.n_kv_heads,
+  return launch(f32_dkv_kernel<DP>, smem + kT * kLd * sizeof(float), &allowed[1], dev, a, l, a.p.n_kv_heads,
                 "f32_dkv_kernel");
 }
 
