@@ -381,8 +381,12 @@ int nat_policy_loss_fwd_bwd(const nat_loss_params* params /* host */, const void
  * through the masked part of a tile.
  * workspace: nat_attn_workspace_bytes(params, B, cap), shared by forward and backward; it holds
  * nothing that must survive between them, and calls that may run at the same time need one each.
- * (About 100 MB where few long sequences are cut into pieces, 20 bytes a row and head or less otherwise:
- * a smaller cap or B may need more than a larger one, so ask for each pair that is called.)
+ * Its parts: NAT_BF16 8 bytes a row and head, and 32 bytes an entry of three lists of tiles (cap / t + B entries, t =
+ * 256 / g, 128 / g and 128 tokens with g = n_heads / n_kv_heads); NAT_F32 4 bytes a row and head, and one list of
+ * cap / 64 + B entries where B n_heads > 2048; each part rounded up to 256 bytes.  Where the tiles are few and long
+ * NAT_BF16 cuts them into pieces, whose partial results take up to 115 MB more.  Only these make a smaller
+ * batch ask for more than a larger one; a call whose workspace does not hold them does without (slower, and its sums in
+ * another order, as fixed), so a workspace for some B and cap serves every smaller B and cap.
  * A call with B = 0 or cap = 0 does nothing, not even to the status word.
  * ------------------------------------------------------------------------- */
 typedef struct {

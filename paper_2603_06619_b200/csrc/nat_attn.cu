@@ -193,7 +193,8 @@ int check(const char* who, const nat_attn_params* p, int32_t B, int64_t cap) {
   return NAT_OK;
 }
 
-int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool bwd) {
+// Chooses the workspace's layout: tiles are cut into pieces where it has room for them.
+int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool bwd, Layout* l) {
   if (!a.cu_seqlens || !a.q || !a.k || !a.v || !a.out || !a.lse)
     return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
   if (bwd && (!a.dout || !a.dq || !a.dk || !a.dv))
@@ -201,9 +202,10 @@ int check_buffers(const char* who, const Args& a, size_t workspace_bytes, bool b
   const uintptr_t all = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.out |
                         (uintptr_t)a.dout | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv;
   if (all & 15u) return fail(NAT_ERR_INVALID_ARG, "%s: rows must be 16-byte aligned", who);
-  const size_t need = layout(a.p, a.B, a.cap).total;
-  if (!a.workspace || workspace_bytes < need)
-    return fail(NAT_ERR_CAPACITY, "%s: workspace too small (%zu < %zu)", who, workspace_bytes, need);
+  *l = layout(a.p, a.B, a.cap, true);
+  if (workspace_bytes < l->total) *l = layout(a.p, a.B, a.cap, false);
+  if (!a.workspace || workspace_bytes < l->total)
+    return fail(NAT_ERR_CAPACITY, "%s: workspace too small (%zu < %zu)", who, workspace_bytes, l->total);
   if ((uintptr_t)a.workspace & 255u)
     return fail(NAT_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
   return NAT_OK;
@@ -217,7 +219,7 @@ int plan_tile(const nat_attn_params& p, Plan which) {
   return which == kPlanFwd ? 2 * tq : which == kPlanDq ? tq : 128;
 }
 
-Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
+Layout layout(const nat_attn_params& p, int32_t B, int64_t cap, bool cut) {
   Layout l;
   size_t at = 256;
   int64_t pieces[3];
@@ -225,7 +227,7 @@ Layout layout(const nat_attn_params& p, int32_t B, int64_t cap) {
     // a sequence's last tile may be part full: at most one extra tile for each sequence
     const int64_t tiles = cap / plan_tile(p, (Plan)w) + B;
     // Few tiles (under two for each multiprocessor), each with many steps: cut into pieces.
-    l.split[w] = p.dtype == NAT_BF16 && cap > 1024 && tiles * p.n_kv_heads <= 2 * 148;
+    l.split[w] = cut && p.dtype == NAT_BF16 && cap > 1024 && tiles * p.n_kv_heads <= 2 * 148;
     pieces[w] = l.split[w] ? tiles + (kSplitBlocks + p.n_kv_heads - 1) / p.n_kv_heads : 0;
     l.entries[w] = l.split[w] ? pieces[w] : tiles;
     l.plan_off[w] = at;
@@ -302,7 +304,7 @@ extern "C" {
 
 size_t nat_attn_workspace_bytes(const nat_attn_params* p, int32_t B, int64_t cap) {
   if (nat::attn::check("nat_attn_workspace_bytes", p, B, cap) != NAT_OK) return 0;
-  return nat::attn::layout(*p, B, cap).total;
+  return nat::attn::layout(*p, B, cap, true).total;
 }
 
 int nat_attn_fwd(const nat_attn_params* p, int32_t B, const int32_t* cu_seqlens, int64_t cap,
@@ -313,9 +315,9 @@ int nat_attn_fwd(const nat_attn_params* p, int32_t B, const int32_t* cu_seqlens,
   nat::attn::Args a{};
   a.p = *p; a.B = B; a.cu_seqlens = cu_seqlens; a.cap = cap; a.q = q; a.k = k; a.v = v;
   a.out = out; a.lse = lse; a.workspace = workspace; a.stream = (cudaStream_t)stream;
-  s = nat::attn::check_buffers("nat_attn_fwd", a, workspace_bytes, false);
+  nat::attn::Layout l;
+  s = nat::attn::check_buffers("nat_attn_fwd", a, workspace_bytes, false, &l);
   if (s != NAT_OK) return s;
-  const nat::attn::Layout l = nat::attn::layout(*p, B, cap);
   return p->dtype == NAT_F32 ? nat::attn::f32_fwd(a, l) : nat::attn::bf16_fwd(a, l);
 }
 
@@ -329,9 +331,9 @@ int nat_attn_bwd(const nat_attn_params* p, int32_t B, const int32_t* cu_seqlens,
   a.p = *p; a.B = B; a.cu_seqlens = cu_seqlens; a.cap = cap; a.q = q; a.k = k; a.v = v;
   a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse); a.dout = dout; a.dq = dq;
   a.dk = dk; a.dv = dv; a.workspace = workspace; a.stream = (cudaStream_t)stream;
-  s = nat::attn::check_buffers("nat_attn_bwd", a, workspace_bytes, true);
+  nat::attn::Layout l;
+  s = nat::attn::check_buffers("nat_attn_bwd", a, workspace_bytes, true, &l);
   if (s != NAT_OK) return s;
-  const nat::attn::Layout l = nat::attn::layout(*p, B, cap);
   return p->dtype == NAT_F32 ? nat::attn::f32_bwd(a, l) : nat::attn::bf16_bwd(a, l);
 }
 

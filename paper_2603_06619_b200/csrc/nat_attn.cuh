@@ -126,7 +126,9 @@ inline size_t partial_floats(const nat_attn_params& p, Plan which) {
   const size_t dp = p.head_dim <= 64 ? 64 : 128;
   return which == kPlanFwd ? 256 * (dp + 2) : which == kPlanDq ? 128 * dp : 128 * 2 * dp;
 }
-Layout layout(const nat_attn_params& p, int32_t B, int64_t cap);
+// The workspace of a call.  `cut`: with room for the pieces, where the tiles of this B and cap are worth cutting;
+// without it the size grows with B and cap, so a workspace for some batch holds every smaller one uncut.
+Layout layout(const nat_attn_params& p, int32_t B, int64_t cap, bool cut);
 
 // Pieces that the splitting of tiles aims at: one and a half for each of the 148 multiprocessors, so that the
 // shorter ones fill the gaps behind the longer (7013 tokens, 4 heads over 2: forward 89 us with 148
