@@ -45,6 +45,8 @@ class PackedSublayer:
                                  torch.empty(rows, groups, dtype=f32, device=dev)) for _ in range(2))
         self.attn_ws = nat.alloc_workspace(nat.nat_attn_workspace_bytes(self.attn, self.B, self.cap), dev)
         self.attn_ws[:4].zero_()  # the status word: a call without rows leaves it alone
+        # the forward's and the backward's words, which share a workspace and would overwrite one another
+        self.status_words = [torch.zeros(4, dtype=torch.uint8, device=dev) for _ in range(2)]
         self.norm_ws = nat.alloc_workspace(nat.nat_resnorm_workspace_bytes(self.norm, self.cap), dev)
 
     def _split(self, qkv):
@@ -54,6 +56,7 @@ class PackedSublayer:
         """qkv [>= cap, n_heads + 2 n_kv_heads, head_dim] -> out [cap, n_heads, head_dim]."""
         q, k, v = self._split(qkv)
         nat.nat_attn_fwd(self.attn, self.B, cu_seqlens, self.cap, q, k, v, self.out, self.lse, self.attn_ws)
+        self.status_words[0].copy_(self.attn_ws[:4])
         return self.out
 
     def join(self, x, y, w_post, gate, w_pre, n_rows):
@@ -76,8 +79,10 @@ class PackedSublayer:
         q, k, v = self._split(qkv)
         nat.nat_attn_bwd(self.attn, self.B, cu_seqlens, self.cap, q, k, v, self.out, self.lse, dout,
                          *self._split(self.dqkv), self.attn_ws)
+        self.status_words[1].copy_(self.attn_ws[:4])
         return self.dqkv
 
     def status(self):
-        """The NAT_DEV_* bits of the last attention call (waits for the stream); 0 before the first."""
-        return nat.nat_poll_status(self.attn_ws)
+        """The NAT_DEV_* bits of the last ``attend`` and the last ``attend_backward`` together (waits for the
+        stream); 0 before the first."""
+        return nat.nat_poll_status(self.status_words[0]) | nat.nat_poll_status(self.status_words[1])
