@@ -73,8 +73,10 @@ class PackedSublayer:
 
     def join(self, x, y, w_post, gate, w_pre, n_rows, r=None, h=None):
         """(r, h): the residual stream and the next block's input, in the tensors given for them (r may be x, h may
-        be y or x) or in the sublayer's own.  Without ``ckpt8`` the backward pass reads y and r: leave them alone."""
-        r, h = self.r if r is None else r, self.h if h is None else h
+        be y or x) or in the sublayer's own; h is None where there is no w_pre.  Without ``ckpt8`` the backward pass
+        reads y and r: leave them alone."""
+        r = self.r if r is None else r
+        h = None if w_pre is None else self.h if h is None else h
         nat.nat_resnorm_fwd(self.norm, x, y, w_post, gate, w_pre, n_rows, self.cap, r, h, self.rstd_y,
                             self.rstd_r, y8=self.y8, r8=self.r8)
         self._joined = None if self.ckpt8 else r

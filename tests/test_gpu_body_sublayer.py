@@ -111,3 +111,21 @@ def test_a_sublayer_holds_what_its_backward_pass_reads_and_no_more():
     spaces = subs[0].attn_ws.numel() + subs[0].norm_ws.numel()
     # and two rows of gradients, the status words, and the allocator's rounding of a dozen tensors to 512 bytes
     assert held <= kept + spaces + 2 * 4 * d + 16 * 512, (held, kept, spaces)
+
+
+@pytest.mark.parametrize("ckpt8", [False, True])
+def test_join_without_a_pre_norm_has_no_next_input(ckpt8):
+    """The last sublayer of a stack: no h, and none of an earlier call in its place."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, y, dr, w, n_rows = rand(64, 64), rand(64, 64), rand(64, 64), 1 + 0.1 * rand(64), _cu(50)
+    sub = _sublayer(dtype=torch.float32, ckpt8=ckpt8)
+    assert sub.join(x, y, w, None, w, n_rows)[1] is sub.h
+    r, h = sub.join(x, y, w, None, None, n_rows)
+    assert h is None
+    rstd = (y[:50].double().square().mean(dim=1, keepdim=True) + 1e-6).rsqrt()
+    # three products and a sum in 32 bits, and a norm of 64 terms
+    assert (r[:50] - (x[:50] + y[:50] * rstd * w)).abs().max() <= 80 * 2.0 ** -24 * 8
+    dx, _ = sub.join_backward(dr, None, w, None, None, n_rows, y=y)
+    assert torch.equal(dx[:50], dr[:50])
