@@ -176,8 +176,9 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t top_bits) {
   const float q = __fmul_rn(top, kInv);
   // 1 / top with the mantissa of top (in [1, 2)), so that no step leaves the normal range: the
   // approximate reciprocal, which one Newton step rounds correctly; then the factor and, exactly, the
-  // power of two (127 / 2, so that the power stays normal).  Checked on the device for every float from
-  // 2^-120 up, against the division and the rounded reciprocal.
+  // power of two (127 / 2, so that the power stays normal).  The tests hold both quotients against float64 for
+  // every mantissa, at 2^-120 (where the scale is subnormal), around 1 and at the largest exponents; between
+  // those only the power differs.
   const float b = __uint_as_float((top_bits & 0x007FFFFFu) | 0x3F800000u);
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(b));
