@@ -465,8 +465,8 @@ int nat_resnorm_bwd(const nat_resnorm_params* params /* host */, const void* y, 
  * Activation checkpoints in 8 bits.  Each group of 128 consecutive columns of a row (the last one
  * may be shorter) holds int8 codes and one float32 scale:
  *   top = max |x|,   code = round(x ((1 / top) 127)) to nearest even,   scale = top / 127,
- * every operation rounded to nearest in fp32 (1 / top to 24 bits also where it is subnormal), and reads back as code scale, rounded to dtype: off by at
- * most scale / 2 (1 + 2^-15) before that rounding.
+ * every operation rounded to nearest in fp32 (1 / top to 24 bits also where it is subnormal), and reads back as
+ * code scale, rounded to dtype: off by at most scale / 2 (1 + 2^-15) before that rounding.
  * A group with top < 2^-120 is stored as zeros; a group that holds an infinity or a NaN gets a NaN scale
  * and reads back as NaN.
  *   src, dst [cap, d] in dtype, codes int8 [cap, d], scales float32 [cap, ceil(d / 128)];

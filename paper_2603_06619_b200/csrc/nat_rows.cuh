@@ -114,14 +114,6 @@ __device__ __forceinline__ void copies_wait(int ahead) {
   else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
-__device__ __forceinline__ void load_weights(const float* p, float2 (&w)[kPairs]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p));
-  const float4 b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  w[0] = make_float2(a.x, a.y);
-  w[1] = make_float2(a.z, a.w);
-  w[2] = make_float2(b.x, b.y);
-  w[3] = make_float2(b.z, b.w);
-}
 
 // ---- 8-bit checkpoints ----------------------------------------------------------------
 // A group of 128 columns holds codes q = round(x ((1 / top) 127)) and one scale top / 127, top the

@@ -24,3 +24,14 @@ def test_data_of_an_overlapped_kernel_is_not_read_through_the_read_only_path():
     for name, head, body in found:
         assert "__ldg(" not in body, name
         assert not re.search(r"const\s+\w+\s*\*\s*__restrict__", head), name
+
+
+def test_every_device_helper_is_reached():
+    texts = {n: open(os.path.join(CSRC, n)).read() for n in os.listdir(CSRC)}
+    everything = "\n".join(texts.values())
+    for name, text in sorted(texts.items()):
+        for helper in set(re.findall(r"__forceinline__[^;{}()]*?\b(\w+)\(", text)):
+            if helper != "operator":
+                uses = re.findall(r"\b%s\b *[(<]" % helper, everything)
+                defined = re.findall(r"__forceinline__[^;{}()]*?\b%s\(" % helper, everything)
+                assert len(uses) > len(defined), (name, helper)
