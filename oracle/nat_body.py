@@ -43,11 +43,16 @@ def attn_fwd(q, k, v, cu, scale):
 
 
 def attn_bwd(q, k, v, out, lse, dout, cu, scale):
-    """dict of dq, dk, dv and, under "abs_" names, the sums of the magnitudes of their terms."""
+    """dict of dq, dk, dv and, under "abs_" names, the sums of the magnitudes of their terms.
+
+    What rounding errors are measured by, each kind by itself: "terms_", the sums of |dS| |k| (or |q|, or P |dout|);
+    "parts_", the same with what dP and delta are summed from in place of |dS|; "squares_", the sums of the
+    terms' squares."""
     q, k, v, out, lse, dout = (np.asarray(x, dtype=np.float64) for x in (q, k, v, out, lse, dout))
     n, Hq, D = q.shape
     g = Hq // k.shape[1]
-    r = {m + x: np.zeros_like(y) for m in ("", "abs_") for x, y in (("dq", q), ("dk", k), ("dv", v))}
+    kinds = ("", "abs_", "terms_", "parts_", "squares_")
+    r = {m + x: np.zeros_like(y) for m in kinds for x, y in (("dq", q), ("dk", k), ("dv", v))}
     for lo, hi in _spans(cu, n):
         if hi <= lo:
             continue
@@ -67,6 +72,11 @@ def attn_bwd(q, k, v, out, lse, dout, cu, scale):
             r["abs_dq"][lo:hi, h] = abs(scale) * mag @ np.abs(k[lo:hi, kh])
             r["abs_dk"][lo:hi, kh] += abs(scale) * mag.T @ np.abs(q[lo:hi, h])
             r["abs_dv"][lo:hi, kh] += P.T @ np.abs(do)
+            for kind, w, e in (("terms_", np.abs(dS), 1), ("parts_", aS, 1), ("squares_", dS * dS, 2)):
+                r[kind + "dq"][lo:hi, h] = abs(scale) ** e * w @ np.abs(k[lo:hi, kh]) ** e
+                r[kind + "dk"][lo:hi, kh] += abs(scale) ** e * w.T @ np.abs(q[lo:hi, h]) ** e
+            r["terms_dv"][lo:hi, kh] += P.T @ np.abs(do)
+            r["squares_dv"][lo:hi, kh] += (P * P).T @ (do * do)
     return r
 
 
