@@ -19,6 +19,7 @@
 #include <cuda.h>
 
 #include "nat_attn.cuh"
+#include "nat_attn_masked.cuh"
 #include "nat_attn_tc.cuh"
 
 namespace nat {
@@ -39,6 +40,7 @@ struct FwdParams {
   int64_t o_stride;
   int n_heads, n_kv_heads, group, tq, head_dim;
   float scale;
+  Rows q, k, v;  // for mend_rows
 };
 
 template <int DP>
@@ -81,10 +83,47 @@ __device__ __forceinline__ Unit unit_of(const FwdParams& p, const Entry* found, 
   return w;
 }
 
+// The rows of this block's units that masked values of v have spoilt, over the keys [first, token] of their piece; to
+// the piece's slot or to out.  For the softmax's threads, each the row that it had.
+template <int DP, bool SPLIT>
+__device__ __noinline__ void mend_rows(const FwdParams& p, const Entry* found, uint32_t units) {
+  const int t = threadIdx.x >> 7, row = threadIdx.x & 127, D = p.head_dim;
+  const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f, sc = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
+  for (uint32_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const Unit w = unit_of<SPLIT>(p, found, u);
+    const int token = w.lo + t * p.tq + row / p.group, head = w.head * p.group + row % p.group;
+    if (row >= p.group * p.tq || token >= w.seq_hi || w.nk[t] == 0) continue;
+    float* piece = w.pieces == 1 ? nullptr : p.partial + ((int64_t)w.slot * p.n_kv_heads + w.head) * fwd_slot<DP>() + t * 128 + row;
+    __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * D;
+    // a piece's weights are relative to its maximum, the whole row's to its log-sum
+    const float base = piece ? __ldcg(piece + DP * 256) * sc : __ldcg(p.lse + (int64_t)token * p.n_heads + head) * kLog2e;
+    if (!(fabsf(base) < INFINITY) || (piece ? finite_piece<256>(piece, 0, D) : finite_row(dst, 0, D))) continue;
+    const int first = w.seq_lo + w.begin * kRows, end = min(first + w.nk[t] * kRows, w.kv_hi);
+    if (!hidden_only(p.v, w.head, 1, D, token + 1, end, max(first, token - (kRows - 1)), token + 1)) continue;
+    float o[DP];
+#pragma unroll
+    for (int c = 0; c < DP; ++c) o[c] = 0.f;
+    for (int j = first; j <= token; ++j) {
+      const float s = row_dot(p.q.at(token, head, D), p.k.at(j, w.head, D), D);
+      row_add<DP>(o, as_bf16(ex2(fmaf(s * sign, sc, -base))), p.v.at(j, w.head, D), 0, D);
+    }
+#pragma unroll
+    for (int c = 0; c < DP; c += 8) {
+      if (piece) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) __stcg(piece + (c + i) * 256, o[c + i]);
+      } else if (c < D) {
+        *reinterpret_cast<uint4*>(dst + c) = make_uint4(bf16_pair(o[c], o[c + 1]), bf16_pair(o[c + 2], o[c + 3]),
+                                                        bf16_pair(o[c + 4], o[c + 5]), bf16_pair(o[c + 6], o[c + 7]));
+      }
+    }
+  }
+}
+
 template <int DP, bool SPLIT>  // SPLIT: some tiles come in pieces
 __global__ void __launch_bounds__(384, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                const __grid_constant__ CUtensorMap map_v, const FwdParams p) {
+                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FwdParams p) {
   using R = FwdShape<DP>;
   constexpr int kNS = R::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -94,8 +133,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint64_t *q_full = bars, *q_empty = bars + 2, *s_full = bars + 4, *o_done = bars + 6, *raw = bars + 8;
   uint64_t *drain = bars + 9, *p_full = bars + 10;  // p_full [row tile][half of the keys]
   uint64_t *full = bars + 14, *empty = bars + 14 + kNS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * kNS);  // address, abort flag, total
-  volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 14 + 2 * kNS);  // address, abort flag, total, odd flag
+  volatile uint32_t *abort_flag = tmem_slot + 1, *odd_flag = tmem_slot + 3;
   Entry* found = reinterpret_cast<Entry*>(tmem_slot + 4);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
 
@@ -114,7 +153,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       tc::mbar_init(&full[s], 1);
       tc::mbar_init(&empty[s], 1);
     }
-    *abort_flag = 0u;
+    *abort_flag = *odd_flag = 0u;
     tc::fence_barrier_init();
   }
   if (warp == 8) {
@@ -376,12 +415,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       const int head = w.head * p.group + head_in;
       __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * p.head_dim;
       float* lse = p.lse + (int64_t)token * p.n_heads + head;
+      float2 odd = {0.f, 0.f};
       if (w.pieces == 1) {
         const float inv = 1.f / l;
 #pragma unroll
         for (int c = 0; c < DP / 32; ++c) {
           float o[32];
           tc::tmem_ld32(o_addr + c * 32, o);
+          odd = finite32(o, odd);
           if (valid) store_row32(dst + c * 32, o, inv, p.head_dim - c * 32, wide);
         }
         if (valid) *lse = fmaf(m, sc * kLn2, logf(l));
@@ -393,6 +434,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           for (int c = 0; c < DP / 32; ++c) {
             float o[32];
             tc::tmem_ld32(o_addr + c * 32, o);
+            odd = finite32(o, odd);
 #pragma unroll
             for (int i = 0; i < 32; ++i) __stcg(own + (c * 32 + i) * 256, o[i]);
           }
@@ -400,6 +442,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         __stcg(own + DP * 256, nk > 0 ? m : -INFINITY);
         __stcg(own + (DP + 1) * 256, nk > 0 ? l : 0.f);
       }
+      if (valid && !is_finite(odd)) *odd_flag = 1u;
       tc::fence_before_sync();
     }
   }
@@ -409,6 +452,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   tc::fence_after_sync();
   if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
   if (warp == 8) tc::tmem_dealloc(tmem, 512);
+  if (warp < 8 && *odd_flag && !*abort_flag) mend_rows<DP, SPLIT>(p, found, units);
 }
 
 // Joins the pieces of a tile, in their order: a block takes 16 columns of the 256 rows of a list entry, a
@@ -528,6 +572,9 @@ int fwd(const Args& a, const Layout& l) {
   fp.tq = tq;
   fp.head_dim = p.head_dim;
   fp.scale = p.scale;
+  fp.q = {(const __nv_bfloat16*)a.q, p.q_stride};
+  fp.k = {(const __nv_bfloat16*)a.k, p.k_stride};
+  fp.v = {(const __nv_bfloat16*)a.v, p.v_stride};
   const unsigned grid = (unsigned)min((int64_t)dev.sms, units);
   const size_t smem = FwdShape<DP>::kSmem;
   if (plan) {

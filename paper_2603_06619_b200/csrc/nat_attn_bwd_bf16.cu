@@ -21,6 +21,7 @@
 #include <cuda.h>
 
 #include "nat_attn.cuh"
+#include "nat_attn_masked.cuh"
 #include "nat_attn_tc.cuh"
 
 namespace nat {
@@ -38,6 +39,7 @@ struct BwdParams {
   int64_t q_stride, k_stride, v_stride;
   int n_heads, n_kv_heads, group, tq, head_dim;
   float scale;
+  Rows q, k, v, dout;  // for mend_dq and mend_dkv
 };
 
 template <int DP>
@@ -55,10 +57,10 @@ struct BwdShape {
   static constexpr uint32_t kSmem = kTiles + kStats + kBars + kSlack;
 };
 
-// Behind the barriers: the address of the block's tensor memory, its abort flag and, without a list, its
-// tile and their number.
+// Behind the barriers: the address of the block's tensor memory, its abort flag, whether a result was not finite and,
+// without a list, its tile and their number.
 struct Found {
-  uint32_t tmem, abort, total, pad;
+  uint32_t tmem, abort, total, odd;
   Entry entry;
 };
 __device__ __forceinline__ void find(const BwdParams& p, uint32_t block, Found* f, bool report) {
@@ -92,33 +94,120 @@ __device__ __forceinline__ void store64(uint32_t addr, const float (&x)[64]) {
 // Where step kk (16 of the contraction) of such an operand lies.
 constexpr __device__ uint32_t half_cols(int kk) { return (uint32_t)(kk < 4 ? kk * 8 : 64 + (kk - 4) * 8); }
 
-// D columns [half * DP/2, ...) of an accumulator row, times f, to global memory.
+// D columns [half * DP/2, ...) of an accumulator row, times f, to global memory.  Returns zero, or NaN where one
+// is not finite.
 template <int DP>
-__device__ __forceinline__ void store_acc(uint32_t addr, int half, __nv_bfloat16* dst, int D, float f, bool valid,
-                                          bool wide) {
+__device__ __forceinline__ float2 store_acc(uint32_t addr, int half, __nv_bfloat16* dst, int D, float f, bool valid,
+                                            bool wide) {
+  float2 odd = {0.f, 0.f};
 #pragma unroll
   for (int c = 0; c < DP / 64; ++c) {
     const int col = half * (DP / 2) + c * 32;
     float o[32];
     tc::tmem_ld32(addr + col, o);
+    odd = finite32(o, odd);
     if (valid) store_row32(dst + col, o, f, D - col, wide);
+  }
+  return odd;
+}
+
+// Where a piece's N accumulators go for one row: [accumulator column][row].
+template <int DP, int N>
+__device__ __forceinline__ float* piece_slot(const BwdParams& p, const Entry& e, int head, int row) {
+  return p.partial + ((int64_t)(e.slot + e.piece) * p.n_kv_heads + head) * (128 * N * DP) + row;
+}
+// One of them, from tensor-memory column `addr` on.  Returns as store_acc.
+template <int DP>
+__device__ __forceinline__ float2 store_piece(float* slot, uint32_t addr, int half) {
+  float2 odd = {0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < DP / 64; ++c) {
+    const int col = half * (DP / 2) + c * 32;
+    float o[32];
+    tc::tmem_ld32(addr + col, o);
+    odd = finite32(o, odd);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) __stcg(slot + (col + i) * 128, o[i]);
+  }
+  return odd;
+}
+
+// A thread's half of a row of gradients that was added up again: to the piece's slot or, times f, to the result.
+template <int DP>
+__device__ __forceinline__ void store_again(const float (&o)[DP / 2], int half, float* slot, __nv_bfloat16* dst, float f, int D) {
+#pragma unroll
+  for (int c = 0; c < DP / 2; c += 8) {
+    const int col = half * (DP / 2) + c;
+    if (slot) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) __stcg(slot + (col + i) * 128, o[c + i]);
+    } else if (col < D) {
+      *reinterpret_cast<uint4*>(dst + col) = make_uint4(bf16_pair(o[c] * f, o[c + 1] * f), bf16_pair(o[c + 2] * f, o[c + 3] * f),
+                                                        bf16_pair(o[c + 4] * f, o[c + 5] * f), bf16_pair(o[c + 6] * f, o[c + 7] * f));
+    }
   }
 }
 
-// A piece's N accumulators, from tensor-memory column `addr` on, to its slot: [accumulator column][row].
-template <int DP, int N>
-__device__ __forceinline__ void store_piece(const BwdParams& p, const Entry& e, int head, uint32_t addr, int half, int row) {
-  float* own = p.partial + ((int64_t)(e.slot + e.piece) * p.n_kv_heads + head) * (128 * N * DP) + row;
+// P and P (dP - delta) of one query and key.
+__device__ __forceinline__ float2 weight_and_slope(const BwdParams& p, int token, int head, int key, int kv_head) {
+  const int D = p.head_dim;
+  const int64_t at = (int64_t)token * p.n_heads + head;
+  const float s = row_dot(p.q.at(token, head, D), p.k.at(key, kv_head, D), D);
+  const float w = ex2(fmaf(s, p.scale * kLog2e, -__ldcg(p.lse2 + at)));
+  return make_float2(w, w * (row_dot(p.dout.at(token, head, D), p.v.at(key, kv_head, D), D) - __ldcg(p.delta + at)));
+}
+
+// The rows of dq of this block's units that masked values of k have spoilt, over the keys [first, token] of their
+// piece.  Each thread takes the half row that it had.
+template <int DP>
+__device__ __noinline__ void mend_dq(const BwdParams& p, const Entry* found, uint32_t units, uint32_t block, uint32_t blocks) {
+  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, D = p.head_dim, lo = half * (DP / 2), hi = min(lo + DP / 2, D);
+  for (uint32_t u = block; u < units; u += blocks) {
+    const Entry e = p.list ? p.list[u / p.n_kv_heads] : *found;
+    const int kv_head = (int)(u % p.n_kv_heads), token = e.lo + row / p.group, head = kv_head * p.group + row % p.group;
+    if (row >= p.group * p.tq || token >= e.seq_hi) continue;
+    float* slot = e.pieces == 1 ? nullptr : piece_slot<DP, 1>(p, e, kv_head, row);
+    __nv_bfloat16* dst = p.dq + (int64_t)token * p.q_stride + (int64_t)head * D;
+    if (slot ? finite_piece<128>(slot, lo, hi) : finite_row(dst, lo, hi)) continue;
+    const int64_t at = (int64_t)token * p.n_heads + head;
+    if (!(fabsf(__ldcg(p.lse2 + at)) < INFINITY && fabsf(__ldcg(p.delta + at)) < INFINITY)) continue;
+    const int first = e.seq_lo + e.begin * kRows, end = min(min(e.lo + p.tq, e.seq_hi), e.end == kAllSteps ? e.seq_hi : e.seq_lo + e.end * kRows);
+    if (!hidden_only(p.k, kv_head, 1, D, token + 1, end, max(first, token - (kRows - 1)), token + 1)) continue;
+    float o[DP / 2];
 #pragma unroll
-  for (int k = 0; k < N; ++k)
+    for (int c = 0; c < DP / 2; ++c) o[c] = 0.f;
+    for (int j = first; j <= token && j < end; ++j)
+      row_add<DP / 2>(o, as_bf16(weight_and_slope(p, token, head, j, kv_head).y), p.k.at(j, kv_head, D), half * (DP / 16), D);
+    store_again<DP>(o, half, slot, dst, p.scale, D);
+  }
+}
+
+// The same for the rows of dv (of_k false) or dk, spoilt by masked values of dout or q, over the queries from the key on.
+template <int DP>
+__device__ __noinline__ void mend_dkv(const BwdParams& p, bool of_k, const Entry* found, uint32_t units, uint32_t block,
+                                      uint32_t blocks) {
+  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, D = p.head_dim, lo = half * (DP / 2), hi = min(lo + DP / 2, D);
+  const Rows& rows = of_k ? p.q : p.dout;
+  for (uint32_t u = block; u < units; u += blocks) {
+    const Entry e = p.list ? p.list[u / p.n_kv_heads] : *found;
+    const int kv_head = (int)(u % p.n_kv_heads), key = e.lo + row, head = kv_head * p.group;
+    if (key >= e.seq_hi) continue;
+    float* slot = e.pieces == 1 ? nullptr : piece_slot<DP, 2>(p, e, kv_head, row) + (of_k ? DP * 128 : 0);
+    __nv_bfloat16* dst = (of_k ? p.dk + (int64_t)key * p.k_stride : p.dv + (int64_t)key * p.v_stride) + (int64_t)kv_head * D;
+    if (slot ? finite_piece<128>(slot, lo, hi) : finite_row(dst, lo, hi)) continue;
+    const int first = e.lo + e.begin * p.tq, end = e.end == kAllSteps ? e.seq_hi : (int)min((int64_t)e.lo + (int64_t)e.end * p.tq, (int64_t)e.seq_hi);
+    const int seen = max(first, key);
+    if (!hidden_only(rows, head, p.group, D, first, min(key, end), seen, min(seen + kRows, end))) continue;
+    float o[DP / 2];
 #pragma unroll
-    for (int c = 0; c < DP / 64; ++c) {
-      const int col = half * (DP / 2) + c * 32;
-      float o[32];
-      tc::tmem_ld32(addr + k * 128 + col, o);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) __stcg(own + (k * DP + col + i) * 128, o[i]);
-    }
+    for (int c = 0; c < DP / 2; ++c) o[c] = 0.f;
+    for (int i = seen; i < end; ++i)
+      for (int h = head; h < head + p.group; ++h) {
+        const float2 w = weight_and_slope(p, i, h, key, kv_head);
+        row_add<DP / 2>(o, as_bf16(of_k ? w.y : w.x), rows.at(i, h, D), half * (DP / 16), D);
+      }
+    store_again<DP>(o, half, slot, dst, of_k ? p.scale : 1.f, D);
+  }
 }
 
 // A ring of N tiles: `item` numbers the loads of a block, stage item % N.
@@ -204,7 +293,7 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
   const Ring<R::kA> ring_k{tc::smem_u32(tiles_a), bars + 10, bars + 10 + R::kA, R::kTile};
   const Ring<R::kB> ring_v{tc::smem_u32(tiles_b), bars + 10 + 2 * R::kA, bars + 10 + 2 * R::kA + R::kB, R::kTile};
   Found* const found = reinterpret_cast<Found*>(bars + 10 + 2 * (R::kA + R::kB));
-  volatile uint32_t* abort_flag = &found->abort;
+  volatile uint32_t *abort_flag = &found->abort, *odd_flag = &found->odd;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -218,7 +307,7 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
     tc::mbar_init(raw, 1);
     tc::mbar_init(drain, 2);
     for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[10 + s], 1);
-    *abort_flag = 0u;
+    *abort_flag = *odd_flag = 0u;
     tc::fence_barrier_init();
   }
   if (warp == 8) {
@@ -383,11 +472,10 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
       ++turns;
       tc::fence_after_sync();
       __nv_bfloat16* dst = p.dq + (int64_t)token * p.q_stride + (int64_t)head * p.head_dim;
-      if (e.pieces == 1) {
-        store_acc<DP>(tmem + 384 + lane_base, half, dst, p.head_dim, p.scale, valid, wide);
-      } else {
-        store_piece<DP, 1>(p, e, (int)(u % p.n_kv_heads), tmem + 384 + lane_base, half, row);
-      }
+      float* slot = e.pieces == 1 ? nullptr : piece_slot<DP, 1>(p, e, (int)(u % p.n_kv_heads), row);
+      const float2 odd = e.pieces == 1 ? store_acc<DP>(tmem + 384 + lane_base, half, dst, p.head_dim, p.scale, valid, wide)
+                                       : store_piece<DP>(slot, tmem + 384 + lane_base, half);
+      if (valid && !is_finite(odd)) *odd_flag = 1u;
       tc::fence_before_sync();
     }
   }
@@ -397,6 +485,7 @@ __device__ __forceinline__ void dq_part(const CUtensorMap& map_q, const CUtensor
   tc::fence_after_sync();
   if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
   if (warp == 8) tc::tmem_dealloc(tmem, 512);
+  if (warp < 8 && *odd_flag && !*abort_flag) mend_dq<DP>(p, &found->entry, units, block, blocks);
 }
 
 template <int DP>
@@ -421,7 +510,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
   const Ring<R::kA> ring_q{tc::smem_u32(tiles_a), bars + 14, bars + 14 + R::kA, R::kTile};
   const Ring<R::kB> ring_do{tc::smem_u32(tiles_b), bars + 14 + 2 * R::kA, bars + 14 + 2 * R::kA + R::kB, R::kTile};
   Found* const found = reinterpret_cast<Found*>(bars + 14 + 2 * (R::kA + R::kB));
-  volatile uint32_t* abort_flag = &found->abort;
+  volatile uint32_t *abort_flag = &found->abort, *odd_flag = &found->odd;
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int q_rows = p.group * p.tq;
 
@@ -441,7 +530,7 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
     }
     tc::mbar_init(p_early, 256);
     for (int s = 0; s < 2 * (R::kA + R::kB); ++s) tc::mbar_init(&bars[14 + s], s < 2 * R::kA + R::kB ? 1 : 2);
-    *abort_flag = 0u;
+    *abort_flag = *odd_flag = 0u;
     tc::fence_barrier_init();
   }
   if (warp == 8) {
@@ -684,12 +773,12 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
       const bool valid = key < e.seq_hi;
       const int64_t col = (int64_t)(u % p.n_kv_heads) * p.head_dim;
       __nv_bfloat16 *dv = p.dv + (int64_t)key * p.v_stride + col, *dk = p.dk + (int64_t)key * p.k_stride + col;
-      if (e.pieces == 1) {
-        store_acc<DP>(tmem + 256 + lane_base, half, dv, p.head_dim, 1.f, valid, wide);
-        store_acc<DP>(tmem + 384 + lane_base, half, dk, p.head_dim, p.scale, valid, wide);
-      } else {
-        store_piece<DP, 2>(p, e, (int)(u % p.n_kv_heads), tmem + 256 + lane_base, half, row);
-      }
+      float* slot = e.pieces == 1 ? nullptr : piece_slot<DP, 2>(p, e, (int)(u % p.n_kv_heads), row);
+      const float2 odd_v = e.pieces == 1 ? store_acc<DP>(tmem + 256 + lane_base, half, dv, p.head_dim, 1.f, valid, wide)
+                                         : store_piece<DP>(slot, tmem + 256 + lane_base, half);
+      const float2 odd_k = e.pieces == 1 ? store_acc<DP>(tmem + 384 + lane_base, half, dk, p.head_dim, p.scale, valid, wide)
+                                         : store_piece<DP>(slot + DP * 128, tmem + 384 + lane_base, half);
+      if (valid && !(is_finite(odd_v) && is_finite(odd_k))) *odd_flag = 1u;
       tc::fence_before_sync();
     }
   }
@@ -699,6 +788,10 @@ __device__ __forceinline__ void dkv_part(const CUtensorMap& map_q, const CUtenso
   tc::fence_after_sync();
   if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, NAT_DEV_TIMEOUT);
   if (warp == 8) tc::tmem_dealloc(tmem, 512);
+  if (warp < 8 && *odd_flag && !*abort_flag) {
+    mend_dkv<DP>(p, false, &found->entry, units, block, blocks);
+    mend_dkv<DP>(p, true, &found->entry, units, block, blocks);
+  }
 }
 
 template <int DP>
@@ -785,6 +878,10 @@ int bwd(const Args& a, const Layout& l) {
   bp.tq = tq;
   bp.head_dim = p.head_dim;
   bp.scale = p.scale;
+  bp.q = {(const __nv_bfloat16*)a.q, p.q_stride};
+  bp.k = {(const __nv_bfloat16*)a.k, p.k_stride};
+  bp.v = {(const __nv_bfloat16*)a.v, p.v_stride};
+  bp.dout = {(const __nv_bfloat16*)a.dout, p.o_stride};
   auto part = [&](Plan which) {
     BwdParams w = bp;
     w.list = plan ? entries(a, l, which) : nullptr;
