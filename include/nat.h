@@ -352,7 +352,11 @@ int nat_policy_loss_fwd_bwd(const nat_loss_params* params /* host */, const void
  * The transformer body on packed sequences (Section 4, the paragraph on compute savings:
  * under RPC the model processes the prefixes 1..L_i only).  After nat_gather_rows the
  * prefixes lie packed, sel_offsets is their cu_seqlens and *n_sel their number of rows; the
- * operators below take both from the device, with the host's bound `cap` on the rows.  Rows at
+ * operators below take both from the device, with the host's bound `cap` on the rows.  A packed sequence holds every
+ * token that its own attend to: where responses follow prompts, compact prompt and prefix as one sequence, i.e.
+ * nat_compact_prefix on the bounds of the whole sequences with prompt length + L_i for cut_len (a prompt that several
+ * responses share is then there once for each).  The response's rows, behind the prompt's in each sequence, are what the
+ * loss takes (nat_gather_rows).  Rows at
  * or after the last sequence are neither read into a result nor written.  Every sum is taken in
  * 32 bits and in a fixed order: a call repeated on the same inputs reproduces its outputs bit
  * for bit.

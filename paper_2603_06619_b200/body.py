@@ -2,7 +2,12 @@
 
 Under prefix cutting the model processes the prefixes only (Section 4, the paragraph on compute
 savings): ``nat_gather_rows`` packs them, ``sel_offsets`` is their ``cu_seqlens`` and ``n_sel`` the
-number of rows.  ``PackedSublayer`` owns what one attention sublayer keeps and writes for batches of up
+number of rows.  A token attends to the packed tokens of its sequence and to nothing else, so responses that follow
+prompts are packed behind them, by ``nat_compact_prefix`` on the bounds of prompt and response together:
+
+    nat.nat_compact_prefix(B, cu_whole, n_whole, prompt_len + cut_len, idx, resp, offs, n_sel, cap)
+
+``PackedSublayer`` owns what one attention sublayer keeps and writes for batches of up
 to ``cap`` such rows (torch is only the allocator and the stream) and exposes its calls in the
 order a trainer makes them, forward and, reversed, backward:
 
