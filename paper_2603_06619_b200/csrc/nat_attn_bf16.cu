@@ -27,6 +27,7 @@ namespace attn {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFar = 16777216.f;  // a shift above this (2^24) is off by more than half a unit
 constexpr float kRescale = 8.f;  // growth of a row's maximum (log2) that is left in P
 
 struct FwdParams {
@@ -381,7 +382,15 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           }
         }
         // a row whose scores are all minus infinity so far has no maximum to subtract
-        const float shift = base == -INFINITY ? 0.f : base * sc;
+        float shift = base == -INFINITY ? 0.f : base * sc;
+        // The fused subtraction below leaves the rounding of the shift in every exponent.  It cancels in out, but of scores
+        // beyond 2^30 it would take the weights out of range: there the maximum is subtracted first.
+        if (__any_sync(0xFFFFFFFFu, fabsf(shift) > kFar)) {
+          const float far = fabsf(shift) > kFar ? base : 0.f;
+          if (far != 0.f) shift = 0.f;
+#pragma unroll
+          for (int c = 0; c < 128; ++c) s[c] -= far;
+        }
         const float2 scale2 = {sc, sc}, shift2 = {-shift, -shift};
         float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
         // P goes out in halves: the first one's product runs during the second one's exponentials

@@ -57,7 +57,7 @@ def test_attention_in_pieces_with_other_scales(scale):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("lengths", [[300, 40], [1700]])
-@pytest.mark.parametrize("size", [1e2, 1e4, 1e6])
+@pytest.mark.parametrize("size", [1e2, 1e4, 1e6, 1e8, 1e9, 1e10, 1e20, 1e30])
 def test_attention_of_large_scores(size, lengths, dtype):
     """A score's error is relative to it, and moves P by as much: out is still a mean of the values, within the
     bound that this gives."""
