@@ -424,6 +424,8 @@ int nat_attn_bwd(const nat_attn_params* params /* host */, int32_t B, const int3
  * w_pre (no h, no rstd_r), y (r = alpha x; then w_post and gate are NULL too).
  * y8, r8 with y8_scales, r8_scales, all or none: 8-bit checkpoints of y and of the stored r, the
  * same bytes as nat_ckpt8_store writes (y8 only where there is a y).
+ * The mean squares of y and r are float32: magnitudes above 10^17 or, where eps does not cover them, below 10^-16
+ * leave its range.
  * n_rows: device int32 scalar (NULL: cap); rows at or after it are not touched.
  * d a multiple of 8, at most 8192; matrices, weights and codes 16-byte aligned.
  *

@@ -9,10 +9,10 @@
 // barrier, not the arithmetic, is what a row waits for: with z = y (w_post gate)
 //   sum r^2 = alpha^2 sum x^2 + 2 alpha rstd_y sum x z + rstd_y^2 sum z^2
 // gives the second norm before r is formed.  Where the terms cancel (below 1/16 of their
-// magnitudes) the row is summed again from r itself.  The weights, multiplied together, are kept in
-// shared memory; from L1 they were half evicted by the rows.  60,000 rows of 4096 bfloat16: 302 us,
-// 0.99 of the measured copy bandwidth; with checkpoints 495 us (0.76; issue slots 72 % busy with the
-// quantisation).
+// magnitudes), or one of the sums has lost its squares to underflow, the row is summed again from r
+// itself.  The weights, multiplied together, are kept in shared memory; from L1 they were half evicted by
+// the rows.  60,000 rows of 4096 bfloat16: 302 us, 0.99 of the measured copy bandwidth; with checkpoints
+// 495 us (0.76; issue slots 72 % busy with the quantisation).
 //
 // Backward, with u = dh w_pre, rhat = r rstd_r, yhat = y rstd_y, e = dr_in + rstd_r u, z = yhat w_post gate:
 //   dr = e - rstd_r rhat mean(u rhat),   dx = alpha dr,   v = dr w_post gate,
@@ -168,6 +168,8 @@ struct Weights {
   }
 };
 
+constexpr float kTiny = 1e-28f;  // of 8192 squares: the larger ones are above 2^-107, normal with all their bits
+
 template <typename T, int NT, int CH, bool C8>
 __global__ void __launch_bounds__(block_threads(NT), blocks_per_sm(fwd_threads(C8, NT), NT))
 resnorm_fwd_kernel(FwdArgs a) {
@@ -249,8 +251,9 @@ resnorm_fwd_kernel(FwdArgs a) {
       // h is formed from r before its rounding: the norm then adds no error of its own
       const float own = a.alpha * a.alpha * sums[1] + f * f * sums[3];
       float square = fmaf(2.f * a.alpha * f, sums[2], own);
-      const bool cancels = !(square > 0.0625f * own);  // the same in all threads of the row
-      if (__any_sync(0xFFFFFFFFu, cancels)) {
+      // the same in all threads of the row; squares that small have left the normal range, or sums of them may have
+      const bool cancels = !(square > 0.0625f * own) || sums[1] < kTiny || (y && sums[3] < kTiny);
+      if (__any_sync(0xFFFFFFFFu, live && cancels)) {
         float2 rr = both(0.f);
 #pragma unroll
         for (int i = 0; i < CH; ++i)

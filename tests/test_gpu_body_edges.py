@@ -5,7 +5,7 @@ import torch
 
 from oracle import nat_body as ob
 from paper_2603_06619_b200 import nat
-from test_gpu_body import DT, Attn, _close, _np
+from test_gpu_body import DT, Attn, Join, _close, _np
 from test_gpu_body_gradients import check_gradients
 
 pytestmark = pytest.mark.gpu
@@ -80,3 +80,27 @@ def test_attention_of_large_scores(size, lengths, dtype):
     top = S.argmax(axis=2)
     for t, h in np.argwhere(clear)[:200]:
         assert np.abs(_np(a.out[t, h]) - v[top[t, h], h]).max() <= 4 * u * np.abs(v[top[t, h], h]).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", ["none", "channel", "row"])
+@pytest.mark.parametrize("n,d", [(7, 64), (5, 128), (3, 256), (4, 512), (3, 4096)])
+@pytest.mark.parametrize("x,y,w,alpha", [(1e-30, 1e-18, 1e-6, 1.0), (1e-18, 1e-18, 1e-6, 1.0), (1e-22, 1.0, 1e-20, 1e10), (0.0, 1e-10, 1e-12, 0.5),
+                                         (1e-21, 0.0, 1.0, 1e15), (1e18, 1.0, 1.0, 1e-18)])
+def test_join_of_rows_far_from_one(x, y, w, alpha, n, d, gate, dtype):
+    """r is of a size that its norm in 32 bits can take, made of parts whose squares are not.  (y and r themselves
+    have to be: the header says so.)"""
+    j = Join(n, d, DT[dtype], gate=gate, seed=81, eps=0.0 if y else 1e-30, alpha=alpha)
+    j.x.mul_(x)
+    j.y.mul_(y)
+    j.w_post.mul_(w)
+    j.fwd()
+    cut = lambda t: _np(t[:n])  # noqa: E731
+    g = None if gate == "none" else cut(j.gate) if gate == "row" else _np(j.gate)
+    ref = ob.resnorm_fwd(cut(j.x), cut(j.y), _np(j.w_post), g, _np(j.w_pre), j.eps, alpha, gate)
+    u, e = torch.finfo(DT[dtype]).eps / 2, (d + 32) * 2.0 ** -24
+    mag = np.abs(alpha * cut(j.x)) + np.abs(ref["r"] - alpha * cut(j.x))
+    _close("rstd_r", j.rstd_r[:n], ref["rstd_r"], 2 * e * ref["rstd_r"] * (1 + 8 * (mag ** 2).sum(axis=1) / (ref["r"] ** 2).sum(axis=1)))
+    unit = np.abs(ref["rstd_r"][:, None] * _np(j.w_pre))
+    ratio = np.sqrt((mag ** 2).sum(axis=1) / (ref["r"] ** 2).sum(axis=1))[:, None]
+    _close("h", j.h[:n], ref["h"], u * np.abs(ref["h"]) + e * ((3 + 16 * ratio ** 2) * np.abs(ref["h"]) + 3 * mag * unit))
