@@ -96,17 +96,32 @@ __device__ __noinline__ void mend_rows(const FwdParams& p, const Entry* found, u
     if (row >= p.group * p.tq || token >= w.seq_hi || w.nk[t] == 0) continue;
     float* piece = w.pieces == 1 ? nullptr : p.partial + ((int64_t)w.slot * p.n_kv_heads + w.head) * fwd_slot<DP>() + t * 128 + row;
     __nv_bfloat16* dst = p.out + (int64_t)token * p.o_stride + (int64_t)head * D;
-    // a piece's weights are relative to its maximum, the whole row's to its log-sum
-    const float base = piece ? __ldcg(piece + DP * 256) * sc : __ldcg(p.lse + (int64_t)token * p.n_heads + head) * kLog2e;
-    if (!(fabsf(base) < INFINITY) || (piece ? finite_piece<256>(piece, 0, D) : finite_row(dst, 0, D))) continue;
+    // the piece's maximum, or the row's log-sum: neither is finite where the softmax itself was not
+    const float top = piece ? __ldcg(piece + DP * 256) : __ldcg(p.lse + (int64_t)token * p.n_heads + head);
+    if (!(fabsf(top) < INFINITY) || (piece ? finite_piece<256>(piece, 0, D) : finite_row(dst, 0, D))) continue;
     const int first = w.seq_lo + w.begin * kRows, end = min(first + w.nk[t] * kRows, w.kv_hi);
     if (!hidden_only(p.v, w.head, 1, D, token + 1, end, max(first, token - (kRows - 1)), token + 1)) continue;
-    float o[DP];
+    float o[DP], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int c = 0; c < DP; ++c) o[c] = 0.f;
     for (int j = first; j <= token; ++j) {
-      const float s = row_dot(p.q.at(token, head, D), p.k.at(j, w.head, D), D);
-      row_add<DP>(o, as_bf16(ex2(fmaf(s * sign, sc, -base))), p.v.at(j, w.head, D), 0, D);
+      const float s = sign * row_dot(p.q.at(token, head, D), p.k.at(j, w.head, D), D);
+      if (s == -INFINITY) continue;
+      if (s > m) {
+        const float f = ex2((m - s) * sc);
+#pragma unroll
+        for (int c = 0; c < DP; ++c) o[c] *= f;
+        l *= f;
+        m = s;
+      }
+      const float weight = ex2((s - m) * sc);
+      l += weight;
+      row_add<DP>(o, as_bf16(weight), p.v.at(j, w.head, D), 0, D);
+    }
+    const float inv = 1.f / l;
+    if (piece) {
+      __stcg(piece + DP * 256, m);
+      __stcg(piece + (DP + 1) * 256, l);
     }
 #pragma unroll
     for (int c = 0; c < DP; c += 8) {
@@ -114,8 +129,8 @@ __device__ __noinline__ void mend_rows(const FwdParams& p, const Entry* found, u
 #pragma unroll
         for (int i = 0; i < 8; ++i) __stcg(piece + (c + i) * 256, o[c + i]);
       } else if (c < D) {
-        *reinterpret_cast<uint4*>(dst + c) = make_uint4(bf16_pair(o[c], o[c + 1]), bf16_pair(o[c + 2], o[c + 3]),
-                                                        bf16_pair(o[c + 4], o[c + 5]), bf16_pair(o[c + 6], o[c + 7]));
+        *reinterpret_cast<uint4*>(dst + c) = make_uint4(bf16_pair(o[c] * inv, o[c + 1] * inv), bf16_pair(o[c + 2] * inv, o[c + 3] * inv),
+                                                        bf16_pair(o[c + 4] * inv, o[c + 5] * inv), bf16_pair(o[c + 6] * inv, o[c + 7] * inv));
       }
     }
   }

@@ -124,3 +124,28 @@ def test_everything_infinite_ends_soon():
             end.synchronize()
         times.append(begin.elapsed_time(end))
     assert max(times[1:]) < 100 * times[0], times
+
+
+@pytest.mark.parametrize("lengths,heads", [([300], (4, 2, 64)), ([2100], (2, 2, 64))])
+@pytest.mark.parametrize("size", [1e5, 1e9])
+def test_rows_of_large_scores_that_do_not_see_them(size, lengths, heads):
+    """Where one key owns a row by far the row is that key's value, spoilt neighbours or not."""
+    a, b = (Attn(lengths, *heads, torch.bfloat16, seed=63) for _ in range(2))
+    for x in (a, b):
+        x.q.mul_(size ** 0.5)
+        x.k.mul_(size ** 0.5)
+    a.fwd()
+    for t in (1, 100, 250, lengths[0] - 5):
+        b.v.copy_(a.v)
+        b.v[t, :, 7] = float("nan")
+        b.fwd()
+        # P is rounded to bfloat16 in both, and the result once more: two half steps of each
+        u = 2.0 ** -8
+        S = a.params.scale * torch.einsum("ihd,jhd->hij", a.q[:t].double(), a.k[:t].double().repeat_interleave(heads[0] // heads[1], 1))
+        S.masked_fill_(torch.ones(t, t, dtype=torch.bool, device="cuda").triu(1), float("-inf"))
+        top = S.topk(min(2, t), dim=2).values
+        clear = (top[:, :, 0] - top[:, :, -1] > 1e-4 * size).t() if t > 1 else torch.ones(1, heads[0], dtype=torch.bool, device="cuda")
+        clear[0] = True
+        x, y = a.out[:t].double(), b.out[:t].double()
+        assert torch.isfinite(y).all()
+        assert ((x - y).abs() <= 4 * u * x.abs())[clear].all()
