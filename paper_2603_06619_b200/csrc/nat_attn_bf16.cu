@@ -14,8 +14,8 @@
 // (bf16 pairs) overwrites the first half of its S.  O is rescaled only when a row's maximum has
 // grown by more than 2^8 since the last time: P stays below 2^8 and the sums in fp32 lose nothing.
 //
-// 33,777 tokens in three sequences, 32 heads over 8, 128 columns: 3.05 ms, 1030 TFLOP/s counted, at the 1000 W
-// cap (1580 MHz; 0.62 of the measured burst rate of a plain product, 0.74 of its sustained rate).
+// 33,777 tokens in three sequences, 32 heads over 8, 128 columns: 3.08 ms, 1020 TFLOP/s counted, at the 1000 W
+// cap (1580 MHz; 0.61 of the measured burst rate of a plain product, 0.74 of its sustained rate).
 #include <cuda.h>
 
 #include "nat_attn.cuh"
