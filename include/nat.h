@@ -487,6 +487,85 @@ int nat_ckpt8_load(int32_t dtype, int64_t d, const int8_t* codes, const float* s
                    const int32_t* n_rows, int64_t cap, void* dst, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Embedding of the packed tokens and the gradient of its table.
+ *   id_k = ids[sel_idx[k]]   (sel_idx NULL: ids[k]),   for rows k < min(*n_rows, cap)
+ *   x_k  = scale table[id_k]
+ *   dtable_v = scale sum over {k : id_k = v} of dx_k     (float32; with accumulate added to its contents)
+ * table [V, d], x, dx [cap, d] row-major in dtype; ids int32 of the packed stream, sel_idx int32 [cap] as nat_compact
+ * leaves it; dtable float32 [V, d]: without accumulate all of it is written, rows of the table that no token names
+ * with zeros; with accumulate those stay untouched.  dtable may be the dW of the policy loss (tied weights).
+ * n_rows: device int32 scalar (NULL: cap); rows at or after it are neither written nor read.
+ * An id outside [0, V) has no row: x_k is NaN, and the gradient leaves the token out and raises NAT_DEV_BAD_TARGET in
+ * the status word at the head of the workspace (nat_poll_status).
+ * The tokens are sorted by id and a table row's are added in 32 bits in ascending order k, in pieces cut at every 128th
+ * sorted token where there are more than 128; a call repeated on the same inputs reproduces its output bit for bit.
+ * d a multiple of 8, at most 65536; V at most 2^30; matrices 16-byte aligned.
+ * workspace (gradient only): nat_embed_workspace_bytes(params, cap), which grows with cap; calls that may run at the
+ * same time need one each.  A call with cap = 0 does nothing (the gradient: it still writes dtable's zeros, and the
+ * status word).
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t V, d;
+  int32_t dtype;      /* NAT_F32 | NAT_BF16 */
+  float scale;
+  int32_t accumulate; /* gradient: 0 overwrite dtable, 1 add to it */
+  int32_t reserved;   /* set to 0 */
+} nat_embed_params;
+
+size_t nat_embed_workspace_bytes(const nat_embed_params* params /* host */, int64_t cap);
+int nat_embed_fwd(const nat_embed_params* params /* host */, const void* table, const int32_t* ids,
+                  const int32_t* sel_idx, const int32_t* n_rows, int64_t cap, void* x, void* stream);
+int nat_embed_bwd(const nat_embed_params* params /* host */, const int32_t* ids, const int32_t* sel_idx,
+                  const int32_t* n_rows, int64_t cap, const void* dx, float* dtable, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The heads' norms of queries and keys and the rotation by position, between the projection and the attention.
+ * For each head's row x of head_dim elements, of the token at position p:
+ *   n = x rstd w,   rstd = (mean(x^2) + eps)^-1/2           (w NULL: n = x)
+ *   out = rot_p(n): the pair (n_a, n_b) number i turns by the angle p inv_freq[i],
+ *     out_a = n_a cos - n_b sin,   out_b = n_b cos + n_a sin,
+ *     a = i, b = i + rot_dim / 2   or, with interleaved,   a = 2 i, b = 2 i + 1,    i < rot_dim / 2;
+ *   the elements from rot_dim on are not turned.
+ * Backward, for a gradient dout of out, with g = rot_{-p}(dout), xhat = x rstd:
+ *   dw = sum over the tokens and heads of g xhat,   u = g w,   dx = rstd (u - xhat mean(u xhat))    (w NULL: dx = g)
+ * q and k are done in one pass, with w_q and w_k float32 [head_dim] for all heads of each (both or neither).
+ * inv_freq float64 [rot_dim / 2] (any law; NULL where rot_dim = 0).  The angles are reduced in 64 bits and their sines and
+ * cosines, the norms and all sums are in 32.
+ * Positions: positions int32 [cap], or NULL: a row's distance from the start of its sequence in cu_seqlens int32 [B+1],
+ * ascending.  Rows: min(*n_rows, cap) (n_rows NULL: cap), and without positions no more than cu_seqlens[B]; rows at or
+ * after that are neither written nor read.
+ * q, dq [cap, n_heads, head_dim] with q_stride elements from a token to the next, heads contiguous; k, dk
+ * [cap, n_kv_heads, head_dim] with k_stride; q_out, dq_out with q_out_stride, k_out, dk_out with k_out_stride.  An
+ * output may lie on an input of the same token stride (q_out on q, dq on dq_out or q, and k alike); other overlaps
+ * are not allowed.  Without norms the backward pass does not read q and k (which may be NULL).
+ * head_dim a multiple of 8, at most 128; rot_dim a multiple of 16, at most head_dim; strides multiples of 8 elements, rows
+ * 16-byte aligned.  dw_q, dw_k float32 [head_dim], overwritten, summed in a fixed order.
+ * Mean squares are float32: magnitudes above 10^17 or, where eps does not cover them, below 10^-16 leave its range.
+ * workspace (backward with norms only): nat_qknorm_workspace_bytes(params, cap) bytes; calls that may run at the same
+ * time need one each.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t rot_dim;     /* elements of a head that turn, from its first on */
+  int32_t interleaved; /* 0: pairs (i, i + rot_dim / 2), 1: pairs (2 i, 2 i + 1) */
+  int32_t dtype;       /* NAT_F32 | NAT_BF16 */
+  float eps;
+  int32_t reserved;    /* set to 0 */
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride; /* elements from a token's row to the next */
+} nat_qknorm_params;
+
+size_t nat_qknorm_workspace_bytes(const nat_qknorm_params* params /* host */, int64_t cap);
+int nat_qknorm_fwd(const nat_qknorm_params* params /* host */, int32_t B, const int32_t* cu_seqlens,
+                   const int32_t* positions, const int32_t* n_rows, int64_t cap, const void* q, const void* k,
+                   const float* w_q, const float* w_k, const double* inv_freq, void* q_out, void* k_out, void* stream);
+int nat_qknorm_bwd(const nat_qknorm_params* params /* host */, int32_t B, const int32_t* cu_seqlens,
+                   const int32_t* positions, const int32_t* n_rows, int64_t cap, const void* q, const void* k,
+                   const float* w_q, const float* w_k, const double* inv_freq, const void* dq_out, const void* dk_out,
+                   void* dq, void* dk, float* dw_q, float* dw_k, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/* ---------------------------------------------------------------------------
  * Per-kernel timing of the bf16 loss kernels (a measurement aid of this library;
  * the paper has no counterpart).  Between nat_trace_begin() and nat_trace_end()
  * every tensor-core kernel launch made by the loss entry points is bracketed by

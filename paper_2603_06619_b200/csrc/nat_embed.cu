@@ -1,0 +1,585 @@
+// Embedding of packed tokens: the lookup, and the table's gradient by tokens sorted by id.
+//
+//   x_k = scale table[id_k]          dtable_v = scale sum_{k : id_k = v} dx_k
+//
+// Both are bound by HBM: the lookup reads the rows that occur and writes one a token, the gradient reads
+// one a token and writes the whole table in 32 bits.  For the gradient the pairs (id, k) are sorted by a stable radix
+// sort, so that the tokens of a table row stand together in ascending order, and every row of the table is written
+// once, by the threads that add up its tokens.  Nothing is added by atomics: the order of the sums is fixed.
+#include <initializer_list>
+
+#include "nat_common.cuh"
+#include "nat_rows.cuh"
+
+namespace nat {
+namespace embed {
+namespace {
+
+using rows::kChunk;
+using rows::kPairs;
+
+constexpr int kThreads = 256;
+constexpr int kTile = 4096;        // pairs a block sorts at a time
+constexpr int kWarps = kThreads / 32;
+constexpr int kRounds = kTile / kThreads;
+constexpr int kMaxDigits = 512;
+constexpr uint32_t kPiece = 128;   // sorted tokens of a piece; a table row with more is added up in pieces
+
+struct Rows {
+  const int32_t *ids, *sel_idx, *n_rows;
+  int64_t cap;
+  int32_t V;
+};
+
+// Positions are unsigned: a tile's end may lie behind 2^31.
+__device__ __forceinline__ uint32_t row_count(const Rows& r) {
+  return (uint32_t)(r.n_rows ? min((int64_t)max(*r.n_rows, 0), r.cap) : r.cap);
+}
+// The id of row k, V where it lies outside the table.
+__device__ __forceinline__ uint32_t row_id(const Rows& r, uint32_t k) {
+  const int32_t id = r.ids[r.sel_idx ? r.sel_idx[k] : k];
+  return (uint32_t)id < (uint32_t)r.V ? (uint32_t)id : (uint32_t)r.V;
+}
+
+// ------------------------------------------------------------------------- lookup
+// `tpr` threads (a power of two) share a row, a chunk of eight elements each at a time; kUnroll rows in flight.
+constexpr int kUnroll = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+lookup_kernel(const T* __restrict__ table, Rows r, T* __restrict__ x, int d, int tpr_log2, float scale) {
+  const uint32_t n = row_count(r);
+  const int rpb = kThreads >> tpr_log2, in_block = threadIdx.x >> tpr_log2;
+  const int first = (threadIdx.x & ((1 << tpr_log2) - 1)) * kChunk, stride = kChunk << tpr_log2;
+  const int64_t step = (int64_t)gridDim.x * rpb;
+  for (int64_t base = (int64_t)blockIdx.x * rpb + in_block; base < n; base += step * kUnroll) {
+    uint32_t id[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t k = base + u * step;
+      id[u] = k < n ? row_id(r, (uint32_t)k) : (uint32_t)r.V;
+    }
+    for (int c = first; c < d; c += stride) {
+      rows::Raw<T> raw[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        if (id[u] < (uint32_t)r.V) raw[u] = rows::load_raw(table + (int64_t)id[u] * d + c);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int64_t k = base + u * step;
+        if (k >= n) break;
+        float2 v[kPairs];
+        if (id[u] < (uint32_t)r.V) {
+          rows::widen(raw[u], v);
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], both(scale));
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) v[i] = both(__uint_as_float(0x7FC00000u));
+        }
+        rows::narrow(v, raw[u]);
+        rows::store_raw(x + k * d + c, raw[u]);
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------- sort
+// Stable sort by digits from the lowest up.  A block owns kTile consecutive pairs and a warp of it 512, in rounds
+// of 32, so that a pair's rank among those of its digit is: what earlier warps counted, what this warp counted in
+// earlier rounds, and the lanes below.
+struct Digit {
+  int shift, bits;
+  __device__ __forceinline__ int of(uint32_t key) const { return (int)(key >> shift) & ((1 << bits) - 1); }
+  __device__ __forceinline__ int count() const { return 1 << bits; }
+};
+
+__device__ __forceinline__ uint32_t slot_of(int round) {
+  return (threadIdx.x >> 5) * (kTile / kWarps) + round * 32 + (threadIdx.x & 31);
+}
+
+// rank[j] of the thread's pairs among their digit within the warp; `counts` [kWarps][digits] holds the warps'
+// totals afterwards.
+__device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint32_t valid, Digit digit, uint32_t* counts,
+                                           uint32_t (&rank)[kRounds]) {
+  const int lane = threadIdx.x & 31;
+  uint32_t* mine = counts + (threadIdx.x >> 5) * digit.count();
+  for (int i = threadIdx.x; i < kWarps * digit.count(); i += kThreads) counts[i] = 0u;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const bool in = slot_of(j) < valid;
+    const int g = in ? digit.of(key[j]) : -1;
+    const unsigned same = __match_any_sync(0xFFFFFFFFu, g);
+    const unsigned below = same & ((1u << lane) - 1u);
+    uint32_t before = 0u;
+    if (in) before = mine[g];
+    __syncwarp();
+    if (in && below == 0u) mine[g] = before + (uint32_t)__popc(same);
+    __syncwarp();
+    rank[j] = before + (uint32_t)__popc(below);
+  }
+  __syncthreads();
+}
+
+// counts[w][g] -> how many of digit g the warps before w hold; returns nothing, leaves the block's total of digit g
+// in total[g].
+__device__ __forceinline__ void across_warps(uint32_t* counts, uint32_t* total, int digits) {
+  for (int g = threadIdx.x; g < digits; g += kThreads) {
+    uint32_t run = 0u;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const uint32_t c = counts[w * digits + g];
+      counts[w * digits + g] = run;
+      run += c;
+    }
+    total[g] = run;
+  }
+  __syncthreads();
+}
+
+// total[0..digits) -> its exclusive prefix sums (digits <= kMaxDigits = 2 kThreads).
+__device__ __forceinline__ void prefix_digits(uint32_t* total, int digits) {
+  __shared__ uint32_t sums[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t a = 2 * threadIdx.x < digits ? total[2 * threadIdx.x] : 0u;
+  uint32_t b = 2 * threadIdx.x + 1 < digits ? total[2 * threadIdx.x + 1] : 0u;
+  uint32_t run = a + b;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+    if (lane >= o) run += left;
+  }
+  if (lane == 31) sums[warp] = run;
+  __syncthreads();
+  uint32_t before = run - (a + b);
+  for (int w = 0; w < warp; ++w) before += sums[w];
+  if (2 * threadIdx.x < digits) total[2 * threadIdx.x] = before;
+  if (2 * threadIdx.x + 1 < digits) total[2 * threadIdx.x + 1] = before + a;
+  __syncthreads();
+}
+
+// Up to kTile pairs: all passes in one block, the pairs in shared memory between them.
+__global__ void __launch_bounds__(kThreads)
+sort_small_kernel(Rows r, int passes, int bits, uint32_t* keys, uint32_t* vals) {
+  __shared__ uint32_t skey[kTile], counts[kWarps * kMaxDigits], total[kMaxDigits];
+  __shared__ uint16_t sval[kTile];
+  const uint32_t n = row_count(r);
+  uint32_t key[kRounds], val[kRounds], rank[kRounds];
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const uint32_t i = slot_of(j);
+    key[j] = i < n ? row_id(r, i) : 0u;
+    val[j] = i;
+  }
+  for (int p = 0; p < passes; ++p) {
+    const Digit digit{p * bits, bits};
+    warp_ranks(key, n, digit, counts, rank);
+    across_warps(counts, total, digit.count());
+    prefix_digits(total, digit.count());
+#pragma unroll
+    for (int j = 0; j < kRounds; ++j) {
+      if (slot_of(j) < n) {
+        const int g = digit.of(key[j]);
+        const uint32_t to = total[g] + counts[(threadIdx.x >> 5) * digit.count() + g] + rank[j];
+        skey[to] = key[j];
+        sval[to] = (uint16_t)val[j];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kRounds; ++j) {
+      const uint32_t i = slot_of(j);
+      if (i < n) {
+        key[j] = skey[i];
+        val[j] = sval[i];
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const uint32_t i = slot_of(j);
+    if (i < n) {
+      keys[i] = key[j];
+      vals[i] = val[j];
+    }
+  }
+}
+
+// How many pairs of each digit a block holds: hist [digits][blocks].
+__global__ void __launch_bounds__(kThreads)
+count_kernel(Rows r, const uint32_t* keys, Digit digit, uint32_t* hist) {
+  __shared__ uint32_t c[kMaxDigits];
+  const uint32_t n = row_count(r);
+  for (int g = threadIdx.x; g < digit.count(); g += kThreads) c[g] = 0u;
+  __syncthreads();
+  const uint32_t base = blockIdx.x * kTile;
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const uint32_t i = base + slot_of(j);
+    if (i < n) atomicAdd(&c[digit.of(keys ? keys[i] : row_id(r, i))], 1u);
+  }
+  __syncthreads();
+  for (int g = threadIdx.x; g < digit.count(); g += kThreads) hist[(int64_t)g * gridDim.x + blockIdx.x] = c[g];
+}
+
+// hist[g][.] -> its exclusive prefix sums, total[g]; a warp a digit.
+__global__ void __launch_bounds__(kThreads)
+prefix_kernel(uint32_t* hist, int blocks, int digits, uint32_t* total) {
+  const int g = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (g >= digits) return;
+  uint32_t before = 0u;
+  for (int base = 0; base < blocks; base += 32) {
+    const int i = base + lane;
+    const uint32_t c = i < blocks ? hist[(int64_t)g * blocks + i] : 0u;
+    uint32_t run = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+      if (lane >= o) run += left;
+    }
+    if (i < blocks) hist[(int64_t)g * blocks + i] = before + run - c;
+    before += __shfl_sync(0xFFFFFFFFu, run, 31);
+  }
+  if (lane == 0) total[g] = before;
+}
+
+__global__ void __launch_bounds__(kThreads)
+scatter_kernel(Rows r, const uint32_t* keys, const uint32_t* vals, Digit digit, const uint32_t* hist,
+               const uint32_t* totals, uint32_t* keys_out, uint32_t* vals_out) {
+  __shared__ uint32_t counts[kWarps * kMaxDigits], total[kMaxDigits];
+  const uint32_t n = row_count(r), base = blockIdx.x * kTile;
+  const int digits = digit.count();
+  if (base >= n) return;
+  uint32_t key[kRounds], rank[kRounds];
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const uint32_t i = base + slot_of(j);
+    key[j] = i < n ? (keys ? keys[i] : row_id(r, i)) : 0u;
+  }
+  warp_ranks(key, n - base, digit, counts, rank);
+  across_warps(counts, total, digits);
+  for (int g = threadIdx.x; g < digits; g += kThreads) total[g] = totals[g];
+  __syncthreads();
+  prefix_digits(total, digits);
+  for (int g = threadIdx.x; g < digits; g += kThreads) total[g] += hist[(int64_t)g * gridDim.x + blockIdx.x];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const uint32_t i = base + slot_of(j);
+    if (i < n) {
+      const int g = digit.of(key[j]);
+      const uint32_t to = total[g] + counts[(threadIdx.x >> 5) * digits + g] + rank[j];
+      keys_out[to] = key[j];
+      vals_out[to] = vals ? vals[i] : i;
+    }
+  }
+}
+
+// -------------------------------------------------------------------------- sums
+struct SumArgs {
+  Rows r;
+  const uint32_t *keys, *vals;  // sorted
+  const void* dx;
+  float *dtable, *partial;      // partial [2 tiles][d]
+  uint32_t* status;
+  int d, tpr_log2, rows_per_block;
+  int tiles;                    // blocks that add up pieces, before those that write rows of the table
+  float scale;
+  bool accumulate;
+};
+
+// First sorted position whose key is not below `key`.
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n, uint32_t key) {
+  uint32_t lo = 0u, hi = n;
+  while (lo < hi) {
+    const uint32_t mid = (lo + hi) >> 1;
+    if (keys[mid] < key) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+// Sum over the sorted tokens [lo, hi) of eight columns, in order.
+template <typename T>
+__device__ __forceinline__ void add_tokens(const SumArgs& a, uint32_t lo, uint32_t hi, int c, float2 (&sum)[kPairs]) {
+  const T* dx = (const T*)a.dx + c;
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) sum[i] = both(0.f);
+  uint32_t i = lo;
+  for (; i + 4 <= hi; i += 4) {
+    rows::Raw<T> raw[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) raw[u] = rows::load_raw(dx + (int64_t)a.vals[i + u] * a.d);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float2 v[kPairs];
+      rows::widen(raw[u], v);
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+    }
+  }
+  for (; i < hi; ++i) {
+    float2 v[kPairs];
+    rows::widen(rows::load_raw(dx + (int64_t)a.vals[i] * a.d), v);
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+  }
+}
+
+// Blocks [0, tiles): the piece of a table row with more than kPiece tokens that lies in a tile of kPiece sorted
+// positions.  A tile meets at most two such rows, one that began before it (slot 0) and one that begins in it and
+// goes on behind it (slot 1).  The blocks behind: rows of the table with up to kPiece tokens.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
+  __shared__ uint32_t start[33];
+  const uint32_t n = row_count(a.r);
+  const int tpr = 1 << a.tpr_log2, group = threadIdx.x >> a.tpr_log2, groups = kThreads >> a.tpr_log2;
+  const int first = (threadIdx.x & (tpr - 1)) * kChunk, stride = kChunk << a.tpr_log2;
+  if (blockIdx.x < (unsigned)a.tiles) {
+    const uint32_t t0 = blockIdx.x * kPiece, t1 = min(t0 + kPiece, n);
+    if (t0 >= n) return;
+    if (threadIdx.x < 4) {
+      const uint32_t key = a.keys[threadIdx.x < 2 ? t0 : t1 - 1];
+      start[threadIdx.x] = key == (uint32_t)a.r.V ? 0u : lower_bound(a.keys, n, key + (threadIdx.x & 1));
+    }
+    __syncthreads();
+    const uint32_t b0 = start[0], e0 = start[1], b1 = start[2], e1 = start[3];
+    for (int s = group; s < 2; s += groups) {
+      const uint32_t b = s == 0 ? b0 : b1, e = s == 0 ? e0 : e1;
+      if (e - b <= kPiece || (s == 0 ? b >= t0 : b < t0)) continue;
+      for (int c = first; c < a.d; c += stride) {
+        float2 sum[kPairs];
+        add_tokens<T>(a, max(b, t0), min(e, t1), c, sum);
+        rows::Raw<float> out;
+        rows::narrow(sum, out);
+        rows::store_raw(a.partial + (2 * (int64_t)blockIdx.x + s) * a.d + c, out);
+      }
+    }
+    return;
+  }
+  const int v0 = (blockIdx.x - a.tiles) * a.rows_per_block, count = min(a.rows_per_block, a.r.V - v0);
+  if (threadIdx.x <= count) start[threadIdx.x] = lower_bound(a.keys, n, (uint32_t)(v0 + threadIdx.x));
+  if (v0 == 0 && threadIdx.x == 0) *a.status = n > 0 && a.keys[n - 1] == (uint32_t)a.r.V ? NAT_DEV_BAD_TARGET : 0u;
+  __syncthreads();
+  for (int i = group; i < count; i += groups) {
+    const uint32_t lo = start[i], hi = start[i + 1];
+    if (hi - lo > kPiece || (a.accumulate && hi == lo)) continue;
+    float* row = a.dtable + (int64_t)(v0 + i) * a.d;
+    for (int c = first; c < a.d; c += stride) {
+      float2 sum[kPairs];
+      add_tokens<T>(a, lo, hi, c, sum);
+      rows::Raw<float> out;
+      float2 old[kPairs];
+      if (a.accumulate) rows::widen(rows::load_raw(row + c), old);
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        sum[j] = mul2(sum[j], both(a.scale));
+        if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+      }
+      rows::narrow(sum, out);
+      rows::store_raw(row + c, out);
+    }
+  }
+}
+
+// Joins the pieces of the row that begins in tile blockIdx.x and goes on behind it: the warps take runs of
+// pieces, 256 columns at a time, and their sums are added in the runs' order.
+__global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
+  __shared__ float2 sums[kWarps][32][kPairs];
+  __shared__ uint32_t bounds[2];
+  const uint32_t n = row_count(a.r), t0 = blockIdx.x * kPiece, t1 = min(t0 + kPiece, n);
+  if (t0 >= n) return;
+  const uint32_t key = a.keys[t1 - 1];
+  if (key == (uint32_t)a.r.V) return;
+  if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(a.keys, n, key + threadIdx.x);
+  __syncthreads();
+  const uint32_t b = bounds[0], e = bounds[1];
+  if (e - b <= kPiece || b < t0) return;
+  const int pieces = (int)((e - 1) / kPiece - blockIdx.x + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (blockIdx.y * 32 + lane) * kChunk;
+  const int per = (pieces + kWarps - 1) / kWarps, lo = warp * per, hi = min(lo + per, pieces);
+  float2 sum[kPairs];
+#pragma unroll
+  for (int j = 0; j < kPairs; ++j) sum[j] = both(0.f);
+  if (c < a.d) {
+#pragma unroll 4
+    for (int p = lo; p < hi; ++p) {
+      // the row's first piece is the second slot of its tile, the others the first slots of theirs
+      const int64_t slot = 2 * ((int64_t)blockIdx.x + p) + (p == 0 ? 1 : 0);
+      float2 v[kPairs];
+      rows::widen(rows::load_raw(a.partial + slot * a.d + c), v);
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kPairs; ++j) sums[warp][lane][j] = sum[j];
+  __syncthreads();
+  if (warp != 0 || c >= a.d) return;
+  float* at = a.dtable + (int64_t)key * a.d + c;
+  float2 old[kPairs];
+  if (a.accumulate) rows::widen(rows::load_raw(at), old);
+  rows::Raw<float> out;
+#pragma unroll
+  for (int j = 0; j < kPairs; ++j) {
+    for (int w = 1; w < kWarps; ++w) sum[j] = add2(sum[j], sums[w][lane][j]);
+    sum[j] = mul2(sum[j], both(a.scale));
+    if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+  }
+  rows::narrow(sum, out);
+  rows::store_raw(at, out);
+}
+
+// --------------------------------------------------------------------------- host
+struct Layout {
+  int passes, bits, blocks, tiles;
+  size_t keys[2], vals[2], hist, total, partial, bytes;
+};
+
+Layout layout(const nat_embed_params& p, int64_t cap) {
+  Layout l;
+  int b = 1;
+  while ((p.V >> b) != 0) ++b;  // ids 0..V, V for those outside
+  l.passes = (b + 8) / 9;
+  l.bits = (b + l.passes - 1) / l.passes;
+  l.blocks = (int)((cap + kTile - 1) / kTile);
+  l.tiles = cap > kPiece ? (int)((cap + kPiece - 1) / kPiece) : 0;
+  size_t at = 256;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at = align_up(at + bytes, 256);
+    return o;
+  };
+  for (int i = 0; i < 2; ++i) {
+    l.keys[i] = take(4 * (size_t)cap);
+    l.vals[i] = take(4 * (size_t)cap);
+  }
+  l.hist = take(4 * (size_t)kMaxDigits * l.blocks);
+  l.total = take(4 * kMaxDigits);
+  l.partial = take(2 * (size_t)l.tiles * p.d * sizeof(float));
+  l.bytes = at;
+  return l;
+}
+
+int check(const char* who, const nat_embed_params* p, int64_t cap) {
+  if (!p) return fail(NAT_ERR_INVALID_ARG, "%s: params is null", who);
+  if (p->dtype != NAT_F32 && p->dtype != NAT_BF16)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, p->dtype);
+  if (p->V <= 0 || p->d <= 0 || cap < 0 || cap > 0x7FFFFFFFll)
+    return fail(NAT_ERR_INVALID_ARG, "%s: V and d must be positive, cap in [0, 2^31)", who);
+  if (p->d % kChunk != 0 || p->d > 65536 || p->V > (1 << 30))
+    return fail(NAT_ERR_UNSUPPORTED, "%s: d must be a multiple of 8, at most 65536, and V at most 2^30 (d = %d, V = %d)",
+                who, p->d, p->V);
+  if (!(p->scale - p->scale == 0.f)) return fail(NAT_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  return NAT_OK;
+}
+
+int check_pointers(const char* who, std::initializer_list<const void*> needed, std::initializer_list<const void*> wide,
+                   std::initializer_list<const void*> words) {
+  for (const void* q : needed)
+    if (!q) return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
+  for (const void* q : wide)
+    if ((uintptr_t)q & 15u) return fail(NAT_ERR_INVALID_ARG, "%s: matrices must be 16-byte aligned", who);
+  for (const void* q : words)
+    if ((uintptr_t)q & 3u) return fail(NAT_ERR_INVALID_ARG, "%s: ids, sel_idx and n_rows must be 4-byte aligned", who);
+  return NAT_OK;
+}
+
+// Threads that share a row of d elements, as a power of two.
+int threads_log2(int d) {
+  int t = 0;
+  while ((kChunk << t) < d && (1 << t) < kThreads) ++t;
+  return t;
+}
+
+template <typename T>
+int fwd(const nat_embed_params& p, const void* table, const Rows& r, void* x, cudaStream_t stream) {
+  const int tpr_log2 = threads_log2(p.d), rpb = kThreads >> tpr_log2;
+  const int64_t want = (r.cap + rpb - 1) / rpb;
+  lookup_kernel<T><<<(unsigned)min(want, (int64_t)148 * 8 * 8), kThreads, 0, stream>>>((const T*)table, r, (T*)x, p.d,
+                                                                                      tpr_log2, p.scale);
+  NAT_LAUNCH_CHECK("embed_lookup");
+  return NAT_OK;
+}
+
+template <typename T>
+int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable, void* workspace, const Layout& l,
+        cudaStream_t stream) {
+  char* ws = (char*)workspace;
+  auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(ws + o); };
+  int src = 0;
+  if (r.cap <= kTile) {
+    sort_small_kernel<<<1, kThreads, 0, stream>>>(r, l.passes, l.bits, at(l.keys[0]), at(l.vals[0]));
+    NAT_LAUNCH_CHECK("embed_sort_small");
+  } else {
+    for (int pass = 0; pass < l.passes; ++pass) {
+      const Digit digit{pass * l.bits, l.bits};
+      const uint32_t* keys = pass ? at(l.keys[src]) : nullptr;
+      const uint32_t* vals = pass ? at(l.vals[src]) : nullptr;
+      const int dst = pass ? src ^ 1 : 0;
+      count_kernel<<<l.blocks, kThreads, 0, stream>>>(r, keys, digit, at(l.hist));
+      NAT_LAUNCH_CHECK("embed_count");
+      prefix_kernel<<<((1 << l.bits) + kWarps - 1) / kWarps, kThreads, 0, stream>>>(at(l.hist), l.blocks, 1 << l.bits,
+                                                                                   at(l.total));
+      NAT_LAUNCH_CHECK("embed_prefix");
+      scatter_kernel<<<l.blocks, kThreads, 0, stream>>>(r, keys, vals, digit, at(l.hist), at(l.total), at(l.keys[dst]),
+                                                       at(l.vals[dst]));
+      NAT_LAUNCH_CHECK("embed_scatter");
+      src = dst;
+    }
+  }
+  SumArgs a{r, at(l.keys[src]), at(l.vals[src]), dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), 32,
+            l.tiles, p.scale, p.accumulate != 0};
+  while (a.rows_per_block > 1 && p.V / a.rows_per_block < 148 * 8) a.rows_per_block >>= 1;
+  sum_kernel<T><<<(unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block), kThreads, 0, stream>>>(a);
+  NAT_LAUNCH_CHECK("embed_sum");
+  if (l.tiles > 0) {
+    join_kernel<<<dim3((unsigned)l.tiles, (unsigned)((p.d + 255) / 256)), kThreads, 0, stream>>>(a);
+    NAT_LAUNCH_CHECK("embed_join");
+  }
+  return NAT_OK;
+}
+
+}  // namespace
+}  // namespace embed
+}  // namespace nat
+
+extern "C" {
+
+size_t nat_embed_workspace_bytes(const nat_embed_params* p, int64_t cap) {
+  if (nat::embed::check("nat_embed_workspace_bytes", p, cap) != NAT_OK) return 0;
+  return nat::embed::layout(*p, cap).bytes;
+}
+
+int nat_embed_fwd(const nat_embed_params* p, const void* table, const int32_t* ids, const int32_t* sel_idx,
+                  const int32_t* n_rows, int64_t cap, void* x, void* stream) {
+  const char* who = "nat_embed_fwd";
+  int s = nat::embed::check(who, p, cap);
+  if (s != NAT_OK || cap == 0) return s;
+  s = nat::embed::check_pointers(who, {table, ids, x}, {table, x}, {ids, sel_idx, n_rows});
+  if (s != NAT_OK) return s;
+  const nat::embed::Rows r{ids, sel_idx, n_rows, cap, p->V};
+  return p->dtype == NAT_F32 ? nat::embed::fwd<float>(*p, table, r, x, (cudaStream_t)stream)
+                             : nat::embed::fwd<__nv_bfloat16>(*p, table, r, x, (cudaStream_t)stream);
+}
+
+int nat_embed_bwd(const nat_embed_params* p, const int32_t* ids, const int32_t* sel_idx, const int32_t* n_rows,
+                  int64_t cap, const void* dx, float* dtable, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "nat_embed_bwd";
+  int s = nat::embed::check(who, p, cap);
+  if (s != NAT_OK) return s;
+  s = cap > 0 ? nat::embed::check_pointers(who, {ids, dx, dtable}, {dx, dtable}, {ids, sel_idx, n_rows})
+              : nat::embed::check_pointers(who, {dtable}, {dtable}, {n_rows});
+  if (s != NAT_OK) return s;
+  const nat::embed::Layout l = nat::embed::layout(*p, cap);
+  if (!workspace || workspace_bytes < l.bytes)
+    return nat::fail(NAT_ERR_CAPACITY, "%s: workspace too small (%zu < %zu)", who, workspace_bytes, l.bytes);
+  if ((uintptr_t)workspace & 255u)
+    return nat::fail(NAT_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+  const nat::embed::Rows r{ids, sel_idx, n_rows, cap, p->V};
+  return p->dtype == NAT_F32 ? nat::embed::bwd<float>(*p, r, dx, dtable, workspace, l, (cudaStream_t)stream)
+                             : nat::embed::bwd<__nv_bfloat16>(*p, r, dx, dtable, workspace, l, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,463 @@
+// The heads' norms of queries and keys with the rotation by position, forward and backward.
+//
+//   n = x rstd w,  out = rot_p(n)          g = rot_{-p}(dout),  dx = rstd (g w - xhat mean(g w xhat)),  dw = sum g xhat
+//
+// Bound by HBM: one pass over the rows.  LANES lanes share a head's row, two chunks of eight elements each, chosen so
+// that both members of a rotated pair are in one lane; a warp owns a token and walks its heads, so that the angles'
+// sines and cosines are found once a token, each by one of the warp's groups of lanes, and dealt to the others.  A warp
+// takes a run of consecutive tokens and finds its first token's sequence once.
+#include <initializer_list>
+
+#include "nat_common.cuh"
+#include "nat_rows.cuh"
+
+namespace nat {
+namespace qknorm {
+namespace {
+
+using rows::kChunk;
+using rows::kPairs;
+using rows::Raw;
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxDim = 128;
+
+struct Args {
+  nat_qknorm_params p;
+  int32_t B;
+  const int32_t *cu, *positions, *n_rows;
+  int64_t cap;
+  const void *q, *k;
+  const float *w_q, *w_k;
+  const double* inv_freq;
+  const void *dq_out, *dk_out;   // backward
+  void *q_to, *k_to;             // q_out and k_out, or dq and dk
+  float* partial;                // backward with norms: [blocks][2][head_dim]
+};
+
+__device__ __forceinline__ int64_t row_count(const Args& a) {
+  int64_t n = a.n_rows ? min((int64_t)max(__ldg(a.n_rows), 0), a.cap) : a.cap;
+  if (!a.positions) n = min(n, (int64_t)max(__ldg(a.cu + a.B), 0));
+  return n;
+}
+
+// The last sequence that begins at or before row n (0 where none does).
+__device__ __forceinline__ int owner(const int32_t* cu, int B, int64_t n) {
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)__ldg(cu + mid) <= n) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// A lane's two chunks of a head's row and the pairs that they hold.
+struct Slot {
+  int a, b;        // first elements; b < 0: none
+  bool turns, in;  // the lane has a part of the row at all
+};
+__device__ __forceinline__ Slot slot_of(const nat_qknorm_params& p, int lane) {
+  const int r16 = p.rot_dim / 16, rest = (p.head_dim - p.rot_dim) / kChunk;
+  if (lane < r16) return {lane * kChunk, (lane + r16) * kChunk, true, true};
+  const int j = 2 * (lane - r16);
+  if (j >= rest) return {0, -1, false, false};
+  return {p.rot_dim + j * kChunk, j + 1 < rest ? p.rot_dim + (j + 1) * kChunk : -1, false, true};
+}
+// Number i of the angle of the lane's e-th pair.
+__device__ __forceinline__ int angle_of(const nat_qknorm_params& p, const Slot& s, int e) {
+  if (!p.interleaved) return s.a + e;
+  return e < 4 ? s.a / 2 + e : s.b / 2 + e - 4;
+}
+
+// Turns a lane's eight pairs; sin < 0 of the angle turns back.
+__device__ __forceinline__ void turn(bool interleaved, float2 (&a)[kPairs], float2 (&b)[kPairs], const float (&c)[8],
+                                     const float (&s)[8]) {
+  auto one = [](float& x, float& y, float cs, float sn) {
+    const float t = fmaf(x, cs, -(y * sn));
+    y = fmaf(y, cs, x * sn);
+    x = t;
+  };
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    if (interleaved) {
+      one(a[i].x, a[i].y, c[i], s[i]);
+      one(b[i].x, b[i].y, c[4 + i], s[4 + i]);
+    } else {
+      one(a[i].x, b[i].x, c[2 * i], s[2 * i]);
+      one(a[i].y, b[i].y, c[2 * i + 1], s[2 * i + 1]);
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void load(const T* row, const Slot& s, bool on, Raw<T>& a, Raw<T>& b) {
+  a = b = rows::zero_raw<T>();
+  if (on && s.in) a = rows::load_raw(row + s.a);
+  if (on && s.in && s.b >= 0) b = rows::load_raw(row + s.b);
+}
+template <typename T>
+__device__ __forceinline__ void store(T* row, const Slot& s, bool on, const float2 (&a)[kPairs], const float2 (&b)[kPairs]) {
+  Raw<T> r;
+  if (on && s.in) {
+    rows::narrow(a, r);
+    rows::store_raw(row + s.a, r);
+  }
+  if (on && s.in && s.b >= 0) {
+    rows::narrow(b, r);
+    rows::store_raw(row + s.b, r);
+  }
+}
+
+__device__ __forceinline__ float squares(const float2 (&a)[kPairs], float sum) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) sum = fmaf(a[i].x, a[i].x, fmaf(a[i].y, a[i].y, sum));
+  return sum;
+}
+__device__ __forceinline__ float products(const float2 (&a)[kPairs], const float2 (&b)[kPairs], float sum) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) sum = fmaf(a[i].x, b[i].x, fmaf(a[i].y, b[i].y, sum));
+  return sum;
+}
+template <int LANES>
+__device__ __forceinline__ float over_row(float x) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  return x;
+}
+
+__device__ __forceinline__ void read8(const float* w, float2 (&x)[kPairs]) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) x[i] = *reinterpret_cast<const float2*>(w + 2 * i);
+}
+
+// One kind of heads (queries or keys) of a token.
+template <typename T, int LANES, bool BWD, bool NORM>
+__device__ __forceinline__ void heads(const Args& args, const Slot& slot, int group, int count, const T* x, const T* dout,
+                                      T* to, const float* w, const float (&c)[8], const float (&s)[8],
+                                      float2 (&dw)[2][kPairs]) {
+  constexpr int kGroups = 32 / LANES, kUnroll = 2;
+  const int D = args.p.head_dim;
+  const float inv_d = 1.f / (float)D;
+  for (int h0 = 0; h0 < count; h0 += kGroups * kUnroll) {
+    Raw<T> xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = h0 + u * kGroups + group;
+      if (!BWD || NORM) load<T>(x + (int64_t)h * D, slot, h < count, xa[u], xb[u]);
+      if (BWD) load<T>(dout + (int64_t)h * D, slot, h < count, ga[u], gb[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = h0 + u * kGroups + group;
+      float2 a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
+      if (NORM) {
+        read8(w + slot.a, wa);
+        read8(w + max(slot.b, 0), wb);
+      }
+      if (!BWD) {
+        rows::widen(xa[u], a);
+        rows::widen(xb[u], b);
+        if (NORM) {
+          const float rstd = rsqrtf(fmaf(over_row<LANES>(squares(a, squares(b, 0.f))), inv_d, args.p.eps));
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            a[i] = mul2(mul2(a[i], both(rstd)), wa[i]);
+            b[i] = mul2(mul2(b[i], both(rstd)), wb[i]);
+          }
+        }
+        if (slot.turns) turn(args.p.interleaved, a, b, c, s);
+      } else {
+        rows::widen(ga[u], a);
+        rows::widen(gb[u], b);
+        if (slot.turns) turn(args.p.interleaved, a, b, c, s);
+        if (NORM) {
+          float2 p[kPairs], q[kPairs];
+          rows::widen(xa[u], p);
+          rows::widen(xb[u], q);
+          const float rstd = rsqrtf(fmaf(over_row<LANES>(squares(p, squares(q, 0.f))), inv_d, args.p.eps));
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            p[i] = mul2(p[i], both(rstd));
+            q[i] = mul2(q[i], both(rstd));
+            dw[0][i] = fma2(a[i], p[i], dw[0][i]);
+            dw[1][i] = fma2(b[i], q[i], dw[1][i]);
+            a[i] = mul2(a[i], wa[i]);
+            b[i] = mul2(b[i], wb[i]);
+          }
+          const float mean = over_row<LANES>(products(a, p, products(b, q, 0.f))) * inv_d;
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            a[i] = mul2(both(rstd), fma2(p[i], both(-mean), a[i]));
+            b[i] = mul2(both(rstd), fma2(q[i], both(-mean), b[i]));
+          }
+        }
+      }
+      store<T>(to + (int64_t)h * D, slot, h < count, a, b);
+    }
+  }
+}
+
+template <typename T, int LANES, bool BWD, bool NORM>
+__global__ void __launch_bounds__(kThreads) qknorm_kernel(const Args args) {
+  constexpr int kGroups = 32 / LANES;
+  constexpr int kAngles = kGroups >= 8 ? 1 : 8 / kGroups;  // that a lane finds
+  __shared__ float weights[2][kMaxDim];
+  __shared__ float sums[kWarps][2][kMaxDim];
+  const nat_qknorm_params& p = args.p;
+  const int D = p.head_dim, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = lane / LANES;
+  const Slot slot = slot_of(p, lane & (LANES - 1));
+  if (NORM) {
+    for (int i = threadIdx.x; i < 2 * kMaxDim; i += kThreads)
+      weights[i / kMaxDim][i % kMaxDim] = i % kMaxDim < D ? (i < kMaxDim ? args.w_q : args.w_k)[i % kMaxDim] : 0.f;
+    __syncthreads();
+  }
+  const int64_t n = row_count(args);
+  const int64_t total = (int64_t)gridDim.x * kWarps, mine = (int64_t)blockIdx.x * kWarps + warp;
+  const int64_t each = n / total, more = n % total;
+  const int64_t begin = mine * each + min(mine, more), end = begin + each + (mine < more ? 1 : 0);
+
+  float2 dwq[2][kPairs], dwk[2][kPairs];
+  if (BWD && NORM) {
+#pragma unroll
+    for (int i = 0; i < 2 * kPairs; ++i) dwq[i / kPairs][i % kPairs] = dwk[i / kPairs][i % kPairs] = both(0.f);
+  }
+  // turns of a full circle a position, of the angles that this lane finds
+  double freq[kAngles];
+#pragma unroll
+  for (int j = 0; j < kAngles; ++j) {
+    const int e = j * kGroups + group;
+    freq[j] = slot.turns && e < 8 ? __ldg(args.inv_freq + angle_of(p, slot, e)) * 0.15915494309189533577 : 0.0;
+  }
+  int seq = 0;
+  int64_t seq_lo = 0, seq_hi = 0;
+  if (!args.positions && begin < end) {
+    seq = owner(args.cu, args.B, begin);
+    seq_lo = __ldg(args.cu + seq);
+    seq_hi = __ldg(args.cu + seq + 1);
+  }
+  for (int64_t t = begin; t < end; ++t) {
+    int64_t pos;
+    if (args.positions) {
+      pos = __ldg(args.positions + t);
+    } else {
+      while (t >= seq_hi && seq + 1 < args.B) {
+        ++seq;
+        seq_lo = seq_hi;
+        seq_hi = __ldg(args.cu + seq + 1);
+      }
+      pos = t - seq_lo;
+    }
+    float c[8], s[8];
+    {
+      float cj[kAngles], sj[kAngles];
+#pragma unroll
+      for (int j = 0; j < kAngles; ++j) {
+        const double x = freq[j] * (double)pos;
+        sincospif((float)(2.0 * (x - rint(x))), &sj[j], &cj[j]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int from = (e % kGroups) * LANES + (lane & (LANES - 1));
+        c[e] = __shfl_sync(0xFFFFFFFFu, cj[e / kGroups], from);
+        s[e] = __shfl_sync(0xFFFFFFFFu, sj[e / kGroups], from);
+        if (BWD) s[e] = -s[e];
+      }
+    }
+    heads<T, LANES, BWD, NORM>(args, slot, group, p.n_heads, (const T*)args.q + t * p.q_stride,
+                               (const T*)args.dq_out + t * p.q_out_stride,
+                               (T*)args.q_to + t * (BWD ? p.q_stride : p.q_out_stride), weights[0], c, s, dwq);
+    heads<T, LANES, BWD, NORM>(args, slot, group, p.n_kv_heads, (const T*)args.k + t * p.k_stride,
+                               (const T*)args.dk_out + t * p.k_out_stride,
+                               (T*)args.k_to + t * (BWD ? p.k_stride : p.k_out_stride), weights[1], c, s, dwk);
+  }
+  if (BWD && NORM) {
+    // over the groups of the warp, over the warps of the block
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      float2(&dw)[2][kPairs] = kind == 0 ? dwq : dwk;
+#pragma unroll
+      for (int i = 0; i < 2 * kPairs; ++i) {
+        float2& v = dw[i / kPairs][i % kPairs];
+#pragma unroll
+        for (int o = LANES; o < 32; o <<= 1) {
+          v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+          v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+        }
+        const int at = i < kPairs ? slot.a + 2 * i : slot.b + 2 * (i - kPairs);
+        if (group == 0 && slot.in && (i < kPairs || slot.b >= 0))
+          *reinterpret_cast<float2*>(&sums[warp][kind][at]) = v;
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) v += sums[w][i / D][i % D];
+      args.partial[(int64_t)blockIdx.x * 2 * D + i] = v;
+    }
+  }
+}
+
+// Adds the blocks' sums in their order: a column a warp, 32 runs of blocks.
+__global__ void __launch_bounds__(kThreads)
+weights_kernel(const float* partial, int blocks, int D, float* dw_q, float* dw_k) {
+  const int i = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (i >= 2 * D) return;
+  const int per = (blocks + 31) / 32;
+  float v = 0.f;
+  for (int b = lane * per; b < min((lane + 1) * per, blocks); ++b) v += partial[(int64_t)b * 2 * D + i];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  if (lane == 0) (i < D ? dw_q : dw_k)[i % D] = v;
+}
+
+// --------------------------------------------------------------------------- host
+// Lanes of a head's row: two chunks each.
+int lanes_of(const nat_qknorm_params& p) {
+  const int slots = p.rot_dim / 16 + ((p.head_dim - p.rot_dim) / kChunk + 1) / 2;
+  return slots > 4 ? 8 : slots > 2 ? 4 : slots > 1 ? 2 : 1;
+}
+
+int blocks_of(int64_t cap, bool bwd) {
+  const int64_t want = (cap + kWarps - 1) / kWarps, most = 148 * (bwd ? 2 : 4);
+  return (int)(want < most ? want : most);
+}
+
+int check(const char* who, const nat_qknorm_params* p, int64_t cap) {
+  if (!p) return fail(NAT_ERR_INVALID_ARG, "%s: params is null", who);
+  if (p->dtype != NAT_F32 && p->dtype != NAT_BF16)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, p->dtype);
+  if (p->n_heads <= 0 || p->n_kv_heads <= 0 || p->head_dim <= 0 || p->rot_dim < 0 || cap < 0 || cap > 0x7FFFFFFFll)
+    return fail(NAT_ERR_INVALID_ARG,
+                "%s: head counts and head_dim must be positive, rot_dim >= 0, cap in [0, 2^31)", who);
+  if (p->head_dim % kChunk != 0 || p->head_dim > kMaxDim)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: head_dim must be a multiple of 8, at most 128 (head_dim = %d)", who,
+                p->head_dim);
+  if (p->rot_dim > p->head_dim)
+    return fail(NAT_ERR_INVALID_ARG, "%s: rot_dim exceeds head_dim", who);
+  if (p->rot_dim % 16 != 0)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: rot_dim must be a multiple of 16 (rot_dim = %d)", who, p->rot_dim);
+  if (p->interleaved != 0 && p->interleaved != 1)
+    return fail(NAT_ERR_INVALID_ARG, "%s: interleaved must be 0 or 1", who);
+  if (!(p->eps >= 0.f) || p->eps - p->eps != 0.f)
+    return fail(NAT_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", who);
+  const int64_t strides[4] = {p->q_stride, p->q_out_stride, p->k_stride, p->k_out_stride};
+  for (int i = 0; i < 4; ++i) {
+    const int64_t width = (int64_t)(i < 2 ? p->n_heads : p->n_kv_heads) * p->head_dim;
+    if (strides[i] < width)
+      return fail(NAT_ERR_INVALID_ARG, "%s: a token's row (stride %lld) is shorter than its heads (%lld)", who,
+                  (long long)strides[i], (long long)width);
+    if (strides[i] % kChunk != 0 || strides[i] >= (1ll << 31))
+      return fail(NAT_ERR_UNSUPPORTED, "%s: strides must be multiples of 8 elements, below 2^31", who);
+  }
+  return NAT_OK;
+}
+
+int check_call(const char* who, const Args& a, std::initializer_list<const void*> matrices) {
+  if (!a.positions && (!a.cu || a.B <= 0))
+    return fail(NAT_ERR_INVALID_ARG, "%s: needs positions, or cu_seqlens of B > 0 sequences", who);
+  if ((a.w_q == nullptr) != (a.w_k == nullptr))
+    return fail(NAT_ERR_INVALID_ARG, "%s: w_q and w_k come together", who);
+  if (a.p.rot_dim > 0 && !a.inv_freq) return fail(NAT_ERR_INVALID_ARG, "%s: inv_freq is null", who);
+  for (const void* m : matrices) {
+    if (!m) return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
+    if ((uintptr_t)m & 15u) return fail(NAT_ERR_INVALID_ARG, "%s: rows must be 16-byte aligned", who);
+  }
+  if (((uintptr_t)a.cu | (uintptr_t)a.positions | (uintptr_t)a.n_rows | (uintptr_t)a.w_q | (uintptr_t)a.w_k) & 3u ||
+      (uintptr_t)a.inv_freq & 7u)
+    return fail(NAT_ERR_INVALID_ARG, "%s: a vector is not aligned to its type", who);
+  return NAT_OK;
+}
+
+template <typename T, int LANES, bool BWD>
+void launch_lanes(const Args& a, int blocks, cudaStream_t stream) {
+  if (a.w_q)
+    qknorm_kernel<T, LANES, BWD, true><<<blocks, kThreads, 0, stream>>>(a);
+  else
+    qknorm_kernel<T, LANES, BWD, false><<<blocks, kThreads, 0, stream>>>(a);
+}
+
+template <typename T, bool BWD>
+int launch(const Args& a, cudaStream_t stream) {
+  const int blocks = blocks_of(a.cap, BWD);
+  switch (lanes_of(a.p)) {
+    case 8: launch_lanes<T, 8, BWD>(a, blocks, stream); break;
+    case 4: launch_lanes<T, 4, BWD>(a, blocks, stream); break;
+    case 2: launch_lanes<T, 2, BWD>(a, blocks, stream); break;
+    default: launch_lanes<T, 1, BWD>(a, blocks, stream);
+  }
+  NAT_LAUNCH_CHECK("qknorm");
+  return NAT_OK;
+}
+
+size_t workspace_bytes_of(const nat_qknorm_params& p, int64_t cap) {
+  return 256 + align_up((size_t)blocks_of(cap, true) * 2 * p.head_dim * sizeof(float), 256);
+}
+
+}  // namespace
+}  // namespace qknorm
+}  // namespace nat
+
+extern "C" {
+
+size_t nat_qknorm_workspace_bytes(const nat_qknorm_params* p, int64_t cap) {
+  if (nat::qknorm::check("nat_qknorm_workspace_bytes", p, cap) != NAT_OK) return 0;
+  return nat::qknorm::workspace_bytes_of(*p, cap);
+}
+
+int nat_qknorm_fwd(const nat_qknorm_params* p, int32_t B, const int32_t* cu_seqlens, const int32_t* positions,
+                   const int32_t* n_rows, int64_t cap, const void* q, const void* k, const float* w_q,
+                   const float* w_k, const double* inv_freq, void* q_out, void* k_out, void* stream) {
+  const char* who = "nat_qknorm_fwd";
+  int s = nat::qknorm::check(who, p, cap);
+  if (s != NAT_OK || cap == 0) return s;
+  nat::qknorm::Args a{};
+  a.p = *p; a.B = B; a.cu = cu_seqlens; a.positions = positions; a.n_rows = n_rows; a.cap = cap; a.q = q; a.k = k;
+  a.w_q = w_q; a.w_k = w_k; a.inv_freq = inv_freq; a.q_to = q_out; a.k_to = k_out;
+  s = nat::qknorm::check_call(who, a, {q, k, q_out, k_out});
+  if (s != NAT_OK) return s;
+  return p->dtype == NAT_F32 ? nat::qknorm::launch<float, false>(a, (cudaStream_t)stream)
+                             : nat::qknorm::launch<__nv_bfloat16, false>(a, (cudaStream_t)stream);
+}
+
+int nat_qknorm_bwd(const nat_qknorm_params* p, int32_t B, const int32_t* cu_seqlens, const int32_t* positions,
+                   const int32_t* n_rows, int64_t cap, const void* q, const void* k, const float* w_q,
+                   const float* w_k, const double* inv_freq, const void* dq_out, const void* dk_out, void* dq,
+                   void* dk, float* dw_q, float* dw_k, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "nat_qknorm_bwd";
+  int s = nat::qknorm::check(who, p, cap);
+  if (s != NAT_OK) return s;
+  nat::qknorm::Args a{};
+  a.p = *p; a.B = B; a.cu = cu_seqlens; a.positions = positions; a.n_rows = n_rows; a.cap = cap; a.q = q; a.k = k;
+  a.w_q = w_q; a.w_k = w_k; a.inv_freq = inv_freq; a.dq_out = dq_out; a.dk_out = dk_out; a.q_to = dq; a.k_to = dk;
+  if (cap > 0)
+    s = w_q ? nat::qknorm::check_call(who, a, {q, k, dq_out, dk_out, dq, dk})
+            : nat::qknorm::check_call(who, a, {dq_out, dk_out, dq, dk});
+  if (s != NAT_OK) return s;
+  if (w_q) {
+    if (!dw_q || !dw_k) return nat::fail(NAT_ERR_INVALID_ARG, "%s: null gradient", who);
+    if (((uintptr_t)dw_q | (uintptr_t)dw_k) & 3u)
+      return nat::fail(NAT_ERR_INVALID_ARG, "%s: a vector is not aligned to its type", who);
+    const size_t need = nat::qknorm::workspace_bytes_of(*p, cap);
+    if (!workspace || workspace_bytes < need)
+      return nat::fail(NAT_ERR_CAPACITY, "%s: workspace too small (%zu < %zu)", who, workspace_bytes, need);
+    if ((uintptr_t)workspace & 255u)
+      return nat::fail(NAT_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+    a.partial = (float*)((char*)workspace + 256);
+  }
+  cudaStream_t st = (cudaStream_t)stream;
+  if (cap > 0) {
+    s = p->dtype == NAT_F32 ? nat::qknorm::launch<float, true>(a, st) : nat::qknorm::launch<__nv_bfloat16, true>(a, st);
+    if (s != NAT_OK) return s;
+  }
+  if (w_q) {
+    using nat::qknorm::kWarps;
+    nat::qknorm::weights_kernel<<<(2 * p->head_dim + kWarps - 1) / kWarps, nat::qknorm::kThreads, 0, st>>>(
+        a.partial, nat::qknorm::blocks_of(cap, true), p->head_dim, dw_q, dw_k);
+    NAT_LAUNCH_CHECK("qknorm_weights");
+  }
+  return NAT_OK;
+}
+
+}  // extern "C"

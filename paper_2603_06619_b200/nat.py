@@ -27,7 +27,8 @@ SYMBOLS = (
     "nat_poll_status", "nat_compact_prefix", "nat_select_cutlaw",
     "nat_select_cutlaw_workspace_bytes", "nat_attn_workspace_bytes", "nat_attn_fwd",
     "nat_attn_bwd", "nat_resnorm_workspace_bytes", "nat_resnorm_fwd", "nat_resnorm_bwd",
-    "nat_ckpt8_store", "nat_ckpt8_load",
+    "nat_ckpt8_store", "nat_ckpt8_load", "nat_embed_workspace_bytes", "nat_embed_fwd", "nat_embed_bwd",
+    "nat_qknorm_workspace_bytes", "nat_qknorm_fwd", "nat_qknorm_bwd",
 )
 TRACE_KINDS = ("fwd", "dz", "dh", "dw", "e")
 
@@ -61,6 +62,18 @@ class AttnParams(ctypes.Structure):
 class ResnormParams(ctypes.Structure):
     _fields_ = [("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("gate_mode", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("alpha", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class EmbedParams(ctypes.Structure):
+    _fields_ = [("V", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("accumulate", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class QknormParams(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -128,8 +141,18 @@ def load():
         [vp] * 8 + [ctypes.c_size_t, vp]
     lib.nat_ckpt8_store.argtypes = [i32, i64, vp, vp, i64, vp, vp, vp]
     lib.nat_ckpt8_load.argtypes = [i32, i64, vp, vp, vp, i64, vp, vp]
+    lib.nat_embed_workspace_bytes.restype = ctypes.c_size_t
+    lib.nat_embed_workspace_bytes.argtypes = [ctypes.POINTER(EmbedParams), i64]
+    lib.nat_embed_fwd.argtypes = [ctypes.POINTER(EmbedParams)] + [vp] * 4 + [i64, vp, vp]
+    lib.nat_embed_bwd.argtypes = [ctypes.POINTER(EmbedParams)] + [vp] * 3 + [i64] + [vp] * 3 + [ctypes.c_size_t, vp]
+    lib.nat_qknorm_workspace_bytes.restype = ctypes.c_size_t
+    lib.nat_qknorm_workspace_bytes.argtypes = [ctypes.POINTER(QknormParams), i64]
+    lib.nat_qknorm_fwd.argtypes = [ctypes.POINTER(QknormParams), i32] + [vp] * 3 + [i64] + [vp] * 8
+    lib.nat_qknorm_bwd.argtypes = [ctypes.POINTER(QknormParams), i32] + [vp] * 3 + [i64] + [vp] * 12 + \
+        [ctypes.c_size_t, vp]
     for name in ("nat_attn_fwd", "nat_attn_bwd", "nat_resnorm_fwd", "nat_resnorm_bwd",
-                 "nat_ckpt8_store", "nat_ckpt8_load"):
+                 "nat_ckpt8_store", "nat_ckpt8_load", "nat_embed_fwd", "nat_embed_bwd", "nat_qknorm_fwd",
+                 "nat_qknorm_bwd"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("nat_grpo_adv", "nat_select", "nat_compact", "nat_policy_loss_fwd",
                  "nat_policy_loss_bwd", "nat_policy_loss_fwd_bwd"):
@@ -452,6 +475,109 @@ def nat_ckpt8_load(codes, scales, n_rows, cap, dst):
     _check(load().nat_ckpt8_load(_DTYPES.get(dst.dtype, -1), d, c, sc,
                                  _rows("n_rows", n_rows, torch.int32, (1,), dev), cap,
                                  _rows("dst", dst, dst.dtype, (cap, d), dev), _raw_stream(dev)))
+
+
+def embed_params(V, d, dtype, scale=1.0, accumulate=False):
+    """``accumulate``: the gradient is added to the table's instead of overwriting it."""
+    return EmbedParams(V=V, d=d, dtype=_DTYPES.get(dtype, dtype), scale=scale, accumulate=int(accumulate), reserved=0)
+
+
+def nat_embed_workspace_bytes(params, cap):
+    return load().nat_embed_workspace_bytes(ctypes.byref(params), cap)
+
+
+def _ids(ids, sel_idx, cap, device):
+    # through indices, ids may be of any length; that they lie within it is the caller's contract
+    return (_rows("ids", ids, torch.int32, (0 if sel_idx is not None else cap,), device),
+            _rows("sel_idx", sel_idx, torch.int32, (cap,), device))
+
+
+def nat_embed_fwd(params, table, ids, sel_idx, n_rows, cap, x):
+    """Row k < n_rows (a device scalar; None: cap) of x from the table's row ids[sel_idx[k]] (sel_idx None: ids[k])."""
+    dev = _device()
+    dt = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
+    _check(load().nat_embed_fwd(
+        ctypes.byref(params), _rows("table", table, dt, (params.V, params.d), dev), *_ids(ids, sel_idx, cap, dev),
+        _rows("n_rows", n_rows, torch.int32, (1,), dev), cap, _rows("x", x, dt, (cap, params.d), dev), _raw_stream(dev)))
+
+
+def nat_embed_bwd(params, ids, sel_idx, n_rows, cap, dx, dtable, workspace):
+    dev = _device()
+    dt = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
+    ws, nbytes = _workspace(workspace, dev)
+    _check(load().nat_embed_bwd(
+        ctypes.byref(params), *_ids(ids, sel_idx, cap, dev), _rows("n_rows", n_rows, torch.int32, (1,), dev), cap,
+        _rows("dx", dx, dt, (cap, params.d), dev), _rows("dtable", dtable, torch.float32, (params.V, params.d), dev),
+        ws, nbytes, _raw_stream(dev)))
+
+
+def rope_freqs(rot_dim, theta=1e6, device="cuda"):
+    """The usual law of the angles a position: theta^(-2 i / rot_dim), i < rot_dim / 2, in float64."""
+    return theta ** (-2.0 * torch.arange(rot_dim // 2, dtype=torch.float64, device=device) / rot_dim)
+
+
+def qknorm_params(n_heads, n_kv_heads, head_dim, dtype, rot_dim=None, interleaved=False, eps=1e-6):
+    """``rot_dim``: the elements of a head that turn, from its first on (None: all).  The strides are those of
+    contiguous tensors; nat_qknorm_fwd / nat_qknorm_bwd set them from theirs."""
+    q, kv = n_heads * head_dim, n_kv_heads * head_dim
+    return QknormParams(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                        rot_dim=head_dim if rot_dim is None else rot_dim, interleaved=int(interleaved),
+                        dtype=_DTYPES.get(dtype, dtype), eps=eps, reserved=0, q_stride=q, k_stride=kv,
+                        q_out_stride=q, k_out_stride=kv)
+
+
+def nat_qknorm_workspace_bytes(params, cap):
+    return load().nat_qknorm_workspace_bytes(ctypes.byref(params), cap)
+
+
+def _qknorm_call(params, B, cu_seqlens, positions, n_rows, cap, w_q, w_k, inv_freq, tensors):
+    """(params with the tensors' strides, leading arguments, weights and frequencies, pointers, device) of a call."""
+    dev, D = _device(), params.head_dim
+    dtype = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
+    p = QknormParams.from_buffer_copy(params)
+    strides, ptrs = {}, []
+    for name, t, field, heads in tensors:
+        if t is None:
+            ptrs.append(None)
+            continue
+        ptr, stride = _heads(name, t, dtype, (cap, heads, D), dev)
+        ptrs.append(ptr)
+        if stride is not None and strides.setdefault(field, stride) != stride:
+            raise NatError(f"{name}: token stride {stride}, its counterpart has {strides[field]}")
+    for field, stride in strides.items():
+        setattr(p, field, stride)
+    where = (B, _rows("cu_seqlens", cu_seqlens, torch.int32, (B + 1,), dev),
+             _rows("positions", positions, torch.int32, (cap,), dev), _rows("n_rows", n_rows, torch.int32, (1,), dev), cap)
+    laws = (_rows("w_q", w_q, torch.float32, (D,), dev), _rows("w_k", w_k, torch.float32, (D,), dev),
+            _rows("inv_freq", inv_freq, torch.float64, (params.rot_dim // 2,), dev))
+    return p, where, laws, ptrs, dev
+
+
+def nat_qknorm_fwd(params, B, cu_seqlens, positions, n_rows, cap, q, k, w_q, w_k, inv_freq, q_out, k_out):
+    """q_out and k_out from q and k, each head normed (w_q, w_k; both None: not) and turned by its token's position
+    (positions None: from cu_seqlens)."""
+    h, kv = params.n_heads, params.n_kv_heads
+    p, where, laws, (q, k, q_out, k_out), dev = _qknorm_call(
+        params, B, cu_seqlens, positions, n_rows, cap, w_q, w_k, inv_freq,
+        (("q", q, "q_stride", h), ("k", k, "k_stride", kv), ("q_out", q_out, "q_out_stride", h),
+         ("k_out", k_out, "k_out_stride", kv)))
+    _check(load().nat_qknorm_fwd(ctypes.byref(p), *where, q, k, *laws, q_out, k_out, _raw_stream(dev)))
+
+
+def nat_qknorm_bwd(params, B, cu_seqlens, positions, n_rows, cap, q, k, w_q, w_k, inv_freq, dq_out, dk_out, dq, dk,
+                   dw_q, dw_k, workspace):
+    """dq, dk have the token strides of q, k.  Without norms (w_q, w_k None) q, k, dw_q, dw_k and the workspace may be
+    None."""
+    h, kv = params.n_heads, params.n_kv_heads
+    p, where, laws, (q, k, dq_out, dk_out, dq, dk), dev = _qknorm_call(
+        params, B, cu_seqlens, positions, n_rows, cap, w_q, w_k, inv_freq,
+        (("q", q, "q_stride", h), ("k", k, "k_stride", kv), ("dq_out", dq_out, "q_out_stride", h),
+         ("dk_out", dk_out, "k_out_stride", kv), ("dq", dq, "q_stride", h), ("dk", dk, "k_stride", kv)))
+    ws, nbytes = (None, 0) if workspace is None else _workspace(workspace, dev)
+    f32, D = torch.float32, (params.head_dim,)
+    _check(load().nat_qknorm_bwd(ctypes.byref(p), *where, q, k, *laws, dq_out, dk_out, dq, dk,
+                                 _rows("dw_q", dw_q, f32, D, dev), _rows("dw_k", dw_k, f32, D, dev), ws, nbytes,
+                                 _raw_stream(dev)))
 
 
 def nat_trace_begin():
