@@ -566,6 +566,43 @@ int nat_qknorm_bwd(const nat_qknorm_params* params /* host */, int32_t B, const 
                    void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Matrix products of rows that are grouped by expert.  Rows [offsets[e], offsets[e+1]) of x belong to expert e, whose
+ * weights are w_e [n_out, n_in]:
+ *   y_r = w_e x_r                                                          (forward)
+ *   dx_r = w_e^T dy_r,   dw_e = sum over the expert's rows of dy_r x_r^T    (backward; dx or dw may be NULL)
+ * offsets int32 [n_experts + 1] on the device, ascending; an expert may have no rows (its dw is then zero).  Rows before
+ * offsets[0], at or after offsets[n_experts], or at or after cap are neither read into a result nor written; offsets
+ * beyond cap, or that do not ascend (then nothing is computed), raise NAT_DEV_CAPACITY in the status word at the head of
+ * the workspace.
+ * x, dx [cap, n_in] with x_stride elements from a row to the next; y, dy [cap, n_out] with y_stride; w [n_experts, n_out,
+ * n_in] row-major in dtype; dw float32 [n_experts, n_out, n_in], overwritten, or with accumulate added to its contents.
+ * dtype NAT_BF16: tensor cores with fp32 accumulation, one rounding of y and dx at the end; NAT_F32: plain fp32
+ * arithmetic.  Sums are taken in a fixed order: a call repeated on the same inputs reproduces its outputs bit for bit.
+ * A row's y and dx depend on that row and the expert's weights alone, infinities and NaN included; an expert's dw on its
+ * own rows alone.
+ * n_in, n_out multiples of 8, at most 2^20; at most 1024 experts; strides multiples of 8 elements, matrices 16-byte
+ * aligned.  Outputs must not overlap inputs.
+ * workspace: nat_experts_workspace_bytes(params, cap), shared by forward and backward; it holds nothing that must survive
+ * between them, and calls that may run at the same time need one each.  Where the weights' gradient has few tiles, the
+ * rows are cut into parts whose partial sums take up to 40 MB of it.
+ * A call with cap = 0 does nothing but write dw's zeros and the status word.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_experts, n_in, n_out;
+  int32_t dtype;      /* NAT_F32 | NAT_BF16 */
+  int32_t accumulate; /* backward: 0 overwrite dw, 1 add to it */
+  int32_t reserved;   /* set to 0 */
+  int64_t x_stride, y_stride; /* elements from a row to the next */
+} nat_experts_params;
+
+size_t nat_experts_workspace_bytes(const nat_experts_params* params /* host */, int64_t cap);
+int nat_experts_fwd(const nat_experts_params* params /* host */, const int32_t* offsets, int64_t cap, const void* x,
+                    const void* w, void* y, void* workspace, size_t workspace_bytes, void* stream);
+int nat_experts_bwd(const nat_experts_params* params /* host */, const int32_t* offsets, int64_t cap, const void* x,
+                    const void* w, const void* dy, void* dx, float* dw, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* ---------------------------------------------------------------------------
  * Per-kernel timing of the bf16 loss kernels (a measurement aid of this library;
  * the paper has no counterpart).  Between nat_trace_begin() and nat_trace_end()
  * every tensor-core kernel launch made by the loss entry points is bracketed by

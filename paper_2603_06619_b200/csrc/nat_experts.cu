@@ -1,0 +1,210 @@
+// Entry points of the products grouped by expert: argument checks, workspace, the list of row tiles, and the sum of
+// the parts of a weights' gradient.
+#include "nat_experts.cuh"
+
+#include "nat_rows.cuh"
+
+namespace nat {
+namespace experts {
+namespace {
+
+constexpr int kMaxExperts = 1024;
+constexpr int kPlanThreads = 1024;
+
+// The row tiles of all experts in their order, and the experts' order by falling number of rows (equal ones by
+// number): the weights' gradient takes its tiles in that order, so that those in flight together are of about the
+// same length and the shortest come last.
+__global__ void __launch_bounds__(kPlanThreads)
+plan_kernel(const int32_t* offsets, int E, int64_t cap, int tile_rows, Head* head, int32_t* order, Tile* tiles) {
+  release_secondary();
+  __shared__ int rows[kMaxExperts];
+  __shared__ int sums[kPlanThreads / 32];
+  const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
+  int lo = 0, hi = 0, fault = 0;
+  if (e < E) {
+    expert_rows(offsets, e, cap, lo, hi);
+    const int a = offsets[e], b = offsets[e + 1];
+    fault = (a < 0 || b < a ? 2 : 0) | ((int64_t)b > cap ? 1 : 0);
+    rows[e] = hi - lo;
+  }
+  const bool broken = __syncthreads_or(fault & 2), any = __syncthreads_or(fault);
+  const int count = (hi - lo + tile_rows - 1) / tile_rows;
+  int run = count;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+    if (lane >= o) run += left;
+  }
+  if (lane == 31) sums[warp] = run;
+  __syncthreads();
+  int first = run - count;
+  for (int w = 0; w < warp; ++w) first += sums[w];
+  if (e == kPlanThreads - 1) {
+    head->tiles = broken ? 0u : (uint32_t)(first + count);
+    head->broken = broken;
+    head->status = any ? NAT_DEV_CAPACITY : 0u;
+  }
+  if (broken) return;
+  for (int i = 0; i < count; ++i)
+    tiles[first + i] = {e, lo + i * tile_rows, min(lo + (i + 1) * tile_rows, hi), 0};
+  if (e < E) {
+    int before = 0;
+    for (int f = 0; f < E; ++f) before += rows[f] > rows[e] || (rows[f] == rows[e] && f < e);
+    order[before] = e;
+  }
+}
+
+// dw (+)= the parts' sums, in their order.
+__global__ void __launch_bounds__(256)
+join_kernel(const float* partial, int parts, int64_t size, const Head* head, bool accumulate, float* dw) {
+  if (head->broken) return;
+  const int64_t step = (int64_t)gridDim.x * 256 * rows::kChunk;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * rows::kChunk; i < size; i += step) {
+    float2 sum[rows::kPairs], v[rows::kPairs];
+    rows::widen(rows::load_raw(partial + i), sum);
+    for (int p = 1; p < parts; ++p) {
+      rows::widen(rows::load_raw(partial + p * size + i), v);
+#pragma unroll
+      for (int j = 0; j < rows::kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+    }
+    if (accumulate) {
+      rows::widen(rows::load_raw(dw + i), v);
+#pragma unroll
+      for (int j = 0; j < rows::kPairs; ++j) sum[j] = add2(v[j], sum[j]);
+    }
+    rows::Raw<float> out;
+    rows::narrow(sum, out);
+    rows::store_raw(dw + i, out);
+  }
+}
+
+int check(const char* who, const nat_experts_params* p, int64_t cap) {
+  if (!p) return fail(NAT_ERR_INVALID_ARG, "%s: params is null", who);
+  if (p->dtype != NAT_F32 && p->dtype != NAT_BF16)
+    return fail(NAT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, p->dtype);
+  if (p->n_experts <= 0 || p->n_in <= 0 || p->n_out <= 0 || cap < 0 || cap > 0x7FFFFFFFll)
+    return fail(NAT_ERR_INVALID_ARG, "%s: n_experts, n_in and n_out must be positive, cap in [0, 2^31)", who);
+  if (p->n_experts > kMaxExperts || p->n_in % 8 != 0 || p->n_out % 8 != 0 || p->n_in > (1 << 20) ||
+      p->n_out > (1 << 20) || (int64_t)p->n_in * p->n_out > (1ll << 31))
+    return fail(NAT_ERR_UNSUPPORTED,
+                "%s: at most 1024 experts; n_in and n_out multiples of 8, at most 2^20 and their product 2^31", who);
+  const int64_t strides[2] = {p->x_stride, p->y_stride};
+  for (int i = 0; i < 2; ++i) {
+    if (strides[i] < (i == 0 ? p->n_in : p->n_out))
+      return fail(NAT_ERR_INVALID_ARG, "%s: a row's stride (%lld) is shorter than the row", who, (long long)strides[i]);
+    if (strides[i] % 8 != 0 || strides[i] >= (1ll << 31))
+      return fail(NAT_ERR_UNSUPPORTED, "%s: strides must be multiples of 8 elements, below 2^31", who);
+  }
+  return NAT_OK;
+}
+
+int check_call(const char* who, const Args& a, size_t workspace_bytes, bool bwd, Layout* l) {
+  const void* needed[4] = {a.x, a.w, bwd ? a.dy : a.y, a.offsets};
+  // without rows the row matrices are not looked at
+  for (int i = a.cap > 0 ? 0 : 3; i < 4; ++i)
+    if (!needed[i]) return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (bwd && !a.dx && !a.dw) return fail(NAT_ERR_INVALID_ARG, "%s: neither dx nor dw", who);
+  if (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.dy | (uintptr_t)a.y | (uintptr_t)a.dx | (uintptr_t)a.dw) & 15u)
+    return fail(NAT_ERR_INVALID_ARG, "%s: matrices must be 16-byte aligned", who);
+  if ((uintptr_t)a.offsets & 3u) return fail(NAT_ERR_INVALID_ARG, "%s: offsets must be 4-byte aligned", who);
+  *l = layout(a.p, a.cap);
+  if (!a.workspace || workspace_bytes < l->total)
+    return fail(NAT_ERR_CAPACITY, "%s: workspace too small (%zu < %zu)", who, workspace_bytes, l->total);
+  if ((uintptr_t)a.workspace & 255u)
+    return fail(NAT_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+  return NAT_OK;
+}
+
+int product(const Args& a, const Layout& l, Product which) {
+  return a.p.dtype == NAT_F32 ? f32_product(a, l, which) : bf16_product(a, l, which);
+}
+
+int launch_plan(const Args& a, const Layout& l, int tile_rows) {
+  plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(a.offsets, a.p.n_experts, a.cap, tile_rows, head(a), order(a, l),
+                                                tiles(a, l));
+  NAT_LAUNCH_CHECK("experts_plan");
+  return NAT_OK;
+}
+
+}  // namespace
+
+Layout layout(const nat_experts_params& p, int64_t cap) {
+  Layout l;
+  const bool f32 = p.dtype == NAT_F32;
+  for (int i = 0; i < 2; ++i) l.tile_rows[i] = f32 ? kF32Tile : bf16_tile_rows(p, (Product)i, cap);
+  // an expert's last tile may be part full: at most one extra tile for each
+  l.most_tiles = cap / min(l.tile_rows[0], l.tile_rows[1]) + p.n_experts;
+  // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows of an average expert at least.
+  const int64_t rows = f32 ? kF32Tile : kDwRowsBf16, cols = f32 ? kF32Tile : kDwColsBf16;
+  const int64_t units = p.n_experts * ((p.n_out + rows - 1) / rows) * ((p.n_in + cols - 1) / cols);
+  const int64_t fit = (f32 ? 296 : 74) / units, worth = cap / p.n_experts / 512;
+  l.parts = (int)max((int64_t)1, min(fit, worth));
+  size_t at = 256;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at = align_up(at + bytes, 256);
+    return o;
+  };
+  l.order_off = take(sizeof(int32_t) * p.n_experts);
+  l.tiles_off = take(sizeof(Tile) * l.most_tiles);
+  l.partial_off = take(l.parts > 1 ? sizeof(float) * (size_t)l.parts * p.n_experts * p.n_out * p.n_in : 0);
+  l.total = at;
+  return l;
+}
+
+}  // namespace experts
+}  // namespace nat
+
+extern "C" {
+
+size_t nat_experts_workspace_bytes(const nat_experts_params* p, int64_t cap) {
+  if (nat::experts::check("nat_experts_workspace_bytes", p, cap) != NAT_OK) return 0;
+  return nat::experts::layout(*p, cap).total;
+}
+
+int nat_experts_fwd(const nat_experts_params* p, const int32_t* offsets, int64_t cap, const void* x, const void* w,
+                    void* y, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace nat::experts;
+  const char* who = "nat_experts_fwd";
+  int s = check(who, p, cap);
+  if (s != NAT_OK) return s;
+  Args a{};
+  a.p = *p; a.offsets = offsets; a.cap = cap; a.x = x; a.w = w; a.y = y; a.workspace = workspace;
+  a.stream = (cudaStream_t)stream;
+  Layout l;
+  s = check_call(who, a, workspace_bytes, false, &l);
+  if (s != NAT_OK) return s;
+  s = launch_plan(a, l, l.tile_rows[kFwd]);
+  return s != NAT_OK || cap == 0 ? s : product(a, l, kFwd);
+}
+
+int nat_experts_bwd(const nat_experts_params* p, const int32_t* offsets, int64_t cap, const void* x, const void* w,
+                    const void* dy, void* dx, float* dw, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace nat::experts;
+  const char* who = "nat_experts_bwd";
+  int s = check(who, p, cap);
+  if (s != NAT_OK) return s;
+  Args a{};
+  a.p = *p; a.offsets = offsets; a.cap = cap; a.x = x; a.w = w; a.dy = dy; a.dx = dx; a.dw = dw;
+  a.workspace = workspace; a.stream = (cudaStream_t)stream;
+  Layout l;
+  s = check_call(who, a, workspace_bytes, true, &l);
+  if (s != NAT_OK) return s;
+  s = launch_plan(a, l, l.tile_rows[kDx]);
+  if (s == NAT_OK && dx && cap > 0) s = product(a, l, kDx);
+  if (s != NAT_OK || !dw) return s;
+  const int64_t size = (int64_t)p->n_experts * p->n_out * p->n_in;
+  if (cap == 0) {
+    if (!p->accumulate) NAT_CUDA(cudaMemsetAsync(dw, 0, size * sizeof(float), a.stream));
+    return NAT_OK;
+  }
+  s = product(a, l, kDw);
+  if (s != NAT_OK || l.parts == 1) return s;
+  const int64_t want = (size / nat::rows::kChunk + 255) / 256;
+  join_kernel<<<(unsigned)min(want, (int64_t)148 * 8), 256, 0, a.stream>>>(partial(a, l), l.parts, size, head(a),
+                                                                          p->accumulate != 0, dw);
+  NAT_LAUNCH_CHECK("experts_join");
+  return NAT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,78 @@
+// Shared parts of the products grouped by expert: arguments, workspace layout, the list of row tiles.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "nat_common.cuh"
+
+namespace nat {
+namespace experts {
+
+struct Args {
+  nat_experts_params p;
+  const int32_t* offsets;
+  int64_t cap;
+  const void *x, *w, *dy;
+  void *y, *dx;
+  float* dw;
+  void* workspace;
+  cudaStream_t stream;
+};
+
+enum Product { kFwd = 0, kDx = 1, kDw = 2 };
+
+// Head of the workspace.  `status` is first, where nat_poll_status reads it.
+struct Head {
+  uint32_t status;
+  uint32_t tiles;   // entries of the list
+  uint32_t broken;  // offsets that do not ascend: nothing is computed
+};
+
+// Rows [lo, hi) of one expert, at most a tile's number.
+struct Tile {
+  int32_t expert, lo, hi, spare;
+};
+
+// Rows of expert e, clamped to [0, cap] whatever the offsets hold.
+__device__ __forceinline__ void expert_rows(const int32_t* offsets, int e, int64_t cap, int& lo, int& hi) {
+  lo = (int)min((int64_t)max(offsets[e], 0), cap);
+  hi = (int)min((int64_t)max(offsets[e + 1], 0), cap);
+  if (hi < lo) hi = lo;
+}
+
+struct Layout {
+  int tile_rows[2];           // of a tile of the list, for kFwd and kDx
+  int64_t most_tiles;
+  int parts;                  // into which the rows are cut for the weights' gradient
+  size_t order_off, tiles_off, partial_off, total;
+};
+Layout layout(const nat_experts_params& p, int64_t cap);
+
+inline Head* head(const Args& a) { return reinterpret_cast<Head*>(a.workspace); }
+inline int32_t* order(const Args& a, const Layout& l) {
+  return reinterpret_cast<int32_t*>((char*)a.workspace + l.order_off);
+}
+inline Tile* tiles(const Args& a, const Layout& l) { return reinterpret_cast<Tile*>((char*)a.workspace + l.tiles_off); }
+inline float* partial(const Args& a, const Layout& l) {
+  return reinterpret_cast<float*>((char*)a.workspace + l.partial_off);
+}
+
+// Rows and columns of a tile of the weights' gradient.
+constexpr int kDwRowsBf16 = 512, kDwColsBf16 = 256, kF32Tile = 128;
+
+// Rows of the k-blocks [lo, hi) that part `part` of `parts` takes of `blocks`.
+__host__ __device__ inline void part_range(int blocks, int part, int parts, int& lo, int& hi) {
+  const int per = (blocks + parts - 1) / parts;
+  lo = part * per < blocks ? part * per : blocks;
+  hi = lo + per < blocks ? lo + per : blocks;
+}
+
+// Tiles of the kernel that `which` of a bfloat16 call takes; see its definition.
+int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap);
+int bf16_product(const Args& a, const Layout& l, Product which);
+int f32_product(const Args& a, const Layout& l, Product which);
+
+}  // namespace experts
+}  // namespace nat

@@ -1,0 +1,572 @@
+// Products grouped by expert on the tensor cores (tcgen05 + TMEM + TMA).
+//
+//   kFwd  y  = x w_e^T     (rows x n_out,  contraction n_in)    x and w_e contiguous along it
+//   kDx   dx = dy w_e      (rows x n_in,   contraction n_out)   w_e contiguous across it
+//   kDw   dw_e = dy^T x    (n_out x n_in,  contraction rows)    both contiguous across it
+//
+// Persistent CTA pairs: the even CTA issues MMAs of M = 256, N = 256 (cta_group::2), each CTA holds SUBS blocks of
+// 128 rows of A and half of B per stage and drains its own rows of the accumulators.  Warp 0 loads by TMA, warp 1
+// issues, four warps for each block of rows write out.  Every wait is bounded and raises NAT_DEV_TIMEOUT.
+//
+// Ragged ends.  A tile's rows behind its expert's last belong to another expert or to none: they give rows of the
+// accumulator that nobody writes out.  Columns behind n_in or n_out, and another expert's weights, lie outside the
+// tensor maps (the weights' has a dimension for the expert) and are read as zeros.  For kDw the rows are the
+// contraction, and a row too many would be added in: where an expert's last block of 64 rows is not full, the loading
+// warp of each CTA waits for its own part of it, writes zeros over the rows behind (both operands': a weight of zero
+// would not hide an infinity), and the odd CTA tells the even one before the MMA warp is let on.
+#include <atomic>
+
+#include "nat_experts.cuh"
+#include "nat_tc.cuh"
+
+namespace nat {
+namespace experts {
+namespace {
+
+constexpr int BM = 128, BN = 256, BK = 64;
+constexpr int kBox = 64 * 64 * 2;            // bytes of a 64 x 64 box of an operand that is contiguous across the contraction
+constexpr int kTmemCols = 512;
+constexpr int kGroup = 8;                    // row tiles that go through the columns together
+
+template <int SUBS>
+struct Ring {
+  static constexpr int kABytes = SUBS * BM * BK * 2, kBBytes = (BN / 2) * BK * 2, kStage = kABytes + kBBytes;
+  static constexpr int kNum = 192 * 1024 / kStage;
+  static constexpr int kStaging = 4 * SUBS * 4096;
+  static constexpr int kThreads = 64 + 128 * SUBS;
+  static constexpr size_t kSmem = (size_t)kNum * kStage + kStaging + 1024 /*alignment*/ + 256 /*barriers*/;
+};
+
+struct TcArgs {
+  Head* head;
+  const Tile* tiles;
+  const int32_t *order, *offsets;
+  int64_t cap;
+  int E, n_cols, k_blocks;     // columns of the result; blocks of the contraction (kFwd, kDx)
+  int m_tiles;                 // kDw: tiles along n_out
+  int parts;
+  bool accumulate;
+  __nv_bfloat16* rows_out;     // kFwd, kDx
+  int64_t rows_stride;
+};
+
+struct Unit {
+  int expert, lo, hi;  // rows of the tile, or of the expert (kDw)
+  int m0, n0;          // kDw: first row of the result; first column
+  int kb_lo, kb_hi, slice;
+};
+
+template <int WHICH>
+__device__ __forceinline__ int unit_count(const TcArgs& a) {
+  const int n_tiles = (a.n_cols + BN - 1) / BN;
+  if (WHICH == kDw) return a.head->broken ? 0 : a.E * a.m_tiles * n_tiles * a.parts;
+  return (int)a.head->tiles * n_tiles;
+}
+
+// kFwd, kDx: groups of kGroup row tiles go through the columns, the row tile varying fastest, so that the pairs at
+// work share few row tiles and few column tiles through L2.  kDw: the experts in the list's order.
+template <int WHICH>
+__device__ __forceinline__ Unit decode(const TcArgs& a, int u) {
+  const int n_tiles = (a.n_cols + BN - 1) / BN;
+  Unit w;
+  if (WHICH == kDw) {
+    const int per = a.m_tiles * n_tiles, rank = u / (per * a.parts), in = u - rank * per * a.parts;
+    const int part = in / per, tile = in - part * per;
+    w.expert = a.order[rank];
+    w.m0 = tile / n_tiles * (kDwRowsBf16);
+    w.n0 = (tile - tile / n_tiles * n_tiles) * BN;
+    expert_rows(a.offsets, w.expert, a.cap, w.lo, w.hi);
+    part_range((w.hi - w.lo + BK - 1) / BK, part, a.parts, w.kb_lo, w.kb_hi);
+    w.slice = part * a.E + w.expert;
+    return w;
+  }
+  const int rows = (int)a.head->tiles, grp = u / (kGroup * n_tiles), in = u - grp * kGroup * n_tiles;
+  const int left = min(kGroup, rows - grp * kGroup);
+  const int n = in / left;
+  const Tile t = a.tiles[grp * kGroup + in - n * left];
+  w.expert = t.expert;
+  w.lo = t.lo;
+  w.hi = t.hi;
+  w.m0 = 0;
+  w.n0 = n * BN;
+  w.kb_lo = 0;
+  w.kb_hi = a.k_blocks;
+  w.slice = 0;
+  return w;
+}
+
+__device__ __forceinline__ void load_3d_pair(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(tc::smem_u32(dst)),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+// A wait for what the other CTA of the pair has written.
+__device__ __forceinline__ bool peer_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  const uint64_t t0 = tc::global_timer_ns();
+  for (uint32_t it = 1;; ++it) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(tc::smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((it & 127u) == 0u) {
+      if (*abort_flag != 0u) return false;
+      if (tc::global_timer_ns() - t0 > tc::kWaitLimitNs) {
+        *abort_flag = 1u;
+        return false;
+      }
+    }
+  }
+}
+
+template <bool ADD>
+__device__ __forceinline__ void put_3d(const CUtensorMap* map, const void* src, int x, int y, int z) {
+  if (ADD)
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+                 "r"(tc::smem_u32(src)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+                 "r"(tc::smem_u32(src)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+
+__device__ __forceinline__ uint32_t pack(uint32_t lo, uint32_t hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+
+template <int WHICH, int SUBS>
+__global__ void __launch_bounds__(Ring<SUBS>::kThreads, 1)
+experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_c, const TcArgs a) {
+  using R = Ring<SUBS>;
+  constexpr int kNS = R::kNum;
+  constexpr uint32_t kAcc = 2 / SUBS;  // accumulators: two tiles in flight, or one
+  constexpr bool kAcross = WHICH == kDw;                    // A is contiguous across the contraction
+  constexpr bool kBcross = WHICH == kDw || WHICH == kDx;
+  constexpr uint32_t kIdesc = tc::instr_desc_bf16(2 * BM, BN, kAcross ? 1 : 0, kBcross ? 1 : 0);
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* staging = smem + (size_t)kNS * R::kStage;
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(staging + R::kStaging);  // [kNS], the even CTA's are used
+  uint64_t* empty_bar = full_bar + kNS;                                     // [kNS]
+  uint64_t* tfull_bar = empty_bar + kNS;                                    // [2]
+  uint64_t* tempty_bar = tfull_bar + 2;                                     // [2], the even CTA's are used
+  uint64_t* tail_bar = tempty_bar + 2;                                      // kDw: this CTA's part of a last block
+  uint64_t* peer_bar = tail_bar + 1;                                        // [kNS] the odd CTA's is done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(peer_bar + kNS);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)(tc::cluster_ctarank() & 1u);
+  const int unit0 = blockIdx.x / 2, stride = gridDim.x / 2;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kNS; ++s) {
+      tc::mbar_init(&full_bar[s], 1);
+      tc::mbar_init(&empty_bar[s], 1);
+      tc::mbar_init(&peer_bar[s], 1);
+    }
+    tc::mbar_init(tail_bar, 1);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&tfull_bar[i], 1);
+      tc::mbar_init(&tempty_bar[i], 4 * SUBS * 2);
+    }
+    *abort_flag = 0u;
+    tc::fence_barrier_init();
+    tc::fence_proxy_async();
+    tc::prefetch_tensormap(&map_a);
+    tc::prefetch_tensormap(&map_b);
+    tc::prefetch_tensormap(&map_c);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc_pair(tmem_slot, kTmemCols);
+    tc::tmem_relinquish_pair();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync_all();  // the peer's barriers exist before anyone signals them
+  tc::fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  wait_for_primary();  // the list of tiles is there
+  const int units = unit_count<WHICH>(a);
+
+  // Whether the second block of 256 rows of a tile holds any (kFwd, kDx with SUBS = 2).
+  auto second = [&](const Unit& w) { return WHICH == kDw || w.hi - w.lo > 2 * BM; };
+  // A gradient that is added to takes nothing from an expert without rows.
+  auto skipped = [&](const Unit& w) {
+    return WHICH == kDw && a.accumulate && a.parts == 1 && w.kb_lo == w.kb_hi;
+  };
+
+  if (warp == 0) {
+    // ------------------------------------------------ TMA producer (lane 0; all lanes for the last rows)
+    auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x ? 1 : 0) != 0; };
+    uint32_t it = 0, tail_phase = 0u, peer_phase = 0u;  // peer_phase: a bit a stage
+    bool ok = true;
+    for (int u = unit0; ok && u < units; u += stride) {
+      const Unit w = decode<WHICH>(a, u);
+      if (skipped(w)) continue;
+      const int n0 = w.n0 + rank * (BN / 2);
+      const bool both = SUBS == 2 && second(w);
+      for (int kb = w.kb_lo; kb < w.kb_hi; ++kb, ++it) {
+        const int s = it % kNS;
+        ok = all(tc::mbar_wait(&empty_bar[s], ((it / kNS) & 1u) ^ 1u, abort_flag));
+        if (!ok) break;
+        uint8_t* a_dst = smem + (size_t)s * R::kStage;
+        uint8_t* b_dst = a_dst + R::kABytes;
+        // both CTAs' loads count on the even CTA's barrier, which its producer arms with the bytes of the pair
+        const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full_bar[s]), 0);
+        if (WHICH == kDw) {
+          const int t = w.lo + kb * BK, len = min(BK, w.hi - t);
+          if (lane == 0) {
+            if (len < BK) tc::mbar_arrive_expect_tx(tail_bar, R::kStage);
+            else if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kStage);
+#pragma unroll
+            for (int j = 0; j < 2 * SUBS + 2; ++j) {  // boxes of A, then of B
+              const CUtensorMap* map = j < 2 * SUBS ? &map_a : &map_b;
+              const int x = j < 2 * SUBS ? w.m0 + j / 2 * 2 * BM + rank * BM + j % 2 * 64 : n0 + (j - 2 * SUBS) * 64;
+              if (len < BK) tc::tma_load_2d(a_dst + j * kBox, map, tail_bar, x, t);
+              else tc::tma_load_2d_pair(a_dst + j * kBox, map, bar, x, t);
+            }
+          }
+          if (len < BK) {
+            ok = all(tc::mbar_wait(tail_bar, tail_phase, abort_flag));
+            if (!ok) break;
+            tail_phase ^= 1u;
+            for (int i = lane; i < (2 * SUBS + 2) * (BK - len) * 8; i += 32) {
+              const int box = i / ((BK - len) * 8), in = i - box * (BK - len) * 8;
+              *reinterpret_cast<uint4*>(a_dst + box * kBox + len * 128 + in * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            tc::fence_proxy_async();
+            __syncwarp();
+            if (rank == 1) {
+              if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_cta(tc::smem_u32(&peer_bar[s]), 0));
+            } else {
+              ok = all(peer_wait(&peer_bar[s], (peer_phase >> s) & 1u, abort_flag));
+              if (!ok) break;
+              peer_phase ^= 1u << s;
+              if (lane == 0) tc::mbar_arrive(&full_bar[s]);
+            }
+          }
+        } else if (lane == 0) {
+          if (rank == 0)
+            tc::mbar_arrive_expect_tx(&full_bar[s],
+                                      2 * (R::kBBytes + (SUBS == 2 && !both ? R::kABytes / 2 : R::kABytes)));
+          tc::tma_load_2d_pair(a_dst, &map_a, bar, kb * BK, w.lo + rank * BM);
+          if (both) tc::tma_load_2d_pair(a_dst + R::kABytes / 2, &map_a, bar, kb * BK, w.lo + 2 * BM + rank * BM);
+          if (WHICH == kFwd) {
+            load_3d_pair(b_dst, &map_b, bar, kb * BK, n0, w.expert);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) load_3d_pair(b_dst + j * kBox, &map_b, bar, n0 + j * 64, kb * BK, w.expert);
+          }
+        }
+      }
+    }
+    // Wait until every stage this warp filled has been released, so that no arrival targets this CTA after it has
+    // left and no load is still writing its shared memory.  Bounded like every wait.
+    const uint32_t pending = it < (uint32_t)kNS ? it : (uint32_t)kNS;
+    for (uint32_t j = 0; ok && j < pending; ++j) {
+      const uint32_t jt = it - 1 - j;
+      ok = all(tc::mbar_wait(&empty_bar[jt % kNS], (jt / kNS) & 1u, abort_flag));
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------ MMA issuer (even CTA)
+    if (lane == 0 && rank == 0) {
+      uint32_t it = 0, tcount = 0;
+      bool ok = true;
+      for (int u = unit0; ok && u < units; u += stride) {
+        const Unit w = decode<WHICH>(a, u);
+        if (skipped(w)) continue;
+        const int subs = SUBS == 2 && second(w) ? 2 : 1;
+        const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
+        ++tcount;
+        if (!tc::mbar_wait(&tempty_bar[acc], aph ^ 1u, abort_flag)) { ok = false; break; }
+        tc::fence_after_sync();
+        const uint32_t d_tmem = tmem_base + acc * SUBS * BN;
+        for (int kb = w.kb_lo; kb < w.kb_hi; ++kb, ++it) {
+          const int s = it % kNS;
+          if (!tc::mbar_wait(&full_bar[s], (it / kNS) & 1u, abort_flag)) { ok = false; break; }
+          tc::fence_after_sync();
+          const uint32_t a_base = tc::smem_u32(smem + (size_t)s * R::kStage), b_base = a_base + R::kABytes;
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk) {
+            // contiguous along the contraction: 16 elements are 32 bytes of the swizzled 128-byte row, groups of eight
+            // rows 1024 bytes apart; across it: 16 rows are two such groups, blocks of 64 columns whole boxes apart
+            const uint64_t bdesc = kBcross ? tc::smem_desc_sw128(b_base + kk * 2048, kBox, 1024)
+                                           : tc::smem_desc_sw128(b_base + kk * 32, 16, 1024);
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+              if (sub >= subs) break;
+              const uint32_t a_sub = a_base + sub * (BM * BK * 2);
+              const uint64_t adesc = kAcross ? tc::smem_desc_sw128(a_sub + kk * 2048, kBox, 1024)
+                                             : tc::smem_desc_sw128(a_sub + kk * 32, 16, 1024);
+              tc::umma_bf16_pair(d_tmem + sub * BN, adesc, bdesc, kIdesc, (kb > w.kb_lo || kk > 0) ? 1u : 0u);
+            }
+          }
+          tc::umma_commit_pair(&empty_bar[s], 3);
+        }
+        if (ok) tc::umma_commit_pair(&tfull_bar[acc], 3);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------ epilogue (four warps for each block of 128 rows)
+    const int q = warp & 3;           // tensor-memory lanes that this warp may read
+    const int sub = (warp - 2) >> 2;
+    uint8_t* stage = staging + (warp - 2) * 4096;
+    const int in_tile = sub * 2 * BM + rank * BM + q * 32;  // first of the warp's rows
+    uint32_t tcount = 0;
+    bool ok = true;
+    for (int u = unit0; ok && u < units; u += stride) {
+      const Unit w = decode<WHICH>(a, u);
+      if (skipped(w)) continue;
+      const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
+      ++tcount;
+      ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(&tfull_bar[acc], aph, abort_flag) ? 1 : 0) != 0;
+      if (!ok) break;
+      tc::fence_after_sync();
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc * SUBS + (uint32_t)sub) * BN;
+      if (WHICH == kDw) {
+        const bool none = w.kb_lo == w.kb_hi;  // no rows: zeros, not what tensor memory holds
+#pragma unroll 1
+        for (int c = 0; c < BN / 32; ++c) {
+          const int col = w.n0 + c * 32;
+          if (col >= a.n_cols) break;
+          uint32_t v[32];
+          tc::tmem_ld32_issue(taddr + c * 32, v);
+          tc::tmem_ld_wait(v);
+          if (lane == 0) tc::bulk_wait_read_all();  // the previous piece has left the block
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                none ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          tc::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            // rows behind n_out are outside the map
+            if (a.accumulate && a.parts == 1) put_3d<true>(&map_c, stage, col, w.m0 + in_tile, w.slice);
+            else put_3d<false>(&map_c, stage, col, w.m0 + in_tile, w.slice);
+            tc::bulk_commit();
+          }
+        }
+      } else {
+        const int valid = min(32, w.hi - w.lo - in_tile);  // of the warp's rows
+#pragma unroll 1
+        for (int c = 0; c < BN / 64 && valid > 0; ++c) {
+          const int col = w.n0 + c * 64;
+          if (col >= a.n_cols) break;
+          uint32_t ra[32], rb[32], packed[32];
+          tc::tmem_ld32_issue(taddr + c * 64, ra);
+          tc::tmem_ld32_issue(taddr + c * 64 + 32, rb);
+          tc::tmem_ld_wait(ra);
+          tc::tmem_ld_pin(rb);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            packed[j] = pack(ra[2 * j], ra[2 * j + 1]);
+            packed[16 + j] = pack(rb[2 * j], rb[2 * j + 1]);
+          }
+          if (valid == 32) {
+            // through the warp's block of shared memory, whole lines at a time
+            if (lane == 0) tc::bulk_wait_read_all();
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                  make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+            tc::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              tc::tma_store_2d(&map_c, stage, col, w.lo + in_tile);
+              tc::bulk_commit();
+            }
+          } else if (lane < valid) {
+            // the expert's last rows: those behind are another's
+            __nv_bfloat16* dst = a.rows_out + (int64_t)(w.lo + in_tile + lane) * a.rows_stride + col;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (col + 8 * j < a.n_cols)
+                *reinterpret_cast<uint4*>(dst + 8 * j) =
+                    make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+          }
+          __syncwarp();
+        }
+      }
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_cta(tc::smem_u32(&tempty_bar[acc]), 0));
+    }
+    if (lane == 0) tc::bulk_wait_all();  // this warp's stores are done
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag != 0u) atomicOr(&a.head->status, NAT_DEV_TIMEOUT);
+  tc::cluster_sync_all();  // the pair leaves together
+  if (warp == 1) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
+// --------------------------------------------------------------------------- host
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encode(CUtensorMap* map, CUtensorMapDataType type, int dims, uintptr_t base, const cuuint64_t* size,
+           const cuuint64_t* pitch, const cuuint32_t* box) {
+  static std::atomic<EncodeTiledFn> cached{nullptr};
+  EncodeTiledFn fn = cached.load(std::memory_order_relaxed);
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    NAT_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found));
+    if (found != cudaDriverEntryPointSuccess || !p)
+      return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    fn = reinterpret_cast<EncodeTiledFn>(p);
+    cached.store(fn, std::memory_order_relaxed);
+  }
+  const cuuint32_t one[3] = {1, 1, 1};
+  const CUresult r = fn(map, type, (cuuint32_t)dims, reinterpret_cast<void*>(base), size, pitch, box, one,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  return NAT_OK;
+}
+
+// Rows of a matrix [rows, cols] of bfloat16: boxes of 64 columns.
+int map_rows(CUtensorMap* map, const void* base, int cols, int64_t rows, int64_t stride, int box_rows) {
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uintptr_t)base, size, pitch, box);
+}
+// The experts' weights [E, n_out, n_in]: boxes of 64 columns by box_rows of one expert.
+int map_weights(CUtensorMap* map, const nat_experts_params& p, const void* w, int box_rows) {
+  const cuuint64_t size[3] = {(cuuint64_t)p.n_in, (cuuint64_t)p.n_out, (cuuint64_t)p.n_experts};
+  const cuuint64_t pitch[2] = {(cuuint64_t)p.n_in * 2, (cuuint64_t)p.n_in * p.n_out * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (uintptr_t)w, size, pitch, box);
+}
+// Their gradient, or the parts' [slices, n_out, n_in] in float32: pieces of 32 x 32.
+int map_gradient(CUtensorMap* map, const nat_experts_params& p, const float* dw, int64_t slices) {
+  const cuuint64_t size[3] = {(cuuint64_t)p.n_in, (cuuint64_t)p.n_out, (cuuint64_t)slices};
+  const cuuint64_t pitch[2] = {(cuuint64_t)p.n_in * 4, (cuuint64_t)p.n_in * p.n_out * 4};
+  const cuuint32_t box[3] = {32, 32, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (uintptr_t)dw, size, pitch, box);
+}
+
+// CTA pairs that the current device holds at a time, found once for each device.
+template <int WHICH, int SUBS>
+int pairs(int* out) {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  NAT_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", dev);
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    int s = require_sm100();
+    if (s != NAT_OK) return s;
+    NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, SUBS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)Ring<SUBS>::kSmem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(148);
+    cfg.blockDim = dim3(Ring<SUBS>::kThreads);
+    cfg.dynamicSmemBytes = Ring<SUBS>::kSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    NAT_CUDA(cudaOccupancyMaxActiveClusters(&n, experts_kernel<WHICH, SUBS>, &cfg));
+    if (n <= 0) return fail(NAT_ERR_UNSUPPORTED, "the device does not hold the experts' CTA pairs");
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  *out = n;
+  return NAT_OK;
+}
+
+template <int WHICH, int SUBS>
+int launch(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const TcArgs& t, int64_t most_units,
+           cudaStream_t stream) {
+  int slots = 0;
+  int s = pairs<WHICH, SUBS>(&slots);
+  if (s != NAT_OK) return s;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * min(most_units, (int64_t)slots)));
+  cfg.blockDim = dim3(Ring<SUBS>::kThreads);
+  cfg.dynamicSmemBytes = Ring<SUBS>::kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, SUBS>, ma, mb, mc, t));
+  return NAT_OK;
+}
+
+}  // namespace
+
+int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
+  (void)p; (void)which; (void)cap;
+  return 2 * BM;
+}
+
+int bf16_product(const Args& a, const Layout& l, Product which) {
+  const nat_experts_params& p = a.p;
+  CUtensorMap ma, mb, mc;
+  int s;
+  TcArgs t{};
+  t.head = head(a);
+  t.tiles = tiles(a, l);
+  t.order = order(a, l);
+  t.offsets = a.offsets;
+  t.cap = a.cap;
+  t.E = p.n_experts;
+  t.parts = which == kDw ? l.parts : 1;
+  t.accumulate = p.accumulate != 0;
+  if (which == kDw) {
+    if ((s = map_rows(&ma, a.dy, p.n_out, a.cap, p.y_stride, BK)) != NAT_OK) return s;
+    if ((s = map_rows(&mb, a.x, p.n_in, a.cap, p.x_stride, BK)) != NAT_OK) return s;
+    if ((s = l.parts > 1 ? map_gradient(&mc, p, partial(a, l), (int64_t)l.parts * p.n_experts)
+                         : map_gradient(&mc, p, a.dw, p.n_experts)) != NAT_OK)
+      return s;
+    t.n_cols = p.n_in;
+    t.m_tiles = (p.n_out + kDwRowsBf16 - 1) / kDwRowsBf16;
+    const int64_t units = (int64_t)t.E * t.m_tiles * ((p.n_in + BN - 1) / BN) * t.parts;
+    return launch<kDw, 2>(ma, mb, mc, t, units, a.stream);
+  }
+  const bool fwd = which == kFwd;
+  const void *in = fwd ? a.x : a.dy;
+  void* out = fwd ? a.y : a.dx;
+  const int k = fwd ? p.n_in : p.n_out, n = fwd ? p.n_out : p.n_in;
+  t.n_cols = n;
+  t.k_blocks = (k + BK - 1) / BK;
+  t.rows_out = (__nv_bfloat16*)out;
+  t.rows_stride = fwd ? p.y_stride : p.x_stride;
+  if ((s = map_rows(&ma, in, k, a.cap, fwd ? p.x_stride : p.y_stride, BM)) != NAT_OK) return s;
+  if ((s = map_weights(&mb, p, a.w, fwd ? BN / 2 : BK)) != NAT_OK) return s;
+  if ((s = map_rows(&mc, out, n, a.cap, t.rows_stride, 32)) != NAT_OK) return s;
+  const int64_t units = l.most_tiles * ((n + BN - 1) / BN);
+  return fwd ? launch<kFwd, 1>(ma, mb, mc, t, units, a.stream) : launch<kDx, 1>(ma, mb, mc, t, units, a.stream);
+}
+
+}  // namespace experts
+}  // namespace nat

@@ -28,7 +28,8 @@ SYMBOLS = (
     "nat_select_cutlaw_workspace_bytes", "nat_attn_workspace_bytes", "nat_attn_fwd",
     "nat_attn_bwd", "nat_resnorm_workspace_bytes", "nat_resnorm_fwd", "nat_resnorm_bwd",
     "nat_ckpt8_store", "nat_ckpt8_load", "nat_embed_workspace_bytes", "nat_embed_fwd", "nat_embed_bwd",
-    "nat_qknorm_workspace_bytes", "nat_qknorm_fwd", "nat_qknorm_bwd",
+    "nat_qknorm_workspace_bytes", "nat_qknorm_fwd", "nat_qknorm_bwd", "nat_experts_workspace_bytes", "nat_experts_fwd",
+    "nat_experts_bwd",
 )
 TRACE_KINDS = ("fwd", "dz", "dh", "dw", "e")
 
@@ -74,6 +75,12 @@ class QknormParams(ctypes.Structure):
                 ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("q_stride", ctypes.c_int64),
                 ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
+
+
+class ExpertsParams(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("accumulate", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -150,9 +157,13 @@ def load():
     lib.nat_qknorm_fwd.argtypes = [ctypes.POINTER(QknormParams), i32] + [vp] * 3 + [i64] + [vp] * 8
     lib.nat_qknorm_bwd.argtypes = [ctypes.POINTER(QknormParams), i32] + [vp] * 3 + [i64] + [vp] * 12 + \
         [ctypes.c_size_t, vp]
+    lib.nat_experts_workspace_bytes.restype = ctypes.c_size_t
+    lib.nat_experts_workspace_bytes.argtypes = [ctypes.POINTER(ExpertsParams), i64]
+    lib.nat_experts_fwd.argtypes = [ctypes.POINTER(ExpertsParams), vp, i64] + [vp] * 4 + [ctypes.c_size_t, vp]
+    lib.nat_experts_bwd.argtypes = [ctypes.POINTER(ExpertsParams), vp, i64] + [vp] * 6 + [ctypes.c_size_t, vp]
     for name in ("nat_attn_fwd", "nat_attn_bwd", "nat_resnorm_fwd", "nat_resnorm_bwd",
                  "nat_ckpt8_store", "nat_ckpt8_load", "nat_embed_fwd", "nat_embed_bwd", "nat_qknorm_fwd",
-                 "nat_qknorm_bwd"):
+                 "nat_qknorm_bwd", "nat_experts_fwd", "nat_experts_bwd"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("nat_grpo_adv", "nat_select", "nat_compact", "nat_policy_loss_fwd",
                  "nat_policy_loss_bwd", "nat_policy_loss_fwd_bwd"):
@@ -578,6 +589,59 @@ def nat_qknorm_bwd(params, B, cu_seqlens, positions, n_rows, cap, q, k, w_q, w_k
     _check(load().nat_qknorm_bwd(ctypes.byref(p), *where, q, k, *laws, dq_out, dk_out, dq, dk,
                                  _rows("dw_q", dw_q, f32, D, dev), _rows("dw_k", dw_k, f32, D, dev), ws, nbytes,
                                  _raw_stream(dev)))
+
+
+def experts_params(n_experts, n_in, n_out, dtype, accumulate=False):
+    """``accumulate``: dw is added to.  The strides are those of contiguous rows; nat_experts_fwd / nat_experts_bwd set
+    them from their tensors'."""
+    return ExpertsParams(n_experts=n_experts, n_in=n_in, n_out=n_out, dtype=_DTYPES.get(dtype, dtype),
+                         accumulate=int(accumulate), reserved=0, x_stride=n_in, y_stride=n_out)
+
+
+def nat_experts_workspace_bytes(params, cap):
+    return load().nat_experts_workspace_bytes(ctypes.byref(params), cap)
+
+
+def _experts_call(params, offsets, cap, w, workspace, tensors):
+    """(params with the tensors' strides, offsets, pointers, w, workspace, its bytes, device) of a call."""
+    dev = _device()
+    dtype = torch.float32 if params.dtype == NAT_F32 else torch.bfloat16
+    p = ExpertsParams.from_buffer_copy(params)
+    strides, ptrs = {}, []
+    for name, t, field, width in tensors:
+        if t is None:
+            ptrs.append(None)
+            continue
+        s = t.shape
+        if t.dtype is not dtype or t.get_device() != dev or len(s) != 2 or s[0] < cap or s[1] != width or t.stride(1) != 1:
+            _bad(name, t, dtype, (cap, width), dev)
+        ptrs.append(t.data_ptr())
+        if s[0] > 1 and strides.setdefault(field, t.stride(0)) != t.stride(0):
+            raise NatError(f"{name}: row stride {t.stride(0)}, its counterpart has {strides[field]}")
+    for field, stride in strides.items():
+        setattr(p, field, stride)
+    ws, nbytes = _workspace(workspace, dev)
+    E = params.n_experts
+    if w is not None and w.shape[0] != E:
+        _bad("w", w, dtype, (E, params.n_out, params.n_in), dev)
+    return (p, _rows("offsets", offsets, torch.int32, (E + 1,), dev), ptrs,
+            _rows("w", w, dtype, (E, params.n_out, params.n_in), dev), ws, nbytes, dev)
+
+
+def nat_experts_fwd(params, offsets, cap, x, w, y, workspace):
+    """y [cap, n_out] from x [cap, n_in], the rows offsets[e] .. offsets[e + 1] with w[e] [n_out, n_in]."""
+    p, offsets, (x, y), w, ws, nbytes, dev = _experts_call(
+        params, offsets, cap, w, workspace, (("x", x, "x_stride", params.n_in), ("y", y, "y_stride", params.n_out)))
+    _check(load().nat_experts_fwd(ctypes.byref(p), offsets, cap, x, w, y, ws, nbytes, _raw_stream(dev)))
+
+
+def nat_experts_bwd(params, offsets, cap, x, w, dy, dx, dw, workspace):
+    """dx (with x's row stride) and dw (float32), either of which may be None, from dy (with y's)."""
+    p, offsets, (x, dy, dx), w, ws, nbytes, dev = _experts_call(
+        params, offsets, cap, w, workspace, (("x", x, "x_stride", params.n_in), ("dy", dy, "y_stride", params.n_out),
+                                             ("dx", dx, "x_stride", params.n_in)))
+    dw = _rows("dw", dw, torch.float32, (params.n_experts, params.n_out, params.n_in), dev)
+    _check(load().nat_experts_bwd(ctypes.byref(p), offsets, cap, x, w, dy, dx, dw, ws, nbytes, _raw_stream(dev)))
 
 
 def nat_trace_begin():

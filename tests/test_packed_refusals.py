@@ -110,15 +110,61 @@ def test_qknorm_workspace_grows_with_cap():
     assert sizes == sorted(sizes) and 0 < sizes[-1] < 1 << 20
 
 
+# ---------------------------------------------------------------------------- experts
+def _ex_fwd(p, cap=8, ws=A, nbytes=1 << 30, **kw):
+    a = dict(dict(offs=A, x=A, w=A, y=A), **kw)
+    return nat.load().nat_experts_fwd(_ref(p), a["offs"], cap, a["x"], a["w"], a["y"], ws, nbytes, None)
+
+
+def _ex_bwd(p, cap=8, ws=A, nbytes=1 << 30, **kw):
+    a = dict(dict(offs=A, x=A, w=A, dy=A, dx=A, dw=A), **kw)
+    return nat.load().nat_experts_bwd(_ref(p), a["offs"], cap, a["x"], a["w"], a["dy"], a["dx"], a["dw"], ws, nbytes, None)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_experts_refusals(dtype):
+    ok = lambda **kw: _with(nat.experts_params(4, 64, 128, dtype), **kw)  # noqa: E731
+    assert nat.nat_experts_workspace_bytes(ok(), 8) > 0
+    for kw, status in [(dict(n_experts=0), -1), (dict(n_in=0), -1), (dict(n_out=-8), -1), (dict(n_in=60), -2),
+                       (dict(n_out=132), -2), (dict(n_experts=1025), -2), (dict(dtype=4), -2), (dict(x_stride=56), -1),
+                       (dict(y_stride=120), -1), (dict(x_stride=68), -2), (dict(y_stride=1 << 31), -2),
+                       (dict(n_in=(1 << 20) + 8, x_stride=1 << 21), -2), (dict(n_out=(1 << 20) + 8, y_stride=1 << 21), -2),
+                       (dict(n_in=1 << 20, n_out=4096, x_stride=1 << 20, y_stride=4096), -2)]:
+        assert _ex_fwd(ok(**kw)) == status and _ex_bwd(ok(**kw)) == status, kw
+        assert nat.nat_experts_workspace_bytes(ok(**kw), 8) == 0
+    need = nat.nat_experts_workspace_bytes(ok(), 8)
+    for f, names in ((_ex_fwd, ("x", "w", "y")), (_ex_bwd, ("x", "w", "dy"))):
+        assert f(None) == -1 and f(ok(), cap=-1) == -1 and f(ok(), cap=1 << 31) == -1
+        assert f(ok(), offs=None) == -1 and f(ok(), offs=A + 2) == -1
+        for name in names:
+            assert f(ok(), **{name: None}) == -1 and f(ok(), **{name: ODD}) == -1, name
+        assert f(ok(), nbytes=need - 1) == -3 and f(ok(), ws=None) == -3 and f(ok(), ws=A + 16) == -1
+    assert _ex_bwd(ok(), dx=None, dw=None) == -1
+    assert _ex_bwd(ok(), dx=ODD) == -1 and _ex_bwd(ok(), dw=ODD) == -1
+
+
+def test_experts_workspace_holds_to_its_bound():
+    for E, n_in, n_out in ((1, 8, 8), (1, 256, 512), (4, 256, 256), (64, 2048, 1536), (1024, 24, 16)):
+        for dtype in (torch.float32, torch.bfloat16):
+            for cap in (0, 1, 5000, 300013):
+                n = nat.nat_experts_workspace_bytes(nat.experts_params(E, n_in, n_out, dtype), cap)
+                assert 0 < n <= 40e6 + 16 * (cap // 128 + E) + 4 * E + 4 * 256
+
+
 def test_binding_refuses_host_tensors_types_shapes_and_strides():
     t = torch.zeros(4, 64)
     i = torch.zeros(4, dtype=torch.int32)
     p = nat.embed_params(4, 64, torch.float32)
     with pytest.raises(nat.NatError, match="not on the current CUDA device|expected"):
         nat.nat_embed_fwd(p, t, i, None, None, 4, t)
-    with pytest.raises(nat.NatError, match="expected torch.int32"):
-        nat.nat_embed_fwd(p, t, i.long(), None, None, 4, t)
+    with pytest.raises(nat.NatError, match="expected torch.float32"):
+        nat.nat_embed_fwd(p, t.bfloat16(), i, None, None, 4, t)
     h = torch.zeros(4, 2, 64)
+    e = nat.experts_params(2, 64, 64, torch.float32)
+    with pytest.raises(nat.NatError, match="not on the current CUDA device|expected"):
+        nat.nat_experts_fwd(e, i, 4, t, t.view(1, 4, 64), t, torch.zeros(4096, dtype=torch.uint8))
+    with pytest.raises(nat.NatError, match="expected torch.float32"):
+        nat.nat_experts_bwd(e, i, 4, t.bfloat16(), t, t, t, None, torch.zeros(4096, dtype=torch.uint8))
     q = nat.qknorm_params(2, 2, 64, torch.float32)
     with pytest.raises(nat.NatError, match="expected torch.float32"):
         nat.nat_qknorm_fwd(q, 1, i, None, None, 4, h.bfloat16(), h, None, None, None, h, h)
