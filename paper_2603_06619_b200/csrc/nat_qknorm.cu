@@ -6,6 +6,7 @@
 // that both members of a rotated pair are in one lane; a warp owns a token and walks its heads, so that the angles'
 // sines and cosines are found once a token, each by one of the warp's groups of lanes, and dealt to the others.  A warp
 // takes a run of consecutive tokens and finds its first token's sequence once.
+#include <atomic>
 #include <initializer_list>
 
 #include "nat_common.cuh"
@@ -91,12 +92,6 @@ __device__ __forceinline__ void turn(bool interleaved, float2 (&a)[kPairs], floa
 }
 
 template <typename T>
-__device__ __forceinline__ void load(const T* row, const Slot& s, bool on, Raw<T>& a, Raw<T>& b) {
-  a = b = rows::zero_raw<T>();
-  if (on && s.in) a = rows::load_raw(row + s.a);
-  if (on && s.in && s.b >= 0) b = rows::load_raw(row + s.b);
-}
-template <typename T>
 __device__ __forceinline__ void store(T* row, const Slot& s, bool on, const float2 (&a)[kPairs], const float2 (&b)[kPairs]) {
   Raw<T> r;
   if (on && s.in) {
@@ -131,82 +126,103 @@ __device__ __forceinline__ void read8(const float* w, float2 (&x)[kPairs]) {
   for (int i = 0; i < kPairs; ++i) x[i] = *reinterpret_cast<const float2*>(w + 2 * i);
 }
 
-// One kind of heads (queries or keys) of a token.
+// Stages of rows on their way into shared memory, and blocks a multiprocessor (see qknorm_kernel).
+template <typename T, bool BWD>
+struct Pipe {
+  static constexpr int kTensors = BWD ? 2 : 1, kPieces = sizeof(Raw<T>) / 16;
+  static constexpr int kStages = BWD && sizeof(T) == 4 ? 3 : 4;
+  static constexpr int kBlocks = BWD ? 2 : 3;
+  static constexpr int kSlot = kTensors * 2 * kPieces * 32;  // 16-byte pieces of a warp and stage
+  static constexpr size_t kBytes = (size_t)kWarps * kStages * kSlot * 16;
+};
+
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A lane's own slots of one stage: [tensor][chunk][piece][lane], so that a warp's accesses fall on consecutive
+// addresses.
+template <typename T>
+__device__ __forceinline__ void copy_chunks(uint4* slot, const T* row, const Slot& s) {
+  constexpr int kPieces = sizeof(Raw<T>) / 16;
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    rows::copy_async<16>(slot + k * 32, reinterpret_cast<const uint4*>(row + s.a) + k);
+    if (s.b >= 0) rows::copy_async<16>(slot + (kPieces + k) * 32, reinterpret_cast<const uint4*>(row + s.b) + k);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void read_chunks(const uint4* slot, bool in_a, bool in_b, float2 (&a)[kPairs], float2 (&b)[kPairs]) {
+  constexpr int kPieces = sizeof(Raw<T>) / 16;
+  Raw<T> ra = rows::zero_raw<T>(), rb = rows::zero_raw<T>();
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    if (in_a) reinterpret_cast<uint4*>(&ra)[k] = slot[k * 32];
+    if (in_b) reinterpret_cast<uint4*>(&rb)[k] = slot[(kPieces + k) * 32];
+  }
+  rows::widen(ra, a);
+  rows::widen(rb, b);
+}
+
+// One step: a head for each group of lanes, from its slots to memory.
 template <typename T, int LANES, bool BWD, bool NORM>
-__device__ __forceinline__ void heads(const Args& args, const Slot& slot, int group, int count, const T* x, const T* dout,
-                                      T* to, const float* w, const float (&c)[8], const float (&s)[8],
-                                      float2 (&dw)[2][kPairs]) {
-  constexpr int kGroups = 32 / LANES, kUnroll = 2;
-  const int D = args.p.head_dim;
-  const float inv_d = 1.f / (float)D;
-  for (int h0 = 0; h0 < count; h0 += kGroups * kUnroll) {
-    Raw<T> xa[kUnroll], xb[kUnroll], ga[kUnroll], gb[kUnroll];
+__device__ __forceinline__ void step(const nat_qknorm_params& p, const Slot& slot, const uint4* from, bool on, T* to,
+                                     const float* w, float inv_d, const float (&c)[8], const float (&s)[8],
+                                     float2 (&dw)[2][kPairs]) {
+  constexpr int kTensor = 2 * (sizeof(Raw<T>) / 16) * 32;
+  const bool in_a = on && slot.in, in_b = in_a && slot.b >= 0;
+  float2 a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
+  read_chunks<T>(BWD ? from + kTensor : from, in_a, in_b, a, b);
+  if (BWD && slot.turns) turn(p.interleaved, a, b, c, s);
+  if (NORM) {
+    float2 x[kPairs], y[kPairs];
+    if (BWD) read_chunks<T>(from, in_a, in_b, x, y);
+    const float2(&xa)[kPairs] = BWD ? x : a;
+    const float2(&xb)[kPairs] = BWD ? y : b;
+    const float rstd = rsqrtf(fmaf(over_row<LANES>(squares(xa, squares(xb, 0.f))), inv_d, p.eps));
+    read8(w + slot.a, wa);
+    read8(w + max(slot.b, 0), wb);
+    if (!BWD) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = h0 + u * kGroups + group;
-      if (!BWD || NORM) load<T>(x + (int64_t)h * D, slot, h < count, xa[u], xb[u]);
-      if (BWD) load<T>(dout + (int64_t)h * D, slot, h < count, ga[u], gb[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = h0 + u * kGroups + group;
-      float2 a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
-      if (NORM) {
-        read8(w + slot.a, wa);
-        read8(w + max(slot.b, 0), wb);
+      for (int i = 0; i < kPairs; ++i) {
+        a[i] = mul2(mul2(a[i], both(rstd)), wa[i]);
+        b[i] = mul2(mul2(b[i], both(rstd)), wb[i]);
       }
-      if (!BWD) {
-        rows::widen(xa[u], a);
-        rows::widen(xb[u], b);
-        if (NORM) {
-          const float rstd = rsqrtf(fmaf(over_row<LANES>(squares(a, squares(b, 0.f))), inv_d, args.p.eps));
+    } else {
 #pragma unroll
-          for (int i = 0; i < kPairs; ++i) {
-            a[i] = mul2(mul2(a[i], both(rstd)), wa[i]);
-            b[i] = mul2(mul2(b[i], both(rstd)), wb[i]);
-          }
-        }
-        if (slot.turns) turn(args.p.interleaved, a, b, c, s);
-      } else {
-        rows::widen(ga[u], a);
-        rows::widen(gb[u], b);
-        if (slot.turns) turn(args.p.interleaved, a, b, c, s);
-        if (NORM) {
-          float2 p[kPairs], q[kPairs];
-          rows::widen(xa[u], p);
-          rows::widen(xb[u], q);
-          const float rstd = rsqrtf(fmaf(over_row<LANES>(squares(p, squares(q, 0.f))), inv_d, args.p.eps));
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) {
-            p[i] = mul2(p[i], both(rstd));
-            q[i] = mul2(q[i], both(rstd));
-            dw[0][i] = fma2(a[i], p[i], dw[0][i]);
-            dw[1][i] = fma2(b[i], q[i], dw[1][i]);
-            a[i] = mul2(a[i], wa[i]);
-            b[i] = mul2(b[i], wb[i]);
-          }
-          const float mean = over_row<LANES>(products(a, p, products(b, q, 0.f))) * inv_d;
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) {
-            a[i] = mul2(both(rstd), fma2(p[i], both(-mean), a[i]));
-            b[i] = mul2(both(rstd), fma2(q[i], both(-mean), b[i]));
-          }
-        }
+      for (int i = 0; i < kPairs; ++i) {
+        x[i] = mul2(x[i], both(rstd));
+        y[i] = mul2(y[i], both(rstd));
+        dw[0][i] = fma2(a[i], x[i], dw[0][i]);
+        dw[1][i] = fma2(b[i], y[i], dw[1][i]);
+        a[i] = mul2(a[i], wa[i]);
+        b[i] = mul2(b[i], wb[i]);
       }
-      store<T>(to + (int64_t)h * D, slot, h < count, a, b);
+      const float mean = over_row<LANES>(products(a, x, products(b, y, 0.f))) * inv_d;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        a[i] = mul2(both(rstd), fma2(x[i], both(-mean), a[i]));
+        b[i] = mul2(both(rstd), fma2(y[i], both(-mean), b[i]));
+      }
     }
   }
+  if (!BWD && slot.turns) turn(p.interleaved, a, b, c, s);
+  store<T>(to, slot, on, a, b);
 }
 
 template <typename T, int LANES, bool BWD, bool NORM>
-__global__ void __launch_bounds__(kThreads) qknorm_kernel(const Args args) {
-  constexpr int kGroups = 32 / LANES;
+__global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kernel(const Args args) {
+  using P = Pipe<T, BWD>;
+  constexpr int kGroups = 32 / LANES, kStages = P::kStages;
   constexpr int kAngles = kGroups >= 8 ? 1 : 8 / kGroups;  // that a lane finds
-  __shared__ float weights[2][kMaxDim];
-  __shared__ float sums[kWarps][2][kMaxDim];
+  constexpr bool kReadsX = !BWD || NORM;
+  extern __shared__ __align__(16) uint4 slots[];
+  __shared__ __align__(16) float weights[2][kMaxDim];
   const nat_qknorm_params& p = args.p;
   const int D = p.head_dim, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = lane / LANES;
   const Slot slot = slot_of(p, lane & (LANES - 1));
+  const float inv_d = 1.f / (float)D;
   if (NORM) {
     for (int i = threadIdx.x; i < 2 * kMaxDim; i += kThreads)
       weights[i / kMaxDim][i % kMaxDim] = i % kMaxDim < D ? (i < kMaxDim ? args.w_q : args.w_k)[i % kMaxDim] : 0.f;
@@ -216,6 +232,34 @@ __global__ void __launch_bounds__(kThreads) qknorm_kernel(const Args args) {
   const int64_t total = (int64_t)gridDim.x * kWarps, mine = (int64_t)blockIdx.x * kWarps + warp;
   const int64_t each = n / total, more = n % total;
   const int64_t begin = mine * each + min(mine, more), end = begin + each + (mine < more ? 1 : 0);
+
+  // steps of a token: its query heads, kGroups at a time, then its key heads
+  const int q_steps = (p.n_heads + kGroups - 1) / kGroups, steps = q_steps + (p.n_kv_heads + kGroups - 1) / kGroups;
+  uint4* own = slots + (size_t)warp * kStages * P::kSlot + lane;
+  int64_t ahead_t = begin;
+  int ahead_step = 0, ahead_stage = 0;
+  auto fetch = [&]() {  // the next step that is not on its way yet
+    if (ahead_t < end) {
+      const bool key = ahead_step >= q_steps;
+      const int h = (key ? ahead_step - q_steps : ahead_step) * kGroups + group;
+      if (slot.in && h < (key ? p.n_kv_heads : p.n_heads)) {
+        uint4* to = own + ahead_stage * P::kSlot;
+        if (kReadsX)
+          copy_chunks<T>(to, (const T*)(key ? args.k : args.q) + ahead_t * (key ? p.k_stride : p.q_stride) + h * D, slot);
+        if (BWD)
+          copy_chunks<T>(to + P::kSlot / 2, (const T*)(key ? args.dk_out : args.dq_out) +
+                                                ahead_t * (key ? p.k_out_stride : p.q_out_stride) + h * D, slot);
+      }
+      if (++ahead_step == steps) {
+        ahead_step = 0;
+        ++ahead_t;
+      }
+    }
+    ahead_stage = ahead_stage + 1 == kStages ? 0 : ahead_stage + 1;
+    rows::copies_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) fetch();
 
   float2 dwq[2][kPairs], dwk[2][kPairs];
   if (BWD && NORM) {
@@ -236,6 +280,7 @@ __global__ void __launch_bounds__(kThreads) qknorm_kernel(const Args args) {
     seq_lo = __ldg(args.cu + seq);
     seq_hi = __ldg(args.cu + seq + 1);
   }
+  int stage = 0;
   for (int64_t t = begin; t < end; ++t) {
     int64_t pos;
     if (args.positions) {
@@ -264,15 +309,30 @@ __global__ void __launch_bounds__(kThreads) qknorm_kernel(const Args args) {
         if (BWD) s[e] = -s[e];
       }
     }
-    heads<T, LANES, BWD, NORM>(args, slot, group, p.n_heads, (const T*)args.q + t * p.q_stride,
-                               (const T*)args.dq_out + t * p.q_out_stride,
-                               (T*)args.q_to + t * (BWD ? p.q_stride : p.q_out_stride), weights[0], c, s, dwq);
-    heads<T, LANES, BWD, NORM>(args, slot, group, p.n_kv_heads, (const T*)args.k + t * p.k_stride,
-                               (const T*)args.dk_out + t * p.k_out_stride,
-                               (T*)args.k_to + t * (BWD ? p.k_stride : p.k_out_stride), weights[1], c, s, dwk);
+    // a stage is fetched anew only after the step that read it has used, and stored, what it read
+    for (int i = 0; i < steps; ++i) {
+      fetch();
+      copies_wait<kStages - 1>();
+      const uint4* from = own + stage * P::kSlot;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+      if (i < q_steps) {
+        const int h = i * kGroups + group;
+        step<T, LANES, BWD, NORM>(p, slot, from, h < p.n_heads,
+                                  (T*)args.q_to + t * (BWD ? p.q_stride : p.q_out_stride) + h * D, weights[0], inv_d, c,
+                                  s, dwq);
+      } else {
+        const int h = (i - q_steps) * kGroups + group;
+        step<T, LANES, BWD, NORM>(p, slot, from, h < p.n_kv_heads,
+                                  (T*)args.k_to + t * (BWD ? p.k_stride : p.k_out_stride) + h * D, weights[1], inv_d, c,
+                                  s, dwk);
+      }
+    }
   }
   if (BWD && NORM) {
-    // over the groups of the warp, over the warps of the block
+    // over the groups of the warp, over the warps of the block (in the slots, which nothing is on its way to now)
+    copies_wait<0>();
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(slots);  // [warp][kind][column]
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
       float2(&dw)[2][kPairs] = kind == 0 ? dwq : dwk;
@@ -286,14 +346,14 @@ __global__ void __launch_bounds__(kThreads) qknorm_kernel(const Args args) {
         }
         const int at = i < kPairs ? slot.a + 2 * i : slot.b + 2 * (i - kPairs);
         if (group == 0 && slot.in && (i < kPairs || slot.b >= 0))
-          *reinterpret_cast<float2*>(&sums[warp][kind][at]) = v;
+          *reinterpret_cast<float2*>(sums + (warp * 2 + kind) * kMaxDim + at) = v;
       }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
       float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) v += sums[w][i / D][i % D];
+      for (int w = 0; w < kWarps; ++w) v += sums[(w * 2 + i / D) * kMaxDim + i % D];
       args.partial[(int64_t)blockIdx.x * 2 * D + i] = v;
     }
   }
@@ -320,7 +380,7 @@ int lanes_of(const nat_qknorm_params& p) {
 }
 
 int blocks_of(int64_t cap, bool bwd) {
-  const int64_t want = (cap + kWarps - 1) / kWarps, most = 148 * (bwd ? 2 : 4);
+  const int64_t want = (cap + kWarps - 1) / kWarps, most = 148 * (bwd ? 2 : 3);
   return (int)(want < most ? want : most);
 }
 
@@ -370,25 +430,30 @@ int check_call(const char* who, const Args& a, std::initializer_list<const void*
   return NAT_OK;
 }
 
-template <typename T, int LANES, bool BWD>
-void launch_lanes(const Args& a, int blocks, cudaStream_t stream) {
-  if (a.w_q)
-    qknorm_kernel<T, LANES, BWD, true><<<blocks, kThreads, 0, stream>>>(a);
-  else
-    qknorm_kernel<T, LANES, BWD, false><<<blocks, kThreads, 0, stream>>>(a);
+template <typename T, int LANES, bool BWD, bool NORM>
+int launch(const Args& a, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed{0};  // a bit for each device whose shared-memory limit is raised
+  constexpr size_t smem = Pipe<T, BWD>::kBytes;
+  int dev = 0;
+  NAT_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", dev);
+  if (!(allowed.load(std::memory_order_relaxed) >> dev & 1u)) {
+    NAT_CUDA(cudaFuncSetAttribute(qknorm_kernel<T, LANES, BWD, NORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  qknorm_kernel<T, LANES, BWD, NORM><<<blocks_of(a.cap, BWD), kThreads, smem, stream>>>(a);
+  NAT_LAUNCH_CHECK("qknorm");
+  return NAT_OK;
 }
 
 template <typename T, bool BWD>
 int launch(const Args& a, cudaStream_t stream) {
-  const int blocks = blocks_of(a.cap, BWD);
-  switch (lanes_of(a.p)) {
-    case 8: launch_lanes<T, 8, BWD>(a, blocks, stream); break;
-    case 4: launch_lanes<T, 4, BWD>(a, blocks, stream); break;
-    case 2: launch_lanes<T, 2, BWD>(a, blocks, stream); break;
-    default: launch_lanes<T, 1, BWD>(a, blocks, stream);
-  }
-  NAT_LAUNCH_CHECK("qknorm");
-  return NAT_OK;
+  const int lanes = lanes_of(a.p);
+  if (a.w_q)
+    return lanes == 8 ? launch<T, 8, BWD, true>(a, stream) : lanes == 4 ? launch<T, 4, BWD, true>(a, stream)
+         : lanes == 2 ? launch<T, 2, BWD, true>(a, stream) : launch<T, 1, BWD, true>(a, stream);
+  return lanes == 8 ? launch<T, 8, BWD, false>(a, stream) : lanes == 4 ? launch<T, 4, BWD, false>(a, stream)
+       : lanes == 2 ? launch<T, 2, BWD, false>(a, stream) : launch<T, 1, BWD, false>(a, stream);
 }
 
 size_t workspace_bytes_of(const nat_qknorm_params& p, int64_t cap) {
