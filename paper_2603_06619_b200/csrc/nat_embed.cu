@@ -17,9 +17,10 @@ namespace {
 
 using rows::kChunk;
 using rows::kPairs;
+using rows::Raw;
 
 constexpr int kThreads = 256;
-constexpr int kTile = 4096;        // pairs a block sorts at a time
+constexpr int kTile = 2048;        // pairs a block sorts at a time
 constexpr int kWarps = kThreads / 32;
 constexpr int kRounds = kTile / kThreads;
 constexpr int kMaxDigits = 512;
@@ -45,6 +46,14 @@ __device__ __forceinline__ uint32_t row_id(const Rows& r, uint32_t k) {
 // `tpr` threads (a power of two) share a row, a chunk of eight elements each at a time; kUnroll rows in flight.
 constexpr int kUnroll = 4;
 
+// Rows of the table are read again and again: they stay in L2 (the output, written once, does not).
+__device__ __forceinline__ Raw<__nv_bfloat16> load_kept(const __nv_bfloat16* p) {
+  return {__ldg(reinterpret_cast<const uint4*>(p))};
+}
+__device__ __forceinline__ Raw<float> load_kept(const float* p) {
+  return {__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1)};
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 lookup_kernel(const T* __restrict__ table, Rows r, T* __restrict__ x, int d, int tpr_log2, float scale) {
@@ -60,10 +69,10 @@ lookup_kernel(const T* __restrict__ table, Rows r, T* __restrict__ x, int d, int
       id[u] = k < n ? row_id(r, (uint32_t)k) : (uint32_t)r.V;
     }
     for (int c = first; c < d; c += stride) {
-      rows::Raw<T> raw[kUnroll];
+      Raw<T> raw[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
-        if (id[u] < (uint32_t)r.V) raw[u] = rows::load_raw(table + (int64_t)id[u] * d + c);
+        if (id[u] < (uint32_t)r.V) raw[u] = load_kept(table + (int64_t)id[u] * d + c);
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t k = base + u * step;
@@ -85,30 +94,34 @@ lookup_kernel(const T* __restrict__ table, Rows r, T* __restrict__ x, int d, int
 }
 
 // --------------------------------------------------------------------------- sort
-// Stable sort by digits from the lowest up.  A block owns kTile consecutive pairs and a warp of it 512, in rounds
-// of 32, so that a pair's rank among those of its digit is: what earlier warps counted, what this warp counted in
-// earlier rounds, and the lanes below.
+// Stable sort by digits from the lowest up.  A block owns up to kTile consecutive pairs and a warp of it a run of
+// them, in rounds of 32, so that a pair's rank among those of its digit is: what earlier warps counted, what this
+// warp counted in earlier rounds, and the lanes below.  Rounds are dealt evenly, so that few pairs take few.
 struct Digit {
   int shift, bits;
   __device__ __forceinline__ int of(uint32_t key) const { return (int)(key >> shift) & ((1 << bits) - 1); }
   __device__ __forceinline__ int count() const { return 1 << bits; }
 };
 
-__device__ __forceinline__ uint32_t slot_of(int round) {
-  return (threadIdx.x >> 5) * (kTile / kWarps) + round * 32 + (threadIdx.x & 31);
+__device__ __forceinline__ int rounds_for(uint32_t valid) {
+  return (int)((min(valid, (uint32_t)kTile) + kThreads - 1) / kThreads);
+}
+__device__ __forceinline__ uint32_t slot_of(int round, int rounds) {
+  return (threadIdx.x >> 5) * rounds * 32 + round * 32 + (threadIdx.x & 31);
 }
 
 // rank[j] of the thread's pairs among their digit within the warp; `counts` [kWarps][digits] holds the warps'
 // totals afterwards.
-__device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint32_t valid, Digit digit, uint32_t* counts,
-                                           uint32_t (&rank)[kRounds]) {
+__device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint32_t valid, int rounds, Digit digit,
+                                           uint32_t* counts, uint32_t (&rank)[kRounds]) {
   const int lane = threadIdx.x & 31;
   uint32_t* mine = counts + (threadIdx.x >> 5) * digit.count();
   for (int i = threadIdx.x; i < kWarps * digit.count(); i += kThreads) counts[i] = 0u;
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kRounds; ++j) {
-    const bool in = slot_of(j) < valid;
+    if (j >= rounds) break;
+    const bool in = slot_of(j, rounds) < valid;
     const int g = in ? digit.of(key[j]) : -1;
     const unsigned same = __match_any_sync(0xFFFFFFFFu, g);
     const unsigned below = same & ((1u << lane) - 1u);
@@ -164,62 +177,75 @@ __global__ void __launch_bounds__(kThreads)
 sort_small_kernel(Rows r, int passes, int bits, uint32_t* keys, uint32_t* vals) {
   __shared__ uint32_t skey[kTile], counts[kWarps * kMaxDigits], total[kMaxDigits];
   __shared__ uint16_t sval[kTile];
+  release_secondary();
   const uint32_t n = row_count(r);
+  const int rounds = rounds_for(n);
   uint32_t key[kRounds], val[kRounds], rank[kRounds];
 #pragma unroll
   for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = slot_of(j);
-    key[j] = i < n ? row_id(r, i) : 0u;
+    const uint32_t i = slot_of(j, rounds);
+    key[j] = j < rounds && i < n ? row_id(r, i) : 0u;
     val[j] = i;
   }
   for (int p = 0; p < passes; ++p) {
     const Digit digit{p * bits, bits};
-    warp_ranks(key, n, digit, counts, rank);
+    warp_ranks(key, n, rounds, digit, counts, rank);
     across_warps(counts, total, digit.count());
     prefix_digits(total, digit.count());
+    const bool last = p == passes - 1;
 #pragma unroll
     for (int j = 0; j < kRounds; ++j) {
-      if (slot_of(j) < n) {
+      if (j < rounds && slot_of(j, rounds) < n) {
         const int g = digit.of(key[j]);
         const uint32_t to = total[g] + counts[(threadIdx.x >> 5) * digit.count() + g] + rank[j];
-        skey[to] = key[j];
-        sval[to] = (uint16_t)val[j];
+        if (last) {
+          keys[to] = key[j];
+          vals[to] = val[j];
+        } else {
+          skey[to] = key[j];
+          sval[to] = (uint16_t)val[j];
+        }
       }
     }
+    if (last) return;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kRounds; ++j) {
-      const uint32_t i = slot_of(j);
-      if (i < n) {
+      const uint32_t i = slot_of(j, rounds);
+      if (j < rounds && i < n) {
         key[j] = skey[i];
         val[j] = sval[i];
       }
     }
     __syncthreads();
   }
+}
+
+// A block's pairs, in registers before anything else is done with them: one round trip to memory.
+__device__ __forceinline__ void load_keys(const Rows& r, const uint32_t* keys, uint32_t base, uint32_t n, int rounds,
+                                          uint32_t (&key)[kRounds]) {
 #pragma unroll
   for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = slot_of(j);
-    if (i < n) {
-      keys[i] = key[j];
-      vals[i] = val[j];
-    }
+    const uint32_t i = base + slot_of(j, rounds);
+    key[j] = j < rounds && i < n ? (keys ? keys[i] : row_id(r, i)) : 0u;
   }
 }
 
 // How many pairs of each digit a block holds: hist [digits][blocks].
 __global__ void __launch_bounds__(kThreads)
 count_kernel(Rows r, const uint32_t* keys, Digit digit, uint32_t* hist) {
+  release_secondary();
   __shared__ uint32_t c[kMaxDigits];
-  const uint32_t n = row_count(r);
   for (int g = threadIdx.x; g < digit.count(); g += kThreads) c[g] = 0u;
   __syncthreads();
-  const uint32_t base = blockIdx.x * kTile;
+  wait_for_primary();
+  const uint32_t n = row_count(r), base = blockIdx.x * kTile;
+  const int rounds = base < n ? rounds_for(n - base) : 0;
+  uint32_t key[kRounds];
+  load_keys(r, keys, base, n, rounds, key);
 #pragma unroll
-  for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = base + slot_of(j);
-    if (i < n) atomicAdd(&c[digit.of(keys ? keys[i] : row_id(r, i))], 1u);
-  }
+  for (int j = 0; j < kRounds; ++j)
+    if (j < rounds && base + slot_of(j, rounds) < n) atomicAdd(&c[digit.of(key[j])], 1u);
   __syncthreads();
   for (int g = threadIdx.x; g < digit.count(); g += kThreads) hist[(int64_t)g * gridDim.x + blockIdx.x] = c[g];
 }
@@ -227,6 +253,8 @@ count_kernel(Rows r, const uint32_t* keys, Digit digit, uint32_t* hist) {
 // hist[g][.] -> its exclusive prefix sums, total[g]; a warp a digit.
 __global__ void __launch_bounds__(kThreads)
 prefix_kernel(uint32_t* hist, int blocks, int digits, uint32_t* total) {
+  release_secondary();
+  wait_for_primary();
   const int g = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (g >= digits) return;
   uint32_t before = 0u;
@@ -248,31 +276,40 @@ prefix_kernel(uint32_t* hist, int blocks, int digits, uint32_t* total) {
 __global__ void __launch_bounds__(kThreads)
 scatter_kernel(Rows r, const uint32_t* keys, const uint32_t* vals, Digit digit, const uint32_t* hist,
                const uint32_t* totals, uint32_t* keys_out, uint32_t* vals_out) {
+  release_secondary();
+  wait_for_primary();
   __shared__ uint32_t counts[kWarps * kMaxDigits], total[kMaxDigits];
   const uint32_t n = row_count(r), base = blockIdx.x * kTile;
   const int digits = digit.count();
   if (base >= n) return;
-  uint32_t key[kRounds], rank[kRounds];
+  const int rounds = rounds_for(n - base);
+  uint32_t key[kRounds], val[kRounds], rank[kRounds];
+  load_keys(r, keys, base, n, rounds, key);
 #pragma unroll
   for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = base + slot_of(j);
-    key[j] = i < n ? (keys ? keys[i] : row_id(r, i)) : 0u;
+    const uint32_t i = base + slot_of(j, rounds);
+    val[j] = vals && j < rounds && i < n ? vals[i] : i;
   }
-  warp_ranks(key, n - base, digit, counts, rank);
-  across_warps(counts, total, digits);
   for (int g = threadIdx.x; g < digits; g += kThreads) total[g] = totals[g];
-  __syncthreads();
+  warp_ranks(key, n - base, rounds, digit, counts, rank);
   prefix_digits(total, digits);
-  for (int g = threadIdx.x; g < digits; g += kThreads) total[g] += hist[(int64_t)g * gridDim.x + blockIdx.x];
+  // where the block's pairs of each digit, and those of each warp of it, begin
+  for (int g = threadIdx.x; g < digits; g += kThreads) {
+    uint32_t run = total[g] + hist[(int64_t)g * gridDim.x + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const uint32_t c = counts[w * digits + g];
+      counts[w * digits + g] = run;
+      run += c;
+    }
+  }
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = base + slot_of(j);
-    if (i < n) {
-      const int g = digit.of(key[j]);
-      const uint32_t to = total[g] + counts[(threadIdx.x >> 5) * digits + g] + rank[j];
+    if (j < rounds && base + slot_of(j, rounds) < n) {
+      const uint32_t to = counts[(threadIdx.x >> 5) * digits + digit.of(key[j])] + rank[j];
       keys_out[to] = key[j];
-      vals_out[to] = vals ? vals[i] : i;
+      vals_out[to] = val[j];
     }
   }
 }
@@ -290,12 +327,25 @@ struct SumArgs {
   bool accumulate;
 };
 
-// First sorted position whose key is not below `key`.
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n, uint32_t key) {
-  uint32_t lo = 0u, hi = n;
+// First sorted position in [lo, hi) whose key is not below `key`, hi if there is none.
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t key) {
   while (lo < hi) {
     const uint32_t mid = (lo + hi) >> 1;
     if (keys[mid] < key) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+// The same in [0, n) by a whole warp, 32 probes at a time: four dependent loads where one lane would take eighteen.
+__device__ __forceinline__ uint32_t warp_lower_bound(const uint32_t* keys, uint32_t n, uint32_t key) {
+  uint32_t lo = 0u, hi = n;  // the answer is in [lo, hi]
+  while (lo < hi) {
+    const uint32_t step = (hi - lo + 31) / 32, at = lo + ((threadIdx.x & 31) + 1) * step - 1;
+    const unsigned not_below = __ballot_sync(0xFFFFFFFFu, at >= hi || keys[at] >= key);
+    // lane f is the first not below: the answer is in its step; lanes past hi count as not below
+    const uint32_t f = not_below ? __ffs(not_below) - 1 : 32;
+    const uint32_t from = lo + f * step;
+    hi = f == 32 ? hi : min(hi, from + step - 1);
+    lo = min(from, hi);
   }
   return lo;
 }
@@ -308,7 +358,7 @@ __device__ __forceinline__ void add_tokens(const SumArgs& a, uint32_t lo, uint32
   for (int i = 0; i < kPairs; ++i) sum[i] = both(0.f);
   uint32_t i = lo;
   for (; i + 4 <= hi; i += 4) {
-    rows::Raw<T> raw[4];
+    Raw<T> raw[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) raw[u] = rows::load_raw(dx + (int64_t)a.vals[i + u] * a.d);
 #pragma unroll
@@ -331,7 +381,9 @@ __device__ __forceinline__ void add_tokens(const SumArgs& a, uint32_t lo, uint32
 // positions.  A tile meets at most two such rows, one that began before it (slot 0) and one that begins in it and
 // goes on behind it (slot 1).  The blocks behind: rows of the table with up to kPiece tokens.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) sum_kernel(SumArgs a) {
+  release_secondary();
+  wait_for_primary();
   __shared__ uint32_t start[33];
   const uint32_t n = row_count(a.r);
   const int tpr = 1 << a.tpr_log2, group = threadIdx.x >> a.tpr_log2, groups = kThreads >> a.tpr_log2;
@@ -339,19 +391,23 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
   if (blockIdx.x < (unsigned)a.tiles) {
     const uint32_t t0 = blockIdx.x * kPiece, t1 = min(t0 + kPiece, n);
     if (t0 >= n) return;
+    // a row that goes on over an end of the tile has the same id on both sides of it; most tiles have none
+    const uint32_t k0 = a.keys[t0], k1 = a.keys[t1 - 1];
+    const bool from_before = t0 > 0 && k0 != (uint32_t)a.r.V && a.keys[t0 - 1] == k0;
+    const bool goes_on = t1 < n && k1 != (uint32_t)a.r.V && a.keys[t1] == k1;
+    if (!from_before && !goes_on) return;
     if (threadIdx.x < 4) {
-      const uint32_t key = a.keys[threadIdx.x < 2 ? t0 : t1 - 1];
-      start[threadIdx.x] = key == (uint32_t)a.r.V ? 0u : lower_bound(a.keys, n, key + (threadIdx.x & 1));
+      const uint32_t key = threadIdx.x < 2 ? k0 : k1;
+      start[threadIdx.x] = lower_bound(a.keys, 0u, n, key + (threadIdx.x & 1));
     }
     __syncthreads();
-    const uint32_t b0 = start[0], e0 = start[1], b1 = start[2], e1 = start[3];
     for (int s = group; s < 2; s += groups) {
-      const uint32_t b = s == 0 ? b0 : b1, e = s == 0 ? e0 : e1;
-      if (e - b <= kPiece || (s == 0 ? b >= t0 : b < t0)) continue;
+      const uint32_t b = start[2 * s], e = start[2 * s + 1];
+      if (e - b <= kPiece || !(s == 0 ? from_before : goes_on && b >= t0)) continue;
       for (int c = first; c < a.d; c += stride) {
         float2 sum[kPairs];
         add_tokens<T>(a, max(b, t0), min(e, t1), c, sum);
-        rows::Raw<float> out;
+        Raw<float> out;
         rows::narrow(sum, out);
         rows::store_raw(a.partial + (2 * (int64_t)blockIdx.x + s) * a.d + c, out);
       }
@@ -359,7 +415,27 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
     return;
   }
   const int v0 = (blockIdx.x - a.tiles) * a.rows_per_block, count = min(a.rows_per_block, a.r.V - v0);
-  if (threadIdx.x <= count) start[threadIdx.x] = lower_bound(a.keys, n, (uint32_t)(v0 + threadIdx.x));
+  // where the block's rows begin among the sorted tokens: its first and last by two warps, those between from the
+  // tokens themselves where they are few
+  __shared__ uint32_t ends[2];
+  if (threadIdx.x < 64) {
+    const uint32_t at = warp_lower_bound(a.keys, n, (uint32_t)(v0 + (threadIdx.x < 32 ? 0 : count)));
+    if ((threadIdx.x & 31) == 0) ends[threadIdx.x >> 5] = at;
+  }
+  __syncthreads();
+  const uint32_t lo0 = ends[0], hi0 = ends[1];
+  if (hi0 - lo0 > kThreads) {
+    if (threadIdx.x <= count) start[threadIdx.x] = lower_bound(a.keys, lo0, hi0, (uint32_t)(v0 + threadIdx.x));
+  } else {
+    // token i tells where the rows after its predecessor's, up to its own, begin; the end tells of the rest
+    const uint32_t i = lo0 + threadIdx.x;
+    if (i <= hi0) {
+      const int from = i == lo0 ? 0 : (int)a.keys[i - 1] - v0 + 1, to = i == hi0 ? count : (int)a.keys[i] - v0;
+      for (int v = from; v <= to; ++v) start[v] = i;
+    }
+    if (hi0 - lo0 == kThreads && threadIdx.x == 0)  // one more than there are threads
+      for (int v = (int)a.keys[hi0 - 1] - v0 + 1; v <= count; ++v) start[v] = hi0;
+  }
   if (v0 == 0 && threadIdx.x == 0) *a.status = n > 0 && a.keys[n - 1] == (uint32_t)a.r.V ? NAT_DEV_BAD_TARGET : 0u;
   __syncthreads();
   for (int i = group; i < count; i += groups) {
@@ -369,7 +445,7 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
     for (int c = first; c < a.d; c += stride) {
       float2 sum[kPairs];
       add_tokens<T>(a, lo, hi, c, sum);
-      rows::Raw<float> out;
+      Raw<float> out;
       float2 old[kPairs];
       if (a.accumulate) rows::widen(rows::load_raw(row + c), old);
 #pragma unroll
@@ -383,52 +459,67 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
   }
 }
 
-// Joins the pieces of the row that begins in tile blockIdx.x and goes on behind it: the warps take runs of
+// Joins the pieces of the rows that begin in one of the block's tiles and go on behind it: the warps take runs of
 // pieces, 256 columns at a time, and their sums are added in the runs' order.
+constexpr int kJoinTiles = 8;
+
 __global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
+  release_secondary();
+  wait_for_primary();
   __shared__ float2 sums[kWarps][32][kPairs];
-  __shared__ uint32_t bounds[2];
-  const uint32_t n = row_count(a.r), t0 = blockIdx.x * kPiece, t1 = min(t0 + kPiece, n);
-  if (t0 >= n) return;
-  const uint32_t key = a.keys[t1 - 1];
-  if (key == (uint32_t)a.r.V) return;
-  if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(a.keys, n, key + threadIdx.x);
-  __syncthreads();
-  const uint32_t b = bounds[0], e = bounds[1];
-  if (e - b <= kPiece || b < t0) return;
-  const int pieces = (int)((e - 1) / kPiece - blockIdx.x + 1);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (blockIdx.y * 32 + lane) * kChunk;
-  const int per = (pieces + kWarps - 1) / kWarps, lo = warp * per, hi = min(lo + per, pieces);
-  float2 sum[kPairs];
-#pragma unroll
-  for (int j = 0; j < kPairs; ++j) sum[j] = both(0.f);
-  if (c < a.d) {
-#pragma unroll 4
-    for (int p = lo; p < hi; ++p) {
-      // the row's first piece is the second slot of its tile, the others the first slots of theirs
-      const int64_t slot = 2 * ((int64_t)blockIdx.x + p) + (p == 0 ? 1 : 0);
-      float2 v[kPairs];
-      rows::widen(rows::load_raw(a.partial + slot * a.d + c), v);
-#pragma unroll
-      for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+  __shared__ uint32_t bounds[kJoinTiles][2];
+  const uint32_t n = row_count(a.r);
+  if (threadIdx.x < 2 * kJoinTiles) {
+    const uint32_t tile = blockIdx.x * kJoinTiles + threadIdx.x / 2, t0 = tile * kPiece, t1 = t0 + kPiece;
+    uint32_t at = 0u;
+    if (t1 < n) {
+      const uint32_t key = a.keys[t1 - 1];
+      if (key != (uint32_t)a.r.V && a.keys[t1] == key && !(t0 > 0 && a.keys[t0 - 1] == key))
+        at = lower_bound(a.keys, t0, n, key + (threadIdx.x & 1));
     }
+    bounds[threadIdx.x / 2][threadIdx.x & 1] = at;
   }
-#pragma unroll
-  for (int j = 0; j < kPairs; ++j) sums[warp][lane][j] = sum[j];
   __syncthreads();
-  if (warp != 0 || c >= a.d) return;
-  float* at = a.dtable + (int64_t)key * a.d + c;
-  float2 old[kPairs];
-  if (a.accumulate) rows::widen(rows::load_raw(at), old);
-  rows::Raw<float> out;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (blockIdx.y * 32 + lane) * kChunk;
+  for (int i = 0; i < kJoinTiles; ++i) {
+    const uint32_t b = bounds[i][0], e = bounds[i][1];
+    if (e - b <= kPiece) continue;  // the same for all threads
+    const uint32_t tile = blockIdx.x * kJoinTiles + i;
+    const int pieces = (int)((e - 1) / kPiece - tile + 1);
+    const int per = (pieces + kWarps - 1) / kWarps, lo = warp * per, hi = min(lo + per, pieces);
+    float2 sum[kPairs];
 #pragma unroll
-  for (int j = 0; j < kPairs; ++j) {
-    for (int w = 1; w < kWarps; ++w) sum[j] = add2(sum[j], sums[w][lane][j]);
-    sum[j] = mul2(sum[j], both(a.scale));
-    if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+    for (int j = 0; j < kPairs; ++j) sum[j] = both(0.f);
+    if (c < a.d) {
+#pragma unroll 4
+      for (int p = lo; p < hi; ++p) {
+        // the row's first piece is the second slot of its tile, the others the first slots of theirs
+        const int64_t slot = 2 * ((int64_t)tile + p) + (p == 0 ? 1 : 0);
+        float2 v[kPairs];
+        rows::widen(rows::load_raw(a.partial + slot * a.d + c), v);
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) sums[warp][lane][j] = sum[j];
+    __syncthreads();
+    if (warp == 0 && c < a.d) {
+      float* at = a.dtable + (int64_t)a.keys[b] * a.d + c;
+      float2 old[kPairs];
+      if (a.accumulate) rows::widen(rows::load_raw(at), old);
+      Raw<float> out;
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        for (int w = 1; w < kWarps; ++w) sum[j] = add2(sum[j], sums[w][lane][j]);
+        sum[j] = mul2(sum[j], both(a.scale));
+        if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+      }
+      rows::narrow(sum, out);
+      rows::store_raw(at, out);
+    }
+    __syncthreads();
   }
-  rows::narrow(sum, out);
-  rows::store_raw(at, out);
 }
 
 // --------------------------------------------------------------------------- host
@@ -508,7 +599,7 @@ int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable,
         cudaStream_t stream) {
   char* ws = (char*)workspace;
   auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(ws + o); };
-  int src = 0;
+  int src = 0, s;
   if (r.cap <= kTile) {
     sort_small_kernel<<<1, kThreads, 0, stream>>>(r, l.passes, l.bits, at(l.keys[0]), at(l.vals[0]));
     NAT_LAUNCH_CHECK("embed_sort_small");
@@ -518,25 +609,32 @@ int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable,
       const uint32_t* keys = pass ? at(l.keys[src]) : nullptr;
       const uint32_t* vals = pass ? at(l.vals[src]) : nullptr;
       const int dst = pass ? src ^ 1 : 0;
-      count_kernel<<<l.blocks, kThreads, 0, stream>>>(r, keys, digit, at(l.hist));
-      NAT_LAUNCH_CHECK("embed_count");
-      prefix_kernel<<<((1 << l.bits) + kWarps - 1) / kWarps, kThreads, 0, stream>>>(at(l.hist), l.blocks, 1 << l.bits,
-                                                                                   at(l.total));
-      NAT_LAUNCH_CHECK("embed_prefix");
-      scatter_kernel<<<l.blocks, kThreads, 0, stream>>>(r, keys, vals, digit, at(l.hist), at(l.total), at(l.keys[dst]),
-                                                       at(l.vals[dst]));
-      NAT_LAUNCH_CHECK("embed_scatter");
+      if (pass == 0) {  // behind whatever wrote the ids: not before that has ended
+        count_kernel<<<l.blocks, kThreads, 0, stream>>>(r, keys, digit, at(l.hist));
+        NAT_LAUNCH_CHECK("embed_count");
+      } else {
+        s = launch_after(count_kernel, dim3(l.blocks), kThreads, 0, stream, "embed_count", r, keys, digit, at(l.hist));
+        if (s != NAT_OK) return s;
+      }
+      s = launch_after(prefix_kernel, dim3(((1 << l.bits) + kWarps - 1) / kWarps), kThreads, 0, stream, "embed_prefix",
+                       at(l.hist), l.blocks, 1 << l.bits, at(l.total));
+      if (s != NAT_OK) return s;
+      s = launch_after(scatter_kernel, dim3(l.blocks), kThreads, 0, stream, "embed_scatter", r, keys, vals, digit,
+                       (const uint32_t*)at(l.hist), (const uint32_t*)at(l.total), at(l.keys[dst]), at(l.vals[dst]));
+      if (s != NAT_OK) return s;
       src = dst;
     }
   }
   SumArgs a{r, at(l.keys[src]), at(l.vals[src]), dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), 32,
             l.tiles, p.scale, p.accumulate != 0};
   while (a.rows_per_block > 1 && p.V / a.rows_per_block < 148 * 8) a.rows_per_block >>= 1;
-  sum_kernel<T><<<(unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block), kThreads, 0, stream>>>(a);
-  NAT_LAUNCH_CHECK("embed_sum");
+  s = launch_after(sum_kernel<T>, dim3((unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block)), kThreads, 0,
+                   stream, "embed_sum", a);
+  if (s != NAT_OK) return s;
   if (l.tiles > 0) {
-    join_kernel<<<dim3((unsigned)l.tiles, (unsigned)((p.d + 255) / 256)), kThreads, 0, stream>>>(a);
-    NAT_LAUNCH_CHECK("embed_join");
+    s = launch_after(join_kernel, dim3((unsigned)((l.tiles + kJoinTiles - 1) / kJoinTiles), (unsigned)((p.d + 255) / 256)),
+                     kThreads, 0, stream, "embed_join", a);
+    if (s != NAT_OK) return s;
   }
   return NAT_OK;
 }
