@@ -107,7 +107,8 @@ def test_qknorm_refusals():
 
 def test_qknorm_workspace_grows_with_cap():
     sizes = [nat.nat_qknorm_workspace_bytes(nat.qknorm_params(4, 2, 128, torch.bfloat16), c) for c in (0, 1, 9, 4096, 10 ** 6)]
-    assert sizes == sorted(sizes) and 0 < sizes[-1] < 1 << 20
+    # sums of the weights' gradients: less than a hundredth of the rows, which are 1536 bytes each
+    assert sizes == sorted(sizes) and 0 < sizes[-1] < 15.36 * 10 ** 6
 
 
 # ---------------------------------------------------------------------------- experts
