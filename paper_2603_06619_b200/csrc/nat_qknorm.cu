@@ -171,7 +171,7 @@ __device__ __forceinline__ void read_chunks(const uint4* slot, bool in_a, bool i
 template <typename T, int LANES, bool BWD, bool NORM>
 __device__ __forceinline__ void step(const nat_qknorm_params& p, const Slot& slot, const uint4* from, bool on, T* to,
                                      const float* w, float inv_d, const float (&c)[8], const float (&s)[8],
-                                     float2 (&dw)[2][kPairs]) {
+                                     float2 (&dwq)[2][kPairs], float2 (&dwk)[2][kPairs], bool key) {
   constexpr int kTensor = 2 * (sizeof(Raw<T>) / 16) * 32;
   const bool in_a = on && slot.in, in_b = in_a && slot.b >= 0;
   float2 a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
@@ -196,8 +196,23 @@ __device__ __forceinline__ void step(const nat_qknorm_params& p, const Slot& slo
       for (int i = 0; i < kPairs; ++i) {
         x[i] = mul2(x[i], both(rstd));
         y[i] = mul2(y[i], both(rstd));
-        dw[0][i] = fma2(a[i], x[i], dw[0][i]);
-        dw[1][i] = fma2(b[i], y[i], dw[1][i]);
+      }
+      // query and key heads have sums of their own
+      if (key) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          dwk[0][i] = fma2(a[i], x[i], dwk[0][i]);
+          dwk[1][i] = fma2(b[i], y[i], dwk[1][i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          dwq[0][i] = fma2(a[i], x[i], dwq[0][i]);
+          dwq[1][i] = fma2(b[i], y[i], dwq[1][i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
         a[i] = mul2(a[i], wa[i]);
         b[i] = mul2(b[i], wb[i]);
       }
@@ -235,22 +250,33 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
   const int64_t each = n / total, more = n % total;
   const int64_t begin = mine * each + min(mine, more), end = begin + each + (mine < more ? 1 : 0);
 
-  // steps of a token: its query heads, kGroups at a time, then its key heads
-  const int q_steps = (p.n_heads + kGroups - 1) / kGroups, steps = q_steps + (p.n_kv_heads + kGroups - 1) / kGroups;
+  // Steps of a token: its query heads and right behind them its key heads, kGroups at a time (one with both kinds in
+  // place of two: 230,000 tokens of 2 and 1 heads forward 227 -> 182 us).
+  const int heads = p.n_heads + p.n_kv_heads, steps = (heads + kGroups - 1) / kGroups;
+  struct Head {
+    bool key, in;
+    int64_t at;  // its first element in a token's row
+  };
+  auto head_of = [&](int i) -> Head {
+    const int h = i * kGroups + group;
+    const bool key = h >= p.n_heads;
+    return {key, h < heads, (int64_t)(key ? h - p.n_heads : h) * D};
+  };
   uint4* own = slots + (size_t)warp * kStages * P::kSlot + lane;
   int64_t ahead_t = begin;
   int ahead_step = 0, ahead_stage = 0;
   auto fetch = [&]() {  // the next step that is not on its way yet
     if (ahead_t < end) {
-      const bool key = ahead_step >= q_steps;
-      const int h = (key ? ahead_step - q_steps : ahead_step) * kGroups + group;
-      if (slot.in && h < (key ? p.n_kv_heads : p.n_heads)) {
+      const Head h = head_of(ahead_step);
+      if (slot.in && h.in) {
         uint4* to = own + ahead_stage * P::kSlot;
         if (kReadsX)
-          copy_chunks<T>(to, (const T*)(key ? args.k : args.q) + ahead_t * (key ? p.k_stride : p.q_stride) + h * D, slot);
+          copy_chunks<T>(to, (const T*)(h.key ? args.k : args.q) + ahead_t * (h.key ? p.k_stride : p.q_stride) + h.at, slot);
         if (BWD)
-          copy_chunks<T>(to + P::kSlot / 2, (const T*)(key ? args.dk_out : args.dq_out) +
-                                                ahead_t * (key ? p.k_out_stride : p.q_out_stride) + h * D, slot);
+          copy_chunks<T>(to + P::kSlot / 2,
+                         (const T*)(h.key ? args.dk_out : args.dq_out) +
+                             ahead_t * (h.key ? p.k_out_stride : p.q_out_stride) + h.at,
+                         slot);
       }
       if (++ahead_step == steps) {
         ahead_step = 0;
@@ -317,17 +343,10 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
       copies_wait<kStages - 1>();
       const uint4* from = own + stage * P::kSlot;
       stage = stage + 1 == kStages ? 0 : stage + 1;
-      if (i < q_steps) {
-        const int h = i * kGroups + group;
-        step<T, LANES, BWD, NORM>(p, slot, from, h < p.n_heads,
-                                  (T*)args.q_to + t * (BWD ? p.q_stride : p.q_out_stride) + h * D, weights[0], inv_d, c,
-                                  s, dwq);
-      } else {
-        const int h = (i - q_steps) * kGroups + group;
-        step<T, LANES, BWD, NORM>(p, slot, from, h < p.n_kv_heads,
-                                  (T*)args.k_to + t * (BWD ? p.k_stride : p.k_out_stride) + h * D, weights[1], inv_d, c,
-                                  s, dwk);
-      }
+      const Head h = head_of(i);
+      T* to = (T*)(h.key ? args.k_to : args.q_to) + h.at +
+              t * (BWD ? (h.key ? p.k_stride : p.q_stride) : (h.key ? p.k_out_stride : p.q_out_stride));
+      step<T, LANES, BWD, NORM>(p, slot, from, h.in, to, weights[h.key ? 1 : 0], inv_d, c, s, dwq, dwk, h.key);
     }
   }
   if (BWD && NORM) {
