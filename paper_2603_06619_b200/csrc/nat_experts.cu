@@ -15,7 +15,7 @@ constexpr int kPlanThreads = 1024;
 // number): the weights' gradient takes its tiles in that order, so that those in flight together are of about the
 // same length and the shortest come last.
 __global__ void __launch_bounds__(kPlanThreads)
-plan_kernel(const int32_t* offsets, int E, int64_t cap, int tile_rows, Head* head, int32_t* order, Tile* tiles) {
+plan_kernel(const int32_t* offsets, int E, int64_t cap, int tile_rows, Head* head, Tile* by_rows, Tile* tiles) {
   release_secondary();
   __shared__ int rows[kMaxExperts];
   __shared__ int sums[kPlanThreads / 32];
@@ -50,7 +50,7 @@ plan_kernel(const int32_t* offsets, int E, int64_t cap, int tile_rows, Head* hea
   if (e < E) {
     int before = 0;
     for (int f = 0; f < E; ++f) before += rows[f] > rows[e] || (rows[f] == rows[e] && f < e);
-    order[before] = e;
+    by_rows[before] = {e, lo, hi, 0};
   }
 }
 
@@ -120,7 +120,7 @@ int product(const Args& a, const Layout& l, Product which) {
 }
 
 int launch_plan(const Args& a, const Layout& l, int tile_rows) {
-  plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(a.offsets, a.p.n_experts, a.cap, tile_rows, head(a), order(a, l),
+  plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(a.offsets, a.p.n_experts, a.cap, tile_rows, head(a), by_rows(a, l),
                                                 tiles(a, l));
   NAT_LAUNCH_CHECK("experts_plan");
   return NAT_OK;
@@ -131,11 +131,11 @@ int launch_plan(const Args& a, const Layout& l, int tile_rows) {
 Layout layout(const nat_experts_params& p, int64_t cap) {
   Layout l;
   const bool f32 = p.dtype == NAT_F32;
-  for (int i = 0; i < 2; ++i) l.tile_rows[i] = f32 ? kF32Tile : bf16_tile_rows(p, (Product)i, cap);
+  for (int i = 0; i < 3; ++i) l.tile_rows[i] = f32 ? kF32Tile : bf16_tile_rows(p, (Product)i, cap);
   // an expert's last tile may be part full: at most one extra tile for each
   l.most_tiles = cap / min(l.tile_rows[0], l.tile_rows[1]) + p.n_experts;
   // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows of an average expert at least.
-  const int64_t rows = f32 ? kF32Tile : kDwRowsBf16, cols = f32 ? kF32Tile : kDwColsBf16;
+  const int64_t rows = l.tile_rows[kDw], cols = f32 ? kF32Tile : kBf16Cols;
   const int64_t units = p.n_experts * ((p.n_out + rows - 1) / rows) * ((p.n_in + cols - 1) / cols);
   const int64_t fit = (f32 ? 296 : 74) / units, worth = cap / p.n_experts / 512;
   l.parts = (int)max((int64_t)1, min(fit, worth));
@@ -145,7 +145,7 @@ Layout layout(const nat_experts_params& p, int64_t cap) {
     at = align_up(at + bytes, 256);
     return o;
   };
-  l.order_off = take(sizeof(int32_t) * p.n_experts);
+  l.by_rows_off = take(sizeof(Tile) * p.n_experts);
   l.tiles_off = take(sizeof(Tile) * l.most_tiles);
   l.partial_off = take(l.parts > 1 ? sizeof(float) * (size_t)l.parts * p.n_experts * p.n_out * p.n_in : 0);
   l.total = at;

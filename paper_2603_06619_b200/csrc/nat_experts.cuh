@@ -43,24 +43,24 @@ __device__ __forceinline__ void expert_rows(const int32_t* offsets, int e, int64
 }
 
 struct Layout {
-  int tile_rows[2];           // of a tile of the list, for kFwd and kDx
+  int tile_rows[3];           // of a tile, for each product: the rows' tiles (kFwd, kDx), or the weights' (kDw)
   int64_t most_tiles;
   int parts;                  // into which the rows are cut for the weights' gradient
-  size_t order_off, tiles_off, partial_off, total;
+  size_t by_rows_off, tiles_off, partial_off, total;
 };
 Layout layout(const nat_experts_params& p, int64_t cap);
 
 inline Head* head(const Args& a) { return reinterpret_cast<Head*>(a.workspace); }
-inline int32_t* order(const Args& a, const Layout& l) {
-  return reinterpret_cast<int32_t*>((char*)a.workspace + l.order_off);
+// All rows of each expert, by falling number.
+inline Tile* by_rows(const Args& a, const Layout& l) {
+  return reinterpret_cast<Tile*>((char*)a.workspace + l.by_rows_off);
 }
 inline Tile* tiles(const Args& a, const Layout& l) { return reinterpret_cast<Tile*>((char*)a.workspace + l.tiles_off); }
 inline float* partial(const Args& a, const Layout& l) {
   return reinterpret_cast<float*>((char*)a.workspace + l.partial_off);
 }
 
-// Rows and columns of a tile of the weights' gradient.
-constexpr int kDwRowsBf16 = 512, kDwColsBf16 = 256, kF32Tile = 128;
+constexpr int kBf16Cols = 256, kF32Tile = 128;  // columns of a tile; rows and columns in float32
 
 // Rows of the k-blocks [lo, hi) that part `part` of `parts` takes of `blocks`.
 __host__ __device__ inline void part_range(int blocks, int part, int parts, int& lo, int& hi) {

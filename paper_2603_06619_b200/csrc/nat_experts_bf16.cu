@@ -18,6 +18,9 @@
 
 #include "nat_experts.cuh"
 #include "nat_tc.cuh"
+#ifndef DW_WIDE
+#define DW_WIDE 1024
+#endif
 
 namespace nat {
 namespace experts {
@@ -28,20 +31,21 @@ constexpr int kBox = 64 * 64 * 2;            // bytes of a 64 x 64 box of an ope
 constexpr int kTmemCols = 512;
 constexpr int kGroup = 8;                    // row tiles that go through the columns together
 
-template <int SUBS>
+// Shared memory: stages of A and half of B, and 4 KB pieces of finished rows for each warp that writes out, from which
+// they leave by TMA: two for kDw, whose epilogue nothing hides, one elsewhere.
+template <int WHICH, int SUBS>
 struct Ring {
   static constexpr int kABytes = SUBS * BM * BK * 2, kBBytes = (BN / 2) * BK * 2, kStage = kABytes + kBBytes;
-  static constexpr int kNum = 192 * 1024 / kStage;
-  static constexpr int kStaging = 4 * SUBS * 4096;
+  static constexpr int kPieces = WHICH == kDw ? 2 : 1;
+  static constexpr int kStaging = 4 * SUBS * kPieces * 4096;
+  static constexpr int kNum = (226 * 1024 - 1024 - 256 - kStaging) / kStage;
   static constexpr int kThreads = 64 + 128 * SUBS;
   static constexpr size_t kSmem = (size_t)kNum * kStage + kStaging + 1024 /*alignment*/ + 256 /*barriers*/;
 };
 
 struct TcArgs {
   Head* head;
-  const Tile* tiles;
-  const int32_t *order, *offsets;
-  int64_t cap;
+  const Tile* tiles;           // row tiles (kFwd, kDx), or the experts by falling number of rows (kDw)
   int E, n_cols, k_blocks;     // columns of the result; blocks of the contraction (kFwd, kDx)
   int m_tiles;                 // kDw: tiles along n_out
   int parts;
@@ -56,32 +60,27 @@ struct Unit {
   int kb_lo, kb_hi, slice;
 };
 
-template <int WHICH>
-__device__ __forceinline__ int unit_count(const TcArgs& a) {
-  const int n_tiles = (a.n_cols + BN - 1) / BN;
-  if (WHICH == kDw) return a.head->broken ? 0 : a.E * a.m_tiles * n_tiles * a.parts;
-  return (int)a.head->tiles * n_tiles;
-}
-
 // kFwd, kDx: groups of kGroup row tiles go through the columns, the row tile varying fastest, so that the pairs at
 // work share few row tiles and few column tiles through L2.  kDw: the experts in the list's order.
-template <int WHICH>
-__device__ __forceinline__ Unit decode(const TcArgs& a, int u) {
+template <int WHICH, int SUBS>
+__device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
   const int n_tiles = (a.n_cols + BN - 1) / BN;
   Unit w;
   if (WHICH == kDw) {
     const int per = a.m_tiles * n_tiles, rank = u / (per * a.parts), in = u - rank * per * a.parts;
     const int part = in / per, tile = in - part * per;
-    w.expert = a.order[rank];
-    w.m0 = tile / n_tiles * (kDwRowsBf16);
+    const Tile t = a.tiles[rank];
+    w.expert = t.expert;
+    w.lo = t.lo;
+    w.hi = t.hi;
+    w.m0 = tile / n_tiles * (2 * BM * SUBS);
     w.n0 = (tile - tile / n_tiles * n_tiles) * BN;
-    expert_rows(a.offsets, w.expert, a.cap, w.lo, w.hi);
     part_range((w.hi - w.lo + BK - 1) / BK, part, a.parts, w.kb_lo, w.kb_hi);
     w.slice = part * a.E + w.expert;
     return w;
   }
-  const int rows = (int)a.head->tiles, grp = u / (kGroup * n_tiles), in = u - grp * kGroup * n_tiles;
-  const int left = min(kGroup, rows - grp * kGroup);
+  const int grp = u / (kGroup * n_tiles), in = u - grp * kGroup * n_tiles;
+  const int left = max(1, min(kGroup, rows - grp * kGroup));
   const int n = in / left;
   const Tile t = a.tiles[grp * kGroup + in - n * left];
   w.expert = t.expert;
@@ -145,10 +144,10 @@ __device__ __forceinline__ uint32_t pack(uint32_t lo, uint32_t hi) {
 }
 
 template <int WHICH, int SUBS>
-__global__ void __launch_bounds__(Ring<SUBS>::kThreads, 1)
-experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_c, const TcArgs a) {
-  using R = Ring<SUBS>;
+__global__ void __launch_bounds__(Ring<WHICH, SUBS>::kThreads, 1)
+experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
+               const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c, const TcArgs a) {
+  using R = Ring<WHICH, SUBS>;
   constexpr int kNS = R::kNum;
   constexpr uint32_t kAcc = 2 / SUBS;  // accumulators: two tiles in flight, or one
   constexpr bool kAcross = WHICH == kDw;                    // A is contiguous across the contraction
@@ -187,6 +186,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::fence_proxy_async();
     tc::prefetch_tensormap(&map_a);
     tc::prefetch_tensormap(&map_b);
+    if (WHICH != kDw) tc::prefetch_tensormap(&map_a32);
     tc::prefetch_tensormap(&map_c);
   }
   if (warp == 1) {
@@ -199,8 +199,12 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   tc::fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   wait_for_primary();  // the list of tiles is there
-  const int units = unit_count<WHICH>(a);
+  const int row_tiles = (int)a.head->tiles;
+  const int units = (a.n_cols + BN - 1) / BN * (WHICH == kDw ? (a.head->broken ? 0 : a.E * a.m_tiles * a.parts) : row_tiles);
 
+  // The entry of the unit after `u` is asked for before u is worked on: it costs a round trip to L2.
+  auto first_unit = [&]() { return decode<WHICH, SUBS>(a, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
+  auto unit_after = [&](int u) { return decode<WHICH, SUBS>(a, row_tiles, u + stride < units ? u + stride : u); };
   // Whether the second block of 256 rows of a tile holds any (kFwd, kDx with SUBS = 2).
   auto second = [&](const Unit& w) { return WHICH == kDw || w.hi - w.lo > 2 * BM; };
   // A gradient that is added to takes nothing from an expert without rows.
@@ -213,11 +217,12 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x ? 1 : 0) != 0; };
     uint32_t it = 0, tail_phase = 0u, peer_phase = 0u;  // peer_phase: a bit a stage
     bool ok = true;
+    Unit next = first_unit();
     for (int u = unit0; ok && u < units; u += stride) {
-      const Unit w = decode<WHICH>(a, u);
+      const Unit w = next;
+      next = unit_after(u);
       if (skipped(w)) continue;
       const int n0 = w.n0 + rank * (BN / 2);
-      const bool both = SUBS == 2 && second(w);
       for (int kb = w.kb_lo; kb < w.kb_hi; ++kb, ++it) {
         const int s = it % kNS;
         ok = all(tc::mbar_wait(&empty_bar[s], ((it / kNS) & 1u) ^ 1u, abort_flag));
@@ -227,7 +232,9 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // both CTAs' loads count on the even CTA's barrier, which its producer arms with the bytes of the pair
         const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full_bar[s]), 0);
         if (WHICH == kDw) {
-          const int t = w.lo + kb * BK, len = min(BK, w.hi - t);
+          // from the last block to the first: the one that is not full, whose way takes longest, is then asked for while
+          // the tile before is still at work
+          const int t = w.lo + (w.kb_hi - 1 - (kb - w.kb_lo)) * BK, len = min(BK, w.hi - t);
           if (lane == 0) {
             if (len < BK) tc::mbar_arrive_expect_tx(tail_bar, R::kStage);
             else if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kStage);
@@ -243,10 +250,10 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             ok = all(tc::mbar_wait(tail_bar, tail_phase, abort_flag));
             if (!ok) break;
             tail_phase ^= 1u;
-            for (int i = lane; i < (2 * SUBS + 2) * (BK - len) * 8; i += 32) {
-              const int box = i / ((BK - len) * 8), in = i - box * (BK - len) * 8;
-              *reinterpret_cast<uint4*>(a_dst + box * kBox + len * 128 + in * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
+#pragma unroll
+            for (int j = 0; j < 2 * SUBS + 2; ++j)
+              for (int i = len * 8 + lane; i < BK * 8; i += 32)
+                *reinterpret_cast<uint4*>(a_dst + j * kBox + i * 16) = make_uint4(0u, 0u, 0u, 0u);
             tc::fence_proxy_async();
             __syncwarp();
             if (rank == 1) {
@@ -259,11 +266,27 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
           }
         } else if (lane == 0) {
-          if (rank == 0)
-            tc::mbar_arrive_expect_tx(&full_bar[s],
-                                      2 * (R::kBBytes + (SUBS == 2 && !both ? R::kABytes / 2 : R::kABytes)));
-          tc::tma_load_2d_pair(a_dst, &map_a, bar, kb * BK, w.lo + rank * BM);
-          if (both) tc::tma_load_2d_pair(a_dst + R::kABytes / 2, &map_a, bar, kb * BK, w.lo + 2 * BM + rank * BM);
+          // of A only what has rows of the tile: whole blocks of 128 rows, or pieces of 32 of a smaller one (the rest of
+          // the stage is what it was: rows of the accumulator that nobody writes out)
+          const int rows = w.hi - w.lo;
+          auto pieces = [&](int first) { return max(0, min(4, (rows - first + 31) / 32)); };
+          if (rank == 0) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 2 * SUBS; ++i) n += pieces(i * BM);
+            tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kBBytes + n * 32 * BK * 2);
+          }
+#pragma unroll
+          for (int sub = 0; sub < SUBS; ++sub) {
+            const int first = sub * 2 * BM + rank * BM, n = pieces(first);
+            uint8_t* dst = a_dst + sub * BM * BK * 2;
+            if (n == 4) {
+              tc::tma_load_2d_pair(dst, &map_a, bar, kb * BK, w.lo + first);
+            } else {
+              for (int i = 0; i < n; ++i)
+                tc::tma_load_2d_pair(dst + i * 32 * BK * 2, &map_a32, bar, kb * BK, w.lo + first + i * 32);
+            }
+          }
           if (WHICH == kFwd) {
             load_3d_pair(b_dst, &map_b, bar, kb * BK, n0, w.expert);
           } else {
@@ -285,8 +308,10 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (lane == 0 && rank == 0) {
       uint32_t it = 0, tcount = 0;
       bool ok = true;
+      Unit next = first_unit();
       for (int u = unit0; ok && u < units; u += stride) {
-        const Unit w = decode<WHICH>(a, u);
+        const Unit w = next;
+        next = unit_after(u);
         if (skipped(w)) continue;
         const int subs = SUBS == 2 && second(w) ? 2 : 1;
         const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
@@ -324,12 +349,15 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     // ------------------------------------------------ epilogue (four warps for each block of 128 rows)
     const int q = warp & 3;           // tensor-memory lanes that this warp may read
     const int sub = (warp - 2) >> 2;
-    uint8_t* stage = staging + (warp - 2) * 4096;
+    uint8_t* const pieces = staging + (warp - 2) * R::kPieces * 4096;
+    uint32_t turn = 0;
     const int in_tile = sub * 2 * BM + rank * BM + q * 32;  // first of the warp's rows
     uint32_t tcount = 0;
     bool ok = true;
+    Unit next = first_unit();
     for (int u = unit0; ok && u < units; u += stride) {
-      const Unit w = decode<WHICH>(a, u);
+      const Unit w = next;
+      next = unit_after(u);
       if (skipped(w)) continue;
       const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
       ++tcount;
@@ -346,7 +374,8 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           uint32_t v[32];
           tc::tmem_ld32_issue(taddr + c * 32, v);
           tc::tmem_ld_wait(v);
-          if (lane == 0) tc::bulk_wait_read_all();  // the previous piece has left the block
+          uint8_t* stage = pieces + (turn++ & 1u) * 4096;
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the piece before the last has left
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < 8; ++j)
@@ -379,6 +408,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           }
           if (valid == 32) {
             // through the warp's block of shared memory, whole lines at a time
+            uint8_t* stage = pieces;
             if (lane == 0) tc::bulk_wait_read_all();
             __syncwarp();
 #pragma unroll
@@ -478,11 +508,11 @@ int pairs(int* out) {
     int s = require_sm100();
     if (s != NAT_OK) return s;
     NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, SUBS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)Ring<SUBS>::kSmem));
+                                  (int)Ring<WHICH, SUBS>::kSmem));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(148);
-    cfg.blockDim = dim3(Ring<SUBS>::kThreads);
-    cfg.dynamicSmemBytes = Ring<SUBS>::kSmem;
+    cfg.blockDim = dim3(Ring<WHICH, SUBS>::kThreads);
+    cfg.dynamicSmemBytes = Ring<WHICH, SUBS>::kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -499,15 +529,15 @@ int pairs(int* out) {
 }
 
 template <int WHICH, int SUBS>
-int launch(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const TcArgs& t, int64_t most_units,
-           cudaStream_t stream) {
+int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb, const CUtensorMap& mc, const TcArgs& t,
+           int64_t most_units, cudaStream_t stream) {
   int slots = 0;
   int s = pairs<WHICH, SUBS>(&slots);
   if (s != NAT_OK) return s;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * min(most_units, (int64_t)slots)));
-  cfg.blockDim = dim3(Ring<SUBS>::kThreads);
-  cfg.dynamicSmemBytes = Ring<SUBS>::kSmem;
+  cfg.blockDim = dim3(Ring<WHICH, SUBS>::kThreads);
+  cfg.dynamicSmemBytes = Ring<WHICH, SUBS>::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -518,27 +548,26 @@ int launch(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, 
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, SUBS>, ma, mb, mc, t));
+  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, SUBS>, ma, ma32, mb, mc, t));
   return NAT_OK;
 }
 
 }  // namespace
 
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
-  (void)p; (void)which; (void)cap;
-  return 2 * BM;
+  if (which != kDw) return 2 * BM;
+  // A tile of 512 rows of the result takes a quarter fewer operand bytes, but leaves no second accumulator in whose
+  // shadow it is written out: worth it where the experts have rows enough (see the table at bf16_product).
+  return cap / p.n_experts >= DW_WIDE ? 4 * BM : 2 * BM;
 }
 
 int bf16_product(const Args& a, const Layout& l, Product which) {
   const nat_experts_params& p = a.p;
-  CUtensorMap ma, mb, mc;
+  CUtensorMap ma, ma32, mb, mc;
   int s;
   TcArgs t{};
   t.head = head(a);
-  t.tiles = tiles(a, l);
-  t.order = order(a, l);
-  t.offsets = a.offsets;
-  t.cap = a.cap;
+  t.tiles = which == kDw ? by_rows(a, l) : tiles(a, l);
   t.E = p.n_experts;
   t.parts = which == kDw ? l.parts : 1;
   t.accumulate = p.accumulate != 0;
@@ -549,23 +578,26 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
                          : map_gradient(&mc, p, a.dw, p.n_experts)) != NAT_OK)
       return s;
     t.n_cols = p.n_in;
-    t.m_tiles = (p.n_out + kDwRowsBf16 - 1) / kDwRowsBf16;
+    t.m_tiles = (p.n_out + l.tile_rows[kDw] - 1) / l.tile_rows[kDw];
     const int64_t units = (int64_t)t.E * t.m_tiles * ((p.n_in + BN - 1) / BN) * t.parts;
-    return launch<kDw, 2>(ma, mb, mc, t, units, a.stream);
+    return l.tile_rows[kDw] == 4 * BM ? launch<kDw, 2>(ma, ma, mb, mc, t, units, a.stream)
+                                      : launch<kDw, 1>(ma, ma, mb, mc, t, units, a.stream);
   }
   const bool fwd = which == kFwd;
   const void *in = fwd ? a.x : a.dy;
   void* out = fwd ? a.y : a.dx;
   const int k = fwd ? p.n_in : p.n_out, n = fwd ? p.n_out : p.n_in;
+  const int64_t in_stride = fwd ? p.x_stride : p.y_stride;
   t.n_cols = n;
   t.k_blocks = (k + BK - 1) / BK;
   t.rows_out = (__nv_bfloat16*)out;
   t.rows_stride = fwd ? p.y_stride : p.x_stride;
-  if ((s = map_rows(&ma, in, k, a.cap, fwd ? p.x_stride : p.y_stride, BM)) != NAT_OK) return s;
+  if ((s = map_rows(&ma, in, k, a.cap, in_stride, BM)) != NAT_OK) return s;
+  if ((s = map_rows(&ma32, in, k, a.cap, in_stride, 32)) != NAT_OK) return s;
   if ((s = map_weights(&mb, p, a.w, fwd ? BN / 2 : BK)) != NAT_OK) return s;
   if ((s = map_rows(&mc, out, n, a.cap, t.rows_stride, 32)) != NAT_OK) return s;
   const int64_t units = l.most_tiles * ((n + BN - 1) / BN);
-  return fwd ? launch<kFwd, 1>(ma, mb, mc, t, units, a.stream) : launch<kDx, 1>(ma, mb, mc, t, units, a.stream);
+  return fwd ? launch<kFwd, 1>(ma, ma32, mb, mc, t, units, a.stream) : launch<kDx, 1>(ma, ma32, mb, mc, t, units, a.stream);
 }
 
 }  // namespace experts

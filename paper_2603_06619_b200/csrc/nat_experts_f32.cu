@@ -21,10 +21,8 @@ struct F32Args {
   int m_size;                            // kDw: rows of the result
   int E, parts;
   bool accumulate;
-  const int32_t *order, *offsets;
-  int64_t cap;
   const Head* head;
-  const Tile* tiles;
+  const Tile* tiles;  // row tiles (kFwd, kDx), or the experts by falling number of rows (kDw)
 };
 
 // A slice [kK][kT] of an operand: rows or columns [o0, o_end) by [k0, k_end) of the contraction, zero outside.
@@ -67,14 +65,14 @@ __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
   if (WHICH == kDw) {
     if (g.head->broken) return;
     const int m_tiles = (g.m_size + kT - 1) / kT, rank = blockIdx.x / m_tiles;
-    expert = g.order[rank];
+    const Tile t = g.tiles[rank];
+    expert = t.expert;
     m0 = (blockIdx.x - rank * m_tiles) * kT;
     m_end = g.m_size;
-    int lo, hi, b_lo, b_hi;
-    expert_rows(g.offsets, expert, g.cap, lo, hi);
-    part_range((hi - lo + kK - 1) / kK, blockIdx.z, g.parts, b_lo, b_hi);
-    k0 = lo + b_lo * kK;
-    k_end = min(lo + b_hi * kK, hi);
+    int b_lo, b_hi;
+    part_range((t.hi - t.lo + kK - 1) / kK, blockIdx.z, g.parts, b_lo, b_hi);
+    k0 = t.lo + b_lo * kK;
+    k_end = min(t.lo + b_hi * kK, t.hi);
     slice = blockIdx.z * g.E + expert;
   } else {
     if (blockIdx.x >= g.head->tiles) return;
@@ -148,11 +146,8 @@ int f32_product(const Args& a, const Layout& l, Product which) {
   F32Args g{};
   g.E = p.n_experts;
   g.parts = 1;
-  g.order = order(a, l);
-  g.offsets = a.offsets;
-  g.cap = a.cap;
   g.head = head(a);
-  g.tiles = tiles(a, l);
+  g.tiles = which == kDw ? by_rows(a, l) : tiles(a, l);
   g.accumulate = p.accumulate != 0;
   if (which == kDw) {
     g.a = (const float*)a.dy;
