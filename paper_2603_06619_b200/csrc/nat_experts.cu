@@ -23,11 +23,10 @@ plan_kernel(const int32_t* offsets, int E, int64_t cap, int tile_rows, Head* hea
   int lo = 0, hi = 0, fault = 0;
   if (e < E) {
     expert_rows(offsets, e, cap, lo, hi);
-    const int a = offsets[e], b = offsets[e + 1];
-    fault = (a < 0 || b < a ? 2 : 0) | ((int64_t)b > cap ? 1 : 0);
+    fault = (int)offsets_fault(offsets, e, cap);
     rows[e] = hi - lo;
   }
-  const bool broken = __syncthreads_or(fault & 2), any = __syncthreads_or(fault);
+  const bool broken = __syncthreads_or(fault & kBroken), any = __syncthreads_or(fault);
   const int count = (hi - lo + tile_rows - 1) / tile_rows;
   int run = count;
 #pragma unroll
@@ -119,7 +118,9 @@ int product(const Args& a, const Layout& l, Product which) {
   return a.p.dtype == NAT_F32 ? f32_product(a, l, which) : bf16_product(a, l, which);
 }
 
+// Not for float32 with rows, whose blocks find their tiles and write the status word themselves.
 int launch_plan(const Args& a, const Layout& l, int tile_rows) {
+  if (a.p.dtype == NAT_F32 && a.cap > 0) return NAT_OK;
   plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(a.offsets, a.p.n_experts, a.cap, tile_rows, head(a), by_rows(a, l),
                                                 tiles(a, l));
   NAT_LAUNCH_CHECK("experts_plan");

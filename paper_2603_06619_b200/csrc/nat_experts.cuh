@@ -42,6 +42,14 @@ __device__ __forceinline__ void expert_rows(const int32_t* offsets, int e, int64
   if (hi < lo) hi = lo;
 }
 
+// What a call finds wrong with the offsets of expert e: kTooMany, more rows than the matrices hold (the surplus is left
+// out), or kBroken, offsets that do not ascend (nothing is computed).
+enum { kTooMany = 1, kBroken = 2 };
+__device__ __forceinline__ unsigned offsets_fault(const int32_t* offsets, int e, int64_t cap) {
+  const int a = offsets[e], b = offsets[e + 1];
+  return (a < 0 || b < a ? kBroken : 0) | ((int64_t)b > cap ? kTooMany : 0);
+}
+
 struct Layout {
   int tile_rows[3];           // of a tile, for each product: the rows' tiles (kFwd, kDx), or the weights' (kDw)
   int64_t most_tiles;
@@ -60,6 +68,7 @@ inline float* partial(const Args& a, const Layout& l) {
   return reinterpret_cast<float*>((char*)a.workspace + l.partial_off);
 }
 
+constexpr int kFewRows = 64;                    // of a tile of the kernel for few rows
 constexpr int kBf16Cols = 256, kF32Tile = 128;  // columns of a tile; rows and columns in float32
 
 // Rows of the k-blocks [lo, hi) that part `part` of `parts` takes of `blocks`.
@@ -72,6 +81,7 @@ __host__ __device__ inline void part_range(int blocks, int part, int parts, int&
 // Tiles of the kernel that `which` of a bfloat16 call takes; see its definition.
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap);
 int bf16_product(const Args& a, const Layout& l, Product which);
+int few_product(const Args& a, const Layout& l, Product which);
 int f32_product(const Args& a, const Layout& l, Product which);
 
 }  // namespace experts

@@ -14,20 +14,13 @@
 // contraction, and a row too many would be added in: where an expert's last block of 64 rows is not full, the loading
 // warp of each CTA waits for its own part of it, writes zeros over the rows behind (both operands': a weight of zero
 // would not hide an infinity), and the odd CTA tells the even one before the MMA warp is let on.
-#include <atomic>
-
-#include "nat_experts.cuh"
-#include "nat_tc.cuh"
-#ifndef DW_WIDE
-#define DW_WIDE 1024
-#endif
+#include "nat_experts_tc.cuh"
 
 namespace nat {
 namespace experts {
 namespace {
 
-constexpr int BM = 128, BN = 256, BK = 64;
-constexpr int kBox = 64 * 64 * 2;            // bytes of a 64 x 64 box of an operand that is contiguous across the contraction
+constexpr int BN = kBf16Cols;
 constexpr int kTmemCols = 512;
 constexpr int kGroup = 8;                    // row tiles that go through the columns together
 
@@ -138,11 +131,6 @@ __device__ __forceinline__ void put_3d(const CUtensorMap* map, const void* src, 
                  : "memory");
 }
 
-__device__ __forceinline__ uint32_t pack(uint32_t lo, uint32_t hi) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
-  return *reinterpret_cast<uint32_t*>(&v);
-}
-
 template <int WHICH, int SUBS>
 __global__ void __launch_bounds__(Ring<WHICH, SUBS>::kThreads, 1)
 experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
@@ -205,8 +193,6 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   // The entry of the unit after `u` is asked for before u is worked on: it costs a round trip to L2.
   auto first_unit = [&]() { return decode<WHICH, SUBS>(a, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
   auto unit_after = [&](int u) { return decode<WHICH, SUBS>(a, row_tiles, u + stride < units ? u + stride : u); };
-  // Whether the second block of 256 rows of a tile holds any (kFwd, kDx with SUBS = 2).
-  auto second = [&](const Unit& w) { return WHICH == kDw || w.hi - w.lo > 2 * BM; };
   // A gradient that is added to takes nothing from an expert without rows.
   auto skipped = [&](const Unit& w) {
     return WHICH == kDw && a.accumulate && a.parts == 1 && w.kb_lo == w.kb_hi;
@@ -313,7 +299,6 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const Unit w = next;
         next = unit_after(u);
         if (skipped(w)) continue;
-        const int subs = SUBS == 2 && second(w) ? 2 : 1;
         const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
         ++tcount;
         if (!tc::mbar_wait(&tempty_bar[acc], aph ^ 1u, abort_flag)) { ok = false; break; }
@@ -332,7 +317,6 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                                            : tc::smem_desc_sw128(b_base + kk * 32, 16, 1024);
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
-              if (sub >= subs) break;
               const uint32_t a_sub = a_base + sub * (BM * BK * 2);
               const uint64_t adesc = kAcross ? tc::smem_desc_sw128(a_sub + kk * 2048, kBox, 1024)
                                              : tc::smem_desc_sw128(a_sub + kk * 32, 16, 1024);
@@ -403,8 +387,8 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           tc::tmem_ld_pin(rb);
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            packed[j] = pack(ra[2 * j], ra[2 * j + 1]);
-            packed[16 + j] = pack(rb[2 * j], rb[2 * j + 1]);
+            packed[j] = pack_bf16(ra[2 * j], ra[2 * j + 1]);
+            packed[16 + j] = pack_bf16(rb[2 * j], rb[2 * j + 1]);
           }
           if (valid == 32) {
             // through the warp's block of shared memory, whole lines at a time
@@ -450,44 +434,6 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // --------------------------------------------------------------------------- host
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-int encode(CUtensorMap* map, CUtensorMapDataType type, int dims, uintptr_t base, const cuuint64_t* size,
-           const cuuint64_t* pitch, const cuuint32_t* box) {
-  static std::atomic<EncodeTiledFn> cached{nullptr};
-  EncodeTiledFn fn = cached.load(std::memory_order_relaxed);
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    NAT_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found));
-    if (found != cudaDriverEntryPointSuccess || !p)
-      return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-    fn = reinterpret_cast<EncodeTiledFn>(p);
-    cached.store(fn, std::memory_order_relaxed);
-  }
-  const cuuint32_t one[3] = {1, 1, 1};
-  const CUresult r = fn(map, type, (cuuint32_t)dims, reinterpret_cast<void*>(base), size, pitch, box, one,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
-  return NAT_OK;
-}
-
-// Rows of a matrix [rows, cols] of bfloat16: boxes of 64 columns.
-int map_rows(CUtensorMap* map, const void* base, int cols, int64_t rows, int64_t stride, int box_rows) {
-  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uintptr_t)base, size, pitch, box);
-}
-// The experts' weights [E, n_out, n_in]: boxes of 64 columns by box_rows of one expert.
-int map_weights(CUtensorMap* map, const nat_experts_params& p, const void* w, int box_rows) {
-  const cuuint64_t size[3] = {(cuuint64_t)p.n_in, (cuuint64_t)p.n_out, (cuuint64_t)p.n_experts};
-  const cuuint64_t pitch[2] = {(cuuint64_t)p.n_in * 2, (cuuint64_t)p.n_in * p.n_out * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (uintptr_t)w, size, pitch, box);
-}
 // Their gradient, or the parts' [slices, n_out, n_in] in float32: pieces of 32 x 32.
 int map_gradient(CUtensorMap* map, const nat_experts_params& p, const float* dw, int64_t slices) {
   const cuuint64_t size[3] = {(cuuint64_t)p.n_in, (cuuint64_t)p.n_out, (cuuint64_t)slices};
@@ -501,12 +447,10 @@ template <int WHICH, int SUBS>
 int pairs(int* out) {
   static std::atomic<int> cached[64];
   int dev = 0;
-  NAT_CUDA(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= 64) return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", dev);
+  int s = device_index(&dev);
+  if (s != NAT_OK) return s;
   int n = cached[dev].load(std::memory_order_relaxed);
   if (n == 0) {
-    int s = require_sm100();
-    if (s != NAT_OK) return s;
     NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, SUBS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)Ring<WHICH, SUBS>::kSmem));
     cudaLaunchConfig_t cfg = {};
@@ -554,15 +498,41 @@ int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb
 
 }  // namespace
 
+// Average rows of an expert (by the capacity, which is what the host knows) up to which the forward product and the rows'
+// gradient go to the kernel for few rows.  us, pairs / few, forward and rows' gradient:
+//   rows an expert                   8         16        31        62
+//   32 experts, 4096 x 1536     90 78, 82 74   94 84, 88 78   99 84, 92 92   106 105, 101 110
+//   128 experts, 2048 x 768     94 76, 87 76        -        101 86, 95 90   106 102, 105 110
+//   8 experts, 4096 x 4096      64 57, 61 58        -         69 59, 70 64    72 80, 73 86
+constexpr int64_t kFew = 32;
+// And from which the weights' gradient takes tiles of 512 rows in place of 256: 312 rows (128 experts, 2048 x 768) 321 us
+// with 512, 286 with 256; 1000 (16, 2048 x 2048) 164, 180; 1875 (64, 2048 x 1024) 536, 631; 4688 (64, 2048 x 1536)
+// 1654, 2021; 7500 (8, 4096 x 4096) 1623, 2054.
+constexpr int64_t kDwWide = 768;
+
+int device_index(int* dev) {
+  static std::atomic<bool> fits[64];
+  NAT_CUDA(cudaGetDevice(dev));
+  if (*dev < 0 || *dev >= 64)
+    return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", *dev);
+  if (!fits[*dev].load(std::memory_order_relaxed)) {
+    const int s = require_sm100();
+    if (s != NAT_OK) return s;
+    fits[*dev].store(true, std::memory_order_relaxed);
+  }
+  return NAT_OK;
+}
+
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
-  if (which != kDw) return 2 * BM;
+  if (which != kDw) return cap / p.n_experts <= kFew ? kFewRows : 2 * BM;
   // A tile of 512 rows of the result takes a quarter fewer operand bytes, but leaves no second accumulator in whose
-  // shadow it is written out: worth it where the experts have rows enough (see the table at bf16_product).
-  return cap / p.n_experts >= DW_WIDE ? 4 * BM : 2 * BM;
+  // shadow it is written out: worth it where the experts have rows enough.
+  return cap / p.n_experts >= kDwWide ? 4 * BM : 2 * BM;
 }
 
 int bf16_product(const Args& a, const Layout& l, Product which) {
   const nat_experts_params& p = a.p;
+  if (which != kDw && l.tile_rows[which] == kFewRows) return few_product(a, l, which);
   CUtensorMap ma, ma32, mb, mc;
   int s;
   TcArgs t{};

@@ -21,8 +21,9 @@ struct F32Args {
   int m_size;                            // kDw: rows of the result
   int E, parts;
   bool accumulate;
-  const Head* head;
-  const Tile* tiles;  // row tiles (kFwd, kDx), or the experts by falling number of rows (kDw)
+  const int32_t* offsets;
+  int64_t cap;
+  Head* head;
 };
 
 // A slice [kK][kT] of an operand: rows or columns [o0, o_end) by [k0, k_end) of the contraction, zero outside.
@@ -57,31 +58,83 @@ struct Slice {
   }
 };
 
+// Tile number `index` of all row tiles in the experts' order, found by one warp (the same in every lane; empty where there
+// are fewer), and what is wrong with the offsets.  A few hundred cycles for every 32 experts: less than a kernel
+// in front that lists the tiles.
+__device__ __forceinline__ Tile find_tile(const F32Args& g, int64_t index, unsigned* faults) {
+  const int lane = threadIdx.x & 31;
+  int64_t before = 0;
+  Tile found{0, 0, 0, 0};
+  *faults = 0u;
+  for (int base = 0; base < g.E; base += 32) {
+    const int e = base + lane;
+    int lo = 0, hi = 0;
+    unsigned fault = 0u;
+    if (e < g.E) {
+      expert_rows(g.offsets, e, g.cap, lo, hi);
+      fault = offsets_fault(g.offsets, e, g.cap);
+    }
+    *faults |= __reduce_or_sync(0xFFFFFFFFu, fault);
+    const int count = (hi - lo + kT - 1) / kT;
+    int run = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+      if (lane >= o) run += left;
+    }
+    const int64_t first = before + run - count;
+    const unsigned who = __ballot_sync(0xFFFFFFFFu, index >= first && index < first + count);
+    if (who) {
+      const int from = __ffs(who) - 1;
+      found.expert = base + from;
+      found.lo = __shfl_sync(0xFFFFFFFFu, lo, from) + (int)(index - __shfl_sync(0xFFFFFFFFu, first, from)) * kT;
+      found.hi = min(found.lo + kT, __shfl_sync(0xFFFFFFFFu, hi, from));
+    }
+    before += __shfl_sync(0xFFFFFFFFu, run, 31);
+  }
+  return found;
+}
+
 template <int WHICH>
 __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
   __shared__ __align__(16) float sa[2][kK][kLd], sb[2][kK][kLd];
+  __shared__ Tile shared_tile;
+  __shared__ unsigned shared_faults;
+  if (threadIdx.x < 32) {
+    unsigned faults;
+    const Tile t = find_tile(g, blockIdx.x, &faults);
+    if (threadIdx.x == 0) {
+      shared_tile = t;
+      shared_faults = faults;
+      if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
+        g.head->status = faults ? NAT_DEV_CAPACITY : 0u;
+        g.head->broken = (faults & kBroken) ? 1u : 0u;
+      }
+    }
+  }
+  __syncthreads();
+  if (shared_faults & kBroken) return;
   int expert, m0, m_end, k0, k_end, slice = 0;
   const int n0 = blockIdx.y * kT;
   if (WHICH == kDw) {
-    if (g.head->broken) return;
-    const int m_tiles = (g.m_size + kT - 1) / kT, rank = blockIdx.x / m_tiles;
-    const Tile t = g.tiles[rank];
-    expert = t.expert;
-    m0 = (blockIdx.x - rank * m_tiles) * kT;
+    const int m_tiles = (g.m_size + kT - 1) / kT;
+    expert = blockIdx.x / m_tiles;
+    m0 = (blockIdx.x - expert * m_tiles) * kT;
     m_end = g.m_size;
-    int b_lo, b_hi;
-    part_range((t.hi - t.lo + kK - 1) / kK, blockIdx.z, g.parts, b_lo, b_hi);
-    k0 = t.lo + b_lo * kK;
-    k_end = min(t.lo + b_hi * kK, t.hi);
+    int lo, hi, b_lo, b_hi;
+    expert_rows(g.offsets, expert, g.cap, lo, hi);
+    part_range((hi - lo + kK - 1) / kK, blockIdx.z, g.parts, b_lo, b_hi);
+    k0 = lo + b_lo * kK;
+    k_end = min(lo + b_hi * kK, hi);
     slice = blockIdx.z * g.E + expert;
   } else {
-    if (blockIdx.x >= g.head->tiles) return;
-    const Tile t = g.tiles[blockIdx.x];
+    const Tile t = shared_tile;
     expert = t.expert;
     m0 = t.lo;
     m_end = t.hi;
     k0 = 0;
     k_end = g.k_size;
+    if (m0 >= m_end) return;
   }
   const float* b = g.b + (WHICH == kDw ? 0 : expert * g.b_expert);
   Slice<WHICH != kDw> na;
@@ -146,8 +199,9 @@ int f32_product(const Args& a, const Layout& l, Product which) {
   F32Args g{};
   g.E = p.n_experts;
   g.parts = 1;
+  g.offsets = a.offsets;
+  g.cap = a.cap;
   g.head = head(a);
-  g.tiles = which == kDw ? by_rows(a, l) : tiles(a, l);
   g.accumulate = p.accumulate != 0;
   if (which == kDw) {
     g.a = (const float*)a.dy;
