@@ -569,7 +569,8 @@ int nat_qknorm_bwd(const nat_qknorm_params* params /* host */, int32_t B, const 
  * Matrix products of rows that are grouped by expert.  Rows [offsets[e], offsets[e+1]) of x belong to expert e, whose
  * weights are w_e [n_out, n_in]:
  *   y_r = w_e x_r                                                          (forward)
- *   dx_r = w_e^T dy_r,   dw_e = sum over the expert's rows of dy_r x_r^T    (backward; dx or dw may be NULL)
+ *   dx_r = w_e^T dy_r,   dw_e = sum over the expert's rows of dy_r x_r^T    (backward; dx or dw may be NULL, and then
+ *   w or x, which that one reads, too)
  * offsets int32 [n_experts + 1] on the device, ascending; an expert may have no rows (its dw is then zero).  Rows before
  * offsets[0], at or after offsets[n_experts], or at or after cap are neither read into a result nor written; offsets
  * beyond cap, or that do not ascend (then nothing is computed), raise NAT_DEV_CAPACITY in the status word at the head of

@@ -98,10 +98,10 @@ int check(const char* who, const nat_experts_params* p, int64_t cap) {
 }
 
 int check_call(const char* who, const Args& a, size_t workspace_bytes, bool bwd, Layout* l) {
-  const void* needed[4] = {a.x, a.w, bwd ? a.dy : a.y, a.offsets};
+  if (!a.offsets) return fail(NAT_ERR_INVALID_ARG, "%s: offsets is null", who);
   // without rows the row matrices are not looked at
-  for (int i = a.cap > 0 ? 0 : 3; i < 4; ++i)
-    if (!needed[i]) return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (a.cap > 0 && (((!bwd || a.dw) && !a.x) || ((!bwd || a.dx) && !a.w) || (bwd ? !a.dy : !a.y)))
+    return fail(NAT_ERR_INVALID_ARG, "%s: null pointer", who);
   if (bwd && !a.dx && !a.dw) return fail(NAT_ERR_INVALID_ARG, "%s: neither dx nor dw", who);
   if (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.dy | (uintptr_t)a.y | (uintptr_t)a.dx | (uintptr_t)a.dw) & 15u)
     return fail(NAT_ERR_INVALID_ARG, "%s: matrices must be 16-byte aligned", who);
@@ -132,13 +132,14 @@ int launch_plan(const Args& a, const Layout& l, int tile_rows) {
 Layout layout(const nat_experts_params& p, int64_t cap) {
   Layout l;
   const bool f32 = p.dtype == NAT_F32;
-  for (int i = 0; i < 3; ++i) l.tile_rows[i] = f32 ? kF32Tile : bf16_tile_rows(p, (Product)i, cap);
+  for (int i = 0; i < 3; ++i) l.tile_rows[i] = f32 ? f32_tile(p, (Product)i, cap) : bf16_tile_rows(p, (Product)i, cap);
   // an expert's last tile may be part full: at most one extra tile for each
   l.most_tiles = cap / min(l.tile_rows[0], l.tile_rows[1]) + p.n_experts;
-  // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows of an average expert at least.
-  const int64_t rows = l.tile_rows[kDw], cols = f32 ? kF32Tile : kBf16Cols;
+  // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows (float32: 128) of an average expert at
+  // least.
+  const int64_t rows = l.tile_rows[kDw], cols = f32 ? rows : kBf16Cols;
   const int64_t units = p.n_experts * ((p.n_out + rows - 1) / rows) * ((p.n_in + cols - 1) / cols);
-  const int64_t fit = (f32 ? 296 : 74) / units, worth = cap / p.n_experts / 512;
+  const int64_t fit = (f32 ? 296 : 74) / units, worth = cap / p.n_experts / (f32 ? 128 : 512);
   l.parts = (int)max((int64_t)1, min(fit, worth));
   size_t at = 256;
   auto take = [&](size_t bytes) {

@@ -1,8 +1,11 @@
 // Products grouped by expert in plain 32-bit arithmetic.
 //
-// 256 threads share a 128 x 128 tile of the result, eight rows by eight columns each, and go through the contraction 16
-// at a time: the next slices of both operands are on their way in registers while the present ones, in shared
-// memory with the contraction slowest, feed 64 multiply-adds a thread from four 16-byte reads.
+// 256 threads share a T x T tile of the result, R x R elements each (T = 16 R), and go through the contraction 16 at a
+// time, three slices of both operands ahead by asynchronous copies; four steps of the contraction are 2 R reads of
+// 16 bytes for 2 R^2 packed multiply-adds.  T = 128, or 64 for small problems, which wait for memory rather than
+// compute.  8000 rows over four experts, 512 x 512: forward 124 us (34 TFLOP/s), both gradients 260.
+#include <atomic>
+
 #include "nat_experts.cuh"
 #include "nat_f32x2.cuh"
 
@@ -10,7 +13,7 @@ namespace nat {
 namespace experts {
 namespace {
 
-constexpr int kT = kF32Tile, kK = 16, kThreads = 256, kLd = kT + 4;
+constexpr int kK = 16, kThreads = 256, kStages = 4;
 
 struct F32Args {
   const float *a, *b;
@@ -26,42 +29,55 @@ struct F32Args {
   Head* head;
 };
 
-// A slice [kK][kT] of an operand: rows or columns [o0, o_end) by [k0, k_end) of the contraction, zero outside.
-// ALONG: the matrix is contiguous along the contraction.
-template <bool ALONG>
-struct Slice {
-  float4 v[2];
-  __device__ __forceinline__ void load(const float* m, int64_t stride, int o0, int o_end, int k0, int k_end) {
+// Slices of an operand on their way: T rows or columns of the result by kK of the contraction, zero outside
+// [o0, o_end) and [k0, k_end).  ALONG: the matrix, and the slice, are contiguous along the contraction.
+template <bool ALONG, int R>
+struct Operand {
+  static constexpr int T = 16 * R, kLd = (ALONG ? kK : T) + 4, kFloats = (ALONG ? T : kK) * kLd;
+  float* at;
+  const float* m;
+  int64_t stride;
+  int o0, o_end, k_end;
+  __device__ __forceinline__ void fetch(int stage, int k0) const {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int o = ALONG ? o0 + (int)threadIdx.x / 4 + 64 * i : o0 + (int)threadIdx.x % 32 * 4;
-      const int k = ALONG ? k0 + (int)threadIdx.x % 4 * 4 : k0 + (int)threadIdx.x / 32 + 8 * i;
+    for (int i = 0; i < R / 4; ++i) {
+      const int c = threadIdx.x + i * kThreads;  // chunk of four
+      const int r = ALONG ? c / (kK / 4) : c / (T / 4), q = (ALONG ? c % (kK / 4) : c % (T / 4)) * 4;
+      const int o = o0 + (ALONG ? r : q), k = k0 + (ALONG ? q : r);
       // sizes along the contiguous dimension are multiples of four, so that four elements are in or out together
       const bool in = o < o_end && k < k_end;
-      v[i] = in ? *reinterpret_cast<const float4*>(m + (ALONG ? (int64_t)o * stride + k : (int64_t)k * stride + o))
-                : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float* src = in ? m + (ALONG ? (int64_t)o * stride + k : (int64_t)k * stride + o) : m;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                       (uint32_t)__cvta_generic_to_shared(at + stage * kFloats + r * kLd + q)),
+                   "l"(src), "r"(in ? 16 : 0)
+                   : "memory");
     }
   }
-  __device__ __forceinline__ void put(float (*s)[kLd]) const {
+  // v[j][i]: step j of four from kk on, element i of the thread's R (runs of four, 64 apart), t its place among 16
+  __device__ __forceinline__ void get(int stage, int kk, int t, float (&v)[4][R]) const {
+    const float* s = at + stage * kFloats;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < R; ++i) {
       if (ALONG) {
-        const int o = threadIdx.x / 4 + 64 * i, k = threadIdx.x % 4 * 4;
-        s[k][o] = v[i].x;
-        s[k + 1][o] = v[i].y;
-        s[k + 2][o] = v[i].z;
-        s[k + 3][o] = v[i].w;
-      } else {
-        *reinterpret_cast<float4*>(&s[threadIdx.x / 32 + 8 * i][threadIdx.x % 32 * 4]) = v[i];
+        const float4 x = *reinterpret_cast<const float4*>(s + (i / 4 * 64 + i % 4 * 16 + t) * kLd + kk);
+        v[0][i] = x.x; v[1][i] = x.y; v[2][i] = x.z; v[3][i] = x.w;
+      } else if (i % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 x = *reinterpret_cast<const float4*>(s + (kk + j) * kLd + i / 4 * 64 + t * 4);
+          v[j][i] = x.x; v[j][i + 1] = x.y; v[j][i + 2] = x.z; v[j][i + 3] = x.w;
+        }
       }
     }
   }
+  // the place in the tile of the thread's element i
+  static __device__ __forceinline__ int place(int i, int t) { return ALONG ? i / 4 * 64 + i % 4 * 16 + t : i / 4 * 64 + t * 4 + i % 4; }
 };
 
 // Tile number `index` of all row tiles in the experts' order, found by one warp (the same in every lane; empty where there
 // are fewer), and what is wrong with the offsets.  A few hundred cycles for every 32 experts: less than a kernel
 // in front that lists the tiles.
-__device__ __forceinline__ Tile find_tile(const F32Args& g, int64_t index, unsigned* faults) {
+__device__ __forceinline__ Tile find_tile(const F32Args& g, int64_t index, int tile_rows, unsigned* faults) {
   const int lane = threadIdx.x & 31;
   int64_t before = 0;
   Tile found{0, 0, 0, 0};
@@ -75,7 +91,7 @@ __device__ __forceinline__ Tile find_tile(const F32Args& g, int64_t index, unsig
       fault = offsets_fault(g.offsets, e, g.cap);
     }
     *faults |= __reduce_or_sync(0xFFFFFFFFu, fault);
-    const int count = (hi - lo + kT - 1) / kT;
+    const int count = (hi - lo + tile_rows - 1) / tile_rows;
     int run = count;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -87,22 +103,25 @@ __device__ __forceinline__ Tile find_tile(const F32Args& g, int64_t index, unsig
     if (who) {
       const int from = __ffs(who) - 1;
       found.expert = base + from;
-      found.lo = __shfl_sync(0xFFFFFFFFu, lo, from) + (int)(index - __shfl_sync(0xFFFFFFFFu, first, from)) * kT;
-      found.hi = min(found.lo + kT, __shfl_sync(0xFFFFFFFFu, hi, from));
+      found.lo = __shfl_sync(0xFFFFFFFFu, lo, from) + (int)(index - __shfl_sync(0xFFFFFFFFu, first, from)) * tile_rows;
+      found.hi = min(found.lo + tile_rows, __shfl_sync(0xFFFFFFFFu, hi, from));
     }
     before += __shfl_sync(0xFFFFFFFFu, run, 31);
   }
   return found;
 }
 
-template <int WHICH>
+template <int WHICH, int R>
 __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
-  __shared__ __align__(16) float sa[2][kK][kLd], sb[2][kK][kLd];
+  using A = Operand<WHICH != kDw, R>;
+  using B = Operand<WHICH == kFwd, R>;
+  constexpr int kT = A::T;
+  extern __shared__ __align__(16) float smem[];
   __shared__ Tile shared_tile;
   __shared__ unsigned shared_faults;
   if (threadIdx.x < 32) {
     unsigned faults;
-    const Tile t = find_tile(g, blockIdx.x, &faults);
+    const Tile t = find_tile(g, blockIdx.x, kT, &faults);
     if (threadIdx.x == 0) {
       shared_tile = t;
       shared_faults = faults;
@@ -136,63 +155,112 @@ __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
     k_end = g.k_size;
     if (m0 >= m_end) return;
   }
-  const float* b = g.b + (WHICH == kDw ? 0 : expert * g.b_expert);
-  Slice<WHICH != kDw> na;
-  Slice<WHICH == kFwd> nb;
+  const A oa{smem, g.a, g.a_stride, m0, m_end, k_end};
+  const B ob{smem + kStages * A::kFloats, g.b + (WHICH == kDw ? 0 : expert * g.b_expert), g.b_stride, n0, g.n_cols, k_end};
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-  float2 acc[8][4];
+  float2 acc[R][R / 2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = both(0.f);
-  na.load(g.a, g.a_stride, m0, m_end, k0, k_end);
-  nb.load(b, g.b_stride, n0, g.n_cols, k0, k_end);
-  int turn = 0;
-  for (int k = k0; k < k_end; k += kK, turn ^= 1) {
-    na.put(sa[turn]);
-    nb.put(sb[turn]);
-    __syncthreads();  // and the other buffers are free: all threads are past their last reads
-    if (k + kK < k_end) {
-      na.load(g.a, g.a_stride, m0, m_end, k + kK, k_end);
-      nb.load(b, g.b_stride, n0, g.n_cols, k + kK, k_end);
+    for (int j = 0; j < R / 2; ++j) acc[i][j] = both(0.f);
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (k0 + i * kK < k_end) {
+      oa.fetch(i, k0 + i * kK);
+      ob.fetch(i, k0 + i * kK);
     }
-#pragma unroll
-    for (int kk = 0; kk < kK; ++kk) {
-      // a thread's rows and columns are two runs of four, 64 apart
-      const float4 a0 = *reinterpret_cast<const float4*>(&sa[turn][kk][ty * 4]);
-      const float4 a1 = *reinterpret_cast<const float4*>(&sa[turn][kk][64 + ty * 4]);
-      const float4 b0 = *reinterpret_cast<const float4*>(&sb[turn][kk][tx * 4]);
-      const float4 b1 = *reinterpret_cast<const float4*>(&sb[turn][kk][64 + tx * 4]);
-      const float x[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
-      const float2 y[4] = {make_float2(b0.x, b0.y), make_float2(b0.z, b0.w), make_float2(b1.x, b1.y),
-                           make_float2(b1.z, b1.w)};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fma2(both(x[i]), y[j], acc[i][j]);
-    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  int stage = 0;
+  for (int k = k0; k < k_end; k += kK) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncthreads();  // the slice is there for all, and all are done with the one that the next copies replace
+    const int ahead = k + (kStages - 1) * kK, to = stage == 0 ? kStages - 1 : stage - 1;
+    if (ahead < k_end) {
+      oa.fetch(to, ahead);
+      ob.fetch(to, ahead);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+    for (int kk = 0; kk < kK; kk += 4) {
+      float x[4][R], y[4][R];
+      oa.get(stage, kk, ty, x);
+      ob.get(stage, kk, tx, y);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int c = 0; c < R / 2; ++c) {
+            if (WHICH == kFwd) {  // neighbouring columns come in different registers: packing them costs more (124 us, 178)
+              acc[i][c].x = fmaf(x[j][i], y[j][2 * c], acc[i][c].x);
+              acc[i][c].y = fmaf(x[j][i], y[j][2 * c + 1], acc[i][c].y);
+            } else {
+              acc[i][c] = fma2(both(x[j][i]), make_float2(y[j][2 * c], y[j][2 * c + 1]), acc[i][c]);
+            }
+          }
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   float* c = g.c + (int64_t)slice * g.c_slice;
+  const bool add = WHICH == kDw && g.accumulate && g.parts == 1;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = m0 + i / 4 * 64 + ty * 4 + i % 4;
+  for (int i = 0; i < R; ++i) {
+    const int r = m0 + A::place(i, ty);
     if (r >= m_end) continue;
+    float* row = c + (int64_t)r * g.c_stride;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int col = n0 + j * 64 + tx * 4;
-      if (col >= g.n_cols) continue;
-      float4* at = reinterpret_cast<float4*>(c + (int64_t)r * g.c_stride + col);
-      float4 v = make_float4(acc[i][2 * j].x, acc[i][2 * j].y, acc[i][2 * j + 1].x, acc[i][2 * j + 1].y);
-      if (WHICH == kDw && g.accumulate && g.parts == 1) {
-        const float4 old = *at;
-        v = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
+    for (int j = 0; j < R; j += 4) {
+      const float v[4] = {acc[i][j / 2].x, acc[i][j / 2].y, acc[i][j / 2 + 1].x, acc[i][j / 2 + 1].y};
+      if (WHICH == kFwd) {  // a thread's columns are 16 apart
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int col = n0 + B::place(j + e, tx);
+          if (col < g.n_cols) row[col] = v[e];
+        }
+      } else {
+        const int col = n0 + B::place(j, tx);
+        if (col >= g.n_cols) continue;
+        float4* at = reinterpret_cast<float4*>(row + col);
+        const float4 old = add ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
+        *at = add ? make_float4(old.x + v[0], old.y + v[1], old.z + v[2], old.w + v[3]) : make_float4(v[0], v[1], v[2], v[3]);
       }
-      *at = v;
     }
   }
 }
 
+template <int WHICH, int R>
+int launch(const F32Args& g, int64_t m_tiles, cudaStream_t stream) {
+  constexpr size_t smem = kStages * (Operand<WHICH != kDw, R>::kFloats + Operand<WHICH == kFwd, R>::kFloats) * sizeof(float);
+  static std::atomic<uint64_t> allowed{0};  // a bit for each device whose shared-memory limit is raised
+  int dev = 0;
+  NAT_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", dev);
+  if (smem > 48 * 1024 && !(allowed.load(std::memory_order_relaxed) >> dev & 1u)) {
+    NAT_CUDA(cudaFuncSetAttribute(f32_kernel<WHICH, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  const dim3 grid((unsigned)m_tiles, (unsigned)((g.n_cols + 16 * R - 1) / (16 * R)), (unsigned)g.parts);
+  f32_kernel<WHICH, R><<<grid, kThreads, smem, stream>>>(g);
+  NAT_LAUNCH_CHECK("experts_f32");
+  return NAT_OK;
+}
+template <int WHICH>
+int launch(const F32Args& g, const Layout& l, int64_t m_tiles, cudaStream_t stream) {
+  return l.tile_rows[WHICH] == 128 ? launch<WHICH, 8>(g, m_tiles, stream) : launch<WHICH, 4>(g, m_tiles, stream);
+}
+
 }  // namespace
+
+int f32_tile(const nat_experts_params& p, Product which, int64_t cap) {
+  // tiles of 64 where those of 128 would leave half of the multiprocessors idle: 508 rows over 16 experts, 408 x 112
+  // forward 48 us with 128, 25 with 64; 2000 rows, 1024 x 1024 (128 tiles) 111, 191
+  auto tiles = [](int64_t n) { return (n + 127) / 128; };
+  const int64_t n = which == kDw ? p.n_experts * tiles(p.n_out) * tiles(p.n_in)
+                                 : tiles(cap) * tiles(which == kFwd ? p.n_out : p.n_in);
+  return n < 148 / 2 ? 64 : 128;
+}
 
 int f32_product(const Args& a, const Layout& l, Product which) {
   const nat_experts_params& p = a.p;
@@ -214,11 +282,7 @@ int f32_product(const Args& a, const Layout& l, Product which) {
     g.n_cols = p.n_in;
     g.m_size = p.n_out;
     g.parts = l.parts;
-    const dim3 grid((unsigned)(p.n_experts * ((p.n_out + kT - 1) / kT)), (unsigned)((p.n_in + kT - 1) / kT),
-                    (unsigned)l.parts);
-    f32_kernel<kDw><<<grid, kThreads, 0, a.stream>>>(g);
-    NAT_LAUNCH_CHECK("experts_dw_f32");
-    return NAT_OK;
+    return launch<kDw>(g, l, p.n_experts * ((p.n_out + l.tile_rows[kDw] - 1) / l.tile_rows[kDw]), a.stream);
   }
   const bool fwd = which == kFwd;
   g.a = (const float*)(fwd ? a.x : a.dy);
@@ -230,11 +294,8 @@ int f32_product(const Args& a, const Layout& l, Product which) {
   g.c_stride = fwd ? p.y_stride : p.x_stride;
   g.n_cols = fwd ? p.n_out : p.n_in;
   g.k_size = fwd ? p.n_in : p.n_out;
-  const dim3 grid((unsigned)l.most_tiles, (unsigned)((g.n_cols + kT - 1) / kT));
-  if (fwd) f32_kernel<kFwd><<<grid, kThreads, 0, a.stream>>>(g);
-  else f32_kernel<kDx><<<grid, kThreads, 0, a.stream>>>(g);
-  NAT_LAUNCH_CHECK("experts_f32");
-  return NAT_OK;
+  const int64_t m_tiles = a.cap / l.tile_rows[which] + p.n_experts;
+  return fwd ? launch<kFwd>(g, l, m_tiles, a.stream) : launch<kDx>(g, l, m_tiles, a.stream);
 }
 
 }  // namespace experts
