@@ -121,6 +121,19 @@ def test_experts_rows_cut_into_parts(loads, accumulate, dtype):
     e.check()
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_experts_sums_longer_than_an_accumulator_takes(accumulate):
+    """Tiles enough that the rows are not cut into parts; sums of thousands of rows are added up in pieces, in order."""
+    e = Experts([7000, 10, 6300, 0, 1, 200, 0, 12500], 520, 1032, torch.bfloat16, seed=12, accumulate=accumulate)
+    assert nat.nat_experts_workspace_bytes(e.params, e.cap) < 1 << 20
+    e.check()
+    first = e.dw.clone()
+    for _ in range(3):
+        e.dw.copy_(e.old)
+        e.bwd(dx=False)
+        assert torch.equal(first, e.dw)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_experts_either_gradient_alone(dtype):
     a, b = (Experts([90, 200, 3], 72, 136, DT[dtype], seed=5) for _ in range(2))
