@@ -57,7 +57,8 @@ __device__ __forceinline__ Raw<float> load_kept(const float* p) {
   return {__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1)};
 }
 
-template <typename T>
+// PLAIN: a scale of one; the rows are moved as they are (at the board's power limit the arithmetic would cost time).
+template <typename T, bool PLAIN>
 __global__ void __launch_bounds__(kThreads, 6)
 lookup_kernel(const T* __restrict__ table, Rows r, T* __restrict__ x, int d, int tpr_log2, float scale) {
   constexpr int A = kAhead<T>;
@@ -76,11 +77,13 @@ lookup_kernel(const T* __restrict__ table, Rows r, T* __restrict__ x, int d, int
 #pragma unroll
     for (int u = 0; u < A; ++u) {
       if (c + u * stride >= d) break;
-      float2 v[kPairs];
-      rows::widen(raw[u], v);
+      if (!PLAIN || !known) {
+        float2 v[kPairs];
+        rows::widen(raw[u], v);
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) v[i] = known ? mul2(v[i], both(scale)) : both(__uint_as_float(0x7FC00000u));
-      rows::narrow(v, raw[u]);
+        for (int i = 0; i < kPairs; ++i) v[i] = known ? mul2(v[i], both(scale)) : both(__uint_as_float(0x7FC00000u));
+        rows::narrow(v, raw[u]);
+      }
       rows::store_raw(to + c + u * stride, raw[u]);
     }
   }
@@ -580,8 +583,11 @@ int threads_log2(int d) {
 template <typename T>
 int fwd(const nat_embed_params& p, const void* table, const Rows& r, void* x, cudaStream_t stream) {
   const int tpr_log2 = min(threads_log2(p.d), 5), rpb = kThreads >> tpr_log2;
-  lookup_kernel<T><<<(unsigned)((r.cap + rpb - 1) / rpb), kThreads, 0, stream>>>((const T*)table, r, (T*)x, p.d, tpr_log2,
-                                                                               p.scale);
+  const unsigned blocks = (unsigned)((r.cap + rpb - 1) / rpb);
+  if (p.scale == 1.f)
+    lookup_kernel<T, true><<<blocks, kThreads, 0, stream>>>((const T*)table, r, (T*)x, p.d, tpr_log2, p.scale);
+  else
+    lookup_kernel<T, false><<<blocks, kThreads, 0, stream>>>((const T*)table, r, (T*)x, p.d, tpr_log2, p.scale);
   NAT_LAUNCH_CHECK("embed_lookup");
   return NAT_OK;
 }

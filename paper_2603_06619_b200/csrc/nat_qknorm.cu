@@ -6,8 +6,10 @@
 // that both members of a rotated pair are in one lane; a warp owns a token and walks its heads, so that the angles'
 // sines and cosines are found once a token, each by one of the warp's groups of lanes, and dealt to the others.  A warp
 // takes a run of consecutive tokens and finds its first token's sequence once; its rows are on their way into
-// shared memory three steps ahead.  160,000 tokens of 32 and 8 heads of 128 in bfloat16: forward 479 us, the rate of a
-// plain copy, backward 756 us, 0.99 of it.
+// shared memory three steps ahead.  156,000 tokens of 32 and 8 heads of 128 in bfloat16 forward, one call after the other:
+// 532 us, 0.92 of the copy rate at the board's power limit (a lone call 480 us, 1.02), 160,000 backward 800 us, 0.94.
+// At that limit instructions count: weights and rotation in one (forward), one exchange of two sums for a row (backward)
+// and packed arithmetic took these from 576 and 914 us.
 #include <atomic>
 #include <initializer_list>
 
@@ -68,27 +70,82 @@ __device__ __forceinline__ Slot slot_of(const nat_qknorm_params& p, int lane) {
   return {p.rot_dim + j * kChunk, j + 1 < rest ? p.rot_dim + (j + 1) * kChunk : -1, false, true};
 }
 // Number i of the angle of the lane's e-th pair.
-__device__ __forceinline__ int angle_of(const nat_qknorm_params& p, const Slot& s, int e) {
-  if (!p.interleaved) return s.a + e;
+template <bool INTER>
+__device__ __forceinline__ int angle_of(const Slot& s, int e) {
+  if (!INTER) return s.a + e;
   return e < 4 ? s.a / 2 + e : s.b / 2 + e - 4;
 }
 
-// Turns a lane's eight pairs; sin < 0 of the angle turns back.
-__device__ __forceinline__ void turn(bool interleaved, float2 (&a)[kPairs], float2 (&b)[kPairs], const float (&c)[8],
-                                     const float (&s)[8]) {
-  auto one = [](float& x, float& y, float cs, float sn) {
-    const float t = fmaf(x, cs, -(y * sn));
-    y = fmaf(y, cs, x * sn);
-    x = t;
+__device__ __forceinline__ float2 swapped(float2 x) { return make_float2(x.y, x.x); }
+
+__device__ __forceinline__ void read8(const float* w, float2 (&x)[kPairs]) {
+#pragma unroll
+  for (int i = 0; i < kPairs; i += 2) {
+    const float4 v = *reinterpret_cast<const float4*>(w + 2 * i);
+    x[i] = make_float2(v.x, v.y);
+    x[i + 1] = make_float2(v.z, v.w);
+  }
+}
+
+// Forward, the weights and the rotation of a lane's two chunks in one: each pair of elements becomes
+//   pair own + other across,
+// other being the same pair of the other chunk, or, with INTER, the pair itself the other way round.
+struct Turn {
+  float2 own[2][kPairs], across[2][kPairs];
+};
+template <bool INTER, bool NORM>
+__device__ __forceinline__ void make_turn(Turn& t, const Slot& slot, const float* w, const float (&c)[8], const float (&s)[8]) {
+  float2 wt[2][kPairs];
+  if (NORM) {
+    read8(w + slot.a, wt[0]);
+    read8(w + max(slot.b, 0), wt[1]);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      const float2 cs = INTER ? both(c[4 * k + i]) : make_float2(c[2 * i], c[2 * i + 1]);
+      const float2 sn = INTER ? both(s[4 * k + i]) : make_float2(s[2 * i], s[2 * i + 1]);
+      const float2 self = NORM ? wt[k][i] : both(1.f), over = NORM ? (INTER ? swapped(wt[k][i]) : wt[1 - k][i]) : both(1.f);
+      t.own[k][i] = slot.turns ? (NORM ? mul2(self, cs) : cs) : self;
+      const float2 x = NORM ? mul2(over, sn) : sn;
+      t.across[k][i] = INTER ? make_float2(-x.x, x.y) : k == 0 ? make_float2(-x.x, -x.y) : x;
+    }
+}
+template <bool INTER>
+__device__ __forceinline__ void apply_turn(const Turn& t, bool turns, float2 (&a)[kPairs], float2 (&b)[kPairs]) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    const float2 x = mul2(a[i], t.own[0][i]), y = mul2(b[i], t.own[1][i]);
+    if (turns) {  // not a product with zero: an infinity of the other element stays out
+      const float2 oa = INTER ? swapped(a[i]) : b[i], ob = INTER ? swapped(b[i]) : a[i];
+      a[i] = fma2(oa, t.across[0][i], x);
+      b[i] = fma2(ob, t.across[1][i], y);
+    } else {
+      a[i] = x;
+      b[i] = y;
+    }
+  }
+}
+
+// Backward, the rotation the other way.
+struct Back {
+  float2 c[kPairs], s[kPairs], minus_s[kPairs];  // with INTER: cosines and sines of chunk a's pairs, then of b's
+};
+template <bool INTER>
+__device__ __forceinline__ void turn_back(const Back& t, float2 (&a)[kPairs], float2 (&b)[kPairs]) {
+  auto one = [](float2& x, float cs, float sn) {
+    x = make_float2(fmaf(x.x, cs, x.y * sn), fmaf(x.y, cs, -(x.x * sn)));
   };
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) {
-    if (interleaved) {
-      one(a[i].x, a[i].y, c[i], s[i]);
-      one(b[i].x, b[i].y, c[4 + i], s[4 + i]);
+    if (INTER) {  // c[i] and s[i] hold those of pair i of chunk a and of chunk b
+      one(a[i], t.c[i].x, t.s[i].x);
+      one(b[i], t.c[i].y, t.s[i].y);
     } else {
-      one(a[i].x, b[i].x, c[2 * i], s[2 * i]);
-      one(a[i].y, b[i].y, c[2 * i + 1], s[2 * i + 1]);
+      const float2 x = fma2(b[i], t.s[i], mul2(a[i], t.c[i]));
+      b[i] = fma2(a[i], t.minus_s[i], mul2(b[i], t.c[i]));
+      a[i] = x;
     }
   }
 }
@@ -106,26 +163,14 @@ __device__ __forceinline__ void store(T* row, const Slot& s, bool on, const floa
   }
 }
 
-__device__ __forceinline__ float squares(const float2 (&a)[kPairs], float sum) {
+__device__ __forceinline__ float products(const float2 (&a)[kPairs], const float2 (&x)[kPairs], const float2 (&b)[kPairs],
+                                          const float2 (&y)[kPairs]) {
+  float2 sum = mul2(a[0], x[0]);
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i) sum = fmaf(a[i].x, a[i].x, fmaf(a[i].y, a[i].y, sum));
-  return sum;
-}
-__device__ __forceinline__ float products(const float2 (&a)[kPairs], const float2 (&b)[kPairs], float sum) {
+  for (int i = 1; i < kPairs; ++i) sum = fma2(a[i], x[i], sum);
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i) sum = fmaf(a[i].x, b[i].x, fmaf(a[i].y, b[i].y, sum));
-  return sum;
-}
-template <int LANES>
-__device__ __forceinline__ float over_row(float x) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-  return x;
-}
-
-__device__ __forceinline__ void read8(const float* w, float2 (&x)[kPairs]) {
-#pragma unroll
-  for (int i = 0; i < kPairs; ++i) x[i] = *reinterpret_cast<const float2*>(w + 2 * i);
+  for (int i = 0; i < kPairs; ++i) sum = fma2(b[i], y[i], sum);
+  return sum.x + sum.y;
 }
 
 // Stages of rows on their way into shared memory, and blocks a multiprocessor (see qknorm_kernel).
@@ -133,7 +178,7 @@ template <typename T, bool BWD>
 struct Pipe {
   static constexpr int kTensors = BWD ? 2 : 1, kPieces = sizeof(Raw<T>) / 16;
   static constexpr int kStages = BWD && sizeof(T) == 4 ? 3 : 4;
-  static constexpr int kBlocks = BWD ? 2 : 3;
+  static constexpr int kBlocks = 2;
   static constexpr int kSlot = kTensors * 2 * kPieces * 32;  // 16-byte pieces of a warp and stage
   static constexpr size_t kBytes = (size_t)kWarps * kStages * kSlot * 16;
 };
@@ -167,68 +212,81 @@ __device__ __forceinline__ void read_chunks(const uint4* slot, bool in_a, bool i
   rows::widen(rb, b);
 }
 
-// One step: a head for each group of lanes, from its slots to memory.
-template <typename T, int LANES, bool BWD, bool NORM>
-__device__ __forceinline__ void step(const nat_qknorm_params& p, const Slot& slot, const uint4* from, bool on, T* to,
-                                     const float* w, float inv_d, const float (&c)[8], const float (&s)[8],
-                                     float2 (&dwq)[2][kPairs], float2 (&dwk)[2][kPairs], bool key) {
+// One step: a head for each group of lanes, from its slots to memory.  Forward: x rstd, then weights and rotation.
+template <typename T, int LANES, bool INTER, bool NORM>
+__device__ __forceinline__ void forward_step(float eps, float inv_d, const Slot& slot, const uint4* from, bool on, T* to,
+                                             const Turn& turn) {
+  const bool in_a = on && slot.in, in_b = in_a && slot.b >= 0;
+  float2 a[kPairs], b[kPairs];
+  read_chunks<T>(from, in_a, in_b, a, b);
+  if (NORM) {
+    float sum = products(a, a, b, b);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    const float2 rstd = both(rsqrtf(fmaf(sum, inv_d, eps)));
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      a[i] = mul2(a[i], rstd);
+      b[i] = mul2(b[i], rstd);
+    }
+  }
+  apply_turn<INTER>(turn, slot.turns, a, b);
+  store<T>(to, slot, on, a, b);
+}
+
+// Backward: g turned back, u = g w, and with one exchange of two sums, of x^2 and of u x:
+//   dx = rstd u - x (mean(u x) rstd) rstd rstd,   dw += g (x rstd)
+template <typename T, int LANES, bool INTER, bool NORM>
+__device__ __forceinline__ void backward_step(float eps, float inv_d, const Slot& slot, const uint4* from, bool on, T* to,
+                                              const Back& back, const float* w, float2 (&dwq)[2][kPairs],
+                                              float2 (&dwk)[2][kPairs], bool key) {
   constexpr int kTensor = 2 * (sizeof(Raw<T>) / 16) * 32;
   const bool in_a = on && slot.in, in_b = in_a && slot.b >= 0;
-  float2 a[kPairs], b[kPairs], wa[kPairs], wb[kPairs];
-  read_chunks<T>(BWD ? from + kTensor : from, in_a, in_b, a, b);
-  if (BWD && slot.turns) turn(p.interleaved, a, b, c, s);
+  float2 a[kPairs], b[kPairs];
+  read_chunks<T>(from + kTensor, in_a, in_b, a, b);
+  if (slot.turns) turn_back<INTER>(back, a, b);
   if (NORM) {
-    float2 x[kPairs], y[kPairs];
-    if (BWD) read_chunks<T>(from, in_a, in_b, x, y);
-    const float2(&xa)[kPairs] = BWD ? x : a;
-    const float2(&xb)[kPairs] = BWD ? y : b;
-    const float rstd = rsqrtf(fmaf(over_row<LANES>(squares(xa, squares(xb, 0.f))), inv_d, p.eps));
-    read8(w + slot.a, wa);
-    read8(w + max(slot.b, 0), wb);
-    if (!BWD) {
+    float2 x[kPairs], y[kPairs], ua[kPairs], ub[kPairs];
+    read_chunks<T>(from, in_a, in_b, x, y);
+    read8(w + slot.a, ua);
+    read8(w + max(slot.b, 0), ub);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      ua[i] = mul2(ua[i], a[i]);
+      ub[i] = mul2(ub[i], b[i]);
+    }
+    float square = products(x, x, y, y), dot = products(ua, x, ub, y);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+      square += __shfl_xor_sync(0xFFFFFFFFu, square, o);
+      dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+    }
+    const float rstd = rsqrtf(fmaf(square, inv_d, eps));
+    const float along = -(dot * inv_d * rstd) * rstd * rstd;  // in this order nothing leaves the range before the result
+    // query and key heads have sums of their own
+    if (key) {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        a[i] = mul2(mul2(a[i], both(rstd)), wa[i]);
-        b[i] = mul2(mul2(b[i], both(rstd)), wb[i]);
+        dwk[0][i] = fma2(a[i], mul2(x[i], both(rstd)), dwk[0][i]);
+        dwk[1][i] = fma2(b[i], mul2(y[i], both(rstd)), dwk[1][i]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        x[i] = mul2(x[i], both(rstd));
-        y[i] = mul2(y[i], both(rstd));
-      }
-      // query and key heads have sums of their own
-      if (key) {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-          dwk[0][i] = fma2(a[i], x[i], dwk[0][i]);
-          dwk[1][i] = fma2(b[i], y[i], dwk[1][i]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-          dwq[0][i] = fma2(a[i], x[i], dwq[0][i]);
-          dwq[1][i] = fma2(b[i], y[i], dwq[1][i]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        a[i] = mul2(a[i], wa[i]);
-        b[i] = mul2(b[i], wb[i]);
-      }
-      const float mean = over_row<LANES>(products(a, x, products(b, y, 0.f))) * inv_d;
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        a[i] = mul2(both(rstd), fma2(x[i], both(-mean), a[i]));
-        b[i] = mul2(both(rstd), fma2(y[i], both(-mean), b[i]));
+        dwq[0][i] = fma2(a[i], mul2(x[i], both(rstd)), dwq[0][i]);
+        dwq[1][i] = fma2(b[i], mul2(y[i], both(rstd)), dwq[1][i]);
       }
     }
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      a[i] = fma2(x[i], both(along), mul2(ua[i], both(rstd)));
+      b[i] = fma2(y[i], both(along), mul2(ub[i], both(rstd)));
+    }
   }
-  if (!BWD && slot.turns) turn(p.interleaved, a, b, c, s);
   store<T>(to, slot, on, a, b);
 }
 
-template <typename T, int LANES, bool BWD, bool NORM>
+template <typename T, int LANES, bool BWD, bool INTER, bool NORM>
 __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kernel(const Args args) {
   using P = Pipe<T, BWD>;
   constexpr int kGroups = 32 / LANES, kStages = P::kStages;
@@ -248,22 +306,23 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
   const int64_t n = row_count(args);
   const int64_t total = (int64_t)gridDim.x * kWarps, mine = (int64_t)blockIdx.x * kWarps + warp;
   const int64_t each = n / total, more = n % total;
-  const int64_t begin = mine * each + min(mine, more), end = begin + each + (mine < more ? 1 : 0);
+  const uint32_t begin = (uint32_t)(mine * each + min(mine, more)), end = begin + (uint32_t)each + (mine < more ? 1u : 0u);
 
   // Steps of a token: its query heads and right behind them its key heads, kGroups at a time (one with both kinds in
   // place of two: 230,000 tokens of 2 and 1 heads forward 227 -> 182 us).
   const int heads = p.n_heads + p.n_kv_heads, steps = (heads + kGroups - 1) / kGroups;
   struct Head {
     bool key, in;
-    int64_t at;  // its first element in a token's row
+    uint32_t at;  // its first element in a token's row
   };
+  auto element = [](uint32_t t, int64_t stride, uint32_t at) { return (int64_t)((uint64_t)t * (uint32_t)stride + at); };
   auto head_of = [&](int i) -> Head {
     const int h = i * kGroups + group;
     const bool key = h >= p.n_heads;
-    return {key, h < heads, (int64_t)(key ? h - p.n_heads : h) * D};
+    return {key, h < heads, (uint32_t)((key ? h - p.n_heads : h) * D)};
   };
   uint4* own = slots + (size_t)warp * kStages * P::kSlot + lane;
-  int64_t ahead_t = begin;
+  uint32_t ahead_t = begin;
   int ahead_step = 0, ahead_stage = 0;
   auto fetch = [&]() {  // the next step that is not on its way yet
     if (ahead_t < end) {
@@ -271,11 +330,11 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
       if (slot.in && h.in) {
         uint4* to = own + ahead_stage * P::kSlot;
         if (kReadsX)
-          copy_chunks<T>(to, (const T*)(h.key ? args.k : args.q) + ahead_t * (h.key ? p.k_stride : p.q_stride) + h.at, slot);
+          copy_chunks<T>(to, (const T*)(h.key ? args.k : args.q) + element(ahead_t, h.key ? p.k_stride : p.q_stride, h.at), slot);
         if (BWD)
           copy_chunks<T>(to + P::kSlot / 2,
                          (const T*)(h.key ? args.dk_out : args.dq_out) +
-                             ahead_t * (h.key ? p.k_out_stride : p.q_out_stride) + h.at,
+                             element(ahead_t, h.key ? p.k_out_stride : p.q_out_stride, h.at),
                          slot);
       }
       if (++ahead_step == steps) {
@@ -299,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
 #pragma unroll
   for (int j = 0; j < kAngles; ++j) {
     const int e = j * kGroups + group;
-    freq[j] = slot.turns && e < 8 ? __ldg(args.inv_freq + angle_of(p, slot, e)) * 0.15915494309189533577 : 0.0;
+    freq[j] = slot.turns && e < 8 ? __ldg(args.inv_freq + angle_of<INTER>(slot, e)) * 0.15915494309189533577 : 0.0;
   }
   int seq = 0;
   int64_t seq_lo = 0, seq_hi = 0;
@@ -309,7 +368,8 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
     seq_hi = __ldg(args.cu + seq + 1);
   }
   int stage = 0;
-  for (int64_t t = begin; t < end; ++t) {
+  const int first_key = p.n_heads / kGroups;  // the step in which the key heads begin
+  for (uint32_t t = begin; t < end; ++t) {
     int64_t pos;
     if (args.positions) {
       pos = __ldg(args.positions + t);
@@ -321,20 +381,30 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
       }
       pos = t - seq_lo;
     }
-    float c[8], s[8];
-    {
-      float cj[kAngles], sj[kAngles];
+    float cj[kAngles], sj[kAngles];
 #pragma unroll
-      for (int j = 0; j < kAngles; ++j) {
-        const double x = freq[j] * (double)pos;
-        sincospif((float)(2.0 * (x - rint(x))), &sj[j], &cj[j]);
-      }
+    for (int j = 0; j < kAngles; ++j) {
+      const double x = freq[j] * (double)pos;
+      sincospif((float)(2.0 * (x - rint(x))), &sj[j], &cj[j]);
+    }
+    auto deal = [&](float (&c)[8], float (&s)[8]) {  // for all lanes
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int from = (e % kGroups) * LANES + (lane & (LANES - 1));
         c[e] = __shfl_sync(0xFFFFFFFFu, cj[e / kGroups], from);
         s[e] = __shfl_sync(0xFFFFFFFFu, sj[e / kGroups], from);
-        if (BWD) s[e] = -s[e];
+      }
+    };
+    Turn turn;
+    Back back;
+    if (BWD) {
+      float c[8], s[8];
+      deal(c, s);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        back.c[i] = INTER ? make_float2(c[i], c[4 + i]) : make_float2(c[2 * i], c[2 * i + 1]);
+        back.s[i] = INTER ? make_float2(s[i], s[4 + i]) : make_float2(s[2 * i], s[2 * i + 1]);
+        back.minus_s[i] = make_float2(-back.s[i].x, -back.s[i].y);
       }
     }
     // a stage is fetched anew only after the step that read it has used, and stored, what it read
@@ -344,9 +414,21 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
       const uint4* from = own + stage * P::kSlot;
       stage = stage + 1 == kStages ? 0 : stage + 1;
       const Head h = head_of(i);
-      T* to = (T*)(h.key ? args.k_to : args.q_to) + h.at +
-              t * (BWD ? (h.key ? p.k_stride : p.q_stride) : (h.key ? p.k_out_stride : p.q_out_stride));
-      step<T, LANES, BWD, NORM>(p, slot, from, h.in, to, weights[h.key ? 1 : 0], inv_d, c, s, dwq, dwk, h.key);
+      T* to = (T*)(h.key ? args.k_to : args.q_to) +
+              element(t, BWD ? (h.key ? p.k_stride : p.q_stride) : (h.key ? p.k_out_stride : p.q_out_stride), h.at);
+      const float* w = weights[h.key ? 1 : 0];
+      if (BWD) {
+        backward_step<T, LANES, INTER, NORM>(p.eps, inv_d, slot, from, h.in, to, back, w, dwq, dwk, h.key);
+      } else {
+        // the weights change with the kind of head: in the first step, in that of the first key heads, and, where that one
+        // has both kinds, in the one behind
+        if (i == 0 || (NORM && (i == first_key || i == first_key + 1))) {
+          float c[8], s[8];
+          deal(c, s);
+          make_turn<INTER, NORM>(turn, slot, w, c, s);
+        }
+        forward_step<T, LANES, INTER, NORM>(p.eps, inv_d, slot, from, h.in, to, turn);
+      }
     }
   }
   if (BWD && NORM) {
@@ -406,7 +488,7 @@ weights_kernel(const float* partial, int blocks, int D, float* dw_q, float* dw_k
 // Lanes of a head's row: two chunks each.
 int lanes_of(const nat_qknorm_params& p) {
   const int slots = p.rot_dim / 16 + ((p.head_dim - p.rot_dim) / kChunk + 1) / 2;
-  return slots > 4 ? 8 : slots > 2 ? 4 : slots > 1 ? 2 : 1;
+  return slots > 4 ? 8 : slots > 2 ? 4 : 2;
 }
 
 // Blocks, and with them the tokens of a warp.  Many short runs in the blocks' order keep what is read and written at any
@@ -418,7 +500,7 @@ int lanes_of(const nat_qknorm_params& p) {
 int blocks_of(const nat_qknorm_params& p, int64_t cap, bool bwd) {
   const int64_t row = (int64_t)(p.n_heads + p.n_kv_heads) * p.head_dim * (p.dtype == NAT_F32 ? 4 : 2);
   const int64_t run = ((bwd ? 32768 : 8192) + row - 1) / row;
-  const int64_t most = (cap + kWarps - 1) / kWarps, held = 148 * (bwd ? 2 : 3);
+  const int64_t most = (cap + kWarps - 1) / kWarps, held = 148 * 2;
   return (int)min(most, max(held, (cap + kWarps * run - 1) / (kWarps * run)));
 }
 
@@ -468,30 +550,35 @@ int check_call(const char* who, const Args& a, std::initializer_list<const void*
   return NAT_OK;
 }
 
-template <typename T, int LANES, bool BWD, bool NORM>
-int launch(const Args& a, cudaStream_t stream) {
+template <typename T, int LANES, bool BWD, bool INTER, bool NORM>
+int launch_kernel(const Args& a, cudaStream_t stream) {
   static std::atomic<uint64_t> allowed{0};  // a bit for each device whose shared-memory limit is raised
   constexpr size_t smem = Pipe<T, BWD>::kBytes;
   int dev = 0;
   NAT_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", dev);
   if (!(allowed.load(std::memory_order_relaxed) >> dev & 1u)) {
-    NAT_CUDA(cudaFuncSetAttribute(qknorm_kernel<T, LANES, BWD, NORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    NAT_CUDA(cudaFuncSetAttribute(qknorm_kernel<T, LANES, BWD, INTER, NORM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)smem));
     allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  qknorm_kernel<T, LANES, BWD, NORM><<<blocks_of(a.p, a.cap, BWD), kThreads, smem, stream>>>(a);
+  qknorm_kernel<T, LANES, BWD, INTER, NORM><<<blocks_of(a.p, a.cap, BWD), kThreads, smem, stream>>>(a);
   NAT_LAUNCH_CHECK("qknorm");
   return NAT_OK;
+}
+
+template <typename T, int LANES, bool BWD>
+int launch_lanes(const Args& a, cudaStream_t stream) {
+  if (a.p.interleaved)
+    return a.w_q ? launch_kernel<T, LANES, BWD, true, true>(a, stream) : launch_kernel<T, LANES, BWD, true, false>(a, stream);
+  return a.w_q ? launch_kernel<T, LANES, BWD, false, true>(a, stream) : launch_kernel<T, LANES, BWD, false, false>(a, stream);
 }
 
 template <typename T, bool BWD>
 int launch(const Args& a, cudaStream_t stream) {
   const int lanes = lanes_of(a.p);
-  if (a.w_q)
-    return lanes == 8 ? launch<T, 8, BWD, true>(a, stream) : lanes == 4 ? launch<T, 4, BWD, true>(a, stream)
-         : lanes == 2 ? launch<T, 2, BWD, true>(a, stream) : launch<T, 1, BWD, true>(a, stream);
-  return lanes == 8 ? launch<T, 8, BWD, false>(a, stream) : lanes == 4 ? launch<T, 4, BWD, false>(a, stream)
-       : lanes == 2 ? launch<T, 2, BWD, false>(a, stream) : launch<T, 1, BWD, false>(a, stream);
+  return lanes == 8 ? launch_lanes<T, 8, BWD>(a, stream) : lanes == 4 ? launch_lanes<T, 4, BWD>(a, stream)
+                                                                      : launch_lanes<T, 2, BWD>(a, stream);
 }
 
 size_t workspace_bytes_of(const nat_qknorm_params& p, int64_t cap) {
