@@ -106,8 +106,8 @@ __device__ __forceinline__ uint32_t slot_of(int round, int rounds) {
   return (threadIdx.x >> 5) * rounds * 32 + round * 32 + (threadIdx.x & 31);
 }
 
-// rank[j] of the thread's pairs among their digit within the warp; `counts` [kWarps][digits] holds the warps'
-// totals afterwards.
+// rank[j] of the thread's pairs among their digit within the warp; `counts` [warps][digits] holds the warps' totals
+// afterwards.
 __device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint32_t valid, int rounds, Digit digit,
                                            uint32_t* counts, uint32_t (&rank)[kRounds]) {
   const int lane = threadIdx.x & 31;
@@ -118,8 +118,13 @@ __device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint3
   for (int j = 0; j < kRounds; ++j) {
     if (j >= rounds) break;
     const bool in = slot_of(j, rounds) < valid;
-    const int g = in ? digit.of(key[j]) : -1;
-    const unsigned same = __match_any_sync(0xFFFFFFFFu, g);
+    const int g = digit.of(key[j]);
+    // the lanes with the same digit, bit by bit (__match_any_sync takes longer)
+    unsigned same = __ballot_sync(0xFFFFFFFFu, in);
+    for (int b = 0; b < digit.bits; ++b) {
+      const unsigned set = __ballot_sync(0xFFFFFFFFu, (g >> b) & 1);
+      same &= (g >> b) & 1 ? set : ~set;
+    }
     const unsigned below = same & ((1u << lane) - 1u);
     uint32_t before = 0u;
     if (in) before = mine[g];
@@ -168,21 +173,30 @@ __device__ __forceinline__ void prefix_digits(uint32_t* total, int digits) {
   __syncthreads();
 }
 
+// A block's pairs (id, row), in registers before anything else is done with them: one round trip to memory.  `pairs`
+// NULL: the rows in their order.
+__device__ __forceinline__ void load_pairs(const Rows& r, const uint2* pairs, uint32_t base, uint32_t n, int rounds,
+                                           uint32_t (&key)[kRounds], uint32_t (&val)[kRounds]) {
+#pragma unroll
+  for (int j = 0; j < kRounds; ++j) {
+    const uint32_t i = base + slot_of(j, rounds);
+    const bool in = j < rounds && i < n;
+    const uint2 p = !in ? make_uint2(0u, 0u) : pairs ? pairs[i] : make_uint2(row_id(r, i), i);
+    key[j] = p.x;
+    val[j] = p.y;
+  }
+}
+
 // Up to kTile pairs: all passes in one block, the pairs in shared memory between them.
 __global__ void __launch_bounds__(kThreads)
-sort_small_kernel(Rows r, int passes, int bits, uint32_t* keys, uint32_t* vals) {
+sort_small_kernel(Rows r, int passes, int bits, uint2* pairs) {
   __shared__ uint32_t skey[kTile], counts[kWarps * kMaxDigits], total[kMaxDigits];
   __shared__ uint16_t sval[kTile];
   release_secondary();
   const uint32_t n = row_count(r);
   const int rounds = rounds_for(n);
   uint32_t key[kRounds], val[kRounds], rank[kRounds];
-#pragma unroll
-  for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = slot_of(j, rounds);
-    key[j] = j < rounds && i < n ? row_id(r, i) : 0u;
-    val[j] = i;
-  }
+  load_pairs(r, nullptr, 0u, n, rounds, key, val);
   for (int p = 0; p < passes; ++p) {
     const Digit digit{p * bits, bits};
     warp_ranks(key, n, rounds, digit, counts, rank);
@@ -195,8 +209,7 @@ sort_small_kernel(Rows r, int passes, int bits, uint32_t* keys, uint32_t* vals) 
         const int g = digit.of(key[j]);
         const uint32_t to = total[g] + counts[(threadIdx.x >> 5) * digit.count() + g] + rank[j];
         if (last) {
-          keys[to] = key[j];
-          vals[to] = val[j];
+          pairs[to] = make_uint2(key[j], val[j]);
         } else {
           skey[to] = key[j];
           sval[to] = (uint16_t)val[j];
@@ -217,19 +230,9 @@ sort_small_kernel(Rows r, int passes, int bits, uint32_t* keys, uint32_t* vals) 
   }
 }
 
-// A block's pairs, in registers before anything else is done with them: one round trip to memory.
-__device__ __forceinline__ void load_keys(const Rows& r, const uint32_t* keys, uint32_t base, uint32_t n, int rounds,
-                                          uint32_t (&key)[kRounds]) {
-#pragma unroll
-  for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = base + slot_of(j, rounds);
-    key[j] = j < rounds && i < n ? (keys ? keys[i] : row_id(r, i)) : 0u;
-  }
-}
-
 // How many pairs of each digit a block holds: hist [digits][blocks].
 __global__ void __launch_bounds__(kThreads)
-count_kernel(Rows r, const uint32_t* keys, Digit digit, uint32_t* hist) {
+count_kernel(Rows r, const uint2* pairs, Digit digit, uint32_t* hist) {
   release_secondary();
   __shared__ uint32_t c[kMaxDigits];
   for (int g = threadIdx.x; g < digit.count(); g += kThreads) c[g] = 0u;
@@ -237,8 +240,8 @@ count_kernel(Rows r, const uint32_t* keys, Digit digit, uint32_t* hist) {
   wait_for_primary();
   const uint32_t n = row_count(r), base = blockIdx.x * kTile;
   const int rounds = base < n ? rounds_for(n - base) : 0;
-  uint32_t key[kRounds];
-  load_keys(r, keys, base, n, rounds, key);
+  uint32_t key[kRounds], val[kRounds];
+  load_pairs(r, pairs, base, n, rounds, key, val);
 #pragma unroll
   for (int j = 0; j < kRounds; ++j)
     if (j < rounds && base + slot_of(j, rounds) < n) atomicAdd(&c[digit.of(key[j])], 1u);
@@ -270,8 +273,7 @@ prefix_kernel(uint32_t* hist, int blocks, int digits, uint32_t* total) {
 }
 
 __global__ void __launch_bounds__(kThreads)
-scatter_kernel(Rows r, const uint32_t* keys, const uint32_t* vals, Digit digit, const uint32_t* hist,
-               const uint32_t* totals, uint32_t* keys_out, uint32_t* vals_out) {
+scatter_kernel(Rows r, const uint2* pairs, Digit digit, const uint32_t* hist, const uint32_t* totals, uint2* out) {
   release_secondary();
   wait_for_primary();
   __shared__ uint32_t counts[kWarps * kMaxDigits], total[kMaxDigits];
@@ -280,12 +282,7 @@ scatter_kernel(Rows r, const uint32_t* keys, const uint32_t* vals, Digit digit, 
   if (base >= n) return;
   const int rounds = rounds_for(n - base);
   uint32_t key[kRounds], val[kRounds], rank[kRounds];
-  load_keys(r, keys, base, n, rounds, key);
-#pragma unroll
-  for (int j = 0; j < kRounds; ++j) {
-    const uint32_t i = base + slot_of(j, rounds);
-    val[j] = vals && j < rounds && i < n ? vals[i] : i;
-  }
+  load_pairs(r, pairs, base, n, rounds, key, val);
   for (int g = threadIdx.x; g < digits; g += kThreads) total[g] = totals[g];
   warp_ranks(key, n - base, rounds, digit, counts, rank);
   prefix_digits(total, digits);
@@ -304,8 +301,7 @@ scatter_kernel(Rows r, const uint32_t* keys, const uint32_t* vals, Digit digit, 
   for (int j = 0; j < kRounds; ++j) {
     if (j < rounds && base + slot_of(j, rounds) < n) {
       const uint32_t to = counts[(threadIdx.x >> 5) * digits + digit.of(key[j])] + rank[j];
-      keys_out[to] = key[j];
-      vals_out[to] = val[j];
+      out[to] = make_uint2(key[j], val[j]);
     }
   }
 }
@@ -313,7 +309,7 @@ scatter_kernel(Rows r, const uint32_t* keys, const uint32_t* vals, Digit digit, 
 // -------------------------------------------------------------------------- sums
 struct SumArgs {
   Rows r;
-  const uint32_t *keys, *vals;  // sorted
+  const uint2* pairs;           // (id, row), sorted
   const void* dx;
   float *dtable, *partial;      // partial [2 tiles][d]
   uint32_t* status;
@@ -324,18 +320,18 @@ struct SumArgs {
 };
 
 // First sorted position in [lo, hi) whose key is not below `key`, hi if there is none.
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t key) {
+__device__ __forceinline__ uint32_t lower_bound(const uint2* pairs, uint32_t lo, uint32_t hi, uint32_t key) {
   while (lo < hi) {
     const uint32_t mid = (lo + hi) >> 1;
-    if (keys[mid] < key) lo = mid + 1; else hi = mid;
+    if (pairs[mid].x < key) lo = mid + 1; else hi = mid;
   }
   return lo;
 }
 // The same by a whole warp, 32 probes at a time: four dependent loads where one lane would take eighteen.
-__device__ __forceinline__ uint32_t warp_lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t key) {
+__device__ __forceinline__ uint32_t warp_lower_bound(const uint2* pairs, uint32_t lo, uint32_t hi, uint32_t key) {
   while (lo < hi) {  // the answer is in [lo, hi]
     const uint32_t step = (hi - lo + 31) / 32, at = lo + ((threadIdx.x & 31) + 1) * step - 1;
-    const unsigned not_below = __ballot_sync(0xFFFFFFFFu, at >= hi || keys[at] >= key);
+    const unsigned not_below = __ballot_sync(0xFFFFFFFFu, at >= hi || pairs[at].x >= key);
     // lane f is the first not below: the answer is in its step; lanes past hi count as not below
     const uint32_t f = not_below ? __ffs(not_below) - 1 : 32;
     const uint32_t from = lo + f * step;
@@ -345,20 +341,27 @@ __device__ __forceinline__ uint32_t warp_lower_bound(const uint32_t* keys, uint3
   return lo;
 }
 
-// Sum over the sorted tokens [lo, hi) of eight columns, in order, four loads on their way at a time (the usual row
-// has a few tokens, and one after the other each would cost a round trip).
+// Sum over the rows row_of(lo) .. row_of(hi - 1) of eight columns, in order, with several loads on their way at a time
+// (the usual row of the table has a few tokens, and one after the other each would cost a round trip).  As many as four
+// blocks a multiprocessor leave registers for: 166,001 bfloat16 rows of 4096, 732 us with four loads and four blocks, 677
+// with six, 692 with four loads and five blocks, 781 with twelve and three.
 template <typename T>
-__device__ __forceinline__ void add_tokens(const SumArgs& a, uint32_t lo, uint32_t hi, int c, float2 (&sum)[kPairs]) {
+constexpr int kFlight = sizeof(T) == 2 ? 6 : 4;
+constexpr int kSumBlocks = 4;
+
+template <typename T, typename R>
+__device__ __forceinline__ void add_tokens(const SumArgs& a, R row_of, uint32_t lo, uint32_t hi, int c, float2 (&sum)[kPairs]) {
+  constexpr int F = kFlight<T>;
   const T* dx = (const T*)a.dx + c;
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) sum[i] = both(0.f);
-  for (uint32_t i = lo; i < hi; i += 4) {
-    Raw<T> raw[4];
+  for (uint32_t i = lo; i < hi; i += F) {
+    Raw<T> raw[F];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u < hi) raw[u] = rows::load_raw(dx + (int64_t)a.vals[i + u] * a.d);
+    for (int u = 0; u < F; ++u)
+      if (i + u < hi) raw[u] = rows::load_raw(dx + (int64_t)row_of(i + u) * a.d);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < F; ++u) {
       if (i + u >= hi) break;
       float2 v[kPairs];
       rows::widen(raw[u], v);
@@ -368,14 +371,18 @@ __device__ __forceinline__ void add_tokens(const SumArgs& a, uint32_t lo, uint32
   }
 }
 
+// Rows of the table a block writes, at most (74,003 tokens, 1024 columns: 175 us with 16, 172 with 24 or 32; 166,001, 4096:
+// 678, 680, 696).
+constexpr int kRowsPerBlock = 24;
+
 // Blocks [0, tiles): the piece of a table row with more than kPiece tokens that lies in a tile of kPiece sorted
 // positions.  A tile meets at most two such rows, one that began before it (slot 0) and one that begins in it and
 // goes on behind it (slot 1).  The blocks behind: rows of the table with up to kPiece tokens.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) sum_kernel(SumArgs a) {
+__global__ void __launch_bounds__(kThreads, kSumBlocks) sum_kernel(SumArgs a) {
   release_secondary();
   wait_for_primary();
-  __shared__ uint32_t start[33];
+  __shared__ uint32_t start[kRowsPerBlock + 1];
   const uint32_t n = row_count(a.r);
   const int tpr = 1 << a.tpr_log2, group = threadIdx.x >> a.tpr_log2, groups = kThreads >> a.tpr_log2;
   const int first = (threadIdx.x & (tpr - 1)) * kChunk, stride = kChunk << a.tpr_log2;
@@ -383,21 +390,25 @@ __global__ void __launch_bounds__(kThreads, 4) sum_kernel(SumArgs a) {
     const uint32_t t0 = blockIdx.x * kPiece, t1 = min(t0 + kPiece, n);
     if (t0 >= n) return;
     // a row that goes on over an end of the tile has the same id on both sides of it; most tiles have none
-    const uint32_t k0 = a.keys[t0], k1 = a.keys[t1 - 1];
-    const bool from_before = t0 > 0 && k0 != (uint32_t)a.r.V && a.keys[t0 - 1] == k0;
-    const bool goes_on = t1 < n && k1 != (uint32_t)a.r.V && a.keys[t1] == k1;
+    const uint32_t k0 = a.pairs[t0].x, k1 = a.pairs[t1 - 1].x;
+    const bool from_before = t0 > 0 && k0 != (uint32_t)a.r.V && a.pairs[t0 - 1].x == k0;
+    const bool goes_on = t1 < n && k1 != (uint32_t)a.r.V && a.pairs[t1].x == k1;
     if (!from_before && !goes_on) return;
-    if (threadIdx.x < 4) {
-      const uint32_t key = threadIdx.x < 2 ? k0 : k1;
-      start[threadIdx.x] = lower_bound(a.keys, 0u, n, key + (threadIdx.x & 1));
+    if (threadIdx.x < 128) {  // where the first and the last token's rows begin and end, a warp each
+      const int warp = threadIdx.x >> 5;
+      const uint32_t key = (warp < 2 ? k0 : k1) + (warp & 1);
+      const uint32_t at = warp == 0 ? warp_lower_bound(a.pairs, 0u, t0, key)
+                                    : warp_lower_bound(a.pairs, warp == 2 ? 0u : warp == 1 ? t0 : t1, warp == 2 ? t1 : n, key);
+      if ((threadIdx.x & 31) == 0) start[warp] = at;
     }
     __syncthreads();
+    auto row_of = [&](uint32_t i) { return a.pairs[i].y; };
     for (int s = group; s < 2; s += groups) {
       const uint32_t b = start[2 * s], e = start[2 * s + 1];
       if (e - b <= kPiece || !(s == 0 ? from_before : goes_on && b >= t0)) continue;
       for (int c = first; c < a.d; c += stride) {
         float2 sum[kPairs];
-        add_tokens<T>(a, max(b, t0), min(e, t1), c, sum);
+        add_tokens<T>(a, row_of, max(b, t0), min(e, t1), c, sum);
         Raw<float> out;
         rows::narrow(sum, out);
         rows::store_raw(a.partial + (2 * (int64_t)blockIdx.x + s) * a.d + c, out);
@@ -408,46 +419,53 @@ __global__ void __launch_bounds__(kThreads, 4) sum_kernel(SumArgs a) {
   const int v0 = (blockIdx.x - a.tiles) * a.rows_per_block, count = min(a.rows_per_block, a.r.V - v0);
   // where the block's rows begin among the sorted tokens: its first and last by two warps, those between from the
   // tokens themselves where they are few
-  __shared__ uint32_t ends[2];
+  __shared__ uint32_t ends[2], row_at[kThreads];
   if (threadIdx.x < 64) {
-    const uint32_t at = warp_lower_bound(a.keys, 0u, n, (uint32_t)(v0 + (threadIdx.x < 32 ? 0 : count)));
+    const uint32_t at = warp_lower_bound(a.pairs, 0u, n, (uint32_t)(v0 + (threadIdx.x < 32 ? 0 : count)));
     if ((threadIdx.x & 31) == 0) ends[threadIdx.x >> 5] = at;
   }
   __syncthreads();
   const uint32_t lo0 = ends[0], hi0 = ends[1];
-  if (hi0 - lo0 > kThreads) {
-    if (threadIdx.x <= count) start[threadIdx.x] = lower_bound(a.keys, lo0, hi0, (uint32_t)(v0 + threadIdx.x));
+  const bool few = hi0 - lo0 <= kThreads;  // their tokens' rows fit into shared memory
+  if (!few) {
+    if (threadIdx.x <= count) start[threadIdx.x] = lower_bound(a.pairs, lo0, hi0, (uint32_t)(v0 + threadIdx.x));
   } else {
     // token i tells where the rows after its predecessor's, up to its own, begin; the end tells of the rest
     const uint32_t i = lo0 + threadIdx.x;
     if (i <= hi0) {
-      const int from = i == lo0 ? 0 : (int)a.keys[i - 1] - v0 + 1, to = i == hi0 ? count : (int)a.keys[i] - v0;
+      const uint2 own = i < hi0 ? a.pairs[i] : make_uint2((uint32_t)(v0 + count), 0u);
+      const int from = i == lo0 ? 0 : (int)a.pairs[i - 1].x - v0 + 1, to = (int)own.x - v0;
+      row_at[threadIdx.x] = own.y;
       for (int v = from; v <= to; ++v) start[v] = i;
     }
     if (hi0 - lo0 == kThreads && threadIdx.x == 0)  // one more than there are threads
-      for (int v = (int)a.keys[hi0 - 1] - v0 + 1; v <= count; ++v) start[v] = hi0;
+      for (int v = (int)a.pairs[hi0 - 1].x - v0 + 1; v <= count; ++v) start[v] = hi0;
   }
-  if (v0 == 0 && threadIdx.x == 0) *a.status = n > 0 && a.keys[n - 1] == (uint32_t)a.r.V ? NAT_DEV_BAD_TARGET : 0u;
+  if (v0 == 0 && threadIdx.x == 0) *a.status = n > 0 && a.pairs[n - 1].x == (uint32_t)a.r.V ? NAT_DEV_BAD_TARGET : 0u;
   __syncthreads();
-  for (int i = group; i < count; i += groups) {
-    const uint32_t lo = start[i], hi = start[i + 1];
-    if (hi - lo > kPiece || (a.accumulate && hi == lo)) continue;
-    float* row = a.dtable + (int64_t)(v0 + i) * a.d;
-    for (int c = first; c < a.d; c += stride) {
-      float2 sum[kPairs];
-      add_tokens<T>(a, lo, hi, c, sum);
-      Raw<float> out;
-      float2 old[kPairs];
-      if (a.accumulate) rows::widen(rows::load_raw(row + c), old);
+  auto write_rows = [&](auto row_of) {
+    for (int i = group; i < count; i += groups) {
+      const uint32_t lo = start[i], hi = start[i + 1];
+      if (hi - lo > kPiece || (a.accumulate && hi == lo)) continue;
+      float* row = a.dtable + (int64_t)(v0 + i) * a.d;
+      for (int c = first; c < a.d; c += stride) {
+        float2 sum[kPairs];
+        add_tokens<T>(a, row_of, lo, hi, c, sum);
+        Raw<float> out;
+        float2 old[kPairs];
+        if (a.accumulate) rows::widen(rows::load_raw(row + c), old);
 #pragma unroll
-      for (int j = 0; j < kPairs; ++j) {
-        sum[j] = mul2(sum[j], both(a.scale));
-        if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+        for (int j = 0; j < kPairs; ++j) {
+          sum[j] = mul2(sum[j], both(a.scale));
+          if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+        }
+        rows::narrow(sum, out);
+        rows::store_raw(row + c, out);
       }
-      rows::narrow(sum, out);
-      rows::store_raw(row + c, out);
     }
-  }
+  };
+  if (few) write_rows([&](uint32_t i) { return row_at[i - lo0]; });
+  else write_rows([&](uint32_t i) { return a.pairs[i].y; });
 }
 
 // Joins the pieces of the rows that begin in one of the block's tiles and go on behind it: the warps take runs of
@@ -465,10 +483,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
     const uint32_t t0 = (blockIdx.x * kJoinTiles + warp) * kPiece, t1 = t0 + kPiece;
     uint32_t b = 0u, e = 0u;
     if (t1 < n) {
-      const uint32_t key = a.keys[t1 - 1], next = a.keys[t1], before = t0 > 0 ? a.keys[t0 - 1] : (uint32_t)a.r.V;
+      const uint32_t key = a.pairs[t1 - 1].x, next = a.pairs[t1].x, before = t0 > 0 ? a.pairs[t0 - 1].x : (uint32_t)a.r.V;
       if (key != (uint32_t)a.r.V && next == key && before != key) {
-        b = warp_lower_bound(a.keys, t0, t1, key);
-        e = warp_lower_bound(a.keys, t1, n, key + 1);
+        b = warp_lower_bound(a.pairs, t0, t1, key);
+        e = warp_lower_bound(a.pairs, t1, n, key + 1);
       }
     }
     if (lane == 0) {
@@ -501,7 +519,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
     for (int j = 0; j < kPairs; ++j) sums[warp][lane][j] = sum[j];
     __syncthreads();
     if (warp == 0 && c < a.d) {
-      float* at = a.dtable + (int64_t)a.keys[b] * a.d + c;
+      float* at = a.dtable + (int64_t)a.pairs[b].x * a.d + c;
       float2 old[kPairs];
       if (a.accumulate) rows::widen(rows::load_raw(at), old);
       Raw<float> out;
@@ -521,7 +539,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
 // --------------------------------------------------------------------------- host
 struct Layout {
   int passes, bits, blocks, tiles;
-  size_t keys[2], vals[2], hist, total, partial, bytes;
+  size_t pairs[2], hist, total, partial, bytes;
 };
 
 Layout layout(const nat_embed_params& p, int64_t cap) {
@@ -538,10 +556,7 @@ Layout layout(const nat_embed_params& p, int64_t cap) {
     at = align_up(at + bytes, 256);
     return o;
   };
-  for (int i = 0; i < 2; ++i) {
-    l.keys[i] = take(4 * (size_t)cap);
-    l.vals[i] = take(4 * (size_t)cap);
-  }
+  for (int i = 0; i < 2; ++i) l.pairs[i] = take(sizeof(uint2) * (size_t)cap);
   l.hist = take(4 * (size_t)kMaxDigits * l.blocks);
   l.total = take(4 * kMaxDigits);
   l.partial = take(2 * (size_t)l.tiles * p.d * sizeof(float));
@@ -597,33 +612,33 @@ int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable,
         cudaStream_t stream) {
   char* ws = (char*)workspace;
   auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(ws + o); };
+  uint2* pairs[2] = {reinterpret_cast<uint2*>(ws + l.pairs[0]), reinterpret_cast<uint2*>(ws + l.pairs[1])};
   int src = 0, s;
   if (r.cap <= kTile) {
-    sort_small_kernel<<<1, kThreads, 0, stream>>>(r, l.passes, l.bits, at(l.keys[0]), at(l.vals[0]));
+    sort_small_kernel<<<1, kThreads, 0, stream>>>(r, l.passes, l.bits, pairs[0]);
     NAT_LAUNCH_CHECK("embed_sort_small");
   } else {
     for (int pass = 0; pass < l.passes; ++pass) {
       const Digit digit{pass * l.bits, l.bits};
-      const uint32_t* keys = pass ? at(l.keys[src]) : nullptr;
-      const uint32_t* vals = pass ? at(l.vals[src]) : nullptr;
+      const uint2* from = pass ? pairs[src] : nullptr;
       const int dst = pass ? src ^ 1 : 0;
       if (pass == 0) {  // behind whatever wrote the ids: not before that has ended
-        count_kernel<<<l.blocks, kThreads, 0, stream>>>(r, keys, digit, at(l.hist));
+        count_kernel<<<l.blocks, kThreads, 0, stream>>>(r, from, digit, at(l.hist));
         NAT_LAUNCH_CHECK("embed_count");
       } else {
-        s = launch_after(count_kernel, dim3(l.blocks), kThreads, 0, stream, "embed_count", r, keys, digit, at(l.hist));
+        s = launch_after(count_kernel, dim3(l.blocks), kThreads, 0, stream, "embed_count", r, from, digit, at(l.hist));
         if (s != NAT_OK) return s;
       }
       s = launch_after(prefix_kernel, dim3(((1 << l.bits) + kWarps - 1) / kWarps), kThreads, 0, stream, "embed_prefix",
                        at(l.hist), l.blocks, 1 << l.bits, at(l.total));
       if (s != NAT_OK) return s;
-      s = launch_after(scatter_kernel, dim3(l.blocks), kThreads, 0, stream, "embed_scatter", r, keys, vals, digit,
-                       (const uint32_t*)at(l.hist), (const uint32_t*)at(l.total), at(l.keys[dst]), at(l.vals[dst]));
+      s = launch_after(scatter_kernel, dim3(l.blocks), kThreads, 0, stream, "embed_scatter", r, from, digit,
+                       (const uint32_t*)at(l.hist), (const uint32_t*)at(l.total), pairs[dst]);
       if (s != NAT_OK) return s;
       src = dst;
     }
   }
-  SumArgs a{r, at(l.keys[src]), at(l.vals[src]), dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), 16,
+  SumArgs a{r, pairs[src], dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), kRowsPerBlock,
             l.tiles, p.scale, p.accumulate != 0};
   while (a.rows_per_block > 1 && p.V / a.rows_per_block < 148 * 8) a.rows_per_block >>= 1;
   s = launch_after(sum_kernel<T>, dim3((unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block)), kThreads, 0,
