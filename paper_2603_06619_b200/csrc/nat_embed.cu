@@ -6,6 +6,7 @@
 // one a token and writes the whole table in 32 bits.  For the gradient the pairs (id, k) are sorted by a stable radix
 // sort, so that the tokens of a table row stand together in ascending order, and every row of the table is written
 // once, by the threads that add up its tokens.  Nothing is added by atomics: the order of the sums is fixed.
+#include <atomic>
 #include <initializer_list>
 
 #include "nat_common.cuh"
@@ -99,8 +100,9 @@ struct Digit {
   __device__ __forceinline__ int count() const { return 1 << bits; }
 };
 
+template <int THREADS = kThreads>
 __device__ __forceinline__ int rounds_for(uint32_t valid) {
-  return (int)((min(valid, (uint32_t)kTile) + kThreads - 1) / kThreads);
+  return (int)((min(valid, (uint32_t)(THREADS * kRounds)) + THREADS - 1) / THREADS);
 }
 __device__ __forceinline__ uint32_t slot_of(int round, int rounds) {
   return (threadIdx.x >> 5) * rounds * 32 + round * 32 + (threadIdx.x & 31);
@@ -108,11 +110,12 @@ __device__ __forceinline__ uint32_t slot_of(int round, int rounds) {
 
 // rank[j] of the thread's pairs among their digit within the warp; `counts` [warps][digits] holds the warps' totals
 // afterwards.
+template <int THREADS = kThreads>
 __device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint32_t valid, int rounds, Digit digit,
                                            uint32_t* counts, uint32_t (&rank)[kRounds]) {
   const int lane = threadIdx.x & 31;
   uint32_t* mine = counts + (threadIdx.x >> 5) * digit.count();
-  for (int i = threadIdx.x; i < kWarps * digit.count(); i += kThreads) counts[i] = 0u;
+  for (int i = threadIdx.x; i < THREADS / 32 * digit.count(); i += THREADS) counts[i] = 0u;
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kRounds; ++j) {
@@ -138,11 +141,12 @@ __device__ __forceinline__ void warp_ranks(const uint32_t (&key)[kRounds], uint3
 
 // counts[w][g] -> how many of digit g the warps before w hold; returns nothing, leaves the block's total of digit g
 // in total[g].
+template <int THREADS>
 __device__ __forceinline__ void across_warps(uint32_t* counts, uint32_t* total, int digits) {
-  for (int g = threadIdx.x; g < digits; g += kThreads) {
+  for (int g = threadIdx.x; g < digits; g += THREADS) {
     uint32_t run = 0u;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
       const uint32_t c = counts[w * digits + g];
       counts[w * digits + g] = run;
       run += c;
@@ -152,9 +156,10 @@ __device__ __forceinline__ void across_warps(uint32_t* counts, uint32_t* total, 
   __syncthreads();
 }
 
-// total[0..digits) -> its exclusive prefix sums (digits <= kMaxDigits = 2 kThreads).
+// total[0..digits) -> its exclusive prefix sums (digits <= kMaxDigits = 2 kThreads: two of each thread).
+template <int THREADS = kThreads>
 __device__ __forceinline__ void prefix_digits(uint32_t* total, int digits) {
-  __shared__ uint32_t sums[kWarps];
+  __shared__ uint32_t sums[THREADS / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t a = 2 * threadIdx.x < digits ? total[2 * threadIdx.x] : 0u;
   uint32_t b = 2 * threadIdx.x + 1 < digits ? total[2 * threadIdx.x + 1] : 0u;
@@ -167,7 +172,7 @@ __device__ __forceinline__ void prefix_digits(uint32_t* total, int digits) {
   if (lane == 31) sums[warp] = run;
   __syncthreads();
   uint32_t before = run - (a + b);
-  for (int w = 0; w < warp; ++w) before += sums[w];
+  for (int w = 0; w < min(warp, kWarps); ++w) before += sums[w];
   if (2 * threadIdx.x < digits) total[2 * threadIdx.x] = before;
   if (2 * threadIdx.x + 1 < digits) total[2 * threadIdx.x + 1] = before + a;
   __syncthreads();
@@ -187,21 +192,30 @@ __device__ __forceinline__ void load_pairs(const Rows& r, const uint2* pairs, ui
   }
 }
 
-// Up to kTile pairs: all passes in one block, the pairs in shared memory between them.
-__global__ void __launch_bounds__(kThreads)
+// Up to eight pairs a thread: all passes in one block, the pairs in shared memory between them.
+template <int THREADS>
+struct Small {
+  static constexpr int kMost = THREADS * kRounds;
+  static constexpr size_t kSmem = (kMost + (THREADS / 32 + 1) * kMaxDigits) * sizeof(uint32_t) + kMost * sizeof(uint16_t);
+};
+constexpr int kSmallThreads = 1024;  // beyond kTile pairs (a gradient of 2500 tokens 54 us, 64 with the kernels below; 8000 tokens 74, 74)
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1)
 sort_small_kernel(Rows r, int passes, int bits, uint2* pairs) {
-  __shared__ uint32_t skey[kTile], counts[kWarps * kMaxDigits], total[kMaxDigits];
-  __shared__ uint16_t sval[kTile];
+  extern __shared__ uint32_t smem[];
+  uint32_t *skey = smem, *counts = smem + Small<THREADS>::kMost, *total = counts + THREADS / 32 * kMaxDigits;
+  uint16_t* sval = reinterpret_cast<uint16_t*>(total + kMaxDigits);
   release_secondary();
   const uint32_t n = row_count(r);
-  const int rounds = rounds_for(n);
+  const int rounds = rounds_for<THREADS>(n);
   uint32_t key[kRounds], val[kRounds], rank[kRounds];
   load_pairs(r, nullptr, 0u, n, rounds, key, val);
   for (int p = 0; p < passes; ++p) {
     const Digit digit{p * bits, bits};
-    warp_ranks(key, n, rounds, digit, counts, rank);
-    across_warps(counts, total, digit.count());
-    prefix_digits(total, digit.count());
+    warp_ranks<THREADS>(key, n, rounds, digit, counts, rank);
+    across_warps<THREADS>(counts, total, digit.count());
+    prefix_digits<THREADS>(total, digit.count());
     const bool last = p == passes - 1;
 #pragma unroll
     for (int j = 0; j < kRounds; ++j) {
@@ -607,6 +621,21 @@ int fwd(const nat_embed_params& p, const void* table, const Rows& r, void* x, cu
   return NAT_OK;
 }
 
+// Raises the larger small sort's shared-memory limit, once for each device.
+int allow_smem() {
+  static std::atomic<uint64_t> allowed{0};
+  int dev = 0;
+  NAT_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", dev);
+  if (!(allowed.load(std::memory_order_relaxed) >> dev & 1u)) {
+    NAT_CUDA(cudaFuncSetAttribute(sort_small_kernel<kSmallThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)Small<kSmallThreads>::kSmem));
+    allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return NAT_OK;
+}
+static_assert(Small<kThreads>::kSmem <= 48 * 1024, "within the limit that needs no raising");
+
 template <typename T>
 int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable, void* workspace, const Layout& l,
         cudaStream_t stream) {
@@ -615,7 +644,12 @@ int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable,
   uint2* pairs[2] = {reinterpret_cast<uint2*>(ws + l.pairs[0]), reinterpret_cast<uint2*>(ws + l.pairs[1])};
   int src = 0, s;
   if (r.cap <= kTile) {
-    sort_small_kernel<<<1, kThreads, 0, stream>>>(r, l.passes, l.bits, pairs[0]);
+    sort_small_kernel<kThreads><<<1, kThreads, Small<kThreads>::kSmem, stream>>>(r, l.passes, l.bits, pairs[0]);
+    NAT_LAUNCH_CHECK("embed_sort_small");
+  } else if (r.cap <= Small<kSmallThreads>::kMost) {
+    s = allow_smem();
+    if (s != NAT_OK) return s;
+    sort_small_kernel<kSmallThreads><<<1, kSmallThreads, Small<kSmallThreads>::kSmem, stream>>>(r, l.passes, l.bits, pairs[0]);
     NAT_LAUNCH_CHECK("embed_sort_small");
   } else {
     for (int pass = 0; pass < l.passes; ++pass) {
