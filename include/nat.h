@@ -27,7 +27,8 @@
  *   - Device-side conditions that cannot be known at launch (a bounded wait
  *     that ran out, n_sel above the stated capacity, a target outside the
  *     vocabulary) are recorded in the 32-bit status word at the start of the
- *     loss or attention workspace (see NAT_DEV_* bits, nat_poll_status); kernels never trap.
+ *     loss, attention, embedding or experts workspace (see NAT_DEV_* bits, nat_poll_status);
+ *     kernels never trap.
  *   - Alignment: mask, pi, surv and q arrays, the compacted lists and every
  *     matrix must start on a 16-byte boundary (the kernels use 16-byte
  *     accesses); a misaligned pointer is refused with NAT_ERR_INVALID_ARG.
@@ -50,14 +51,15 @@ typedef enum {
   NAT_ERR_CUDA = -4         /* a CUDA runtime/driver call failed; see nat_last_error() */
 } nat_status;
 
-/* Bits of the device status word (first 4 bytes of a loss or attention workspace). */
+/* Bits of the device status word (first 4 bytes of a loss, attention, embedding or experts workspace). */
 #define NAT_DEV_TIMEOUT 1u  /* a bounded mbarrier wait gave up; outputs are invalid */
-#define NAT_DEV_CAPACITY 2u /* *n_sel exceeded n_sel_cap (attention: cu_seqlens exceeded cap, or is
-                                not ascending); surplus rows were ignored */
+#define NAT_DEV_CAPACITY 2u /* *n_sel exceeded n_sel_cap (attention and experts: cu_seqlens or offsets
+                                exceeded cap, or are not ascending); surplus rows were ignored */
 #define NAT_DEV_FALLBACK 4u /* informational: nat_policy_loss_fwd_bwd redid some row chunk with
                                the two-pass kernels (results are valid) */
 #define NAT_DEV_BAD_TARGET 8u /* some selected token's target lies outside [0, V): that token
-                                 was left out (zero loss term and gradient, logp = NaN) */
+                                 was left out (zero loss term and gradient, logp = NaN); embedding:
+                                 an id outside [0, V), left out of the table's gradient */
 
 const char* nat_status_string(int status);
 const char* nat_last_error(void); /* host string, valid until the thread's next failing call */
@@ -533,8 +535,8 @@ int nat_embed_bwd(const nat_embed_params* params /* host */, const int32_t* ids,
  * inv_freq float64 [rot_dim / 2] (any law; NULL where rot_dim = 0).  The angles are reduced in 64 bits and their sines and
  * cosines, the norms and all sums are in 32.
  * Positions: positions int32 [cap], or NULL: a row's distance from the start of its sequence in cu_seqlens int32 [B+1],
- * ascending.  Rows: min(*n_rows, cap) (n_rows NULL: cap), and without positions no more than cu_seqlens[B]; rows at or
- * after that are neither written nor read.
+ * ascending.  Rows: min(*n_rows, cap) (n_rows NULL: cap), and without positions those from cu_seqlens[0] to
+ * cu_seqlens[B]; others are neither written nor read.
  * q, dq [cap, n_heads, head_dim] with q_stride elements from a token to the next, heads contiguous; k, dk
  * [cap, n_kv_heads, head_dim] with k_stride; q_out, dq_out with q_out_stride, k_out, dk_out with k_out_stride.  An
  * output may lie on an input of the same token stride (q_out on q, dq on dq_out or q, and k alike); other overlaps

@@ -41,10 +41,14 @@ struct Args {
   float* partial;                // backward with norms: [blocks][2][head_dim]
 };
 
-__device__ __forceinline__ int64_t row_count(const Args& a) {
-  int64_t n = a.n_rows ? min((int64_t)max(__ldg(a.n_rows), 0), a.cap) : a.cap;
-  if (!a.positions) n = min(n, (int64_t)max(__ldg(a.cu + a.B), 0));
-  return n;
+// Rows [first, end) of the call.
+__device__ __forceinline__ void row_range(const Args& a, int64_t& first, int64_t& end) {
+  end = a.n_rows ? min((int64_t)max(__ldg(a.n_rows), 0), a.cap) : a.cap;
+  first = 0;
+  if (!a.positions) {
+    first = max(__ldg(a.cu), 0);
+    end = max(first, min(end, (int64_t)max(__ldg(a.cu + a.B), 0)));
+  }
 }
 
 // The last sequence that begins at or before row n (0 where none does).
@@ -303,10 +307,13 @@ __global__ void __launch_bounds__(kThreads, (Pipe<T, BWD>::kBlocks)) qknorm_kern
       weights[i / kMaxDim][i % kMaxDim] = i % kMaxDim < D ? (i < kMaxDim ? args.w_q : args.w_k)[i % kMaxDim] : 0.f;
     __syncthreads();
   }
-  const int64_t n = row_count(args);
+  int64_t first_row, end_row;
+  row_range(args, first_row, end_row);
+  const int64_t n = end_row - first_row;
   const int64_t total = (int64_t)gridDim.x * kWarps, mine = (int64_t)blockIdx.x * kWarps + warp;
   const int64_t each = n / total, more = n % total;
-  const uint32_t begin = (uint32_t)(mine * each + min(mine, more)), end = begin + (uint32_t)each + (mine < more ? 1u : 0u);
+  const uint32_t begin = (uint32_t)(first_row + mine * each + min(mine, more)),
+                 end = begin + (uint32_t)each + (mine < more ? 1u : 0u);
 
   // Steps of a token: its query heads and right behind them its key heads, kGroups at a time (one with both kinds in
   // place of two: 230,000 tokens of 2 and 1 heads forward 227 -> 182 us).

@@ -1,5 +1,9 @@
 """The body from ids to expert products on packed prefixes, against the same chain in float64; captured and replayed; and
 one table's gradient from both its ends."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -94,3 +98,42 @@ def test_one_step_captured_beside_an_eager_one():
         for x, y in zip(results(a[1], a[3], n), results(b[1], b[3], n)):
             assert torch.equal(x, y)
         assert all(p.status() == 0 for p in (*a[:3], *b[:3]))
+
+
+FIRST_CALLS = """
+import sys
+sys.path.insert(0, {root!r})
+sys.path.insert(0, {root!r} + "/tests")
+import torch
+from test_gpu_embed import Embed
+from test_gpu_experts import Experts
+from test_gpu_qknorm import Heads
+dt = torch.{dtype}
+ops = [Embed(7000, 300, 128, dt, seed=1), Embed(4000, 90, 64, dt, seed=2), Heads([90, 41], 4, 2, 64, dt, seed=3),
+       Experts([300, 0, 41], 136, 264, dt, seed=4), Experts([9, 0, 4, 1], 136, 264, dt, seed=5),
+       Experts([5000, 4000], 72, 136, dt, seed=6)]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    for op in ops:
+        op.fwd()
+        op.bwd()
+graph.replay()
+torch.cuda.synchronize()
+names = {{Embed: ("x", "dtable"), Heads: ("out", "dqkv", "dw_q", "dw_k"), Experts: ("y", "dx", "dw")}}
+got = [[getattr(op, k).clone() for k in names[type(op)]] for op in ops]
+for op, first in zip(ops, got):
+    op.fwd()
+    op.bwd()
+    assert all(torch.equal(a, getattr(op, k)) for a, k in zip(first, names[type(op)])), type(op)
+print("same bits")
+"""
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_first_calls_of_a_process_inside_a_capture(dtype):
+    """Whatever a first call sets up needs no call before the capture."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(root=root, dtype=dtype)], capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0 and "same bits" in r.stdout, r.stdout + r.stderr

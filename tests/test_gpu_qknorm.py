@@ -232,6 +232,17 @@ def test_qknorm_without_rows():
     assert (h.dw_q == 0).all() and (h.dq == 7).all()
 
 
+def test_qknorm_rows_in_front_of_the_first_sequence():
+    h = Heads([30, 50], 4, 2, 64, torch.float32, seed=7)
+    whole = Heads([30, 50], 4, 2, 64, torch.float32, seed=7)
+    whole.fwd()
+    h.cu.copy_(torch.tensor([30, 30, 80]))
+    h.fwd()
+    h.bwd()
+    assert (h.out[:30] == 7).all() and (h.dqkv[:30] == 7).all() and (h.out[80:] == 7).all()
+    assert torch.equal(h.out[30:80], whole.out[30:80])
+
+
 def test_qknorm_fewer_rows_than_the_sequences_hold():
     h = Heads([30, 50], 4, 2, 64, torch.float32, seed=7, count=True)
     h.n_rows.fill_(41)
