@@ -8,7 +8,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnat_b200.so")
 SOURCES = ["nat_api.cu", "nat_token.cu", "nat_select.cu", "nat_prefix.cu", "nat_loss_f32.cu",
-           "nat_loss_bf16.cu", "nat_ckpt8.cu", "nat_resnorm.cu", "nat_embed.cu", "nat_qknorm.cu", "nat_experts.cu", "nat_experts_f32.cu", "nat_experts_bf16.cu", "nat_experts_few.cu", "nat_attn.cu", "nat_attn_f32.cu", "nat_attn_bf16.cu", "nat_attn_bwd_bf16.cu"]
+           "nat_loss_bf16.cu", "nat_ckpt8.cu", "nat_resnorm.cu", "nat_embed.cu", "nat_qknorm.cu", "nat_experts.cu", "nat_experts_f32.cu", "nat_experts_bf16.cu", "nat_attn.cu", "nat_attn_f32.cu", "nat_attn_bf16.cu", "nat_attn_bwd_bf16.cu"]
 
 
 def _stale():

@@ -190,24 +190,8 @@ __device__ __forceinline__ void regs_dec() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// One lane of a converged warp.  Together with a warp index and a tensor-memory address that the
-// compiler knows to be the same in all lanes (uniform()) this keeps the operands of the MMAs in
-// uniform registers: moved there one by one they cost 75 cycles an MMA, more than its 64.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t one;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "elect.sync _|p, 0xffffffff;\n"
-      "selp.u32 %0, 1, 0, p;\n"
-      "}\n"
-      : "=r"(one));
-  return one != 0;
-}
-template <typename T>
-__device__ __forceinline__ T uniform(T x) {
-  return __shfl_sync(0xFFFFFFFFu, x, 0);
-}
+using tc::elect_one;
+using tc::uniform;
 
 // Tensor map of [cap, heads, D] bfloat16 with a token stride: boxes of 64 columns x box_heads x
 // box_tokens, zero outside.

@@ -68,8 +68,7 @@ inline float* partial(const Args& a, const Layout& l) {
   return reinterpret_cast<float*>((char*)a.workspace + l.partial_off);
 }
 
-constexpr int kFewRows = 64;                    // of a tile of the kernel for few rows
-constexpr int kBf16Cols = 256;                   // columns of a tile (float32: as many as rows)
+constexpr int kBf16Cols = 256;  // columns of a tile (float32: as many as rows)
 
 // Rows of the k-blocks [lo, hi) that part `part` of `parts` takes of `blocks`.
 __host__ __device__ inline void part_range(int blocks, int part, int parts, int& lo, int& hi) {
@@ -82,7 +81,6 @@ __host__ __device__ inline void part_range(int blocks, int part, int parts, int&
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap);
 int f32_tile(const nat_experts_params& p, Product which, int64_t cap);
 int bf16_product(const Args& a, const Layout& l, Product which);
-int few_product(const Args& a, const Layout& l, Product which);
 int f32_product(const Args& a, const Layout& l, Product which);
 
 }  // namespace experts

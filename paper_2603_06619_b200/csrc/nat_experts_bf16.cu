@@ -4,8 +4,8 @@
 //   kDx   dx = dy w_e      (rows x n_in,   contraction n_out)   w_e contiguous across it
 //   kDw   dw_e = dy^T x    (n_out x n_in,  contraction rows)    both contiguous across it
 //
-// Persistent CTA pairs: the even CTA issues MMAs of M = 256, N = 256 (cta_group::2), each CTA holds SUBS blocks of
-// 128 rows of A and half of B per stage and drains its own rows of the accumulators.  Warp 0 loads by TMA, warp 1
+// Persistent CTA pairs: the even CTA issues MMAs of M = 256, N = 256 (cta_group::2), each CTA holds one or two
+// blocks of 128 rows of A and half of B per stage and drains its own rows of the accumulators.  Warp 0 loads by TMA, warp 1
 // issues, four warps for each block of rows write out.  Every wait is bounded and raises NAT_DEV_TIMEOUT.
 //
 // Ragged ends.  A tile's rows behind its expert's last belong to another expert or to none: they give rows of the
@@ -28,18 +28,22 @@ constexpr int kTmemCols = 512;
 // 4.7e-6 with 96; 6.6e-6, 9.0e-6, 8.2e-6 with whole sums, which take 2 % less time; 1.8e-6 for the last with 32, which
 // takes 17 % more.
 constexpr int kSegment = 96;
-constexpr int kGroup = 8;                    // row tiles that go through the columns together
+constexpr int kFewRows = 64;  // of a tile where the experts have few rows
+constexpr int kGroup = 8;     // row tiles that go through the columns together
 
-// Shared memory: stages of A and half of B, and 4 KB pieces of finished rows for each warp that writes out, from which
-// they leave by TMA: two for kDw, whose epilogue nothing hides, one elsewhere.
-template <int WHICH, int SUBS>
+// ROWS: of a tile.  Shared memory: stages of A and half of B, and 4 KB pieces of finished rows for each warp that writes
+// out, from which they leave by TMA: two for kDw, whose epilogue nothing hides, one elsewhere.
+template <int WHICH, int ROWS>
 struct Ring {
-  static constexpr int kABytes = SUBS * BM * BK * 2, kBBytes = (BN / 2) * BK * 2, kStage = kABytes + kBBytes;
+  static constexpr int kSubs = ROWS <= 2 * BM ? 1 : 2;  // blocks of 128 rows of A a CTA holds
+  static constexpr int kABytes = ROWS / 2 * BK * 2, kBBytes = (BN / 2) * BK * 2, kStage = kABytes + kBBytes;
   static constexpr int kPieces = WHICH == kDw ? 2 : 1;
-  static constexpr int kStaging = 4 * SUBS * kPieces * 4096;
-  static constexpr int kNum = (226 * 1024 - 1024 - 256 - kStaging) / kStage;
-  static constexpr int kThreads = 64 + 128 * SUBS;
-  static constexpr size_t kSmem = (size_t)kNum * kStage + kStaging + 1024 /*alignment*/ + 256 /*barriers*/;
+  static constexpr int kStaging = 4 * kSubs * kPieces * 4096;
+  static constexpr int kBarriers = 512;
+  static constexpr int kNum = (226 * 1024 - 1024 - kBarriers - kStaging) / kStage;
+  static_assert((3 * kNum + 5) * 8 + 8 <= kBarriers, "barriers, tensor memory's address and the abort flag");
+  static constexpr int kThreads = 64 + 128 * kSubs;
+  static constexpr size_t kSmem = (size_t)kNum * kStage + kStaging + 1024 /*alignment*/ + kBarriers;
 };
 
 struct TcArgs {
@@ -61,7 +65,7 @@ struct Unit {
 
 // kFwd, kDx: groups of kGroup row tiles go through the columns, the row tile varying fastest, so that the pairs at
 // work share few row tiles and few column tiles through L2.  kDw: the experts in the list's order.
-template <int WHICH, int SUBS>
+template <int WHICH, int ROWS>
 __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
   const int n_tiles = (a.n_cols + BN - 1) / BN;
   Unit w;
@@ -72,7 +76,7 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
     w.expert = t.expert;
     w.lo = t.lo;
     w.hi = t.hi;
-    w.m0 = tile / n_tiles * (2 * BM * SUBS);
+    w.m0 = tile / n_tiles * ROWS;
     w.n0 = (tile - tile / n_tiles * n_tiles) * BN;
     part_range((w.hi - w.lo + BK - 1) / BK, part, a.parts, w.kb_lo, w.kb_hi);
     w.slice = part * a.E + w.expert;
@@ -91,6 +95,24 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
   w.kb_hi = a.k_blocks;
   w.slice = 0;
   return w;
+}
+
+// kFwd, kDx: a tile of up to 128 rows is turned: the weights' columns go along M and its rows along N, whose length an
+// MMA's time follows in steps of 32 (16 rows of each CTA), with the same loads into the same places.  Its N, 0 for a tile
+// that is not turned.  us, without / with this: 62 rows an expert (32 experts, 4096 x 1536) 112 / 91, 1875 (64, 2048 x
+// 1024) 457 / 452.  Tiles of up to 224 rows turned as well, 5000 rows over 32 experts take 114 in place of 110: less of an
+// MMA is saved, and its operands are no fewer.
+__device__ __forceinline__ int turned_rows(const Unit& w) {
+  const int n = (w.hi - w.lo + 31) / 32 * 32;
+  return n <= BM ? n : 0;
+}
+
+// The operand of the MMA step kk (16 elements of the contraction) in a stage.  Contiguous along it: 32 bytes of the swizzled
+// 128-byte row, groups of eight rows 1024 bytes apart; across it: 16 rows are two such groups, blocks of 64 columns
+// whole boxes apart.
+template <bool ACROSS>
+__device__ __forceinline__ uint64_t step_desc(uint32_t base, int kk) {
+  return ACROSS ? tc::smem_desc_sw128(base + kk * 2048, kBox, 1024) : tc::smem_desc_sw128(base + kk * 32, 16, 1024);
 }
 
 __device__ __forceinline__ void load_3d_pair(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
@@ -137,12 +159,12 @@ __device__ __forceinline__ void put_3d(const CUtensorMap* map, const void* src, 
                  : "memory");
 }
 
-template <int WHICH, int SUBS>
-__global__ void __launch_bounds__(Ring<WHICH, SUBS>::kThreads, 1)
+template <int WHICH, int ROWS>
+__global__ void __launch_bounds__(Ring<WHICH, ROWS>::kThreads, 1)
 experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
                const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c, const TcArgs a) {
-  using R = Ring<WHICH, SUBS>;
-  constexpr int kNS = R::kNum;
+  using R = Ring<WHICH, ROWS>;
+  constexpr int kNS = R::kNum, SUBS = R::kSubs;
   constexpr uint32_t kAcc = 2 / SUBS;  // accumulators: two tiles in flight, or one
   constexpr bool kAcross = WHICH == kDw;                    // A is contiguous across the contraction
   constexpr bool kBcross = WHICH == kDw || WHICH == kDx;
@@ -160,7 +182,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(peer_bar + kNS);
   volatile uint32_t* abort_flag = tmem_slot + 1;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = tc::uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int rank = (int)(tc::cluster_ctarank() & 1u);
   const int unit0 = blockIdx.x / 2, stride = gridDim.x / 2;
 
@@ -191,14 +213,15 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   __syncthreads();
   tc::cluster_sync_all();  // the peer's barriers exist before anyone signals them
   tc::fence_after_sync();
-  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_base = tc::uniform(*tmem_slot);
   wait_for_primary();  // the list of tiles is there
   const int row_tiles = (int)a.head->tiles;
   const int units = (a.n_cols + BN - 1) / BN * (WHICH == kDw ? (a.head->broken ? 0 : a.E * a.m_tiles * a.parts) : row_tiles);
 
+  auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x ? 1 : 0) != 0; };
   // The entry of the unit after `u` is asked for before u is worked on: it costs a round trip to L2.
-  auto first_unit = [&]() { return decode<WHICH, SUBS>(a, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
-  auto unit_after = [&](int u) { return decode<WHICH, SUBS>(a, row_tiles, u + stride < units ? u + stride : u); };
+  auto first_unit = [&]() { return decode<WHICH, ROWS>(a, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
+  auto unit_after = [&](int u) { return decode<WHICH, ROWS>(a, row_tiles, u + stride < units ? u + stride : u); };
   auto segments_of = [&](const Unit& w) { return WHICH == kDw ? max(1, (w.kb_hi - w.kb_lo + kSegment - 1) / kSegment) : 1; };
   // A gradient that is added to takes nothing from an expert without rows.
   auto skipped = [&](const Unit& w) {
@@ -207,7 +230,6 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
   if (warp == 0) {
     // ------------------------------------------------ TMA producer (lane 0; all lanes for the last rows)
-    auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x ? 1 : 0) != 0; };
     uint32_t it = 0, tail_phase = 0u, peer_phase = 0u;  // peer_phase: a bit a stage
     bool ok = true;
     Unit next = first_unit();
@@ -216,6 +238,10 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       next = unit_after(u);
       if (skipped(w)) continue;
       const int n0 = w.n0 + rank * (BN / 2);
+      // the tile's row slots of each CTA, and the pieces of 32 of them that have rows
+      const int turned = turned_rows(w), each = turned ? turned / 2 : BM, first = rank * each;
+      auto pieces_from = [&](int r) { return max(0, (min(w.hi - w.lo - r, each) + 31) / 32); };
+      const int pieces = pieces_from(first), all_pieces = pieces + pieces_from(each - first);
       for (int kb = w.kb_lo; kb < w.kb_hi; ++kb, ++it) {
         const int s = it % kNS;
         ok = all(tc::mbar_wait(&empty_bar[s], ((it / kNS) & 1u) ^ 1u, abort_flag));
@@ -259,26 +285,14 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
           }
         } else if (lane == 0) {
-          // of A only what has rows of the tile: whole blocks of 128 rows, or pieces of 32 of a smaller one (the rest of
-          // the stage is what it was: rows of the accumulator that nobody writes out)
-          const int rows = w.hi - w.lo;
-          auto pieces = [&](int first) { return max(0, min(4, (rows - first + 31) / 32)); };
-          if (rank == 0) {
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < 2 * SUBS; ++i) n += pieces(i * BM);
-            tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kBBytes + n * 32 * BK * 2);
-          }
-#pragma unroll
-          for (int sub = 0; sub < SUBS; ++sub) {
-            const int first = sub * 2 * BM + rank * BM, n = pieces(first);
-            uint8_t* dst = a_dst + sub * BM * BK * 2;
-            if (n == 4) {
-              tc::tma_load_2d_pair(dst, &map_a, bar, kb * BK, w.lo + first);
-            } else {
-              for (int i = 0; i < n; ++i)
-                tc::tma_load_2d_pair(dst + i * 32 * BK * 2, &map_a32, bar, kb * BK, w.lo + first + i * 32);
-            }
+          // of A only what has rows of the tile: 128 of them, or fewer in pieces of 32 (the rest of the stage is what it
+          // was: rows of the accumulator that nobody writes out)
+          if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kBBytes + all_pieces * 32 * BK * 2);
+          if (pieces == 4) {
+            tc::tma_load_2d_pair(a_dst, &map_a, bar, kb * BK, w.lo + first);
+          } else {
+            for (int i = 0; i < pieces; ++i)
+              tc::tma_load_2d_pair(a_dst + i * 32 * BK * 2, &map_a32, bar, kb * BK, w.lo + first + i * 32);
           }
           if (WHICH == kFwd) {
             load_3d_pair(b_dst, &map_b, bar, kb * BK, n0, w.expert);
@@ -302,7 +316,9 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
   } else if (warp == 1) {
     // ------------------------------------------------ MMA issuer (even CTA)
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
+      // The whole warp goes through the loops and one elected lane issues: what the instructions need has to be in uniform
+      // registers, and what one lane alone has worked out is moved there value by value.
       uint32_t it = 0, tcount = 0;
       bool ok = true;
       Unit next = first_unit();
@@ -311,35 +327,44 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         next = unit_after(u);
         if (skipped(w)) continue;
         const int segments = segments_of(w);
+        const int turned = WHICH == kDw ? 0 : tc::uniform(turned_rows(w));
+        const uint32_t turned_idesc = tc::instr_desc_bf16(2 * BM, turned, kBcross ? 1 : 0, 0);
         for (int seg = 0; ok && seg < segments; ++seg, ++tcount) {
           const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
           int kb_lo, kb_hi;
           part_range(w.kb_hi - w.kb_lo, seg, segments, kb_lo, kb_hi);
-          if (!tc::mbar_wait(&tempty_bar[acc], aph ^ 1u, abort_flag)) { ok = false; break; }
+          ok = all(tc::mbar_wait(&tempty_bar[acc], aph ^ 1u, abort_flag));
+          if (!ok) break;
           tc::fence_after_sync();
           const uint32_t d_tmem = tmem_base + acc * SUBS * BN;
           for (int kb = kb_lo; kb < kb_hi; ++kb, ++it) {
             const int s = it % kNS;
-            if (!tc::mbar_wait(&full_bar[s], (it / kNS) & 1u, abort_flag)) { ok = false; break; }
+            ok = all(tc::mbar_wait(&full_bar[s], (it / kNS) & 1u, abort_flag));
+            if (!ok) break;
             tc::fence_after_sync();
             const uint32_t a_base = tc::smem_u32(smem + (size_t)s * R::kStage), b_base = a_base + R::kABytes;
-  #pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk) {
-              // contiguous along the contraction: 16 elements are 32 bytes of the swizzled 128-byte row, groups of eight
-              // rows 1024 bytes apart; across it: 16 rows are two such groups, blocks of 64 columns whole boxes apart
-              const uint64_t bdesc = kBcross ? tc::smem_desc_sw128(b_base + kk * 2048, kBox, 1024)
-                                             : tc::smem_desc_sw128(b_base + kk * 32, 16, 1024);
-  #pragma unroll
-              for (int sub = 0; sub < SUBS; ++sub) {
-                const uint32_t a_sub = a_base + sub * (BM * BK * 2);
-                const uint64_t adesc = kAcross ? tc::smem_desc_sw128(a_sub + kk * 2048, kBox, 1024)
-                                               : tc::smem_desc_sw128(a_sub + kk * 32, 16, 1024);
-                tc::umma_bf16_pair(d_tmem + sub * BN, adesc, bdesc, kIdesc, (kb > kb_lo || kk > 0) ? 1u : 0u);
+            if (tc::elect_one()) {
+              if (WHICH != kDw && turned) {
+#pragma unroll
+                for (int kk = 0; kk < BK / 16; ++kk)
+                  tc::umma_bf16_pair(d_tmem, step_desc<kBcross>(b_base, kk), step_desc<kAcross>(a_base, kk), turned_idesc,
+                                     (kb > kb_lo || kk > 0) ? 1u : 0u);
+              } else {
+#pragma unroll
+                for (int kk = 0; kk < BK / 16; ++kk) {
+                  const uint64_t bdesc = step_desc<kBcross>(b_base, kk);
+#pragma unroll
+                  for (int sub = 0; sub < SUBS; ++sub)
+                    tc::umma_bf16_pair(d_tmem + sub * BN, step_desc<kAcross>(a_base + sub * (BM * BK * 2), kk), bdesc, kIdesc,
+                                       (kb > kb_lo || kk > 0) ? 1u : 0u);
+                }
               }
+              tc::umma_commit_pair(&empty_bar[s], 3);
             }
-            tc::umma_commit_pair(&empty_bar[s], 3);
+            __syncwarp();
           }
-          if (ok) tc::umma_commit_pair(&tfull_bar[acc], 3);
+          if (ok && tc::elect_one()) tc::umma_commit_pair(&tfull_bar[acc], 3);
+          __syncwarp();
         }
       }
     }
@@ -361,7 +386,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const int segments = segments_of(w);
       for (int seg = 0; seg < segments; ++seg, ++tcount) {
         const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
-        ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(&tfull_bar[acc], aph, abort_flag) ? 1 : 0) != 0;
+        ok = all(tc::mbar_wait(&tfull_bar[acc], aph, abort_flag));
         if (!ok) break;
         tc::fence_after_sync();
         const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc * SUBS + (uint32_t)sub) * BN;
@@ -393,6 +418,30 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               tc::bulk_commit();
             }
           }
+        } else if (const int turned = turned_rows(w)) {
+          // a lane a column of the result: 32 rows of 64 bytes through the warp's block of shared memory, then 16 bytes a
+          // lane (single elements straight to memory: 8 us for a tile of 184 rows)
+          const int rows = w.hi - w.lo, col = w.n0 + rank * BM + q * 32 + lane % 4 * 8;
+          __nv_bfloat16* stage = reinterpret_cast<__nv_bfloat16*>(pieces);
+          if (lane == 0) tc::bulk_wait_read_all();
+#pragma unroll 1
+          for (int c = 0; c < turned; c += 32) {
+            uint32_t v[32];
+            tc::tmem_ld32_issue(taddr + c, v);
+            tc::tmem_ld_wait(v);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) stage[j * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[j]));
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int row = c + j * 8 + lane / 4;
+              if (row < rows && col < a.n_cols)
+                *reinterpret_cast<uint4*>(a.rows_out + (int64_t)(w.lo + row) * a.rows_stride + col) =
+                    *reinterpret_cast<const uint4*>(stage + (j * 8 + lane / 4) * 32 + lane % 4 * 8);
+            }
+          }
+          __syncwarp();
         } else {
           const int valid = min(32, w.hi - w.lo - in_tile);  // of the warp's rows
 #pragma unroll 1
@@ -463,7 +512,7 @@ int map_gradient(CUtensorMap* map, const nat_experts_params& p, const float* dw,
 }
 
 // CTA pairs that the current device holds at a time, found once for each device.
-template <int WHICH, int SUBS>
+template <int WHICH, int ROWS>
 int pairs(int* out) {
   static std::atomic<int> cached[64];
   int dev = 0;
@@ -471,12 +520,12 @@ int pairs(int* out) {
   if (s != NAT_OK) return s;
   int n = cached[dev].load(std::memory_order_relaxed);
   if (n == 0) {
-    NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, SUBS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)Ring<WHICH, SUBS>::kSmem));
+    NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)Ring<WHICH, ROWS>::kSmem));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(148);
-    cfg.blockDim = dim3(Ring<WHICH, SUBS>::kThreads);
-    cfg.dynamicSmemBytes = Ring<WHICH, SUBS>::kSmem;
+    cfg.blockDim = dim3(Ring<WHICH, ROWS>::kThreads);
+    cfg.dynamicSmemBytes = Ring<WHICH, ROWS>::kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -484,7 +533,7 @@ int pairs(int* out) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    NAT_CUDA(cudaOccupancyMaxActiveClusters(&n, experts_kernel<WHICH, SUBS>, &cfg));
+    NAT_CUDA(cudaOccupancyMaxActiveClusters(&n, experts_kernel<WHICH, ROWS>, &cfg));
     if (n <= 0) return fail(NAT_ERR_UNSUPPORTED, "the device does not hold the experts' CTA pairs");
     cached[dev].store(n, std::memory_order_relaxed);
   }
@@ -492,16 +541,16 @@ int pairs(int* out) {
   return NAT_OK;
 }
 
-template <int WHICH, int SUBS>
+template <int WHICH, int ROWS>
 int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb, const CUtensorMap& mc, const TcArgs& t,
            int64_t most_units, cudaStream_t stream) {
   int slots = 0;
-  int s = pairs<WHICH, SUBS>(&slots);
+  int s = pairs<WHICH, ROWS>(&slots);
   if (s != NAT_OK) return s;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * min(most_units, (int64_t)slots)));
-  cfg.blockDim = dim3(Ring<WHICH, SUBS>::kThreads);
-  cfg.dynamicSmemBytes = Ring<WHICH, SUBS>::kSmem;
+  cfg.blockDim = dim3(Ring<WHICH, ROWS>::kThreads);
+  cfg.dynamicSmemBytes = Ring<WHICH, ROWS>::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -512,19 +561,21 @@ int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, SUBS>, ma, ma32, mb, mc, t));
+  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, ROWS>, ma, ma32, mb, mc, t));
   return NAT_OK;
 }
 
 }  // namespace
 
-// Average rows of an expert (by the capacity, which is what the host knows) up to which the forward product and the rows'
-// gradient go to the kernel for few rows.  us, pairs / few, forward and rows' gradient:
-//   rows an expert                   8         16        31        62
-//   32 experts, 4096 x 1536     90 78, 82 74   94 84, 88 78   99 84, 92 92   106 105, 101 110
-//   128 experts, 2048 x 768     94 76, 87 76        -        101 86, 95 90   106 102, 105 110
-//   8 experts, 4096 x 4096      64 57, 61 58        -         69 59, 70 64    72 80, 73 86
-constexpr int64_t kFew = 32;
+// Average rows of an expert (by the capacity, which is what the host knows) up to which the forward product takes tiles of
+// 64 rows, whose small stages leave room for ten in place of six: what bounds it then is the reading of the weights.  us, tiles
+// of 256 rows / of 64:
+//   rows an expert                   8            31           47           62
+//   32 experts, 4096 x 1536     80.6, 76.6   84.1, 80.2   87.6, 81.9   92.7, 100.0
+//   128 experts, 2048 x 768     78.5, 75.7   82.8, 80.1       -        91.4, 103.3
+//   8 experts, 4096 x 4096      55.3, 52.7   57.2, 54.8       -        62.4, 72.8
+// The rows' gradient reads the weights in longer pieces, and takes the same time with either.
+constexpr int64_t kFew = 48;
 // And from which the weights' gradient takes tiles of 512 rows in place of 256: 312 rows (128 experts, 2048 x 768) 321 us
 // with 512, 286 with 256; 1000 (16, 2048 x 2048) 164, 180; 1875 (64, 2048 x 1024) 536, 631; 4688 (64, 2048 x 1536)
 // 1654, 2021; 7500 (8, 4096 x 4096) 1623, 2054.
@@ -544,7 +595,7 @@ int device_index(int* dev) {
 }
 
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
-  if (which != kDw) return cap / p.n_experts <= kFew ? kFewRows : 2 * BM;
+  if (which != kDw) return which == kFwd && cap / p.n_experts <= kFew ? kFewRows : 2 * BM;
   // A tile of 512 rows of the result takes a quarter fewer operand bytes, but leaves no second accumulator in whose
   // shadow it is written out: worth it where the experts have rows enough.
   return cap / p.n_experts >= kDwWide ? 4 * BM : 2 * BM;
@@ -552,7 +603,6 @@ int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
 
 int bf16_product(const Args& a, const Layout& l, Product which) {
   const nat_experts_params& p = a.p;
-  if (which != kDw && l.tile_rows[which] == kFewRows) return few_product(a, l, which);
   CUtensorMap ma, ma32, mb, mc;
   int s;
   TcArgs t{};
@@ -570,8 +620,8 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
     t.n_cols = p.n_in;
     t.m_tiles = (p.n_out + l.tile_rows[kDw] - 1) / l.tile_rows[kDw];
     const int64_t units = (int64_t)t.E * t.m_tiles * ((p.n_in + BN - 1) / BN) * t.parts;
-    return l.tile_rows[kDw] == 4 * BM ? launch<kDw, 2>(ma, ma, mb, mc, t, units, a.stream)
-                                      : launch<kDw, 1>(ma, ma, mb, mc, t, units, a.stream);
+    return l.tile_rows[kDw] == 4 * BM ? launch<kDw, 4 * BM>(ma, ma, mb, mc, t, units, a.stream)
+                                      : launch<kDw, 2 * BM>(ma, ma, mb, mc, t, units, a.stream);
   }
   const bool fwd = which == kFwd;
   const void *in = fwd ? a.x : a.dy;
@@ -587,7 +637,9 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   if ((s = map_weights(&mb, p, a.w, fwd ? BN / 2 : BK)) != NAT_OK) return s;
   if ((s = map_rows(&mc, out, n, a.cap, t.rows_stride, 32)) != NAT_OK) return s;
   const int64_t units = l.most_tiles * ((n + BN - 1) / BN);
-  return fwd ? launch<kFwd, 1>(ma, ma32, mb, mc, t, units, a.stream) : launch<kDx, 1>(ma, ma32, mb, mc, t, units, a.stream);
+  if (l.tile_rows[which] == kFewRows) return launch<kFwd, kFewRows>(ma, ma32, mb, mc, t, units, a.stream);
+  return fwd ? launch<kFwd, 2 * BM>(ma, ma32, mb, mc, t, units, a.stream)
+             : launch<kDx, 2 * BM>(ma, ma32, mb, mc, t, units, a.stream);
 }
 
 }  // namespace experts

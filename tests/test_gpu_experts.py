@@ -103,6 +103,15 @@ def test_experts_parity(loads, sizes, dtype):
     Experts(LOADS[loads], *sizes, DT[dtype], seed=len(loads)).check()
 
 
+@pytest.mark.parametrize("loads", [[16, 17, 32, 33, 48, 95, 96, 97, 127, 128, 129, 160, 161, 224, 225, 255, 384, 385, 640],
+                                   [0] * 20 + [700] + [1, 15, 63, 64, 65, 0, 0, 31, 130] + [0] * 20],
+                         ids=["last_tiles", "lopsided"])
+@pytest.mark.parametrize("sizes", [(72, 264), (328, 136), (512, 512)])
+def test_experts_last_tiles_of_every_length(loads, sizes):
+    """Tiles with few rows lie the other way round; and one expert with many rows among many with few."""
+    Experts(loads, *sizes, torch.bfloat16, seed=21, strides=(8, 16)).check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_experts_strides_rows_in_front_and_accumulation(dtype):
     Experts([40, 300, 0, 5], 136, 200, DT[dtype], seed=1, first=13, strides=(24, 8)).check()
