@@ -14,13 +14,17 @@
 // contraction, and a row too many would be added in: where an expert's last block of 64 rows is not full, the loading
 // warp of each CTA waits for its own part of it, writes zeros over the rows behind (both operands': a weight of zero
 // would not hide an infinity), and the odd CTA tells the even one before the MMA warp is let on.
-#include "nat_experts_tc.cuh"
+#include <atomic>
+
+#include "nat_experts.cuh"
+#include "nat_tc.cuh"
 
 namespace nat {
 namespace experts {
 namespace {
 
-constexpr int BN = kBf16Cols;
+constexpr int BM = 128, BK = 64, BN = kBf16Cols;
+constexpr int kBox = 64 * 64 * 2;  // bytes of a 64 x 64 box of an operand that is contiguous across the contraction
 constexpr int kTmemCols = 512;
 // Blocks of the contraction that a kDw tile's accumulator takes at most: the tensor cores cut off what they add (toward
 // zero, about half a step of 2^-23 each time), so after that many the sum is added to the result in memory, rounded to
@@ -95,6 +99,11 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
   w.kb_hi = a.k_blocks;
   w.slice = 0;
   return w;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+  return *reinterpret_cast<uint32_t*>(&v);
 }
 
 // kFwd, kDx: a tile of up to 128 rows is turned: the weights' columns go along M and its rows along N, whose length an
@@ -503,12 +512,64 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // --------------------------------------------------------------------------- host
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encode(CUtensorMap* map, CUtensorMapDataType type, int dims, uintptr_t base, const cuuint64_t* size,
+           const cuuint64_t* pitch, const cuuint32_t* box) {
+  static std::atomic<EncodeTiledFn> cached{nullptr};
+  EncodeTiledFn fn = cached.load(std::memory_order_relaxed);
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    NAT_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found));
+    if (found != cudaDriverEntryPointSuccess || !p)
+      return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    fn = reinterpret_cast<EncodeTiledFn>(p);
+    cached.store(fn, std::memory_order_relaxed);
+  }
+  const cuuint32_t one[3] = {1, 1, 1};
+  const CUresult r = fn(map, type, (cuuint32_t)dims, reinterpret_cast<void*>(base), size, pitch, box, one,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(NAT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  return NAT_OK;
+}
+
+// Rows of a matrix [rows, cols] of bfloat16: boxes of 64 columns.
+int map_rows(CUtensorMap* map, const void* base, int cols, int64_t rows, int64_t stride, int box_rows) {
+  const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uintptr_t)base, size, pitch, box);
+}
+// The experts' weights [E, n_out, n_in]: boxes of 64 columns by box_rows of one expert.
+int map_weights(CUtensorMap* map, const nat_experts_params& p, const void* w, int box_rows) {
+  const cuuint64_t size[3] = {(cuuint64_t)p.n_in, (cuuint64_t)p.n_out, (cuuint64_t)p.n_experts};
+  const cuuint64_t pitch[2] = {(cuuint64_t)p.n_in * 2, (cuuint64_t)p.n_in * p.n_out * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (uintptr_t)w, size, pitch, box);
+}
 // Their gradient, or the parts' [slices, n_out, n_in] in float32: pieces of 32 x 32.
 int map_gradient(CUtensorMap* map, const nat_experts_params& p, const float* dw, int64_t slices) {
   const cuuint64_t size[3] = {(cuuint64_t)p.n_in, (cuuint64_t)p.n_out, (cuuint64_t)slices};
   const cuuint64_t pitch[2] = {(cuuint64_t)p.n_in * 4, (cuuint64_t)p.n_in * p.n_out * 4};
   const cuuint32_t box[3] = {32, 32, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (uintptr_t)dw, size, pitch, box);
+}
+
+// Of the current device, below 64.
+int device_index(int* dev) {
+  static std::atomic<bool> fits[64];
+  NAT_CUDA(cudaGetDevice(dev));
+  if (*dev < 0 || *dev >= 64)
+    return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", *dev);
+  if (!fits[*dev].load(std::memory_order_relaxed)) {
+    const int s = require_sm100();
+    if (s != NAT_OK) return s;
+    fits[*dev].store(true, std::memory_order_relaxed);
+  }
+  return NAT_OK;
 }
 
 // CTA pairs that the current device holds at a time, found once for each device.
@@ -580,19 +641,6 @@ constexpr int64_t kFew = 48;
 // with 512, 286 with 256; 1000 (16, 2048 x 2048) 164, 180; 1875 (64, 2048 x 1024) 536, 631; 4688 (64, 2048 x 1536)
 // 1654, 2021; 7500 (8, 4096 x 4096) 1623, 2054.
 constexpr int64_t kDwWide = 768;
-
-int device_index(int* dev) {
-  static std::atomic<bool> fits[64];
-  NAT_CUDA(cudaGetDevice(dev));
-  if (*dev < 0 || *dev >= 64)
-    return fail(NAT_ERR_UNSUPPORTED, "device index %d is beyond the 64 this library tracks", *dev);
-  if (!fits[*dev].load(std::memory_order_relaxed)) {
-    const int s = require_sm100();
-    if (s != NAT_OK) return s;
-    fits[*dev].store(true, std::memory_order_relaxed);
-  }
-  return NAT_OK;
-}
 
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
   if (which != kDw) return which == kFwd && cap / p.n_experts <= kFew ? kFewRows : 2 * BM;
