@@ -15,6 +15,7 @@
 // warp of each CTA waits for its own part of it, writes zeros over the rows behind (both operands': a weight of zero
 // would not hide an infinity), and the odd CTA tells the even one before the MMA warp is let on.
 #include <atomic>
+#include <type_traits>
 
 #include "nat_experts.cuh"
 #include "nat_tc.cuh"
@@ -32,15 +33,16 @@ constexpr int kTmemCols = 512;
 // 4.7e-6 with 96; 6.6e-6, 9.0e-6, 8.2e-6 with whole sums, which take 2 % less time; 1.8e-6 for the last with 32, which
 // takes 17 % more.
 constexpr int kSegment = 96;
-constexpr int kFewRows = 64;  // of a tile where the experts have few rows
-constexpr int kGroup = 8;     // row tiles that go through the columns together
+constexpr int kGroup = 8;  // row tiles that go through the columns together
 
 // ROWS: of a tile.  Shared memory: stages of A and half of B, and 4 KB pieces of finished rows for each warp that writes
 // out, from which they leave by TMA: two for kDw, whose epilogue nothing hides, one elsewhere.
 template <int WHICH, int ROWS>
 struct Ring {
   static constexpr int kSubs = ROWS <= 2 * BM ? 1 : 2;  // blocks of 128 rows of A a CTA holds
-  static constexpr int kABytes = ROWS / 2 * BK * 2, kBBytes = (BN / 2) * BK * 2, kStage = kABytes + kBBytes;
+  static constexpr int kABytes = ROWS / 2 * BK * 2, kBBytes = (BN / 2) * BK * 2;
+  static constexpr int kPer = ROWS < 2 * BM ? 2 : 1;  // blocks of the contraction in a stage
+  static constexpr int kBlock = kABytes + kBBytes, kStage = kPer * kBlock;
   static constexpr int kPieces = WHICH == kDw ? 2 : 1;
   static constexpr int kStaging = 4 * kSubs * kPieces * 4096;
   static constexpr int kBarriers = 512;
@@ -77,9 +79,9 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
     const int per = a.m_tiles * n_tiles, rank = u / (per * a.parts), in = u - rank * per * a.parts;
     const int part = in / per, tile = in - part * per;
     const Tile t = a.tiles[rank];
-    w.expert = t.expert;
-    w.lo = t.lo;
-    w.hi = t.hi;
+    w.expert = tc::uniform(t.expert);
+    w.lo = tc::uniform(t.lo);
+    w.hi = tc::uniform(t.hi);
     w.m0 = tile / n_tiles * ROWS;
     w.n0 = (tile - tile / n_tiles * n_tiles) * BN;
     part_range((w.hi - w.lo + BK - 1) / BK, part, a.parts, w.kb_lo, w.kb_hi);
@@ -90,9 +92,9 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
   const int left = max(1, min(kGroup, rows - grp * kGroup));
   const int n = in / left;
   const Tile t = a.tiles[grp * kGroup + in - n * left];
-  w.expert = t.expert;
-  w.lo = t.lo;
-  w.hi = t.hi;
+  w.expert = tc::uniform(t.expert);
+  w.lo = tc::uniform(t.lo);
+  w.hi = tc::uniform(t.hi);
   w.m0 = 0;
   w.n0 = n * BN;
   w.kb_lo = 0;
@@ -251,7 +253,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const int turned = turned_rows(w), each = turned ? turned / 2 : BM, first = rank * each;
       auto pieces_from = [&](int r) { return max(0, (min(w.hi - w.lo - r, each) + 31) / 32); };
       const int pieces = pieces_from(first), all_pieces = pieces + pieces_from(each - first);
-      for (int kb = w.kb_lo; kb < w.kb_hi; ++kb, ++it) {
+      for (int kb = w.kb_lo; kb < w.kb_hi; kb += R::kPer, ++it) {
         const int s = it % kNS;
         ok = all(tc::mbar_wait(&empty_bar[s], ((it / kNS) & 1u) ^ 1u, abort_flag));
         if (!ok) break;
@@ -263,7 +265,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           // from the last block to the first: the one that is not full, whose way takes longest, is then asked for while
           // the tile before is still at work
           const int t = w.lo + (w.kb_hi - 1 - (kb - w.kb_lo)) * BK, len = min(BK, w.hi - t);
-          if (lane == 0) {
+          if (tc::elect_one()) {
             if (len < BK) tc::mbar_arrive_expect_tx(tail_bar, R::kStage);
             else if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kStage);
 #pragma unroll
@@ -274,6 +276,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               else tc::tma_load_2d_pair(a_dst + j * kBox, map, bar, x, t);
             }
           }
+          __syncwarp();
           if (len < BK) {
             ok = all(tc::mbar_wait(tail_bar, tail_phase, abort_flag));
             if (!ok) break;
@@ -293,21 +296,27 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               if (lane == 0) tc::mbar_arrive(&full_bar[s]);
             }
           }
-        } else if (lane == 0) {
+        } else if (tc::elect_one()) {
           // of A only what has rows of the tile: 128 of them, or fewer in pieces of 32 (the rest of the stage is what it
           // was: rows of the accumulator that nobody writes out)
-          if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kBBytes + all_pieces * 32 * BK * 2);
-          if (pieces == 4) {
-            tc::tma_load_2d_pair(a_dst, &map_a, bar, kb * BK, w.lo + first);
-          } else {
-            for (int i = 0; i < pieces; ++i)
-              tc::tma_load_2d_pair(a_dst + i * 32 * BK * 2, &map_a32, bar, kb * BK, w.lo + first + i * 32);
-          }
-          if (WHICH == kFwd) {
-            load_3d_pair(b_dst, &map_b, bar, kb * BK, n0, w.expert);
-          } else {
+          const int here = min(R::kPer, w.kb_hi - kb);
+          if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], here * (2 * R::kBBytes + all_pieces * 32 * BK * 2));
 #pragma unroll
-            for (int j = 0; j < 2; ++j) load_3d_pair(b_dst + j * kBox, &map_b, bar, n0 + j * 64, kb * BK, w.expert);
+          for (int h = 0; h < R::kPer; ++h) {
+            if (h >= here) break;
+            const int at = h * R::kBlock, k0 = (kb + h) * BK;
+            if (pieces == 4) {
+              tc::tma_load_2d_pair(a_dst + at, &map_a, bar, k0, w.lo + first);
+            } else {
+              for (int i = 0; i < pieces; ++i)
+                tc::tma_load_2d_pair(a_dst + at + i * 32 * BK * 2, &map_a32, bar, k0, w.lo + first + i * 32);
+            }
+            if (WHICH == kFwd) {
+              load_3d_pair(b_dst + at, &map_b, bar, k0, n0, w.expert);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) load_3d_pair(b_dst + at + j * kBox, &map_b, bar, n0 + j * 64, k0, w.expert);
+            }
           }
         }
       }
@@ -336,7 +345,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         next = unit_after(u);
         if (skipped(w)) continue;
         const int segments = segments_of(w);
-        const int turned = WHICH == kDw ? 0 : tc::uniform(turned_rows(w));
+        const int turned = WHICH == kDw ? 0 : turned_rows(w);
         const uint32_t turned_idesc = tc::instr_desc_bf16(2 * BM, turned, kBcross ? 1 : 0, 0);
         for (int seg = 0; ok && seg < segments; ++seg, ++tcount) {
           const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
@@ -346,26 +355,31 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           if (!ok) break;
           tc::fence_after_sync();
           const uint32_t d_tmem = tmem_base + acc * SUBS * BN;
-          for (int kb = kb_lo; kb < kb_hi; ++kb, ++it) {
+          for (int kb = kb_lo; kb < kb_hi; kb += R::kPer, ++it) {
             const int s = it % kNS;
             ok = all(tc::mbar_wait(&full_bar[s], (it / kNS) & 1u, abort_flag));
             if (!ok) break;
             tc::fence_after_sync();
-            const uint32_t a_base = tc::smem_u32(smem + (size_t)s * R::kStage), b_base = a_base + R::kABytes;
+            const uint32_t stage = tc::smem_u32(smem + (size_t)s * R::kStage);
             if (tc::elect_one()) {
-              if (WHICH != kDw && turned) {
 #pragma unroll
-                for (int kk = 0; kk < BK / 16; ++kk)
-                  tc::umma_bf16_pair(d_tmem, step_desc<kBcross>(b_base, kk), step_desc<kAcross>(a_base, kk), turned_idesc,
-                                     (kb > kb_lo || kk > 0) ? 1u : 0u);
-              } else {
+              for (int h = 0; h < R::kPer; ++h) {
+                if (kb + h >= kb_hi) break;
+                const uint32_t a_base = stage + h * R::kBlock, b_base = a_base + R::kABytes;
+                if (WHICH != kDw && turned) {
 #pragma unroll
-                for (int kk = 0; kk < BK / 16; ++kk) {
-                  const uint64_t bdesc = step_desc<kBcross>(b_base, kk);
+                  for (int kk = 0; kk < BK / 16; ++kk)
+                    tc::umma_bf16_pair(d_tmem, step_desc<kBcross>(b_base, kk), step_desc<kAcross>(a_base, kk), turned_idesc,
+                                       (kb + h > kb_lo || kk > 0) ? 1u : 0u);
+                } else {
 #pragma unroll
-                  for (int sub = 0; sub < SUBS; ++sub)
-                    tc::umma_bf16_pair(d_tmem + sub * BN, step_desc<kAcross>(a_base + sub * (BM * BK * 2), kk), bdesc, kIdesc,
-                                       (kb > kb_lo || kk > 0) ? 1u : 0u);
+                  for (int kk = 0; kk < BK / 16; ++kk) {
+                    const uint64_t bdesc = step_desc<kBcross>(b_base, kk);
+#pragma unroll
+                    for (int sub = 0; sub < SUBS; ++sub)
+                      tc::umma_bf16_pair(d_tmem + sub * BN, step_desc<kAcross>(a_base + sub * (BM * BK * 2), kk), bdesc,
+                                         kIdesc, (kb + h > kb_lo || kk > 0) ? 1u : 0u);
+                  }
                 }
               }
               tc::umma_commit_pair(&empty_bar[s], 3);
@@ -628,25 +642,26 @@ int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb
 
 }  // namespace
 
-// Average rows of an expert (by the capacity, which is what the host knows) up to which the forward product takes tiles of
-// 64 rows, whose small stages leave room for ten in place of six: what bounds it then is the reading of the weights.  us, tiles
-// of 256 rows / of 64:
-//   rows an expert                   8            31           47           62
-//   32 experts, 4096 x 1536     80.6, 76.6   84.1, 80.2   87.6, 81.9   92.7, 100.0
-//   128 experts, 2048 x 768     78.5, 75.7   82.8, 80.1       -        91.4, 103.3
-//   8 experts, 4096 x 4096      55.3, 52.7   57.2, 54.8       -        62.4, 72.8
-// The rows' gradient reads the weights in longer pieces, and takes the same time with either.
-constexpr int64_t kFew = 48;
+// Average rows of an expert (by the capacity, which is what the host knows) up to which a row tile has 64 or 128 rows in
+// place of 256.  All are turned then, a stage holds two blocks of the contraction (a block with few rows is done with
+// sooner than its barriers are), and what is left to bound it is the reading of the weights.  us, tiles of 256, 128 and 64
+// rows, forward:
+//   rows an expert                  31             47             62             94             125
+//   32 experts, 4096 x 1536     83, 77, 75     86, 79, 76     90, 83, 85     94, 87, 106    98, 100, -
+//   128 experts, 2048 x 768         -          85, 80, 78     89, 83, 84     96, 88, 105    104, 103, -
+//   8 experts, 4096 x 4096          -          59, 55, 53     60, 56, 62         -          66, 74, -
+constexpr int64_t kFew = 48, kSome = 96;
 // And from which the weights' gradient takes tiles of 512 rows in place of 256: 312 rows (128 experts, 2048 x 768) 321 us
 // with 512, 286 with 256; 1000 (16, 2048 x 2048) 164, 180; 1875 (64, 2048 x 1024) 536, 631; 4688 (64, 2048 x 1536)
 // 1654, 2021; 7500 (8, 4096 x 4096) 1623, 2054.
 constexpr int64_t kDwWide = 768;
 
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
-  if (which != kDw) return which == kFwd && cap / p.n_experts <= kFew ? kFewRows : 2 * BM;
+  const int64_t rows = cap / p.n_experts;
+  if (which != kDw) return rows <= kFew ? BM / 2 : rows <= kSome ? BM : 2 * BM;
   // A tile of 512 rows of the result takes a quarter fewer operand bytes, but leaves no second accumulator in whose
   // shadow it is written out: worth it where the experts have rows enough.
-  return cap / p.n_experts >= kDwWide ? 4 * BM : 2 * BM;
+  return rows >= kDwWide ? 4 * BM : 2 * BM;
 }
 
 int bf16_product(const Args& a, const Layout& l, Product which) {
@@ -685,9 +700,15 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   if ((s = map_weights(&mb, p, a.w, fwd ? BN / 2 : BK)) != NAT_OK) return s;
   if ((s = map_rows(&mc, out, n, a.cap, t.rows_stride, 32)) != NAT_OK) return s;
   const int64_t units = l.most_tiles * ((n + BN - 1) / BN);
-  if (l.tile_rows[which] == kFewRows) return launch<kFwd, kFewRows>(ma, ma32, mb, mc, t, units, a.stream);
-  return fwd ? launch<kFwd, 2 * BM>(ma, ma32, mb, mc, t, units, a.stream)
-             : launch<kDx, 2 * BM>(ma, ma32, mb, mc, t, units, a.stream);
+  auto product = [&](auto tile_rows) {
+    constexpr int kRows = decltype(tile_rows)::value;
+    return fwd ? launch<kFwd, kRows>(ma, ma32, mb, mc, t, units, a.stream) : launch<kDx, kRows>(ma, ma32, mb, mc, t, units, a.stream);
+  };
+  switch (l.tile_rows[which]) {
+    case BM / 2: return product(std::integral_constant<int, BM / 2>());
+    case BM: return product(std::integral_constant<int, BM>());
+    default: return product(std::integral_constant<int, 2 * BM>());
+  }
 }
 
 }  // namespace experts
