@@ -30,8 +30,8 @@ constexpr int kTmemCols = 512;
 // Blocks of the contraction that a kDw tile's accumulator takes at most: the tensor cores cut off what they add (toward
 // zero, about half a step of 2^-23 each time), so after that many the sum is added to the result in memory, rounded to
 // nearest, and begun anew.  Relative error of a gradient of 6,058, 8,193 and up to 17,389 rows an expert: 6.6e-6, 4.4e-6,
-// 4.7e-6 with 96; 6.6e-6, 9.0e-6, 8.2e-6 with whole sums, which take 2 % less time; 1.8e-6 for the last with 32, which
-// takes 17 % more.
+// 4.7e-6 with 96; 6.6e-6, 9.0e-6, 8.2e-6 with whole sums, which take 0 to 7 % less time; 1.8e-6 for the last with 32, which
+// takes 11 to 20 % more.
 constexpr int kSegment = 96;
 constexpr int kGroup = 8;  // row tiles that go through the columns together
 
@@ -651,9 +651,9 @@ int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb
 //   128 experts, 2048 x 768         -          85, 80, 78     89, 83, 84     96, 88, 105    104, 103, -
 //   8 experts, 4096 x 4096          -          59, 55, 53     60, 56, 62         -          66, 74, -
 constexpr int64_t kFew = 48, kSome = 96;
-// And from which the weights' gradient takes tiles of 512 rows in place of 256: 312 rows (128 experts, 2048 x 768) 321 us
-// with 512, 286 with 256; 1000 (16, 2048 x 2048) 164, 180; 1875 (64, 2048 x 1024) 536, 631; 4688 (64, 2048 x 1536)
-// 1654, 2021; 7500 (8, 4096 x 4096) 1623, 2054.
+// And from which the weights' gradient takes tiles of 512 rows in place of 256: 312 rows (128 experts, 2048 x 768) 316 us
+// with 512, 280 with 256; 500 (32, 2048 x 1024) 114, 115; 1000 (16, 2048 x 2048) 161, 163; 1875 (64, 2048 x 1024) 556, 552;
+// 4688 (64, 2048 x 1536) 1760, 1863; 7500 (8, 4096 x 4096) 1764, 1863.
 constexpr int64_t kDwWide = 768;
 
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
