@@ -313,13 +313,12 @@ GROUP8 = 128                 # columns that share a scale in an 8-bit checkpoint
 
 def _device():
     try:
-        return torch.cuda.current_device()
-    except (RuntimeError, AssertionError):
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
         return None                # no CUDA device: no tensor is on it
 
 
-def _raw_stream(device):
-    return torch._C._cuda_getCurrentRawStream(device)
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _bad(what, t, dtype, shape, device):
@@ -349,9 +348,9 @@ def _heads(what, t, dtype, shape, device):
     if t.dtype is dtype and t.get_device() == device:
         s = t.shape
         if s == shape or (len(s) == 3 and s[0] >= shape[0] and s[1:] == shape[1:]):
-            st = t.stride()
-            if st[2] == 1 and (s[1] == 1 or st[1] == s[2]):
-                return t.data_ptr(), st[0] if s[0] > 1 else None
+            token, head, one = t.stride()
+            if one == 1 and (head == shape[2] or shape[1] == 1):
+                return t.data_ptr(), token if shape[0] > 1 or s[0] > 1 else None
     _bad(what, t, dtype, shape, device)
 
 
@@ -553,14 +552,17 @@ def _qknorm_call(params, B, cu_seqlens, positions, n_rows, cap, w_q, w_k, inv_fr
             continue
         ptr, stride = _heads(name, t, dtype, (cap, heads, D), dev)
         ptrs.append(ptr)
-        if stride is not None and strides.setdefault(field, stride) != stride:
-            raise NatError(f"{name}: token stride {stride}, its counterpart has {strides[field]}")
-    for field, stride in strides.items():
-        setattr(p, field, stride)
-    where = (B, _rows("cu_seqlens", cu_seqlens, torch.int32, (B + 1,), dev),
-             _rows("positions", positions, torch.int32, (cap,), dev), _rows("n_rows", n_rows, torch.int32, (1,), dev), cap)
-    laws = (_rows("w_q", w_q, torch.float32, (D,), dev), _rows("w_k", w_k, torch.float32, (D,), dev),
-            _rows("inv_freq", inv_freq, torch.float64, (params.rot_dim // 2,), dev))
+        if stride is not None:
+            if field not in strides:
+                strides[field] = stride
+                setattr(p, field, stride)
+            elif strides[field] != stride:
+                raise NatError(f"{name}: token stride {stride}, its counterpart has {strides[field]}")
+    i32, f32 = torch.int32, torch.float32
+    where = (B, _rows("cu_seqlens", cu_seqlens, i32, (B + 1,), dev), _rows("positions", positions, i32, (cap,), dev),
+             _rows("n_rows", n_rows, i32, (1,), dev), cap)
+    laws = (_rows("w_q", w_q, f32, (D,), dev), _rows("w_k", w_k, f32, (D,), dev),
+            _rows("inv_freq", inv_freq, torch.float64, (p.rot_dim // 2,), dev))
     return p, where, laws, ptrs, dev
 
 
@@ -612,14 +614,16 @@ def _experts_call(params, offsets, cap, w, workspace, tensors):
         if t is None:
             ptrs.append(None)
             continue
-        s = t.shape
-        if t.dtype is not dtype or t.get_device() != dev or len(s) != 2 or s[0] < cap or s[1] != width or t.stride(1) != 1:
+        s, st = t.shape, t.stride()
+        if t.dtype is not dtype or t.get_device() != dev or len(s) != 2 or s[0] < cap or s[1] != width or st[1] != 1:
             _bad(name, t, dtype, (cap, width), dev)
         ptrs.append(t.data_ptr())
-        if s[0] > 1 and strides.setdefault(field, t.stride(0)) != t.stride(0):
-            raise NatError(f"{name}: row stride {t.stride(0)}, its counterpart has {strides[field]}")
-    for field, stride in strides.items():
-        setattr(p, field, stride)
+        if s[0] > 1:
+            if field not in strides:
+                strides[field] = st[0]
+                setattr(p, field, st[0])
+            elif strides[field] != st[0]:
+                raise NatError(f"{name}: row stride {st[0]}, its counterpart has {strides[field]}")
     ws, nbytes = _workspace(workspace, dev)
     E = params.n_experts
     if w is not None and w.shape[0] != E:
@@ -662,7 +666,8 @@ def alloc_workspace(nbytes, device):
 
 
 def nat_poll_status(workspace):
-    """The NAT_DEV_* bits the last loss or attention call left in its workspace (waits for the stream)."""
+    """The NAT_DEV_* bits the last loss, attention, embedding or experts call left in its workspace (waits for the
+    stream)."""
     word = ctypes.c_uint32(0)
     _check(load().nat_poll_status(_ptr(workspace), _stream(), ctypes.byref(word)))
     return int(word.value)
