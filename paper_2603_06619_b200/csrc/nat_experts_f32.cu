@@ -3,7 +3,8 @@
 // 256 threads share a T x T tile of the result, R x R elements each (T = 16 R), and go through the contraction 16 at a
 // time, three slices of both operands ahead by asynchronous copies; four steps of the contraction are 2 R reads of
 // 16 bytes for 2 R^2 packed multiply-adds.  T = 128, or 64 for small problems, which wait for memory rather than
-// compute.  8000 rows over four experts, 512 x 512: forward 124 us (34 TFLOP/s), both gradients 260.
+// compute.  8000 rows over four experts, 1024 x 1024: forward 453 us (37 TFLOP/s of 74), the rows' gradient 413, the weights'
+// 426.
 #include <atomic>
 
 #include "nat_experts.cuh"
@@ -158,11 +159,14 @@ __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
   const A oa{smem, g.a, g.a_stride, m0, m_end, k_end};
   const B ob{smem + kStages * A::kFloats, g.b + (WHICH == kDw ? 0 : expert * g.b_expert), g.b_stride, n0, g.n_cols, k_end};
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-  float2 acc[R][R / 2];
+  // kFwd: a pair is the sums over even and odd steps, neighbours in registers as they come (453 us; neighbouring columns
+  // one by one 471, packed 680); elsewhere it is two neighbouring columns
+  constexpr int kCols = WHICH == kFwd ? R : R / 2;
+  float2 acc[R][kCols];
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < R / 2; ++j) acc[i][j] = both(0.f);
+    for (int j = 0; j < kCols; ++j) acc[i][j] = both(0.f);
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) {
     if (k0 + i * kK < k_end) {
@@ -187,17 +191,15 @@ __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
       oa.get(stage, kk, ty, x);
       ob.get(stage, kk, tx, y);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; j += WHICH == kFwd ? 2 : 1)
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-          for (int c = 0; c < R / 2; ++c) {
-            if (WHICH == kFwd) {  // neighbouring columns come in different registers: packing them costs more (124 us, 178)
-              acc[i][c].x = fmaf(x[j][i], y[j][2 * c], acc[i][c].x);
-              acc[i][c].y = fmaf(x[j][i], y[j][2 * c + 1], acc[i][c].y);
-            } else {
+          for (int c = 0; c < kCols; ++c) {
+            if (WHICH == kFwd)
+              acc[i][c] = fma2(make_float2(x[j][i], x[j + 1][i]), make_float2(y[j][c], y[j + 1][c]), acc[i][c]);
+            else
               acc[i][c] = fma2(both(x[j][i]), make_float2(y[j][2 * c], y[j][2 * c + 1]), acc[i][c]);
-            }
           }
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -212,14 +214,14 @@ __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
     float* row = c + (int64_t)r * g.c_stride;
 #pragma unroll
     for (int j = 0; j < R; j += 4) {
-      const float v[4] = {acc[i][j / 2].x, acc[i][j / 2].y, acc[i][j / 2 + 1].x, acc[i][j / 2 + 1].y};
       if (WHICH == kFwd) {  // a thread's columns are 16 apart
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int col = n0 + B::place(j + e, tx);
-          if (col < g.n_cols) row[col] = v[e];
+          if (col < g.n_cols) row[col] = acc[i][(j + e) % kCols].x + acc[i][(j + e) % kCols].y;
         }
       } else {
+        const float v[4] = {acc[i][j / 2].x, acc[i][j / 2].y, acc[i][j / 2 + 1].x, acc[i][j / 2 + 1].y};
         const int col = n0 + B::place(j, tx);
         if (col >= g.n_cols) continue;
         float4* at = reinterpret_cast<float4*>(row + col);
