@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(kThreads) f32_kernel(const F32Args g) {
   const A oa{smem, g.a, g.a_stride, m0, m_end, k_end};
   const B ob{smem + kStages * A::kFloats, g.b + (WHICH == kDw ? 0 : expert * g.b_expert), g.b_stride, n0, g.n_cols, k_end};
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-  // kFwd: a pair is the sums over even and odd steps, neighbours in registers as they come (453 us; neighbouring columns
-  // one by one 471, packed 680); elsewhere it is two neighbouring columns
+  // kFwd: a pair is the sums over even and odd steps, neighbours in registers as they come (453 us; neighbouring columns,
+  // which have to be brought together, 471); elsewhere it is two neighbouring columns
   constexpr int kCols = WHICH == kFwd ? R : R / 2;
   float2 acc[R][kCols];
 #pragma unroll

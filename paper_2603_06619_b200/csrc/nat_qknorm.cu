@@ -61,7 +61,9 @@ __device__ __forceinline__ int owner(const int32_t* cu, int B, int64_t n) {
   return lo;
 }
 
-// A lane's two chunks of a head's row and the pairs that they hold.
+// A lane's two chunks of a head's row and the pairs that they hold.  First chunks of neighbouring lanes lie side by side,
+// and second ones: whole sectors at a time (a lane's two side by side instead, for the elements that do not turn: 160,000
+// tokens of 32 and 8 heads of 128 of which 64 turn forward 657 us, 564 like this; backward 1004, 839).
 struct Slot {
   int a, b;        // first elements; b < 0: none
   bool turns, in;  // the lane has a part of the row at all
@@ -69,9 +71,9 @@ struct Slot {
 __device__ __forceinline__ Slot slot_of(const nat_qknorm_params& p, int lane) {
   const int r16 = p.rot_dim / 16, rest = (p.head_dim - p.rot_dim) / kChunk;
   if (lane < r16) return {lane * kChunk, (lane + r16) * kChunk, true, true};
-  const int j = 2 * (lane - r16);
-  if (j >= rest) return {0, -1, false, false};
-  return {p.rot_dim + j * kChunk, j + 1 < rest ? p.rot_dim + (j + 1) * kChunk : -1, false, true};
+  const int j = lane - r16, half = (rest + 1) / 2;
+  if (j >= half) return {0, -1, false, false};
+  return {p.rot_dim + j * kChunk, j + half < rest ? p.rot_dim + (j + half) * kChunk : -1, false, true};
 }
 // Number i of the angle of the lane's e-th pair.
 template <bool INTER>
