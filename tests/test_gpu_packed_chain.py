@@ -100,6 +100,29 @@ def test_one_step_captured_beside_an_eager_one():
         assert all(p.status() == 0 for p in (*a[:3], *b[:3]))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_positions_that_are_given_leave_the_rows_behind_the_last_sequence_alone(dtype):
+    """The same positions, given and from the bounds, with NaN rows behind: the same bits."""
+    B, n, cap, Hq, Hkv, D = 2, 33, 50, 4, 2, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    cu = torch.tensor([0, 20, n], dtype=torch.int32, device="cuda")
+    qkv, dqk = rand(cap, Hq + 2 * Hkv, D).to(dtype), rand(cap, Hq + Hkv, D).to(dtype)
+    qkv[n:], dqk[n:] = float("nan"), float("nan")
+    positions = torch.full((cap,), 5, dtype=torch.int32, device="cuda")
+    positions[:20], positions[20:n] = torch.arange(20), torch.arange(n - 20)
+    w, freq = 1 + 0.1 * rand(D), nat.rope_freqs(D, 1e4)
+    got = []
+    for at in (None, positions):
+        sub = PackedSublayer(cap, B, 128, Hq, Hkv, D, dtype)
+        qk = sub.rotate(qkv, cu, w, w, freq, positions=at, qk=torch.full_like(dqk, 7.0))
+        dqkv = sub.rotate_backward(qkv, cu, w, w, freq, torch.full_like(qkv, 7.0), positions=at, dqk=dqk)
+        got.append((qk, dqkv, sub.dw_q, sub.dw_k))
+        assert (qk[n:] == 7).all() and (dqkv[n:] == 7).all() and sub.dw_q.isfinite().all() and sub.dw_k.isfinite().all()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
 FIRST_CALLS = """
 import sys
 sys.path.insert(0, {root!r})
