@@ -385,9 +385,10 @@ __device__ __forceinline__ void add_tokens(const SumArgs& a, R row_of, uint32_t 
   }
 }
 
-// Rows of the table a block writes, at most (74,003 tokens, 1024 columns: 175 us with 16, 172 with 24 or 32; 166,001, 4096:
-// 678, 680, 696).
-constexpr int kRowsPerBlock = 24;
+// Rows of the table a block writes: 96 KB of them, between 24 and 128 (74,003 tokens, 1024 columns: 175 us with 16, 172 with
+// 24 or 32; 166,001, 4096: 678, 680, 696; 40,000 tokens, 128 columns, V 152,000: 76 us with 24, 65 with 128; 9,000 tokens,
+// 64 columns, V 1,000,000: 155, 90).
+constexpr int kRowsPerBlock = 128, kFewestRows = 24, kBlockBytes = 96 * 1024;
 
 // Blocks [0, tiles): the piece of a table row with more than kPiece tokens that lies in a tile of kPiece sorted
 // positions.  A tile meets at most two such rows, one that began before it (slot 0) and one that begins in it and
@@ -672,7 +673,7 @@ int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable,
       src = dst;
     }
   }
-  SumArgs a{r, pairs[src], dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), kRowsPerBlock,
+  SumArgs a{r, pairs[src], dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), max(kFewestRows, min(kRowsPerBlock, kBlockBytes / (4 * p.d))),
             l.tiles, p.scale, p.accumulate != 0};
   while (a.rows_per_block > 1 && p.V / a.rows_per_block < 148 * 8) a.rows_per_block >>= 1;
   s = launch_after(sum_kernel<T>, dim3((unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block)), kThreads, 0,
