@@ -25,7 +25,9 @@ constexpr int kTile = 2048;        // pairs a block sorts at a time
 constexpr int kWarps = kThreads / 32;
 constexpr int kRounds = kTile / kThreads;
 constexpr int kMaxDigits = 512;
-constexpr uint32_t kPiece = 128;   // sorted tokens of a piece; a table row with more is added up in pieces
+// Sorted tokens of a piece; a table row with more is added up in pieces.  us with 128, 64, 32: 20,000 tokens of 512 columns
+// 100, 93, 89; 166,001 of 4096 687, 677, 701; 5,000 of 512 with two ids 27, 21, 20; 166,001 of 1024 with 512 ids 93, 99, 113.
+constexpr uint32_t kPiece = 64;
 
 struct Rows {
   const int32_t *ids, *sel_idx, *n_rows;

@@ -56,11 +56,11 @@ def test_embed_refusals():
 
 def test_embed_workspace_grows_with_cap():
     sizes = [nat.nat_embed_workspace_bytes(nat.embed_params(151936, 4096, torch.bfloat16), c)
-             for c in (0, 1, 127, 128, 129, 4096, 4097, 166001, 1 << 24)]
+             for c in (0, 1, 63, 64, 65, 127, 128, 129, 4096, 4097, 166001, 1 << 24)]
     assert sizes == sorted(sizes) and sizes[0] > 0
-    # pairs twice, their counts, and two pieces of a row for every 128 tokens
+    # pairs twice, their counts, and two pieces of a row for every 64 tokens
     n, d = 166001, 4096
-    assert sizes[7] <= 16 * n + 4 * 512 * (n // 2048 + 2) + 2 * 4 * d * (n // 128 + 1) + 8 * 256
+    assert sizes[10] <= 16 * n + 4 * 512 * (n // 2048 + 2) + 2 * 4 * d * (n // 64 + 1) + 8 * 256
 
 
 # ------------------------------------------------------------------------- head norms
@@ -149,7 +149,7 @@ def test_experts_workspace_holds_to_its_bound():
         for dtype in (torch.float32, torch.bfloat16):
             for cap in (0, 1, 5000, 300013):
                 n = nat.nat_experts_workspace_bytes(nat.experts_params(E, n_in, n_out, dtype), cap)
-                assert 0 < n <= 40e6 + 16 * (cap // 128 + E) + 4 * E + 4 * 256
+                assert 0 < n <= 40e6 + 16 * (cap // 64 + 2 * E) + 4 * 256
 
 
 def test_binding_refuses_host_tensors_types_shapes_and_strides():
