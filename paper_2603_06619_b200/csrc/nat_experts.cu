@@ -53,27 +53,45 @@ plan_kernel(const int32_t* offsets, int E, int64_t cap, int tile_rows, Head* hea
   }
 }
 
-// dw (+)= the parts' sums, in their order.
-__global__ void __launch_bounds__(256)
+// dw (+)= the parts' sums: the warps take runs of parts, 256 elements at a time, and their sums are added in the runs' order
+// (a thread for all parts of an element: 37,106 rows, 40 x 16, 289 parts, both gradients 92 us, 38 like this).
+constexpr int kJoinWarps = 8;
+
+__global__ void __launch_bounds__(kJoinWarps * 32)
 join_kernel(const float* partial, int parts, int64_t size, const Head* head, bool accumulate, float* dw) {
+  __shared__ float2 sums[kJoinWarps][32][rows::kPairs];
   if (head->broken) return;
-  const int64_t step = (int64_t)gridDim.x * 256 * rows::kChunk;
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * rows::kChunk; i < size; i += step) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = (parts + kJoinWarps - 1) / kJoinWarps, lo = min(warp * per, parts), hi = min(lo + per, parts);
+  const int64_t step = (int64_t)gridDim.x * 32 * rows::kChunk;
+  for (int64_t first = (int64_t)blockIdx.x * 32 * rows::kChunk; first < size; first += step) {
+    const int64_t i = first + lane * rows::kChunk;
     float2 sum[rows::kPairs], v[rows::kPairs];
-    rows::widen(rows::load_raw(partial + i), sum);
-    for (int p = 1; p < parts; ++p) {
-      rows::widen(rows::load_raw(partial + p * size + i), v);
 #pragma unroll
-      for (int j = 0; j < rows::kPairs; ++j) sum[j] = add2(sum[j], v[j]);
-    }
-    if (accumulate) {
-      rows::widen(rows::load_raw(dw + i), v);
+    for (int j = 0; j < rows::kPairs; ++j) sum[j] = both(0.f);
+    if (i < size) {
+#pragma unroll 4
+      for (int p = lo; p < hi; ++p) {
+        rows::widen(rows::load_raw(partial + p * size + i), v);
 #pragma unroll
-      for (int j = 0; j < rows::kPairs; ++j) sum[j] = add2(v[j], sum[j]);
+        for (int j = 0; j < rows::kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+      }
     }
-    rows::Raw<float> out;
-    rows::narrow(sum, out);
-    rows::store_raw(dw + i, out);
+#pragma unroll
+    for (int j = 0; j < rows::kPairs; ++j) sums[warp][lane][j] = sum[j];
+    __syncthreads();
+    if (warp == 0 && i < size) {
+      if (accumulate) rows::widen(rows::load_raw(dw + i), v);
+#pragma unroll
+      for (int j = 0; j < rows::kPairs; ++j) {
+        for (int w = 1; w < kJoinWarps; ++w) sum[j] = add2(sum[j], sums[w][lane][j]);
+        if (accumulate) sum[j] = add2(v[j], sum[j]);
+      }
+      rows::Raw<float> out;
+      rows::narrow(sum, out);
+      rows::store_raw(dw + i, out);
+    }
+    __syncthreads();
   }
 }
 
@@ -135,12 +153,22 @@ Layout layout(const nat_experts_params& p, int64_t cap) {
   for (int i = 0; i < 3; ++i) l.tile_rows[i] = f32 ? f32_tile(p, (Product)i, cap) : bf16_tile_rows(p, (Product)i, cap);
   // an expert's last tile may be part full: at most one extra tile for each
   l.most_tiles = cap / min(l.tile_rows[0], l.tile_rows[1]) + p.n_experts;
-  // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows (float32: 128) of an average expert at
-  // least.
+  // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows (float32: 64) of an average expert at
+  // least, whose sums take up to 40 MB.  One expert's parts are of one length, and as many as are held at a time; of
+  // several experts one may have most of the rows, so there are up to four times as many.  us, as many as held / twice / four
+  // times (float32: as many, of 128 rows at least / four times, of 64):
+  //   one expert's 300,000 rows, 256 x 256          156, 171, 191
+  //   4 experts, 245,491 rows, 560 x 16, uneven     369, 274, 236     6, 85,068, 432 x 16, uneven   152, 106, 96
+  //   4, 100,000, 256 x 512, nearly even             92, 103, 103     15, 66,802, 24 x 912, even     74, 77, 82
+  //   float32: 10, 61,655, 104 x 296                618, 325          80, 32,601, 48 x 136, uneven  450, 164
+  //            2, 178,829, 8 x 16, even               82, 97
+  const bool lone = p.n_experts == 1;
   const int64_t rows = l.tile_rows[kDw], cols = f32 ? rows : kBf16Cols;
   const int64_t units = p.n_experts * ((p.n_out + rows - 1) / rows) * ((p.n_in + cols - 1) / cols);
-  const int64_t fit = (f32 ? 296 : 74) / units, worth = cap / p.n_experts / (f32 ? 128 : 512);
-  l.parts = (int)max((int64_t)1, min(fit, worth));
+  const int64_t fit = (f32 ? (lone ? 296 : 1184) : (lone ? 74 : 296)) / units;
+  const int64_t worth = cap / p.n_experts / (f32 ? (lone ? 128 : 64) : 512);
+  const int64_t room = 40000000 / ((int64_t)p.n_experts * p.n_out * p.n_in * 4);
+  l.parts = (int)max((int64_t)1, min(min(fit, worth), room));
   size_t at = 256;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -202,8 +230,8 @@ int nat_experts_bwd(const nat_experts_params* p, const int32_t* offsets, int64_t
   }
   s = product(a, l, kDw);
   if (s != NAT_OK || l.parts == 1) return s;
-  const int64_t want = (size / nat::rows::kChunk + 255) / 256;
-  join_kernel<<<(unsigned)min(want, (int64_t)148 * 8), 256, 0, a.stream>>>(partial(a, l), l.parts, size, head(a),
+  const int64_t want = (size / nat::rows::kChunk + 31) / 32;
+  join_kernel<<<(unsigned)min(want, (int64_t)148 * 8), kJoinWarps * 32, 0, a.stream>>>(partial(a, l), l.parts, size, head(a),
                                                                           p->accumulate != 0, dw);
   NAT_LAUNCH_CHECK("experts_join");
   return NAT_OK;

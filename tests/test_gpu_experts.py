@@ -133,7 +133,7 @@ def test_experts_rows_cut_into_parts(loads, accumulate, dtype):
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_experts_sums_longer_than_an_accumulator_takes(accumulate):
     """Tiles enough that the rows are not cut into parts; sums of thousands of rows are added up in pieces, in order."""
-    e = Experts([7000, 10, 6300, 0, 1, 200, 0, 12500], 520, 1032, torch.bfloat16, seed=12, accumulate=accumulate)
+    e = Experts([7000, 10, 6300, 0, 1, 200, 0, 12500], 520, 2056, torch.bfloat16, seed=12, accumulate=accumulate)
     assert nat.nat_experts_workspace_bytes(e.params, e.cap) < 1 << 20
     e.check()
     first = e.dw.clone()
