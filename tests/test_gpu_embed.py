@@ -81,7 +81,7 @@ class Embed:
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,V,d", [(0, 5, 8), (1, 1, 8), (1, 700, 64), (290, 512, 64), (128, 3, 136), (129, 1, 40),
                                    (700, 2, 256), (4096, 300, 72), (4097, 300, 72), (9001, 70000, 24), (500, 50, 2056),
-                                   (20000, 37, 16), (300, 9, 4096), (40, 1000, 8200), (2049, 5, 8), (70001, 400, 8),
+                                   (20000, 37, 16), (300, 9, 4096), (40, 1000, 8200), (2049, 5, 8), (1024, 700, 40), (1025, 9, 72), (70001, 400, 8),
                                    (70001, 1 << 20, 8), (300001, 150000, 8), (262144, 200, 8)])
 def test_embed_parity(n, V, d, dtype):
     Embed(n, V, d, DT[dtype], seed=n + V, scale=0.75 if d > 64 else 1.0, picked=n % 2 == 1).check()

@@ -60,7 +60,7 @@ def test_embed_workspace_grows_with_cap():
     assert sizes == sorted(sizes) and sizes[0] > 0
     # pairs twice, their counts, and two pieces of a row for every 64 tokens
     n, d = 166001, 4096
-    assert sizes[10] <= 16 * n + 4 * 512 * (n // 2048 + 2) + 2 * 4 * d * (n // 64 + 1) + 8 * 256
+    assert sizes[10] <= 16 * n + 4 * 512 * (n // 1024 + 2) + 2 * 4 * d * (n // 64 + 1) + 8 * 256
 
 
 # ------------------------------------------------------------------------- head norms
