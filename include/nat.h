@@ -499,8 +499,9 @@ int nat_ckpt8_load(int32_t dtype, int64_t d, const int8_t* codes, const float* s
  * n_rows: device int32 scalar (NULL: cap); rows at or after it are neither written nor read.
  * An id outside [0, V) has no row: x_k is NaN, and the gradient leaves the token out and raises NAT_DEV_BAD_TARGET in
  * the status word at the head of the workspace (nat_poll_status).
- * The tokens are sorted by id and a table row's are added in 32 bits in ascending order k, in pieces cut at every 64th
- * sorted token where there are more than 64; a call repeated on the same inputs reproduces its output bit for bit.
+ * The tokens are sorted by id and a table row's are added in 32 bits in ascending order k, in pieces of up to 64
+ * where there are more than 64, whose cuts the sizes and positions determine; a call repeated on the same inputs
+ * reproduces its output bit for bit.
  * d a multiple of 8, at most 65536; V at most 2^30; matrices 16-byte aligned.
  * workspace (gradient only): nat_embed_workspace_bytes(params, cap), which grows with cap; calls that may run at the
  * same time need one each.  A call with cap = 0 does nothing (the gradient: it still writes dtable's zeros, and the

@@ -396,8 +396,9 @@ constexpr int kRowsPerBlock = 128, kFewestRows = 24, kBlockBytes = 96 * 1024;
 
 // Blocks [0, tiles): the piece of a table row with more than kPiece tokens that lies in a tile of kPiece sorted
 // positions.  A tile meets at most two such rows, one that began before it (slot 0) and one that begins in it and
-// goes on behind it (slot 1).  The blocks behind: rows of the table with up to kPiece tokens.
-template <typename T>
+// goes on behind it (slot 1).  The blocks behind: rows of the table with up to kPiece tokens, or, where there are no
+// blocks for pieces, all.
+template <typename T, bool PIECES>
 __global__ void __launch_bounds__(kThreads, kSumBlocks) sum_kernel(SumArgs a) {
   release_secondary();
   wait_for_primary();
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, kSumBlocks) sum_kernel(SumArgs a) {
   const uint32_t n = row_count(a.r);
   const int tpr = 1 << a.tpr_log2, group = threadIdx.x >> a.tpr_log2, groups = kThreads >> a.tpr_log2;
   const int first = (threadIdx.x & (tpr - 1)) * kChunk, stride = kChunk << a.tpr_log2;
-  if (blockIdx.x < (unsigned)a.tiles) {
+  if (PIECES && blockIdx.x < (unsigned)a.tiles) {
     const uint32_t t0 = blockIdx.x * kPiece, t1 = min(t0 + kPiece, n);
     if (t0 >= n) return;
     // a row that goes on over an end of the tile has the same id on both sides of it; most tiles have none
@@ -485,6 +486,37 @@ __global__ void __launch_bounds__(kThreads, kSumBlocks) sum_kernel(SumArgs a) {
   };
   if (few) write_rows([&](uint32_t i) { return row_at[i - lo0]; });
   else write_rows([&](uint32_t i) { return a.pairs[i].y; });
+  if (PIECES || hi0 - lo0 <= kPiece) return;
+  // without blocks for pieces: a row with more than kPiece tokens by the whole block, a run of them a group
+  __shared__ float2 sums[PIECES ? 1 : kThreads][kPairs];
+  for (int i = 0; i < count; ++i) {
+    const uint32_t lo = start[i], hi = start[i + 1];
+    if (hi - lo <= kPiece) continue;  // the same for all threads
+    const uint32_t per = (hi - lo + groups - 1) / groups, from = min(lo + group * per, hi), to = min(from + per, hi);
+    float* row = a.dtable + (int64_t)(v0 + i) * a.d;
+    for (int base = 0; base < a.d; base += stride) {
+      const int c = base + first;
+      float2 sum[kPairs];
+      if (c < a.d) add_tokens<T>(a, [&](uint32_t k) { return a.pairs[k].y; }, from, to, c, sum);
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) sums[threadIdx.x][j] = sum[j];
+      __syncthreads();
+      if (group == 0 && c < a.d) {
+        float2 old[kPairs];
+        if (a.accumulate) rows::widen(rows::load_raw(row + c), old);
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+          for (int g = 1; g < groups; ++g) sum[j] = add2(sum[j], sums[g * tpr + threadIdx.x][j]);
+          sum[j] = mul2(sum[j], both(a.scale));
+          if (a.accumulate) sum[j] = add2(old[j], sum[j]);
+        }
+        Raw<float> out;
+        rows::narrow(sum, out);
+        rows::store_raw(row + c, out);
+      }
+      __syncthreads();
+    }
+  }
 }
 
 // Joins the pieces of the rows that begin in one of the block's tiles and go on behind it: the warps take runs of
@@ -556,6 +588,13 @@ __global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
 }
 
 // --------------------------------------------------------------------------- host
+// Threads that share a row of d elements, as a power of two.
+int threads_log2(int d) {
+  int t = 0;
+  while ((kChunk << t) < d && (1 << t) < kThreads) ++t;
+  return t;
+}
+
 struct Layout {
   int passes, bits, blocks, tiles;
   size_t pairs[2], hist, total, partial, bytes;
@@ -568,7 +607,10 @@ Layout layout(const nat_embed_params& p, int64_t cap) {
   l.passes = (b + 8) / 9;
   l.bits = (b + l.passes - 1) / l.passes;
   l.blocks = (int)((cap + kTile - 1) / kTile);
-  l.tiles = cap > kPiece ? (int)((cap + kPiece - 1) / kPiece) : 0;
+  // none where the groups of threads of a block that writes rows can share any row among them, kPiece tokens each at most:
+  // 290 tokens of 64 columns 12.8 us with blocks for pieces, 10.2 without (a kernel of its own: in one with the other it
+  // would cost the large ones 2 to 6 %)
+  l.tiles = cap > kPiece * (kThreads >> threads_log2(p.d)) ? (int)((cap + kPiece - 1) / kPiece) : 0;
   size_t at = 256;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -605,13 +647,6 @@ int check_pointers(const char* who, std::initializer_list<const void*> needed, s
   for (const void* q : words)
     if ((uintptr_t)q & 3u) return fail(NAT_ERR_INVALID_ARG, "%s: ids, sel_idx and n_rows must be 4-byte aligned", who);
   return NAT_OK;
-}
-
-// Threads that share a row of d elements, as a power of two.
-int threads_log2(int d) {
-  int t = 0;
-  while ((kChunk << t) < d && (1 << t) < kThreads) ++t;
-  return t;
 }
 
 template <typename T>
@@ -680,7 +715,7 @@ int bwd(const nat_embed_params& p, const Rows& r, const void* dx, float* dtable,
   SumArgs a{r, pairs[src], dx, dtable, (float*)(ws + l.partial), at(0), p.d, threads_log2(p.d), max(kFewestRows, min(kRowsPerBlock, kBlockBytes / (4 * p.d))),
             l.tiles, p.scale, p.accumulate != 0};
   while (a.rows_per_block > 1 && p.V / a.rows_per_block < 148 * 8) a.rows_per_block >>= 1;
-  s = launch_after(sum_kernel<T>, dim3((unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block)), kThreads, 0,
+  s = launch_after(l.tiles > 0 ? sum_kernel<T, true> : sum_kernel<T, false>, dim3((unsigned)(l.tiles + (p.V + a.rows_per_block - 1) / a.rows_per_block)), kThreads, 0,
                    stream, "embed_sum", a);
   if (s != NAT_OK) return s;
   if (l.tiles > 0) {
