@@ -204,7 +204,7 @@ int nat_experts_fwd(const nat_experts_params* p, const int32_t* offsets, int64_t
   Layout l;
   s = check_call(who, a, workspace_bytes, false, &l);
   if (s != NAT_OK) return s;
-  s = launch_plan(a, l, l.tile_rows[kFwd]);
+  if (p->dtype == NAT_F32 || p->n_experts > kOwnExperts || cap == 0) s = launch_plan(a, l, l.tile_rows[kFwd]);
   return s != NAT_OK || cap == 0 ? s : product(a, l, kFwd);
 }
 

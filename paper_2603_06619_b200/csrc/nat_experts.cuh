@@ -68,6 +68,9 @@ inline float* partial(const Args& a, const Layout& l) {
   return reinterpret_cast<float*>((char*)a.workspace + l.partial_off);
 }
 
+// Experts up to which the blocks of the forward product (bfloat16) find the row tiles themselves, in place of a kernel in front
+// that lists them: LISTUS.
+constexpr int kOwnExperts = 64;
 constexpr int kBf16Cols = 256;  // columns of a tile (float32: as many as rows)
 
 // Rows of the k-blocks [lo, hi) that part `part` of `parts` takes of `blocks`.

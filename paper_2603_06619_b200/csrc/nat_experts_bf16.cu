@@ -61,7 +61,46 @@ struct TcArgs {
   bool accumulate;
   __nv_bfloat16* rows_out;     // kFwd, kDx
   int64_t rows_stride;
+  const int32_t* offsets;      // kFwd with few experts: the blocks find the tiles themselves
+  int64_t cap;
 };
+
+// Where each expert's tiles begin, and its rows.
+struct Own {
+  int first[kOwnExperts + 1], lo[kOwnExperts], hi[kOwnExperts];
+};
+// By one warp; block 0 writes the status word too.
+template <int ROWS>
+__device__ __forceinline__ void find_tiles(const TcArgs& a, Own& own) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  unsigned faults = 0u;
+  for (int base = 0; base < a.E; base += 32) {
+    const int e = base + lane;
+    int lo = 0, hi = 0;
+    unsigned fault = 0u;
+    if (e < a.E) {
+      expert_rows(a.offsets, e, a.cap, lo, hi);
+      fault = offsets_fault(a.offsets, e, a.cap);
+      own.lo[e] = lo;
+      own.hi[e] = hi;
+    }
+    faults |= __reduce_or_sync(0xFFFFFFFFu, fault);
+    const int count = (hi - lo + ROWS - 1) / ROWS;
+    int run = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int left = __shfl_up_sync(0xFFFFFFFFu, run, o);
+      if (lane >= o) run += left;
+    }
+    if (e < a.E) own.first[e] = before + run - count;
+    before += __shfl_sync(0xFFFFFFFFu, run, 31);
+  }
+  if (lane == 0) {
+    own.first[a.E] = (faults & kBroken) ? 0 : before;
+    if (blockIdx.x == 0) a.head->status = faults ? NAT_DEV_CAPACITY : 0u;
+  }
+}
 
 struct Unit {
   int expert, lo, hi;  // rows of the tile, or of the expert (kDw)
@@ -72,7 +111,7 @@ struct Unit {
 // kFwd, kDx: groups of kGroup row tiles go through the columns, the row tile varying fastest, so that the pairs at
 // work share few row tiles and few column tiles through L2.  kDw: the experts in the list's order.
 template <int WHICH, int ROWS>
-__device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
+__device__ __forceinline__ Unit decode(const TcArgs& a, const Own& own, int rows, int u) {
   const int n_tiles = (a.n_cols + BN - 1) / BN;
   Unit w;
   if (WHICH == kDw) {
@@ -91,7 +130,20 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, int rows, int u) {
   const int grp = u / (kGroup * n_tiles), in = u - grp * kGroup * n_tiles;
   const int left = max(1, min(kGroup, rows - grp * kGroup));
   const int n = in / left;
-  const Tile t = a.tiles[grp * kGroup + in - n * left];
+  const int index = grp * kGroup + in - n * left;
+  Tile t;
+  if (WHICH == kFwd && a.offsets) {  // the last expert whose tiles begin at or before it
+    int e = 0, end = a.E;
+    while (end - e > 1) {
+      const int mid = (e + end) >> 1;
+      if (own.first[mid] <= index) e = mid; else end = mid;
+    }
+    t.expert = e;
+    t.lo = own.lo[e] + (index - own.first[e]) * ROWS;
+    t.hi = min(t.lo + ROWS, own.hi[e]);
+  } else {
+    t = a.tiles[index];
+  }
   w.expert = tc::uniform(t.expert);
   w.lo = tc::uniform(t.lo);
   w.hi = tc::uniform(t.hi);
@@ -225,14 +277,19 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   tc::cluster_sync_all();  // the peer's barriers exist before anyone signals them
   tc::fence_after_sync();
   const uint32_t tmem_base = tc::uniform(*tmem_slot);
-  wait_for_primary();  // the list of tiles is there
-  const int row_tiles = (int)a.head->tiles;
+  wait_for_primary();  // the list of tiles, or what it is made from, is there
+  __shared__ Own own;
+  if (WHICH == kFwd && a.offsets) {
+    if (warp == 0) find_tiles<ROWS>(a, own);
+    __syncthreads();
+  }
+  const int row_tiles = WHICH == kFwd && a.offsets ? tc::uniform(own.first[a.E]) : (int)a.head->tiles;
   const int units = (a.n_cols + BN - 1) / BN * (WHICH == kDw ? (a.head->broken ? 0 : a.E * a.m_tiles * a.parts) : row_tiles);
 
   auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x ? 1 : 0) != 0; };
   // The entry of the unit after `u` is asked for before u is worked on: it costs a round trip to L2.
-  auto first_unit = [&]() { return decode<WHICH, ROWS>(a, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
-  auto unit_after = [&](int u) { return decode<WHICH, ROWS>(a, row_tiles, u + stride < units ? u + stride : u); };
+  auto first_unit = [&]() { return decode<WHICH, ROWS>(a, own, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
+  auto unit_after = [&](int u) { return decode<WHICH, ROWS>(a, own, row_tiles, u + stride < units ? u + stride : u); };
   auto segments_of = [&](const Unit& w) { return WHICH == kDw ? max(1, (w.kb_hi - w.kb_lo + kSegment - 1) / kSegment) : 1; };
   // A gradient that is added to takes nothing from an expert without rows.
   auto skipped = [&](const Unit& w) {
@@ -694,6 +751,8 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   t.n_cols = n;
   t.k_blocks = (k + BK - 1) / BK;
   t.rows_out = (__nv_bfloat16*)out;
+  t.offsets = fwd && p.n_experts <= kOwnExperts ? a.offsets : nullptr;
+  t.cap = a.cap;
   t.rows_stride = fwd ? p.y_stride : p.x_stride;
   if ((s = map_rows(&ma, in, k, a.cap, in_stride, BM)) != NAT_OK) return s;
   if ((s = map_rows(&ma32, in, k, a.cap, in_stride, 32)) != NAT_OK) return s;
