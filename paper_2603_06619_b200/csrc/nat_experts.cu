@@ -136,9 +136,9 @@ int product(const Args& a, const Layout& l, Product which) {
   return a.p.dtype == NAT_F32 ? f32_product(a, l, which) : bf16_product(a, l, which);
 }
 
-// Not for float32 with rows, whose blocks find their tiles and write the status word themselves.
+// Not for float32, nor for few experts, with rows: the blocks find their tiles and write the status word themselves.
 int launch_plan(const Args& a, const Layout& l, int tile_rows) {
-  if (a.p.dtype == NAT_F32 && a.cap > 0) return NAT_OK;
+  if ((a.p.dtype == NAT_F32 || a.p.n_experts <= kOwnExperts) && a.cap > 0) return NAT_OK;
   plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(a.offsets, a.p.n_experts, a.cap, tile_rows, head(a), by_rows(a, l),
                                                 tiles(a, l));
   NAT_LAUNCH_CHECK("experts_plan");
@@ -204,7 +204,7 @@ int nat_experts_fwd(const nat_experts_params* p, const int32_t* offsets, int64_t
   Layout l;
   s = check_call(who, a, workspace_bytes, false, &l);
   if (s != NAT_OK) return s;
-  if (p->dtype == NAT_F32 || p->n_experts > kOwnExperts || cap == 0) s = launch_plan(a, l, l.tile_rows[kFwd]);
+  s = launch_plan(a, l, l.tile_rows[kFwd]);
   return s != NAT_OK || cap == 0 ? s : product(a, l, kFwd);
 }
 

@@ -61,16 +61,18 @@ struct TcArgs {
   bool accumulate;
   __nv_bfloat16* rows_out;     // kFwd, kDx
   int64_t rows_stride;
-  const int32_t* offsets;      // kFwd with few experts: the blocks find the tiles themselves
+  const int32_t* offsets;      // with few experts: the blocks find the tiles themselves
   int64_t cap;
+  bool tells;                  // the first product of a call, whose block 0 writes the status word then
 };
 
-// Where each expert's tiles begin, and its rows.
+// Where each expert's row tiles begin, and its rows; the experts by falling number of rows, equal ones by number (kDw).
 struct Own {
-  int first[kOwnExperts + 1], lo[kOwnExperts], hi[kOwnExperts];
+  int first[kOwnExperts + 1], lo[kOwnExperts], hi[kOwnExperts], order[kOwnExperts];
+  bool broken;
 };
-// By one warp; block 0 writes the status word too.
-template <int ROWS>
+// By one warp.
+template <int WHICH, int ROWS>
 __device__ __forceinline__ void find_tiles(const TcArgs& a, Own& own) {
   const int lane = threadIdx.x & 31;
   int before = 0;
@@ -98,7 +100,23 @@ __device__ __forceinline__ void find_tiles(const TcArgs& a, Own& own) {
   }
   if (lane == 0) {
     own.first[a.E] = (faults & kBroken) ? 0 : before;
-    if (blockIdx.x == 0) a.head->status = faults ? NAT_DEV_CAPACITY : 0u;
+    own.broken = (faults & kBroken) != 0;
+    if (a.tells && blockIdx.x == 0) {
+      a.head->status = faults ? NAT_DEV_CAPACITY : 0u;
+      a.head->broken = own.broken;
+    }
+  }
+  if (WHICH == kDw) {
+    __syncwarp();
+    for (int e = lane; e < a.E; e += 32) {
+      const int rows = own.hi[e] - own.lo[e];
+      int before_it = 0;
+      for (int f = 0; f < a.E; ++f) {
+        const int other = own.hi[f] - own.lo[f];
+        before_it += other > rows || (other == rows && f < e);
+      }
+      own.order[before_it] = e;
+    }
   }
 }
 
@@ -117,7 +135,14 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, const Own& own, int rows
   if (WHICH == kDw) {
     const int per = a.m_tiles * n_tiles, rank = u / (per * a.parts), in = u - rank * per * a.parts;
     const int part = in / per, tile = in - part * per;
-    const Tile t = a.tiles[rank];
+    Tile t;
+    if (a.offsets) {
+      t.expert = own.order[rank];
+      t.lo = own.lo[t.expert];
+      t.hi = own.hi[t.expert];
+    } else {
+      t = a.tiles[rank];
+    }
     w.expert = tc::uniform(t.expert);
     w.lo = tc::uniform(t.lo);
     w.hi = tc::uniform(t.hi);
@@ -132,15 +157,13 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, const Own& own, int rows
   const int n = in / left;
   const int index = grp * kGroup + in - n * left;
   Tile t;
-  if (WHICH == kFwd && a.offsets) {  // the last expert whose tiles begin at or before it
-    int e = 0, end = a.E;
-    while (end - e > 1) {
-      const int mid = (e + end) >> 1;
-      if (own.first[mid] <= index) e = mid; else end = mid;
-    }
-    t.expert = e;
-    t.lo = own.lo[e] + (index - own.first[e]) * ROWS;
-    t.hi = min(t.lo + ROWS, own.hi[e]);
+  if (a.offsets) {  // the last expert whose tiles begin at or before it, by the whole warp
+    static_assert(kOwnExperts == 64, "two a lane");
+    const int e = threadIdx.x & 31;
+    t.expert = __popc(__ballot_sync(0xFFFFFFFFu, e < a.E && own.first[e] <= index)) +
+               __popc(__ballot_sync(0xFFFFFFFFu, e + 32 < a.E && own.first[e + 32] <= index)) - 1;
+    t.lo = own.lo[t.expert] + (index - own.first[t.expert]) * ROWS;
+    t.hi = min(t.lo + ROWS, own.hi[t.expert]);
   } else {
     t = a.tiles[index];
   }
@@ -279,12 +302,13 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   const uint32_t tmem_base = tc::uniform(*tmem_slot);
   wait_for_primary();  // the list of tiles, or what it is made from, is there
   __shared__ Own own;
-  if (WHICH == kFwd && a.offsets) {
-    if (warp == 0) find_tiles<ROWS>(a, own);
+  if (a.offsets) {
+    if (warp == 0) find_tiles<WHICH, ROWS>(a, own);
     __syncthreads();
   }
-  const int row_tiles = WHICH == kFwd && a.offsets ? tc::uniform(own.first[a.E]) : (int)a.head->tiles;
-  const int units = (a.n_cols + BN - 1) / BN * (WHICH == kDw ? (a.head->broken ? 0 : a.E * a.m_tiles * a.parts) : row_tiles);
+  const int row_tiles = a.offsets ? tc::uniform(own.first[a.E]) : (int)a.head->tiles;
+  const bool broken = a.offsets ? own.broken : a.head->broken != 0;
+  const int units = (a.n_cols + BN - 1) / BN * (WHICH == kDw ? (broken ? 0 : a.E * a.m_tiles * a.parts) : row_tiles);
 
   auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x ? 1 : 0) != 0; };
   // The entry of the unit after `u` is asked for before u is worked on: it costs a round trip to L2.
@@ -731,6 +755,9 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   t.E = p.n_experts;
   t.parts = which == kDw ? l.parts : 1;
   t.accumulate = p.accumulate != 0;
+  t.offsets = p.n_experts <= kOwnExperts ? a.offsets : nullptr;
+  t.cap = a.cap;
+  t.tells = which != kDw || !a.dx;
   if (which == kDw) {
     if ((s = map_rows(&ma, a.dy, p.n_out, a.cap, p.y_stride, BK)) != NAT_OK) return s;
     if ((s = map_rows(&mb, a.x, p.n_in, a.cap, p.x_stride, BK)) != NAT_OK) return s;
@@ -751,8 +778,6 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   t.n_cols = n;
   t.k_blocks = (k + BK - 1) / BK;
   t.rows_out = (__nv_bfloat16*)out;
-  t.offsets = fwd && p.n_experts <= kOwnExperts ? a.offsets : nullptr;
-  t.cap = a.cap;
   t.rows_stride = fwd ? p.y_stride : p.x_stride;
   if ((s = map_rows(&ma, in, k, a.cap, in_stride, BM)) != NAT_OK) return s;
   if ((s = map_rows(&ma32, in, k, a.cap, in_stride, 32)) != NAT_OK) return s;
