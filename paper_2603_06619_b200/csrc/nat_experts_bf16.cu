@@ -4,9 +4,9 @@
 //   kDx   dx = dy w_e      (rows x n_in,   contraction n_out)   w_e contiguous across it
 //   kDw   dw_e = dy^T x    (n_out x n_in,  contraction rows)    both contiguous across it
 //
-// Persistent CTA pairs: the even CTA issues MMAs of M = 256, N = 256 (cta_group::2), each CTA holds one or two
-// blocks of 128 rows of A and half of B per stage and drains its own rows of the accumulators.  Warp 0 loads by TMA, warp 1
-// issues, four warps for each block of rows write out.  Every wait is bounded and raises NAT_DEV_TIMEOUT.
+// Persistent CTA pairs: the even CTA issues MMAs of M = 256, N = 256 (cta_group::2), each CTA loads its half of A and of B
+// for each stage and drains its own rows of the two accumulators.  Warp 0 loads by TMA, warp 1 issues, four warps (kDw:
+// eight) write out.  Every wait is bounded and raises NAT_DEV_TIMEOUT.
 //
 // Ragged ends.  A tile's rows behind its expert's last belong to another expert or to none: they give rows of the
 // accumulator that nobody writes out.  Columns behind n_in or n_out, and another expert's weights, lie outside the
@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "nat_experts.cuh"
+#include "nat_f32x2.cuh"
 #include "nat_tc.cuh"
 
 namespace nat {
@@ -27,28 +28,27 @@ namespace {
 constexpr int BM = 128, BK = 64, BN = kBf16Cols;
 constexpr int kBox = 64 * 64 * 2;  // bytes of a 64 x 64 box of an operand that is contiguous across the contraction
 constexpr int kTmemCols = 512;
-// Blocks of the contraction that a kDw tile's accumulator takes at most: the tensor cores cut off what they add (toward
-// zero, about half a step of 2^-23 each time), so after that many the sum is added to the result in memory, rounded to
-// nearest, and begun anew.  Relative error of a gradient of 6,058, 8,193 and up to 17,389 rows an expert: 6.6e-6, 4.4e-6,
-// 4.7e-6 with 96; 6.6e-6, 9.0e-6, 8.2e-6 with whole sums, which take 0 to 7 % less time; 1.8e-6 for the last with 32, which
-// takes 11 to 20 % more.
-constexpr int kSegment = 96;
+// Blocks of the contraction (64 rows each) that a kDw tile's accumulator takes at most: the tensor cores cut off what they
+// add (toward zero, about half a step of 2^-23 each time), so after that many the sum goes to registers, where it is added
+// to those before, rounded to nearest, and is begun anew in the other accumulator.  Relative error of a gradient of up to
+// 17,389 rows an expert: 4.6e-7 with 8, 9.0e-7 with 16, 8.2e-6 with whole sums (plain float32 3.8e-7).  300,013 rows take
+// the same time with 8 and 16, 2 % less with 32.
+constexpr int kSegment = 8;
 constexpr int kGroup = 8;  // row tiles that go through the columns together
 
-// ROWS: of a tile.  Shared memory: stages of A and half of B, and 4 KB pieces of finished rows for each warp that writes
-// out, from which they leave by TMA: two for kDw, whose epilogue nothing hides, one elsewhere.
+// ROWS: of a tile.  Shared memory: stages of A and half of B, and a 4 KB piece of finished rows for each warp that writes
+// out, from which it leaves by TMA.
 template <int WHICH, int ROWS>
 struct Ring {
-  static constexpr int kSubs = ROWS <= 2 * BM ? 1 : 2;  // blocks of 128 rows of A a CTA holds
   static constexpr int kABytes = ROWS / 2 * BK * 2, kBBytes = (BN / 2) * BK * 2;
   static constexpr int kPer = ROWS < 2 * BM ? 2 : 1;  // blocks of the contraction in a stage
   static constexpr int kBlock = kABytes + kBBytes, kStage = kPer * kBlock;
-  static constexpr int kPieces = WHICH == kDw ? 2 : 1;
-  static constexpr int kStaging = 4 * kSubs * kPieces * 4096;
+  static constexpr int kWriters = WHICH == kDw ? 8 : 4;  // warps that write out
+  static constexpr int kStaging = kWriters * 4096;
   static constexpr int kBarriers = 512;
   static constexpr int kNum = (226 * 1024 - 1024 - kBarriers - kStaging) / kStage;
   static_assert((3 * kNum + 5) * 8 + 8 <= kBarriers, "barriers, tensor memory's address and the abort flag");
-  static constexpr int kThreads = 64 + 128 * kSubs;
+  static constexpr int kThreads = 64 + 32 * kWriters;
   static constexpr size_t kSmem = (size_t)kNum * kStage + kStaging + 1024 /*alignment*/ + kBarriers;
 };
 
@@ -59,6 +59,7 @@ struct TcArgs {
   int m_tiles;                 // kDw: tiles along n_out
   int parts;
   bool accumulate;
+  bool merged;                 // kDw: both operands' columns are whole blocks of 64, loaded two at a time
   __nv_bfloat16* rows_out;     // kFwd, kDx
   int64_t rows_stride;
   const int32_t* offsets;      // with few experts: the blocks find the tiles themselves
@@ -201,6 +202,13 @@ __device__ __forceinline__ uint64_t step_desc(uint32_t base, int kk) {
   return ACROSS ? tc::smem_desc_sw128(base + kk * 2048, kBox, 1024) : tc::smem_desc_sw128(base + kk * 32, 16, 1024);
 }
 
+__device__ __forceinline__ void load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(tc::smem_u32(dst)),
+      "l"(map), "r"(tc::smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 __device__ __forceinline__ void load_3d_pair(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
@@ -250,8 +258,7 @@ __global__ void __launch_bounds__(Ring<WHICH, ROWS>::kThreads, 1)
 experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
                const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c, const TcArgs a) {
   using R = Ring<WHICH, ROWS>;
-  constexpr int kNS = R::kNum, SUBS = R::kSubs;
-  constexpr uint32_t kAcc = 2 / SUBS;  // accumulators: two tiles in flight, or one
+  constexpr int kNS = R::kNum;
   constexpr bool kAcross = WHICH == kDw;                    // A is contiguous across the contraction
   constexpr bool kBcross = WHICH == kDw || WHICH == kDx;
   constexpr uint32_t kIdesc = tc::instr_desc_bf16(2 * BM, BN, kAcross ? 1 : 0, kBcross ? 1 : 0);
@@ -281,7 +288,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::mbar_init(tail_bar, 1);
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(&tfull_bar[i], 1);
-      tc::mbar_init(&tempty_bar[i], 4 * SUBS * 2);
+      tc::mbar_init(&tempty_bar[i], R::kWriters * 2);
     }
     *abort_flag = 0u;
     tc::fence_barrier_init();
@@ -349,12 +356,23 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           if (tc::elect_one()) {
             if (len < BK) tc::mbar_arrive_expect_tx(tail_bar, R::kStage);
             else if (rank == 0) tc::mbar_arrive_expect_tx(&full_bar[s], 2 * R::kStage);
+            if (a.merged) {
+              const int ax = (w.m0 + rank * BM) / 64, bx = n0 / 64;
+              if (len < BK) {
+                load_3d(a_dst, &map_a, tail_bar, 0, t, ax);
+                load_3d(b_dst, &map_b, tail_bar, 0, t, bx);
+              } else {
+                load_3d_pair(a_dst, &map_a, bar, 0, t, ax);
+                load_3d_pair(b_dst, &map_b, bar, 0, t, bx);
+              }
+            } else {
 #pragma unroll
-            for (int j = 0; j < 2 * SUBS + 2; ++j) {  // boxes of A, then of B
-              const CUtensorMap* map = j < 2 * SUBS ? &map_a : &map_b;
-              const int x = j < 2 * SUBS ? w.m0 + j / 2 * 2 * BM + rank * BM + j % 2 * 64 : n0 + (j - 2 * SUBS) * 64;
-              if (len < BK) tc::tma_load_2d(a_dst + j * kBox, map, tail_bar, x, t);
-              else tc::tma_load_2d_pair(a_dst + j * kBox, map, bar, x, t);
+              for (int j = 0; j < 4; ++j) {  // boxes of A, then of B
+                const CUtensorMap* map = j < 2 ? &map_a : &map_b;
+                const int x = j < 2 ? w.m0 + rank * BM + j * 64 : n0 + (j - 2) * 64;
+                if (len < BK) tc::tma_load_2d(a_dst + j * kBox, map, tail_bar, x, t);
+                else tc::tma_load_2d_pair(a_dst + j * kBox, map, bar, x, t);
+              }
             }
           }
           __syncwarp();
@@ -363,7 +381,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (!ok) break;
             tail_phase ^= 1u;
 #pragma unroll
-            for (int j = 0; j < 2 * SUBS + 2; ++j)
+            for (int j = 0; j < 4; ++j)
               for (int i = len * 8 + lane; i < BK * 8; i += 32)
                 *reinterpret_cast<uint4*>(a_dst + j * kBox + i * 16) = make_uint4(0u, 0u, 0u, 0u);
             tc::fence_proxy_async();
@@ -429,13 +447,13 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const int turned = WHICH == kDw ? 0 : turned_rows(w);
         const uint32_t turned_idesc = tc::instr_desc_bf16(2 * BM, turned, kBcross ? 1 : 0, 0);
         for (int seg = 0; ok && seg < segments; ++seg, ++tcount) {
-          const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
+          const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
           int kb_lo, kb_hi;
           part_range(w.kb_hi - w.kb_lo, seg, segments, kb_lo, kb_hi);
           ok = all(tc::mbar_wait(&tempty_bar[acc], aph ^ 1u, abort_flag));
           if (!ok) break;
           tc::fence_after_sync();
-          const uint32_t d_tmem = tmem_base + acc * SUBS * BN;
+          const uint32_t d_tmem = tmem_base + acc * BN;
           for (int kb = kb_lo; kb < kb_hi; kb += R::kPer, ++it) {
             const int s = it % kNS;
             ok = all(tc::mbar_wait(&full_bar[s], (it / kNS) & 1u, abort_flag));
@@ -454,13 +472,9 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                                        (kb + h > kb_lo || kk > 0) ? 1u : 0u);
                 } else {
 #pragma unroll
-                  for (int kk = 0; kk < BK / 16; ++kk) {
-                    const uint64_t bdesc = step_desc<kBcross>(b_base, kk);
-#pragma unroll
-                    for (int sub = 0; sub < SUBS; ++sub)
-                      tc::umma_bf16_pair(d_tmem + sub * BN, step_desc<kAcross>(a_base + sub * (BM * BK * 2), kk), bdesc,
-                                         kIdesc, (kb + h > kb_lo || kk > 0) ? 1u : 0u);
-                  }
+                  for (int kk = 0; kk < BK / 16; ++kk)
+                    tc::umma_bf16_pair(d_tmem, step_desc<kAcross>(a_base, kk), step_desc<kBcross>(b_base, kk), kIdesc,
+                                       (kb + h > kb_lo || kk > 0) ? 1u : 0u);
                 }
               }
               tc::umma_commit_pair(&empty_bar[s], 3);
@@ -474,12 +488,10 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     __syncwarp();
   } else {
-    // ------------------------------------------------ epilogue (four warps for each block of 128 rows)
-    const int q = warp & 3;           // tensor-memory lanes that this warp may read
-    const int sub = (warp - 2) >> 2;
-    uint8_t* const pieces = staging + (warp - 2) * R::kPieces * 4096;
-    uint32_t turn = 0;
-    const int in_tile = sub * 2 * BM + rank * BM + q * 32;  // first of the warp's rows
+    // ------------------------------------------------ epilogue
+    const int q = warp & 3;                     // tensor-memory lanes that this warp may read
+    uint8_t* const stage = staging + (warp - 2) * 4096;
+    const int in_tile = rank * BM + q * 32;     // first of the warp's rows
     uint32_t tcount = 0;
     bool ok = true;
     Unit next = first_unit();
@@ -487,46 +499,69 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const Unit w = next;
       next = unit_after(u);
       if (skipped(w)) continue;
-      const int segments = segments_of(w);
-      for (int seg = 0; seg < segments; ++seg, ++tcount) {
-        const uint32_t acc = tcount % kAcc, aph = (tcount / kAcc) & 1u;
-        ok = all(tc::mbar_wait(&tfull_bar[acc], aph, abort_flag));
-        if (!ok) break;
-        tc::fence_after_sync();
-        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc * SUBS + (uint32_t)sub) * BN;
-        if (WHICH == kDw) {
-          const bool none = w.kb_lo == w.kb_hi;  // no rows: zeros, not what tensor memory holds
-          const bool add = seg > 0 || (a.accumulate && a.parts == 1);
-          if (seg > 0 && lane == 0) tc::bulk_wait_all();  // the segments are added one after the other
-          __syncwarp();
-#pragma unroll 1
-          for (int c = 0; c < BN / 32; ++c) {
-            const int col = w.n0 + c * 32;
-            if (col >= a.n_cols) break;
+      if (WHICH == kDw) {
+        // two warps for 32 rows, half of the columns each: the segments' sums are added up in registers
+        const int segments = segments_of(w), half = (warp - 2) >> 2;
+        float2 sum[BN / 4];
+#pragma unroll
+        for (int j = 0; j < BN / 4; ++j) sum[j] = both(0.f);
+        for (int seg = 0; seg < segments; ++seg, ++tcount) {
+          const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
+          ok = all(tc::mbar_wait(&tfull_bar[acc], aph, abort_flag));
+          if (!ok) break;
+          tc::fence_after_sync();
+          const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * (BN / 2);
+#pragma unroll
+          for (int c = 0; c < BN / 64; ++c) {
             uint32_t v[32];
             tc::tmem_ld32_issue(taddr + c * 32, v);
             tc::tmem_ld_wait(v);
-            uint8_t* stage = pieces + (turn++ & 1u) * 4096;
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the piece before the last has left
-            __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                  none ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-            tc::fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) {
-              // rows behind n_out are outside the map
-              if (add) put_3d<true>(&map_c, stage, col, w.m0 + in_tile, w.slice);
-              else put_3d<false>(&map_c, stage, col, w.m0 + in_tile, w.slice);
-              tc::bulk_commit();
-            }
+            for (int j = 0; j < 16; ++j)
+              sum[c * 16 + j] = add2(sum[c * 16 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
           }
-        } else if (const int turned = turned_rows(w)) {
+          tc::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_cta(tc::smem_u32(&tempty_bar[acc]), 0));
+        }
+        if (!ok) break;
+        const bool none = w.kb_lo == w.kb_hi;  // no rows: zeros, not what tensor memory held
+        const bool add = a.accumulate && a.parts == 1;
+#pragma unroll
+        for (int c = 0; c < BN / 64; ++c) {
+          const int col = w.n0 + half * (BN / 2) + c * 32;
+          if (col >= a.n_cols) break;
+          if (lane == 0) tc::bulk_wait_read_all();  // the piece before has left
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 x = sum[c * 16 + 2 * j], y = sum[c * 16 + 2 * j + 1];
+            *reinterpret_cast<float4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x, x.y, y.x, y.y);
+          }
+          tc::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            // rows behind n_out are outside the map
+            if (add) put_3d<true>(&map_c, stage, col, w.m0 + in_tile, w.slice);
+            else put_3d<false>(&map_c, stage, col, w.m0 + in_tile, w.slice);
+            tc::bulk_commit();
+          }
+        }
+        continue;
+      }
+      {
+        const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
+        ++tcount;
+        ok = all(tc::mbar_wait(&tfull_bar[acc], aph, abort_flag));
+        if (!ok) break;
+        tc::fence_after_sync();
+        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN;
+        if (const int turned = turned_rows(w)) {
           // a lane a column of the result: 32 rows of 64 bytes through the warp's block of shared memory, then 16 bytes a
           // lane (single elements straight to memory: 8 us for a tile of 184 rows)
           const int rows = w.hi - w.lo, col = w.n0 + rank * BM + q * 32 + lane % 4 * 8;
-          __nv_bfloat16* stage = reinterpret_cast<__nv_bfloat16*>(pieces);
+          __nv_bfloat16* rows32 = reinterpret_cast<__nv_bfloat16*>(stage);
           if (lane == 0) tc::bulk_wait_read_all();
 #pragma unroll 1
           for (int c = 0; c < turned; c += 32) {
@@ -535,14 +570,14 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             tc::tmem_ld_wait(v);
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) stage[j * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[j]));
+            for (int j = 0; j < 32; ++j) rows32[j * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[j]));
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const int row = c + j * 8 + lane / 4;
               if (row < rows && col < a.n_cols)
                 *reinterpret_cast<uint4*>(a.rows_out + (int64_t)(w.lo + row) * a.rows_stride + col) =
-                    *reinterpret_cast<const uint4*>(stage + (j * 8 + lane / 4) * 32 + lane % 4 * 8);
+                    *reinterpret_cast<const uint4*>(rows32 + (j * 8 + lane / 4) * 32 + lane % 4 * 8);
             }
           }
           __syncwarp();
@@ -564,7 +599,6 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
             if (valid == 32) {
               // through the warp's block of shared memory, whole lines at a time
-              uint8_t* stage = pieces;
               if (lane == 0) tc::bulk_wait_read_all();
               __syncwarp();
 #pragma unroll
@@ -637,6 +671,13 @@ int map_rows(CUtensorMap* map, const void* base, int cols, int64_t rows, int64_t
   const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)stride * 2};
   const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uintptr_t)base, size, pitch, box);
+}
+// The same with the columns in blocks of 64: boxes of two blocks by BK rows (one load in place of two: the weights' gradient
+// takes 5 to 7 % less).  cols a multiple of 64.
+int map_blocks(CUtensorMap* map, const void* base, int cols, int64_t rows, int64_t stride) {
+  const cuuint64_t size[3] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64)}, pitch[2] = {(cuuint64_t)stride * 2, 128};
+  const cuuint32_t box[3] = {64, (cuuint32_t)BK, 2};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (uintptr_t)base, size, pitch, box);
 }
 // The experts' weights [E, n_out, n_in]: boxes of 64 columns by box_rows of one expert.
 int map_weights(CUtensorMap* map, const nat_experts_params& p, const void* w, int box_rows) {
@@ -732,17 +773,10 @@ int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb
 //   128 experts, 2048 x 768         -          85, 80, 78     89, 83, 84     96, 88, 105    104, 103, -
 //   8 experts, 4096 x 4096          -          59, 55, 53     60, 56, 62         -          66, 74, -
 constexpr int64_t kFew = 48, kSome = 96;
-// And from which the weights' gradient takes tiles of 512 rows in place of 256: 312 rows (128 experts, 2048 x 768) 316 us
-// with 512, 280 with 256; 500 (32, 2048 x 1024) 114, 115; 1000 (16, 2048 x 2048) 161, 163; 1875 (64, 2048 x 1024) 556, 552;
-// 4688 (64, 2048 x 1536) 1760, 1863; 7500 (8, 4096 x 4096) 1764, 1863.
-constexpr int64_t kDwWide = 768;
-
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
   const int64_t rows = cap / p.n_experts;
   if (which != kDw) return rows <= kFew ? BM / 2 : rows <= kSome ? BM : 2 * BM;
-  // A tile of 512 rows of the result takes a quarter fewer operand bytes, but leaves no second accumulator in whose
-  // shadow it is written out: worth it where the experts have rows enough.
-  return rows >= kDwWide ? 4 * BM : 2 * BM;
+  return 2 * BM;
 }
 
 int bf16_product(const Args& a, const Layout& l, Product which) {
@@ -759,16 +793,20 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   t.cap = a.cap;
   t.tells = which != kDw || !a.dx;
   if (which == kDw) {
-    if ((s = map_rows(&ma, a.dy, p.n_out, a.cap, p.y_stride, BK)) != NAT_OK) return s;
-    if ((s = map_rows(&mb, a.x, p.n_in, a.cap, p.x_stride, BK)) != NAT_OK) return s;
+    t.merged = p.n_out % 64 == 0 && p.n_in % 64 == 0;
+    if ((s = t.merged ? map_blocks(&ma, a.dy, p.n_out, a.cap, p.y_stride)
+                      : map_rows(&ma, a.dy, p.n_out, a.cap, p.y_stride, BK)) != NAT_OK)
+      return s;
+    if ((s = t.merged ? map_blocks(&mb, a.x, p.n_in, a.cap, p.x_stride)
+                      : map_rows(&mb, a.x, p.n_in, a.cap, p.x_stride, BK)) != NAT_OK)
+      return s;
     if ((s = l.parts > 1 ? map_gradient(&mc, p, partial(a, l), (int64_t)l.parts * p.n_experts)
                          : map_gradient(&mc, p, a.dw, p.n_experts)) != NAT_OK)
       return s;
     t.n_cols = p.n_in;
     t.m_tiles = (p.n_out + l.tile_rows[kDw] - 1) / l.tile_rows[kDw];
     const int64_t units = (int64_t)t.E * t.m_tiles * ((p.n_in + BN - 1) / BN) * t.parts;
-    return l.tile_rows[kDw] == 4 * BM ? launch<kDw, 4 * BM>(ma, ma, mb, mc, t, units, a.stream)
-                                      : launch<kDw, 2 * BM>(ma, ma, mb, mc, t, units, a.stream);
+    return launch<kDw, 2 * BM>(ma, ma, mb, mc, t, units, a.stream);
   }
   const bool fwd = which == kFwd;
   const void *in = fwd ? a.x : a.dy;
