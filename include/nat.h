@@ -581,7 +581,10 @@ int nat_qknorm_bwd(const nat_qknorm_params* params /* host */, int32_t B, const 
  * x, dx [cap, n_in] with x_stride elements from a row to the next; y, dy [cap, n_out] with y_stride; w [n_experts, n_out,
  * n_in] row-major in dtype; dw float32 [n_experts, n_out, n_in], overwritten, or with accumulate added to its contents.
  * dtype NAT_BF16: tensor cores with fp32 accumulation, one rounding of y and dx at the end; NAT_F32: plain fp32
- * arithmetic.  Sums are taken in a fixed order: a call repeated on the same inputs reproduces its outputs bit for bit.
+ * arithmetic.  The tensor cores cut off what they add: an accumulator takes up to 4096 terms of y and dx in one go (a sum
+ * of terms of one sign is then off by up to about 2.4e-5 of itself); of longer contractions it takes 1024 and of dw 512,
+ * and its sum is added to one in registers, rounded to nearest.  Sums are taken in a fixed order: a call repeated on the
+ * same inputs reproduces its outputs bit for bit.
  * A row's y and dx depend on that row and the expert's weights alone, infinities and NaN included; an expert's dw on its
  * own rows alone.
  * n_in, n_out multiples of 8, at most 2^20; at most 1024 experts; strides multiples of 8 elements, matrices 16-byte

@@ -18,7 +18,7 @@
 #include <type_traits>
 
 #include "nat_experts.cuh"
-#include "nat_f32x2.cuh"
+#include "nat_rows.cuh"
 #include "nat_tc.cuh"
 
 namespace nat {
@@ -28,23 +28,28 @@ namespace {
 constexpr int BM = 128, BK = 64, BN = kBf16Cols;
 constexpr int kBox = 64 * 64 * 2;  // bytes of a 64 x 64 box of an operand that is contiguous across the contraction
 constexpr int kTmemCols = 512;
-// Blocks of the contraction (64 rows each) that a kDw tile's accumulator takes at most: the tensor cores cut off what they
+// Blocks of the contraction (64 terms each) that an accumulator takes at most (kDw; kFwd and kDx where LONG): the tensor cores cut off what they
 // add (toward zero, about half a step of 2^-23 each time), so after that many the sum goes to registers, where it is added
 // to those before, rounded to nearest, and is begun anew in the other accumulator.  Relative error of a gradient of up to
 // 17,389 rows an expert: 4.6e-7 with 8, 9.0e-7 with 16, 8.2e-6 with whole sums (plain float32 3.8e-7).  300,013 rows take
-// the same time with 8 and 16, 2 % less with 32.
-constexpr int kSegment = 8;
+// the same time with 8 and 16, 2 % less with 32.  kFwd and kDx with 8, whose result is rounded to bfloat16 anyway, would take
+// 6 to 13 % more than with 16 (200 rows over 32 experts 75 us and 67).
+template <int WHICH>
+constexpr int kSegment = WHICH == kDw ? 8 : 16;
 constexpr int kGroup = 8;  // row tiles that go through the columns together
 
-// ROWS: of a tile.  Shared memory: stages of A and half of B, and a 4 KB piece of finished rows for each warp that writes
+// ROWS: of a tile.  LONG (kFwd, kDx): a contraction whose sum goes to registers every kSegment blocks.  Shared memory: stages of A and half of B, and a 4 KB piece of finished rows for each warp that writes
 // out, from which it leaves by TMA.
-template <int WHICH, int ROWS>
+template <int WHICH, int ROWS, bool LONG>
 struct Ring {
   static constexpr int kABytes = ROWS / 2 * BK * 2, kBBytes = (BN / 2) * BK * 2;
   static constexpr int kPer = ROWS < 2 * BM ? 2 : 1;  // blocks of the contraction in a stage
   static constexpr int kBlock = kABytes + kBBytes, kStage = kPer * kBlock;
-  static constexpr int kWriters = WHICH == kDw ? 8 : 4;  // warps that write out
-  static constexpr int kStaging = kWriters * 4096;
+  static constexpr bool kSums = WHICH == kDw || LONG;    // in registers
+  static constexpr int kWriters = kSums ? 8 : 4;         // warps that write out
+  // of finished rows: 32 x 64 of bfloat16 or 32 x 32 of float; 32 x 32 of bfloat16 where all tiles are turned
+  static constexpr int kPiece = LONG && ROWS < 2 * BM ? 2048 : 4096;
+  static constexpr int kStaging = kWriters * kPiece;
   static constexpr int kBarriers = 512;
   static constexpr int kNum = (226 * 1024 - 1024 - kBarriers - kStaging) / kStage;
   static_assert((3 * kNum + 5) * 8 + 8 <= kBarriers, "barriers, tensor memory's address and the abort flag");
@@ -180,8 +185,7 @@ __device__ __forceinline__ Unit decode(const TcArgs& a, const Own& own, int rows
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
-  return *reinterpret_cast<uint32_t*>(&v);
+  return rows::pack_bf16(make_float2(__uint_as_float(lo), __uint_as_float(hi)));
 }
 
 // kFwd, kDx: a tile of up to 128 rows is turned: the weights' columns go along M and its rows along N, whose length an
@@ -253,11 +257,11 @@ __device__ __forceinline__ void put_3d(const CUtensorMap* map, const void* src, 
                  : "memory");
 }
 
-template <int WHICH, int ROWS>
-__global__ void __launch_bounds__(Ring<WHICH, ROWS>::kThreads, 1)
+template <int WHICH, int ROWS, bool LONG>
+__global__ void __launch_bounds__(Ring<WHICH, ROWS, LONG>::kThreads, 1)
 experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
                const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c, const TcArgs a) {
-  using R = Ring<WHICH, ROWS>;
+  using R = Ring<WHICH, ROWS, LONG>;
   constexpr int kNS = R::kNum;
   constexpr bool kAcross = WHICH == kDw;                    // A is contiguous across the contraction
   constexpr bool kBcross = WHICH == kDw || WHICH == kDx;
@@ -321,7 +325,9 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   // The entry of the unit after `u` is asked for before u is worked on: it costs a round trip to L2.
   auto first_unit = [&]() { return decode<WHICH, ROWS>(a, own, row_tiles, units > 0 ? min(unit0, units - 1) : 0); };
   auto unit_after = [&](int u) { return decode<WHICH, ROWS>(a, own, row_tiles, u + stride < units ? u + stride : u); };
-  auto segments_of = [&](const Unit& w) { return WHICH == kDw ? max(1, (w.kb_hi - w.kb_lo + kSegment - 1) / kSegment) : 1; };
+  auto segments_of = [&](const Unit& w) {
+    return R::kSums ? max(1, (w.kb_hi - w.kb_lo + kSegment<WHICH> - 1) / kSegment<WHICH>) : 1;
+  };
   // A gradient that is added to takes nothing from an expert without rows.
   auto skipped = [&](const Unit& w) {
     return WHICH == kDw && a.accumulate && a.parts == 1 && w.kb_lo == w.kb_hi;
@@ -443,13 +449,15 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const Unit w = next;
         next = unit_after(u);
         if (skipped(w)) continue;
-        const int segments = segments_of(w);
+        // of about the same length, whole stages each; none is empty, as none has more than kSegment blocks
+        static_assert(kSegment<WHICH> % R::kPer == 0, "whole stages");
+        const int blocks = w.kb_hi - w.kb_lo, segments = segments_of(w);
+        const int per = R::kSums ? ((blocks + segments - 1) / segments + R::kPer - 1) / R::kPer * R::kPer : blocks;
         const int turned = WHICH == kDw ? 0 : turned_rows(w);
         const uint32_t turned_idesc = tc::instr_desc_bf16(2 * BM, turned, kBcross ? 1 : 0, 0);
         for (int seg = 0; ok && seg < segments; ++seg, ++tcount) {
           const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
-          int kb_lo, kb_hi;
-          part_range(w.kb_hi - w.kb_lo, seg, segments, kb_lo, kb_hi);
+          const int kb_lo = seg * per, kb_hi = min(kb_lo + per, blocks);
           ok = all(tc::mbar_wait(&tempty_bar[acc], aph ^ 1u, abort_flag));
           if (!ok) break;
           tc::fence_after_sync();
@@ -490,7 +498,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   } else {
     // ------------------------------------------------ epilogue
     const int q = warp & 3;                     // tensor-memory lanes that this warp may read
-    uint8_t* const stage = staging + (warp - 2) * 4096;
+    uint8_t* const stage = staging + (warp - 2) * R::kPiece;
     const int in_tile = rank * BM + q * 32;     // first of the warp's rows
     uint32_t tcount = 0;
     bool ok = true;
@@ -499,22 +507,75 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const Unit w = next;
       next = unit_after(u);
       if (skipped(w)) continue;
-      if (WHICH == kDw) {
-        // two warps for 32 rows, half of the columns each: the segments' sums are added up in registers
-        const int segments = segments_of(w), half = (warp - 2) >> 2;
-        float2 sum[BN / 4];
+      const int turned_n = WHICH == kDw ? 0 : turned_rows(w);
+      const bool turned = WHICH != kDw && (ROWS <= BM || turned_n > 0);
+      const int valid = WHICH == kDw ? 32 : min(32, w.hi - w.lo - in_tile);  // of the warp's rows, where not turned
+      // Columns [col, col + 64) of the warp's rows, two to a register.
+      auto put_rows = [&](int col, const uint32_t (&packed)[32]) {
+        if (valid == 32) {
+          // through the warp's block of shared memory, whole lines at a time
+          if (lane == 0) tc::bulk_wait_read_all();
+          __syncwarp();
 #pragma unroll
-        for (int j = 0; j < BN / 4; ++j) sum[j] = both(0.f);
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+          tc::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            tc::tma_store_2d(&map_c, stage, col, w.lo + in_tile);
+            tc::bulk_commit();
+          }
+        } else if (lane < valid) {
+          // the expert's last rows: those behind are another's
+          __nv_bfloat16* dst = a.rows_out + (int64_t)(w.lo + in_tile + lane) * a.rows_stride + col;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (col + 8 * j < a.n_cols)
+              *reinterpret_cast<uint4*>(dst + 8 * j) =
+                  make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+        }
+        __syncwarp();
+      };
+      // Rows [first, first + 32) of a turned tile, element(j) of each lane, which has a column of the result: 32 rows of 64
+      // bytes through the warp's block of shared memory, then 16 bytes a lane (single elements straight to memory: 8 us
+      // for a tile of 184 rows).  Before the first, what left the block by TMA has to have been read.
+      auto put_turned = [&](int first, auto element) {
+        const int rows = w.hi - w.lo, col = w.n0 + in_tile + lane % 4 * 8;
+        __nv_bfloat16* rows32 = reinterpret_cast<__nv_bfloat16*>(stage);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) rows32[j * 32 + lane] = __float2bfloat16_rn(element(j));
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int row = first + j * 8 + lane / 4;
+          if (row < rows && col < a.n_cols)
+            *reinterpret_cast<uint4*>(a.rows_out + (int64_t)(w.lo + row) * a.rows_stride + col) =
+                *reinterpret_cast<const uint4*>(rows32 + (j * 8 + lane / 4) * 32 + lane % 4 * 8);
+        }
+      };
+      if constexpr (R::kSums) {
+        // Two warps for 32 lanes of tensor memory, with 32 columns at a time of their half, or, of a turned tile, every
+        // other 32: the segments' sums are added up in registers.
+        constexpr int kRuns = WHICH != kDw && ROWS <= BM ? ROWS / 64 : BN / 64;
+        const int segments = segments_of(w), half = (warp - 2) >> 2;
+        auto run_at = [&](int c) { return turned ? (2 * c + half) * 32 : half * (BN / 2) + c * 32; };
+        auto run_has = [&](int c) { return turned ? run_at(c) < turned_n : valid > 0; };
+        float2 sum[kRuns * 16];
+#pragma unroll
+        for (int j = 0; j < kRuns * 16; ++j) sum[j] = both(0.f);
         for (int seg = 0; seg < segments; ++seg, ++tcount) {
           const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
           ok = all(tc::mbar_wait(&tfull_bar[acc], aph, abort_flag));
           if (!ok) break;
           tc::fence_after_sync();
-          const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN + half * (BN / 2);
+          const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN;
 #pragma unroll
-          for (int c = 0; c < BN / 64; ++c) {
+          for (int c = 0; c < kRuns; ++c) {
+            if (!run_has(c)) break;
             uint32_t v[32];
-            tc::tmem_ld32_issue(taddr + c * 32, v);
+            tc::tmem_ld32_issue(taddr + run_at(c), v);
             tc::tmem_ld_wait(v);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -525,64 +586,67 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           if (lane == 0) tc::mbar_arrive_cluster(tc::map_to_cta(tc::smem_u32(&tempty_bar[acc]), 0));
         }
         if (!ok) break;
-        const bool none = w.kb_lo == w.kb_hi;  // no rows: zeros, not what tensor memory held
-        const bool add = a.accumulate && a.parts == 1;
+        if (WHICH != kDw && turned) {
+          if (lane == 0) tc::bulk_wait_read_all();
 #pragma unroll
-        for (int c = 0; c < BN / 64; ++c) {
-          const int col = w.n0 + half * (BN / 2) + c * 32;
-          if (col >= a.n_cols) break;
-          if (lane == 0) tc::bulk_wait_read_all();  // the piece before has left
-          __syncwarp();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 x = sum[c * 16 + 2 * j], y = sum[c * 16 + 2 * j + 1];
-            *reinterpret_cast<float4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x, x.y, y.x, y.y);
+          for (int c = 0; c < min(kRuns, BM / 64); ++c) {
+            if (!run_has(c)) break;
+            put_turned(run_at(c), [&](int j) { return j & 1 ? sum[c * 16 + j / 2].y : sum[c * 16 + j / 2].x; });
           }
-          tc::fence_proxy_async();
           __syncwarp();
-          if (lane == 0) {
-            // rows behind n_out are outside the map
-            if (add) put_3d<true>(&map_c, stage, col, w.m0 + in_tile, w.slice);
-            else put_3d<false>(&map_c, stage, col, w.m0 + in_tile, w.slice);
-            tc::bulk_commit();
+        } else if constexpr (WHICH != kDw && ROWS > BM) {
+#pragma unroll
+          for (int c = 0; c < kRuns; c += 2) {
+            const int col = w.n0 + run_at(c);
+            if (valid <= 0 || col >= a.n_cols) break;
+            uint32_t packed[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) packed[j] = rows::pack_bf16(sum[c * 16 + j]);
+            put_rows(col, packed);
+          }
+        } else if constexpr (WHICH == kDw) {
+          const bool none = w.kb_lo == w.kb_hi;  // no rows: zeros, not what tensor memory held
+          const bool add = a.accumulate && a.parts == 1;
+#pragma unroll
+          for (int c = 0; c < kRuns; ++c) {
+            const int col = w.n0 + run_at(c);
+            if (col >= a.n_cols) break;
+            if (lane == 0) tc::bulk_wait_read_all();  // the piece before has left
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float2 x = sum[c * 16 + 2 * j], y = sum[c * 16 + 2 * j + 1];
+              *reinterpret_cast<float4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                  none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x, x.y, y.x, y.y);
+            }
+            tc::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              // rows behind n_out are outside the map
+              if (add) put_3d<true>(&map_c, stage, col, w.m0 + in_tile, w.slice);
+              else put_3d<false>(&map_c, stage, col, w.m0 + in_tile, w.slice);
+              tc::bulk_commit();
+            }
           }
         }
-        continue;
-      }
-      {
+      } else {
         const uint32_t acc = tcount & 1u, aph = (tcount >> 1) & 1u;
         ++tcount;
         ok = all(tc::mbar_wait(&tfull_bar[acc], aph, abort_flag));
         if (!ok) break;
         tc::fence_after_sync();
         const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + acc * BN;
-        if (const int turned = turned_rows(w)) {
-          // a lane a column of the result: 32 rows of 64 bytes through the warp's block of shared memory, then 16 bytes a
-          // lane (single elements straight to memory: 8 us for a tile of 184 rows)
-          const int rows = w.hi - w.lo, col = w.n0 + rank * BM + q * 32 + lane % 4 * 8;
-          __nv_bfloat16* rows32 = reinterpret_cast<__nv_bfloat16*>(stage);
+        if (turned) {
           if (lane == 0) tc::bulk_wait_read_all();
 #pragma unroll 1
-          for (int c = 0; c < turned; c += 32) {
+          for (int c = 0; c < turned_n; c += 32) {
             uint32_t v[32];
             tc::tmem_ld32_issue(taddr + c, v);
             tc::tmem_ld_wait(v);
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) rows32[j * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[j]));
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int row = c + j * 8 + lane / 4;
-              if (row < rows && col < a.n_cols)
-                *reinterpret_cast<uint4*>(a.rows_out + (int64_t)(w.lo + row) * a.rows_stride + col) =
-                    *reinterpret_cast<const uint4*>(rows32 + (j * 8 + lane / 4) * 32 + lane % 4 * 8);
-            }
+            put_turned(c, [&](int j) { return __uint_as_float(v[j]); });
           }
           __syncwarp();
         } else {
-          const int valid = min(32, w.hi - w.lo - in_tile);  // of the warp's rows
 #pragma unroll 1
           for (int c = 0; c < BN / 64 && valid > 0; ++c) {
             const int col = w.n0 + c * 64;
@@ -597,30 +661,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
               packed[j] = pack_bf16(ra[2 * j], ra[2 * j + 1]);
               packed[16 + j] = pack_bf16(rb[2 * j], rb[2 * j + 1]);
             }
-            if (valid == 32) {
-              // through the warp's block of shared memory, whole lines at a time
-              if (lane == 0) tc::bulk_wait_read_all();
-              __syncwarp();
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                    make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
-              tc::fence_proxy_async();
-              __syncwarp();
-              if (lane == 0) {
-                tc::tma_store_2d(&map_c, stage, col, w.lo + in_tile);
-                tc::bulk_commit();
-              }
-            } else if (lane < valid) {
-              // the expert's last rows: those behind are another's
-              __nv_bfloat16* dst = a.rows_out + (int64_t)(w.lo + in_tile + lane) * a.rows_stride + col;
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (col + 8 * j < a.n_cols)
-                  *reinterpret_cast<uint4*>(dst + 8 * j) =
-                      make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
-            }
-            __syncwarp();
+            put_rows(col, packed);
           }
         }
         tc::fence_before_sync();
@@ -709,7 +750,7 @@ int device_index(int* dev) {
 }
 
 // CTA pairs that the current device holds at a time, found once for each device.
-template <int WHICH, int ROWS>
+template <int WHICH, int ROWS, bool LONG>
 int pairs(int* out) {
   static std::atomic<int> cached[64];
   int dev = 0;
@@ -717,12 +758,12 @@ int pairs(int* out) {
   if (s != NAT_OK) return s;
   int n = cached[dev].load(std::memory_order_relaxed);
   if (n == 0) {
-    NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)Ring<WHICH, ROWS>::kSmem));
+    NAT_CUDA(cudaFuncSetAttribute(experts_kernel<WHICH, ROWS, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)Ring<WHICH, ROWS, LONG>::kSmem));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(148);
-    cfg.blockDim = dim3(Ring<WHICH, ROWS>::kThreads);
-    cfg.dynamicSmemBytes = Ring<WHICH, ROWS>::kSmem;
+    cfg.blockDim = dim3(Ring<WHICH, ROWS, LONG>::kThreads);
+    cfg.dynamicSmemBytes = Ring<WHICH, ROWS, LONG>::kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -730,7 +771,7 @@ int pairs(int* out) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    NAT_CUDA(cudaOccupancyMaxActiveClusters(&n, experts_kernel<WHICH, ROWS>, &cfg));
+    NAT_CUDA(cudaOccupancyMaxActiveClusters(&n, experts_kernel<WHICH, ROWS, LONG>, &cfg));
     if (n <= 0) return fail(NAT_ERR_UNSUPPORTED, "the device does not hold the experts' CTA pairs");
     cached[dev].store(n, std::memory_order_relaxed);
   }
@@ -738,16 +779,16 @@ int pairs(int* out) {
   return NAT_OK;
 }
 
-template <int WHICH, int ROWS>
+template <int WHICH, int ROWS, bool LONG>
 int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb, const CUtensorMap& mc, const TcArgs& t,
            int64_t most_units, cudaStream_t stream) {
   int slots = 0;
-  int s = pairs<WHICH, ROWS>(&slots);
+  int s = pairs<WHICH, ROWS, LONG>(&slots);
   if (s != NAT_OK) return s;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * min(most_units, (int64_t)slots)));
-  cfg.blockDim = dim3(Ring<WHICH, ROWS>::kThreads);
-  cfg.dynamicSmemBytes = Ring<WHICH, ROWS>::kSmem;
+  cfg.blockDim = dim3(Ring<WHICH, ROWS, LONG>::kThreads);
+  cfg.dynamicSmemBytes = Ring<WHICH, ROWS, LONG>::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -758,11 +799,18 @@ int launch(const CUtensorMap& ma, const CUtensorMap& ma32, const CUtensorMap& mb
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, ROWS>, ma, ma32, mb, mc, t));
+  NAT_CUDA(cudaLaunchKernelEx(&cfg, experts_kernel<WHICH, ROWS, LONG>, ma, ma32, mb, mc, t));
   return NAT_OK;
 }
 
 }  // namespace
+
+// Terms of a contraction up to which one accumulator takes them all (kFwd, kDx).  Where the terms have one sign, what the
+// tensor cores cut off adds up to 6e-9 of the sum a term: 2.4e-5 at 4096, a hundredth of bfloat16's half step, but 1.5e-3
+// at 262,144, where a quarter of the results was not the nearest.  Sums in registers, us without / with: 20,000 rows over 8
+// experts, 14,336 x 2048, 953 / 961; 1500 over 32, 8192 x 1536, 132 / 134; up to 4096 terms they would cost as much and
+// gain nothing: 120,007 over 64, 2048 x 1024, 432 / 438, rows' gradient 441 / 453.
+constexpr int kWhole = 4096;
 
 // Average rows of an expert (by the capacity, which is what the host knows) up to which a row tile has 64 or 128 rows in
 // place of 256.  All are turned then, a stage holds two blocks of the contraction (a block with few rows is done with
@@ -806,7 +854,7 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
     t.n_cols = p.n_in;
     t.m_tiles = (p.n_out + l.tile_rows[kDw] - 1) / l.tile_rows[kDw];
     const int64_t units = (int64_t)t.E * t.m_tiles * ((p.n_in + BN - 1) / BN) * t.parts;
-    return launch<kDw, 2 * BM>(ma, ma, mb, mc, t, units, a.stream);
+    return launch<kDw, 2 * BM, false>(ma, ma, mb, mc, t, units, a.stream);
   }
   const bool fwd = which == kFwd;
   const void *in = fwd ? a.x : a.dy;
@@ -824,7 +872,11 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   const int64_t units = l.most_tiles * ((n + BN - 1) / BN);
   auto product = [&](auto tile_rows) {
     constexpr int kRows = decltype(tile_rows)::value;
-    return fwd ? launch<kFwd, kRows>(ma, ma32, mb, mc, t, units, a.stream) : launch<kDx, kRows>(ma, ma32, mb, mc, t, units, a.stream);
+    if (k > kWhole)
+      return fwd ? launch<kFwd, kRows, true>(ma, ma32, mb, mc, t, units, a.stream)
+                 : launch<kDx, kRows, true>(ma, ma32, mb, mc, t, units, a.stream);
+    return fwd ? launch<kFwd, kRows, false>(ma, ma32, mb, mc, t, units, a.stream)
+               : launch<kDx, kRows, false>(ma, ma32, mb, mc, t, units, a.stream);
   };
   switch (l.tile_rows[which]) {
     case BM / 2: return product(std::integral_constant<int, BM / 2>());
