@@ -536,8 +536,8 @@ int nat_embed_bwd(const nat_embed_params* params /* host */, const int32_t* ids,
  * inv_freq float64 [rot_dim / 2] (any law; NULL where rot_dim = 0).  The angles are reduced in 64 bits and their sines and
  * cosines, the norms and all sums are in 32.
  * Positions: positions int32 [cap], or NULL: a row's distance from the start of its sequence in cu_seqlens int32 [B+1],
- * ascending.  Rows: min(*n_rows, cap) (n_rows NULL: cap), and without positions those from cu_seqlens[0] to
- * cu_seqlens[B]; others are neither written nor read.
+ * ascending; one of the two is needed.  Rows: min(*n_rows, cap) (n_rows NULL: cap), of which, with cu_seqlens (positions
+ * or not), those from cu_seqlens[0] to cu_seqlens[B]; others are neither written nor read.
  * q, dq [cap, n_heads, head_dim] with q_stride elements from a token to the next, heads contiguous; k, dk
  * [cap, n_kv_heads, head_dim] with k_stride; q_out, dq_out with q_out_stride, k_out, dk_out with k_out_stride.  An
  * output may lie on an input of the same token stride (q_out on q, dq on dq_out or q, and k alike); other overlaps

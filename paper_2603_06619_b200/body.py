@@ -82,17 +82,13 @@ class PackedSublayer:
     def _split_qk(self, qk):
         return qk.split([self.n_heads, self.n_kv_heads], dim=1)
 
-    def _rows(self, cu_seqlens, positions):
-        # with positions of their own the heads' calls do not look at the sequences: their end is told apart
-        return None if positions is None else cu_seqlens[self.B:self.B + 1]
-
     def rotate(self, qkv, cu_seqlens, w_q, w_k, inv_freq, positions=None, qk=None):
         """qk [cap, n_heads + n_kv_heads, head_dim]: queries and keys of qkv, each head normed (w_q and w_k None: not)
         and turned by its token's position (in its sequence, or as given), in the tensor given for it or the
         sublayer's own.  inv_freq: ``nat.rope_freqs``, or any law."""
         qk = self.qk if qk is None else qk
         q, k, _ = self._split(qkv)
-        nat.nat_qknorm_fwd(self.heads, self.B, cu_seqlens, positions, self._rows(cu_seqlens, positions), self.cap, q, k, w_q, w_k, inv_freq,
+        nat.nat_qknorm_fwd(self.heads, self.B, cu_seqlens, positions, None, self.cap, q, k, w_q, w_k, inv_freq,
                            *self._split_qk(qk))
         return qk
 
@@ -151,7 +147,7 @@ class PackedSublayer:
         q, k, _ = self._split(qkv)
         dq, dk, _ = self._split(dqkv)
         norms = (self.dw_q, self.dw_k, self.heads_ws) if w_q is not None else (None, None, None)
-        nat.nat_qknorm_bwd(self.heads, self.B, cu_seqlens, positions, self._rows(cu_seqlens, positions), self.cap, q, k, w_q, w_k, inv_freq,
+        nat.nat_qknorm_bwd(self.heads, self.B, cu_seqlens, positions, None, self.cap, q, k, w_q, w_k, inv_freq,
                            *self._split_qk(self.dqk if dqk is None else dqk), dq, dk, *norms)
         return dqkv
 

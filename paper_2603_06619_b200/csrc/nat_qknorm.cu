@@ -41,11 +41,11 @@ struct Args {
   float* partial;                // backward with norms: [blocks][2][head_dim]
 };
 
-// Rows [first, end) of the call.
+// Rows [first, end) of the call: those of the sequences, where there are any, whether or not the positions are given.
 __device__ __forceinline__ void row_range(const Args& a, int64_t& first, int64_t& end) {
   end = a.n_rows ? min((int64_t)max(__ldg(a.n_rows), 0), a.cap) : a.cap;
   first = 0;
-  if (!a.positions) {
+  if (a.cu) {
     first = max(__ldg(a.cu), 0);
     end = max(first, min(end, (int64_t)max(__ldg(a.cu + a.B), 0)));
   }
@@ -612,7 +612,7 @@ int nat_qknorm_fwd(const nat_qknorm_params* p, int32_t B, const int32_t* cu_seql
   int s = nat::qknorm::check(who, p, cap);
   if (s != NAT_OK || cap == 0) return s;
   nat::qknorm::Args a{};
-  a.p = *p; a.B = B; a.cu = cu_seqlens; a.positions = positions; a.n_rows = n_rows; a.cap = cap; a.q = q; a.k = k;
+  a.p = *p; a.B = B; a.cu = B >= 0 ? cu_seqlens : nullptr; a.positions = positions; a.n_rows = n_rows; a.cap = cap; a.q = q; a.k = k;
   a.w_q = w_q; a.w_k = w_k; a.inv_freq = inv_freq; a.q_to = q_out; a.k_to = k_out;
   s = nat::qknorm::check_call(who, a, {q, k, q_out, k_out});
   if (s != NAT_OK) return s;
@@ -628,7 +628,7 @@ int nat_qknorm_bwd(const nat_qknorm_params* p, int32_t B, const int32_t* cu_seql
   int s = nat::qknorm::check(who, p, cap);
   if (s != NAT_OK) return s;
   nat::qknorm::Args a{};
-  a.p = *p; a.B = B; a.cu = cu_seqlens; a.positions = positions; a.n_rows = n_rows; a.cap = cap; a.q = q; a.k = k;
+  a.p = *p; a.B = B; a.cu = B >= 0 ? cu_seqlens : nullptr; a.positions = positions; a.n_rows = n_rows; a.cap = cap; a.q = q; a.k = k;
   a.w_q = w_q; a.w_k = w_k; a.inv_freq = inv_freq; a.dq_out = dq_out; a.dk_out = dk_out; a.q_to = dq; a.k_to = dk;
   if (cap > 0)
     s = w_q ? nat::qknorm::check_call(who, a, {q, k, dq_out, dk_out, dq, dk})

@@ -568,7 +568,8 @@ def _qknorm_call(params, B, cu_seqlens, positions, n_rows, cap, w_q, w_k, inv_fr
 
 def nat_qknorm_fwd(params, B, cu_seqlens, positions, n_rows, cap, q, k, w_q, w_k, inv_freq, q_out, k_out):
     """q_out and k_out from q and k, each head normed (w_q, w_k; both None: not) and turned by its token's position
-    (positions None: from cu_seqlens)."""
+    (positions None: from cu_seqlens).  Rows that no sequence of cu_seqlens owns are left alone (cu_seqlens None: none are
+    told apart)."""
     h, kv = params.n_heads, params.n_kv_heads
     p, where, laws, (q, k, q_out, k_out), dev = _qknorm_call(
         params, B, cu_seqlens, positions, n_rows, cap, w_q, w_k, inv_freq,
