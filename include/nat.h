@@ -589,9 +589,10 @@ int nat_qknorm_bwd(const nat_qknorm_params* params /* host */, int32_t B, const 
  * own rows alone.
  * n_in, n_out multiples of 8, at most 2^20; at most 1024 experts; strides multiples of 8 elements, matrices 16-byte
  * aligned.  Outputs must not overlap inputs.
- * workspace: nat_experts_workspace_bytes(params, cap), shared by forward and backward; it holds nothing that must survive
- * between them, and calls that may run at the same time need one each.  Where the weights' gradient has few tiles, the
- * rows are cut into parts whose partial sums take up to 40 MB of it.
+ * workspace: nat_experts_workspace_bytes(params, cap), which grows with cap, so that one made for the largest batch serves
+ * every smaller one; shared by forward and backward; it holds nothing that must survive between them, and calls that may
+ * run at the same time need one each.  Where the weights' gradient has few tiles, the rows are cut into parts whose partial
+ * sums take up to 40 MB of it.
  * A call with cap = 0 does nothing but write dw's zeros and the status word.
  * ------------------------------------------------------------------------- */
 typedef struct {

@@ -151,8 +151,6 @@ Layout layout(const nat_experts_params& p, int64_t cap) {
   Layout l;
   const bool f32 = p.dtype == NAT_F32;
   for (int i = 0; i < 3; ++i) l.tile_rows[i] = f32 ? f32_tile(p, (Product)i, cap) : bf16_tile_rows(p, (Product)i, cap);
-  // an expert's last tile may be part full: at most one extra tile for each
-  l.most_tiles = cap / min(l.tile_rows[0], l.tile_rows[1]) + p.n_experts;
   // Few tiles of the weights' gradient: their rows are cut into parts, of 512 rows (float32: 64) of an average expert at
   // least, whose sums take up to 40 MB.  One expert's parts are of one length, and as many as are held at a time; of
   // several experts one may have most of the rows, so there are up to four times as many.  us, as many as held / twice / four
@@ -176,7 +174,9 @@ Layout layout(const nat_experts_params& p, int64_t cap) {
     return o;
   };
   l.by_rows_off = take(sizeof(Tile) * p.n_experts);
-  l.tiles_off = take(sizeof(Tile) * l.most_tiles);
+  // room for as many tiles as the smallest ones would be, so that it grows with cap whatever the tiles' size; none where the
+  // blocks find their tiles themselves
+  l.tiles_off = take(f32 || p.n_experts <= kOwnExperts ? 0 : sizeof(Tile) * (size_t)most_tiles(p, cap, kFewestRows));
   l.partial_off = take(l.parts > 1 ? sizeof(float) * (size_t)l.parts * p.n_experts * p.n_out * p.n_in : 0);
   l.total = at;
   return l;

@@ -52,7 +52,6 @@ __device__ __forceinline__ unsigned offsets_fault(const int32_t* offsets, int e,
 
 struct Layout {
   int tile_rows[3];           // of a tile, for each product: the rows' tiles (kFwd, kDx), or the weights' (kDw)
-  int64_t most_tiles;
   int parts;                  // into which the rows are cut for the weights' gradient
   size_t by_rows_off, tiles_off, partial_off, total;
 };
@@ -79,6 +78,10 @@ __host__ __device__ inline void part_range(int blocks, int part, int parts, int&
   lo = part * per < blocks ? part * per : blocks;
   hi = lo + per < blocks ? lo + per : blocks;
 }
+
+// Row tiles of a call at most: an expert's last one may be part full.
+inline int64_t most_tiles(const nat_experts_params& p, int64_t cap, int tile_rows) { return cap / tile_rows + p.n_experts; }
+constexpr int kFewestRows = 64;  // of a row tile
 
 // Rows of a tile of the kernel that `which` of a call takes.
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap);

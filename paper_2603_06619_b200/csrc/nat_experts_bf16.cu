@@ -821,6 +821,7 @@ constexpr int kWhole = 4096;
 //   128 experts, 2048 x 768         -          85, 80, 78     89, 83, 84     96, 88, 105    104, 103, -
 //   8 experts, 4096 x 4096          -          59, 55, 53     60, 56, 62         -          66, 74, -
 constexpr int64_t kFew = 48, kSome = 96;
+static_assert(BM / 2 == kFewestRows, "the list of tiles has room for the smallest");
 int bf16_tile_rows(const nat_experts_params& p, Product which, int64_t cap) {
   const int64_t rows = cap / p.n_experts;
   if (which != kDw) return rows <= kFew ? BM / 2 : rows <= kSome ? BM : 2 * BM;
@@ -869,7 +870,7 @@ int bf16_product(const Args& a, const Layout& l, Product which) {
   if ((s = map_rows(&ma32, in, k, a.cap, in_stride, 32)) != NAT_OK) return s;
   if ((s = map_weights(&mb, p, a.w, fwd ? BN / 2 : BK)) != NAT_OK) return s;
   if ((s = map_rows(&mc, out, n, a.cap, t.rows_stride, 32)) != NAT_OK) return s;
-  const int64_t units = l.most_tiles * ((n + BN - 1) / BN);
+  const int64_t units = most_tiles(p, a.cap, l.tile_rows[which]) * ((n + BN - 1) / BN);
   auto product = [&](auto tile_rows) {
     constexpr int kRows = decltype(tile_rows)::value;
     if (k > kWhole)

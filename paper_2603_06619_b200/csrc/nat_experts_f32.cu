@@ -299,7 +299,7 @@ int f32_product(const Args& a, const Layout& l, Product which) {
   g.c_stride = fwd ? p.y_stride : p.x_stride;
   g.n_cols = fwd ? p.n_out : p.n_in;
   g.k_size = fwd ? p.n_in : p.n_out;
-  const int64_t m_tiles = a.cap / l.tile_rows[which] + p.n_experts;
+  const int64_t m_tiles = most_tiles(p, a.cap, l.tile_rows[which]);
   return fwd ? launch<kFwd>(g, l, m_tiles, a.stream) : launch<kDx>(g, l, m_tiles, a.stream);
 }
 
