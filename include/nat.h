@@ -587,8 +587,8 @@ int nat_qknorm_bwd(const nat_qknorm_params* params /* host */, int32_t B, const 
  * same inputs reproduces its outputs bit for bit.
  * A row's y and dx depend on that row and the expert's weights alone, infinities and NaN included; an expert's dw on its
  * own rows alone.
- * n_in, n_out multiples of 8, at most 2^20; at most 1024 experts; strides multiples of 8 elements, matrices 16-byte
- * aligned.  Outputs must not overlap inputs.
+ * n_in, n_out multiples of 8, at most 2^20; at most 1024 experts; cap at most 2^31 - 1024; strides multiples of 8 elements,
+ * matrices 16-byte aligned.  Outputs must not overlap inputs.
  * workspace: nat_experts_workspace_bytes(params, cap), which grows with cap, so that one made for the largest batch serves
  * every smaller one; shared by forward and backward; it holds nothing that must survive between them, and calls that may
  * run at the same time need one each.  Where the weights' gradient has few tiles, the rows are cut into parts whose partial

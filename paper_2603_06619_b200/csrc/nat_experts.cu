@@ -10,6 +10,9 @@ namespace {
 
 constexpr int kMaxExperts = 1024;
 constexpr int kPlanThreads = 1024;
+// The kernels' row numbers are of 32 bits, and they look up to a tile and some slices of the contraction past an expert's
+// last row: with more rows than this the next tile's first would lie past 2^31, and the expert be taken to have none.
+constexpr int64_t kMostRows = 0x7FFFFFFFll - 1023;
 
 // The row tiles of all experts in their order, and the experts' order by falling number of rows (equal ones by
 // number): the weights' gradient takes its tiles in that order, so that those in flight together are of about the
@@ -99,8 +102,8 @@ int check(const char* who, const nat_experts_params* p, int64_t cap) {
   if (!p) return fail(NAT_ERR_INVALID_ARG, "%s: params is null", who);
   if (p->dtype != NAT_F32 && p->dtype != NAT_BF16)
     return fail(NAT_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, p->dtype);
-  if (p->n_experts <= 0 || p->n_in <= 0 || p->n_out <= 0 || cap < 0 || cap > 0x7FFFFFFFll)
-    return fail(NAT_ERR_INVALID_ARG, "%s: n_experts, n_in and n_out must be positive, cap in [0, 2^31)", who);
+  if (p->n_experts <= 0 || p->n_in <= 0 || p->n_out <= 0 || cap < 0 || cap > kMostRows)
+    return fail(NAT_ERR_INVALID_ARG, "%s: n_experts, n_in and n_out must be positive, cap in [0, 2^31 - 1024]", who);
   if (p->n_experts > kMaxExperts || p->n_in % 8 != 0 || p->n_out % 8 != 0 || p->n_in > (1 << 20) ||
       p->n_out > (1 << 20) || (int64_t)p->n_in * p->n_out > (1ll << 31))
     return fail(NAT_ERR_UNSUPPORTED,
