@@ -311,14 +311,16 @@ _DTYPES = {torch.float32: NAT_F32, torch.bfloat16: NAT_BF16}
 GROUP8 = 128                 # columns that share a scale in an 8-bit checkpoint
 
 
+# a torch that was built without CUDA has neither: its tensors are refused as being on no device
+_get_device = getattr(torch._C, "_cuda_getDevice", lambda: None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _device():
     try:
-        return torch._C._cuda_getDevice()
+        return _get_device()
     except RuntimeError:
         return None                # no CUDA device: no tensor is on it
-
-
-_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _bad(what, t, dtype, shape, device):
