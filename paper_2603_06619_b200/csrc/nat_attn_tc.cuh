@@ -2,6 +2,7 @@
 // tensor-memory stores, 3-D tile loads, and the operand tiles' geometry.
 #pragma once
 
+#include "nat_elect.cuh"
 #include "nat_f32x2.cuh"
 #include "nat_tc.cuh"
 

@@ -17,6 +17,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "nat_elect.cuh"
 #include "nat_experts.cuh"
 #include "nat_rows.cuh"
 #include "nat_tc.cuh"

@@ -303,25 +303,6 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, 
       : "memory");
 }
 
-// One lane of a converged warp.  Together with a warp index and a tensor-memory address that the
-// compiler knows to be the same in all lanes (uniform()) this keeps the operands of the MMAs in
-// uniform registers: moved there one by one they cost 75 cycles an MMA, more than its 64.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t one;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "elect.sync _|p, 0xffffffff;\n"
-      "selp.u32 %0, 1, 0, p;\n"
-      "}\n"
-      : "=r"(one));
-  return one != 0;
-}
-template <typename T>
-__device__ __forceinline__ T uniform(T x) {
-  return __shfl_sync(0xFFFFFFFFu, x, 0);
-}
-
 // Four consecutive floats added to global memory without a return value (16-byte aligned).
 __device__ __forceinline__ void red_add_f32x4(float* addr, float a, float b, float c, float d) {
   asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(addr), "f"(a), "f"(b),
