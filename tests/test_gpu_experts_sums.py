@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from paper_2603_06619_b200 import nat
+from test_gpu_experts import Experts
 
 pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
@@ -59,3 +60,39 @@ def test_long_contractions_round_once(terms, loads):
                 ref = (x[lo:hi].double() @ m.double()).cpu().numpy()
                 over = _beyond_rounding(out[lo:hi], ref)
                 assert over.max() <= _sum_bound(terms), (backward, e, float(over.max()), _sum_bound(terms), float((over > _sum_bound(terms)).mean()))
+
+
+@pytest.mark.parametrize("sizes", [(4104, 40), (4160, 264), (5128, 24), (8200, 136), (20000, 8)])
+@pytest.mark.parametrize("loads", [[7, 40, 0, 100], [200, 0, 33, 300, 257], [600, 1, 1023], [k * 37 % 90 for k in range(70)],
+                                   [k * 37 % 190 for k in range(70)], [k * 37 % 600 for k in range(70)]],
+                         ids=["turned", "mixed", "whole", "many_few", "many_some", "many"])
+def test_long_contractions_count_every_term_once(loads, sizes):
+    """Whole numbers, whose sums are exact: y and dx are those, rounded once; forward and, the other way round, backward."""
+    for n_in, n_out in (sizes, sizes[::-1]):
+        e = Experts(loads, n_in, n_out, BF16, seed=1, first=2, strides=(8, 16))
+        g = torch.Generator(device="cuda")
+        g.manual_seed(2)
+        for t in (e.x, e.dy):
+            t[e.lo:e.hi] = torch.randint(-3, 4, (e.hi - e.lo, t.shape[1]), generator=g, device="cuda").to(BF16)
+        e.w.copy_(torch.randint(-3, 4, e.w.shape, generator=g, device="cuda"))
+        e.fwd()
+        e.bwd(dw=False)
+        for i in range(e.E):
+            rows = slice(int(e.offs_h[i]), int(e.offs_h[i + 1]))
+            assert torch.equal(e.y[rows], (e.x[rows].double() @ e.w[i].double().t()).to(BF16)), i
+            assert torch.equal(e.dx[rows], (e.dy[rows].double() @ e.w[i].double()).to(BF16)), i
+        for t in (e.y, e.dx):
+            assert (t[:e.lo] == 7).all() and (t[e.hi:] == 7).all()
+
+
+def test_infinities_and_nan_stay_in_their_row_in_long_contractions():
+    loads = [70, 0, 333, 20]
+    a, b = (Experts(loads, 6000, 136, BF16, seed=6) for _ in range(2))
+    b.x[80, 5000], b.x[402, 3] = float("nan"), float("inf")
+    b.w[3] = float("nan")
+    for e in (a, b):
+        e.fwd()
+    keep = torch.ones(a.cap, dtype=torch.bool, device="cuda")
+    keep[80], keep[402], keep[403:423] = False, False, False
+    assert torch.equal(a.y[keep], b.y[keep])
+    assert not torch.isfinite(b.y[80]).any() and not torch.isfinite(b.y[402]).any() and b.y[403:423].isnan().all()
