@@ -205,7 +205,8 @@ int nat_compact_prefix(int32_t B, const int32_t* cu_seqlens, int64_t n_tot,
  *                     dst[sel_idx[k], :] = src[k, :]   (e.g. compact dHidden back
  *                     to the packed stream; unselected tokens get zero gradient)
  * Rows are row_bytes bytes (a positive multiple of 16) of any element type;
- * src and dst are 16-byte aligned and must not overlap.  After nat_compact under
+ * src and dst are 16-byte aligned and must not overlap.  nat_gather_rows may name a row twice; nat_scatter_rows
+ * may not (it overwrites and adds nothing up: which of two rows stays is not determined).  After nat_compact under
  * RPC or truncation, sel_offsets is the cu_seqlens of the packed prefixes.
  * ------------------------------------------------------------------------- */
 int nat_gather_rows(const void* src, int64_t row_bytes, const int32_t* sel_idx,

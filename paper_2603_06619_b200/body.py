@@ -29,7 +29,9 @@ buffers of its own that are allocated when first needed (so make a first call be
 which the backward pass needs what the forward pass left, kept or made anew by another ``rotate``.
 
 ``PackedEmbedding`` gives the first rows from the packed tokens' ids, and its table's gradient; ``PackedExperts`` multiplies
-rows that are grouped by expert (``nat_gather_rows`` and ``nat_scatter_rows`` bring them there and back).
+rows that are grouped by expert.  ``nat_gather_rows`` brings them there, a token's row to each of its experts; back brings
+``nat_scatter_rows`` where a token has one expert.  It writes a row to one place and adds nothing up: with several experts a
+token their rows are weighted and summed by the caller, and so are the gradients of the rows that were gathered.
 """
 import torch
 
