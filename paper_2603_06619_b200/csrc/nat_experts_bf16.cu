@@ -5,8 +5,8 @@
 //   kDw   dw_e = dy^T x    (n_out x n_in,  contraction rows)    both contiguous across it
 //
 // Persistent CTA pairs: the even CTA issues MMAs of M = 256, N = 256 (cta_group::2), each CTA loads its half of A and of B
-// for each stage and drains its own rows of the two accumulators.  Warp 0 loads by TMA, warp 1 issues, four warps (kDw:
-// eight) write out.  Every wait is bounded and raises NAT_DEV_TIMEOUT.
+// for each stage and drains its own rows of the two accumulators.  Warp 0 loads by TMA, warp 1 issues, four warps (eight
+// where sums go to registers: kDw, and long contractions) write out.  Every wait is bounded and raises NAT_DEV_TIMEOUT.
 //
 // Ragged ends.  A tile's rows behind its expert's last belong to another expert or to none: they give rows of the
 // accumulator that nobody writes out.  Columns behind n_in or n_out, and another expert's weights, lie outside the
@@ -29,18 +29,18 @@ namespace {
 constexpr int BM = 128, BK = 64, BN = kBf16Cols;
 constexpr int kBox = 64 * 64 * 2;  // bytes of a 64 x 64 box of an operand that is contiguous across the contraction
 constexpr int kTmemCols = 512;
-// Blocks of the contraction (64 terms each) that an accumulator takes at most (kDw; kFwd and kDx where LONG): the tensor cores cut off what they
-// add (toward zero, about half a step of 2^-23 each time), so after that many the sum goes to registers, where it is added
-// to those before, rounded to nearest, and is begun anew in the other accumulator.  Relative error of a gradient of up to
-// 17,389 rows an expert: 4.6e-7 with 8, 9.0e-7 with 16, 8.2e-6 with whole sums (plain float32 3.8e-7).  300,013 rows take
-// the same time with 8 and 16, 2 % less with 32.  kFwd and kDx with 8, whose result is rounded to bfloat16 anyway, would take
-// 6 to 13 % more than with 16 (200 rows over 32 experts 75 us and 67).
+// Blocks of the contraction (64 terms each) that an accumulator takes at most (kDw; kFwd and kDx where LONG): the tensor
+// cores cut off what they add (toward zero, about half a step of 2^-23 each time), so after that many the sum goes to
+// registers, where it is added to those before, rounded to nearest, and is begun anew in the other accumulator.  Relative
+// error of a gradient of up to 17,389 rows an expert: 4.6e-7 with 8, 9.0e-7 with 16, 8.2e-6 with whole sums (plain float32
+// 3.8e-7).  300,013 rows take the same time with 8 and 16, 2 % less with 32.  kFwd and kDx, whose result is rounded to
+// bfloat16 anyway, take less with 16 (200 rows over 32 experts, 4096 terms, 67 us; with 8 75).
 template <int WHICH>
 constexpr int kSegment = WHICH == kDw ? 8 : 16;
 constexpr int kGroup = 8;  // row tiles that go through the columns together
 
-// ROWS: of a tile.  LONG (kFwd, kDx): a contraction whose sum goes to registers every kSegment blocks.  Shared memory: stages of A and half of B, and a 4 KB piece of finished rows for each warp that writes
-// out, from which it leaves by TMA.
+// ROWS: of a tile.  LONG (kFwd, kDx): a contraction whose sum goes to registers every kSegment blocks.  Shared memory:
+// stages of A and half of B, and a piece of finished rows for each warp that writes out, from which it leaves by TMA.
 template <int WHICH, int ROWS, bool LONG>
 struct Ring {
   static constexpr int kABytes = ROWS / 2 * BK * 2, kBBytes = (BN / 2) * BK * 2;
